@@ -448,6 +448,47 @@ size_t fpq_gemm_grouped_workspace_size(const fpq_gemm_problem_t *problems, int c
 int fpq_gemm_grouped(const fpq_gemm_problem_t *problems, int count, int x_is_fp32, fpq_format_t fx,
                      fpq_format_t fw, int acc_mode, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- attention between the projections, and its gradient ---------------------------------------
+ *
+ * The attention blocks of the network (Section VI-A keeps them in full precision) between the quantized projections around them,
+ * and the backward pass that training adapters of those projections needs.  Per sample b, query head x and its key head
+ * x / (q_heads / kv_heads), with n = kv_lens[b] keys (kv_len when kv_lens is NULL; values outside 0 .. kv_len are clamped):
+ *   s_ij = scale q_i . k_j over the visible keys j < n, and under `causal` j <= i + n - q_len (the last query sees all keys);
+ *   lse_i = log sum_j exp(s_ij),  o_i = sum_j exp(s_ij - lse_i) v_j.
+ * A query that sees no key gets o = 0, lse = -infinity and no gradient.  The backward pass computes the probabilities again from
+ * lse and writes the gradients of q, k and v for grad_o; keys and values past n get zeros, and those of a key head the sum over
+ * the query heads that share it.  Memory past n is not used, whatever it holds; infinities and NaN in places that are used make
+ * the rows that see them infinite or NaN (in FPQ_TYPE_FP32 always NaN), and under `causal` also rows of the same tile that do not.
+ *
+ * type: of q, k, v, o and the gradients.  Sums, maxima and log-sums are fp32.  Products of FPQ_TYPE_BF16 are exact, the
+ * probabilities and their gradients are rounded to bf16 where they are multiplied; FPQ_TYPE_FP32 splits operands into three bf16
+ * parts as fpq_rl_step does (an error of fp32's order; magnitudes below 2^-110 keep fewer bits).  The bits of a result do not
+ * depend on anything but the arguments: no atomics.
+ * Tensors are [batch, tokens, heads, head_dim] with strides (sample, token, head; in elements) of their own, so that q, k and v can
+ * be columns of one projection's result; the elements of a head are neighbours.  Rows of a multiple of 16 bytes that start at one
+ * are what the kernels are tuned for; others work.  lse: fp32 [batch, q_heads, q_len], may be NULL in the forward call.
+ * workspace: the stated bytes, 16-byte aligned, no initialisation (NULL when that is 0).  Calls that share one are ordered on
+ * one stream.
+ * Limits: head_dim <= 160 (FPQ_ERR_UNSUPPORTED beyond); scale positive and finite (FPQ_ERR_SCALE); q_heads a multiple of
+ * kv_heads; each size, and q_len times the heads of a group, at most 2^30 (FPQ_ERR_SHAPE). */
+typedef enum fpq_type { FPQ_TYPE_FP32 = 0, FPQ_TYPE_BF16 = 1 } fpq_type;
+typedef struct fpq_attention_args {
+    int32_t type;   /* fpq_type */
+    int32_t causal; /* 0 or 1 */
+    int64_t batch, q_heads, kv_heads, q_len, kv_len, head_dim;
+    float scale;
+    const int32_t *kv_lens; /* device, [batch], or NULL */
+    int64_t q_strides[3], k_strides[3], v_strides[3], o_strides[3];
+    int64_t grad_o_strides[3], grad_q_strides[3], grad_k_strides[3], grad_v_strides[3]; /* backward only */
+} fpq_attention_args_t;
+size_t fpq_attention_workspace_size(const fpq_attention_args_t *args);
+int fpq_attention(const fpq_attention_args_t *args, const void *q, const void *k, const void *v, void *o, float *lse,
+                  void *workspace, size_t workspace_bytes, void *stream);
+size_t fpq_attention_backward_workspace_size(const fpq_attention_args_t *args);
+int fpq_attention_backward(const fpq_attention_args_t *args, const void *q, const void *k, const void *v, const void *o,
+                           const float *lse, const void *grad_o, void *grad_q, void *grad_k, void *grad_v, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
 /* ---- machine-ceiling probes (for the benchmark's roofline object) -------------------------------
  *
  * What this GPU sustains with nothing but the instruction in question in the loop, to set beside the published peaks

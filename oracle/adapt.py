@@ -1,0 +1,108 @@
+"""numpy oracle, in 64 bits, of the operators for adapting a quantized model: attention and its gradient.
+
+Next to a result, `bounds` functions give how far a computation in 32-bit sums may be from it: every rounding it makes, times what
+that rounding scales."""
+import numpy as np
+
+U32 = 2.0 ** -24              # half a unit in the last place of an fp32 number near 1
+U16 = 2.0 ** -8               # and of a bf16 number, which has 8 significant bits
+
+
+def keys_of(lens, b, kv_len):
+    return kv_len if lens is None else int(min(max(int(lens[b]), 0), kv_len))
+
+
+def visible(q_len, n, causal):
+    """[q_len, n]: which keys a query sees."""
+    i, j = np.arange(q_len)[:, None], np.arange(n)[None, :]
+    return (j <= i + n - q_len) if causal else np.ones((q_len, n), bool)
+
+
+def _head(q, k, v, b, x, group, n):
+    f = np.float64
+    return q[b, :, x].astype(f), k[b, :n, x // group].astype(f), v[b, :n, x // group].astype(f)
+
+
+def _probabilities(Q, K, scale, causal):
+    """p and lse of one head; rows that see nothing: zeros and -infinity."""
+    see = visible(len(Q), len(K), causal)
+    s = np.where(see, scale * (Q @ K.T), -np.inf)
+    top = s.max(1, initial=-np.inf, keepdims=True)
+    some = np.isfinite(top)
+    e = np.where(see, np.exp(s - np.where(some, top, 0.0)), 0.0)
+    total = e.sum(1, keepdims=True)
+    with np.errstate(divide="ignore"):
+        lse = np.where(some, top + np.log(total), -np.inf)[:, 0]
+    return np.where(some, e / np.where(total > 0, total, 1.0), 0.0), lse
+
+
+def attention(q, k, v, scale, causal=False, lens=None):
+    """o, lse of [B, L, H, D] arrays."""
+    B, Lq, Hq, D = q.shape
+    o, lse = np.zeros(q.shape), np.full((B, Hq, Lq), -np.inf)
+    for b in range(B):
+        n = keys_of(lens, b, k.shape[1])
+        for x in range(Hq):
+            Q, K, V = _head(q, k, v, b, x, Hq // k.shape[2], n)
+            p, lse[b, x] = _probabilities(Q, K, scale, causal)
+            o[b, :, x] = p @ V
+    return o, lse
+
+
+def attention_backward(q, k, v, go, scale, causal=False, lens=None):
+    gq, gk, gv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
+    G = q.shape[2] // k.shape[2]
+    for b in range(q.shape[0]):
+        n = keys_of(lens, b, k.shape[1])
+        for x in range(q.shape[2]):
+            Q, K, V = _head(q, k, v, b, x, G, n)
+            dO = go[b, :, x].astype(np.float64)
+            p, _ = _probabilities(Q, K, scale, causal)
+            dp = dO @ V.T
+            ds = p * (dp - (p * dp).sum(1, keepdims=True))
+            gq[b, :, x] = scale * (ds @ K)
+            gk[b, :n, x // G] += scale * (ds.T @ Q)
+            gv[b, :n, x // G] += p.T @ dO
+    return gq, gk, gv
+
+
+def attention_bounds(q, k, v, scale, causal, lens, bf16, go=None):
+    """Bounds of |error| for o and lse (and, with go, for gq, gk, gv).
+
+    A score's error is that of its fp32 sum, D + 16 roundings (16: the parts of a split operand and the scale) of at most
+    scale sum |q k|; a probability's relative error is e^2d - 1 for scores within d, with a few roundings of its own.  Sums over
+    n terms make n roundings.  With bf16 operands, p and ds are rounded once more where they are multiplied, and so are results."""
+    B, Lq, Hq, D = q.shape
+    G = Hq // k.shape[2]
+    r = U16 if bf16 else 4 * U32                       # of p or ds as an operand, and of a result
+    to, tl = np.zeros(q.shape), np.zeros((B, Hq, Lq))
+    tq, tk, tv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
+    for b in range(B):
+        n = keys_of(lens, b, k.shape[1])
+        for x in range(Hq):
+            Q, K, V = _head(q, k, v, b, x, G, n)
+            p, lse = _probabilities(Q, K, scale, causal)
+            see = visible(Lq, n, causal)
+            mass = np.where(see, scale * (np.abs(Q) @ np.abs(K).T), 0.0).max(1, initial=0.0, keepdims=True)
+            d = (D + 16) * U32 * mass + 8 * U32
+            dp_rel = np.expm1(2 * d) + (n + 16) * U32  # of a normalised probability
+            tl[b, x] = (d[:, 0] + (n + 16) * U32) + 2 * U32 * np.abs(np.where(np.isfinite(lse), lse, 0.0))
+            pv = p @ np.abs(V)
+            to[b, :, x] = pv * (dp_rel + r + (n + 8) * U32) * (1 + r) + r * np.abs(p @ V)
+            if go is None:
+                continue
+            dO = go[b, :, x].astype(np.float64)
+            A = np.abs(dO) @ np.abs(V).T
+            dp = dO @ V.T
+            delta = (p * dp).sum(1, keepdims=True)
+            d_delta = (np.abs(dO) * to[b, :, x]).sum(1, keepdims=True) + (D + 8) * U32 * (np.abs(dO) * pv).sum(1, keepdims=True)
+            ds = p * (dp - delta)
+            d_ds = p * ((D + 16) * U32 * A + d_delta) * (1 + dp_rel) + np.abs(ds) * (dp_rel + r + 4 * U32)
+            m_ds = np.abs(ds) + d_ds
+            tq[b, :, x] = scale * (d_ds @ np.abs(K) + (n + 8) * U32 * (m_ds @ np.abs(K)))
+            tk[b, :n, x // G] += scale * (d_ds.T @ np.abs(Q) + (G * Lq + 8) * U32 * (m_ds.T @ np.abs(Q)))
+            tv[b, :n, x // G] += (p * (dp_rel + r + (G * Lq + 8) * U32)).T @ np.abs(dO) * (1 + r)
+    if go is None:
+        return to, tl
+    gq, gk, gv = attention_backward(q, k, v, go, scale, causal, lens)
+    return to, tl, tq + r * np.abs(gq), tk + r * np.abs(gk), tv + r * np.abs(gv)

@@ -43,6 +43,17 @@ class fpq_gemm_problem_t(C.Structure):
                 ("bias", C.c_void_p), ("y", C.c_void_p), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64)]
 
 
+FPQ_TYPE_FP32, FPQ_TYPE_BF16 = 0, 1
+
+
+class fpq_attention_args_t(C.Structure):
+    _fields_ = [("type", C.c_int32), ("causal", C.c_int32), ("batch", C.c_int64), ("q_heads", C.c_int64), ("kv_heads", C.c_int64),
+                ("q_len", C.c_int64), ("kv_len", C.c_int64), ("head_dim", C.c_int64), ("scale", C.c_float), ("kv_lens", C.c_void_p),
+                ("q_strides", C.c_int64 * 3), ("k_strides", C.c_int64 * 3), ("v_strides", C.c_int64 * 3), ("o_strides", C.c_int64 * 3),
+                ("grad_o_strides", C.c_int64 * 3), ("grad_q_strides", C.c_int64 * 3), ("grad_k_strides", C.c_int64 * 3),
+                ("grad_v_strides", C.c_int64 * 3)]
+
+
 class FpqError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -158,6 +169,13 @@ def lib():
     L.fpq_int_gemm.argtypes = [u8p, fl, C.c_int32, vp, vp, i32, f32p, vp, f32p, f32p, i64, i64, i64, vp, sz, vp]
     L.fpq_probe_peak.restype = i32
     L.fpq_probe_peak.argtypes = [i32, i32, vp, vp, sz, C.POINTER(C.c_double), vp]
+    for name in ("fpq_attention_workspace_size", "fpq_attention_backward_workspace_size"):
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = [C.POINTER(fpq_attention_args_t)]
+    L.fpq_attention.restype = i32
+    L.fpq_attention.argtypes = [C.POINTER(fpq_attention_args_t)] + [vp] * 6 + [sz, vp]
+    L.fpq_attention_backward.restype = i32
+    L.fpq_attention_backward.argtypes = [C.POINTER(fpq_attention_args_t)] + [vp] * 10 + [sz, vp]
     L.fpq_gemm_noalloc.restype = i32
     L.fpq_gemm_noalloc.argtypes = [vp, i32, F, fl, f32p, vp, F, f32p, f32p, f32p, i64, i64, i64, i32, vp]
     _lib = L
@@ -173,7 +191,8 @@ EXPORTS = ["fpq_strerror", "fpq_format_max", "fpq_format_check", "fpq_bias_to_sc
            "fpq_gemm_plan", "fpq_conv2d_plan", "fpq_gemm_launch_plan", "fpq_conv2d_launch_plan", "fpq_gemm_noalloc", "fpq_gemm_grouped_workspace_size", "fpq_gemm_grouped", "fpq_probe_peak",
            "fpq_packed_sparse_size", "fpq_pack_weights_sparse", "fpq_gemm_sparse", "fpq_conv2d_sparse",
            "fpq_int_calibrate_workspace_size", "fpq_int_calibrate", "fpq_int_quantize", "fpq_int_packed_size",
-           "fpq_int_pack_weights", "fpq_int_gemm_workspace_size", "fpq_int_gemm"]
+           "fpq_int_pack_weights", "fpq_int_gemm_workspace_size", "fpq_int_gemm",
+           "fpq_attention_workspace_size", "fpq_attention", "fpq_attention_backward_workspace_size", "fpq_attention_backward"]
 
 
 def fmt(f):
@@ -367,6 +386,19 @@ def fpq_probe_peak(kind, iterations, src, dst):
     return work.value
 
 
+def _attention_sizes(batch, q_heads, kv_heads, q_len, kv_len, head_dim, type):
+    return C.byref(fpq_attention_args_t(type=type, batch=batch, q_heads=q_heads, kv_heads=kv_heads, q_len=q_len, kv_len=kv_len,
+                                        head_dim=head_dim, scale=1.0))
+
+
+def fpq_attention_workspace_size(batch, q_heads, kv_heads, q_len, kv_len, head_dim, type):
+    return lib().fpq_attention_workspace_size(_attention_sizes(batch, q_heads, kv_heads, q_len, kv_len, head_dim, type))
+
+
+def fpq_attention_backward_workspace_size(batch, q_heads, kv_heads, q_len, kv_len, head_dim, type):
+    return lib().fpq_attention_backward_workspace_size(_attention_sizes(batch, q_heads, kv_heads, q_len, kv_len, head_dim, type))
+
+
 def fpq_rl_workspace_size(M, N, K):
     return lib().fpq_rl_workspace_size(M, N, K)
 
@@ -413,10 +445,15 @@ def fpq_rl_im2col(x, kh, kw, stride, pad, a):
 #       encodings: [(e, m), ...]; mse_out: float32 tensor [n_enc * n_bias] or None; result: uint8 tensor of 40 bytes
 #       (read it back with search_result())
 
+#   fpq_attention(q, k, v, o, lse, scale, causal=0, kv_lens=None, workspace=None)
+#       q, o: [batch, q_len, q_heads, dim], k, v: [batch, kv_len, kv_heads, dim], float32 or bfloat16, of any strides but the last;
+#       lse: float32 [batch, q_heads, q_len] or None; kv_lens: int32 [batch] or None
+#   fpq_attention_backward(q, k, v, o, lse, grad_o, grad_q, grad_k, grad_v, scale, causal=0, kv_lens=None, workspace=None)
+
 NATIVE = ["fpq_gemm", "fpq_gemm_noalloc", "fpq_conv2d", "fpq_gemm_codes_out", "fpq_conv2d_codes_out",
           "fpq_gemm_sparse", "fpq_conv2d_sparse", "fpq_gemm_grouped", "fpq_absmax", "fpq_quantize",
           "fpq_quantize_nhwc", "fpq_int_calibrate", "fpq_int_quantize", "fpq_int_gemm", "fpq_rl_step",
-          "fpq_search_format"]
+          "fpq_search_format", "fpq_attention", "fpq_attention_backward"]
 
 
 def _resolve(name):

@@ -1,0 +1,179 @@
+// C ABI of the operators for adapting a quantized model (see include/fpq.h): argument validation on the host, then kernel
+// launches on the caller's stream.
+#include <math.h>
+
+#include "attention.h"
+
+using namespace fpq;
+
+namespace {
+
+constexpr int64_t kMost = (int64_t)1 << 30;
+
+size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
+size_t size_of(int type) { return type == FPQ_TYPE_FP32 ? 4 : 2; }
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int check_attention(const fpq_attention_args_t* p)
+{
+    if (!p) return FPQ_ERR_NULL;
+    if (p->type != FPQ_TYPE_FP32 && p->type != FPQ_TYPE_BF16) return FPQ_ERR_UNSUPPORTED;
+    if (p->causal != 0 && p->causal != 1) return FPQ_ERR_UNSUPPORTED;
+    for (int64_t v : {p->batch, p->q_heads, p->kv_heads, p->q_len, p->kv_len, p->head_dim})
+        if (v < 0 || v > kMost) return FPQ_ERR_SHAPE;
+    if (p->q_heads == 0 || p->kv_heads == 0 || p->head_dim == 0 || p->q_heads % p->kv_heads) return FPQ_ERR_SHAPE;
+    if (p->head_dim > 160) return FPQ_ERR_UNSUPPORTED;
+    if (p->q_heads / p->kv_heads * p->q_len > kMost) return FPQ_ERR_SHAPE;
+    if (!(p->scale > 0.0f) || isinf(p->scale)) return FPQ_ERR_SCALE;
+    // the grids, and the sizes of the partial results
+    const double rows = (double)p->batch * p->q_heads * (p->q_len + 128), keys = (double)p->batch * p->kv_heads * (p->kv_len + 128);
+    if (rows > 0x1p31 || keys > 0x1p36) return FPQ_ERR_SHAPE;
+    return FPQ_OK;
+}
+
+AttentionPlan plan_of(const fpq_attention_args_t* p)
+{
+    return plan_attention(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->q_len, p->kv_len, p->type);
+}
+
+size_t rows_of(const fpq_attention_args_t* p) { return (size_t)p->batch * p->q_heads * p->q_len; }
+size_t keys_of(const fpq_attention_args_t* p) { return (size_t)p->batch * p->kv_heads * p->kv_len; }
+bool empty(const fpq_attention_args_t* p) { return rows_of(p) == 0; }
+
+Strides strides(const int64_t* s) { return Strides{s[0], s[1], s[2]}; }
+
+// Every row of [batch, len, heads, dim] starts at a multiple of `to` bytes.
+bool rows_aligned(const void* p, const int64_t* s, int64_t batch, int64_t len, int64_t heads, size_t size, size_t to)
+{
+    auto ok = [&](int64_t stride, int64_t n) { return n <= 1 || (stride * (int64_t)size) % (int64_t)to == 0; };
+    return aligned(p, to) && ok(s[0], batch) && ok(s[1], len) && ok(s[2], heads);
+}
+
+// A workgroup per block and part: fits a grid's dimension.
+bool grid_ok(const fpq_attention_args_t* p, int64_t blocks, int64_t parts)
+{
+    return (double)p->batch * (double)p->kv_heads * (double)blocks * (double)parts < 0x1p31;
+}
+
+AttentionArgs args_of(const fpq_attention_args_t* p)
+{
+    AttentionArgs a{};
+    a.lens = p->kv_lens;
+    a.qs = strides(p->q_strides);
+    a.ks = strides(p->k_strides);
+    a.vs = strides(p->v_strides);
+    a.os = strides(p->o_strides);
+    a.batch = (int)p->batch;
+    a.kv_heads = (int)p->kv_heads;
+    a.group = (int)(p->q_heads / p->kv_heads);
+    a.q_len = (int)p->q_len;
+    a.kv_len = (int)p->kv_len;
+    a.dim = (int)p->head_dim;
+    a.causal = p->causal;
+    a.scale = p->scale;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fpq_attention_workspace_size(const fpq_attention_args_t* p)
+{
+    if (check_attention(p) != FPQ_OK || empty(p)) return 0;
+    const AttentionPlan plan = plan_of(p);
+    const size_t rows = rows_of(p);
+    return plan.splits > 1 ? align_up(plan.splits * rows * p->head_dim * 4) + align_up(plan.splits * rows * 4) : 0;
+}
+
+int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* workspace,
+                  size_t workspace_bytes, void* stream)
+{
+    const int st = check_attention(p);
+    if (st != FPQ_OK) return st;
+    if (empty(p)) return FPQ_OK;
+    if (!q || !o || (p->kv_len && (!k || !v))) return FPQ_ERR_NULL;
+    const size_t size = size_of(p->type);
+    if (!aligned(q, size) || !aligned(k, size) || !aligned(v, size) || !aligned(o, size) || !aligned(lse, 4) || !aligned(p->kv_lens, 4))
+        return FPQ_ERR_ALIGN;
+    const AttentionPlan plan = plan_of(p);
+    if (!grid_ok(p, plan.blocks, plan.splits)) return FPQ_ERR_SHAPE;
+    const size_t need = fpq_attention_workspace_size(p);
+    if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 16)) return FPQ_ERR_ALIGN;
+    AttentionArgs a = args_of(p);
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = o;
+    a.lse = lse;
+    a.blocks = plan.blocks;
+    a.splits = plan.splits;
+    a.per_split = plan.per_split;
+    a.vec_out = p->head_dim % 4 == 0 && rows_aligned(o, p->o_strides, p->batch, p->q_len, p->q_heads, size, 4 * size);
+    if (plan.splits > 1) {
+        a.part = static_cast<float*>(workspace);
+        a.part_lse = a.part + align_up(plan.splits * rows_of(p) * p->head_dim * 4) / 4;
+    }
+    const bool vec = p->head_dim * size % 16 == 0 && rows_aligned(q, p->q_strides, p->batch, p->q_len, p->q_heads, size, 16) &&
+                     rows_aligned(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, size, 16) &&
+                     rows_aligned(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, size, 16);
+    return launch_attention(a, p->type, vec, plan, static_cast<hipStream_t>(stream));
+}
+
+size_t fpq_attention_backward_workspace_size(const fpq_attention_args_t* p)
+{
+    if (check_attention(p) != FPQ_OK) return 0;
+    const AttentionPlan plan = plan_of(p);
+    const size_t dim = p->head_dim;
+    return align_up(rows_of(p) * 4) + (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
+           (plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * dim * 4) : 0);
+}
+
+int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const void* k, const void* v, const void* o, const float* lse,
+                           const void* grad_o, void* grad_q, void* grad_k, void* grad_v, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int st = check_attention(p);
+    if (st != FPQ_OK) return st;
+    if (p->batch == 0 || (p->q_len == 0 && p->kv_len == 0)) return FPQ_OK;
+    if (p->q_len && (!q || !o || !lse || !grad_o || !grad_q)) return FPQ_ERR_NULL;
+    if (p->kv_len && (!k || !v || !grad_k || !grad_v)) return FPQ_ERR_NULL;
+    const size_t size = size_of(p->type);
+    for (const void* x : {q, k, v, o, grad_o, static_cast<const void*>(grad_q), static_cast<const void*>(grad_k), static_cast<const void*>(grad_v)})
+        if (!aligned(x, size)) return FPQ_ERR_ALIGN;
+    if (!aligned(lse, 4) || !aligned(p->kv_lens, 4)) return FPQ_ERR_ALIGN;
+    const AttentionPlan plan = plan_of(p);
+    if (!grid_ok(p, plan.q_blocks, plan.q_splits) || !grid_ok(p, plan.k_blocks, plan.k_splits)) return FPQ_ERR_SHAPE;
+    const size_t need = fpq_attention_backward_workspace_size(p);
+    if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 16)) return FPQ_ERR_ALIGN;
+    AttentionArgs a = args_of(p);
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.o = o;
+    a.go = grad_o;
+    a.gq = grad_q;
+    a.gk = grad_k;
+    a.gv = grad_v;
+    a.lse = const_cast<float*>(lse);
+    a.gos = strides(p->grad_o_strides);
+    a.gqs = strides(p->grad_q_strides);
+    a.gks = strides(p->grad_k_strides);
+    a.gvs = strides(p->grad_v_strides);
+    a.vec_out = p->head_dim % 4 == 0 && rows_aligned(grad_q, p->grad_q_strides, p->batch, p->q_len, p->q_heads, size, 4 * size);
+    char* at = static_cast<char*>(workspace);
+    a.delta = reinterpret_cast<float*>(at);
+    at += align_up(rows_of(p) * 4);
+    float* const part_q = reinterpret_cast<float*>(at);
+    if (plan.q_splits > 1) at += align_up(plan.q_splits * rows_of(p) * p->head_dim * 4);
+    float* const part_kv = reinterpret_cast<float*>(at);
+    const bool vec = p->head_dim * size % 16 == 0 && rows_aligned(q, p->q_strides, p->batch, p->q_len, p->q_heads, size, 16) &&
+                     rows_aligned(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, size, 16) &&
+                     rows_aligned(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, size, 16) &&
+                     rows_aligned(o, p->o_strides, p->batch, p->q_len, p->q_heads, size, 16) &&
+                     rows_aligned(grad_o, p->grad_o_strides, p->batch, p->q_len, p->q_heads, size, 16);
+    return launch_attention_backward(a, p->type, vec, plan, part_q, part_kv, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"

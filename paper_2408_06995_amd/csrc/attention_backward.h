@@ -1,0 +1,367 @@
+// Attention, backward.  The probabilities are computed again from the rows' log-sums, p = exp(scale q.k - lse), so nothing of size
+// q_len x kv_len is kept:
+//   delta_i = do_i . o_i,  ds_ij = p_ij (do_i . v_j - delta_i),  dq_i = scale sum_j ds_ij k_j,
+//   dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i   (i over the queries of all heads of the group).
+// Two kernels, each of which owns what it writes: no atomics, the same bits in every run.  The price is that scores and dp are
+// computed twice, seven products instead of five.
+//   queries: a wavefront keeps 32 rows of q and do, reads tiles of keys and values, and sums dq^T = K^T ds^T; writes delta.
+//   keys:    a wavefront keeps 32 keys and values, reads tiles of queries and do, and sums dk and dv over all heads of the group.
+// As in the forward pass p and ds go into the next product from the registers they were computed in.
+#pragma once
+#include "attention.h"
+
+namespace fpq {
+
+template <typename T, int KS>
+struct QueriesShape {
+    static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2, NW = 4;
+    static constexpr int KT = NP == 3 ? 32 : 64;
+    static constexpr int LDS = 2 * NP * KT * RS * 2;
+};
+
+template <typename T, int KS, bool VEC>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_queries_kernel(AttentionArgs a)
+{
+    typedef QueriesShape<T, KS> Sh;
+    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, KT = Sh::KT, NT = 256;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    __bf16* const kt = reinterpret_cast<__bf16*>(lds);
+    __bf16* const vt = kt + NP * KT * RS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
+    const Place at = place_of(a);
+    const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
+    const int rows = a.group * a.q_len, n = keys_of(a, b);
+    const int block = a.causal ? a.blocks - 1 - at.block : at.block;
+    const int r_first = block * 128, r = r_first + 32 * wave + l32;
+    const RowRange range = visible(a, n, r_first, min(r_first + 128, rows) - 1);
+    const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
+
+    const int rc = min(r, rows - 1), g = rc / a.q_len, i = rc - g * a.q_len, head = hk * a.group + g;
+    const int end = a.causal ? max(0, min(n, i + n - a.q_len + 1)) : n;
+    const size_t row_id = (size_t)at.bh * rows + rc;
+    Frag<NP> qf[KS], gf[KS];
+    float delta = 0.0f;
+    {
+        const T* q = static_cast<const T*>(a.q) + b * a.qs.b + i * a.qs.t + head * a.qs.h;
+        const T* o = static_cast<const T*>(a.o) + b * a.os.b + i * a.os.t + head * a.os.h;
+        const T* go = static_cast<const T*>(a.go) + b * a.gos.b + i * a.gos.t + head * a.gos.h;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            float v[8], w[8];
+            row8<T, VEC>(q, 16 * s + 8 * h, a.dim, v);
+            qf[s] = frag_of<NP>(v);
+            row8<T, VEC>(go, 16 * s + 8 * h, a.dim, v);
+            gf[s] = frag_of<NP>(v);
+            row8<T, VEC>(o, 16 * s + 8 * h, a.dim, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf(v[e], w[e], delta);
+        }
+        delta += __shfl_xor(delta, 32);
+    }
+    if (r < rows && h == 0 && at.split == 0) a.delta[row_id] = delta;
+    const float log_sum = a.lse[row_id];
+    const float c = a.scale * kLog2e, lse2 = log_sum == -kInf ? kInf : log_sum * kLog2e;   // a row without keys: every p is 0
+
+    const T* const kbase = static_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
+    const T* const vbase = static_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
+    v16f acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = zero16();
+    Stage<T, KS, VEC, KT, NT> sk, sv;
+    if (kbeg < kend) {
+        sk.load(kbase, a.ks.t, kbeg, kend - 1, a.dim, tid);
+        sv.load(vbase, a.vs.t, kbeg, kend - 1, a.dim, tid);
+    }
+    for (int j0 = kbeg; j0 < kend; j0 += KT) {
+        __syncthreads();
+        sk.store(kt, j0, kend, a.dim, tid);
+        sv.store(vt, j0, kend, a.dim, tid);
+        __syncthreads();
+        if (j0 + KT < kend) {
+            sk.load(kbase, a.ks.t, j0 + KT, kend - 1, a.dim, tid);
+            sv.load(vbase, a.vs.t, j0 + KT, kend - 1, a.dim, tid);
+        }
+        const bool masked = j0 + KT > min(range.lo, kend);
+#pragma unroll
+        for (int u = 0; u < KT / 32; ++u) {
+            v16f s = zero16(), dp = zero16();
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+                mma<NP>(s, row_frag<NP, RS, KT>(kt, 32 * u + l32, 16 * t + 8 * h), qf[t]);
+                mma<NP>(dp, row_frag<NP, RS, KT>(vt, 32 * u + l32, 16 * t + 8 * h), gf[t]);
+            }
+            if (masked) {
+                const int left = end - j0 - 32 * u;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e / 4) + 4 * h + e % 4 >= left) s[e] = -kInf;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -lse2)) * (dp[e] - delta);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = s[8 * t + e];
+                const Frag<NP> ds = frag_of<NP>(v);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) mma<NP>(acc[d], col_frag<NP, RS, KT>(kt, 32 * u + 16 * t, 32 * d, lane), ds);
+            }
+        }
+    }
+    if (r >= rows) return;
+    float* const part = a.splits > 1 ? a.part + (size_t)at.split * a.batch * a.kv_heads * rows * a.dim : nullptr;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int col = 32 * d + 8 * t + 4 * h;
+            const float v[4] = {acc[d][4 * t] * a.scale, acc[d][4 * t + 1] * a.scale, acc[d][4 * t + 2] * a.scale, acc[d][4 * t + 3] * a.scale};
+            if (part)
+                store4(part + row_id * a.dim, col, a.dim, a.dim % 4 == 0, v);
+            else
+                store4(static_cast<T*>(a.gq) + b * a.gqs.b + i * a.gqs.t + head * a.gqs.h, col, a.dim, a.vec_out, v);
+        }
+}
+
+// WHAT: 1 dv, 2 dk, 3 both in one pass.  In fp32 at the largest dimension the planes of 32 keys and values and both sums do not fit
+// a wavefront's registers together: two passes.
+template <typename T, int KS>
+struct KeysShape {
+    static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2;
+    static constexpr int QT = KeysTile<T>;
+    static constexpr int LDS = 2 * NP * QT * RS * 2 + 2 * QT * 4;
+};
+
+template <typename T, int KS, bool VEC, int WHAT>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 6 ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
+{
+    typedef KeysShape<T, KS> Sh;
+    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, QT = Sh::QT, NT = 256;
+    constexpr bool DV = WHAT & 1, DK = WHAT & 2;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    __bf16* const qt = reinterpret_cast<__bf16*>(lds);
+    __bf16* const gt = qt + NP * QT * RS;
+    float* const ls = reinterpret_cast<float*>(gt + NP * QT * RS);             // [QT] log-sums in base 2, [QT] deltas
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
+    const Place at = place_of(a);
+    const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
+    const int n = keys_of(a, b), off = n - a.q_len, j_first = at.block * 128, key = j_first + 32 * wave + l32;
+    // tiles of queries, head by head, from the first that sees a key of this block
+    const int tiles_all = (a.q_len + QT - 1) / QT, skip = a.causal ? min(max(0, j_first - off) / QT, tiles_all) : 0;
+    const int per_head = j_first < n ? tiles_all - skip : 0;
+    const int64_t tiles = (int64_t)per_head * a.group;
+    const int64_t tbeg = min((int64_t)at.split * a.per_split, tiles), tend = min(tbeg + a.per_split, tiles);
+
+    Frag<NP> kf[KS], vf[DK ? KS : 1];
+    {
+        const int kc = max(0, min(key, n - 1));
+        const T* k = static_cast<const T*>(a.k) + b * a.ks.b + kc * a.ks.t + hk * a.ks.h;
+        const T* v = static_cast<const T*>(a.v) + b * a.vs.b + kc * a.vs.t + hk * a.vs.h;
+        if (tbeg < tend) {                         // (no tile: no key either, perhaps)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                float x[8];
+                row8<T, VEC>(k, 16 * s + 8 * h, a.dim, x);
+                kf[s] = frag_of<NP>(x);
+                if constexpr (DK) {
+                    row8<T, VEC>(v, 16 * s + 8 * h, a.dim, x);
+                    vf[s] = frag_of<NP>(x);
+                }
+            }
+        }
+    }
+    v16f av[DV ? DT : 1], ak[DK ? DT : 1];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+        if constexpr (DV) av[d] = zero16();
+        if constexpr (DK) ak[d] = zero16();
+    }
+    const float c = a.scale * kLog2e;
+    Stage<T, KS, VEC, QT, NT> sq, sg;
+    float stat = 0.0f;                             // log-sum (first QT threads) or delta (the next QT) of a row of the tile
+    auto load = [&](int64_t t) {
+        const int g = (int)(t / per_head), i0 = (skip + (int)(t - (int64_t)g * per_head)) * QT, head = hk * a.group + g;
+        sq.load(static_cast<const T*>(a.q) + b * a.qs.b + head * a.qs.h, a.qs.t, i0, a.q_len - 1, a.dim, tid);
+        sg.load(static_cast<const T*>(a.go) + b * a.gos.b + head * a.gos.h, a.gos.t, i0, a.q_len - 1, a.dim, tid);
+        if (tid < 2 * QT) {
+            const int i = i0 + (tid & (QT - 1));
+            const size_t id = ((size_t)at.bh * a.group + g) * a.q_len + min(i, a.q_len - 1);
+            const float x = tid < QT ? a.lse[id] : a.delta[id];
+            stat = tid < QT ? (i >= a.q_len || x == -kInf ? kInf : x * kLog2e) : x;         // rows that are none: p = 0
+            if (tid >= QT && i >= a.q_len) stat = 0.0f;
+        }
+    };
+    if (tbeg < tend) load(tbeg);
+    for (int64_t t = tbeg; t < tend; ++t) {
+        const int g = (int)(t / per_head), i0 = (skip + (int)(t - (int64_t)g * per_head)) * QT;
+        __syncthreads();
+        sq.store(qt, i0, a.q_len, a.dim, tid);
+        sg.store(gt, i0, a.q_len, a.dim, tid);
+        if (tid < 2 * QT) ls[tid] = stat;
+        __syncthreads();
+        if (t + 1 < tend) load(t + 1);
+        const bool masked = a.causal && j_first + 127 > i0 + off;
+#pragma unroll
+        for (int u = 0; u < QT / 32; ++u) {
+            v16f s = zero16(), dp = zero16();
+#pragma unroll
+            for (int x = 0; x < KS; ++x) {
+                mma<NP>(s, row_frag<NP, RS, QT>(qt, 32 * u + l32, 16 * x + 8 * h), kf[x]);
+                if constexpr (DK) mma<NP>(dp, row_frag<NP, RS, QT>(gt, 32 * u + l32, 16 * x + 8 * h), vf[x]);
+            }
+            if (masked) {
+                const int from = key - off - i0 - 32 * u;      // the first query that sees the key
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e / 4) + 4 * h + e % 4 < from) s[e] = -kInf;
+            }
+            float4 lse[4], delta[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                lse[e] = *reinterpret_cast<const float4*>(ls + 32 * u + 8 * e + 4 * h);
+                if constexpr (DK) delta[e] = *reinterpret_cast<const float4*>(ls + QT + 32 * u + 8 * e + 4 * h);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float* y = reinterpret_cast<const float*>(&lse[e / 4]);
+                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -y[e % 4]));
+                if constexpr (DK) {
+                    const float* z = reinterpret_cast<const float*>(&delta[e / 4]);
+                    dp[e] = s[e] * (dp[e] - z[e % 4]);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float v[8];
+                if constexpr (DV) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = s[8 * x + e];
+                    const Frag<NP> p = frag_of<NP>(v);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) mma<NP>(av[d], p, col_frag<NP, RS, QT>(gt, 32 * u + 16 * x, 32 * d, lane));
+                }
+                if constexpr (DK) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = dp[8 * x + e];
+                    const Frag<NP> ds = frag_of<NP>(v);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) mma<NP>(ak[d], ds, col_frag<NP, RS, QT>(qt, 32 * u + 16 * x, 32 * d, lane));
+                }
+            }
+        }
+    }
+    // lane: column l32 of the 16 keys that its values stand for; keys that the sample does not have get zeros
+    const size_t keys_all = (size_t)a.batch * a.kv_heads * a.kv_len;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int j = j_first + 32 * wave + 8 * (e / 4) + 4 * h + e % 4;
+        if (j >= a.kv_len) continue;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const int col = 32 * d + l32;
+            if (col >= a.dim) continue;
+            if constexpr (DV) {
+                const float v = j < n ? av[d][e] : 0.0f;
+                if (a.splits > 1)
+                    a.part[((size_t)at.split * 2 * keys_all + keys_all + (size_t)at.bh * a.kv_len + j) * a.dim + col] = v;
+                else
+                    static_cast<T*>(a.gv)[b * a.gvs.b + j * a.gvs.t + hk * a.gvs.h + col] = (T)v;
+            }
+            if constexpr (DK) {
+                const float v = j < n ? ak[d][e] * a.scale : 0.0f;
+                if (a.splits > 1)
+                    a.part[((size_t)at.split * 2 * keys_all + (size_t)at.bh * a.kv_len + j) * a.dim + col] = v;
+                else
+                    static_cast<T*>(a.gk)[b * a.gks.b + j * a.gks.t + hk * a.gks.h + col] = (T)v;
+            }
+        }
+    }
+}
+
+// out[b, t, head] = the sum of the parts, in order.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_sum_kernel(const float* part, int parts, size_t part_stride, size_t n, int len, int heads, int dim,
+                                                            T* out, Strides st)
+{
+    for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (size_t)gridDim.x * 256) {
+        float v = part[e];
+        for (int s = 1; s < parts; ++s) v += part[s * part_stride + e];
+        const size_t row = e / dim, bh = row / len;
+        const int64_t b = bh / heads, head = bh - (size_t)b * heads;
+        out[b * st.b + (int64_t)(row - bh * len) * st.t + head * st.h + (int64_t)(e - row * dim)] = (T)v;
+    }
+}
+
+template <typename T>
+int launch_sum(const float* part, int parts, size_t part_stride, size_t rows, int len, int heads, int dim, void* out, const Strides& st, hipStream_t s)
+{
+    const size_t n = rows * dim, want = (n + 255) / 256;
+    attention_sum_kernel<T><<<dim3((unsigned)(want < 4096 ? want : 4096)), dim3(256), 0, s>>>(part, parts, part_stride, n, len, heads, dim,
+                                                                                             static_cast<T*>(out), st);
+    return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
+}
+
+template <typename T, int KS, bool VEC>
+int launch_queries(const AttentionArgs& a, hipStream_t s)
+{
+    typedef QueriesShape<T, KS> Sh;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_queries_kernel<T, KS, VEC>), Sh::LDS, done)) return FPQ_ERR_LAUNCH;
+    const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
+    attention_queries_kernel<T, KS, VEC><<<dim3((unsigned)grid), dim3(256), Sh::LDS, s>>>(a);
+    return FPQ_OK;
+}
+
+template <typename T, int KS, bool VEC, int WHAT>
+int launch_keys(const AttentionArgs& a, hipStream_t s)
+{
+    typedef KeysShape<T, KS> Sh;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_kernel<T, KS, VEC, WHAT>), Sh::LDS, done)) return FPQ_ERR_LAUNCH;
+    const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
+    attention_keys_kernel<T, KS, VEC, WHAT><<<dim3((unsigned)grid), dim3(256), Sh::LDS, s>>>(a);
+    return FPQ_OK;
+}
+
+template <typename T, int KS, bool VEC>
+int launch_both(const AttentionArgs& aq, const AttentionArgs& ak, hipStream_t s)
+{
+    // (the keys kernel reads the deltas that the queries kernel writes)
+    int st = aq.q_len > 0 ? launch_queries<T, KS, VEC>(aq, s) : FPQ_OK;
+    if (st != FPQ_OK || ak.kv_len == 0) return st;
+    if constexpr (sizeof(T) == 4 && KS > 8) {
+        st = launch_keys<T, KS, VEC, 1>(ak, s);
+        return st != FPQ_OK ? st : launch_keys<T, KS, VEC, 2>(ak, s);
+    } else {
+        return launch_keys<T, KS, VEC, 3>(ak, s);
+    }
+}
+
+template <typename T>
+int launch_backward(const AttentionArgs& aq, const AttentionArgs& ak, bool vec, hipStream_t s)
+{
+    const int ks = (aq.dim + 15) / 16;
+    int st;
+    if (vec)
+        st = ks <= 3 ? launch_both<T, 3, true>(aq, ak, s) : ks == 4 ? launch_both<T, 4, true>(aq, ak, s) : ks == 5 ? launch_both<T, 5, true>(aq, ak, s)
+           : ks == 6 ? launch_both<T, 6, true>(aq, ak, s) : ks <= 8 ? launch_both<T, 8, true>(aq, ak, s) : launch_both<T, 10, true>(aq, ak, s);
+    else
+        st = ks <= 4 ? launch_both<T, 4, false>(aq, ak, s) : ks <= 8 ? launch_both<T, 8, false>(aq, ak, s) : launch_both<T, 10, false>(aq, ak, s);
+    if (st != FPQ_OK) return st;
+    if (aq.splits > 1) {
+        const size_t rows = (size_t)aq.batch * aq.kv_heads * aq.group * aq.q_len;
+        st = launch_sum<T>(aq.part, aq.splits, rows * aq.dim, rows, aq.q_len, aq.kv_heads * aq.group, aq.dim, aq.gq, aq.gqs, s);
+        if (st != FPQ_OK) return st;
+    }
+    if (ak.splits > 1) {
+        const size_t rows = (size_t)ak.batch * ak.kv_heads * ak.kv_len;
+        st = launch_sum<T>(ak.part, ak.splits, 2 * rows * ak.dim, rows, ak.kv_len, ak.kv_heads, ak.dim, ak.gk, ak.gks, s);
+        if (st != FPQ_OK) return st;
+        st = launch_sum<T>(ak.part + rows * ak.dim, ak.splits, 2 * rows * ak.dim, rows, ak.kv_len, ak.kv_heads, ak.dim, ak.gv, ak.gvs, s);
+        if (st != FPQ_OK) return st;
+    }
+    return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
+}
+
+}  // namespace fpq

@@ -1,0 +1,22 @@
+// Backward attention in bf16, and the call of both types.
+#include "attention_backward.h"
+
+namespace fpq {
+
+int launch_attention_backward_f32(const AttentionArgs& aq, const AttentionArgs& ak, bool vec, hipStream_t s);
+
+int launch_attention_backward(const AttentionArgs& a, int type, bool vec, const AttentionPlan& p, float* part_q, float* part_kv, hipStream_t s)
+{
+    AttentionArgs aq = a, ak = a;
+    aq.blocks = p.q_blocks;
+    aq.splits = p.q_splits;
+    aq.per_split = p.q_per_split;
+    aq.part = part_q;
+    ak.blocks = p.k_blocks;
+    ak.splits = p.k_splits;
+    ak.per_split = p.k_per_split;
+    ak.part = part_kv;
+    return type == FPQ_TYPE_FP32 ? launch_attention_backward_f32(aq, ak, vec, s) : launch_backward<__bf16>(aq, ak, vec, s);
+}
+
+}  // namespace fpq

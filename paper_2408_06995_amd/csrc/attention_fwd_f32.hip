@@ -1,0 +1,8 @@
+// Forward attention in fp32.
+#include "attention_forward.h"
+
+namespace fpq {
+
+int launch_attention_f32(const AttentionArgs& a, bool vec, bool by_keys, hipStream_t s) { return launch_forward<float>(a, vec, by_keys, s); }
+
+}  // namespace fpq

@@ -19,7 +19,8 @@ namespace {
 PyObject* g_resolve = nullptr;      // resolver(name) -> address of the C function
 PyObject* g_check = nullptr;        // checker(status, name): raises
 PyObject *g_format = nullptr, *g_problem = nullptr, *g_array = nullptr;   // fpq_format_t, fpq_gemm_problem_t, ctypes.Array
-PyObject *s_type, *s_data_ptr, *s_numel, *s_element_size, *s_shape;
+PyObject *s_type, *s_data_ptr, *s_numel, *s_element_size, *s_shape, *s_stride, *s_dtype, *s_is_contiguous;
+PyObject *g_float32 = nullptr, *g_bfloat16 = nullptr;
 PyObject *g_get_device = nullptr, *g_get_stream = nullptr;
 
 constexpr int kBad = 1;             // a Python error is set (statuses of the library are <= 0)
@@ -111,6 +112,81 @@ struct Args {
         Py_DECREF(d);
         if (v == -1 && PyErr_Occurred()) bad = true;
         return v;
+    }
+    // shape and strides of a tensor that must have `ndim` dimensions, the elements of the last one neighbours
+    void layout(int k, int ndim, int64_t* size, int64_t* stride, const char* name)
+    {
+        if (bad) return;
+        PyObject* sh = PyObject_GetAttr(a[k], s_shape);
+        PyObject* st = sh ? PyObject_CallMethodNoArgs(a[k], s_stride) : nullptr;
+        if (!st) { Py_XDECREF(sh); bad = true; return; }
+        if (PySequence_Size(sh) != ndim || PySequence_Size(st) != ndim) {
+            PyErr_Format(PyExc_ValueError, "%s: a tensor of %d dimensions expected", name, ndim);
+            bad = true;
+        }
+        for (int d = 0; d < ndim && !bad; ++d) {
+            PyObject* n = PySequence_GetItem(sh, d);
+            PyObject* m = n ? PySequence_GetItem(st, d) : nullptr;
+            if (m) {
+                size[d] = PyLong_AsLongLong(n);
+                stride[d] = PyLong_AsLongLong(m);
+            }
+            bad = !m || PyErr_Occurred();
+            Py_XDECREF(n);
+            Py_XDECREF(m);
+        }
+        Py_DECREF(sh);
+        Py_DECREF(st);
+        if (!bad && size[ndim - 1] > 1 && stride[ndim - 1] != 1) {
+            PyErr_Format(PyExc_ValueError, "%s: the elements of the last dimension are not neighbours", name);
+            bad = true;
+        }
+    }
+    // fpq_type of a tensor
+    int type(int k, const char* name)
+    {
+        if (bad) return 0;
+        if (!g_float32) {
+            PyObject* m = PyImport_ImportModule("torch");
+            if (!m) { bad = true; return 0; }
+            g_float32 = PyObject_GetAttrString(m, "float32");
+            g_bfloat16 = PyObject_GetAttrString(m, "bfloat16");
+            Py_DECREF(m);
+            if (!g_float32 || !g_bfloat16) { Py_CLEAR(g_float32); bad = true; return 0; }
+        }
+        PyObject* t = PyObject_GetAttr(a[k], s_dtype);
+        if (!t) { bad = true; return 0; }
+        const int r = t == g_float32 ? FPQ_TYPE_FP32 : t == g_bfloat16 ? FPQ_TYPE_BF16 : -1;
+        if (r < 0) {
+            PyErr_Format(PyExc_TypeError, "%s: float32 or bfloat16 expected, not %S", name, t);
+            bad = true;
+        }
+        Py_DECREF(t);
+        return r;
+    }
+    void same(bool ok, const char* what)
+    {
+        if (bad || ok) return;
+        PyErr_SetString(PyExc_ValueError, what);
+        bad = true;
+    }
+    // elements of a contiguous tensor of 4-byte values, given as None or with exactly n
+    template <typename P>
+    P* words(int k, int64_t n, const char* name)
+    {
+        if (bad || a[k] == Py_None) return nullptr;
+        if (method(a[k], s_numel) != (size_t)n || method(a[k], s_element_size) != 4) {
+            if (!bad) PyErr_Format(PyExc_ValueError, "%s: %lld elements of four bytes expected", name, (long long)n);
+            bad = true;
+            return nullptr;
+        }
+        PyObject* c = PyObject_CallMethodNoArgs(a[k], s_is_contiguous);
+        if (!c || c != Py_True) {
+            if (c) PyErr_Format(PyExc_ValueError, "%s: not contiguous", name);
+            bad = true;
+        }
+        Py_XDECREF(c);
+        return static_cast<P*>(p(k));
     }
     // the ctypes structure, or anything with four elements (e, m, b, c)
     fpq_format_t fmt(int k)
@@ -327,6 +403,64 @@ int do_search_format(Args& A)
                   static_cast<fpq_search_result*>(A.p(4)), A.p(5), A.bytes(5), A.stream());
 }
 
+// [batch, tokens, heads, dim] tensors: sizes, strides and type, which all must agree
+fpq_attention_args_t attention_args(Args& A, int scale, int causal, int lens)
+{
+    fpq_attention_args_t r;
+    memset(&r, 0, sizeof r);
+    int64_t q[4], k[4], v[4], o[4], s[4];
+    A.layout(0, 4, q, s, "q");
+    memcpy(r.q_strides, s, sizeof r.q_strides);
+    A.layout(1, 4, k, s, "k");
+    memcpy(r.k_strides, s, sizeof r.k_strides);
+    A.layout(2, 4, v, s, "v");
+    memcpy(r.v_strides, s, sizeof r.v_strides);
+    A.layout(3, 4, o, s, "o");
+    memcpy(r.o_strides, s, sizeof r.o_strides);
+    r.type = A.type(0, "q");
+    if (A.bad) return r;
+    A.same(A.type(1, "k") == r.type && A.type(2, "v") == r.type && A.type(3, "o") == r.type, "q, k, v and o of one type expected");
+    A.same(!memcmp(q, o, sizeof q), "o: the shape of q expected");
+    A.same(!memcmp(k, v, sizeof k), "v: the shape of k expected");
+    A.same(q[0] == k[0] && q[3] == k[3], "k: the samples and the head dimension of q expected");
+    if (A.bad) return r;
+    r.batch = q[0];
+    r.q_len = q[1];
+    r.q_heads = q[2];
+    r.head_dim = q[3];
+    r.kv_len = k[1];
+    r.kv_heads = k[2];
+    r.scale = A.f(scale);
+    r.causal = A.i(causal);
+    r.kv_lens = A.words<const int32_t>(lens, r.batch, "kv_lens");
+    return r;
+}
+int do_attention(Args& A)
+{
+    FN(fpq_attention);
+    const fpq_attention_args_t r = attention_args(A, 5, 6, 7);
+    float* const lse = A.words<float>(4, r.batch * r.q_heads * r.q_len, "lse");
+    return invoke(A, fn, &r, A.p(0), A.p(1), A.p(2), A.p(3), lse, A.p(8), A.bytes(8), A.stream());
+}
+int do_attention_backward(Args& A)
+{
+    FN(fpq_attention_backward);
+    fpq_attention_args_t r = attention_args(A, 9, 10, 11);
+    static const char* const names[4] = {"grad_o", "grad_q", "grad_k", "grad_v"};
+    int64_t* const strides[4] = {r.grad_o_strides, r.grad_q_strides, r.grad_k_strides, r.grad_v_strides};
+    for (int t = 0; t < 4 && !A.bad; ++t) {
+        int64_t n[4], s[4];
+        A.layout(5 + t, 4, n, s, names[t]);
+        memcpy(strides[t], s, sizeof r.grad_o_strides);
+        A.same(A.type(5 + t, names[t]) == r.type, "gradients: the type of q expected");
+        if (A.bad) break;
+        const int64_t len = t < 2 ? r.q_len : r.kv_len, heads = t < 2 ? r.q_heads : r.kv_heads;
+        A.same(n[0] == r.batch && n[1] == len && n[2] == heads && n[3] == r.head_dim, "gradients: the shapes of o, q, k and v expected");
+    }
+    const float* const lse = A.words<const float>(4, r.batch * r.q_heads * r.q_len, "lse");
+    return invoke(A, fn, &r, A.p(0), A.p(1), A.p(2), A.p(3), lse, A.p(5), A.p(6), A.p(7), A.p(8), A.p(12), A.bytes(12), A.stream());
+}
+
 // ---- names, parameters and defaults
 
 enum { kMaxParams = 26 };
@@ -334,7 +468,7 @@ struct Entry {
     const char* name;
     int (*run)(Args&);
     const char* params;                          // blank-separated
-    int required;                                // the others default to 0 ("acc_mode") or None
+    int required;                                // the others default to 0 ("acc_mode", "causal") or None
     int count;
     PyObject* names[kMaxParams];
     PyObject* defaults[kMaxParams];
@@ -359,6 +493,8 @@ Entry g_entries[] = {
     {"fpq_int_gemm", do_int_gemm, "xcodes sx zx px_dev packed_w wbits sw zw bias y M N K workspace", 14},
     {"fpq_rl_step", do_rl_step, "w sw f alpha a lr reg_weight loss_out grad_out workspace", 10},
     {"fpq_search_format", do_search_format, "x encodings n_bias mse_out result workspace", 6},
+    {"fpq_attention", do_attention, "q k v o lse scale causal kv_lens workspace", 6},
+    {"fpq_attention_backward", do_attention_backward, "q k v o lse grad_o grad_q grad_k grad_v scale causal kv_lens workspace", 10},
 };
 constexpr int kEntries = sizeof g_entries / sizeof g_entries[0];
 
@@ -430,6 +566,9 @@ PyMODINIT_FUNC PyInit__fpqcall(void)
     s_numel = PyUnicode_InternFromString("numel");
     s_element_size = PyUnicode_InternFromString("element_size");
     s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     PyObject* zero = PyLong_FromLong(0);
     for (int i = 0; i < kEntries; ++i) {
         Entry& e = g_entries[i];
@@ -441,7 +580,7 @@ PyMODINIT_FUNC PyInit__fpqcall(void)
             PyObject* name = PyUnicode_FromStringAndSize(p, (Py_ssize_t)len);
             PyUnicode_InternInPlace(&name);
             e.names[e.count] = name;
-            e.defaults[e.count] = e.count < e.required ? nullptr : (strncmp(p, "acc_mode", 8) == 0 ? zero : Py_None);
+            e.defaults[e.count] = e.count < e.required ? nullptr : (strncmp(p, "acc_mode", 8) == 0 || strncmp(p, "causal", 6) == 0 ? zero : Py_None);
             ++e.count;
             p += len + (q ? 1 : 0);
         }
