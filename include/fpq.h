@@ -489,6 +489,46 @@ int fpq_attention_backward(const fpq_attention_args_t *args, const void *q, cons
                            const float *lse, const void *grad_o, void *grad_q, void *grad_k, void *grad_v, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* ---- AdamW over many tensors ------------------------------------------------------------------------
+ *
+ * One optimizer step for any number of tensors (the adapters of a network, or the alpha of every layer in rounding learning, whose
+ * gradient fpq_rl_step writes to grad_out when called with lr = 0) in one launch.  For each element, in fp32, every operation
+ * rounded by itself in this order:
+ *   g = grad grad_scale;  m = m beta1 + g (1 - beta1);  v = v beta2 + (g (1 - beta2)) g;
+ *   param = param (1 - lr weight_decay) - (m / (sqrt(v) (1 - beta2^step)^(-1/2) + eps)) (lr / (1 - beta1^step)).
+ * state_bits 32: m and v are fp32 [n].  state_bits 8: m and v are one byte per element, codes of the format (4, 3, 7, 448) (hardware
+ *   E4M3) that stand for m and for the square root of v in units of a scale per 256 neighbouring elements of the tensor (the last
+ *   ones may be fewer), m_scale and v_scale fp32 [(n + 255) / 256]: the largest magnitude of the 256 times fl32(1 / 448) (1 when all
+ *   are zero; at least the smallest normal number).  Codes are rounded to nearest, a positive root to no less than 2^-9 scale.  A
+ *   state before the first step: codes 0 and any finite scales.  The step itself uses the unrounded m and v.
+ * param and grad are fp32 or bf16 (rounded to nearest); copy, if not NULL, receives param rounded to bf16 (the weights a layer
+ *   reads while fp32 ones are trained).  A gradient that is no finite number makes its element's param and states NaN or infinite,
+ *   with 8-bit states those of its 256 neighbours in the next step too.
+ * fpq_adamw_plan lays the tensors out for the steps: tensors is a HOST array, read during the call only (it travels as kernel
+ *   arguments); plan is fpq_adamw_plan_size bytes of device memory, 16-byte aligned; pieces_out (host) receives a number that the
+ *   steps are called with.  The addresses and sizes are those of the plan until it is written anew.  Arrays aligned for four
+ *   elements at a time (16, 8 or 4 bytes by type) are what the kernel is tuned for; others work.
+ * fpq_adamw_step: lr and weight_decay finite and >= 0, 0 <= beta < 1, eps positive and finite (FPQ_ERR_SCALE otherwise); step
+ *   counts from 1; grad_scale (device, one float, or NULL for 1) multiplies every gradient: a clipping factor or an inverse loss
+ *   scale.
+ * Limits: count and the elements of a tensor below 2^31 (FPQ_ERR_SHAPE). */
+typedef struct fpq_adamw_tensor {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale; /* state_bits 8 */
+    void *copy;               /* bf16, or NULL */
+    int64_t n;
+    int32_t param_type, grad_type; /* fpq_type */
+    int32_t state_bits;            /* 32 or 8 */
+    int32_t reserved;              /* 0 */
+} fpq_adamw_tensor_t;
+size_t fpq_adamw_plan_size(const fpq_adamw_tensor_t *tensors, int count);
+int fpq_adamw_plan(const fpq_adamw_tensor_t *tensors, int count, void *plan, size_t plan_bytes, int64_t *pieces_out,
+                   void *stream);
+int fpq_adamw_step(const void *plan, int64_t pieces, double lr, double beta1, double beta2, double eps, double weight_decay,
+                   int64_t step, const float *grad_scale, void *stream);
+
 /* ---- machine-ceiling probes (for the benchmark's roofline object) -------------------------------
  *
  * What this GPU sustains with nothing but the instruction in question in the loop, to set beside the published peaks

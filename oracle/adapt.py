@@ -1,4 +1,4 @@
-"""numpy oracle, in 64 bits, of the operators for adapting a quantized model: attention and its gradient.
+"""numpy oracle, in 64 bits, of the operators for adapting a quantized model: attention and its gradient, AdamW.
 
 Next to a result, `bounds` functions give how far a computation in 32-bit sums may be from it: every rounding it makes, times what
 that rounding scales."""
@@ -106,3 +106,56 @@ def attention_bounds(q, k, v, scale, causal, lens, bf16, go=None):
         return to, tl
     gq, gk, gv = attention_backward(q, k, v, go, scale, causal, lens)
     return to, tl, tq + r * np.abs(gq), tk + r * np.abs(gk), tv + r * np.abs(gv)
+
+
+# ------------------------------------------------------------------------------------------------ AdamW
+
+BLOCK, E4M3_MAX = 256, 448.0
+
+
+def e4m3_values():
+    """Value of every code of the format (4, 3, 7, 448); the two codes without one are NaN."""
+    c = np.arange(256)
+    e, f = (c >> 3) & 15, c & 7
+    v = np.where(e == 0, f * 2.0 ** -9, (1 + f / 8.0) * 2.0 ** (e - 7.0))
+    v = np.where((c & 127) == 127, np.nan, v)
+    return np.where(c & 128, -v, v).astype(np.float32)
+
+
+def e4m3_codes(x):
+    """Codes of fp32 values of magnitude at most 448, to nearest, ties to the even code."""
+    grid = e4m3_values()[:127].astype(np.float64)
+    a = np.abs(x.astype(np.float64))
+    hi = np.minimum(np.searchsorted(grid, a), 126)
+    lo = np.maximum(hi - 1, 0)
+    up, down = grid[hi] - a, a - grid[lo]
+    code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)
+    return (code + 128 * np.signbit(x)).astype(np.uint8)
+
+
+def state_codes(x, root):
+    """8-bit codes and scales of a flat fp32 state (a root of v: a positive value gets no code 0)."""
+    n = len(x)
+    b = np.zeros(-(-n // BLOCK) * BLOCK, np.float32)
+    b[:n] = x
+    b = b.reshape(-1, BLOCK)
+    top = np.abs(b).max(1)
+    scale = np.where(top == 0, np.float32(1), np.maximum(top * np.float32(np.float32(1) / np.float32(E4M3_MAX)), np.float32(2.0 ** -126))).astype(np.float32)
+    y = np.clip(b * (np.float32(1) / scale)[:, None], np.float32(-E4M3_MAX), np.float32(E4M3_MAX))
+    if root:
+        y = np.where(b > 0, np.maximum(y, np.float32(2.0 ** -9)), y)
+    return e4m3_codes(y.reshape(-1)[:n]), scale
+
+
+def state_values(codes, scale):
+    return (e4m3_values()[codes] * np.repeat(scale, BLOCK)[:len(codes)]).astype(np.float32)
+
+
+def adamw(param, grad, m, v, lr, beta1, beta2, eps, weight_decay, step, grad_scale=1.0):
+    """param, m, v after one step, in the precision of the arrays (all of one type), every operation rounded by itself."""
+    t = param.dtype.type
+    g = grad * t(grad_scale)
+    m = m * t(beta1) + g * t(1 - beta1)
+    v = v * t(beta2) + g * t(1 - beta2) * g
+    by = m / (np.sqrt(v) * t((1 - beta2 ** step) ** -0.5) + t(eps))
+    return param * t(1 - lr * weight_decay) - by * t(lr / (1 - beta1 ** step)), m, v

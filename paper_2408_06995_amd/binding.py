@@ -54,6 +54,12 @@ class fpq_attention_args_t(C.Structure):
                 ("grad_v_strides", C.c_int64 * 3)]
 
 
+class fpq_adamw_tensor_t(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32),
+                ("state_bits", C.c_int32), ("reserved", C.c_int32)]
+
+
 class FpqError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -176,6 +182,12 @@ def lib():
     L.fpq_attention.argtypes = [C.POINTER(fpq_attention_args_t)] + [vp] * 6 + [sz, vp]
     L.fpq_attention_backward.restype = i32
     L.fpq_attention_backward.argtypes = [C.POINTER(fpq_attention_args_t)] + [vp] * 10 + [sz, vp]
+    L.fpq_adamw_plan_size.restype = sz
+    L.fpq_adamw_plan_size.argtypes = [C.POINTER(fpq_adamw_tensor_t), i32]
+    L.fpq_adamw_plan.restype = i32
+    L.fpq_adamw_plan.argtypes = [C.POINTER(fpq_adamw_tensor_t), i32, vp, sz, C.POINTER(i64), vp]
+    L.fpq_adamw_step.restype = i32
+    L.fpq_adamw_step.argtypes = [vp, i64] + [C.c_double] * 5 + [i64, f32p, vp]
     L.fpq_gemm_noalloc.restype = i32
     L.fpq_gemm_noalloc.argtypes = [vp, i32, F, fl, f32p, vp, F, f32p, f32p, f32p, i64, i64, i64, i32, vp]
     _lib = L
@@ -192,7 +204,8 @@ EXPORTS = ["fpq_strerror", "fpq_format_max", "fpq_format_check", "fpq_bias_to_sc
            "fpq_packed_sparse_size", "fpq_pack_weights_sparse", "fpq_gemm_sparse", "fpq_conv2d_sparse",
            "fpq_int_calibrate_workspace_size", "fpq_int_calibrate", "fpq_int_quantize", "fpq_int_packed_size",
            "fpq_int_pack_weights", "fpq_int_gemm_workspace_size", "fpq_int_gemm",
-           "fpq_attention_workspace_size", "fpq_attention", "fpq_attention_backward_workspace_size", "fpq_attention_backward"]
+           "fpq_attention_workspace_size", "fpq_attention", "fpq_attention_backward_workspace_size", "fpq_attention_backward",
+           "fpq_adamw_plan_size", "fpq_adamw_plan", "fpq_adamw_step"]
 
 
 def fmt(f):
@@ -399,6 +412,51 @@ def fpq_attention_backward_workspace_size(batch, q_heads, kv_heads, q_len, kv_le
     return lib().fpq_attention_backward_workspace_size(_attention_sizes(batch, q_heads, kv_heads, q_len, kv_len, head_dim, type))
 
 
+def _type(t, what):
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("%s: float32 or bfloat16 expected, not %s" % (what, t.dtype))
+    return FPQ_TYPE_FP32 if t.dtype == torch.float32 else FPQ_TYPE_BF16
+
+
+def adamw_tensors(items):
+    """[(param, grad, m, v, m_scale or None, v_scale or None, copy or None), ...] of contiguous torch tensors -> ctypes array for
+    fpq_adamw_plan.  States are float32, or uint8 / float8_e4m3fn with a float32 scale per 256 elements.  The tensors must stay
+    alive, where they are, for as long as steps are made with the plan."""
+    import torch
+    arr = (fpq_adamw_tensor_t * len(items))()
+    for i, (param, grad, m, v, m_scale, v_scale, copy) in enumerate(items):
+        n, eight = param.numel(), m.dtype in (torch.uint8, torch.float8_e4m3fn)
+        if not eight and m.dtype != torch.float32:
+            raise TypeError("states: float32, uint8 or float8_e4m3fn expected, not %s" % m.dtype)
+        if v.dtype != m.dtype or (copy is not None and copy.dtype != torch.bfloat16):
+            raise TypeError("m and v of one type, and a copy in bfloat16, expected")
+        if eight and (m_scale is None or v_scale is None or m_scale.dtype != torch.float32 or v_scale.dtype != torch.float32):
+            raise TypeError("8-bit states: float32 scales expected")
+        scales = [m_scale, v_scale] if eight else []
+        whole = [param, grad, m, v] + ([copy] if copy is not None else [])
+        if any(t.numel() != n for t in whole) or any(t.numel() != (n + 255) // 256 for t in scales):
+            raise ValueError("tensors of one size, and one scale per 256 elements, expected")
+        if not all(t.is_contiguous() for t in whole + scales):
+            raise ValueError("contiguous tensors expected")
+        arr[i] = fpq_adamw_tensor_t(param.data_ptr(), grad.data_ptr(), m.data_ptr(), v.data_ptr(), *([t.data_ptr() for t in scales] or [None, None]),
+                                    None if copy is None else copy.data_ptr(), n, _type(param, "param"), _type(grad, "grad"),
+                                    8 if eight else 32, 0)
+    return arr
+
+
+def fpq_adamw_plan_size(tensors):
+    return lib().fpq_adamw_plan_size(tensors, len(tensors))
+
+
+def fpq_adamw_plan(tensors, plan):
+    """tensors: adamw_tensors().  Returns the number of pieces that the steps are called with."""
+    pieces = C.c_int64(0)
+    _check(lib().fpq_adamw_plan(tensors, len(tensors), _ptr(plan), plan.numel() * plan.element_size(), C.byref(pieces), _stream()),
+           "fpq_adamw_plan")
+    return pieces.value
+
+
 def fpq_rl_workspace_size(M, N, K):
     return lib().fpq_rl_workspace_size(M, N, K)
 
@@ -449,11 +507,12 @@ def fpq_rl_im2col(x, kh, kw, stride, pad, a):
 #       q, o: [batch, q_len, q_heads, dim], k, v: [batch, kv_len, kv_heads, dim], float32 or bfloat16, of any strides but the last;
 #       lse: float32 [batch, q_heads, q_len] or None; kv_lens: int32 [batch] or None
 #   fpq_attention_backward(q, k, v, o, lse, grad_o, grad_q, grad_k, grad_v, scale, causal=0, kv_lens=None, workspace=None)
+#   fpq_adamw_step(plan, pieces, lr, beta1, beta2, eps, weight_decay, step, grad_scale=None)    pieces: what fpq_adamw_plan returned
 
 NATIVE = ["fpq_gemm", "fpq_gemm_noalloc", "fpq_conv2d", "fpq_gemm_codes_out", "fpq_conv2d_codes_out",
           "fpq_gemm_sparse", "fpq_conv2d_sparse", "fpq_gemm_grouped", "fpq_absmax", "fpq_quantize",
           "fpq_quantize_nhwc", "fpq_int_calibrate", "fpq_int_quantize", "fpq_int_gemm", "fpq_rl_step",
-          "fpq_search_format", "fpq_attention", "fpq_attention_backward"]
+          "fpq_search_format", "fpq_attention", "fpq_attention_backward", "fpq_adamw_step"]
 
 
 def _resolve(name):

@@ -2,6 +2,7 @@
 // launches on the caller's stream.
 #include <math.h>
 
+#include "adamw.h"
 #include "attention.h"
 
 using namespace fpq;
@@ -74,9 +75,70 @@ AttentionArgs args_of(const fpq_attention_args_t* p)
     return a;
 }
 
+// FPQ_OK and the pieces of all tensors
+int check_adamw(const fpq_adamw_tensor_t* t, int count, int64_t* pieces)
+{
+    if (count < 0) return FPQ_ERR_SHAPE;
+    if (count && !t) return FPQ_ERR_NULL;
+    int64_t sum = 0;
+    for (int k = 0; k < count; ++k) {
+        const fpq_adamw_tensor_t& x = t[k];
+        if (x.n < 0 || x.n >= (int64_t)1 << 31) return FPQ_ERR_SHAPE;
+        for (int type : {x.param_type, x.grad_type})
+            if (type != FPQ_TYPE_FP32 && type != FPQ_TYPE_BF16) return FPQ_ERR_UNSUPPORTED;
+        if ((x.state_bits != 32 && x.state_bits != 8) || x.reserved) return FPQ_ERR_UNSUPPORTED;
+        if (x.n == 0) continue;
+        if (!x.param || !x.grad || !x.m || !x.v || (x.state_bits == 8 && (!x.m_scale || !x.v_scale))) return FPQ_ERR_NULL;
+        const size_t state = x.state_bits == 8 ? 1 : 4;
+        if (!aligned(x.param, size_of(x.param_type)) || !aligned(x.grad, size_of(x.grad_type)) || !aligned(x.m, state) || !aligned(x.v, state) ||
+            !aligned(x.copy, 2) || (state == 1 && (!aligned(x.m_scale, 4) || !aligned(x.v_scale, 4))))
+            return FPQ_ERR_ALIGN;
+        sum += (x.n + kAdamwPiece - 1) / kAdamwPiece;
+    }
+    if (sum >= (int64_t)1 << 31) return FPQ_ERR_SHAPE;
+    *pieces = sum;
+    return FPQ_OK;
+}
+
+bool finite_not_negative(double v) { return v >= 0.0 && !isinf(v); }
+
 }  // namespace
 
 extern "C" {
+
+size_t fpq_adamw_plan_size(const fpq_adamw_tensor_t* tensors, int count)
+{
+    int64_t pieces;
+    if (check_adamw(tensors, count, &pieces) != FPQ_OK) return 0;
+    return adamw_entries_at(pieces) + (size_t)count * sizeof(AdamwEntry);
+}
+
+int fpq_adamw_plan(const fpq_adamw_tensor_t* tensors, int count, void* plan, size_t plan_bytes, int64_t* pieces_out, void* stream)
+{
+    int64_t pieces;
+    const int st = check_adamw(tensors, count, &pieces);
+    if (st != FPQ_OK) return st;
+    if (!pieces_out) return FPQ_ERR_NULL;
+    if (pieces && !plan) return FPQ_ERR_NULL;
+    if (plan_bytes < fpq_adamw_plan_size(tensors, count)) return FPQ_ERR_WORKSPACE;
+    if (!aligned(plan, 16)) return FPQ_ERR_ALIGN;
+    *pieces_out = pieces;
+    if (!pieces) return FPQ_OK;
+    return launch_adamw_plan(tensors, count, pieces, plan, static_cast<hipStream_t>(stream));
+}
+
+int fpq_adamw_step(const void* plan, int64_t pieces, double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
+                   const float* grad_scale, void* stream)
+{
+    if (pieces < 0 || pieces >= (int64_t)1 << 31 || step < 1) return FPQ_ERR_SHAPE;
+    if (!finite_not_negative(lr) || !finite_not_negative(weight_decay) || !(eps > 0.0) || isinf(eps) || !(beta1 >= 0.0 && beta1 < 1.0) ||
+        !(beta2 >= 0.0 && beta2 < 1.0))
+        return FPQ_ERR_SCALE;
+    if (!pieces) return FPQ_OK;
+    if (!plan) return FPQ_ERR_NULL;
+    if (!aligned(plan, 16) || !aligned(grad_scale, 4)) return FPQ_ERR_ALIGN;
+    return launch_adamw(plan, pieces, lr, beta1, beta2, eps, weight_decay, step, grad_scale, static_cast<hipStream_t>(stream));
+}
 
 size_t fpq_attention_workspace_size(const fpq_attention_args_t* p)
 {

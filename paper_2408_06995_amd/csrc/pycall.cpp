@@ -66,6 +66,13 @@ struct Args {
         if (v == -1.0 && PyErr_Occurred()) bad = true;
         return (float)v;
     }
+    double real(int k)
+    {
+        if (bad) return 0.0;
+        const double v = PyFloat_AsDouble(a[k]);
+        if (v == -1.0 && PyErr_Occurred()) bad = true;
+        return v;
+    }
     // data_ptr() of a tensor; None: null
     void* ptr_of(PyObject* o)
     {
@@ -461,6 +468,13 @@ int do_attention_backward(Args& A)
     return invoke(A, fn, &r, A.p(0), A.p(1), A.p(2), A.p(3), lse, A.p(5), A.p(6), A.p(7), A.p(8), A.p(12), A.bytes(12), A.stream());
 }
 
+int do_adamw_step(Args& A)
+{
+    FN(fpq_adamw_step);
+    const float* const scale = A.words<const float>(8, 1, "grad_scale");
+    return invoke(A, fn, A.p(0), A.l(1), A.real(2), A.real(3), A.real(4), A.real(5), A.real(6), A.l(7), scale, A.stream());
+}
+
 // ---- names, parameters and defaults
 
 enum { kMaxParams = 26 };
@@ -495,6 +509,7 @@ Entry g_entries[] = {
     {"fpq_search_format", do_search_format, "x encodings n_bias mse_out result workspace", 6},
     {"fpq_attention", do_attention, "q k v o lse scale causal kv_lens workspace", 6},
     {"fpq_attention_backward", do_attention_backward, "q k v o lse grad_o grad_q grad_k grad_v scale causal kv_lens workspace", 10},
+    {"fpq_adamw_step", do_adamw_step, "plan pieces lr beta1 beta2 eps weight_decay step grad_scale", 8},
 };
 constexpr int kEntries = sizeof g_entries / sizeof g_entries[0];
 

@@ -69,3 +69,44 @@ def test_attention_binding_checks():
         B.fpq_attention_backward(q, k, k, q, lse, q, q, k[:, :3], k, 1.0)
     with pytest.raises(ValueError, match="gradients"):
         B.fpq_attention_backward(q, k, k, q, lse, q.bfloat16(), q, k, k, 1.0)
+
+
+def adamw_tensor(**kw):
+    t = B.fpq_adamw_tensor_t(param=4096, grad=8192, m=4096 * 3, v=4096 * 4, m_scale=4096 * 5, v_scale=4096 * 6, copy=None, n=1000, param_type=0, grad_type=1,
+                             state_bits=8)
+    for n, v in kw.items():
+        setattr(t, n, v)
+    return (B.fpq_adamw_tensor_t * 1)(t)
+
+
+def test_adamw_refusals():
+    L, p, out = B.lib(), C.c_void_p(4096), C.c_int64(0)
+    plan = lambda a, n=1, at=p, size=1 << 20, o=C.byref(out): L.fpq_adamw_plan(a, n, at, size, o, None)
+    for kw, status in ((dict(n=-1), -4), (dict(n=1 << 31), -4), (dict(param_type=2), -8), (dict(grad_type=-1), -8), (dict(state_bits=16), -8), (dict(reserved=1), -8),
+                       (dict(param=None), -1), (dict(grad=None), -1), (dict(m=None), -1), (dict(v=None), -1), (dict(m_scale=None), -1), (dict(v_scale=None), -1),
+                       (dict(param=4098), -5), (dict(grad=4097), -5), (dict(m=4098, state_bits=32), -5), (dict(v_scale=4098), -5), (dict(copy=4097), -5)):
+        assert plan(adamw_tensor(**kw)) == status, kw
+        assert L.fpq_adamw_plan_size(adamw_tensor(**kw), 1) == 0
+    good = adamw_tensor()
+    need = L.fpq_adamw_plan_size(good, 1)
+    assert need == 16 + 80 and plan(good, size=need - 1) == -6 and plan(good, at=None) == -1 and plan(good, at=C.c_void_p(4104)) == -5
+    assert plan(good, n=-1) == -4 and plan(None) == -1 and plan(good, o=None) == -1 and plan(None, n=0) == 0 and out.value == 0
+    step = lambda pieces=1, lr=1e-3, b1=0.9, b2=0.99, eps=1e-8, wd=0.0, t=1, at=p, gs=None: L.fpq_adamw_step(at, pieces, lr, b1, b2, eps, wd, t, gs, None)
+    nan, inf = float("nan"), float("inf")
+    for kw in (dict(lr=-1.0), dict(lr=nan), dict(lr=inf), dict(b1=1.0), dict(b1=-0.1), dict(b1=nan), dict(b2=1.0), dict(b2=nan), dict(eps=0.0), dict(eps=nan),
+               dict(eps=inf), dict(wd=-1.0), dict(wd=nan)):
+        assert step(**kw) == -3, kw
+    assert step(t=0) == -4 and step(pieces=-1) == -4 and step(at=None) == -1 and step(at=C.c_void_p(4104)) == -5 and step(gs=C.c_void_p(4098)) == -5
+    assert step(pieces=0) == 0
+
+
+def test_adamw_binding_checks():
+    f, b = torch.zeros(300), torch.zeros(300, dtype=torch.uint8)
+    s = torch.ones(2)
+    B.adamw_tensors([(f, f, f, f, None, None, None), (f, f.bfloat16(), b, b, s, s, f.bfloat16())])
+    for error, item in ((TypeError, (f.double(), f, f, f, None, None, None)), (TypeError, (f, f, f.double(), f.double(), None, None, None)),
+                        (TypeError, (f, f, f, b, None, None, None)), (TypeError, (f, f, b, b, s, None, None)), (TypeError, (f, f, f, f, None, None, f)),
+                        (ValueError, (f, f[:299], f, f, None, None, None)), (ValueError, (f, f, b, b, s, s[:1], None)),
+                        (ValueError, (torch.zeros(600)[::2], f, f, f, None, None, None))):
+        with pytest.raises(error):
+            B.adamw_tensors([item])

@@ -26,3 +26,25 @@ def test_attention_of_rows_that_see_nothing():
     o, lse = adapt.attention(q, k, v, 1.0, True, [3, 0])
     assert np.all(o[0, :2] == 0) and np.all(np.isneginf(lse[0, 0, :2])) and np.all(o[1] == 0) and np.all(np.isneginf(lse[1]))
     assert np.allclose(o[0, 2], v[0, 0]) and np.isclose(lse[0, 0, 2], (q[0, 2] * k[0, 0]).sum())
+
+
+def test_state_codes_are_the_nearest():
+    values = adapt.e4m3_values()
+    assert values[126] == 448 and values[8] == 2.0 ** -6 and values[1] == 2.0 ** -9 and values[254] == -448
+    finite = values[np.isfinite(values)]
+    assert np.array_equal(adapt.e4m3_codes(finite), np.arange(256)[np.isfinite(values)])
+    x = np.random.default_rng(5).standard_normal(4000).astype(np.float32) * np.float32(100)
+    x = np.clip(x, -448, 448)
+    got = values[adapt.e4m3_codes(x)]
+    assert np.all(np.abs(got - x) <= np.abs(finite[:, None] - x).min(0))
+    assert adapt.e4m3_codes(np.float32([1.0625, 1.1875, 2.0 ** -10, 3 * 2.0 ** -10]))[:4].tolist() == [56, 58, 0, 2]
+
+
+def test_adamw_step_is_the_textbook_one():
+    rng = np.random.default_rng(6)
+    p, g, m = (rng.standard_normal(50) for _ in range(3))
+    v = rng.random(50)
+    new, m1, v1 = adapt.adamw(p, g, m, v, 0.01, 0.9, 0.99, 1e-6, 0.1, 7, 0.5)
+    m2, v2 = 0.9 * m + 0.1 * (g / 2), 0.99 * v + 0.01 * (g / 2) ** 2
+    want = p - 0.01 * (0.1 * p + (m2 / (1 - 0.9 ** 7)) / (np.sqrt(v2 / (1 - 0.99 ** 7)) + 1e-6))
+    assert np.allclose(m1, m2) and np.allclose(v1, v2) and np.allclose(new, want, rtol=1e-12)
