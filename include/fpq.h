@@ -489,6 +489,45 @@ int fpq_attention_backward(const fpq_attention_args_t *args, const void *q, cons
                            const float *lse, const void *grad_o, void *grad_q, void *grad_k, void *grad_v, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* ---- low-rank adapters of many requests beside a shared projection -------------------------------------
+ *
+ * A quantized layer's weights are codes and stay as they are; what a model learns on top of them is a low-rank term per layer.  The
+ * rows of x are those of several requests, each with an adapter of its own out of a pool, or none:
+ *   rows row_start[r] .. row_start[r + 1] - 1 (device, requests + 1 values, not descending) use adapter[r] (device; negative or
+ *   past the pool: none; several requests may share one);
+ *   t_m = A x_m,  y_m = base_m + scaling B t_m  with A = a[adapter] [R, K], B = b[adapter] [N, R], scaling[adapter] fp32.
+ * Rows of no request, and of requests without an adapter, get t = 0 and y = base.  base is what the shared layer gave (fpq_gemm's y);
+ * it may be y itself, or NULL for zeros.  t: fp32 [M, R], for the backward call, or NULL.
+ * fpq_adapter_backward: with grad_y the gradient of y,
+ *   dt_m = scaling B^T grad_y_m,  grad_x_m = grad_x_base_m + A^T dt_m (not computed when grad_x is NULL; grad_x_base as base),
+ *   grad_a[i] = sum of dt_m x_m^T,  grad_b[i] = scaling sum of grad_y_m t_m^T over the rows m of adapter i: fp32, written for
+ *   every adapter of the pool, zeros for those without rows.  t is what the forward call wrote.
+ * x_type: of x, base, y and their gradients; w_type: of a and b; fp32 with either, or bf16 with bf16.  Operands that are fp32 are
+ * split into three bf16 parts as in FPQ_TYPE_FP32 attention, t and its gradient always are; sums are fp32, and only bf16 results are
+ * rounded to bf16.  Infinities and NaN make what depends on them infinite or NaN.  No atomics: the same bits in every run.
+ * a and b are contiguous; rows of the other matrices have the strides ld_* (in elements), their elements are neighbours.
+ * Adapters of a smaller rank are filled up with zero rows of A and columns of B, which stay zero in training.  Rows of 16-byte
+ * multiples that start at one, and ranks that are multiples of 8, are what the kernels are tuned for; others work.
+ * workspace: the stated bytes, 16-byte aligned (NULL when that is 0); calls that share one are ordered on one stream.
+ * Limits: R <= 128 (FPQ_ERR_UNSUPPORTED beyond); M, N, K, requests, R K and R N at most 2^30, adapters at most 65535 (FPQ_ERR_SHAPE). */
+typedef struct fpq_adapter_args {
+    int32_t x_type, w_type; /* fpq_type */
+    int64_t M, N, K, R;
+    int64_t requests, adapters;
+    const float *scaling;     /* [adapters] */
+    const int32_t *row_start; /* [requests + 1] */
+    const int32_t *adapter;   /* [requests] */
+    int64_t ld_x, ld_base, ld_y;
+    int64_t ld_grad_y, ld_grad_x_base, ld_grad_x; /* backward only */
+} fpq_adapter_args_t;
+size_t fpq_adapter_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters);
+int fpq_adapter_apply(const fpq_adapter_args_t *args, const void *x, const void *a, const void *b, const void *base, void *y,
+                      float *t, void *workspace, size_t workspace_bytes, void *stream);
+size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters);
+int fpq_adapter_backward(const fpq_adapter_args_t *args, const void *x, const void *a, const void *b, const float *t,
+                         const void *grad_y, const void *grad_x_base, void *grad_x, float *grad_a, float *grad_b,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- AdamW over many tensors ------------------------------------------------------------------------
  *
  * One optimizer step for any number of tensors (the adapters of a network, or the alpha of every layer in rounding learning, whose

@@ -1,4 +1,5 @@
-"""numpy oracle, in 64 bits, of the operators for adapting a quantized model: attention and its gradient, AdamW.
+"""numpy oracle, in 64 bits, of the operators for adapting a quantized model: attention and its gradient, low-rank adapters and
+theirs, AdamW.
 
 Next to a result, `bounds` functions give how far a computation in 32-bit sums may be from it: every rounding it makes, times what
 that rounding scales."""
@@ -159,3 +160,63 @@ def adamw(param, grad, m, v, lr, beta1, beta2, eps, weight_decay, step, grad_sca
     v = v * t(beta2) + g * t(1 - beta2) * g
     by = m / (np.sqrt(v) * t((1 - beta2 ** step) ** -0.5) + t(eps))
     return param * t(1 - lr * weight_decay) - by * t(lr / (1 - beta1 ** step)), m, v
+
+
+# ------------------------------------------------------------------------------------------------ adapters
+
+def requests_of(row_start, adapter, M, adapters):
+    """(rows, adapter) of the requests that have one."""
+    for r, i in enumerate(adapter):
+        lo, hi = (int(min(max(v, 0), M)) for v in row_start[r:r + 2])
+        if 0 <= i < adapters and lo < hi:
+            yield slice(lo, hi), int(i)
+
+
+def adapter_apply(x, a, b, scaling, row_start, adapter, base):
+    """y, t."""
+    y, t = base.astype(np.float64).copy(), np.zeros((len(x), a.shape[1]))
+    for rows, i in requests_of(row_start, adapter, len(x), len(a)):
+        t[rows] = x[rows] @ a[i].T
+        y[rows] += scaling[i] * (t[rows] @ b[i].T)
+    return y, t
+
+
+def adapter_backward(x, a, b, scaling, row_start, adapter, gy, gx_base):
+    """gx, ga, gb."""
+    gx, ga, gb = gx_base.astype(np.float64).copy(), np.zeros(a.shape), np.zeros(b.shape)
+    for rows, i in requests_of(row_start, adapter, len(x), len(a)):
+        t, dt = x[rows] @ a[i].T, scaling[i] * (gy[rows] @ b[i])
+        gx[rows] += dt @ a[i]
+        ga[i] += dt.T @ x[rows]
+        gb[i] += scaling[i] * (gy[rows].T @ t)
+    return gx, ga, gb
+
+
+def adapter_bounds(x, a, b, scaling, row_start, adapter, base, bf16, gy=None, gx_base=None):
+    """Bounds of |error| for y and t (and, with gy, for gx, ga, gb): a sum over n terms makes n + 16 roundings (16: the parts of split
+    operands, the scale, the sum of parts) of at most the sum of its terms' magnitudes, on top of what its operands are off."""
+    u = lambda n: (n + 16) * U32
+    r = U16 if bf16 else U32
+    M, (_, R, K), N = len(x), a.shape, b.shape[1]
+    t_off, y_off = np.zeros((M, R)), np.zeros((M, N))
+    A, B, X = np.abs(a), np.abs(b), np.abs(x)
+    y, _ = adapter_apply(x, a, b, scaling, row_start, adapter, base)
+    out = []
+    for rows, i in requests_of(row_start, adapter, M, len(a)):
+        mass = X[rows] @ A[i].T
+        t_off[rows] = u(K) * mass
+        y_off[rows] = scaling[i] * ((t_off[rows] + u(R) * mass) @ B[i].T)
+    y_off += U32 * (np.abs(base) + np.abs(y)) + r * (np.abs(y) + y_off)
+    if gy is None:
+        return y_off, t_off
+    gx_off, ga_off, gb_off = np.zeros((M, K)), np.zeros(a.shape), np.zeros(b.shape)
+    G = np.abs(gy)
+    gx, _, _ = adapter_backward(x, a, b, scaling, row_start, adapter, gy, gx_base)
+    for rows, i in requests_of(row_start, adapter, M, len(a)):
+        mass_t, mass_d = X[rows] @ A[i].T, scaling[i] * (G[rows] @ B[i])
+        d_off = u(N) * mass_d
+        gx_off[rows] = (d_off + u(R) * mass_d) @ A[i]
+        ga_off[i] += (d_off + u(M) * mass_d).T @ X[rows]
+        gb_off[i] += scaling[i] * (G[rows].T @ (t_off[rows] + u(M) * mass_t))
+    gx_off += U32 * (np.abs(gx_base) + np.abs(gx)) + r * (np.abs(gx) + gx_off)
+    return y_off, t_off, gx_off, ga_off, gb_off

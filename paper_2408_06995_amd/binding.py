@@ -54,6 +54,13 @@ class fpq_attention_args_t(C.Structure):
                 ("grad_v_strides", C.c_int64 * 3)]
 
 
+class fpq_adapter_args_t(C.Structure):
+    _fields_ = [("x_type", C.c_int32), ("w_type", C.c_int32), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("R", C.c_int64),
+                ("requests", C.c_int64), ("adapters", C.c_int64), ("scaling", C.c_void_p), ("row_start", C.c_void_p),
+                ("adapter", C.c_void_p), ("ld_x", C.c_int64), ("ld_base", C.c_int64), ("ld_y", C.c_int64), ("ld_grad_y", C.c_int64),
+                ("ld_grad_x_base", C.c_int64), ("ld_grad_x", C.c_int64)]
+
+
 class fpq_adamw_tensor_t(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32),
@@ -182,6 +189,13 @@ def lib():
     L.fpq_attention.argtypes = [C.POINTER(fpq_attention_args_t)] + [vp] * 6 + [sz, vp]
     L.fpq_attention_backward.restype = i32
     L.fpq_attention_backward.argtypes = [C.POINTER(fpq_attention_args_t)] + [vp] * 10 + [sz, vp]
+    for name in ("fpq_adapter_workspace_size", "fpq_adapter_backward_workspace_size"):
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = [i64] * 6
+    L.fpq_adapter_apply.restype = i32
+    L.fpq_adapter_apply.argtypes = [C.POINTER(fpq_adapter_args_t)] + [vp] * 7 + [sz, vp]
+    L.fpq_adapter_backward.restype = i32
+    L.fpq_adapter_backward.argtypes = [C.POINTER(fpq_adapter_args_t)] + [vp] * 10 + [sz, vp]
     L.fpq_adamw_plan_size.restype = sz
     L.fpq_adamw_plan_size.argtypes = [C.POINTER(fpq_adamw_tensor_t), i32]
     L.fpq_adamw_plan.restype = i32
@@ -205,6 +219,7 @@ EXPORTS = ["fpq_strerror", "fpq_format_max", "fpq_format_check", "fpq_bias_to_sc
            "fpq_int_calibrate_workspace_size", "fpq_int_calibrate", "fpq_int_quantize", "fpq_int_packed_size",
            "fpq_int_pack_weights", "fpq_int_gemm_workspace_size", "fpq_int_gemm",
            "fpq_attention_workspace_size", "fpq_attention", "fpq_attention_backward_workspace_size", "fpq_attention_backward",
+           "fpq_adapter_workspace_size", "fpq_adapter_apply", "fpq_adapter_backward_workspace_size", "fpq_adapter_backward",
            "fpq_adamw_plan_size", "fpq_adamw_plan", "fpq_adamw_step"]
 
 
@@ -412,6 +427,14 @@ def fpq_attention_backward_workspace_size(batch, q_heads, kv_heads, q_len, kv_le
     return lib().fpq_attention_backward_workspace_size(_attention_sizes(batch, q_heads, kv_heads, q_len, kv_len, head_dim, type))
 
 
+def fpq_adapter_workspace_size(M, N, K, R, requests, adapters):
+    return lib().fpq_adapter_workspace_size(M, N, K, R, requests, adapters)
+
+
+def fpq_adapter_backward_workspace_size(M, N, K, R, requests, adapters):
+    return lib().fpq_adapter_backward_workspace_size(M, N, K, R, requests, adapters)
+
+
 def _type(t, what):
     import torch
     if t.dtype not in (torch.float32, torch.bfloat16):
@@ -507,12 +530,18 @@ def fpq_rl_im2col(x, kh, kw, stride, pad, a):
 #       q, o: [batch, q_len, q_heads, dim], k, v: [batch, kv_len, kv_heads, dim], float32 or bfloat16, of any strides but the last;
 #       lse: float32 [batch, q_heads, q_len] or None; kv_lens: int32 [batch] or None
 #   fpq_attention_backward(q, k, v, o, lse, grad_o, grad_q, grad_k, grad_v, scale, causal=0, kv_lens=None, workspace=None)
+#   fpq_adapter_apply(x, a, b, scaling, row_start, adapter, base, y, t, workspace=None)
+#       x: [M, K], base (or None), y: [M, N], rows of any stride; a: [adapters, R, K], b: [adapters, N, R], scaling: float32 [adapters];
+#       row_start: int32 [requests + 1], adapter: int32 [requests]; t: float32 [M, R] or None
+#   fpq_adapter_backward(x, a, b, scaling, row_start, adapter, t, grad_y, grad_x_base, grad_x, grad_a, grad_b, workspace=None)
+#       grad_x_base and grad_x may be None; grad_a, grad_b: float32, the shapes of a and b
 #   fpq_adamw_step(plan, pieces, lr, beta1, beta2, eps, weight_decay, step, grad_scale=None)    pieces: what fpq_adamw_plan returned
 
 NATIVE = ["fpq_gemm", "fpq_gemm_noalloc", "fpq_conv2d", "fpq_gemm_codes_out", "fpq_conv2d_codes_out",
           "fpq_gemm_sparse", "fpq_conv2d_sparse", "fpq_gemm_grouped", "fpq_absmax", "fpq_quantize",
           "fpq_quantize_nhwc", "fpq_int_calibrate", "fpq_int_quantize", "fpq_int_gemm", "fpq_rl_step",
-          "fpq_search_format", "fpq_attention", "fpq_attention_backward", "fpq_adamw_step"]
+          "fpq_search_format", "fpq_attention", "fpq_attention_backward", "fpq_adapter_apply", "fpq_adapter_backward",
+          "fpq_adamw_step"]
 
 
 def _resolve(name):

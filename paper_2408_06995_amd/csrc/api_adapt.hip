@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include "adamw.h"
+#include "adapter.h"
 #include "attention.h"
 
 using namespace fpq;
@@ -100,11 +101,147 @@ int check_adamw(const fpq_adamw_tensor_t* t, int count, int64_t* pieces)
     return FPQ_OK;
 }
 
+int check_adapter_sizes(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
+{
+    for (int64_t v : {M, N, K, R, requests, adapters})
+        if (v < 0 || v > kMost) return FPQ_ERR_SHAPE;
+    if (N == 0 || K == 0 || R == 0 || adapters == 0 || adapters > 65535) return FPQ_ERR_SHAPE;
+    if (R > kMaxRank) return FPQ_ERR_UNSUPPORTED;
+    if (R * K > kMost || R * N > kMost) return FPQ_ERR_SHAPE;
+    return FPQ_OK;
+}
+
+// Every row of [rows, n] starts at a multiple of `to` bytes.
+bool matrix_aligned(const void* p, int64_t ld, int64_t rows, size_t size, size_t to)
+{
+    return aligned(p, to) && (rows <= 1 || ld * (int64_t)size % (int64_t)to == 0);
+}
+
+// Sizes and pointers that both calls have; a row of fewer elements than its stride's claim is an error.
+int check_adapter(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b)
+{
+    if (!p) return FPQ_ERR_NULL;
+    if (p->x_type != FPQ_TYPE_FP32 && p->x_type != FPQ_TYPE_BF16) return FPQ_ERR_UNSUPPORTED;
+    if (p->w_type != FPQ_TYPE_FP32 && p->w_type != FPQ_TYPE_BF16) return FPQ_ERR_UNSUPPORTED;
+    if (p->x_type == FPQ_TYPE_BF16 && p->w_type != FPQ_TYPE_BF16) return FPQ_ERR_UNSUPPORTED;
+    const int st = check_adapter_sizes(p->M, p->N, p->K, p->R, p->requests, p->adapters);
+    if (st != FPQ_OK) return st;
+    if (p->M && p->ld_x < p->K) return FPQ_ERR_SHAPE;
+    if (!p->scaling || !p->row_start || (p->requests && !p->adapter) || !a || !b || (p->M && !x)) return FPQ_ERR_NULL;
+    if (!aligned(p->scaling, 4) || !aligned(p->row_start, 4) || !aligned(p->adapter, 4) || !aligned(x, size_of(p->x_type)) ||
+        !aligned(a, size_of(p->w_type)) || !aligned(b, size_of(p->w_type)))
+        return FPQ_ERR_ALIGN;
+    return FPQ_OK;
+}
+
+AdapterArgs args_of(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b, const float* t)
+{
+    AdapterArgs r{};
+    r.x = x;
+    r.a = a;
+    r.b = b;
+    r.scaling = p->scaling;
+    r.row_start = p->row_start;
+    r.adapter = p->adapter;
+    r.ldx = p->ld_x;
+    r.M = (int)p->M;
+    r.N = (int)p->N;
+    r.K = (int)p->K;
+    r.R = (int)p->R;
+    r.requests = (int)p->requests;
+    r.adapters = (int)p->adapters;
+    const size_t w = size_of(p->w_type);
+    r.vec_r = p->R % 8 == 0 && aligned(b, 16) && aligned(t, 16);
+    r.vec_a = p->K * w % 16 == 0 && aligned(a, 16);
+    return r;
+}
+
 bool finite_not_negative(double v) { return v >= 0.0 && !isinf(v); }
 
 }  // namespace
 
 extern "C" {
+
+size_t fpq_adapter_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
+{
+    if (check_adapter_sizes(M, N, K, R, requests, adapters) != FPQ_OK) return 0;
+    // t of each part of K; of the only one when the caller wants none
+    return align_up((size_t)plan_adapter(M, N, K, R, requests, adapters).parts * M * R * 4);
+}
+
+int fpq_adapter_apply(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b, const void* base, void* y, float* t,
+                      void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int st = check_adapter(p, x, a, b);
+    if (st != FPQ_OK) return st;
+    if (p->M == 0) return FPQ_OK;
+    if (!y) return FPQ_ERR_NULL;
+    if (p->ld_y < p->N || (base && p->ld_base < p->N)) return FPQ_ERR_SHAPE;
+    const size_t size = size_of(p->x_type);
+    if (!aligned(y, size) || !aligned(base, size) || !aligned(t, 4)) return FPQ_ERR_ALIGN;
+    const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->R, p->requests, p->adapters);
+    if (plan.parts > 1 || !t) {
+        if (!workspace || workspace_bytes < fpq_adapter_workspace_size(p->M, p->N, p->K, p->R, p->requests, p->adapters)) return FPQ_ERR_WORKSPACE;
+        if (!aligned(workspace, 16)) return FPQ_ERR_ALIGN;
+    }
+    AdapterArgs r = args_of(p, x, a, b, t);
+    r.base = base;
+    r.y = y;
+    r.ld_base = p->ld_base;
+    r.ldy = p->ld_y;
+    r.parts = plan.parts;
+    r.steps_per_part = plan.steps_per_part;
+    r.t = t || plan.parts > 1 ? t : static_cast<float*>(workspace);
+    r.t_part = plan.parts > 1 ? static_cast<float*>(workspace) : nullptr;
+    r.vec_y = p->N % 4 == 0 && matrix_aligned(y, p->ld_y, p->M, size, 4 * size) && (!base || matrix_aligned(base, p->ld_base, p->M, size, 4 * size));
+    const bool vec_k = r.vec_a && p->K * size % 16 == 0 && matrix_aligned(x, p->ld_x, p->M, size, 16);
+    return launch_adapter_apply(r, p->x_type, p->w_type, vec_k, plan, static_cast<hipStream_t>(stream));
+}
+
+size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
+{
+    if (check_adapter_sizes(M, N, K, R, requests, adapters) != FPQ_OK) return 0;
+    const AdapterPlan plan = plan_adapter(M, N, K, R, requests, adapters);
+    const size_t each = (size_t)adapters * R * 4;
+    return align_up((size_t)M * R * 4) + (plan.splits > 1 ? align_up(plan.splits * each * K) + align_up(plan.splits * each * N) : 0);
+}
+
+int fpq_adapter_backward(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b, const float* t, const void* grad_y,
+                         const void* grad_x_base, void* grad_x, float* grad_a, float* grad_b, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int st = check_adapter(p, x, a, b);
+    if (st != FPQ_OK) return st;
+    if (!grad_a || !grad_b || (p->M && (!t || !grad_y))) return FPQ_ERR_NULL;
+    if (p->M && (p->ld_grad_y < p->N || (grad_x && (p->ld_grad_x < p->K || (grad_x_base && p->ld_grad_x_base < p->K))))) return FPQ_ERR_SHAPE;
+    const size_t size = size_of(p->x_type);
+    if (!aligned(t, 4) || !aligned(grad_y, size) || !aligned(grad_x_base, size) || !aligned(grad_x, size) || !aligned(grad_a, 4) || !aligned(grad_b, 4))
+        return FPQ_ERR_ALIGN;
+    const size_t need = fpq_adapter_backward_workspace_size(p->M, p->N, p->K, p->R, p->requests, p->adapters);
+    if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 16)) return FPQ_ERR_ALIGN;
+    const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->R, p->requests, p->adapters);
+    AdapterArgs r = args_of(p, x, a, b, t);
+    r.t_in = t;
+    r.gy = grad_y;
+    r.ld_gy = p->ld_grad_y;
+    r.gx_base = grad_x_base;
+    r.ld_gx_base = p->ld_grad_x_base;
+    r.gx = p->M ? grad_x : nullptr;
+    r.ld_gx = p->ld_grad_x;
+    r.ga = grad_a;
+    r.gb = grad_b;
+    r.splits = plan.splits;
+    char* at = static_cast<char*>(workspace);
+    r.dt = reinterpret_cast<float*>(at);
+    at += align_up((size_t)p->M * p->R * 4);
+    r.part_a = reinterpret_cast<float*>(at);
+    r.part_b = reinterpret_cast<float*>(at + align_up((size_t)plan.splits * p->adapters * p->R * p->K * 4));
+    r.vec_y = p->K % 4 == 0 && matrix_aligned(grad_x, p->ld_grad_x, p->M, size, 4 * size) &&
+              (!grad_x_base || matrix_aligned(grad_x_base, p->ld_grad_x_base, p->M, size, 4 * size));
+    const bool vec_n = p->N * size % 16 == 0 && matrix_aligned(grad_y, p->ld_grad_y, p->M, size, 16);
+    const bool vec_k = p->K * size % 16 == 0 && matrix_aligned(x, p->ld_x, p->M, size, 16);
+    return launch_adapter_backward(r, p->x_type, p->w_type, vec_n, vec_k, plan, static_cast<hipStream_t>(stream));
+}
 
 size_t fpq_adamw_plan_size(const fpq_adamw_tensor_t* tensors, int count)
 {

@@ -468,6 +468,72 @@ int do_attention_backward(Args& A)
     return invoke(A, fn, &r, A.p(0), A.p(1), A.p(2), A.p(3), lse, A.p(5), A.p(6), A.p(7), A.p(8), A.p(12), A.bytes(12), A.stream());
 }
 
+// x, a, b, scaling, row_start, adapter: the first six arguments of both calls
+fpq_adapter_args_t adapter_args(Args& A)
+{
+    fpq_adapter_args_t r;
+    memset(&r, 0, sizeof r);
+    int64_t x[2] = {}, sx[2] = {}, a[3] = {}, b[3] = {}, s[3] = {}, q[1] = {};
+    A.layout(0, 2, x, sx, "x");
+    A.layout(1, 3, a, s, "a");
+    if (!A.bad) A.same(s[1] == a[2] || a[1] <= 1, "a: not contiguous");
+    if (!A.bad) A.same(s[0] == a[1] * a[2] || a[0] <= 1, "a: not contiguous");
+    A.layout(2, 3, b, s, "b");
+    if (!A.bad) A.same(s[1] == b[2] || b[1] <= 1, "b: not contiguous");
+    if (!A.bad) A.same(s[0] == b[1] * b[2] || b[0] <= 1, "b: not contiguous");
+    A.layout(5, 1, q, s, "adapter");
+    r.x_type = A.type(0, "x");
+    r.w_type = A.type(1, "a");
+    if (A.bad) return r;
+    A.same(A.type(2, "b") == r.w_type, "a and b of one type expected");
+    A.same(a[0] == b[0] && a[1] == b[2], "a [adapters, R, K] and b [adapters, N, R] expected");
+    A.same(x[1] == a[2], "x: rows of the adapters' K expected");
+    r.M = x[0];
+    r.K = x[1];
+    r.R = a[1];
+    r.N = b[1];
+    r.adapters = a[0];
+    r.requests = q[0];
+    r.ld_x = x[0] > 1 ? sx[0] : x[1];
+    r.scaling = A.words<const float>(3, r.adapters, "scaling");
+    r.row_start = A.words<const int32_t>(4, r.requests + 1, "row_start");
+    r.adapter = A.words<const int32_t>(5, r.requests, "adapter");
+    return r;
+}
+// A matrix of `rows` x `cols` of x's type, or None: its row stride
+int64_t adapter_rows(Args& A, int k, const fpq_adapter_args_t& r, int64_t cols, const char* name)
+{
+    if (A.bad || A.a[k] == Py_None) return cols;
+    int64_t n[2], s[2];
+    A.layout(k, 2, n, s, name);
+    if (A.bad) return 0;
+    if (n[0] != r.M || n[1] != cols || A.type(k, name) != r.x_type) {
+        if (!A.bad) PyErr_Format(PyExc_ValueError, "%s: rows of x, %lld columns and the type of x expected", name, (long long)cols);
+        A.bad = true;
+    }
+    return n[0] > 1 ? s[0] : cols;
+}
+int do_adapter_apply(Args& A)
+{
+    FN(fpq_adapter_apply);
+    fpq_adapter_args_t r = adapter_args(A);
+    r.ld_base = adapter_rows(A, 6, r, r.N, "base");
+    r.ld_y = adapter_rows(A, 7, r, r.N, "y");
+    float* const t = A.words<float>(8, r.M * r.R, "t");
+    return invoke(A, fn, &r, A.p(0), A.p(1), A.p(2), A.p(6), A.p(7), t, A.p(9), A.bytes(9), A.stream());
+}
+int do_adapter_backward(Args& A)
+{
+    FN(fpq_adapter_backward);
+    fpq_adapter_args_t r = adapter_args(A);
+    const float* const t = A.words<const float>(6, r.M * r.R, "t");
+    r.ld_grad_y = adapter_rows(A, 7, r, r.N, "grad_y");
+    r.ld_grad_x_base = adapter_rows(A, 8, r, r.K, "grad_x_base");
+    r.ld_grad_x = adapter_rows(A, 9, r, r.K, "grad_x");
+    float* const ga = A.words<float>(10, r.adapters * r.R * r.K, "grad_a");
+    float* const gb = A.words<float>(11, r.adapters * r.R * r.N, "grad_b");
+    return invoke(A, fn, &r, A.p(0), A.p(1), A.p(2), t, A.p(7), A.p(8), A.p(9), ga, gb, A.p(12), A.bytes(12), A.stream());
+}
 int do_adamw_step(Args& A)
 {
     FN(fpq_adamw_step);
@@ -509,6 +575,9 @@ Entry g_entries[] = {
     {"fpq_search_format", do_search_format, "x encodings n_bias mse_out result workspace", 6},
     {"fpq_attention", do_attention, "q k v o lse scale causal kv_lens workspace", 6},
     {"fpq_attention_backward", do_attention_backward, "q k v o lse grad_o grad_q grad_k grad_v scale causal kv_lens workspace", 10},
+    {"fpq_adapter_apply", do_adapter_apply, "x a b scaling row_start adapter base y t workspace", 9},
+    {"fpq_adapter_backward", do_adapter_backward,
+     "x a b scaling row_start adapter t grad_y grad_x_base grad_x grad_a grad_b workspace", 12},
     {"fpq_adamw_step", do_adamw_step, "plan pieces lr beta1 beta2 eps weight_decay step grad_scale", 8},
 };
 constexpr int kEntries = sizeof g_entries / sizeof g_entries[0];

@@ -110,3 +110,67 @@ def test_adamw_binding_checks():
                         (ValueError, (torch.zeros(600)[::2], f, f, f, None, None, None))):
         with pytest.raises(error):
             B.adamw_tensors([item])
+
+
+def adapter_args(**kw):
+    a = B.fpq_adapter_args_t(x_type=0, w_type=1, M=10, N=32, K=64, R=8, requests=2, adapters=3, scaling=4096, row_start=4096, adapter=4096, ld_x=64, ld_base=32, ld_y=32,
+                             ld_grad_y=32, ld_grad_x_base=64, ld_grad_x=64)
+    for n, v in kw.items():
+        setattr(a, n, v)
+    return a
+
+
+def test_adapter_refusals():
+    L, p, big = B.lib(), C.c_void_p(4096), 1 << 40
+    fwd = lambda a, x=p, wa=p, wb=p, base=p, y=p, t=p, ws=p, n=big: L.fpq_adapter_apply(C.byref(a), x, wa, wb, base, y, t, ws, n, None)
+    back = lambda a, ws=p, n=big, **kw: L.fpq_adapter_backward(C.byref(a), *[kw.get(v, p) for v in "x wa wb t gy gxb gx ga gb".split()], ws, n, None)
+    assert L.fpq_adapter_apply(None, p, p, p, p, p, p, p, big, None) == -1
+    for kw, status in ((dict(x_type=2), -8), (dict(w_type=-1), -8), (dict(x_type=1, w_type=0), -8), (dict(R=129), -8), (dict(R=0), -4), (dict(N=0), -4), (dict(K=0), -4),
+                       (dict(M=-1), -4), (dict(adapters=0), -4), (dict(adapters=65536), -4), (dict(requests=-1), -4), (dict(K=1 << 28, R=8, ld_x=1 << 28), -4),
+                       (dict(ld_x=63), -4), (dict(scaling=None), -1), (dict(row_start=None), -1), (dict(adapter=None), -1), (dict(scaling=4097), -5),
+                       (dict(row_start=4098), -5), (dict(adapter=4098), -5)):
+        assert fwd(adapter_args(**kw)) == status, kw
+        assert back(adapter_args(**kw)) == status, kw
+    for kw in (dict(ld_y=31), dict(ld_base=31)):
+        assert fwd(adapter_args(**kw)) == -4
+    for kw in (dict(ld_grad_y=31), dict(ld_grad_x=63), dict(ld_grad_x_base=63)):
+        assert back(adapter_args(**kw)) == -4
+    a = adapter_args()
+    for name in ("x", "wa", "wb", "y"):
+        assert fwd(a, **{name: None}) == -1 and fwd(a, **{name: C.c_void_p(4097)}) == -5
+    assert fwd(a, base=C.c_void_p(4098)) == -5 and fwd(a, t=C.c_void_p(4098)) == -5
+    for name in ("x", "wa", "wb", "t", "gy", "ga", "gb"):
+        assert back(a, **{name: None}) == -1 and back(a, **{name: C.c_void_p(4097)}) == -5, name
+    assert back(a, gx=C.c_void_p(4098)) == -5 and back(a, gxb=C.c_void_p(4098)) == -5
+    need = L.fpq_adapter_workspace_size(10, 32, 64, 8, 2, 3)
+    assert need > 0 and fwd(a, t=None, n=need - 1) == -6 and fwd(a, t=None, ws=None) == -6 and fwd(a, t=None, ws=C.c_void_p(4100)) == -5
+    need = L.fpq_adapter_backward_workspace_size(10, 32, 64, 8, 2, 3)
+    assert need > 0 and back(a, n=need - 1) == -6 and back(a, ws=None) == -6 and back(a, ws=C.c_void_p(4100)) == -5
+    assert fwd(adapter_args(M=0)) == 0
+    assert L.fpq_adapter_workspace_size(10, 32, 64, 129, 2, 3) == 0 and L.fpq_adapter_backward_workspace_size(10, 32, 0, 8, 2, 3) == 0
+
+
+def test_adapter_binding_checks():
+    x, a, b = torch.zeros(10, 64), torch.zeros(3, 8, 64), torch.zeros(3, 32, 8)
+    s, start, of = torch.ones(3), torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    y, t = torch.zeros(10, 32), torch.zeros(10, 8)
+
+    def refused(error, match, *args):
+        with pytest.raises(error, match=match):
+            B.fpq_adapter_apply(*args)
+
+    refused(ValueError, "2 dimensions", x[0], a, b, s, start, of, y, y, t)
+    refused(ValueError, "b \\[adapters", x, a, b[:2], s, start, of, y, y, t)
+    refused(ValueError, "contiguous", x, torch.zeros(3, 16, 64)[:, :8], b, s, start, of, y, y, t)
+    refused(ValueError, "contiguous", x, a, torch.zeros(3, 64, 8)[:, ::2], s, start, of, y, y, t)
+    refused(ValueError, "the adapters' K", x[:, :32], a, b, s, start, of, y, y, t)
+    refused(ValueError, "scaling", x, a, b, s[:2], start, of, y, y, t)
+    refused(ValueError, "row_start", x, a, b, s, start[:2], of, y, y, t)
+    refused(ValueError, "adapter", x, a, b, s, start, of.long(), y, y, t)
+    refused(ValueError, "base", x, a, b, s, start, of, y[:5], y, t)
+    refused(ValueError, "y:", x, a, b, s, start, of, None, y.bfloat16(), t)
+    refused(ValueError, "t:", x, a, b, s, start, of, None, y, t[:5])
+    refused(TypeError, "float32 or bfloat16", x.double(), a, b, s, start, of, None, y, t)
+    refused(ValueError, "one type", x, a, b.bfloat16(), s, start, of, None, y, t)
+    with pytest.raises(ValueError, match="grad_a"):
+        B.fpq_adapter_backward(x, a, b, s, start, of, t, y, None, x, a[:2], b)

@@ -48,3 +48,19 @@ def test_adamw_step_is_the_textbook_one():
     m2, v2 = 0.9 * m + 0.1 * (g / 2), 0.99 * v + 0.01 * (g / 2) ** 2
     want = p - 0.01 * (0.1 * p + (m2 / (1 - 0.9 ** 7)) / (np.sqrt(v2 / (1 - 0.99 ** 7)) + 1e-6))
     assert np.allclose(m1, m2) and np.allclose(v1, v2) and np.allclose(new, want, rtol=1e-12)
+
+
+def test_adapter_gradient_against_differences():
+    rng = np.random.default_rng(8)
+    starts, of = [1, 4, 4, 9, 11], [2, 0, 0, -1]
+    x, base, gy = rng.standard_normal((12, 6)), rng.standard_normal((12, 5)), rng.standard_normal((12, 5))
+    a, b, s = rng.standard_normal((3, 2, 6)), rng.standard_normal((3, 5, 2)), np.array([0.5, 2.0, 1.5])
+    loss = lambda x, a, b: (adapt.adapter_apply(x, a, b, s, starts, of, base)[0] * gy).sum()
+    grads = adapt.adapter_backward(x, a, b, s, starts, of, gy, np.zeros_like(x))
+    for k, g in enumerate(grads):
+        args = [x, a, b]
+        step, h = rng.standard_normal(args[k].shape), 1e-5
+        up, down = ([v + z * h * step if n == k else v for n, v in enumerate(args)] for z in (1, -1))
+        assert abs((loss(*up) - loss(*down)) / (2 * h) - (g * step).sum()) <= 1e-8 * np.abs(g * step).sum() + 1e-9
+    y, t = adapt.adapter_apply(x, a, b, s, starts, of, base)
+    assert np.array_equal(y[[0, 9, 10, 11]], base[[0, 9, 10, 11]]) and np.all(t[9:] == 0) and np.all(grads[1][1] == 0)
