@@ -35,20 +35,28 @@ int check_attention(const fpq_attention_args_t* p)
 
 AttentionPlan plan_of(const fpq_attention_args_t* p)
 {
-    return plan_attention(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->q_len, p->kv_len, p->type);
+    return plan_attention(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->q_len, p->kv_len);
 }
 
 size_t rows_of(const fpq_attention_args_t* p) { return (size_t)p->batch * p->q_heads * p->q_len; }
 size_t keys_of(const fpq_attention_args_t* p) { return (size_t)p->batch * p->kv_heads * p->kv_len; }
 bool empty(const fpq_attention_args_t* p) { return rows_of(p) == 0; }
 
-Strides strides(const int64_t* s) { return Strides{s[0], s[1], s[2]}; }
+// (a single token's stride says nothing)
+Strides strides(const int64_t* s, int64_t len, int64_t dim) { return Strides{s[0], len <= 1 ? dim : s[1], s[2]}; }
 
 // Every row of [batch, len, heads, dim] starts at a multiple of `to` bytes.
 bool rows_aligned(const void* p, const int64_t* s, int64_t batch, int64_t len, int64_t heads, size_t size, size_t to)
 {
     auto ok = [&](int64_t stride, int64_t n) { return n <= 1 || (stride * (int64_t)size) % (int64_t)to == 0; };
     return aligned(p, to) && ok(s[0], batch) && ok(s[1], len) && ok(s[2], heads);
+}
+
+// Rows that the kernels can take 16 bytes at a time: aligned, whole pieces, one behind the other, and a tile of them within 32-bit
+// offsets.
+bool rows_vec(const void* p, const int64_t* s, int64_t batch, int64_t len, int64_t heads, int64_t dim, size_t size)
+{
+    return rows_aligned(p, s, batch, len, heads, size, 16) && dim * size % 16 == 0 && (len <= 1 || (s[1] >= dim && s[1] < (int64_t)1 << 22));
 }
 
 // A workgroup per block and part: fits a grid's dimension.
@@ -61,10 +69,10 @@ AttentionArgs args_of(const fpq_attention_args_t* p)
 {
     AttentionArgs a{};
     a.lens = p->kv_lens;
-    a.qs = strides(p->q_strides);
-    a.ks = strides(p->k_strides);
-    a.vs = strides(p->v_strides);
-    a.os = strides(p->o_strides);
+    a.qs = strides(p->q_strides, p->q_len, p->head_dim);
+    a.ks = strides(p->k_strides, p->kv_len, p->head_dim);
+    a.vs = strides(p->v_strides, p->kv_len, p->head_dim);
+    a.os = strides(p->o_strides, p->q_len, p->head_dim);
     a.batch = (int)p->batch;
     a.kv_heads = (int)p->kv_heads;
     a.group = (int)(p->q_heads / p->kv_heads);
@@ -314,9 +322,9 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
         a.part = static_cast<float*>(workspace);
         a.part_lse = a.part + align_up(plan.splits * rows_of(p) * p->head_dim * 4) / 4;
     }
-    const bool vec = p->head_dim * size % 16 == 0 && rows_aligned(q, p->q_strides, p->batch, p->q_len, p->q_heads, size, 16) &&
-                     rows_aligned(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, size, 16) &&
-                     rows_aligned(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, size, 16);
+    const bool vec = rows_vec(q, p->q_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
+                     rows_vec(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
+                     rows_vec(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size);
     return launch_attention(a, p->type, vec, plan, static_cast<hipStream_t>(stream));
 }
 
@@ -325,7 +333,7 @@ size_t fpq_attention_backward_workspace_size(const fpq_attention_args_t* p)
     if (check_attention(p) != FPQ_OK) return 0;
     const AttentionPlan plan = plan_of(p);
     const size_t dim = p->head_dim;
-    return align_up(rows_of(p) * 4) + (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
+    return align_up(2 * rows_of(p) * 4) + (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
            (plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * dim * 4) : 0);
 }
 
@@ -356,22 +364,22 @@ int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const v
     a.gk = grad_k;
     a.gv = grad_v;
     a.lse = const_cast<float*>(lse);
-    a.gos = strides(p->grad_o_strides);
-    a.gqs = strides(p->grad_q_strides);
-    a.gks = strides(p->grad_k_strides);
-    a.gvs = strides(p->grad_v_strides);
+    a.gos = strides(p->grad_o_strides, p->q_len, p->head_dim);
+    a.gqs = strides(p->grad_q_strides, p->q_len, p->head_dim);
+    a.gks = strides(p->grad_k_strides, p->kv_len, p->head_dim);
+    a.gvs = strides(p->grad_v_strides, p->kv_len, p->head_dim);
     a.vec_out = p->head_dim % 4 == 0 && rows_aligned(grad_q, p->grad_q_strides, p->batch, p->q_len, p->q_heads, size, 4 * size);
     char* at = static_cast<char*>(workspace);
-    a.delta = reinterpret_cast<float*>(at);
-    at += align_up(rows_of(p) * 4);
+    a.stats = reinterpret_cast<float*>(at);
+    at += align_up(2 * rows_of(p) * 4);
     float* const part_q = reinterpret_cast<float*>(at);
     if (plan.q_splits > 1) at += align_up(plan.q_splits * rows_of(p) * p->head_dim * 4);
     float* const part_kv = reinterpret_cast<float*>(at);
-    const bool vec = p->head_dim * size % 16 == 0 && rows_aligned(q, p->q_strides, p->batch, p->q_len, p->q_heads, size, 16) &&
-                     rows_aligned(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, size, 16) &&
-                     rows_aligned(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, size, 16) &&
-                     rows_aligned(o, p->o_strides, p->batch, p->q_len, p->q_heads, size, 16) &&
-                     rows_aligned(grad_o, p->grad_o_strides, p->batch, p->q_len, p->q_heads, size, 16);
+    const bool vec = rows_vec(q, p->q_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
+                     rows_vec(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
+                     rows_vec(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
+                     rows_vec(o, p->o_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
+                     rows_vec(grad_o, p->grad_o_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size);
     return launch_attention_backward(a, p->type, vec, plan, part_q, part_kv, static_cast<hipStream_t>(stream));
 }
 

@@ -14,6 +14,7 @@
 #pragma once
 #include "fpq_dev.h"
 #include "fpq_host.h"
+#include "lds_dma.h"
 
 namespace fpq {
 
@@ -31,10 +32,12 @@ constexpr float kInf = __builtin_inff();
 template <typename T>
 constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
 
-// Columns of a tile row in LDS for KS steps of 16: whole 32-column output tiles, and 16 bytes that make the row an odd number
-// of 16-byte places, so that the 16 rows of a quarter wave's read start in different banks.
+// Elements of a tile row in LDS for KS steps of 16 columns: 16 bytes more, which make the row an odd number of 16-byte places, so
+// that the 16 rows of a quarter wave's read start in different banks.  Output tiles of 32 columns may reach past a row with an odd
+// KS: those columns of the result are not used, and the tile has kSlack bytes behind it.
 template <int KS>
-constexpr int kRowStride = (KS + 1) / 2 * 32 + 8;
+constexpr int kRowStride = 16 * KS + 8;
+constexpr int kSlack = 64;
 
 template <int NP>
 struct Frag {
@@ -206,6 +209,95 @@ struct Stage {
     }
 };
 
+// Two matrices on their way through LDS, tile by tile of ROWS rows from the same row on.  begin() starts a tile, ready()
+// makes it readable for the whole workgroup.
+//
+// bf16 rows of whole 16-byte pieces go from memory to LDS directly, a tile ahead, into the other one of two buffers: no registers, no
+// instructions per piece, one barrier per tile.  A descriptor per tile bounds the reads, so that rows past the last and columns past
+// the dimension (whose offsets are out of range) become zeros; its base moves in 64 bits, offsets within a tile fit 32.
+// Others pass through registers (fp32: split on the way).
+template <typename T, int KS, bool VEC, int ROWS, int NW, bool DIRECT = (sizeof(T) == 2 && VEC)>
+struct Feed {
+    static constexpr int CHP = 2 * KS + 1, N = (ROWS * CHP + 63) / 64, PW = (N + NW - 1) / NW, TILE = N * 1024, RS = kRowStride<KS>;
+    static constexpr int LDS = 4 * TILE + kSlack;
+    static constexpr bool kDirect = true;
+    unsigned off[2][PW];
+    const T* base[2];
+    int64_t stride[2];
+    unsigned lds;
+    int dim, buf, now;
+    __device__ __forceinline__ void init(unsigned char* at, const T* a, int64_t sa, const T* b, int64_t sb, int dim_)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        base[0] = a;
+        base[1] = b;
+        stride[0] = sa;
+        stride[1] = sb;
+        dim = dim_;
+        buf = 1;
+        lds = lds_address(at);
+#pragma unroll
+        for (int i = 0; i < PW; ++i) {
+            const int q = (wave + NW * i) * 64 + lane, row = q / CHP, c = q - row * CHP;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) off[m][i] = row < ROWS && 8 * c < dim ? (unsigned)row * (unsigned)(2 * stride[m]) + 16u * c : 0x80000000u;
+        }
+    }
+    // rows row0 .. end - 1 of the tile exist (at least one)
+    __device__ __forceinline__ void begin(int row0, int end)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rows = min(ROWS, end - row0);
+        buf ^= 1;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const v4i r = make_rsrc(base[m] + (int64_t)row0 * stride[m], 2u * ((unsigned)(rows - 1) * (unsigned)stride[m] + (unsigned)dim));
+#pragma unroll
+            for (int i = 0; i < PW; ++i)
+                if (wave + NW * i < N) dma16(r, off[m][i], lds + (2 * buf + m) * TILE + (wave + NW * i) * 1024);
+        }
+    }
+    __device__ __forceinline__ void ready(int, int)
+    {
+        dma_barrier();
+        now = buf;
+    }
+    __device__ __forceinline__ int at(int m) const { return (2 * now + m) * (TILE / 2); }      // the readable tile, in elements
+};
+
+template <typename T, int KS, bool VEC, int ROWS, int NW>
+struct Feed<T, KS, VEC, ROWS, NW, false> {
+    static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, TILE = NP * ROWS * RS * 2;
+    static constexpr int LDS = 2 * TILE + kSlack;
+    static constexpr bool kDirect = false;
+    Stage<T, KS, VEC, ROWS, 64 * NW> st[2];
+    const T* base[2];
+    int64_t stride[2];
+    __bf16* tile;
+    int dim;
+    __device__ __forceinline__ void init(unsigned char* at, const T* a, int64_t sa, const T* b, int64_t sb, int dim_)
+    {
+        tile = reinterpret_cast<__bf16*>(at);
+        base[0] = a;
+        base[1] = b;
+        stride[0] = sa;
+        stride[1] = sb;
+        dim = dim_;
+    }
+    __device__ __forceinline__ void begin(int row0, int end)
+    {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) st[m].load(base[m], stride[m], row0, end - 1, dim, threadIdx.x);
+    }
+    __device__ __forceinline__ void ready(int row0, int end)
+    {
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < 2; ++m) st[m].store(tile + m * TILE / 2, row0, end, dim, threadIdx.x);
+        __syncthreads();
+    }
+    __device__ __forceinline__ int at(int m) const { return m * (TILE / 2); }
+};
+
 // Four neighbouring values from column d on; `vec`: the row is aligned for one store.
 __device__ __forceinline__ void store4(float* row, int d, int dim, bool vec, const float (&v)[4])
 {
@@ -236,7 +328,7 @@ struct Strides {
 struct AttentionArgs {
     const void *q, *k, *v, *o, *go;
     void *out, *gq, *gk, *gv;
-    float *lse, *delta;
+    float *lse, *stats;         // stats: per row its log-sum in base 2 (infinity for a row without keys) and its delta
     const int32_t* lens;
     Strides qs, ks, vs, os, gos, gqs, gks, gvs;
     int batch, kv_heads, group, q_len, kv_len, dim, causal;
@@ -248,16 +340,27 @@ struct AttentionArgs {
 };
 
 // The part of the grid that a workgroup works on.  Workgroups go round-robin over the eight XCDs; each XCD takes a contiguous run
-// of them, so that the blocks that read the same keys share an L2.
+// of them, so that the blocks that read the same keys share an L2.  Under `causal` blocks differ in length by up to their number:
+// the longest (number 0) of all heads of an XCD go first.
 struct Place {
     int bh, split, block;
 };
 __device__ __forceinline__ Place place_of(const AttentionArgs& a)
 {
-    const int total = gridDim.x, per = total >> 3;
+    const int total = gridDim.x, per = total >> 3, bhs = a.batch * a.kv_heads;
     int id = blockIdx.x;
-    if (id < (per << 3)) id = (id & 7) * per + (id >> 3);
     Place p;
+    if (a.causal) {
+        const bool whole = (bhs & 7) == 0;
+        const int local = whole ? bhs >> 3 : bhs;
+        if (whole) id >>= 3;
+        p.split = id % a.splits;
+        id /= a.splits;
+        p.bh = id % local + (whole ? (int)(blockIdx.x & 7) * local : 0);
+        p.block = id / local;
+        return p;
+    }
+    if (id < (per << 3)) id = (id & 7) * per + (id >> 3);
     p.block = id % a.blocks;
     id /= a.blocks;
     p.split = id % a.splits;
@@ -287,9 +390,7 @@ __device__ __forceinline__ RowRange visible(const AttentionArgs& a, int n, int f
     return v;
 }
 
-// Queries of a tile of the backward pass's keys kernel (host and device).
-template <typename T>
-constexpr int KeysTile = kPlanes<T> == 3 ? 32 : 64;
+constexpr int KeysTile = 32;    // queries of a tile of the backward pass's keys kernel (host and device)
 
 // How a call's kernels are chosen and cut (host): by sizes, type and alignment only, the same for the size of the workspace.
 struct AttentionPlan {
@@ -301,6 +402,6 @@ struct AttentionPlan {
 
 int launch_attention(const AttentionArgs& a, int type, bool vec, const AttentionPlan& p, hipStream_t s);
 int launch_attention_backward(const AttentionArgs& a, int type, bool vec, const AttentionPlan& p, float* part_q, float* part_kv, hipStream_t s);
-AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int type);
+AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len);
 
 }  // namespace fpq

@@ -12,21 +12,20 @@
 
 namespace fpq {
 
-template <typename T, int KS>
+template <typename T, int KS, bool VEC>
 struct QueriesShape {
-    static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2, NW = 4;
-    static constexpr int KT = NP == 3 ? 32 : 64;
-    static constexpr int LDS = 2 * NP * KT * RS * 2;
+    static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2;
+    static constexpr int KT = NP == 3 || KS > 8 ? 32 : 64;
+    typedef Feed<T, KS, VEC, KT, 4> Tiles;
+    static constexpr int LDS = Tiles::LDS;
 };
 
 template <typename T, int KS, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_queries_kernel(AttentionArgs a)
 {
-    typedef QueriesShape<T, KS> Sh;
-    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, KT = Sh::KT, NT = 256;
+    typedef QueriesShape<T, KS, VEC> Sh;
+    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, KT = Sh::KT;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    __bf16* const kt = reinterpret_cast<__bf16*>(lds);
-    __bf16* const vt = kt + NP * KT * RS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const Place at = place_of(a);
     const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
@@ -58,29 +57,25 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
         }
         delta += __shfl_xor(delta, 32);
     }
-    if (r < rows && h == 0 && at.split == 0) a.delta[row_id] = delta;
     const float log_sum = a.lse[row_id];
     const float c = a.scale * kLog2e, lse2 = log_sum == -kInf ? kInf : log_sum * kLog2e;   // a row without keys: every p is 0
+    if (r < rows && h == 0 && at.split == 0) {
+        reinterpret_cast<float2*>(a.stats)[row_id] = make_float2(lse2, delta);
+    }
 
     const T* const kbase = static_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
     const T* const vbase = static_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
     v16f acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = zero16();
-    Stage<T, KS, VEC, KT, NT> sk, sv;
-    if (kbeg < kend) {
-        sk.load(kbase, a.ks.t, kbeg, kend - 1, a.dim, tid);
-        sv.load(vbase, a.vs.t, kbeg, kend - 1, a.dim, tid);
-    }
+    typename Sh::Tiles feed;
+    feed.init(lds, kbase, a.ks.t, vbase, a.vs.t, a.dim);
+    if (kbeg < kend) feed.begin(kbeg, kend);
     for (int j0 = kbeg; j0 < kend; j0 += KT) {
-        __syncthreads();
-        sk.store(kt, j0, kend, a.dim, tid);
-        sv.store(vt, j0, kend, a.dim, tid);
-        __syncthreads();
-        if (j0 + KT < kend) {
-            sk.load(kbase, a.ks.t, j0 + KT, kend - 1, a.dim, tid);
-            sv.load(vbase, a.vs.t, j0 + KT, kend - 1, a.dim, tid);
-        }
+        feed.ready(j0, kend);
+        const __bf16* const kt = reinterpret_cast<const __bf16*>(lds) + feed.at(0);
+        const __bf16* const vt = reinterpret_cast<const __bf16*>(lds) + feed.at(1);
+        if (j0 + KT < kend) feed.begin(j0 + KT, kend);
         const bool masked = j0 + KT > min(range.lo, kend);
 #pragma unroll
         for (int u = 0; u < KT / 32; ++u) {
@@ -126,23 +121,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
 
 // WHAT: 1 dv, 2 dk, 3 both in one pass.  In fp32 at the largest dimension the planes of 32 keys and values and both sums do not fit
 // a wavefront's registers together: two passes.
-template <typename T, int KS>
+template <typename T, int KS, bool VEC>
 struct KeysShape {
     static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2;
-    static constexpr int QT = KeysTile<T>;
-    static constexpr int LDS = 2 * NP * QT * RS * 2 + 2 * QT * 4;
+    static constexpr int QT = KeysTile;
+    typedef Feed<T, KS, VEC, QT, 4> Tiles;
+    static constexpr int STATS = (Tiles::LDS + 15) / 16 * 16;          // two buffers of the rows' pairs of log-sum and delta
+    static constexpr int LDS = STATS + 2 * QT * 8;
+    static_assert(QT == 32, "the pairs of a tile are one load of four bytes per lane");
 };
 
 template <typename T, int KS, bool VEC, int WHAT>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 6 ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
+__global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
 {
-    typedef KeysShape<T, KS> Sh;
-    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, QT = Sh::QT, NT = 256;
+    typedef KeysShape<T, KS, VEC> Sh;
+    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, QT = Sh::QT;
     constexpr bool DV = WHAT & 1, DK = WHAT & 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    __bf16* const qt = reinterpret_cast<__bf16*>(lds);
-    __bf16* const gt = qt + NP * QT * RS;
-    float* const ls = reinterpret_cast<float*>(gt + NP * QT * RS);             // [QT] log-sums in base 2, [QT] deltas
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const Place at = place_of(a);
     const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
@@ -178,30 +173,38 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 6 ? 2 : 1) void
         if constexpr (DK) ak[d] = zero16();
     }
     const float c = a.scale * kLog2e;
-    Stage<T, KS, VEC, QT, NT> sq, sg;
-    float stat = 0.0f;                             // log-sum (first QT threads) or delta (the next QT) of a row of the tile
-    auto load = [&](int64_t t) {
-        const int g = (int)(t / per_head), i0 = (skip + (int)(t - (int64_t)g * per_head)) * QT, head = hk * a.group + g;
-        sq.load(static_cast<const T*>(a.q) + b * a.qs.b + head * a.qs.h, a.qs.t, i0, a.q_len - 1, a.dim, tid);
-        sg.load(static_cast<const T*>(a.go) + b * a.gos.b + head * a.gos.h, a.gos.t, i0, a.q_len - 1, a.dim, tid);
-        if (tid < 2 * QT) {
-            const int i = i0 + (tid & (QT - 1));
-            const size_t id = ((size_t)at.bh * a.group + g) * a.q_len + min(i, a.q_len - 1);
-            const float x = tid < QT ? a.lse[id] : a.delta[id];
-            stat = tid < QT ? (i >= a.q_len || x == -kInf ? kInf : x * kLog2e) : x;         // rows that are none: p = 0
-            if (tid >= QT && i >= a.q_len) stat = 0.0f;
-        }
+    const int per = max(per_head, 1);
+    typename Sh::Tiles feed;
+    int g = (int)(tbeg / per), i0 = (skip + (int)(tbeg - (int64_t)g * per)) * QT, slot = 0;
+    // rows past the last get zeros, and so p = 1 next to zeros of q and do
+    auto begin = [&](int g, int i0) {
+        feed.begin(i0, a.q_len);
+        if (wave == 0)
+            dma4(make_rsrc(a.stats + 2 * (((size_t)at.bh * a.group + g) * a.q_len + i0), 8u * (unsigned)min(QT, a.q_len - i0)), 4u * lane,
+                 lds_address(lds) + Sh::STATS + slot * QT * 8);
+        slot ^= 1;
     };
-    if (tbeg < tend) load(tbeg);
+    feed.init(lds, static_cast<const T*>(a.q) + b * a.qs.b + (hk * a.group + g) * a.qs.h, a.qs.t,
+              static_cast<const T*>(a.go) + b * a.gos.b + (hk * a.group + g) * a.gos.h, a.gos.t, a.dim);
+    if (tbeg < tend) begin(g, i0);
     for (int64_t t = tbeg; t < tend; ++t) {
-        const int g = (int)(t / per_head), i0 = (skip + (int)(t - (int64_t)g * per_head)) * QT;
-        __syncthreads();
-        sq.store(qt, i0, a.q_len, a.dim, tid);
-        sg.store(gt, i0, a.q_len, a.dim, tid);
-        if (tid < 2 * QT) ls[tid] = stat;
-        __syncthreads();
-        if (t + 1 < tend) load(t + 1);
-        const bool masked = a.causal && j_first + 127 > i0 + off;
+        feed.ready(i0, a.q_len);
+        if constexpr (!Sh::Tiles::kDirect) dma_barrier();              // (the statistics)
+        const __bf16* const qt = reinterpret_cast<const __bf16*>(lds) + feed.at(0);
+        const __bf16* const gt = reinterpret_cast<const __bf16*>(lds) + feed.at(1);
+        const float* const ls = reinterpret_cast<const float*>(lds + Sh::STATS) + (slot ^ 1) * 2 * QT;
+        const int i_now = i0;
+        if (t + 1 < tend) {
+            i0 += QT;
+            if (i0 >= a.q_len) {                   // the next head of the group
+                i0 = skip * QT;
+                ++g;
+                feed.base[0] += a.qs.h;
+                feed.base[1] += a.gos.h;
+            }
+            begin(g, i0);
+        }
+        const bool masked = a.causal && j_first + 127 > i_now + off;
 #pragma unroll
         for (int u = 0; u < QT / 32; ++u) {
             v16f s = zero16(), dp = zero16();
@@ -211,24 +214,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 6 ? 2 : 1) void
                 if constexpr (DK) mma<NP>(dp, row_frag<NP, RS, QT>(gt, 32 * u + l32, 16 * x + 8 * h), vf[x]);
             }
             if (masked) {
-                const int from = key - off - i0 - 32 * u;      // the first query that sees the key
+                const int from = key - off - i_now - 32 * u;      // the first query that sees the key
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (8 * (e / 4) + 4 * h + e % 4 < from) s[e] = -kInf;
             }
-            float4 lse[4], delta[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                lse[e] = *reinterpret_cast<const float4*>(ls + 32 * u + 8 * e + 4 * h);
-                if constexpr (DK) delta[e] = *reinterpret_cast<const float4*>(ls + QT + 32 * u + 8 * e + 4 * h);
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float* y = reinterpret_cast<const float*>(&lse[e / 4]);
-                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -y[e % 4]));
+            for (int e = 0; e < 16; e += 2) {      // two rows' pairs at a time
+                const float4 y = *reinterpret_cast<const float4*>(ls + 2 * (32 * u + 8 * (e / 4) + 4 * h + e % 4));
+                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -y.x));
+                s[e + 1] = __builtin_amdgcn_exp2f(fmaf(s[e + 1], c, -y.z));
                 if constexpr (DK) {
-                    const float* z = reinterpret_cast<const float*>(&delta[e / 4]);
-                    dp[e] = s[e] * (dp[e] - z[e % 4]);
+                    dp[e] = s[e] * (dp[e] - y.y);
+                    dp[e + 1] = s[e + 1] * (dp[e + 1] - y.w);
                 }
             }
 #pragma unroll
@@ -305,7 +303,7 @@ int launch_sum(const float* part, int parts, size_t part_stride, size_t rows, in
 template <typename T, int KS, bool VEC>
 int launch_queries(const AttentionArgs& a, hipStream_t s)
 {
-    typedef QueriesShape<T, KS> Sh;
+    typedef QueriesShape<T, KS, VEC> Sh;
     static std::atomic<uint64_t> done{0};
     if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_queries_kernel<T, KS, VEC>), Sh::LDS, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
@@ -316,7 +314,7 @@ int launch_queries(const AttentionArgs& a, hipStream_t s)
 template <typename T, int KS, bool VEC, int WHAT>
 int launch_keys(const AttentionArgs& a, hipStream_t s)
 {
-    typedef KeysShape<T, KS> Sh;
+    typedef KeysShape<T, KS, VEC> Sh;
     static std::atomic<uint64_t> done{0};
     if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_kernel<T, KS, VEC, WHAT>), Sh::LDS, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;

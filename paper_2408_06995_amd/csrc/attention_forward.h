@@ -1,5 +1,5 @@
-// Attention, forward: o = softmax(scale q k^T) v in one pass over the keys, with the running maximum m and sum l of a row's
-// exponentials (o and l are rescaled when m grows).  m, l and o are held in 32 bits; the probabilities are rounded to the
+// Attention, forward: o = softmax(scale q k^T) v in one pass over the keys, with the running maximum m (a lower bound
+// of it, within 2^8 after the exponential) and sum l of a row's exponentials; o and l are rescaled when m grows.  m, l and o are held in 32 bits; the probabilities are rounded to the
 // operand's planes (8 bits for bf16 results, 24 for fp32) where they enter the second product.
 //
 // A wavefront has 32 rows of queries in registers and takes S^T = K Q^T per 32 keys, so that a lane holds 16 scores of one row and
@@ -12,26 +12,25 @@
 
 namespace fpq {
 
-template <typename T, int KS, bool KEYS>
+template <typename T, int KS, bool VEC, bool KEYS>
 struct ForwardShape {
     static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2;
     static constexpr int NW = KEYS && NP == 3 ? 2 : 4;
-    static constexpr int KT = KEYS ? 32 * NW : NP == 3 ? 32 : 64;
-    static constexpr int TILES = 2 * NP * KT * RS * 2;
+    static constexpr int KT = KEYS ? 32 * NW : NP == 3 || KS > 8 ? 32 : 64;
+    typedef Feed<T, KS, VEC, KT, NW, sizeof(T) == 2 && VEC && !KEYS> Tiles;
+    static constexpr int TILES = Tiles::LDS;
     static constexpr int JOIN = KEYS ? (2 * NW * 32 + 32 + NW * DT * 32 * 33) * 4 : 0;
     static constexpr int LDS = TILES > JOIN ? TILES : JOIN;
     static constexpr bool AHEAD = !(KEYS && NP == 3);     // a tile waits in registers while the one before is multiplied
 };
 
 template <typename T, int KS, bool VEC, bool KEYS>
-__global__ __launch_bounds__((64 * ForwardShape<T, KS, KEYS>::NW), sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_kernel(AttentionArgs a)
+__global__ __launch_bounds__((64 * ForwardShape<T, KS, VEC, KEYS>::NW), sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_kernel(AttentionArgs a)
 {
-    typedef ForwardShape<T, KS, KEYS> Sh;
+    typedef ForwardShape<T, KS, VEC, KEYS> Sh;
     constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, NW = Sh::NW, KT = Sh::KT, NT = 64 * NW, NS = KEYS ? 1 : KT / 32;
     constexpr int RB = KEYS ? 32 : 32 * NW;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    __bf16* const kt = reinterpret_cast<__bf16*>(lds);
-    __bf16* const vt = kt + NP * KT * RS;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const Place at = place_of(a);
     const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
@@ -59,26 +58,20 @@ __global__ __launch_bounds__((64 * ForwardShape<T, KS, KEYS>::NW), sizeof(T) == 
     v16f acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = zero16();
-    const float c = a.scale * kLog2e;
+    const float c = a.scale * kLog2e, slack = 8.0f / c;
     float m = -kInf, l = 0.0f;                     // of the raw scores; l over this lane's keys only
-    Stage<T, KS, VEC, KT, NT> sk, sv;
-    if (Sh::AHEAD && kbeg < kend) {
-        sk.load(kbase, a.ks.t, kbeg, kend - 1, a.dim, tid);
-        sv.load(vbase, a.vs.t, kbeg, kend - 1, a.dim, tid);
-    }
+    typename Sh::Tiles feed;
+    feed.init(lds, kbase, a.ks.t, vbase, a.vs.t, a.dim);
+    if (Sh::AHEAD && kbeg < kend) feed.begin(kbeg, kend);
     for (int j0 = kbeg; j0 < kend; j0 += KT) {
-        __syncthreads();
         if (!Sh::AHEAD) {
-            sk.load(kbase, a.ks.t, j0, kend - 1, a.dim, tid);
-            sv.load(vbase, a.vs.t, j0, kend - 1, a.dim, tid);
+            __syncthreads();
+            feed.begin(j0, kend);
         }
-        sk.store(kt, j0, kend, a.dim, tid);
-        sv.store(vt, j0, kend, a.dim, tid);
-        __syncthreads();
-        if (Sh::AHEAD && j0 + KT < kend) {
-            sk.load(kbase, a.ks.t, j0 + KT, kend - 1, a.dim, tid);
-            sv.load(vbase, a.vs.t, j0 + KT, kend - 1, a.dim, tid);
-        }
+        feed.ready(j0, kend);
+        const __bf16* const kt = reinterpret_cast<const __bf16*>(lds) + feed.at(0);
+        const __bf16* const vt = reinterpret_cast<const __bf16*>(lds) + feed.at(1);
+        if (Sh::AHEAD && j0 + KT < kend) feed.begin(j0 + KT, kend);
         const int sub0 = KEYS ? 32 * wave : 0;
         v16f s[NS];
 #pragma unroll
@@ -101,7 +94,9 @@ __global__ __launch_bounds__((64 * ForwardShape<T, KS, KEYS>::NW), sizeof(T) == 
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
         top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > m)) {
+        // m follows the maximum only when it lags by more than a factor of 2^8: until then exponentials are up to 2^8, which
+        // neither the sums nor the operands notice, and o and l need no rescaling.
+        if (__any(top > m + slack)) {
             const float next = fmaxf(m, top), by = m == next ? 1.0f : __builtin_amdgcn_exp2f((m - next) * c);
             m = next;
             l *= by;
@@ -229,7 +224,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
 template <typename T, int KS, bool VEC, bool KEYS>
 int launch_forward(const AttentionArgs& a, hipStream_t s)
 {
-    typedef ForwardShape<T, KS, KEYS> Sh;
+    typedef ForwardShape<T, KS, VEC, KEYS> Sh;
     static std::atomic<uint64_t> done{0};
     const void* kernel = reinterpret_cast<const void*>(&attention_kernel<T, KS, VEC, KEYS>);
     if (!allow_dynamic_lds(kernel, Sh::LDS, done)) return FPQ_ERR_LAUNCH;

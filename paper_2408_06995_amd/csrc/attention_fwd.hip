@@ -14,7 +14,7 @@ static int parts(int64_t have, int64_t units, int64_t least, int64_t want)
     return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
 
-AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int type)
+AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len)
 {
     AttentionPlan p;
     const int64_t bh = batch * kv_heads, rows = group * q_len;
@@ -32,8 +32,8 @@ AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int
     p.q_blocks = (int)wide;
     fit(kv_len, bh * p.q_blocks, 64, 256, &p.q_splits, &p.q_per_split);
     p.k_blocks = (int)((kv_len + 127) / 128);
-    const int64_t tile = type == FPQ_TYPE_FP32 ? KeysTile<float> : KeysTile<__bf16>, tiles = group * ((q_len + tile - 1) / tile);
-    fit(tiles, bh * p.k_blocks, 1, 2, &p.k_splits, &p.k_per_split);
+    const int64_t tiles = group * ((q_len + KeysTile - 1) / KeysTile);
+    fit(tiles, bh * p.k_blocks, 1, 4, &p.k_splits, &p.k_per_split);
     return p;
 }
 

@@ -28,23 +28,9 @@
 #include <type_traits>
 
 #include "gemm_common.h"
+#include "lds_dma.h"
 
 namespace fpq {
-
-typedef int v4i __attribute__((ext_vector_type(4)));
-
-// One wave-wide 16-byte-per-lane load from a buffer straight into LDS: lane i's bytes land at
-// lds_addr + 16 i; a lane whose voff is not below the buffer's size gets zeros.  Written as inline
-// assembly so that the compiler's wait-count insertion does not see an LDS write here (it would
-// drain every outstanding load before each following LDS read); the waits are placed by hand in
-// the main loop.  m0 carries the LDS base; nothing else in these kernels uses m0.
-__device__ __forceinline__ void dma16(v4i rsrc, unsigned voff, unsigned lds_addr)
-{
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 :
-                 : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(rsrc)   // uniform, but may live in a VGPR
-                 : "memory");
-}
 
 // The same for a wavefront that may have nothing left to load: live = -1, or 1, and then the first lane takes part alone.  That load
 // counts in vmcnt like any other (whether one without lanes would is not relied on), so the waits stay as they are, and it moves 16
@@ -60,22 +46,6 @@ __device__ __forceinline__ void dma16_live(v4i rsrc, unsigned voff, unsigned lds
                    "s"(__builtin_amdgcn_readfirstlane(live >> 1))
                  : "memory");
 }
-
-// Raw buffer descriptor: base address, no stride, size in bytes, 32-bit untyped data.
-__device__ __forceinline__ v4i make_rsrc(const void* base, unsigned bytes)
-{
-    const unsigned long long b = reinterpret_cast<unsigned long long>(base);
-    v4i r;
-    r.x = (int)(unsigned)b;
-    r.y = (int)((unsigned)(b >> 32) & 0xffffu);
-    r.z = (int)bytes;
-    r.w = 0x00020000;
-    return r;
-}
-
-// s_waitcnt immediate that waits for vmcnt <= n only (gfx9 encoding: vmcnt in bits 3:0 and 15:14,
-// expcnt 6:4 and lgkmcnt 11:8 left at their maxima).
-constexpr int vmcnt_imm(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));   // a 16-byte store at any 4-byte address
