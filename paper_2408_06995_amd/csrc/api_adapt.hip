@@ -35,12 +35,12 @@ int check_attention(const fpq_attention_args_t* p)
 
 AttentionPlan plan_of(const fpq_attention_args_t* p)
 {
-    return plan_attention(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->q_len, p->kv_len);
+    return plan_attention(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->q_len, p->kv_len, p->head_dim, p->type);
 }
 
 size_t rows_of(const fpq_attention_args_t* p) { return (size_t)p->batch * p->q_heads * p->q_len; }
 size_t keys_of(const fpq_attention_args_t* p) { return (size_t)p->batch * p->kv_heads * p->kv_len; }
-bool empty(const fpq_attention_args_t* p) { return rows_of(p) == 0; }
+bool no_rows(const fpq_attention_args_t* p) { return rows_of(p) == 0; }
 
 // (a single token's stride says nothing)
 Strides strides(const int64_t* s, int64_t len, int64_t dim) { return Strides{s[0], len <= 1 ? dim : s[1], s[2]}; }
@@ -82,6 +82,33 @@ AttentionArgs args_of(const fpq_attention_args_t* p)
     a.causal = p->causal;
     a.scale = p->scale;
     return a;
+}
+
+// Room for the planes of `rows` packed rows of a tensor.
+size_t planes_size(const fpq_attention_args_t* p, size_t rows)
+{
+    return align_up(rows * ((p->head_dim + 7) / 8 * 8) * 2 * (p->type == FPQ_TYPE_FP32 ? 3 : 1));
+}
+
+PackArgs pack_args(const fpq_attention_args_t* p)
+{
+    PackArgs a{};
+    a.batch = (int)p->batch;
+    a.kv_len = (int)p->kv_len;
+    a.dim = (int)p->head_dim;
+    a.lens = p->kv_lens;
+    return a;
+}
+
+// How the feed reads a tensor: as it is, or packed at `at` by the call's packing launch.
+Source source(PackArgs& pack, const fpq_attention_args_t* p, const void* t, const int64_t* s, int64_t len, int64_t heads, bool keys, char*& at)
+{
+    const Strides st = strides(s, len, p->head_dim);
+    if (p->type == FPQ_TYPE_BF16 && rows_vec(t, s, p->batch, len, heads, p->head_dim, 2)) return Source{static_cast<const __bf16*>(t), st, 0};
+    Pack& m = pack.m[pack.count++];
+    m = Pack{t, st, reinterpret_cast<__bf16*>(at), (int)heads, (int)len, keys};
+    at += planes_size(p, (size_t)p->batch * len * heads);
+    return packed_source(m, p->batch, p->head_dim);
 }
 
 // FPQ_OK and the pieces of all tensors
@@ -287,10 +314,11 @@ int fpq_adamw_step(const void* plan, int64_t pieces, double lr, double beta1, do
 
 size_t fpq_attention_workspace_size(const fpq_attention_args_t* p)
 {
-    if (check_attention(p) != FPQ_OK || empty(p)) return 0;
+    if (check_attention(p) != FPQ_OK || no_rows(p)) return 0;
     const AttentionPlan plan = plan_of(p);
     const size_t rows = rows_of(p);
-    return plan.splits > 1 ? align_up(plan.splits * rows * p->head_dim * 4) + align_up(plan.splits * rows * 4) : 0;
+    return (plan.splits > 1 ? align_up(plan.splits * rows * p->head_dim * 4) + align_up(plan.splits * rows * 4) : 0) +
+           (plan.by_keys ? 0 : 2 * planes_size(p, keys_of(p)));
 }
 
 int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* workspace,
@@ -298,7 +326,7 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
 {
     const int st = check_attention(p);
     if (st != FPQ_OK) return st;
-    if (empty(p)) return FPQ_OK;
+    if (no_rows(p)) return FPQ_OK;
     if (!q || !o || (p->kv_len && (!k || !v))) return FPQ_ERR_NULL;
     const size_t size = size_of(p->type);
     if (!aligned(q, size) || !aligned(k, size) || !aligned(v, size) || !aligned(o, size) || !aligned(lse, 4) || !aligned(p->kv_lens, 4))
@@ -318,14 +346,24 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
     a.splits = plan.splits;
     a.per_split = plan.per_split;
     a.vec_out = p->head_dim % 4 == 0 && rows_aligned(o, p->o_strides, p->batch, p->q_len, p->q_heads, size, 4 * size);
+    a.vec = rows_vec(q, p->q_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
+            rows_vec(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
+            rows_vec(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size);
+    char* at = static_cast<char*>(workspace);
     if (plan.splits > 1) {
-        a.part = static_cast<float*>(workspace);
-        a.part_lse = a.part + align_up(plan.splits * rows_of(p) * p->head_dim * 4) / 4;
+        a.part = reinterpret_cast<float*>(at);
+        at += align_up(plan.splits * rows_of(p) * p->head_dim * 4);
+        a.part_lse = reinterpret_cast<float*>(at);
+        at += align_up(plan.splits * rows_of(p) * 4);
     }
-    const bool vec = rows_vec(q, p->q_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
-                     rows_vec(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
-                     rows_vec(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size);
-    return launch_attention(a, p->type, vec, plan, static_cast<hipStream_t>(stream));
+    if (!plan.by_keys) {
+        PackArgs pack = pack_args(p);
+        a.fk = source(pack, p, k, p->k_strides, p->kv_len, p->kv_heads, true, at);
+        a.fv = source(pack, p, v, p->v_strides, p->kv_len, p->kv_heads, true, at);
+        const int packed = launch_pack(pack, p->type, static_cast<hipStream_t>(stream));
+        if (packed != FPQ_OK) return packed;
+    }
+    return launch_attention(a, p->type, plan, static_cast<hipStream_t>(stream));
 }
 
 size_t fpq_attention_backward_workspace_size(const fpq_attention_args_t* p)
@@ -333,8 +371,9 @@ size_t fpq_attention_backward_workspace_size(const fpq_attention_args_t* p)
     if (check_attention(p) != FPQ_OK) return 0;
     const AttentionPlan plan = plan_of(p);
     const size_t dim = p->head_dim;
-    return align_up(2 * rows_of(p) * 4) + (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
-           (plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * dim * 4) : 0);
+    return align_up(rows_of(p) * 8) + (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
+           (plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * dim * 4) : 0) + 2 * planes_size(p, keys_of(p)) +
+           2 * planes_size(p, rows_of(p));
 }
 
 int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -369,18 +408,26 @@ int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const v
     a.gks = strides(p->grad_k_strides, p->kv_len, p->head_dim);
     a.gvs = strides(p->grad_v_strides, p->kv_len, p->head_dim);
     a.vec_out = p->head_dim % 4 == 0 && rows_aligned(grad_q, p->grad_q_strides, p->batch, p->q_len, p->q_heads, size, 4 * size);
+    a.vec = rows_vec(q, p->q_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
+            rows_vec(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
+            rows_vec(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
+            rows_vec(o, p->o_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
+            rows_vec(grad_o, p->grad_o_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size);
     char* at = static_cast<char*>(workspace);
     a.stats = reinterpret_cast<float*>(at);
-    at += align_up(2 * rows_of(p) * 4);
+    at += align_up(rows_of(p) * 8);
     float* const part_q = reinterpret_cast<float*>(at);
     if (plan.q_splits > 1) at += align_up(plan.q_splits * rows_of(p) * p->head_dim * 4);
     float* const part_kv = reinterpret_cast<float*>(at);
-    const bool vec = rows_vec(q, p->q_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
-                     rows_vec(k, p->k_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
-                     rows_vec(v, p->v_strides, p->batch, p->kv_len, p->kv_heads, p->head_dim, size) &&
-                     rows_vec(o, p->o_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&
-                     rows_vec(grad_o, p->grad_o_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size);
-    return launch_attention_backward(a, p->type, vec, plan, part_q, part_kv, static_cast<hipStream_t>(stream));
+    if (plan.k_splits > 1) at += align_up(2 * plan.k_splits * keys_of(p) * p->head_dim * 4);
+    PackArgs pack = pack_args(p);
+    a.fk = source(pack, p, k, p->k_strides, p->kv_len, p->kv_heads, true, at);
+    a.fv = source(pack, p, v, p->v_strides, p->kv_len, p->kv_heads, true, at);
+    a.fq = source(pack, p, q, p->q_strides, p->q_len, p->q_heads, false, at);
+    a.fgo = source(pack, p, grad_o, p->grad_o_strides, p->q_len, p->q_heads, false, at);
+    const int packed = launch_pack(pack, p->type, static_cast<hipStream_t>(stream));
+    if (packed != FPQ_OK) return packed;
+    return launch_attention_backward(a, p->type, plan, part_q, part_kv, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

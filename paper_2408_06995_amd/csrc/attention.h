@@ -130,6 +130,15 @@ __device__ __forceinline__ void row8(const T* row, int col, int dim, float (&v)[
     }
 }
 
+template <typename T>
+__device__ __forceinline__ void row8(const T* row, int col, int dim, int vec, float (&v)[8])
+{
+    if (vec)
+        row8<T, true>(row, col, dim, v);
+    else
+        row8<T, false>(row, col, dim, v);
+}
+
 // Operand rows from LDS: lane r's row, eight columns.
 template <int NP, int RS, int ROWS>
 __device__ __forceinline__ Frag<NP> row_frag(const __bf16* tile, int row, int col)
@@ -209,93 +218,117 @@ struct Stage {
     }
 };
 
-// Two matrices on their way through LDS, tile by tile of ROWS rows from the same row on.  begin() starts a tile, ready()
-// makes it readable for the whole workgroup.
-//
-// bf16 rows of whole 16-byte pieces go from memory to LDS directly, a tile ahead, into the other one of two buffers: no registers, no
-// instructions per piece, one barrier per tile.  A descriptor per tile bounds the reads, so that rows past the last and columns past
-// the dimension (whose offsets are out of range) become zeros; its base moves in 64 bits, offsets within a tile fit 32.
-// Others pass through registers (fp32: split on the way).
-template <typename T, int KS, bool VEC, int ROWS, int NW, bool DIRECT = (sizeof(T) == 2 && VEC)>
+// Strides in elements: sample, token, head.
+struct Strides {
+    int64_t b, t, h;
+};
+
+// A matrix as the feed reads it: NP planes of bf16 rows of whole 16-byte pieces.  bf16 tensors with such rows are read where they
+// are; others are packed first (attention_pack.hip).
+struct Source {
+    const __bf16* p;
+    Strides s;                  // in elements
+    int64_t plane;              // from one plane to the next
+};
+
+// LDS tiles of the feed: a row has CS places of 16 bytes, and place c ^ swap(row) holds piece c, so that neither kind of read
+// meets a bank twice: 16 rows of one piece (operand rows) start in the 16 different groups of four banks, and so do four rows of
+// four pieces (transposed reads, half a wavefront at a time).
+template <int KS>
+struct Places {
+    static constexpr int CS = KS <= 4 ? 8 : KS <= 6 ? 12 : KS <= 8 ? 16 : 20, RS = 8 * CS, DT = (KS + 1) / 2;
+    static __device__ __forceinline__ int swap(int row)
+    {
+        if (CS == 8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+        if (CS == 16) return (row & 3) << 2 | ((row >> 2) & 3);
+        return (row >> 2) & 3;
+    }
+    int row[KS];                // of this lane, in elements: its row (lane % 32), step t
+    int col[DT][2];             // its part of a transposed read: output columns 32 d, rows 0 .. 3 and 8 .. 11 (+ 4 h)
+    __device__ __forceinline__ void init(int lane)
+    {
+        const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+        for (int t = 0; t < KS; ++t) row[t] = r * RS + 8 * ((2 * t + h) ^ swap(r));
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int q = 4 * h + ((lane & 15) >> 2) + 8 * e, c = 4 * d + ((lane & 16) >> 3) + ((lane & 3) >> 1);
+                col[d][e] = q * RS + 8 * (c ^ swap(q)) + 4 * (lane & 1);
+            }
+    }
+};
+
+// Operand rows 32 u + lane % 32, step t, and operand columns 32 d + lane % 32 of the rows r0 .. r0 + 15 (r0 a multiple of 16), of a
+// tile whose planes are `plane` elements apart.
+template <int NP, int KS>
+__device__ __forceinline__ Frag<NP> rows_at(const __bf16* tile, int plane, const Places<KS>& at, int u, int t)
+{
+    Frag<NP> f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) f.p[p] = *reinterpret_cast<const v8bf*>(tile + p * plane + 32 * u * Places<KS>::RS + at.row[t]);
+    return f;
+}
+template <int NP, int KS>
+__device__ __forceinline__ Frag<NP> cols_at(const __bf16* tile, int plane, const Places<KS>& at, int r0, int d)
+{
+    Frag<NP> f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(tile + p * plane + r0 * Places<KS>::RS + at.col[d][0]));
+        const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(tile + p * plane + r0 * Places<KS>::RS + at.col[d][1]));
+        f.p[p] = __builtin_bit_cast(v8bf, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    return f;
+}
+
+// M matrices from memory to LDS, tile by tile of ROWS rows, a tile ahead, into the other one of two buffers: no registers, no
+// instructions per piece, one barrier per tile.  A descriptor per tile bounds the reads, so that rows past the last and columns
+// past the dimension (whose offsets are out of range) become zeros; its base moves in 64 bits, offsets within a tile fit 32.
+// begin() starts a tile, ready() makes the one begun last readable for the whole workgroup.
+template <int NP, int KS, int ROWS, int M>
 struct Feed {
-    static constexpr int CHP = 2 * KS + 1, N = (ROWS * CHP + 63) / 64, PW = (N + NW - 1) / NW, TILE = N * 1024, RS = kRowStride<KS>;
-    static constexpr int LDS = 4 * TILE + kSlack;
-    static constexpr bool kDirect = true;
-    unsigned off[2][PW];
-    const T* base[2];
-    int64_t stride[2];
+    static constexpr int CS = Places<KS>::CS, N = ROWS * CS / 64, PW = (N + 3) / 4, PLANE = ROWS * CS * 16, TILE = NP * PLANE, LDS = 2 * M * TILE;
+    unsigned off[M][PW];
+    Source src[M];              // p: of row 0 of the head
     unsigned lds;
-    int dim, buf, now;
-    __device__ __forceinline__ void init(unsigned char* at, const T* a, int64_t sa, const T* b, int64_t sb, int dim_)
+    int buf, now, cols;         // cols: columns that exist, in whole pieces
+    __device__ __forceinline__ void init(unsigned lds_at, int dim)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        base[0] = a;
-        base[1] = b;
-        stride[0] = sa;
-        stride[1] = sb;
-        dim = dim_;
         buf = 1;
-        lds = lds_address(at);
+        lds = lds_at;
+        cols = (dim + 7) / 8 * 8;
 #pragma unroll
         for (int i = 0; i < PW; ++i) {
-            const int q = (wave + NW * i) * 64 + lane, row = q / CHP, c = q - row * CHP;
+            const int q = (wave + 4 * i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ Places<KS>::swap(row);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) off[m][i] = row < ROWS && 8 * c < dim ? (unsigned)row * (unsigned)(2 * stride[m]) + 16u * c : 0x80000000u;
+            for (int m = 0; m < M; ++m) off[m][i] = 8 * c < cols ? (unsigned)row * (unsigned)(2 * src[m].s.t) + 16u * c : 0x80000000u;
         }
     }
-    // rows row0 .. end - 1 of the tile exist (at least one)
+    // rows row0 .. end - 1 exist (at least one)
     __device__ __forceinline__ void begin(int row0, int end)
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rows = min(ROWS, end - row0);
         buf ^= 1;
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const v4i r = make_rsrc(base[m] + (int64_t)row0 * stride[m], 2u * ((unsigned)(rows - 1) * (unsigned)stride[m] + (unsigned)dim));
+        for (int m = 0; m < M; ++m)
 #pragma unroll
-            for (int i = 0; i < PW; ++i)
-                if (wave + NW * i < N) dma16(r, off[m][i], lds + (2 * buf + m) * TILE + (wave + NW * i) * 1024);
-        }
+            for (int p = 0; p < NP; ++p) {
+                const v4i r = make_rsrc(src[m].p + p * src[m].plane + (int64_t)row0 * src[m].s.t,
+                                        2u * ((unsigned)(rows - 1) * (unsigned)src[m].s.t + (unsigned)cols));
+#pragma unroll
+                for (int i = 0; i < PW; ++i)
+                    if (N % 4 == 0 || wave + 4 * i < N) dma16(r, off[m][i], lds + (M * buf + m) * TILE + p * PLANE + (wave + 4 * i) * 1024);
+            }
     }
-    __device__ __forceinline__ void ready(int, int)
+    __device__ __forceinline__ void ready()
     {
         dma_barrier();
         now = buf;
     }
-    __device__ __forceinline__ int at(int m) const { return (2 * now + m) * (TILE / 2); }      // the readable tile, in elements
-};
-
-template <typename T, int KS, bool VEC, int ROWS, int NW>
-struct Feed<T, KS, VEC, ROWS, NW, false> {
-    static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, TILE = NP * ROWS * RS * 2;
-    static constexpr int LDS = 2 * TILE + kSlack;
-    static constexpr bool kDirect = false;
-    Stage<T, KS, VEC, ROWS, 64 * NW> st[2];
-    const T* base[2];
-    int64_t stride[2];
-    __bf16* tile;
-    int dim;
-    __device__ __forceinline__ void init(unsigned char* at, const T* a, int64_t sa, const T* b, int64_t sb, int dim_)
-    {
-        tile = reinterpret_cast<__bf16*>(at);
-        base[0] = a;
-        base[1] = b;
-        stride[0] = sa;
-        stride[1] = sb;
-        dim = dim_;
-    }
-    __device__ __forceinline__ void begin(int row0, int end)
-    {
-#pragma unroll
-        for (int m = 0; m < 2; ++m) st[m].load(base[m], stride[m], row0, end - 1, dim, threadIdx.x);
-    }
-    __device__ __forceinline__ void ready(int row0, int end)
-    {
-        __syncthreads();
-#pragma unroll
-        for (int m = 0; m < 2; ++m) st[m].store(tile + m * TILE / 2, row0, end, dim, threadIdx.x);
-        __syncthreads();
-    }
-    __device__ __forceinline__ int at(int m) const { return m * (TILE / 2); }
+    __device__ __forceinline__ int at(int m) const { return (M * now + m) * (TILE / 2); }      // the readable tile, in elements
 };
 
 // Four neighbouring values from column d on; `vec`: the row is aligned for one store.
@@ -320,16 +353,13 @@ __device__ __forceinline__ void store4(__bf16* row, int d, int dim, bool vec, co
     }
 }
 
-// Strides in elements: sample, token, head.
-struct Strides {
-    int64_t b, t, h;
-};
-
 struct AttentionArgs {
     const void *q, *k, *v, *o, *go;
     void *out, *gq, *gk, *gv;
     float *lse, *stats;         // stats: per row its log-sum in base 2 (infinity for a row without keys) and its delta
     const int32_t* lens;
+    Source fq, fk, fv, fgo;     // as the feed reads them
+    int vec;                    // rows of the tensors may be read 16 bytes at a time
     Strides qs, ks, vs, os, gos, gqs, gks, gvs;
     int batch, kv_heads, group, q_len, kv_len, dim, causal;
     float scale;
@@ -390,18 +420,38 @@ __device__ __forceinline__ RowRange visible(const AttentionArgs& a, int n, int f
     return v;
 }
 
-constexpr int KeysTile = 32;    // queries of a tile of the backward pass's keys kernel (host and device)
+// Queries of a tile of the backward pass's keys kernel.
+template <int NP, int KS>
+constexpr int kKeysTile = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 6 ? 64 : 32;
 
-// How a call's kernels are chosen and cut (host): by sizes, type and alignment only, the same for the size of the workspace.
+// How a call's kernels are chosen and cut (host): by sizes and type only, the same for the size of the workspace.
 struct AttentionPlan {
     bool by_keys;               // forward: the wavefronts of a workgroup share 32 rows and divide the keys
     int blocks, splits, per_split;
     int q_blocks, q_splits, q_per_split;      // backward, gradient of the queries
     int k_blocks, k_splits, k_per_split;      // backward, gradient of the keys and values
 };
+AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int64_t dim, int type);
 
-int launch_attention(const AttentionArgs& a, int type, bool vec, const AttentionPlan& p, hipStream_t s);
-int launch_attention_backward(const AttentionArgs& a, int type, bool vec, const AttentionPlan& p, float* part_q, float* part_kv, hipStream_t s);
-AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len);
+// A tensor and where its planes go: [plane][batch * heads][len][cols], cols = dim rounded up to 8.
+struct Pack {
+    const void* src;
+    Strides s;
+    __bf16* dst;
+    int heads, len, by_lens;    // by_lens: rows past a sample's keys are not needed
+};
+struct PackArgs {
+    Pack m[4];
+    int count, batch, kv_len, dim;
+    const int32_t* lens;
+};
+inline Source packed_source(const Pack& p, int64_t batch, int64_t dim)
+{
+    const int64_t cols = (dim + 7) / 8 * 8;
+    return Source{p.dst, Strides{p.heads * p.len * cols, cols, p.len * cols}, batch * p.heads * p.len * cols};
+}
+int launch_pack(const PackArgs& a, int type, hipStream_t s);
+int launch_attention(const AttentionArgs& a, int type, const AttentionPlan& p, hipStream_t s);
+int launch_attention_backward(const AttentionArgs& a, int type, const AttentionPlan& p, float* part_q, float* part_kv, hipStream_t s);
 
 }  // namespace fpq

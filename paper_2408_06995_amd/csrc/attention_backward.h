@@ -12,19 +12,19 @@
 
 namespace fpq {
 
-template <typename T, int KS, bool VEC>
+template <int NP, int KS>
 struct QueriesShape {
-    static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2;
-    static constexpr int KT = NP == 3 || KS > 8 ? 32 : 64;
-    typedef Feed<T, KS, VEC, KT, 4> Tiles;
-    static constexpr int LDS = Tiles::LDS;
+    static constexpr int KT = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 8 ? 64 : 32;
+    typedef Feed<NP, KS, KT, 2> Tiles;
 };
 
-template <typename T, int KS, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_queries_kernel(AttentionArgs a)
+template <typename T, int KS>
+__global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void attention_queries_kernel(AttentionArgs a)
 {
-    typedef QueriesShape<T, KS, VEC> Sh;
-    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, KT = Sh::KT;
+    constexpr int NP = kPlanes<T>, DT = (KS + 1) / 2;
+    typedef QueriesShape<NP, KS> Sh;
+    typedef typename Sh::Tiles Tiles;
+    constexpr int KT = Sh::KT, PLANE = Tiles::PLANE / 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const Place at = place_of(a);
@@ -34,6 +34,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
     const int r_first = block * 128, r = r_first + 32 * wave + l32;
     const RowRange range = visible(a, n, r_first, min(r_first + 128, rows) - 1);
     const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
+    Tiles feed;
+    feed.src[0] = a.fk;
+    feed.src[1] = a.fv;
+    feed.src[0].p += b * a.fk.s.b + hk * a.fk.s.h;
+    feed.src[1].p += b * a.fv.s.b + hk * a.fv.s.h;
+    feed.init(lds_address(lds), a.dim);
+    if (kbeg < kend) feed.begin(kbeg, kend);
 
     const int rc = min(r, rows - 1), g = rc / a.q_len, i = rc - g * a.q_len, head = hk * a.group + g;
     const int end = a.causal ? max(0, min(n, i + n - a.q_len + 1)) : n;
@@ -47,11 +54,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             float v[8], w[8];
-            row8<T, VEC>(q, 16 * s + 8 * h, a.dim, v);
+            row8(q, 16 * s + 8 * h, a.dim, a.vec, v);
             qf[s] = frag_of<NP>(v);
-            row8<T, VEC>(go, 16 * s + 8 * h, a.dim, v);
+            row8(go, 16 * s + 8 * h, a.dim, a.vec, v);
             gf[s] = frag_of<NP>(v);
-            row8<T, VEC>(o, 16 * s + 8 * h, a.dim, w);
+            row8(o, 16 * s + 8 * h, a.dim, a.vec, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) delta = fmaf(v[e], w[e], delta);
         }
@@ -59,40 +66,43 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
     }
     const float log_sum = a.lse[row_id];
     const float c = a.scale * kLog2e, lse2 = log_sum == -kInf ? kInf : log_sum * kLog2e;   // a row without keys: every p is 0
-    if (r < rows && h == 0 && at.split == 0) {
-        reinterpret_cast<float2*>(a.stats)[row_id] = make_float2(lse2, delta);
-    }
-
-    const T* const kbase = static_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
-    const T* const vbase = static_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
+    Places<KS> places;
+    places.init(lane);
     v16f acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = zero16();
-    typename Sh::Tiles feed;
-    feed.init(lds, kbase, a.ks.t, vbase, a.vs.t, a.dim);
-    if (kbeg < kend) feed.begin(kbeg, kend);
     for (int j0 = kbeg; j0 < kend; j0 += KT) {
-        feed.ready(j0, kend);
-        const __bf16* const kt = reinterpret_cast<const __bf16*>(lds) + feed.at(0);
-        const __bf16* const vt = reinterpret_cast<const __bf16*>(lds) + feed.at(1);
+        feed.ready();
+        const __bf16* kt = reinterpret_cast<const __bf16*>(lds) + feed.at(0);
+        const __bf16* vt = reinterpret_cast<const __bf16*>(lds) + feed.at(1);
         if (j0 + KT < kend) feed.begin(j0 + KT, kend);
-        const bool masked = j0 + KT > min(range.lo, kend);
-#pragma unroll
-        for (int u = 0; u < KT / 32; ++u) {
+#pragma unroll 1
+        for (int j = j0; j < min(j0 + KT, kend); j += 32) {
             v16f s = zero16(), dp = zero16();
 #pragma unroll
             for (int t = 0; t < KS; ++t) {
-                mma<NP>(s, row_frag<NP, RS, KT>(kt, 32 * u + l32, 16 * t + 8 * h), qf[t]);
-                mma<NP>(dp, row_frag<NP, RS, KT>(vt, 32 * u + l32, 16 * t + 8 * h), gf[t]);
+                mma<NP>(s, rows_at<NP, KS>(kt, PLANE, places, 0, t), qf[t]);
+                mma<NP>(dp, rows_at<NP, KS>(vt, PLANE, places, 0, t), gf[t]);
             }
-            if (masked) {
-                const int left = end - j0 - 32 * u;
+            if (j + 32 > min(range.lo, kend)) {
+                const int left = end - j;
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (8 * (e / 4) + 4 * h + e % 4 >= left) s[e] = -kInf;
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -lse2)) * (dp[e] - delta);
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -lse2));
+            if (j == 0) {
+                // Rows of at most 32 keys have them all here: their delta from the products themselves instead of from o, whose
+                // rounding weighs most where o is an average of few values.
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum = fmaf(s[e], dp[e], sum);
+                sum += __shfl_xor(sum, 32);
+                if (end <= 32) delta = sum;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] *= dp[e] - delta;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 float v[8];
@@ -100,11 +110,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
                 for (int e = 0; e < 8; ++e) v[e] = s[8 * t + e];
                 const Frag<NP> ds = frag_of<NP>(v);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) mma<NP>(acc[d], col_frag<NP, RS, KT>(kt, 32 * u + 16 * t, 32 * d, lane), ds);
+                for (int d = 0; d < DT; ++d) mma<NP>(acc[d], cols_at<NP, KS>(kt, PLANE, places, 16 * t, d), ds);
             }
+            kt += 32 * Places<KS>::RS;
+            vt += 32 * Places<KS>::RS;
         }
     }
     if (r >= rows) return;
+    if (h == 0 && at.split == 0) reinterpret_cast<float2*>(a.stats)[row_id] = make_float2(lse2, delta);
     float* const part = a.splits > 1 ? a.part + (size_t)at.split * a.batch * a.kv_heads * rows * a.dim : nullptr;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -120,23 +133,27 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
 }
 
 // WHAT: 1 dv, 2 dk, 3 both in one pass.  In fp32 at the largest dimension the planes of 32 keys and values and both sums do not fit
-// a wavefront's registers together: two passes.
-template <typename T, int KS, bool VEC>
+// a wavefront's registers together: two passes.  VLDS: the workgroup's values stay in LDS and not in registers, which lets two
+// workgroups share a compute unit at a dimension of 128 in bf16.
+template <int NP, int KS>
 struct KeysShape {
-    static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2;
-    static constexpr int QT = KeysTile;
-    typedef Feed<T, KS, VEC, QT, 4> Tiles;
-    static constexpr int STATS = (Tiles::LDS + 15) / 16 * 16;          // two buffers of the rows' pairs of log-sum and delta
-    static constexpr int LDS = STATS + 2 * QT * 8;
-    static_assert(QT == 32, "the pairs of a tile are one load of four bytes per lane");
+    static constexpr int QT = kKeysTile<NP, KS>;
+    static constexpr bool VLDS = NP == 1 && KS > 6 && KS <= 8;
+    typedef Feed<NP, KS, QT, 2> Tiles;
+    typedef Feed<NP, KS, 128, 1> Values;
+    static constexpr int STATS = Tiles::LDS, PAIRS = QT < 32 ? 32 : QT;        // two buffers of the rows' pairs of log-sum and delta
+    static constexpr int VALUES = STATS + 2 * PAIRS * 8;
+    static constexpr int LDS = VALUES + (VLDS ? Values::TILE : 0);
 };
 
-template <typename T, int KS, bool VEC, int WHAT>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
+template <typename T, int KS, int WHAT>
+__global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
 {
-    typedef KeysShape<T, KS, VEC> Sh;
-    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, QT = Sh::QT;
-    constexpr bool DV = WHAT & 1, DK = WHAT & 2;
+    constexpr int NP = kPlanes<T>, DT = (KS + 1) / 2;
+    typedef KeysShape<NP, KS> Sh;
+    typedef typename Sh::Tiles Tiles;
+    constexpr int QT = Sh::QT, PLANE = Tiles::PLANE / 2;
+    constexpr bool DV = WHAT & 1, DK = WHAT & 2, VLDS = Sh::VLDS && DK;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const Place at = place_of(a);
@@ -144,11 +161,37 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
     const int n = keys_of(a, b), off = n - a.q_len, j_first = at.block * 128, key = j_first + 32 * wave + l32;
     // tiles of queries, head by head, from the first that sees a key of this block
     const int tiles_all = (a.q_len + QT - 1) / QT, skip = a.causal ? min(max(0, j_first - off) / QT, tiles_all) : 0;
-    const int per_head = j_first < n ? tiles_all - skip : 0;
+    const int per_head = j_first < n ? tiles_all - skip : 0, per = max(per_head, 1);
     const int64_t tiles = (int64_t)per_head * a.group;
     const int64_t tbeg = min((int64_t)at.split * a.per_split, tiles), tend = min(tbeg + a.per_split, tiles);
-
-    Frag<NP> kf[KS], vf[DK ? KS : 1];
+    Tiles feed;
+    int g = (int)(tbeg / per), i0 = (skip + (int)(tbeg - (int64_t)g * per)) * QT, slot = 0;
+    feed.src[0] = a.fq;
+    feed.src[1] = a.fgo;
+    feed.src[0].p += b * a.fq.s.b + (hk * a.group + g) * a.fq.s.h;
+    feed.src[1].p += b * a.fgo.s.b + (hk * a.group + g) * a.fgo.s.h;
+    feed.init(lds_address(lds), a.dim);
+    // the rows' pairs come with a tile; rows past the last get zeros, and so p = 1 next to zeros of q and do
+    auto begin = [&](int g, int i0) {
+        feed.begin(i0, a.q_len);
+        if (wave == 0) {
+            const v4i r = make_rsrc(a.stats + 2 * (((size_t)at.bh * a.group + g) * a.q_len + i0), 8u * (unsigned)min(QT, a.q_len - i0));
+#pragma unroll
+            for (int e = 0; e < Sh::PAIRS / 32; ++e) dma4(r, 4u * lane + 256u * e, lds_address(lds) + Sh::STATS + slot * Sh::PAIRS * 8 + 256 * e);
+        }
+        slot ^= 1;
+    };
+    if (tbeg < tend) {
+        if constexpr (VLDS) {
+            typename Sh::Values values;
+            values.src[0] = a.fv;
+            values.src[0].p += b * a.fv.s.b + hk * a.fv.s.h;
+            values.init(lds_address(lds) + Sh::VALUES, a.dim);
+            values.begin(j_first, n);
+        }
+        begin(g, i0);
+    }
+    Frag<NP> kf[KS], vf[DK && !VLDS ? KS : 1];
     {
         const int kc = max(0, min(key, n - 1));
         const T* k = static_cast<const T*>(a.k) + b * a.ks.b + kc * a.ks.t + hk * a.ks.h;
@@ -157,15 +200,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 float x[8];
-                row8<T, VEC>(k, 16 * s + 8 * h, a.dim, x);
+                row8(k, 16 * s + 8 * h, a.dim, a.vec, x);
                 kf[s] = frag_of<NP>(x);
-                if constexpr (DK) {
-                    row8<T, VEC>(v, 16 * s + 8 * h, a.dim, x);
+                if constexpr (DK && !VLDS) {
+                    row8(v, 16 * s + 8 * h, a.dim, a.vec, x);
                     vf[s] = frag_of<NP>(x);
                 }
             }
         }
     }
+    Places<KS> places;
+    places.init(lane);
+    const __bf16* const vt = reinterpret_cast<const __bf16*>(lds + Sh::VALUES) + 32 * wave * Places<KS>::RS;
     v16f av[DV ? DT : 1], ak[DK ? DT : 1];
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
@@ -173,55 +219,42 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
         if constexpr (DK) ak[d] = zero16();
     }
     const float c = a.scale * kLog2e;
-    const int per = max(per_head, 1);
-    typename Sh::Tiles feed;
-    int g = (int)(tbeg / per), i0 = (skip + (int)(tbeg - (int64_t)g * per)) * QT, slot = 0;
-    // rows past the last get zeros, and so p = 1 next to zeros of q and do
-    auto begin = [&](int g, int i0) {
-        feed.begin(i0, a.q_len);
-        if (wave == 0)
-            dma4(make_rsrc(a.stats + 2 * (((size_t)at.bh * a.group + g) * a.q_len + i0), 8u * (unsigned)min(QT, a.q_len - i0)), 4u * lane,
-                 lds_address(lds) + Sh::STATS + slot * QT * 8);
-        slot ^= 1;
-    };
-    feed.init(lds, static_cast<const T*>(a.q) + b * a.qs.b + (hk * a.group + g) * a.qs.h, a.qs.t,
-              static_cast<const T*>(a.go) + b * a.gos.b + (hk * a.group + g) * a.gos.h, a.gos.t, a.dim);
-    if (tbeg < tend) begin(g, i0);
     for (int64_t t = tbeg; t < tend; ++t) {
-        feed.ready(i0, a.q_len);
-        if constexpr (!Sh::Tiles::kDirect) dma_barrier();              // (the statistics)
-        const __bf16* const qt = reinterpret_cast<const __bf16*>(lds) + feed.at(0);
-        const __bf16* const gt = reinterpret_cast<const __bf16*>(lds) + feed.at(1);
-        const float* const ls = reinterpret_cast<const float*>(lds + Sh::STATS) + (slot ^ 1) * 2 * QT;
-        const int i_now = i0;
+        feed.ready();
+        const __bf16* qt = reinterpret_cast<const __bf16*>(lds) + feed.at(0);
+        const __bf16* gt = reinterpret_cast<const __bf16*>(lds) + feed.at(1);
+        const float* ls = reinterpret_cast<const float*>(lds + Sh::STATS) + (slot ^ 1) * 2 * Sh::PAIRS + 8 * h;
+        const int i_now = i0, i_end = min(i0 + QT, a.q_len);
         if (t + 1 < tend) {
             i0 += QT;
             if (i0 >= a.q_len) {                   // the next head of the group
                 i0 = skip * QT;
                 ++g;
-                feed.base[0] += a.qs.h;
-                feed.base[1] += a.gos.h;
+                feed.src[0].p += a.fq.s.h;
+                feed.src[1].p += a.fgo.s.h;
             }
             begin(g, i0);
         }
-        const bool masked = a.causal && j_first + 127 > i_now + off;
-#pragma unroll
-        for (int u = 0; u < QT / 32; ++u) {
+#pragma unroll 1
+        for (int i = i_now; i < i_end; i += 32) {
             v16f s = zero16(), dp = zero16();
 #pragma unroll
             for (int x = 0; x < KS; ++x) {
-                mma<NP>(s, row_frag<NP, RS, QT>(qt, 32 * u + l32, 16 * x + 8 * h), kf[x]);
-                if constexpr (DK) mma<NP>(dp, row_frag<NP, RS, QT>(gt, 32 * u + l32, 16 * x + 8 * h), vf[x]);
+                mma<NP>(s, rows_at<NP, KS>(qt, PLANE, places, 0, x), kf[x]);
+                if constexpr (VLDS)
+                    mma<NP>(dp, rows_at<NP, KS>(gt, PLANE, places, 0, x), rows_at<NP, KS>(vt, 0, places, 0, x));
+                else if constexpr (DK)
+                    mma<NP>(dp, rows_at<NP, KS>(gt, PLANE, places, 0, x), vf[x]);
             }
-            if (masked) {
-                const int from = key - off - i_now - 32 * u;      // the first query that sees the key
+            if (a.causal && j_first + 127 > i + off) {
+                const int from = key - off - i;    // the first query that sees the key
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (8 * (e / 4) + 4 * h + e % 4 < from) s[e] = -kInf;
             }
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {      // two rows' pairs at a time
-                const float4 y = *reinterpret_cast<const float4*>(ls + 2 * (32 * u + 8 * (e / 4) + 4 * h + e % 4));
+                const float4 y = *reinterpret_cast<const float4*>(ls + 2 * (8 * (e / 4) + e % 4));
                 s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -y.x));
                 s[e + 1] = __builtin_amdgcn_exp2f(fmaf(s[e + 1], c, -y.z));
                 if constexpr (DK) {
@@ -237,16 +270,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
                     for (int e = 0; e < 8; ++e) v[e] = s[8 * x + e];
                     const Frag<NP> p = frag_of<NP>(v);
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) mma<NP>(av[d], p, col_frag<NP, RS, QT>(gt, 32 * u + 16 * x, 32 * d, lane));
+                    for (int d = 0; d < DT; ++d) mma<NP>(av[d], p, cols_at<NP, KS>(gt, PLANE, places, 16 * x, d));
                 }
                 if constexpr (DK) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = dp[8 * x + e];
                     const Frag<NP> ds = frag_of<NP>(v);
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) mma<NP>(ak[d], ds, col_frag<NP, RS, QT>(qt, 32 * u + 16 * x, 32 * d, lane));
+                    for (int d = 0; d < DT; ++d) mma<NP>(ak[d], ds, cols_at<NP, KS>(qt, PLANE, places, 16 * x, d));
                 }
             }
+            qt += 32 * Places<KS>::RS;
+            gt += 32 * Places<KS>::RS;
+            ls += 64;
         }
     }
     // lane: column l32 of the 16 keys that its values stand for; keys that the sample does not have get zeros
@@ -300,52 +336,48 @@ int launch_sum(const float* part, int parts, size_t part_stride, size_t rows, in
     return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
 }
 
-template <typename T, int KS, bool VEC>
+template <typename T, int KS>
 int launch_queries(const AttentionArgs& a, hipStream_t s)
 {
-    typedef QueriesShape<T, KS, VEC> Sh;
+    constexpr int lds = QueriesShape<kPlanes<T>, KS>::Tiles::LDS;
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_queries_kernel<T, KS, VEC>), Sh::LDS, done)) return FPQ_ERR_LAUNCH;
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_queries_kernel<T, KS>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_queries_kernel<T, KS, VEC><<<dim3((unsigned)grid), dim3(256), Sh::LDS, s>>>(a);
+    attention_queries_kernel<T, KS><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
     return FPQ_OK;
 }
 
-template <typename T, int KS, bool VEC, int WHAT>
+template <typename T, int KS, int WHAT>
 int launch_keys(const AttentionArgs& a, hipStream_t s)
 {
-    typedef KeysShape<T, KS, VEC> Sh;
+    constexpr int lds = KeysShape<kPlanes<T>, KS>::LDS;
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_kernel<T, KS, VEC, WHAT>), Sh::LDS, done)) return FPQ_ERR_LAUNCH;
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_kernel<T, KS, WHAT>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_keys_kernel<T, KS, VEC, WHAT><<<dim3((unsigned)grid), dim3(256), Sh::LDS, s>>>(a);
+    attention_keys_kernel<T, KS, WHAT><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
     return FPQ_OK;
 }
 
-template <typename T, int KS, bool VEC>
+template <typename T, int KS>
 int launch_both(const AttentionArgs& aq, const AttentionArgs& ak, hipStream_t s)
 {
-    // (the keys kernel reads the deltas that the queries kernel writes)
-    int st = aq.q_len > 0 ? launch_queries<T, KS, VEC>(aq, s) : FPQ_OK;
+    // (the keys kernel reads the pairs that the queries kernel writes)
+    int st = aq.q_len > 0 ? launch_queries<T, KS>(aq, s) : FPQ_OK;
     if (st != FPQ_OK || ak.kv_len == 0) return st;
     if constexpr (sizeof(T) == 4 && KS > 8) {
-        st = launch_keys<T, KS, VEC, 1>(ak, s);
-        return st != FPQ_OK ? st : launch_keys<T, KS, VEC, 2>(ak, s);
+        st = launch_keys<T, KS, 1>(ak, s);
+        return st != FPQ_OK ? st : launch_keys<T, KS, 2>(ak, s);
     } else {
-        return launch_keys<T, KS, VEC, 3>(ak, s);
+        return launch_keys<T, KS, 3>(ak, s);
     }
 }
 
 template <typename T>
-int launch_backward(const AttentionArgs& aq, const AttentionArgs& ak, bool vec, hipStream_t s)
+int launch_backward(const AttentionArgs& aq, const AttentionArgs& ak, hipStream_t s)
 {
     const int ks = (aq.dim + 15) / 16;
-    int st;
-    if (vec)
-        st = ks <= 3 ? launch_both<T, 3, true>(aq, ak, s) : ks == 4 ? launch_both<T, 4, true>(aq, ak, s) : ks == 5 ? launch_both<T, 5, true>(aq, ak, s)
-           : ks == 6 ? launch_both<T, 6, true>(aq, ak, s) : ks <= 8 ? launch_both<T, 8, true>(aq, ak, s) : launch_both<T, 10, true>(aq, ak, s);
-    else
-        st = ks <= 4 ? launch_both<T, 4, false>(aq, ak, s) : ks <= 8 ? launch_both<T, 8, false>(aq, ak, s) : launch_both<T, 10, false>(aq, ak, s);
+    int st = ks <= 3 ? launch_both<T, 3>(aq, ak, s) : ks == 4 ? launch_both<T, 4>(aq, ak, s) : ks == 5 ? launch_both<T, 5>(aq, ak, s)
+           : ks == 6 ? launch_both<T, 6>(aq, ak, s) : ks <= 8 ? launch_both<T, 8>(aq, ak, s) : launch_both<T, 10>(aq, ak, s);
     if (st != FPQ_OK) return st;
     if (aq.splits > 1) {
         const size_t rows = (size_t)aq.batch * aq.kv_heads * aq.group * aq.q_len;

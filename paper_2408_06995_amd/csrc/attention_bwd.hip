@@ -3,9 +3,9 @@
 
 namespace fpq {
 
-int launch_attention_backward_f32(const AttentionArgs& aq, const AttentionArgs& ak, bool vec, hipStream_t s);
+int launch_attention_backward_f32(const AttentionArgs& aq, const AttentionArgs& ak, hipStream_t s);
 
-int launch_attention_backward(const AttentionArgs& a, int type, bool vec, const AttentionPlan& p, float* part_q, float* part_kv, hipStream_t s)
+int launch_attention_backward(const AttentionArgs& a, int type, const AttentionPlan& p, float* part_q, float* part_kv, hipStream_t s)
 {
     AttentionArgs aq = a, ak = a;
     aq.blocks = p.q_blocks;
@@ -16,7 +16,7 @@ int launch_attention_backward(const AttentionArgs& a, int type, bool vec, const 
     ak.splits = p.k_splits;
     ak.per_split = p.k_per_split;
     ak.part = part_kv;
-    return type == FPQ_TYPE_FP32 ? launch_attention_backward_f32(aq, ak, vec, s) : launch_backward<__bf16>(aq, ak, vec, s);
+    return type == FPQ_TYPE_FP32 ? launch_attention_backward_f32(aq, ak, s) : launch_backward<__bf16>(aq, ak, s);
 }
 
 }  // namespace fpq

@@ -3,6 +3,6 @@
 
 namespace fpq {
 
-int launch_attention_backward_f32(const AttentionArgs& aq, const AttentionArgs& ak, bool vec, hipStream_t s) { return launch_backward<float>(aq, ak, vec, s); }
+int launch_attention_backward_f32(const AttentionArgs& aq, const AttentionArgs& ak, hipStream_t s) { return launch_backward<float>(aq, ak, s); }
 
 }  // namespace fpq
