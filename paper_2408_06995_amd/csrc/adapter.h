@@ -16,8 +16,6 @@
 
 namespace fpq {
 
-typedef float v4f __attribute__((ext_vector_type(4)));
-
 constexpr int kTile = 32;          // rows of a tile
 constexpr int kMaxRank = 128;
 

@@ -84,6 +84,9 @@ AttentionArgs args_of(const fpq_attention_args_t* p)
     return a;
 }
 
+// Two values per row of 32 at a time of each head.
+size_t stats_size(const fpq_attention_args_t* p) { return (size_t)p->batch * p->q_heads * ((p->q_len + 31) / 32) * 256; }
+
 // Room for the planes of `rows` packed rows of a tensor.
 size_t planes_size(const fpq_attention_args_t* p, size_t rows)
 {
@@ -371,7 +374,7 @@ size_t fpq_attention_backward_workspace_size(const fpq_attention_args_t* p)
     if (check_attention(p) != FPQ_OK) return 0;
     const AttentionPlan plan = plan_of(p);
     const size_t dim = p->head_dim;
-    return align_up(rows_of(p) * 8) + (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
+    return stats_size(p) + (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
            (plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * dim * 4) : 0) + 2 * planes_size(p, keys_of(p)) +
            2 * planes_size(p, rows_of(p));
 }
@@ -415,7 +418,7 @@ int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const v
             rows_vec(grad_o, p->grad_o_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size);
     char* at = static_cast<char*>(workspace);
     a.stats = reinterpret_cast<float*>(at);
-    at += align_up(rows_of(p) * 8);
+    at += stats_size(p);
     float* const part_q = reinterpret_cast<float*>(at);
     if (plan.q_splits > 1) at += align_up(plan.q_splits * rows_of(p) * p->head_dim * 4);
     float* const part_kv = reinterpret_cast<float*>(at);

@@ -22,6 +22,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) v4s* lds_v4s;
@@ -126,17 +127,32 @@ __device__ __forceinline__ void row8(const T* row, int col, int dim, float (&v)[
         }
     } else {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] = col + t < dim ? (float)row[min(col + t, dim - 1)] : 0.0f;
+        for (int t = 0; t < 8; ++t) {
+            const float x = (float)row[min(col + t, dim - 1)];           // (loaded in any case: no branch)
+            v[t] = col + t < dim ? x : 0.0f;
+        }
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void row8(const T* row, int col, int dim, int vec, float (&v)[8])
+// A lane's part of a whole row: columns 16 s + 8 h .. + 7 of every step s.  All loads are under way before the first is waited for.
+template <typename T, int KS>
+__device__ __forceinline__ void row_all(const T* row, int h, int dim, int vec, float (&v)[KS][8])
 {
-    if (vec)
-        row8<T, true>(row, col, dim, v);
-    else
-        row8<T, false>(row, col, dim, v);
+    if (vec) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) row8<T, true>(row, 16 * s + 8 * h, dim, v[s]);
+    } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) row8<T, false>(row, 16 * s + 8 * h, dim, v[s]);
+    }
+}
+template <typename T, int KS, int NP>
+__device__ __forceinline__ void row_frags(const T* row, int h, int dim, int vec, Frag<NP> (&f)[KS])
+{
+    float v[KS][8];
+    row_all<T, KS>(row, h, dim, vec, v);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) f[s] = frag_of<NP>(v[s]);
 }
 
 // Operand rows from LDS: lane r's row, eight columns.
@@ -287,9 +303,9 @@ __device__ __forceinline__ Frag<NP> cols_at(const __bf16* tile, int plane, const
 // instructions per piece, one barrier per tile.  A descriptor per tile bounds the reads, so that rows past the last and columns
 // past the dimension (whose offsets are out of range) become zeros; its base moves in 64 bits, offsets within a tile fit 32.
 // begin() starts a tile, ready() makes the one begun last readable for the whole workgroup.
-template <int NP, int KS, int ROWS, int M>
+template <int NP, int KS, int ROWS, int M, int NW>
 struct Feed {
-    static constexpr int CS = Places<KS>::CS, N = ROWS * CS / 64, PW = (N + 3) / 4, PLANE = ROWS * CS * 16, TILE = NP * PLANE, LDS = 2 * M * TILE;
+    static constexpr int CS = Places<KS>::CS, N = ROWS * CS / 64, PW = (N + NW - 1) / NW, PLANE = ROWS * CS * 16, TILE = NP * PLANE, LDS = 2 * M * TILE;
     unsigned off[M][PW];
     Source src[M];              // p: of row 0 of the head
     unsigned lds;
@@ -302,7 +318,7 @@ struct Feed {
         cols = (dim + 7) / 8 * 8;
 #pragma unroll
         for (int i = 0; i < PW; ++i) {
-            const int q = (wave + 4 * i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ Places<KS>::swap(row);
+            const int q = (wave + NW * i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ Places<KS>::swap(row);
 #pragma unroll
             for (int m = 0; m < M; ++m) off[m][i] = 8 * c < cols ? (unsigned)row * (unsigned)(2 * src[m].s.t) + 16u * c : 0x80000000u;
         }
@@ -320,7 +336,7 @@ struct Feed {
                                         2u * ((unsigned)(rows - 1) * (unsigned)src[m].s.t + (unsigned)cols));
 #pragma unroll
                 for (int i = 0; i < PW; ++i)
-                    if (N % 4 == 0 || wave + 4 * i < N) dma16(r, off[m][i], lds + (M * buf + m) * TILE + p * PLANE + (wave + 4 * i) * 1024);
+                    if (N % NW == 0 || wave + NW * i < N) dma16(r, off[m][i], lds + (M * buf + m) * TILE + p * PLANE + (wave + NW * i) * 1024);
             }
     }
     __device__ __forceinline__ void ready()
@@ -356,7 +372,7 @@ __device__ __forceinline__ void store4(__bf16* row, int d, int dim, bool vec, co
 struct AttentionArgs {
     const void *q, *k, *v, *o, *go;
     void *out, *gq, *gk, *gv;
-    float *lse, *stats;         // stats: per row its log-sum in base 2 (infinity for a row without keys) and its delta
+    float *lse, *stats;         // stats: two values per row, from the queries kernel for the keys kernel
     const int32_t* lens;
     Source fq, fk, fv, fgo;     // as the feed reads them
     int vec;                    // rows of the tensors may be read 16 bytes at a time
@@ -371,7 +387,7 @@ struct AttentionArgs {
 
 // The part of the grid that a workgroup works on.  Workgroups go round-robin over the eight XCDs; each XCD takes a contiguous run
 // of them, so that the blocks that read the same keys share an L2.  Under `causal` blocks differ in length by up to their number:
-// the longest (number 0) of all heads of an XCD go first.
+// the longest (number 0) of all heads of an XCD go first, or, where the whole grid runs at once, the longest next to the shortest.
 struct Place {
     int bh, split, block;
 };
@@ -388,6 +404,8 @@ __device__ __forceinline__ Place place_of(const AttentionArgs& a)
         id /= a.splits;
         p.bh = id % local + (whole ? (int)(blockIdx.x & 7) * local : 0);
         p.block = id / local;
+        // all resident at once, two per compute unit: a long one and a short one each
+        if (total <= 512 && 2 * p.block >= a.blocks) p.block = a.blocks - 1 - (p.block - a.blocks / 2 - (a.blocks & 1));
         return p;
     }
     if (id < (per << 3)) id = (id & 7) * per + (id >> 3);
@@ -427,9 +445,9 @@ constexpr int kKeysTile = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 6 ? 64 : 32;
 // How a call's kernels are chosen and cut (host): by sizes and type only, the same for the size of the workspace.
 struct AttentionPlan {
     bool by_keys;               // forward: the wavefronts of a workgroup share 32 rows and divide the keys
-    int blocks, splits, per_split;
-    int q_blocks, q_splits, q_per_split;      // backward, gradient of the queries
-    int k_blocks, k_splits, k_per_split;      // backward, gradient of the keys and values
+    int waves, blocks, splits, per_split;             // waves: of a workgroup, with 32 rows (or keys) each
+    int q_waves, q_blocks, q_splits, q_per_split;     // backward, gradient of the queries
+    int k_waves, k_blocks, k_splits, k_per_split;     // backward, gradient of the keys and values
 };
 AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int64_t dim, int type);
 

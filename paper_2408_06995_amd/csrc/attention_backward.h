@@ -12,17 +12,24 @@
 
 namespace fpq {
 
-template <int NP, int KS>
+// What the keys kernel needs of a row: -log-sum / scale and -delta, the initial values of a score and of dp in the matrix unit (a row
+// without keys: -infinity, and so p = 0).  32 rows of a head at a time, first those, then these.
+__device__ __forceinline__ size_t stats_at(const AttentionArgs& a, size_t head, int i)
+{
+    return (head * ((a.q_len + 31) / 32) + (i >> 5)) * 64 + (i & 31);
+}
+
+template <int NP, int KS, int NW>
 struct QueriesShape {
-    static constexpr int KT = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 8 ? 64 : 32;
-    typedef Feed<NP, KS, KT, 2> Tiles;
+    static constexpr int KT = NP == 3 || KS > 8 ? 32 : 64;
+    typedef Feed<NP, KS, KT, 2, NW> Tiles;
 };
 
-template <typename T, int KS>
-__global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void attention_queries_kernel(AttentionArgs a)
+template <typename T, int KS, int NW>
+__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 3 : KS <= 8 ? 2 : 1) : KS <= 5 ? 2 : 1) void attention_queries_kernel(AttentionArgs a)
 {
     constexpr int NP = kPlanes<T>, DT = (KS + 1) / 2;
-    typedef QueriesShape<NP, KS> Sh;
+    typedef QueriesShape<NP, KS, NW> Sh;
     typedef typename Sh::Tiles Tiles;
     constexpr int KT = Sh::KT, PLANE = Tiles::PLANE / 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -31,8 +38,8 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
     const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
     const int rows = a.group * a.q_len, n = keys_of(a, b);
     const int block = a.causal ? a.blocks - 1 - at.block : at.block;
-    const int r_first = block * 128, r = r_first + 32 * wave + l32;
-    const RowRange range = visible(a, n, r_first, min(r_first + 128, rows) - 1);
+    const int r_first = block * 32 * NW, r = r_first + 32 * wave + l32;
+    const RowRange range = visible(a, n, r_first, min(r_first + 32 * NW, rows) - 1);
     const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
     Tiles feed;
     feed.src[0] = a.fk;
@@ -48,21 +55,17 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
     Frag<NP> qf[KS], gf[KS];
     float delta = 0.0f;
     {
-        const T* q = static_cast<const T*>(a.q) + b * a.qs.b + i * a.qs.t + head * a.qs.h;
-        const T* o = static_cast<const T*>(a.o) + b * a.os.b + i * a.os.t + head * a.os.h;
-        const T* go = static_cast<const T*>(a.go) + b * a.gos.b + i * a.gos.t + head * a.gos.h;
+        float v[KS][8], w[KS][8];
+        row_all<T, KS>(static_cast<const T*>(a.go) + b * a.gos.b + i * a.gos.t + head * a.gos.h, h, a.dim, a.vec, v);
+        row_all<T, KS>(static_cast<const T*>(a.o) + b * a.os.b + i * a.os.t + head * a.os.h, h, a.dim, a.vec, w);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            float v[8], w[8];
-            row8(q, 16 * s + 8 * h, a.dim, a.vec, v);
-            qf[s] = frag_of<NP>(v);
-            row8(go, 16 * s + 8 * h, a.dim, a.vec, v);
-            gf[s] = frag_of<NP>(v);
-            row8(o, 16 * s + 8 * h, a.dim, a.vec, w);
+            gf[s] = frag_of<NP>(v[s]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) delta = fmaf(v[e], w[e], delta);
+            for (int e = 0; e < 8; ++e) delta = fmaf(v[s][e], w[s][e], delta);
         }
         delta += __shfl_xor(delta, 32);
+        row_frags<T, KS, NP>(static_cast<const T*>(a.q) + b * a.qs.b + i * a.qs.t + head * a.qs.h, h, a.dim, a.vec, qf);
     }
     const float log_sum = a.lse[row_id];
     const float c = a.scale * kLog2e, lse2 = log_sum == -kInf ? kInf : log_sum * kLog2e;   // a row without keys: every p is 0
@@ -117,7 +120,11 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
         }
     }
     if (r >= rows) return;
-    if (h == 0 && at.split == 0) reinterpret_cast<float2*>(a.stats)[row_id] = make_float2(lse2, delta);
+    if (h == 0 && at.split == 0) {
+        float* const st = a.stats + stats_at(a, (size_t)at.bh * a.group + g, i);
+        st[0] = log_sum == -kInf ? -kInf : -log_sum / a.scale;
+        st[32] = -delta;
+    }
     float* const part = a.splits > 1 ? a.part + (size_t)at.split * a.batch * a.kv_heads * rows * a.dim : nullptr;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -132,25 +139,25 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
         }
 }
 
-// WHAT: 1 dv, 2 dk, 3 both in one pass.  In fp32 at the largest dimension the planes of 32 keys and values and both sums do not fit
+// WHAT: 1 dv, 2 dk, 3 both in one pass.  In fp32 at dimensions past 96 the planes of 32 keys and values and both sums do not fit
 // a wavefront's registers together: two passes.  VLDS: the workgroup's values stay in LDS and not in registers, which lets two
 // workgroups share a compute unit at a dimension of 128 in bf16.
-template <int NP, int KS>
+template <int NP, int KS, int NW>
 struct KeysShape {
     static constexpr int QT = kKeysTile<NP, KS>;
     static constexpr bool VLDS = NP == 1 && KS > 6 && KS <= 8;
-    typedef Feed<NP, KS, QT, 2> Tiles;
-    typedef Feed<NP, KS, 128, 1> Values;
-    static constexpr int STATS = Tiles::LDS, PAIRS = QT < 32 ? 32 : QT;        // two buffers of the rows' pairs of log-sum and delta
-    static constexpr int VALUES = STATS + 2 * PAIRS * 8;
+    typedef Feed<NP, KS, QT, 2, NW> Tiles;
+    typedef Feed<NP, KS, 32 * NW, 1, NW> Values;
+    static constexpr int STATS = Tiles::LDS;                                   // two buffers of the rows' two statistics
+    static constexpr int VALUES = STATS + 2 * QT * 8;
     static constexpr int LDS = VALUES + (VLDS ? Values::TILE : 0);
 };
 
-template <typename T, int KS, int WHAT>
-__global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
+template <typename T, int KS, int WHAT, int NW>
+__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
 {
     constexpr int NP = kPlanes<T>, DT = (KS + 1) / 2;
-    typedef KeysShape<NP, KS> Sh;
+    typedef KeysShape<NP, KS, NW> Sh;
     typedef typename Sh::Tiles Tiles;
     constexpr int QT = Sh::QT, PLANE = Tiles::PLANE / 2;
     constexpr bool DV = WHAT & 1, DK = WHAT & 2, VLDS = Sh::VLDS && DK;
@@ -158,7 +165,7 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const Place at = place_of(a);
     const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
-    const int n = keys_of(a, b), off = n - a.q_len, j_first = at.block * 128, key = j_first + 32 * wave + l32;
+    const int n = keys_of(a, b), off = n - a.q_len, j_first = at.block * 32 * NW, key = j_first + 32 * wave + l32;
     // tiles of queries, head by head, from the first that sees a key of this block
     const int tiles_all = (a.q_len + QT - 1) / QT, skip = a.causal ? min(max(0, j_first - off) / QT, tiles_all) : 0;
     const int per_head = j_first < n ? tiles_all - skip : 0, per = max(per_head, 1);
@@ -171,13 +178,14 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
     feed.src[0].p += b * a.fq.s.b + (hk * a.group + g) * a.fq.s.h;
     feed.src[1].p += b * a.fgo.s.b + (hk * a.group + g) * a.fgo.s.h;
     feed.init(lds_address(lds), a.dim);
-    // the rows' pairs come with a tile; rows past the last get zeros, and so p = 1 next to zeros of q and do
+    // the rows' statistics come with a tile; rows past the last get zeros, and so p = 1 next to zeros of q and do
     auto begin = [&](int g, int i0) {
         feed.begin(i0, a.q_len);
         if (wave == 0) {
-            const v4i r = make_rsrc(a.stats + 2 * (((size_t)at.bh * a.group + g) * a.q_len + i0), 8u * (unsigned)min(QT, a.q_len - i0));
+            const v4i r = make_rsrc(a.stats + stats_at(a, (size_t)at.bh * a.group + g, i0), QT * 8);
 #pragma unroll
-            for (int e = 0; e < Sh::PAIRS / 32; ++e) dma4(r, 4u * lane + 256u * e, lds_address(lds) + Sh::STATS + slot * Sh::PAIRS * 8 + 256 * e);
+            for (int e = 0; e < QT / 32; ++e)
+                dma4(r, i0 + 32 * e + l32 < a.q_len ? 4u * lane + 256u * e : 0x80000000u, lds_address(lds) + Sh::STATS + slot * QT * 8 + 256 * e);
         }
         slot ^= 1;
     };
@@ -197,16 +205,8 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
         const T* k = static_cast<const T*>(a.k) + b * a.ks.b + kc * a.ks.t + hk * a.ks.h;
         const T* v = static_cast<const T*>(a.v) + b * a.vs.b + kc * a.vs.t + hk * a.vs.h;
         if (tbeg < tend) {                         // (no tile: no key either, perhaps)
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                float x[8];
-                row8(k, 16 * s + 8 * h, a.dim, a.vec, x);
-                kf[s] = frag_of<NP>(x);
-                if constexpr (DK && !VLDS) {
-                    row8(v, 16 * s + 8 * h, a.dim, a.vec, x);
-                    vf[s] = frag_of<NP>(x);
-                }
-            }
+            row_frags<T, KS, NP>(k, h, a.dim, a.vec, kf);
+            if constexpr (DK && !VLDS) row_frags<T, KS, NP>(v, h, a.dim, a.vec, vf);
         }
     }
     Places<KS> places;
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
         feed.ready();
         const __bf16* qt = reinterpret_cast<const __bf16*>(lds) + feed.at(0);
         const __bf16* gt = reinterpret_cast<const __bf16*>(lds) + feed.at(1);
-        const float* ls = reinterpret_cast<const float*>(lds + Sh::STATS) + (slot ^ 1) * 2 * Sh::PAIRS + 8 * h;
+        const float* ls = reinterpret_cast<const float*>(lds + Sh::STATS) + (slot ^ 1) * 2 * QT + 4 * h;
         const int i_now = i0, i_end = min(i0 + QT, a.q_len);
         if (t + 1 < tend) {
             i0 += QT;
@@ -237,7 +237,19 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
         }
 #pragma unroll 1
         for (int i = i_now; i < i_end; i += 32) {
-            v16f s = zero16(), dp = zero16();
+            v16f s, dp, log_sum, delta;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const v4f y = *reinterpret_cast<const v4f*>(ls + 8 * e), z = *reinterpret_cast<const v4f*>(ls + 32 + 8 * e);
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    log_sum[4 * e + f] = y[f];
+                    delta[4 * e + f] = z[f];
+                }
+            }
+            // (fp32 sums the small parts of its products first: from zero)
+            s = NP == 1 ? log_sum : zero16();
+            dp = NP == 1 ? delta : zero16();
 #pragma unroll
             for (int x = 0; x < KS; ++x) {
                 mma<NP>(s, rows_at<NP, KS>(qt, PLANE, places, 0, x), kf[x]);
@@ -246,21 +258,16 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
                 else if constexpr (DK)
                     mma<NP>(dp, rows_at<NP, KS>(gt, PLANE, places, 0, x), vf[x]);
             }
-            if (a.causal && j_first + 127 > i + off) {
+            if (a.causal && j_first + 32 * NW - 1 > i + off) {
                 const int from = key - off - i;    // the first query that sees the key
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (8 * (e / 4) + 4 * h + e % 4 < from) s[e] = -kInf;
             }
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {      // two rows' pairs at a time
-                const float4 y = *reinterpret_cast<const float4*>(ls + 2 * (8 * (e / 4) + e % 4));
-                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -y.x));
-                s[e + 1] = __builtin_amdgcn_exp2f(fmaf(s[e + 1], c, -y.z));
-                if constexpr (DK) {
-                    dp[e] = s[e] * (dp[e] - y.y);
-                    dp[e + 1] = s[e + 1] * (dp[e + 1] - y.w);
-                }
+            for (int e = 0; e < 16; ++e) {
+                s[e] = __builtin_amdgcn_exp2f((NP == 1 ? s[e] : s[e] + log_sum[e]) * c);
+                if constexpr (DK) dp[e] = s[e] * (NP == 1 ? dp[e] : dp[e] + delta[e]);
             }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -313,83 +320,115 @@ __global__ __launch_bounds__(256, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void atten
     }
 }
 
-// out[b, t, head] = the sum of the parts, in order.
+// out[b, t, head] = the sum of the parts, in order: up to three results in one launch, a row per 32 lanes.
+struct SumOut {
+    const float* part;
+    size_t stride;              // from one part to the next
+    int parts, len, heads;
+    int64_t rows;               // 0: none
+    void* out;
+    Strides s;
+};
+struct SumArgs {
+    SumOut m[3];
+    int dim;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void attention_sum_kernel(const float* part, int parts, size_t part_stride, size_t n, int len, int heads, int dim,
-                                                            T* out, Strides st)
+__global__ __launch_bounds__(256) void attention_sum_kernel(SumArgs a)
 {
-    for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (size_t)gridDim.x * 256) {
-        float v = part[e];
-        for (int s = 1; s < parts; ++s) v += part[s * part_stride + e];
-        const size_t row = e / dim, bh = row / len;
-        const int64_t b = bh / heads, head = bh - (size_t)b * heads;
-        out[b * st.b + (int64_t)(row - bh * len) * st.t + head * st.h + (int64_t)(e - row * dim)] = (T)v;
+    const SumOut& m = a.m[blockIdx.y];
+    const int lane = threadIdx.x & 31;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < m.rows; row += (int64_t)gridDim.x * 8) {
+        const int64_t bh = row / m.len, b = bh / m.heads;
+        T* const out = static_cast<T*>(m.out) + b * m.s.b + (row - bh * m.len) * m.s.t + (bh - b * m.heads) * m.s.h;
+        const float* const in = m.part + row * a.dim;
+        float v[5] = {0, 0, 0, 0, 0};
+        for (int s0 = 0; s0 < m.parts; s0 += 4) {
+            float p[4][5];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int d = 0; d < 5; ++d) p[u][d] = in[min(s0 + u, m.parts - 1) * m.stride + min(lane + 32 * d, a.dim - 1)];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int d = 0; d < 5; ++d) v[d] += s0 + u < m.parts ? p[u][d] : 0.0f;
+        }
+#pragma unroll
+        for (int d = 0; d < 5; ++d)
+            if (lane + 32 * d < a.dim) out[lane + 32 * d] = (T)v[d];
     }
 }
 
-template <typename T>
-int launch_sum(const float* part, int parts, size_t part_stride, size_t rows, int len, int heads, int dim, void* out, const Strides& st, hipStream_t s)
-{
-    const size_t n = rows * dim, want = (n + 255) / 256;
-    attention_sum_kernel<T><<<dim3((unsigned)(want < 4096 ? want : 4096)), dim3(256), 0, s>>>(part, parts, part_stride, n, len, heads, dim,
-                                                                                             static_cast<T*>(out), st);
-    return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
-}
-
-template <typename T, int KS>
+template <typename T, int KS, int NW>
 int launch_queries(const AttentionArgs& a, hipStream_t s)
 {
-    constexpr int lds = QueriesShape<kPlanes<T>, KS>::Tiles::LDS;
+    constexpr int lds = QueriesShape<kPlanes<T>, KS, NW>::Tiles::LDS;
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_queries_kernel<T, KS>), lds, done)) return FPQ_ERR_LAUNCH;
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_queries_kernel<T, KS, NW>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_queries_kernel<T, KS><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
+    attention_queries_kernel<T, KS, NW><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
+    return FPQ_OK;
+}
+
+template <typename T, int KS, int WHAT, int NW>
+int launch_keys(const AttentionArgs& a, hipStream_t s)
+{
+    constexpr int lds = KeysShape<kPlanes<T>, KS, NW>::LDS;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_kernel<T, KS, WHAT, NW>), lds, done)) return FPQ_ERR_LAUNCH;
+    const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
+    attention_keys_kernel<T, KS, WHAT, NW><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
     return FPQ_OK;
 }
 
 template <typename T, int KS, int WHAT>
-int launch_keys(const AttentionArgs& a, hipStream_t s)
+int launch_keys(const AttentionArgs& a, int waves, hipStream_t s)
 {
-    constexpr int lds = KeysShape<kPlanes<T>, KS>::LDS;
-    static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_kernel<T, KS, WHAT>), lds, done)) return FPQ_ERR_LAUNCH;
-    const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_keys_kernel<T, KS, WHAT><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
-    return FPQ_OK;
+    return waves == 4 ? launch_keys<T, KS, WHAT, 4>(a, s) : launch_keys<T, KS, WHAT, 2>(a, s);
 }
 
 template <typename T, int KS>
-int launch_both(const AttentionArgs& aq, const AttentionArgs& ak, hipStream_t s)
+int launch_both(const AttentionArgs& aq, const AttentionArgs& ak, const AttentionPlan& p, hipStream_t s)
 {
-    // (the keys kernel reads the pairs that the queries kernel writes)
-    int st = aq.q_len > 0 ? launch_queries<T, KS>(aq, s) : FPQ_OK;
+    // (the keys kernel reads what the queries kernel writes)
+    int st = FPQ_OK;
+    if (aq.q_len > 0) st = p.q_waves == 4 ? launch_queries<T, KS, 4>(aq, s) : launch_queries<T, KS, 2>(aq, s);
     if (st != FPQ_OK || ak.kv_len == 0) return st;
-    if constexpr (sizeof(T) == 4 && KS > 8) {
-        st = launch_keys<T, KS, 1>(ak, s);
-        return st != FPQ_OK ? st : launch_keys<T, KS, 2>(ak, s);
+    if constexpr (sizeof(T) == 4 && KS > 6) {
+        st = launch_keys<T, KS, 1>(ak, p.k_waves, s);
+        return st != FPQ_OK ? st : launch_keys<T, KS, 2>(ak, p.k_waves, s);
     } else {
-        return launch_keys<T, KS, 3>(ak, s);
+        return launch_keys<T, KS, 3>(ak, p.k_waves, s);
     }
 }
 
 template <typename T>
-int launch_backward(const AttentionArgs& aq, const AttentionArgs& ak, hipStream_t s)
+int launch_backward(const AttentionArgs& aq, const AttentionArgs& ak, const AttentionPlan& p, hipStream_t s)
 {
     const int ks = (aq.dim + 15) / 16;
-    int st = ks <= 3 ? launch_both<T, 3>(aq, ak, s) : ks == 4 ? launch_both<T, 4>(aq, ak, s) : ks == 5 ? launch_both<T, 5>(aq, ak, s)
-           : ks == 6 ? launch_both<T, 6>(aq, ak, s) : ks <= 8 ? launch_both<T, 8>(aq, ak, s) : launch_both<T, 10>(aq, ak, s);
+    int st = ks <= 3 ? launch_both<T, 3>(aq, ak, p, s) : ks == 4 ? launch_both<T, 4>(aq, ak, p, s) : ks == 5 ? launch_both<T, 5>(aq, ak, p, s)
+           : ks == 6 ? launch_both<T, 6>(aq, ak, p, s) : ks <= 8 ? launch_both<T, 8>(aq, ak, p, s) : launch_both<T, 10>(aq, ak, p, s);
     if (st != FPQ_OK) return st;
-    if (aq.splits > 1) {
-        const size_t rows = (size_t)aq.batch * aq.kv_heads * aq.group * aq.q_len;
-        st = launch_sum<T>(aq.part, aq.splits, rows * aq.dim, rows, aq.q_len, aq.kv_heads * aq.group, aq.dim, aq.gq, aq.gqs, s);
-        if (st != FPQ_OK) return st;
-    }
+    SumArgs sums{};
+    sums.dim = aq.dim;
+    int count = 0;
+    int64_t most = 0;
+    auto add = [&](const AttentionArgs& a, const float* part, size_t stride, int len, int heads, void* out, const Strides& st) {
+        const int64_t rows = (int64_t)a.batch * heads * len;
+        sums.m[count++] = SumOut{part, stride, a.splits, len, heads, rows, out, st};
+        if (rows > most) most = rows;
+    };
+    if (aq.splits > 1)
+        add(aq, aq.part, (size_t)aq.batch * aq.kv_heads * aq.group * aq.q_len * aq.dim, aq.q_len, aq.kv_heads * aq.group, aq.gq, aq.gqs);
     if (ak.splits > 1) {
-        const size_t rows = (size_t)ak.batch * ak.kv_heads * ak.kv_len;
-        st = launch_sum<T>(ak.part, ak.splits, 2 * rows * ak.dim, rows, ak.kv_len, ak.kv_heads, ak.dim, ak.gk, ak.gks, s);
-        if (st != FPQ_OK) return st;
-        st = launch_sum<T>(ak.part + rows * ak.dim, ak.splits, 2 * rows * ak.dim, rows, ak.kv_len, ak.kv_heads, ak.dim, ak.gv, ak.gvs, s);
-        if (st != FPQ_OK) return st;
+        const size_t keys = (size_t)ak.batch * ak.kv_heads * ak.kv_len * ak.dim;
+        add(ak, ak.part, 2 * keys, ak.kv_len, ak.kv_heads, ak.gk, ak.gks);
+        add(ak, ak.part + keys, 2 * keys, ak.kv_len, ak.kv_heads, ak.gv, ak.gvs);
+    }
+    if (most) {
+        const int64_t want = (most + 7) / 8;
+        attention_sum_kernel<T><<<dim3((unsigned)(want < 16384 ? want : 16384), count), dim3(256), 0, s>>>(sums);
     }
     return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
 }

@@ -3,7 +3,7 @@
 
 namespace fpq {
 
-int launch_attention_backward_f32(const AttentionArgs& aq, const AttentionArgs& ak, hipStream_t s);
+int launch_attention_backward_f32(const AttentionArgs& aq, const AttentionArgs& ak, const AttentionPlan& p, hipStream_t s);
 
 int launch_attention_backward(const AttentionArgs& a, int type, const AttentionPlan& p, float* part_q, float* part_kv, hipStream_t s)
 {
@@ -16,7 +16,7 @@ int launch_attention_backward(const AttentionArgs& a, int type, const AttentionP
     ak.splits = p.k_splits;
     ak.per_split = p.k_per_split;
     ak.part = part_kv;
-    return type == FPQ_TYPE_FP32 ? launch_attention_backward_f32(aq, ak, s) : launch_backward<__bf16>(aq, ak, s);
+    return type == FPQ_TYPE_FP32 ? launch_attention_backward_f32(aq, ak, p, s) : launch_backward<__bf16>(aq, ak, p, s);
 }
 
 }  // namespace fpq

@@ -5,7 +5,7 @@
 //
 // A wavefront has 32 rows of queries in registers and takes S^T = K Q^T per 32 keys, so that a lane holds 16 scores of one row and
 // its maximum and sum need one exchange with the lane 32 on; P^T is then the operand of O^T = V^T P^T as it lies.
-//   rows form: four wavefronts with 32 rows each share tiles of keys and values in LDS.
+//   rows form: two or four wavefronts with 32 rows each share tiles of keys and values in LDS.
 //   keys form: the wavefronts share one or two sets of 32 rows and divide each tile's keys; their results are joined at the end.
 //     For few rows: single tokens, small batches.
 #pragma once
@@ -59,17 +59,17 @@ __device__ __forceinline__ float inverse(float sum)       // no key: zeros; a su
     return sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
 }
 
-template <int NP, int KS>
+template <int NP, int KS, int NW>
 struct RowsShape {
-    static constexpr int KT = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 8 ? 64 : 32, NS = KT < 64 ? 1 : 2;
-    typedef Feed<NP, KS, KT, 2> Tiles;
+    static constexpr int KT = NP == 3 || KS > 8 ? 32 : 64, NS = KT < 64 ? 1 : 2;
+    typedef Feed<NP, KS, KT, 2, NW> Tiles;
 };
 
-template <typename T, int KS>
-__global__ __launch_bounds__(256, 2) void attention_rows_kernel(AttentionArgs a)
+template <typename T, int KS, int NW>
+__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 4 : 2) : KS <= 6 ? 2 : 1) void attention_rows_kernel(AttentionArgs a)
 {
     constexpr int NP = kPlanes<T>, DT = (KS + 1) / 2;
-    typedef RowsShape<NP, KS> Sh;
+    typedef RowsShape<NP, KS, NW> Sh;
     typedef typename Sh::Tiles Tiles;
     constexpr int KT = Sh::KT, NS = Sh::NS, PLANE = Tiles::PLANE / 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -78,8 +78,8 @@ __global__ __launch_bounds__(256, 2) void attention_rows_kernel(AttentionArgs a)
     const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
     const int rows = a.group * a.q_len, n = keys_of(a, b);
     const int block = a.causal ? a.blocks - 1 - at.block : at.block;          // the longest rows first
-    const int r_first = block * 128, r = r_first + 32 * wave + l32;
-    const RowRange range = visible(a, n, r_first, min(r_first + 128, rows) - 1);
+    const int r_first = block * 32 * NW, r = r_first + 32 * wave + l32;
+    const RowRange range = visible(a, n, r_first, min(r_first + 32 * NW, rows) - 1);
     const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
     Tiles feed;
     feed.src[0] = a.fk;
@@ -92,15 +92,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_kernel(AttentionArgs a)
     const int rc = min(r, rows - 1), g = rc / a.q_len, i = rc - g * a.q_len, head = hk * a.group + g;
     const int end = a.causal ? max(0, min(n, i + n - a.q_len + 1)) : n;       // the row sees keys below it
     Frag<NP> qf[KS];
-    {
-        const T* row = static_cast<const T*>(a.q) + b * a.qs.b + i * a.qs.t + head * a.qs.h;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            float v[8];
-            row8(row, 16 * s + 8 * h, a.dim, a.vec, v);
-            qf[s] = frag_of<NP>(v);
-        }
-    }
+    row_frags<T, KS, NP>(static_cast<const T*>(a.q) + b * a.qs.b + i * a.qs.t + head * a.qs.h, h, a.dim, a.vec, qf);
     Places<KS> places;
     places.init(lane);
     v16f acc[DT];
@@ -197,15 +189,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
     const int rc = min(r, rows - 1), g = rc / a.q_len, i = rc - g * a.q_len, head = hk * a.group + g;
     const int end = a.causal ? max(0, min(n, i + n - a.q_len + 1)) : n;
     Frag<NP> qf[KS];
-    {
-        const T* row = static_cast<const T*>(a.q) + b * a.qs.b + i * a.qs.t + head * a.qs.h;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            float v[8];
-            row8<T, VEC>(row, 16 * s + 8 * h, a.dim, v);
-            qf[s] = frag_of<NP>(v);
-        }
-    }
+    row_frags<T, KS, NP>(static_cast<const T*>(a.q) + b * a.qs.b + i * a.qs.t + head * a.qs.h, h, a.dim, VEC, qf);
     v16f acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = zero16();
@@ -286,50 +270,66 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
     }
 }
 
-// The parts of a row, each normalised with its own log-sum, joined: o = sum_s exp(lse_s - lse) o_s.  One wavefront per row; lane s
-// has the weight of part s (there are at most 64).
+// The parts of a row, each normalised with its own log-sum, joined: o = sum_s exp(lse_s - lse) o_s.  32 lanes per row.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
 {
-    const size_t rows = (size_t)a.batch * a.kv_heads * a.group * a.q_len, row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (row >= rows) return;
-    const float mine = lane < a.splits ? a.part_lse[lane * rows + row] : -kInf;
-    float top = mine;
+    const size_t rows = (size_t)a.batch * a.kv_heads * a.group * a.q_len;
+    const size_t at = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5), row = at < rows ? at : rows - 1;
+    const int lane = threadIdx.x & 31;
+    // four parts at a time, their log-sums and values loaded together, with a running maximum
+    float base = -kInf, sum = 0.0f, v[5] = {0, 0, 0, 0, 0};
+    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+        float ls[4], p[4][5];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float base = top == -kInf ? 0.0f : top, w = __builtin_amdgcn_exp2f((mine - base) * kLog2e);
-    float sum = w;
+        for (int u = 0; u < 4; ++u) {
+            const size_t s = min(s0 + u, a.splits - 1);
+            ls[u] = a.part_lse[s * rows + row];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+            for (int d = 0; d < 5; ++d) p[u][d] = a.part[(s * rows + row) * a.dim + min(lane + 32 * d, a.dim - 1)];
+        }
+        float top = base;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) top = fmaxf(top, ls[u]);
+        const float to = top == -kInf ? 0.0f : top, by = __builtin_amdgcn_exp2f((base - to) * kLog2e);
+        sum *= by;
+#pragma unroll
+        for (int d = 0; d < 5; ++d) v[d] *= by;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float w = s0 + u < a.splits ? __builtin_amdgcn_exp2f((ls[u] - to) * kLog2e) : 0.0f;
+            sum += w;
+#pragma unroll
+            for (int d = 0; d < 5; ++d) v[d] += w == 0.0f ? 0.0f : w * p[u][d];
+        }
+        base = top;
+    }
+    if (at >= rows) return;
     if (lane == 0 && a.lse) a.lse[row] = sum == 0.0f ? -kInf : base + logf(sum);
     const size_t bh = row / a.q_len;
     const int i = (int)(row - bh * a.q_len), heads = a.kv_heads * a.group;
     const int64_t b = bh / heads, head = bh - (size_t)b * heads;
     T* const out = static_cast<T*>(a.out) + b * a.os.b + i * a.os.t + head * a.os.h;
     const float inv = inverse(sum);
-    float v[3] = {0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float ws = __shfl(w, s);
-        const float* const p = a.part + (s * rows + row) * a.dim;
 #pragma unroll
-        for (int d = 0; d < 3; ++d)
-            if (lane + 64 * d < a.dim) v[d] += ws * p[lane + 64 * d];
-    }
-#pragma unroll
-    for (int d = 0; d < 3; ++d)
-        if (lane + 64 * d < a.dim) out[lane + 64 * d] = (T)(v[d] * inv);
+    for (int d = 0; d < 5; ++d)
+        if (lane + 32 * d < a.dim) out[lane + 32 * d] = (T)(v[d] * inv);
 }
 
-template <typename T, int KS>
+template <typename T, int KS, int NW>
 int launch_rows(const AttentionArgs& a, hipStream_t s)
 {
-    constexpr int lds = RowsShape<kPlanes<T>, KS>::Tiles::LDS;
+    constexpr int lds = RowsShape<kPlanes<T>, KS, NW>::Tiles::LDS;
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_rows_kernel<T, KS>), lds, done)) return FPQ_ERR_LAUNCH;
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_rows_kernel<T, KS, NW>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_rows_kernel<T, KS><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
+    attention_rows_kernel<T, KS, NW><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
     return FPQ_OK;
+}
+template <typename T, int KS>
+int launch_rows(const AttentionArgs& a, int waves, hipStream_t s)
+{
+    return waves == 4 ? launch_rows<T, KS, 4>(a, s) : launch_rows<T, KS, 2>(a, s);
 }
 
 template <typename T, int KS, bool VEC>
@@ -344,13 +344,13 @@ int launch_keys_form(const AttentionArgs& a, hipStream_t s)
 }
 
 template <typename T>
-int launch_forward(const AttentionArgs& a, bool by_keys, hipStream_t s)
+int launch_forward(const AttentionArgs& a, bool by_keys, int waves, hipStream_t s)
 {
     const int ks = (a.dim + 15) / 16;
     int st;
     if (!by_keys)
-        st = ks <= 3 ? launch_rows<T, 3>(a, s) : ks == 4 ? launch_rows<T, 4>(a, s) : ks == 5 ? launch_rows<T, 5>(a, s)
-           : ks == 6 ? launch_rows<T, 6>(a, s) : ks <= 8 ? launch_rows<T, 8>(a, s) : launch_rows<T, 10>(a, s);
+        st = ks <= 3 ? launch_rows<T, 3>(a, waves, s) : ks == 4 ? launch_rows<T, 4>(a, waves, s) : ks == 5 ? launch_rows<T, 5>(a, waves, s)
+           : ks == 6 ? launch_rows<T, 6>(a, waves, s) : ks <= 8 ? launch_rows<T, 8>(a, waves, s) : launch_rows<T, 10>(a, waves, s);
     else if (a.vec)
         st = ks <= 4 ? launch_keys_form<T, 4, true>(a, s) : ks <= 6 ? launch_keys_form<T, 6, true>(a, s)
            : ks <= 8 ? launch_keys_form<T, 8, true>(a, s) : launch_keys_form<T, 10, true>(a, s);
@@ -359,7 +359,7 @@ int launch_forward(const AttentionArgs& a, bool by_keys, hipStream_t s)
     if (st != FPQ_OK) return st;
     if (a.splits > 1) {
         const size_t rows = (size_t)a.batch * a.kv_heads * a.group * a.q_len;
-        attention_join_kernel<T><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s>>>(a);
+        attention_join_kernel<T><<<dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s>>>(a);
     }
     return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
 }

@@ -3,14 +3,14 @@
 
 namespace fpq {
 
-int launch_attention_f32(const AttentionArgs& a, bool by_keys, hipStream_t s);
+int launch_attention_f32(const AttentionArgs& a, bool by_keys, int waves, hipStream_t s);
 
-// Parts of an axis of `len` in units: until there are about two workgroups per compute unit, with no fewer than `least` each.
-static void cut(int64_t len, int64_t have, int unit, int64_t least, int* n, int* per)
+// Parts of an axis of `len` in units: until there are about `want` workgroups, with no fewer than `least` each.
+static void cut(int64_t len, int64_t have, int64_t want, int unit, int64_t least, int* n, int* per)
 {
-    int64_t s = have > 0 ? (512 + have - 1) / have : 1;
+    int64_t s = have > 0 ? (want + have - 1) / have : 1;
     if (s > len / least) s = len / least;
-    s = s < 1 ? 1 : s > 64 ? 64 : s;
+    s = s < 1 ? 1 : s > 32 ? 32 : s;
     if (len < 1) len = 1;
     *per = (int)(((len + s - 1) / s + unit - 1) / unit * unit);
     *n = (int)((len + *per - 1) / *per);
@@ -19,24 +19,39 @@ static void cut(int64_t len, int64_t have, int unit, int64_t least, int* n, int*
 AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int64_t dim, int type)
 {
     AttentionPlan p;
-    const int64_t bh = batch * kv_heads, rows = group * q_len, wide = (rows + 127) / 128, few = type == FPQ_TYPE_FP32 ? 64 : 32;
+    const bool fp32 = type == FPQ_TYPE_FP32;
+    const int64_t bh = batch * kv_heads, rows = group * q_len, few = fp32 ? 64 : 32;
     const int ks = (int)(dim + 15) / 16;
-    // the rows form wherever its workgroups, the keys cut into parts of at least 256, fill the compute units
-    p.by_keys = rows <= few || bh * wide * (kv_len / 256 > 1 ? kv_len / 256 : 1) < 256;
-    p.blocks = (int)(p.by_keys ? (rows + few - 1) / few : wide);
-    cut(kv_len, bh * p.blocks, 128, 256, &p.splits, &p.per_split);
-    p.q_blocks = (int)wide;
-    cut(kv_len, bh * wide, 128, 256, &p.q_splits, &p.q_per_split);
-    p.k_blocks = (int)((kv_len + 127) / 128);
-    const int tile = type == FPQ_TYPE_FP32 ? kKeysTile<3, 3> : ks <= 4 ? kKeysTile<1, 4> : ks <= 6 ? kKeysTile<1, 6> : kKeysTile<1, 8>;
+    // Two workgroups of four wavefronts per compute unit in bf16, where one's arithmetic covers the other's matrix steps; fp32 has six
+    // matrix steps for each.  Fewer rows than that: two wavefronts, and parts of the keys (of the queries, for the gradient of the
+    // keys), of no less than takes longer than the pass that joins them.  Measured over 256 or 512 workgroups and parts of no less
+    // than 64 to 512: backward of 4 x 16 heads on 4 x 2048 x 128, bf16: 604 us with 256 workgroups, 517 with 512; forward of 8 x 8 x
+    // 256 x 160, bf16: 25 us with parts of 128, 13 with 256; backward of 8 x 256 x 160, fp32: 71 us with parts of 64, 127 with
+    // 256; forward and backward of 2 x 8 x 1024 x 80, fp32: 205 us with 256 workgroups, 229 with 512.
+    const int64_t want = fp32 ? 256 : 512, least = fp32 ? 64 : 256;
+    auto waves = [&](int64_t n) { return bh * ((n + 127) / 128) >= want / 2 ? 4 : 2; };
+    auto blocks = [](int64_t n, int waves) { return (int)((n + 32 * waves - 1) / (32 * waves)); };
+    p.waves = p.q_waves = waves(rows);
+    p.q_blocks = blocks(rows, p.q_waves);
+    cut(kv_len, bh * p.q_blocks, want, (int)least, least, &p.q_splits, &p.q_per_split);
+    // keys form: few rows, or grids of the rows form that leave half of the compute units idle
+    p.by_keys = rows <= few || bh * p.q_blocks * p.q_splits < 128;
+    p.blocks = p.by_keys ? (int)((rows + few - 1) / few) : p.q_blocks;
+    if (p.by_keys)
+        cut(kv_len, bh * p.blocks, 512, 128, fp32 ? 128 : 256, &p.splits, &p.per_split);
+    else
+        p.splits = p.q_splits, p.per_split = p.q_per_split;
+    p.k_waves = waves(kv_len);
+    p.k_blocks = blocks(kv_len, p.k_waves);
+    const int tile = fp32 ? kKeysTile<3, 3> : ks <= 4 ? kKeysTile<1, 4> : ks <= 6 ? kKeysTile<1, 6> : kKeysTile<1, 8>;
     const int64_t tiles = group * ((q_len + tile - 1) / tile);
-    cut(tiles, bh * p.k_blocks, 1, 128 / tile, &p.k_splits, &p.k_per_split);
+    cut(tiles, bh * p.k_blocks, want, 1, (least + tile - 1) / tile, &p.k_splits, &p.k_per_split);
     return p;
 }
 
 int launch_attention(const AttentionArgs& a, int type, const AttentionPlan& p, hipStream_t s)
 {
-    return type == FPQ_TYPE_FP32 ? launch_attention_f32(a, p.by_keys, s) : launch_forward<__bf16>(a, p.by_keys, s);
+    return type == FPQ_TYPE_FP32 ? launch_attention_f32(a, p.by_keys, p.waves, s) : launch_forward<__bf16>(a, p.by_keys, p.waves, s);
 }
 
 }  // namespace fpq

@@ -3,6 +3,6 @@
 
 namespace fpq {
 
-int launch_attention_f32(const AttentionArgs& a, bool by_keys, hipStream_t s) { return launch_forward<float>(a, by_keys, s); }
+int launch_attention_f32(const AttentionArgs& a, bool by_keys, int waves, hipStream_t s) { return launch_forward<float>(a, by_keys, waves, s); }
 
 }  // namespace fpq
