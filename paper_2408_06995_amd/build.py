@@ -15,7 +15,8 @@ CALLS = os.path.join(HERE, "_fpqcall.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "quant.hip", "search.hip", "sparsity.hip", "rounding.hip", "gemm.hip", "gemm_dma.hip", "gemm_dma_q.hip", "gemm_dma_s.hip", "gemm_dma_sq.hip", "gemm_strip.hip", "gemm_strip_h.hip", "gemm_strip_q.hip", "gemm_wk.hip", "gemm_wk_q.hip", "gemm_wk16.hip", "gemm_wk16_h.hip", "peaks.hip", "gemm_sparse.hip", "igemm.hip",
            "api_adapt.hip", "attention_fwd.hip", "attention_fwd_f32.hip", "attention_bwd.hip", "attention_bwd_f32.hip", "attention_pack.hip", "adapter.hip",
-           "adapter_f32.hip", "adapter_mixed.hip", "adapter_bf16.hip", "adamw.hip"]
+           "adapter_map_f32.hip", "adapter_map_f32_bf16.hip", "adapter_map_f32_packed.hip", "adapter_map_bf16.hip",
+           "adapter_map_f32_bf16_packed.hip", "adapter_map_bf16_packed.hip", "adapter_outer.hip", "adamw.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

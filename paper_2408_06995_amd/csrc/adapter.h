@@ -6,9 +6,9 @@
 // Products are 16 x 16 x 32 steps of the bf16 matrix instruction with fp32 sums on operands split into planes as in attention.h: x and
 // the gradients of fp32 activations and fp32 weights three planes, bf16 ones their own, t and dt always three, so that nothing is
 // rounded below 24 bits before a result.  Lane 16 g + r: A holds row r, B column r, each the k-places 8 g .. 8 g + 7; C holds
-// column r and rows 4 g .. 4 g + 3.
+// column r and rows 4 g .. 4 g + 3.  The columns of y are tiles of the 32 x 32 x 16 instruction (attention.h).
 //
-// All of it is bound by the rows read and written (32 rows of the largest listed shapes: 16 to 64 flops per byte); the adapters
+// All of it is bound by the rows read and written (a rank of 16 makes 8 flops per byte, one of 64 in bf16 64); the adapters
 // themselves come from the caches.  Rows are cut into tiles that end with their request, so that a workgroup sees one adapter;
 // which tile a workgroup has it finds by a scan of the requests' lengths, 64 at a time.
 #pragma once
@@ -16,25 +16,43 @@
 
 namespace fpq {
 
-constexpr int kTile = 32;          // rows of a tile
 constexpr int kMaxRank = 128;
 
+// Weights of one contraction: [adapters][rows][cols], the contraction along the columns; or packed in the order in which the matrix
+// instructions take them, 64 lanes x 8 elements at a time, zeros outside the matrix:
+//   W1, steps of 32 columns:  [adapter][plane][step][group of 16 ranks][lane]: rank 16 group + lane % 16, columns 32 step + 8 (lane / 16) ..
+//   W2, blocks of 32 rows:    [adapter][plane][block][step of 16 ranks][lane]: row 32 block + lane % 32, ranks 16 step + 8 (lane / 32) ..
+struct Weights {
+    const void* p;
+    int64_t each;                   // elements of an adapter
+    int64_t plane;                  // packed: elements of a plane
+    int ld;                         // from one row to the next
+    int vec;                        // rows may be read 16 bytes at a time
+};
+
+// One call's map of rows through a rank: t = x W1^T, y = base + t W2^T.
 struct AdapterArgs {
-    const void *x, *a, *b, *base, *gy, *gx_base;
-    void *y, *gx;
-    const float *scaling;
+    const void *x, *base;
+    void* y;                        // null: t only
+    float* t;                       // [M, R], or null
+    Weights w1, w2;                 // [R, L1], [L2, R]
+    const float *scale1, *scale2;   // per adapter: of t, of what enters y; null: 1
     const int32_t *row_start, *adapter;
-    float *t, *t_part;              // t_part: parts of t over K, or null
-    const float *t_in;
-    float *dt, *ga, *gb, *part_a, *part_b;
-    int64_t ldx, ld_base, ldy, ld_gy, ld_gx_base, ld_gx;
-    int M, N, K, R, requests, adapters;
-    int parts, steps_per_part;      // of t over K
-    int columns;                    // of a workgroup that writes rows
-    int splits;                     // of the rows in the gradients of the adapters
-    int vec_r;                      // rows along the rank may be read 16 bytes at a time (t and the weights)
-    int vec_a;                      // the weights [rank, K] along K
-    int vec_y;                      // rows of results and their bases, four values at a time
+    int64_t ldx, ld_base, ldy;
+    int M, L1, L2, R, requests, adapters;
+    int vec_x;                      // rows of x, 16 bytes at a time
+};
+
+// The gradients of the adapters: out[0][a][r][k] = sum dt_m[r] x_m[k], out[1][a][n][r] = scale sum dy_m[n] t_m[r].
+struct OuterArgs {
+    const void* rows[2];            // x, dy
+    const float* t[2];              // dt, t
+    float* out[2];                  // of a part: in `part` when there are several
+    const float* scaling;
+    const int32_t *row_start, *adapter;
+    int64_t ld[2];
+    int L[2], M, R, requests, adapters, splits;
+    int vec_rows[2], vec_t;
 };
 
 // c += a b over the planes whose product counts: of x = sum_i x_i with x_i about 2^-8i of x, those with i + j <= 2.
@@ -48,7 +66,17 @@ __device__ __forceinline__ void mma16(v4f& c, const Frag<NA>& a, const Frag<NB>&
             if (sum - i >= 0 && sum - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[sum - i], c, 0, 0, 0);
 }
 
-// Operand columns from a wavefront's view of a tile in LDS: lane (g, r) gets column c0 + r of rows r0 + 8 g .. + 7.
+template <int NA, int NB>
+__device__ __forceinline__ void mma32(v16f& c, const Frag<NA>& a, const Frag<NB>& b)
+{
+#pragma unroll
+    for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (sum - i >= 0 && sum - i < NB) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[i], b.p[sum - i], c, 0, 0, 0);
+}
+
+// Operand columns of a tile in LDS: lane (g, r) gets column c0 + r of rows r0 + 8 g .. + 7.
 template <int NP>
 __device__ __forceinline__ Frag<NP> col_frag16(const __bf16* tile, int rs, int plane, int r0, int c0, int lane)
 {
@@ -67,14 +95,15 @@ __device__ __forceinline__ Frag<NP> col_frag16(const __bf16* tile, int rs, int p
 struct Rows {
     int lo, hi, adapter;            // adapter < 0: none
 };
-__device__ __forceinline__ Rows rows_of(const AdapterArgs& p, int v)
+template <typename Args>
+__device__ __forceinline__ Rows rows_of(const Args& p, int v)
 {
     Rows r = {0, 0, -1};
     if (v <= p.requests + 1) {
         const int lo = v > 0 ? p.row_start[v - 1] : 0, hi = v <= p.requests ? p.row_start[v] : p.M;
+        if (v > 0 && v <= p.requests) r.adapter = p.adapter[v - 1];
         r.lo = min(max(lo, 0), p.M);
         r.hi = max(min(hi, p.M), r.lo);
-        if (v > 0 && v <= p.requests) r.adapter = p.adapter[v - 1];
         if (r.adapter >= p.adapters) r.adapter = -1;
     }
     return r;
@@ -91,20 +120,21 @@ __device__ __forceinline__ int scan64(int v)      // inclusive sum over the lane
     return v;
 }
 
-// Tile number `tile` of all rows: its rows and adapter; lo == hi when there is no such tile.  The same for all lanes.
+// Tile number `tile` (of TM rows) of all rows: its rows and adapter; lo == hi when there is no such tile.  The same for all lanes.
+template <int TM>
 __device__ __forceinline__ Rows find_tile(const AdapterArgs& p, int tile)
 {
     for (int v0 = 0; v0 < p.requests + 2; v0 += 64) {
         const Rows r = rows_of(p, v0 + (threadIdx.x & 63));
-        const int tiles = (r.hi - r.lo + kTile - 1) / kTile, upto = scan64(tiles);
+        const int tiles = (r.hi - r.lo + TM - 1) / TM, upto = scan64(tiles);
         const uint64_t past = __ballot(upto > tile);
         if (past) {
             const int who = __ffsll((unsigned long long)past) - 1;
             Rows f;
             const int first = __shfl(upto - tiles, who);
             f.hi = __shfl(r.hi, who);
-            f.lo = __shfl(r.lo, who) + (tile - first) * kTile;
-            f.hi = min(f.hi, f.lo + kTile);
+            f.lo = __shfl(r.lo, who) + (tile - first) * TM;
+            f.hi = min(f.hi, f.lo + TM);
             f.adapter = __shfl(r.adapter, who);
             f.lo = __builtin_amdgcn_readfirstlane(f.lo);
             f.hi = __builtin_amdgcn_readfirstlane(f.hi);
@@ -116,17 +146,25 @@ __device__ __forceinline__ Rows find_tile(const AdapterArgs& p, int tile)
     return Rows{0, 0, -1};
 }
 
-static inline int64_t tiles_of(int64_t rows, int64_t requests) { return rows / kTile + requests + 2; }
-
 // Sizes only; the same for the workspace.
 struct AdapterPlan {
-    int parts, steps_per_part;      // of t over K
-    int columns_y, columns_x;       // columns of a workgroup that writes y, or dx
-    int splits;
+    int waves;                      // of a workgroup of the map: 4, or 16 (as many as the rank lets)
+    int splits;                     // of an adapter's rows in the gradients
 };
 AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters);
 
-int launch_adapter_apply(const AdapterArgs& a, int x_type, int w_type, bool vec_k, const AdapterPlan& plan, hipStream_t s);
-int launch_adapter_backward(const AdapterArgs& a, int x_type, int w_type, bool vec_n, bool vec_k, const AdapterPlan& plan, hipStream_t s);
+// Both weights of the backward call, packed: W1 from b [adapters][N][R], W2 from a [adapters][R][K].
+struct AdapterPack {
+    const void *a, *b;
+    __bf16 *w1, *w2;
+    int N, K, R, adapters;
+};
+static inline int rank_groups(int64_t R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
+static inline int64_t packed_elements(int64_t len, int64_t R) { return (len + 63) / 64 * 2 * rank_groups(R) * 512; }     // of a plane: N or K
+
+int launch_adapter_map(const AdapterArgs& a, int x_type, int w_type, bool packed, int waves, hipStream_t s);
+int launch_adapter_pack(const AdapterPack& a, int w_type, hipStream_t s);
+int launch_adapter_outer(const OuterArgs& a, int x_type, hipStream_t s);
+int launch_adapter_sums(const float* part_a, const float* part_b, int splits, size_t na, size_t nb, float* ga, float* gb, hipStream_t s);
 
 }  // namespace fpq

@@ -1,72 +1,107 @@
-// The adapters' plan of a call, the choice of its types, and the sums of partial gradients.
+// The adapters' plan of a call, the choice of its types, the packing of weights and the sums of partial gradients.
 #include "adapter.h"
 
 namespace fpq {
 
-int launch_apply_f32(const AdapterArgs& a, bool vec_k, const AdapterPlan& plan, hipStream_t s);
-int launch_apply_mixed(const AdapterArgs& a, bool vec_k, const AdapterPlan& plan, hipStream_t s);
-int launch_apply_bf16(const AdapterArgs& a, bool vec_k, const AdapterPlan& plan, hipStream_t s);
-int launch_backward_f32(const AdapterArgs& a, bool vec_n, bool vec_k, const AdapterPlan& plan, hipStream_t s);
-int launch_backward_mixed(const AdapterArgs& a, bool vec_n, bool vec_k, const AdapterPlan& plan, hipStream_t s);
-int launch_backward_bf16(const AdapterArgs& a, bool vec_n, bool vec_k, const AdapterPlan& plan, hipStream_t s);
+int launch_map_f32(const AdapterArgs& a, int waves, hipStream_t s);
+int launch_map_f32_bf16(const AdapterArgs& a, int waves, hipStream_t s);
+int launch_map_f32_packed(const AdapterArgs& a, int waves, hipStream_t s);
+int launch_map_bf16(const AdapterArgs& a, int waves, hipStream_t s);
+int launch_map_f32_bf16_packed(const AdapterArgs& a, int waves, hipStream_t s);
+int launch_map_bf16_packed(const AdapterArgs& a, int waves, hipStream_t s);
 
-// Few tiles of rows: the sums over K are cut into parts and the columns of a result go to more workgroups, until about two (four)
-// workgroups per compute unit; a part keeps two steps of 32 for each of a workgroup's wavefronts.
+// Four wavefronts per tile of 32 rows where there are enough tiles to fill the compute units; else 16, which divide the columns.
+// The gradients' rows are cut until there are about four workgroups per compute unit, with no fewer than eight tiles each.
 AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
 {
     auto clamp = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
-    const int64_t tiles = clamp(M / kTile + (requests < M ? requests : M), 1, (int64_t)1 << 31), steps = (K + 31) / 32;
     AdapterPlan p;
-    p.parts = (int)clamp(512 / tiles, 1, clamp(steps / 8, 1, 16));
-    p.steps_per_part = (int)((steps + p.parts - 1) / p.parts);
-    p.parts = (int)((steps + p.steps_per_part - 1) / p.steps_per_part);
-    auto columns = [&](int64_t L) {
-        const int64_t blocks = (L + 127) / 128, chunks = clamp(1024 / tiles, 1, blocks);
-        return (int)((blocks + chunks - 1) / chunks * 128);
-    };
-    p.columns_y = columns(N);
-    p.columns_x = columns(K);
+    p.waves = M / 32 + (requests < M / 32 ? requests : M / 32) >= 512 ? 4 : 16;
     const int64_t blocks = adapters * ((K + 127) / 128 + (N + 127) / 128);
-    p.splits = (int)clamp(1024 / (blocks > 0 ? blocks : 1), 1, clamp(M / (8 * kTile), 1, 64));
+    p.splits = (int)clamp(1024 / (blocks > 0 ? blocks : 1), 1, clamp(M / 256, 1, 64));
     (void)R;
     return p;
 }
 
 namespace {
 
-__global__ __launch_bounds__(256) void adapter_sums_kernel(AdapterArgs p, size_t na, size_t nb)
+// A lane of an operand (see Weights) per thread: blockIdx.y = 2 adapter + which.
+template <typename T>
+__global__ __launch_bounds__(256) void adapter_pack_kernel(AdapterPack p, int groups, int64_t n1, int64_t n2)
 {
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < na + nb; i += (size_t)gridDim.x * 256) {
-        const bool b = i >= na;
-        const size_t e = b ? i - na : i, n = b ? nb : na;
-        const float* const part = b ? p.part_b : p.part_a;
-        float v = part[e];
-        for (int s = 1; s < p.splits; ++s) v += part[s * n + e];
-        (b ? p.gb : p.ga)[e] = v;
+    constexpr int NP = kPlanes<T>;
+    const bool second = blockIdx.y & 1;
+    const int adapter = blockIdx.y >> 1, lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), n = second ? n2 : n1;                // an operand of 64 lanes
+    if (unit * 512 >= n) return;
+    const int64_t outer = unit / groups;
+    const int q = (int)(unit - outer * groups), L = second ? p.K : p.N;
+    const T* const src = static_cast<const T*>(second ? p.a : p.b) + (size_t)adapter * p.R * L;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        // (rank, place along N or K) of the element
+        const int rank = second ? 16 * q + 8 * (lane >> 5) + e : 16 * q + (lane & 15);
+        const int64_t at = second ? 32 * outer + (lane & 31) : 32 * outer + 8 * (lane >> 4) + e;
+        const int rc = min(rank, p.R - 1);
+        const int64_t ac = min(at, (int64_t)L - 1);
+        const float x = (float)src[second ? rc * (int64_t)L + ac : ac * p.R + rc];
+        v[e] = rank < p.R && at < L ? x : 0.0f;
     }
+    const Frag<NP> f = frag_of<NP>(v);
+    __bf16* const dst = (second ? p.w2 : p.w1) + (size_t)adapter * NP * n + unit * 512 + lane * 8;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) *reinterpret_cast<v8bf*>(dst + i * n) = f.p[i];
+}
+
+// 64 results per workgroup; its four wavefronts have a quarter of the parts each.
+__global__ __launch_bounds__(256) void adapter_sums_kernel(const float* part_a, const float* part_b, int splits, size_t na, size_t nb, float* ga, float* gb)
+{
+    __shared__ float sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const size_t i = (size_t)blockIdx.x * 64 + lane;
+    const bool b = i >= na, in = i < na + nb;
+    const size_t e = b ? i - na : i, n = b ? nb : na;
+    const float* const part = (b ? part_b : part_a) + (in ? e : 0);
+    const int each = (splits + 3) / 4, s0 = wave * each, s1 = min(s0 + each, splits);
+    float v = 0.0f;
+    for (int s = s0; s < s1; s += 4) {
+        float x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = part[min(s + u, s1 - 1) * n];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v += s + u < s1 ? x[u] : 0.0f;
+    }
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave == 0 && in) (b ? gb : ga)[e] = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
 }
 
 }  // namespace
 
-int launch_adapter_sums(const AdapterArgs& a, hipStream_t s)
+int launch_adapter_pack(const AdapterPack& a, int w_type, hipStream_t s)
 {
-    const size_t na = (size_t)a.adapters * a.R * a.K, nb = (size_t)a.adapters * a.R * a.N, want = (na + nb + 255) / 256;
-    adapter_sums_kernel<<<dim3((unsigned)(want < 4096 ? want : 4096)), dim3(256), 0, s>>>(a, na, nb);
-    return FPQ_OK;
+    const int64_t n1 = packed_elements(a.N, a.R), n2 = packed_elements(a.K, a.R), most = n1 > n2 ? n1 : n2;
+    const dim3 grid((unsigned)((most + 2047) / 2048), 2 * a.adapters);
+    const int groups = rank_groups(a.R);
+    if (w_type == FPQ_TYPE_FP32)
+        adapter_pack_kernel<float><<<grid, dim3(256), 0, s>>>(a, groups, n1, n2);
+    else
+        adapter_pack_kernel<__bf16><<<grid, dim3(256), 0, s>>>(a, groups, n1, n2);
+    return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
 }
 
-int launch_adapter_apply(const AdapterArgs& a, int x_type, int w_type, bool vec_k, const AdapterPlan& plan, hipStream_t s)
+int launch_adapter_sums(const float* part_a, const float* part_b, int splits, size_t na, size_t nb, float* ga, float* gb, hipStream_t s)
 {
-    return x_type == FPQ_TYPE_BF16   ? launch_apply_bf16(a, vec_k, plan, s)
-           : w_type == FPQ_TYPE_BF16 ? launch_apply_mixed(a, vec_k, plan, s)
-                                     : launch_apply_f32(a, vec_k, plan, s);
+    adapter_sums_kernel<<<dim3((unsigned)((na + nb + 63) / 64)), dim3(256), 0, s>>>(part_a, part_b, splits, na, nb, ga, gb);
+    return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
 }
 
-int launch_adapter_backward(const AdapterArgs& a, int x_type, int w_type, bool vec_n, bool vec_k, const AdapterPlan& plan, hipStream_t s)
+int launch_adapter_map(const AdapterArgs& a, int x_type, int w_type, bool packed, int waves, hipStream_t s)
 {
-    return x_type == FPQ_TYPE_BF16   ? launch_backward_bf16(a, vec_n, vec_k, plan, s)
-           : w_type == FPQ_TYPE_BF16 ? launch_backward_mixed(a, vec_n, vec_k, plan, s)
-                                     : launch_backward_f32(a, vec_n, vec_k, plan, s);
+    if (x_type == FPQ_TYPE_BF16) return packed ? launch_map_bf16_packed(a, waves, s) : launch_map_bf16(a, waves, s);
+    if (w_type == FPQ_TYPE_BF16) return packed ? launch_map_f32_bf16_packed(a, waves, s) : launch_map_f32_bf16(a, waves, s);
+    return packed ? launch_map_f32_packed(a, waves, s) : launch_map_f32(a, waves, s);
 }
 
 }  // namespace fpq

@@ -1,283 +1,323 @@
-// The adapters' kernels (see adapter.h).  Three shapes of work:
-//   shrink   rows x weights over a long axis -> [rows, rank]:   t (weights [rank, K]), dt (weights [N, rank])
-//   expand   [rows, rank] x weights -> rows of a long axis:     y (weights [N, rank]), dx (weights [rank, K])
-//   outer    columns of rows x [rows, rank], over the rows:     dA, dB
-// Weights whose contraction runs along their rows are read as operands from memory as they lie; the other two (dt, dx) pass through
-// a wavefront's own LDS tile and the transposing read.
+// The adapters' kernels (see adapter.h).
 #pragma once
 #include "adapter.h"
 
 namespace fpq {
 
-// Eight values along the rank, zero from R on; the branch is the same for all lanes of a launch.
-template <typename T>
-__device__ __forceinline__ void rank8(const T* row, int col, int R, int vec, float (&v)[8])
-{
-    if (vec)
-        row8<T, true>(row, col, R, v);
-    else
-        row8<T, false>(row, col, R, v);
-}
-
-// This wavefront's tile of ROWS rows from a matrix in memory: rows from `rows` on and columns from `cols` on become zero.
-template <typename T, int ROWS, int COLS, int RS>
-__device__ __forceinline__ void stage_wave(__bf16* tile, const T* base, int64_t stride, int rows, int cols, bool vec, int lane)
-{
-    constexpr int NP = kPlanes<T>, CH = COLS / 8, N = ROWS * CH, PT = (N + 63) / 64;
-    float v[PT][8];
+// ROWS rows of COLS neighbouring columns on their way from memory to a wavefront's own LDS: neighbouring lanes read neighbouring
+// pieces of a row (an operand's lanes read different rows: loaded as operands, every lane's piece is a memory access of its own, and
+// their number, not the bytes, is what bounds such a kernel).  LDS rows are 16 bytes longer than whole 64 bytes, so that 16 rows
+// start in different banks.
+template <typename T, int ROWS, int COLS, bool VEC>
+struct WaveTile {
+    static constexpr int E = 16 / (int)sizeof(T), CH = COLS / E, N = ROWS * CH, PT = (N + 63) / 64, RS = COLS + E;      // RS: elements of an LDS row
+    static constexpr int BYTES = ROWS * RS * (int)sizeof(T);
+    v4i reg[PT];
+    // row r of the tile is at base + r ld; columns from `dim` on and rows from `rows` on are not read (they hold others' values)
+    __device__ __forceinline__ void load(const T* base, unsigned ld, int rows, int col, int dim, int lane)
+    {
 #pragma unroll
-    for (int it = 0; it < PT; ++it) {
-        const int id = it * 64 + lane, row = id / CH, c = (id - row * CH) * 8;
-        const T* at = base + (int64_t)min(row, rows - 1) * stride;
-        if (vec)
-            row8<T, true>(at, c, cols, v[it]);
-        else
-            row8<T, false>(at, c, cols, v[it]);
-    }
-#pragma unroll
-    for (int it = 0; it < PT; ++it) {
-        const int id = it * 64 + lane, row = id / CH, c = (id - row * CH) * 8;
-        if (N % 64 != 0 && id >= N) continue;
-        if (row >= rows) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[it][e] = 0.0f;
-        }
-        const Frag<NP> f = frag_of<NP>(v[it]);
-#pragma unroll
-        for (int p = 0; p < NP; ++p) *reinterpret_cast<v8bf*>(tile + (p * ROWS + row) * RS + c) = f.p[p];
-    }
-}
-
-// A wavefront's own LDS writes ahead of its reads, and its reads ahead of the next writes.
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
-// TRANS false: weights [adapters][R][L] (t from x, L = K); true: [adapters][L][R] (dt from dy, L = N, scaled).
-// A workgroup takes one tile of rows and, of its part of L, its four wavefronts steps of 32 in turn.
-template <typename TX, typename TW, int RT, bool VEC, bool TRANS>
-__global__ __launch_bounds__(256) void adapter_shrink_kernel(AdapterArgs p)
-{
-    constexpr int NX = kPlanes<TX>, NW = kPlanes<TW>, RP = 16 * RT + 4, RS = 16 * RT + 8;
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
-    const Rows rows = find_tile(p, blockIdx.x);
-    if (rows.lo >= rows.hi) return;
-    const int L = TRANS ? p.N : p.K, R = p.R, count = rows.hi - rows.lo;
-    const int64_t ld = TRANS ? p.ld_gy : p.ldx;
-    float* const out = p.t_part ? p.t_part + (size_t)blockIdx.y * p.M * R : TRANS ? p.dt : p.t;
-    if (rows.adapter < 0) {
-        for (int id = threadIdx.x; id < count * R; id += 256) out[(size_t)rows.lo * R + id] = 0.0f;
-        return;
-    }
-    const TX* const x = static_cast<const TX*>(TRANS ? p.gy : p.x) + (int64_t)rows.lo * ld;
-    const TW* const w = static_cast<const TW*>(TRANS ? p.b : p.a) + (size_t)rows.adapter * R * L;
-    __bf16* const tile = reinterpret_cast<__bf16*>(lds) + wave * NW * 32 * RS;      // TRANS
-    v4f acc[RT][2];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int m = 0; m < 2; ++m) acc[r][m] = v4f{0, 0, 0, 0};
-    const int steps = (L + 31) / 32, beg = TRANS ? 0 : min((int)blockIdx.y * p.steps_per_part, steps), end = TRANS ? steps : min(beg + p.steps_per_part, steps);
-    const TX* const x0 = x + (int64_t)min(r16, count - 1) * ld;
-    const TX* const x1 = x + (int64_t)min(r16 + 16, count - 1) * ld;
-    const bool both = count > 16;
-    for (int s = beg + wave; s < end; s += 4) {
-        const int col = 32 * s + 8 * g;
-        float v[8];
-        Frag<NX> xf[2];
-        row8<TX, VEC>(x0, col, L, v);
-        xf[0] = frag_of<NX>(v);
-        if (both) {
-            row8<TX, VEC>(x1, col, L, v);
-            xf[1] = frag_of<NX>(v);
-        }
-        if (TRANS) {
-            wave_sync();
-            stage_wave<TW, 32, 16 * RT, RS>(tile, w + (size_t)32 * s * R, R, min(32, L - 32 * s), R, p.vec_r, lane);
-            wave_sync();
-        }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            Frag<NW> wf;
-            if constexpr (TRANS) {
-                wf = col_frag16<NW>(tile, RS, 32 * RS, 0, 16 * r, lane);
+        for (int i = 0; i < PT; ++i) {
+            const int id = i * 64 + lane, row = id / CH, c = col + (id - row * CH) * E;
+            const unsigned at = (unsigned)min(row, rows - 1) * ld;
+            if constexpr (VEC) {
+                reg[i] = *reinterpret_cast<const v4i*>(base + (at + (unsigned)min(c, dim - E)));
             } else {
-                const int row = 16 * r + r16;
-                row8<TW, VEC>(w + (size_t)min(row, R - 1) * L, col, L, v);
-                wf = frag_of<NW>(v);
+                T v[E];
+                v4i w;
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = base[at + (unsigned)min(c + e, dim - 1)];
+                __builtin_memcpy(&w, v, 16);
+                reg[i] = w;
             }
-            mma16<NW, NX>(acc[r][0], wf, xf[0]);
-            if (both) mma16<NW, NX>(acc[r][1], wf, xf[1]);
         }
     }
-    // the four sums of a value, in order: [wave][row][rank]
-    float* const sums = reinterpret_cast<float*>(lds);
-    __syncthreads();
+    __device__ __forceinline__ void store(unsigned char* lds, int lane) const
+    {
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-            *reinterpret_cast<v4f*>(sums + (wave * kTile + 16 * m + r16) * RP + 16 * r + 4 * g) = acc[r][m];
-    __syncthreads();
-    const float scale = TRANS ? p.scaling[rows.adapter] : 1.0f;
-    for (int id = threadIdx.x; id < count * 16 * RT; id += 256) {
-        const int m = id / (16 * RT), r = id - m * 16 * RT;
-        if (r >= R) continue;
-        const float* at = sums + m * RP + r;
-        out[(size_t)(rows.lo + m) * R + r] = scale * (((at[0] + at[kTile * RP]) + at[2 * kTile * RP]) + at[3 * kTile * RP]);
+        for (int i = 0; i < PT; ++i) {
+            const int id = i * 64 + lane, row = id / CH;
+            if (N % 64 != 0 && id >= N) continue;
+            *reinterpret_cast<v4i*>(lds + (row * RS + (id - row * CH) * E) * (int)sizeof(T)) = reg[i];
+        }
     }
-}
+    // Eight columns of a row as an operand; the first `left` of them, the others zero.
+    static __device__ __forceinline__ Frag<kPlanes<T>> frag(const unsigned char* lds, int row, int col, int left)
+    {
+        const uint4* const at = reinterpret_cast<const uint4*>(lds + (row * RS + col) * (int)sizeof(T));
+        if constexpr (sizeof(T) == 2) {
+            const uint4 w = at[0];
+            uint32_t v[4] = {w.x, w.y, w.z, w.w};
+            if (left < 8) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = 2 * e + 1 < left ? v[e] : 2 * e < left ? v[e] & 0xffffu : 0u;
+            }
+            Frag<1> f;
+            f.p[0] = __builtin_bit_cast(v8bf, make_uint4(v[0], v[1], v[2], v[3]));
+            return f;
+        } else {
+            const uint4 a = at[0], b = at[1];
+            const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(u[e]);
+            if (left < 8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = e < left ? v[e] : 0.0f;
+            }
+            return frag_of<3>(v);
+        }
+    }
+};
 
-// TRANS false: weights [adapters][L][R] (y from t, scaled, L = N); true: [adapters][R][L] (dx from dt, L = K).
-// A workgroup takes a tile of rows and p.columns columns, its wavefronts 32 columns at a time.
-template <typename TX, typename TW, int RT, bool TRANS>
-__global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs p)
+// A wavefront's LDS writes ahead of its reads, and its reads ahead of the next writes (the LDS itself keeps their order).
+__device__ __forceinline__ void wave_order() { __builtin_amdgcn_wave_barrier(); }
+
+template <int W>
+struct WeightType {
+    typedef __bf16 T;
+};
+template <>
+struct WeightType<0> {
+    typedef float T;
+};
+
+// LDS of a wavefront: a tile of x and one of weights, or the weights of 32 columns of y.
+template <typename TX, int W, int RT>
+struct MapShape {
+    typedef typename WeightType<W>::T TW;
+    static constexpr int SC = 128 / (int)sizeof(TX), RC = RT < 4 ? RT : 4;              // columns of a step; groups of 16 ranks staged at once
+    typedef WaveTile<TX, 32, SC, true> XT;
+    typedef WaveTile<TW, 16 * RC, SC, true> W1T;
+    typedef WaveTile<TW, 32, 16 * RC, true> W2T;
+    static constexpr int FIRST = XT::BYTES + (W == 3 || W == 2 ? 0 : W1T::BYTES), SECOND = W == 3 || W == 2 ? 0 : W2T::BYTES;
+    static constexpr int WAVE = FIRST > SECOND ? FIRST : SECOND;
+    static constexpr int RP = 16 * RT + 4;
+    static int bytes(int waves)
+    {
+        const int work = waves * WAVE, sums = (waves + 1) * 32 * RP * 4;                // the sums reuse it; t is behind them
+        return work > sums ? work : sums;
+    }
+};
+
+// Rows through a rank: t = scale1 x W1^T, y = base + scale2 t W2^T, in one pass.  A workgroup takes a tile of 32 rows of one request:
+// its wavefronts divide the columns of x in steps of 128 bytes, their sums meet in LDS, and they divide the columns of y, 32 at a
+// time, in tiles of the 32 x 32 instruction whose lanes hold neighbouring columns.  t never leaves the workgroup unless it is
+// asked for.  W: 0 fp32 weights, split where they are read; 1 bf16; 2, 3 packed in the order of the operands, bf16 and three
+// planes of fp32.
+template <typename TX, int W, int RT, int NWV, bool VEC, bool WVEC>
+__global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_kernel(AdapterArgs p)
 {
-    constexpr int NW = kPlanes<TW>, RK = (RT + 1) / 2, RS = 32 + 8, ROWS = 32 * RK;
+    typedef MapShape<TX, W, RT> Sh;
+    typedef typename Sh::TW TW;
+    constexpr int NX = kPlanes<TX>, NW = W == 1 || W == 2 ? 1 : 3, SC = Sh::SC, RC = Sh::RC, RP = Sh::RP;
+    constexpr bool PACKED = W >= 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
-    const Rows rows = find_tile(p, blockIdx.x);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4, l32 = lane & 31, h = lane >> 5;
+    unsigned char* const mine = lds + wave * Sh::WAVE;
+    const Rows rows = find_tile<32>(p, blockIdx.x);
     if (rows.lo >= rows.hi) return;
-    const int L = TRANS ? p.K : p.N, R = p.R, count = rows.hi - rows.lo;
-    const int cbeg = blockIdx.y * p.columns, cend = min(cbeg + p.columns, L);
-    const TX* const base = static_cast<const TX*>(TRANS ? p.gx_base : p.base);
-    TX* const y = static_cast<TX*>(TRANS ? p.gx : p.y);
-    const int64_t ldb = TRANS ? p.ld_gx_base : p.ld_base, ldy = TRANS ? p.ld_gx : p.ldy;
-    __bf16* const tile = reinterpret_cast<__bf16*>(lds) + wave * NW * ROWS * RS;    // TRANS
-    const bool some = rows.adapter >= 0, both = count > 16;
+    const int count = rows.hi - rows.lo, R = p.R;
+    const bool some = rows.adapter >= 0;
+    const size_t adapter = some ? rows.adapter : 0;
 
-    Frag<3> tf[2][RK];
-    const float scale = some && !TRANS ? p.scaling[rows.adapter] : 1.0f;
+    // Element e of a lane in a 32 x 32 tile of y is in row 8 (e / 4) + 4 h + e % 4.  (The row's offset is made where it is used: kept,
+    // it would take 32 registers.)
+    auto row_at = [&](int e, int ld) {
+        asm volatile("" : "+s"(ld));
+        return (unsigned)min(8 * (e / 4) + 4 * h + e % 4, count - 1) * (unsigned)ld;
+    };
+    const TX* const base = p.base ? static_cast<const TX*>(p.base) + (int64_t)rows.lo * p.ld_base : nullptr;
+    TX* const y = static_cast<TX*>(p.y) + (int64_t)rows.lo * p.ldy;
+    v16f have;
+    auto load_base = [&](int c0) {
+        const unsigned col = (unsigned)min(c0 + l32, p.L2 - 1);
+        if (base) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (8 * q < count) {
+#pragma unroll
+                    for (int e = 4 * q; e < 4 * q + 4; ++e) have[e] = (float)base[row_at(e, (int)p.ld_base) + col];
+                }
+        } else {
+            have = zero16();
+        }
+    };
+    int c0 = p.y ? 32 * wave : p.L2;
+    if (c0 < p.L2) load_base(c0);
+
+    Frag<3> tf[RT];
     if (some) {
-        const float* const t = TRANS ? p.dt : p.t_part ? p.t_part : p.t;
+        const TX* const x = static_cast<const TX*>(p.x) + (int64_t)rows.lo * p.ldx;
+        const TW* const w1 = static_cast<const TW*>(p.w1.p) + adapter * p.w1.each;
+        v4f acc[RT][2];
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int k = 0; k < RK; ++k) {
-                const int row = min(16 * m + r16, count - 1);
-                float v[8], u[8];
-                rank8(t + (size_t)(rows.lo + row) * R, 32 * k + 8 * g, R, p.vec_r, v);
-                if (!TRANS && p.t_part) {
-                    for (int s = 1; s < p.parts; ++s) {
-                        rank8(t + ((size_t)s * p.M + rows.lo + row) * R, 32 * k + 8 * g, R, p.vec_r, u);
+            for (int m = 0; m < 2; ++m) acc[r][m] = v4f{0, 0, 0, 0};
+        const int steps = (p.L1 + SC - 1) / SC;
+        const bool both = count > 16;
+        WaveTile<TX, 32, SC, VEC> xt;
+        WaveTile<TW, 16 * RC, SC, WVEC> wt;
+        auto load_w = [&](int q, int s) {
+            if constexpr (!PACKED)
+                wt.load(w1 + (size_t)min(16 * RC * q, R - 1) * p.w1.ld, (unsigned)p.w1.ld, max(R - 16 * RC * q, 1), s * SC, p.L1, lane);
+        };
+        if (wave < steps) {
+            xt.load(x, (unsigned)p.ldx, count, wave * SC, p.L1, lane);
+            load_w(0, wave);
+        }
+        for (int s = wave; s < steps; s += NWV) {
+            const int next = min(s + NWV, steps - 1);                     // (loaded for nothing behind the last)
+            wave_order();
+            xt.store(mine, lane);
+            if constexpr (!PACKED) wt.store(mine + Sh::XT::BYTES, lane);
+            wave_order();
+            xt.load(x, (unsigned)p.ldx, count, next * SC, p.L1, lane);
+            load_w(RT > RC ? 1 : 0, RT > RC ? s : next);
+            Frag<NX> xf[SC / 32][2];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += u[e];
-                    }
-                    if (blockIdx.y == 0 && wave == 0 && p.t && 16 * m + r16 < count) {
+            for (int k = 0; k < SC / 32; ++k)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (32 * k + 8 * g + e < R) p.t[(size_t)(rows.lo + row) * R + 32 * k + 8 * g + e] = v[e];
-                    }
-                }
+                for (int m = 0; m < 2; ++m)
+                    if (m == 0 || both) xf[k][m] = Sh::XT::frag(mine, 16 * m + r16, 32 * k + 8 * g, p.L1 - s * SC - 32 * k - 8 * g);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= scale;
-                tf[m][k] = frag_of<3>(v);
-            }
-    } else if (!TRANS && p.t_part && p.t && blockIdx.y == 0) {
-        for (int id = threadIdx.x; id < count * R; id += 256) p.t[(size_t)rows.lo * R + id] = 0.0f;
-    }
-    const TW* const w = static_cast<const TW*>(TRANS ? p.a : p.b) + (size_t)max(rows.adapter, 0) * R * L;
-    for (int c0 = cbeg + 32 * wave; c0 < cend; c0 += 128) {
-        float have[2][2][4];       // of the base: [columns][rows]
-        const bool left = c0 + 16 < cend;
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) have[c][m][e] = 0.0f;
-                const int row = min(16 * m + r16, count - 1), col = c0 + 16 * c + 4 * g;
-                if (base && (m == 0 || both) && (c == 0 || left)) {
-                    const TX* at = base + (int64_t)(rows.lo + row) * ldb;
-                    if (p.vec_y) {
-                        if (col < L) {
-                            if constexpr (sizeof(TX) == 4) {
-                                const float4 f = *reinterpret_cast<const float4*>(at + col);
-                                have[c][m][0] = f.x; have[c][m][1] = f.y; have[c][m][2] = f.z; have[c][m][3] = f.w;
-                            } else {
-                                const uint2 f = *reinterpret_cast<const uint2*>(at + col);
-                                have[c][m][0] = __uint_as_float(f.x << 16); have[c][m][1] = __uint_as_float(f.x & 0xffff0000u);
-                                have[c][m][2] = __uint_as_float(f.y << 16); have[c][m][3] = __uint_as_float(f.y & 0xffff0000u);
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) have[c][m][e] = col + e < L ? (float)at[col + e] : 0.0f;
+            for (int r = 0; r < RT; ++r) {
+                if constexpr (!PACKED && RT > RC) {
+                    if (r > 0 && r % RC == 0) {
+                        wave_order();
+                        wt.store(mine + Sh::XT::BYTES, lane);
+                        wave_order();
+                        load_w(r / RC + 1 < RT / RC ? r / RC + 1 : 0, r / RC + 1 < RT / RC ? s : next);
                     }
                 }
-            }
-        v4f acc[2][2];
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int m = 0; m < 2; ++m) acc[c][m] = v4f{0, 0, 0, 0};
-        if (some) {
-            if (TRANS) {
-                wave_sync();
-                stage_wave<TW, ROWS, 32, RS>(tile, w + c0, L, R, L - c0, p.vec_a, lane);
-                wave_sync();
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (c == 1 && !left) continue;
-#pragma unroll
-                for (int k = 0; k < RK; ++k) {
+                for (int k = 0; k < SC / 32; ++k) {
                     Frag<NW> wf;
-                    if constexpr (TRANS) {
-                        wf = col_frag16<NW>(tile, RS, ROWS * RS, 32 * k, 16 * c, lane);
+                    if constexpr (PACKED) {
+                        const v8bf* const at = reinterpret_cast<const v8bf*>(w1) + ((size_t)(s * (SC / 32) + k) * RT + r) * 64 + lane;
+#pragma unroll
+                        for (int q = 0; q < NW; ++q) wf.p[q] = at[q * (p.w1.plane / 8)];
                     } else {
-                        float v[8];
-                        rank8(w + (size_t)min(c0 + 16 * c + r16, L - 1) * R, 32 * k + 8 * g, R, p.vec_r, v);
-                        wf = frag_of<NW>(v);
+                        wf = Sh::W1T::frag(mine + Sh::XT::BYTES, 16 * (r % RC) + r16, 32 * k + 8 * g, p.L1 - s * SC - 32 * k - 8 * g);
                     }
-                    mma16<NW, 3>(acc[c][0], wf, tf[0][k]);
-                    if (both) mma16<NW, 3>(acc[c][1], wf, tf[1][k]);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+                        if (m == 0 || both) mma16<NW, NX>(acc[r][m], wf, xf[k][m]);
                 }
             }
         }
+        // the wavefronts' sums of a value, in order
+        float* const sums = reinterpret_cast<float*>(lds);                // [NWV][32][RP], then t: [32][RP]
+        float* const ts = sums + NWV * 32 * RP;
+        __syncthreads();
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const int row = 16 * m + r16, col = c0 + 16 * c + 4 * g;
-                if (row >= count || (c == 1 && !left)) continue;
-                const float v[4] = {have[c][m][0] + acc[c][m][0], have[c][m][1] + acc[c][m][1], have[c][m][2] + acc[c][m][2],
-                                    have[c][m][3] + acc[c][m][3]};
-                store4(y + (int64_t)(rows.lo + row) * ldy, col, L, p.vec_y, v);
+            for (int m = 0; m < 2; ++m) *reinterpret_cast<v4f*>(sums + (wave * 32 + 16 * m + r16) * RP + 16 * r + 4 * g) = acc[r][m];
+        __syncthreads();
+        const float scale1 = p.scale1 ? p.scale1[adapter] : 1.0f, scale2 = p.scale2 ? p.scale2[adapter] : 1.0f;
+        for (int id = threadIdx.x; id < 32 * 16 * RT; id += 64 * NWV) {
+            const int m = id / (16 * RT), r = id - m * 16 * RT;
+            float v = 0.0f;
+            if (r < R && m < count) {
+#pragma unroll
+                for (int w = 0; w < NWV; ++w) v += sums[(w * 32 + m) * RP + r];
+                v *= scale1;
+                if (p.t) p.t[(size_t)(rows.lo + m) * R + r] = v;
+                v *= scale2;
             }
+            ts[m * RP + r] = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < RT; ++k) {
+            float v[8];
+            *reinterpret_cast<v4f*>(v) = *reinterpret_cast<const v4f*>(ts + l32 * RP + 16 * k + 8 * h);
+            *reinterpret_cast<v4f*>(v + 4) = *reinterpret_cast<const v4f*>(ts + l32 * RP + 16 * k + 8 * h + 4);
+            tf[k] = frag_of<3>(v);
+        }
+        __syncthreads();                                                  // (the weights' tiles reuse t's place)
+    } else if (p.t) {
+        for (int id = threadIdx.x; id < count * R; id += 64 * NWV) p.t[(size_t)rows.lo * R + id] = 0.0f;
+    }
+
+    // columns of y: the base's values and the weights of the wavefront's next 32 are loaded ahead of this one's products
+    const TW* const w2 = static_cast<const TW*>(p.w2.p) + adapter * p.w2.each;
+    WaveTile<TW, 32, 16 * RC, WVEC> wt;
+    auto load_w = [&](int q, int c0) { wt.load(w2 + (size_t)c0 * p.w2.ld, (unsigned)p.w2.ld, p.L2 - c0, 16 * RC * q, R, lane); };
+    if (!PACKED && some && c0 < p.L2) load_w(0, c0);
+    for (; c0 < p.L2; c0 += 32 * NWV) {
+        const int next = c0 + 32 * NWV < p.L2 ? c0 + 32 * NWV : c0;       // (loaded for nothing behind the last)
+        v16f acc = have;
+        if (some) {
+            Frag<NW> wf[PACKED ? RT : 1];
+            if constexpr (PACKED) {
+                const v8bf* const at = reinterpret_cast<const v8bf*>(w2) + (size_t)(c0 / 32) * RT * 64 + lane;
+#pragma unroll
+                for (int k = 0; k < RT; ++k)
+#pragma unroll
+                    for (int q = 0; q < NW; ++q) wf[k].p[q] = at[k * 64 + q * (p.w2.plane / 8)];
+            }
+            load_base(next);
+#pragma unroll
+            for (int k = 0; k < RT; ++k) {
+                if constexpr (PACKED) {
+                    mma32<3, NW>(acc, tf[k], wf[k]);
+                } else {
+                    if (k % RC == 0) {
+                        wave_order();
+                        wt.store(mine, lane);
+                        wave_order();
+                        if (k / RC + 1 < RT / RC)
+                            load_w(k / RC + 1, c0);
+                        else
+                            load_w(0, next);
+                    }
+                    mma32<3, NW>(acc, tf[k], Sh::W2T::frag(mine, l32, 16 * (k % RC) + 8 * h, R - 16 * k - 8 * h));
+                }
+            }
+        } else {
+            load_base(next);
+        }
+        const unsigned col = c0 + l32;
+        if (col < (unsigned)p.L2) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (8 * q < count) {
+#pragma unroll
+                    for (int e = 4 * q; e < 4 * q + 4; ++e)
+                        if (8 * q + 4 * h + e % 4 < count) y[row_at(e, (int)p.ldy) + col] = (TX)acc[e];
+                }
+        }
     }
 }
 
 constexpr int kListed = 512;        // requests that a workgroup looks over at a time
 
-// B false: dA[a][r][k] from dt and x; true: dB[a][n][r] from dy and t, scaled.
-// A workgroup has 128 columns of one adapter's rows; of the adapter's tiles of 32 rows it takes its share of p.splits.
+// The gradients of the adapters.  A workgroup has 128 columns of x (B false: dA) or dy (true: dB) and of an adapter's tiles of 32 rows
+// its share of p.splits; both kinds are in one launch.
 template <typename TX, int RT, bool VEC, bool B>
-__global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterArgs p)
+__device__ __forceinline__ void outer(const OuterArgs& p, unsigned char* lds, int chunk)
 {
     constexpr int NX = kPlanes<TX>, CS = kRowStride<8>, RS = kRowStride<RT>;
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     __bf16* const xt = reinterpret_cast<__bf16*>(lds);                   // [NX][32][CS]
     __bf16* const tt = xt + NX * 32 * CS;                                // [3][32][RS]
     int* const upto = reinterpret_cast<int*>(tt + 3 * 32 * RS);          // [kListed + 1] tiles ahead of a request, [kListed] first rows
     int* const first = upto + kListed + 1;
-    int* const wsum = first + kListed;                                   // [8]
+    int* const wsum = first + kListed;                                   // [4]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
-    const int L = B ? p.N : p.K, R = p.R, c0 = blockIdx.x * 128, adapter = blockIdx.y, split = blockIdx.z;
-    const TX* const x = static_cast<const TX*>(B ? p.gy : p.x) + c0;
-    const int64_t ld = B ? p.ld_gy : p.ldx;
-    const float* const t = B ? p.t_in : p.dt;
+    const int L = p.L[B], R = p.R, c0 = chunk * 128, adapter = blockIdx.y, split = blockIdx.z;
+    const TX* const x = static_cast<const TX*>(p.rows[B]) + c0;
+    const int64_t ld = p.ld[B];
+    const float* const t = p.t[B];
     v4f acc[2][RT];
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[c][r] = v4f{0, 0, 0, 0};
     Stage<TX, 8, VEC, 32, 256> sx;
-    Stage<float, RT, true, 32, 256> sv;
-    Stage<float, RT, false, 32, 256> ss;
+    Stage<float, RT, VEC, 32, 256> st;
     for (int q0 = 1; q0 <= p.requests; q0 += kListed) {
         __syncthreads();
         int before = 0;                              // tiles of this adapter in the requests listed so far
@@ -285,7 +325,7 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterArgs p)
             const int v = q0 + part + tid;
             Rows r = {0, 0, -1};
             if (v <= p.requests) r = rows_of(p, v);
-            const int tiles = r.adapter == adapter ? (r.hi - r.lo + kTile - 1) / kTile : 0, sum = scan64(tiles);
+            const int tiles = r.adapter == adapter ? (r.hi - r.lo + 31) / 32 : 0, sum = scan64(tiles);
             if (lane == 63) wsum[wave] = sum;
             __syncthreads();
             int ahead = before + sum - tiles;
@@ -311,22 +351,16 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterArgs p)
                     b = m;
             }
             const Rows r = rows_of(p, q0 + a);
-            lo = first[a] + (tile - upto[a]) * kTile;
-            hi = min(r.hi, lo + kTile);
+            lo = first[a] + (tile - upto[a]) * 32;
+            hi = min(r.hi, lo + 32);
             sx.load(x, ld, lo, hi - 1, L - c0, tid);
-            if (p.vec_r)
-                sv.load(t, R, lo, hi - 1, R, tid);
-            else
-                ss.load(t, R, lo, hi - 1, R, tid);
+            st.load(t, R, lo, hi - 1, R, tid);
         };
         if (tbeg < tend) load(tbeg);
         for (int tile = tbeg; tile < tend; ++tile) {
             __syncthreads();
             sx.store(xt, lo, hi, L - c0, tid);
-            if (p.vec_r)
-                sv.store(tt, lo, hi, R, tid);
-            else
-                ss.store(tt, lo, hi, R, tid);
+            st.store(tt, lo, hi, R, tid);
             __syncthreads();
             if (tile + 1 < tend) load(tile + 1);
             Frag<NX> xf[2];
@@ -346,8 +380,7 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterArgs p)
         }
     }
     const float scale = B ? p.scaling[adapter] : 1.0f;
-    const size_t each = (size_t)p.adapters * L * R;
-    float* const out = (p.splits > 1 ? (B ? p.part_b : p.part_a) + split * each : B ? p.gb : p.ga) + (size_t)adapter * L * R;
+    float* const out = p.out[B] + (size_t)split * p.adapters * L * R + (size_t)adapter * L * R;
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -360,72 +393,69 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterArgs p)
             }
 }
 
-template <typename TX, typename TW, int RT, bool VEC, bool TRANS>
-int launch_shrink(const AdapterArgs& a, int parts, hipStream_t s)
+template <typename TX, int RT, bool VEC>
+__global__ __launch_bounds__(256) void adapter_outer_kernel(OuterArgs p)
 {
-    constexpr int tile = TRANS ? 4 * kPlanes<TW> * 32 * (16 * RT + 8) * 2 : 0, sums = 4 * kTile * (16 * RT + 4) * 4, lds = tile > sums ? tile : sums;
+    extern __shared__ __attribute__((aligned(16))) unsigned char outer_lds[];
+    const int chunks_a = (p.L[0] + 127) / 128;
+    if ((int)blockIdx.x < chunks_a)
+        outer<TX, RT, VEC, false>(p, outer_lds, blockIdx.x);
+    else
+        outer<TX, RT, VEC, true>(p, outer_lds, blockIdx.x - chunks_a);
+}
+
+template <typename TX, int W, int RT, int NWV, bool VEC, bool WVEC>
+int launch_map(const AdapterArgs& a, hipStream_t s)
+{
+    const int lds = MapShape<TX, W, RT>::bytes(NWV);
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&adapter_shrink_kernel<TX, TW, RT, VEC, TRANS>), lds, done)) return FPQ_ERR_LAUNCH;
-    adapter_shrink_kernel<TX, TW, RT, VEC, TRANS><<<dim3((unsigned)tiles_of(a.M, a.requests), parts), dim3(256), lds, s>>>(a);
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&adapter_map_kernel<TX, W, RT, NWV, VEC, WVEC>), lds, done)) return FPQ_ERR_LAUNCH;
+    const int64_t tiles = (int64_t)a.M / 32 + a.requests + 2;
+    adapter_map_kernel<TX, W, RT, NWV, VEC, WVEC><<<dim3((unsigned)tiles), dim3(64 * NWV), lds, s>>>(a);
     return FPQ_OK;
 }
 
-template <typename TX, typename TW, int RT, bool TRANS>
-int launch_expand(AdapterArgs a, int columns, hipStream_t s)
+template <typename TX, int W, int RT, int NWV>
+int map_of_tile(const AdapterArgs& a, hipStream_t s)
 {
-    constexpr int lds = TRANS ? 4 * kPlanes<TW> * 32 * ((RT + 1) / 2) * 40 * 2 : 0;
-    static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&adapter_expand_kernel<TX, TW, RT, TRANS>), lds, done)) return FPQ_ERR_LAUNCH;
-    a.columns = columns;
-    const int L = TRANS ? a.K : a.N;
-    adapter_expand_kernel<TX, TW, RT, TRANS><<<dim3((unsigned)tiles_of(a.M, a.requests), (L + columns - 1) / columns), dim3(256), lds, s>>>(a);
-    return FPQ_OK;
+    if (a.w1.vec && a.w2.vec) return a.vec_x ? launch_map<TX, W, RT, NWV, true, true>(a, s) : launch_map<TX, W, RT, NWV, false, true>(a, s);
+    if constexpr (W >= 2)
+        return FPQ_ERR_UNSUPPORTED;                  // (packed weights always are)
+    else
+        return a.vec_x ? launch_map<TX, W, RT, NWV, true, false>(a, s) : launch_map<TX, W, RT, NWV, false, false>(a, s);
 }
 
-template <typename TX, int RT, bool VEC, bool B>
-int launch_outer(const AdapterArgs& a, hipStream_t s)
+template <typename TX, int W, int RT>
+int map_of_rank(const AdapterArgs& a, int waves, hipStream_t s)
 {
-    constexpr int lds = kPlanes<TX> * 32 * kRowStride<8> * 2 + 3 * 32 * kRowStride<RT> * 2 + (2 * kListed + 16) * 4;
-    static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&adapter_outer_kernel<TX, RT, VEC, B>), lds, done)) return FPQ_ERR_LAUNCH;
-    const int L = B ? a.N : a.K;
-    adapter_outer_kernel<TX, RT, VEC, B><<<dim3((L + 127) / 128, a.adapters, a.splits), dim3(256), lds, s>>>(a);
-    return FPQ_OK;
+    constexpr int many = RT <= 2 ? 16 : 8;                                // (registers)
+    return waves == 16 ? map_of_tile<TX, W, RT, many>(a, s) : map_of_tile<TX, W, RT, 4>(a, s);
 }
 
-template <typename TX, typename TW, int RT>
-int apply_of_rank(const AdapterArgs& a, bool vec_k, const AdapterPlan& plan, hipStream_t s)
+template <typename TX, int W>
+int launch_map(const AdapterArgs& a, int waves, hipStream_t s)
 {
-    const int st = vec_k ? launch_shrink<TX, TW, RT, true, false>(a, plan.parts, s) : launch_shrink<TX, TW, RT, false, false>(a, plan.parts, s);
-    return st != FPQ_OK ? st : launch_expand<TX, TW, RT, false>(a, plan.columns_y, s);
-}
-
-template <typename TX, typename TW>
-int launch_apply(const AdapterArgs& a, bool vec_k, const AdapterPlan& plan, hipStream_t s)
-{
-    const int st = a.R <= 16 ? apply_of_rank<TX, TW, 1>(a, vec_k, plan, s) : a.R <= 32 ? apply_of_rank<TX, TW, 2>(a, vec_k, plan, s)
-                 : a.R <= 64 ? apply_of_rank<TX, TW, 4>(a, vec_k, plan, s) : apply_of_rank<TX, TW, 8>(a, vec_k, plan, s);
+    const int st = a.R <= 16 ? map_of_rank<TX, W, 1>(a, waves, s) : a.R <= 32 ? map_of_rank<TX, W, 2>(a, waves, s)
+                 : a.R <= 64 ? map_of_rank<TX, W, 4>(a, waves, s) : map_of_rank<TX, W, 8>(a, waves, s);
     return st != FPQ_OK ? st : hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
 }
 
-int launch_adapter_sums(const AdapterArgs& a, hipStream_t s);
-
-template <typename TX, typename TW, int RT>
-int backward_of_rank(const AdapterArgs& a, bool vec_n, bool vec_k, const AdapterPlan& plan, hipStream_t s)
+template <typename TX, int RT, bool VEC>
+int launch_outer(const OuterArgs& a, hipStream_t s)
 {
-    int st = vec_n ? launch_shrink<TX, TW, RT, true, true>(a, 1, s) : launch_shrink<TX, TW, RT, false, true>(a, 1, s);
-    if (st == FPQ_OK && a.gx) st = launch_expand<TX, TW, RT, true>(a, plan.columns_x, s);
-    if (st == FPQ_OK) st = vec_k ? launch_outer<TX, RT, true, false>(a, s) : launch_outer<TX, RT, false, false>(a, s);
-    if (st == FPQ_OK) st = vec_n ? launch_outer<TX, RT, true, true>(a, s) : launch_outer<TX, RT, false, true>(a, s);
-    return st;
+    constexpr int lds = kPlanes<TX> * 32 * kRowStride<8> * 2 + 3 * 32 * kRowStride<RT> * 2 + (2 * kListed + 8) * 4;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&adapter_outer_kernel<TX, RT, VEC>), lds, done)) return FPQ_ERR_LAUNCH;
+    const int chunks = (a.L[0] + 127) / 128 + (a.L[1] + 127) / 128;
+    adapter_outer_kernel<TX, RT, VEC><<<dim3(chunks, a.adapters, a.splits), dim3(256), lds, s>>>(a);
+    return FPQ_OK;
 }
 
-template <typename TX, typename TW>
-int launch_backward(const AdapterArgs& a, bool vec_n, bool vec_k, const AdapterPlan& plan, hipStream_t s)
+template <typename TX, bool VEC>
+int launch_outer(const OuterArgs& a, hipStream_t s)
 {
-    int st = a.R <= 16 ? backward_of_rank<TX, TW, 1>(a, vec_n, vec_k, plan, s) : a.R <= 32 ? backward_of_rank<TX, TW, 2>(a, vec_n, vec_k, plan, s)
-           : a.R <= 64 ? backward_of_rank<TX, TW, 4>(a, vec_n, vec_k, plan, s) : backward_of_rank<TX, TW, 8>(a, vec_n, vec_k, plan, s);
-    if (st == FPQ_OK && a.splits > 1) st = launch_adapter_sums(a, s);
+    const int st = a.R <= 16 ? launch_outer<TX, 1, VEC>(a, s) : a.R <= 32 ? launch_outer<TX, 2, VEC>(a, s) : a.R <= 64 ? launch_outer<TX, 4, VEC>(a, s)
+                                                                                                            : launch_outer<TX, 8, VEC>(a, s);
     return st != FPQ_OK ? st : hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
 }
 

@@ -10,7 +10,7 @@ using namespace fpq;
 
 namespace {
 
-constexpr int64_t kMost = (int64_t)1 << 30;
+constexpr int64_t kMost = (int64_t)1 << 30, kMostColumns = (int64_t)1 << 24;
 
 size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
 size_t size_of(int type) { return type == FPQ_TYPE_FP32 ? 4 : 2; }
@@ -145,7 +145,7 @@ int check_adapter_sizes(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requ
         if (v < 0 || v > kMost) return FPQ_ERR_SHAPE;
     if (N == 0 || K == 0 || R == 0 || adapters == 0 || adapters > 65535) return FPQ_ERR_SHAPE;
     if (R > kMaxRank) return FPQ_ERR_UNSUPPORTED;
-    if (R * K > kMost || R * N > kMost) return FPQ_ERR_SHAPE;
+    if (N > kMostColumns || K > kMostColumns) return FPQ_ERR_SHAPE;
     return FPQ_OK;
 }
 
@@ -154,6 +154,9 @@ bool matrix_aligned(const void* p, int64_t ld, int64_t rows, size_t size, size_t
 {
     return aligned(p, to) && (rows <= 1 || ld * (int64_t)size % (int64_t)to == 0);
 }
+
+// A tile of rows is addressed with 32-bit offsets.
+bool stride_ok(int64_t ld, int64_t cols) { return ld >= cols && ld <= kMostColumns; }
 
 // Sizes and pointers that both calls have; a row of fewer elements than its stride's claim is an error.
 int check_adapter(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b)
@@ -164,7 +167,7 @@ int check_adapter(const fpq_adapter_args_t* p, const void* x, const void* a, con
     if (p->x_type == FPQ_TYPE_BF16 && p->w_type != FPQ_TYPE_BF16) return FPQ_ERR_UNSUPPORTED;
     const int st = check_adapter_sizes(p->M, p->N, p->K, p->R, p->requests, p->adapters);
     if (st != FPQ_OK) return st;
-    if (p->M && p->ld_x < p->K) return FPQ_ERR_SHAPE;
+    if (p->M && !stride_ok(p->ld_x, p->K)) return FPQ_ERR_SHAPE;
     if (!p->scaling || !p->row_start || (p->requests && !p->adapter) || !a || !b || (p->M && !x)) return FPQ_ERR_NULL;
     if (!aligned(p->scaling, 4) || !aligned(p->row_start, 4) || !aligned(p->adapter, 4) || !aligned(x, size_of(p->x_type)) ||
         !aligned(a, size_of(p->w_type)) || !aligned(b, size_of(p->w_type)))
@@ -172,26 +175,22 @@ int check_adapter(const fpq_adapter_args_t* p, const void* x, const void* a, con
     return FPQ_OK;
 }
 
-AdapterArgs args_of(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b, const float* t)
+AdapterArgs args_of(const fpq_adapter_args_t* p)
 {
     AdapterArgs r{};
-    r.x = x;
-    r.a = a;
-    r.b = b;
-    r.scaling = p->scaling;
     r.row_start = p->row_start;
     r.adapter = p->adapter;
-    r.ldx = p->ld_x;
     r.M = (int)p->M;
-    r.N = (int)p->N;
-    r.K = (int)p->K;
     r.R = (int)p->R;
     r.requests = (int)p->requests;
     r.adapters = (int)p->adapters;
-    const size_t w = size_of(p->w_type);
-    r.vec_r = p->R % 8 == 0 && aligned(b, 16) && aligned(t, 16);
-    r.vec_a = p->K * w % 16 == 0 && aligned(a, 16);
     return r;
+}
+
+// Bytes of a pool's packed weights along `len`, fp32 or bf16.
+size_t packed_weights(int w_type, int64_t adapters, int64_t len, int64_t R)
+{
+    return align_up((size_t)adapters * packed_elements(len, R) * 2 * (w_type == FPQ_TYPE_FP32 ? 3 : 1));
 }
 
 bool finite_not_negative(double v) { return v >= 0.0 && !isinf(v); }
@@ -202,38 +201,38 @@ extern "C" {
 
 size_t fpq_adapter_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
 {
-    if (check_adapter_sizes(M, N, K, R, requests, adapters) != FPQ_OK) return 0;
-    // t of each part of K; of the only one when the caller wants none
-    return align_up((size_t)plan_adapter(M, N, K, R, requests, adapters).parts * M * R * 4);
+    (void)check_adapter_sizes(M, N, K, R, requests, adapters);
+    return 0;                                              // t stays in the workgroups
 }
 
 int fpq_adapter_apply(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b, const void* base, void* y, float* t,
                       void* workspace, size_t workspace_bytes, void* stream)
 {
+    (void)workspace;
+    (void)workspace_bytes;
     const int st = check_adapter(p, x, a, b);
     if (st != FPQ_OK) return st;
     if (p->M == 0) return FPQ_OK;
     if (!y) return FPQ_ERR_NULL;
-    if (p->ld_y < p->N || (base && p->ld_base < p->N)) return FPQ_ERR_SHAPE;
-    const size_t size = size_of(p->x_type);
+    if (!stride_ok(p->ld_y, p->N) || (base && !stride_ok(p->ld_base, p->N))) return FPQ_ERR_SHAPE;
+    const size_t size = size_of(p->x_type), w = size_of(p->w_type);
     if (!aligned(y, size) || !aligned(base, size) || !aligned(t, 4)) return FPQ_ERR_ALIGN;
     const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->R, p->requests, p->adapters);
-    if (plan.parts > 1 || !t) {
-        if (!workspace || workspace_bytes < fpq_adapter_workspace_size(p->M, p->N, p->K, p->R, p->requests, p->adapters)) return FPQ_ERR_WORKSPACE;
-        if (!aligned(workspace, 16)) return FPQ_ERR_ALIGN;
-    }
-    AdapterArgs r = args_of(p, x, a, b, t);
+    AdapterArgs r = args_of(p);
+    r.x = x;
+    r.ldx = p->ld_x;
     r.base = base;
-    r.y = y;
     r.ld_base = p->ld_base;
+    r.y = y;
     r.ldy = p->ld_y;
-    r.parts = plan.parts;
-    r.steps_per_part = plan.steps_per_part;
-    r.t = t || plan.parts > 1 ? t : static_cast<float*>(workspace);
-    r.t_part = plan.parts > 1 ? static_cast<float*>(workspace) : nullptr;
-    r.vec_y = p->N % 4 == 0 && matrix_aligned(y, p->ld_y, p->M, size, 4 * size) && (!base || matrix_aligned(base, p->ld_base, p->M, size, 4 * size));
-    const bool vec_k = r.vec_a && p->K * size % 16 == 0 && matrix_aligned(x, p->ld_x, p->M, size, 16);
-    return launch_adapter_apply(r, p->x_type, p->w_type, vec_k, plan, static_cast<hipStream_t>(stream));
+    r.t = t;
+    r.w1 = Weights{a, p->R * p->K, 0, (int)p->K, p->K * w % 16 == 0 && aligned(a, 16)};
+    r.w2 = Weights{b, p->N * p->R, 0, (int)p->R, p->R * w % 16 == 0 && aligned(b, 16)};
+    r.scale2 = p->scaling;
+    r.L1 = (int)p->K;
+    r.L2 = (int)p->N;
+    r.vec_x = p->K * size % 16 == 0 && matrix_aligned(x, p->ld_x, p->M, size, 16);
+    return launch_adapter_map(r, p->x_type, p->w_type, false, plan.waves, static_cast<hipStream_t>(stream));
 }
 
 size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
@@ -241,7 +240,8 @@ size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int6
     if (check_adapter_sizes(M, N, K, R, requests, adapters) != FPQ_OK) return 0;
     const AdapterPlan plan = plan_adapter(M, N, K, R, requests, adapters);
     const size_t each = (size_t)adapters * R * 4;
-    return align_up((size_t)M * R * 4) + (plan.splits > 1 ? align_up(plan.splits * each * K) + align_up(plan.splits * each * N) : 0);
+    return align_up((size_t)M * R * 4) + packed_weights(FPQ_TYPE_FP32, adapters, N, R) + packed_weights(FPQ_TYPE_FP32, adapters, K, R) +
+           (plan.splits > 1 ? align_up(plan.splits * each * K) + align_up(plan.splits * each * N) : 0);
 }
 
 int fpq_adapter_backward(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b, const float* t, const void* grad_y,
@@ -250,35 +250,75 @@ int fpq_adapter_backward(const fpq_adapter_args_t* p, const void* x, const void*
     const int st = check_adapter(p, x, a, b);
     if (st != FPQ_OK) return st;
     if (!grad_a || !grad_b || (p->M && (!t || !grad_y))) return FPQ_ERR_NULL;
-    if (p->M && (p->ld_grad_y < p->N || (grad_x && (p->ld_grad_x < p->K || (grad_x_base && p->ld_grad_x_base < p->K))))) return FPQ_ERR_SHAPE;
+    if (p->M && !stride_ok(p->ld_grad_y, p->N)) return FPQ_ERR_SHAPE;
+    if (p->M && grad_x && (!stride_ok(p->ld_grad_x, p->K) || (grad_x_base && !stride_ok(p->ld_grad_x_base, p->K)))) return FPQ_ERR_SHAPE;
     const size_t size = size_of(p->x_type);
     if (!aligned(t, 4) || !aligned(grad_y, size) || !aligned(grad_x_base, size) || !aligned(grad_x, size) || !aligned(grad_a, 4) || !aligned(grad_b, 4))
         return FPQ_ERR_ALIGN;
     const size_t need = fpq_adapter_backward_workspace_size(p->M, p->N, p->K, p->R, p->requests, p->adapters);
-    if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;
-    if (need && !aligned(workspace, 16)) return FPQ_ERR_ALIGN;
+    if (!workspace || workspace_bytes < need) return FPQ_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return FPQ_ERR_ALIGN;
     const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->R, p->requests, p->adapters);
-    AdapterArgs r = args_of(p, x, a, b, t);
-    r.t_in = t;
-    r.gy = grad_y;
-    r.ld_gy = p->ld_grad_y;
-    r.gx_base = grad_x_base;
-    r.ld_gx_base = p->ld_grad_x_base;
-    r.gx = p->M ? grad_x : nullptr;
-    r.ld_gx = p->ld_grad_x;
-    r.ga = grad_a;
-    r.gb = grad_b;
-    r.splits = plan.splits;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int N = (int)p->N, K = (int)p->K, R = (int)p->R;
     char* at = static_cast<char*>(workspace);
-    r.dt = reinterpret_cast<float*>(at);
-    at += align_up((size_t)p->M * p->R * 4);
-    r.part_a = reinterpret_cast<float*>(at);
-    r.part_b = reinterpret_cast<float*>(at + align_up((size_t)plan.splits * p->adapters * p->R * p->K * 4));
-    r.vec_y = p->K % 4 == 0 && matrix_aligned(grad_x, p->ld_grad_x, p->M, size, 4 * size) &&
-              (!grad_x_base || matrix_aligned(grad_x_base, p->ld_grad_x_base, p->M, size, 4 * size));
-    const bool vec_n = p->N * size % 16 == 0 && matrix_aligned(grad_y, p->ld_grad_y, p->M, size, 16);
-    const bool vec_k = p->K * size % 16 == 0 && matrix_aligned(x, p->ld_x, p->M, size, 16);
-    return launch_adapter_backward(r, p->x_type, p->w_type, vec_n, vec_k, plan, static_cast<hipStream_t>(stream));
+    auto take = [&](size_t bytes) {
+        char* const r = at;
+        at += bytes;
+        return r;
+    };
+    float* const dt = reinterpret_cast<float*>(take(align_up((size_t)p->M * R * 4)));
+    int done = FPQ_OK;
+    if (p->M) {
+        AdapterPack pack{a, b, nullptr, nullptr, N, K, R, (int)p->adapters};
+        pack.w1 = reinterpret_cast<__bf16*>(take(packed_weights(p->w_type, p->adapters, N, R)));
+        pack.w2 = reinterpret_cast<__bf16*>(take(packed_weights(p->w_type, p->adapters, K, R)));
+        done = launch_adapter_pack(pack, p->w_type, s);
+        if (done != FPQ_OK) return done;
+        AdapterArgs r = args_of(p);
+        r.x = grad_y;
+        r.ldx = p->ld_grad_y;
+        r.base = grad_x ? grad_x_base : nullptr;
+        r.ld_base = p->ld_grad_x_base;
+        r.y = grad_x;
+        r.ldy = p->ld_grad_x;
+        r.t = dt;
+        const int64_t planes = p->w_type == FPQ_TYPE_FP32 ? 3 : 1, n1 = packed_elements(N, R), n2 = packed_elements(K, R);
+        r.w1 = Weights{pack.w1, planes * n1, n1, 0, 1};
+        r.w2 = Weights{pack.w2, planes * n2, n2, 0, 1};
+        r.scale1 = p->scaling;
+        r.L1 = N;
+        r.L2 = K;
+        r.vec_x = p->N * size % 16 == 0 && matrix_aligned(grad_y, p->ld_grad_y, p->M, size, 16);
+        done = launch_adapter_map(r, p->x_type, p->w_type, true, plan.waves, s);
+        if (done != FPQ_OK) return done;
+    }
+    const size_t na = (size_t)p->adapters * R * K, nb = (size_t)p->adapters * R * N;
+    OuterArgs o{};
+    o.rows[0] = x;
+    o.rows[1] = grad_y;
+    o.ld[0] = p->ld_x;
+    o.ld[1] = p->ld_grad_y;
+    o.t[0] = dt;
+    o.t[1] = t;
+    o.L[0] = K;
+    o.L[1] = N;
+    o.scaling = p->scaling;
+    o.row_start = p->row_start;
+    o.adapter = p->adapter;
+    o.M = (int)p->M;
+    o.R = R;
+    o.requests = (int)p->requests;
+    o.adapters = (int)p->adapters;
+    o.splits = plan.splits;
+    o.out[0] = plan.splits > 1 ? reinterpret_cast<float*>(take(align_up(plan.splits * na * 4))) : grad_a;
+    o.out[1] = plan.splits > 1 ? reinterpret_cast<float*>(take(align_up(plan.splits * nb * 4))) : grad_b;
+    o.vec_rows[0] = p->K * size % 16 == 0 && matrix_aligned(x, p->ld_x, p->M, size, 16);
+    o.vec_rows[1] = p->N * size % 16 == 0 && matrix_aligned(grad_y, p->ld_grad_y, p->M, size, 16);
+    o.vec_t = R % 4 == 0 && aligned(t, 16);
+    done = launch_adapter_outer(o, p->x_type, s);
+    if (done != FPQ_OK || plan.splits == 1) return done;
+    return launch_adapter_sums(o.out[0], o.out[1], plan.splits, na, nb, grad_a, grad_b, s);
 }
 
 size_t fpq_adamw_plan_size(const fpq_adamw_tensor_t* tensors, int count)
