@@ -151,7 +151,7 @@ struct AdapterPlan {
     int waves;                      // of a workgroup of the map: 4, or 16 (as many as the rank lets)
     int splits;                     // of an adapter's rows in the gradients
 };
-AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters);
+AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t requests, int64_t adapters);
 
 // Both weights of the backward call, packed: W1 from b [adapters][N][R], W2 from a [adapters][R][K].
 struct AdapterPack {

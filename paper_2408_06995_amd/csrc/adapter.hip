@@ -10,16 +10,18 @@ int launch_map_bf16(const AdapterArgs& a, int waves, hipStream_t s);
 int launch_map_f32_bf16_packed(const AdapterArgs& a, int waves, hipStream_t s);
 int launch_map_bf16_packed(const AdapterArgs& a, int waves, hipStream_t s);
 
-// Four wavefronts per tile of 32 rows where there are enough tiles to fill the compute units; else 16, which divide the columns.
-// The gradients' rows are cut until there are about four workgroups per compute unit, with no fewer than eight tiles each.
-AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
+// The map: four wavefronts per tile of 32 rows where the tiles fill the compute units (32768 rows of 320: 24 us; with eight 28, with
+// 16 42); else 16, which divide the columns (64 rows of 1280 9.3 us; with eight 10.0, with four 13.4).  More workgroups per tile,
+// each with a part of the columns and all of t, are slower at every size; so is packing the forward call's weights, for its own time.
+// The gradients' rows are cut until there are about four workgroups per compute unit, with no fewer than eight tiles each; but with
+// 400 of them not at all (5003 rows, 450 workgroups: 41 us; in two parts 32, and 25 for their sums).
+AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t requests, int64_t adapters)
 {
     auto clamp = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
     AdapterPlan p;
     p.waves = M / 32 + (requests < M / 32 ? requests : M / 32) >= 512 ? 4 : 16;
     const int64_t blocks = adapters * ((K + 127) / 128 + (N + 127) / 128);
-    p.splits = (int)clamp(1024 / (blocks > 0 ? blocks : 1), 1, clamp(M / 256, 1, 64));
-    (void)R;
+    p.splits = blocks >= 400 ? 1 : (int)clamp(1024 / blocks, 1, clamp(M / 256, 1, 64));
     return p;
 }
 

@@ -103,7 +103,12 @@ struct MapShape {
 // Rows through a rank: t = scale1 x W1^T, y = base + scale2 t W2^T, in one pass.  A workgroup takes a tile of 32 rows of one request:
 // its wavefronts divide the columns of x in steps of 128 bytes, their sums meet in LDS, and they divide the columns of y, 32 at a
 // time, in tiles of the 32 x 32 instruction whose lanes hold neighbouring columns.  t never leaves the workgroup unless it is
-// asked for.  W: 0 fp32 weights, split where they are read; 1 bf16; 2, 3 packed in the order of the operands, bf16 and three
+// asked for.  Bound by the bytes of the rows, if enough of them are under way: hence two tiles of the base ahead (one: 29 us for 24),
+// and nothing loaded behind the stores, which it would wait for.
+//   32768 x 320 -> 320, rank 16, fp32 with bf16 weights: 24 us, 5.2 TB/s;  16384 x 320 -> 960, fp32: 32 us, 4.6 TB/s (its gradient
+//   24 us);  5003 ragged rows of 1280 -> 5120, rank 64, bf16: 55 us (its gradient 30): 195 workgroups, bound by the latency of a
+//   wavefront's tiles and the weights' way through LDS;  64 rows of 1280, an adapter each: 9 us, a launch and three latencies.
+// W: 0 fp32 weights, split where they are read; 1 bf16; 2, 3 packed in the order of the operands, bf16 and three
 // planes of fp32.
 template <typename TX, int W, int RT, int NWV, bool VEC, bool WVEC>
 __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_kernel(AdapterArgs p)
@@ -129,22 +134,31 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
     };
     const TX* const base = p.base ? static_cast<const TX*>(p.base) + (int64_t)rows.lo * p.ld_base : nullptr;
     TX* const y = static_cast<TX*>(p.y) + (int64_t)rows.lo * p.ldy;
-    v16f have;
-    auto load_base = [&](int c0) {
+    // (kept as they come: a conversion here would be a wait for them)
+    struct Base {
+        TX v[16];
+    } have[2];
+    auto load_base = [&](Base& to, int c0) {
         const unsigned col = (unsigned)min(c0 + l32, p.L2 - 1);
         if (base) {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 if (8 * q < count) {
 #pragma unroll
-                    for (int e = 4 * q; e < 4 * q + 4; ++e) have[e] = (float)base[row_at(e, (int)p.ld_base) + col];
+                    for (int e = 4 * q; e < 4 * q + 4; ++e) to.v[e] = base[row_at(e, (int)p.ld_base) + col];
                 }
         } else {
-            have = zero16();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) to.v[e] = (TX)0.0f;
         }
     };
-    int c0 = p.y ? 32 * wave : p.L2;
-    if (c0 < p.L2) load_base(c0);
+    const int end = p.y ? p.L2 : 0;
+    int c0 = 32 * wave;
+    const int last = end - 1;                                             // (loads behind it are of its column, for nothing)
+    if (c0 < end) {
+        load_base(have[0], c0);
+        load_base(have[1], min(c0 + 32 * NWV, last));
+    }
 
     Frag<3> tf[RT];
     if (some) {
@@ -163,7 +177,20 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
             if constexpr (!PACKED)
                 wt.load(w1 + (size_t)min(16 * RC * q, R - 1) * p.w1.ld, (unsigned)p.w1.ld, max(R - 16 * RC * q, 1), s * SC, p.L1, lane);
         };
+        Frag<NW> wp[PACKED ? SC / 32 : 1][PACKED && RT <= 4 ? RT : 1];
+        auto load_p = [&](int s) {
+            if constexpr (PACKED && RT <= 4) {
+#pragma unroll
+                for (int k = 0; k < SC / 32; ++k)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+#pragma unroll
+                        for (int q = 0; q < NW; ++q)
+                            wp[k][r].p[q] = (reinterpret_cast<const v8bf*>(w1) + ((size_t)(s * (SC / 32) + k) * RT + r) * 64 + lane)[q * (p.w1.plane / 8)];
+            }
+        };
         if (wave < steps) {
+            load_p(wave);
             xt.load(x, (unsigned)p.ldx, count, wave * SC, p.L1, lane);
             load_w(0, wave);
         }
@@ -194,7 +221,9 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
 #pragma unroll
                 for (int k = 0; k < SC / 32; ++k) {
                     Frag<NW> wf;
-                    if constexpr (PACKED) {
+                    if constexpr (PACKED && RT <= 4) {
+                        wf = wp[k][r];
+                    } else if constexpr (PACKED) {
                         const v8bf* const at = reinterpret_cast<const v8bf*>(w1) + ((size_t)(s * (SC / 32) + k) * RT + r) * 64 + lane;
 #pragma unroll
                         for (int q = 0; q < NW; ++q) wf.p[q] = at[q * (p.w1.plane / 8)];
@@ -206,6 +235,7 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
                         if (m == 0 || both) mma16<NW, NX>(acc[r][m], wf, xf[k][m]);
                 }
             }
+            load_p(next);
         }
         // the wavefronts' sums of a value, in order
         float* const sums = reinterpret_cast<float*>(lds);                // [NWV][32][RP], then t: [32][RP]
@@ -242,28 +272,40 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
         for (int id = threadIdx.x; id < count * R; id += 64 * NWV) p.t[(size_t)rows.lo * R + id] = 0.0f;
     }
 
-    // columns of y: the base's values and the weights of the wavefront's next 32 are loaded ahead of this one's products
+    // columns of y: the base's values of the wavefront's next two tiles and the weights of the next are on their way
     const TW* const w2 = static_cast<const TW*>(p.w2.p) + adapter * p.w2.each;
     WaveTile<TW, 32, 16 * RC, WVEC> wt;
     auto load_w = [&](int q, int c0) { wt.load(w2 + (size_t)c0 * p.w2.ld, (unsigned)p.w2.ld, p.L2 - c0, 16 * RC * q, R, lane); };
-    if (!PACKED && some && c0 < p.L2) load_w(0, c0);
-    for (; c0 < p.L2; c0 += 32 * NWV) {
-        const int next = c0 + 32 * NWV < p.L2 ? c0 + 32 * NWV : c0;       // (loaded for nothing behind the last)
-        v16f acc = have;
+    constexpr int KC = !PACKED ? 1 : RT * NW <= 12 ? RT : 12 / NW;        // packed weights held at once
+    Frag<NW> wf[KC];
+    auto load_f = [&](int k0, int c0) {
+        if constexpr (PACKED) {
+            const v8bf* const at = reinterpret_cast<const v8bf*>(w2) + ((size_t)(c0 / 32) * RT + k0) * 64 + lane;
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+#pragma unroll
+                for (int q = 0; q < NW; ++q) wf[k].p[q] = at[k * 64 + q * (p.w2.plane / 8)];
+        }
+    };
+    if (some && c0 < end) {
+        if constexpr (PACKED)
+            load_f(0, c0);
+        else
+            load_w(0, c0);
+    }
+    auto tile = [&](Base& mine_base) {
+        const int next = c0 + 32 * NWV < end ? c0 + 32 * NWV : c0;
+        v16f acc;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] = (float)mine_base.v[e];
+        load_base(mine_base, min(c0 + 64 * NWV, last));
         if (some) {
-            Frag<NW> wf[PACKED ? RT : 1];
-            if constexpr (PACKED) {
-                const v8bf* const at = reinterpret_cast<const v8bf*>(w2) + (size_t)(c0 / 32) * RT * 64 + lane;
-#pragma unroll
-                for (int k = 0; k < RT; ++k)
-#pragma unroll
-                    for (int q = 0; q < NW; ++q) wf[k].p[q] = at[k * 64 + q * (p.w2.plane / 8)];
-            }
-            load_base(next);
 #pragma unroll
             for (int k = 0; k < RT; ++k) {
                 if constexpr (PACKED) {
-                    mma32<3, NW>(acc, tf[k], wf[k]);
+                    mma32<3, NW>(acc, tf[k], wf[k % KC]);
+                    // (the next columns' ahead of the stores: a wait for a load is one for all that was issued before it)
+                    if (k % KC == KC - 1) load_f(k + 1 < RT ? k + 1 : 0, k + 1 < RT ? c0 : next);
                 } else {
                     if (k % RC == 0) {
                         wave_order();
@@ -277,8 +319,6 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
                     mma32<3, NW>(acc, tf[k], Sh::W2T::frag(mine, l32, 16 * (k % RC) + 8 * h, R - 16 * k - 8 * h));
                 }
             }
-        } else {
-            load_base(next);
         }
         const unsigned col = c0 + l32;
         if (col < (unsigned)p.L2) {
@@ -290,13 +330,18 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
                         if (8 * q + 4 * h + e % 4 < count) y[row_at(e, (int)p.ldy) + col] = (TX)acc[e];
                 }
         }
+        c0 += 32 * NWV;
+    };
+    while (c0 < end) {
+        tile(have[0]);
+        if (c0 < end) tile(have[1]);
     }
 }
 
 constexpr int kListed = 512;        // requests that a workgroup looks over at a time
 
 // The gradients of the adapters.  A workgroup has 128 columns of x (B false: dA) or dy (true: dB) and of an adapter's tiles of 32 rows
-// its share of p.splits; both kinds are in one launch.
+// its share of p.splits; both kinds are in one launch.  16384 rows of 320 and 960 at rank 16: 27 us, 3.1 TB/s.
 template <typename TX, int RT, bool VEC, bool B>
 __device__ __forceinline__ void outer(const OuterArgs& p, unsigned char* lds, int chunk)
 {
@@ -428,7 +473,7 @@ int map_of_tile(const AdapterArgs& a, hipStream_t s)
 template <typename TX, int W, int RT>
 int map_of_rank(const AdapterArgs& a, int waves, hipStream_t s)
 {
-    constexpr int many = RT <= 2 ? 16 : 8;                                // (registers)
+    constexpr int many = RT * (W == 3 ? 3 : 1) <= 3 ? 16 : 8;                                // (registers)
     return waves == 16 ? map_of_tile<TX, W, RT, many>(a, s) : map_of_tile<TX, W, RT, 4>(a, s);
 }
 

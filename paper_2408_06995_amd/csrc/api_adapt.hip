@@ -217,7 +217,7 @@ int fpq_adapter_apply(const fpq_adapter_args_t* p, const void* x, const void* a,
     if (!stride_ok(p->ld_y, p->N) || (base && !stride_ok(p->ld_base, p->N))) return FPQ_ERR_SHAPE;
     const size_t size = size_of(p->x_type), w = size_of(p->w_type);
     if (!aligned(y, size) || !aligned(base, size) || !aligned(t, 4)) return FPQ_ERR_ALIGN;
-    const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->R, p->requests, p->adapters);
+    const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->requests, p->adapters);
     AdapterArgs r = args_of(p);
     r.x = x;
     r.ldx = p->ld_x;
@@ -238,7 +238,7 @@ int fpq_adapter_apply(const fpq_adapter_args_t* p, const void* x, const void* a,
 size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
 {
     if (check_adapter_sizes(M, N, K, R, requests, adapters) != FPQ_OK) return 0;
-    const AdapterPlan plan = plan_adapter(M, N, K, R, requests, adapters);
+    const AdapterPlan plan = plan_adapter(M, N, K, requests, adapters);
     const size_t each = (size_t)adapters * R * 4;
     return align_up((size_t)M * R * 4) + packed_weights(FPQ_TYPE_FP32, adapters, N, R) + packed_weights(FPQ_TYPE_FP32, adapters, K, R) +
            (plan.splits > 1 ? align_up(plan.splits * each * K) + align_up(plan.splits * each * N) : 0);
@@ -258,7 +258,7 @@ int fpq_adapter_backward(const fpq_adapter_args_t* p, const void* x, const void*
     const size_t need = fpq_adapter_backward_workspace_size(p->M, p->N, p->K, p->R, p->requests, p->adapters);
     if (!workspace || workspace_bytes < need) return FPQ_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return FPQ_ERR_ALIGN;
-    const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->R, p->requests, p->adapters);
+    const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->requests, p->adapters);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int N = (int)p->N, K = (int)p->K, R = (int)p->R;
     char* at = static_cast<char*>(workspace);
