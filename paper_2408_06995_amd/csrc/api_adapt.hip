@@ -141,11 +141,10 @@ int check_adamw(const fpq_adamw_tensor_t* t, int count, int64_t* pieces)
 
 int check_adapter_sizes(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
 {
-    for (int64_t v : {M, N, K, R, requests, adapters})
-        if (v < 0 || v > kMost) return FPQ_ERR_SHAPE;
-    if (N == 0 || K == 0 || R == 0 || adapters == 0 || adapters > 65535) return FPQ_ERR_SHAPE;
+    // (of M, requests and adapters, so that no dimension of a grid is too large)
+    if (M < 0 || M > (int64_t)1 << 28 || requests < 0 || requests > 1 << 21 || adapters < 1 || adapters > 32767) return FPQ_ERR_SHAPE;
+    if (N < 1 || N > kMostColumns || K < 1 || K > kMostColumns || R < 1) return FPQ_ERR_SHAPE;
     if (R > kMaxRank) return FPQ_ERR_UNSUPPORTED;
-    if (N > kMostColumns || K > kMostColumns) return FPQ_ERR_SHAPE;
     return FPQ_OK;
 }
 
