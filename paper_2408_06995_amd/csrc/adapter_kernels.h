@@ -340,17 +340,28 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
 
 constexpr int kListed = 512;        // requests that a workgroup looks over at a time
 
+// LDS of the gradients: a tile of x or dy and one of t or dt; two of each, for one barrier per tile instead of two, where three
+// workgroups still fit.
+template <typename TX, int RT>
+struct OuterShape {
+    static constexpr int X = kPlanes<TX> * 32 * kRowStride<8>, T = 3 * 32 * kRowStride<RT>, BUFFERS = (X + T) * 2 <= 24 << 10 ? 2 : 1;
+    static constexpr int LDS = BUFFERS * (X + T) * 2 + (3 * kListed + 12) * 4;
+};
+
 // The gradients of the adapters.  A workgroup has 128 columns of x (B false: dA) or dy (true: dB) and of an adapter's tiles of 32 rows
-// its share of p.splits; both kinds are in one launch.  16384 rows of 320 and 960 at rank 16: 27 us, 3.1 TB/s.
+// its share of p.splits; both kinds are in one launch.  Bound by the latency of a step, not by bytes: hence two tiles under way, and
+// the adapter's requests listed once, so that a step finds its rows without a search (38 us with one, 29 without: 5003 ragged rows
+// of 1280 and 5120 at rank 64, bf16, whose longest adapter sets the time).  16384 rows of 320 and 960 at rank 16, fp32: 27 us, 3.1 TB/s.
 template <typename TX, int RT, bool VEC, bool B>
 __device__ __forceinline__ void outer(const OuterArgs& p, unsigned char* lds, int chunk)
 {
     constexpr int NX = kPlanes<TX>, CS = kRowStride<8>, RS = kRowStride<RT>;
-    __bf16* const xt = reinterpret_cast<__bf16*>(lds);                   // [NX][32][CS]
-    __bf16* const tt = xt + NX * 32 * CS;                                // [3][32][RS]
-    int* const upto = reinterpret_cast<int*>(tt + 3 * 32 * RS);          // [kListed + 1] tiles ahead of a request, [kListed] first rows
-    int* const first = upto + kListed + 1;
-    int* const wsum = first + kListed;                                   // [4]
+    typedef OuterShape<TX, RT> Sh;
+    __bf16* const tiles = reinterpret_cast<__bf16*>(lds);                // [BUFFERS] x [NX][32][CS], t [3][32][RS]
+    int* const upto = reinterpret_cast<int*>(tiles + Sh::BUFFERS * (Sh::X + Sh::T));
+    int* const first = upto + kListed + 1;           // this adapter's requests: upto [kListed + 1] tiles ahead of it, rows from first to behind
+    int* const behind = first + kListed;
+    int* const wsum = behind + kListed;              // [8]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
     const int L = p.L[B], R = p.R, c0 = chunk * 128, adapter = blockIdx.y, split = blockIdx.z;
     const TX* const x = static_cast<const TX*>(p.rows[B]) + c0;
@@ -361,53 +372,71 @@ __device__ __forceinline__ void outer(const OuterArgs& p, unsigned char* lds, in
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[c][r] = v4f{0, 0, 0, 0};
-    Stage<TX, 8, VEC, 32, 256> sx;
-    Stage<float, RT, VEC, 32, 256> st;
+    struct Tile {
+        Stage<TX, 8, VEC, 32, 256> sx;
+        Stage<float, RT, VEC, 32, 256> st;
+        int lo, hi;
+    } ahead[2];                                      // the two tiles on their way
     for (int q0 = 1; q0 <= p.requests; q0 += kListed) {
         __syncthreads();
-        int before = 0;                              // tiles of this adapter in the requests listed so far
+        int before = 0, listed = 0;                  // tiles and requests of this adapter so far
         for (int part = 0; part < kListed; part += 256) {
             const int v = q0 + part + tid;
             Rows r = {0, 0, -1};
             if (v <= p.requests) r = rows_of(p, v);
-            const int tiles = r.adapter == adapter ? (r.hi - r.lo + 31) / 32 : 0, sum = scan64(tiles);
-            if (lane == 63) wsum[wave] = sum;
-            __syncthreads();
-            int ahead = before + sum - tiles;
-            for (int w = 0; w < 4; ++w) {
-                if (w < wave) ahead += wsum[w];
-                before += wsum[w];
+            const int has = r.adapter == adapter ? (r.hi - r.lo + 31) / 32 : 0, sum = scan64(has), count = scan64(has > 0);
+            if (lane == 63) {
+                wsum[wave] = sum;
+                wsum[4 + wave] = count;
             }
-            upto[part + tid] = ahead;
-            first[part + tid] = r.lo;
+            __syncthreads();
+            int at = listed + count - (has > 0), ahead_of = before + sum - has;
+            for (int w = 0; w < 4; ++w) {
+                if (w < wave) {
+                    ahead_of += wsum[w];
+                    at += wsum[4 + w];
+                }
+                before += wsum[w];
+                listed += wsum[4 + w];
+            }
+            if (has > 0) {
+                upto[at] = ahead_of;
+                first[at] = r.lo;
+                behind[at] = r.hi;
+            }
             __syncthreads();
         }
-        if (tid == 0) upto[kListed] = before;
+        if (tid == 0) upto[listed] = before;
         __syncthreads();
         const int tbeg = (int)((int64_t)before * split / p.splits), tend = (int)((int64_t)before * (split + 1) / p.splits);
-        int lo = 0, hi = 0;                          // of the tile last loaded
-        auto load = [&](int tile) {
-            int a = 0, b = kListed;                  // upto[a] <= tile < upto[b]
-            while (b - a > 1) {
-                const int m = (a + b) >> 1;
-                if (upto[m] <= tile)
-                    a = m;
-                else
-                    b = m;
+        int a = 0;                                   // upto[a] <= tbeg < upto[a + 1]; from there on one by one
+        for (int b = listed; b - a > 1;) {
+            const int m = (a + b) >> 1;
+            if (upto[m] <= tbeg)
+                a = m;
+            else
+                b = m;
+        }
+        int from = 0, next = 0, row0 = 0, end = 0;
+        if (tbeg < tend) from = upto[a], next = upto[a + 1], row0 = first[a], end = behind[a];
+        auto load = [&](Tile& its, int tile) {
+            if (tile >= next) {
+                ++a;
+                from = next, next = upto[a + 1], row0 = first[a], end = behind[a];
             }
-            const Rows r = rows_of(p, q0 + a);
-            lo = first[a] + (tile - upto[a]) * 32;
-            hi = min(r.hi, lo + 32);
-            sx.load(x, ld, lo, hi - 1, L - c0, tid);
-            st.load(t, R, lo, hi - 1, R, tid);
+            its.lo = row0 + (tile - from) * 32;
+            its.hi = min(end, its.lo + 32);
+            its.sx.load(x, ld, its.lo, its.hi - 1, L - c0, tid);
+            its.st.load(t, R, its.lo, its.hi - 1, R, tid);
         };
-        if (tbeg < tend) load(tbeg);
-        for (int tile = tbeg; tile < tend; ++tile) {
+        auto step = [&](Tile& its, int tile, int buffer) {
+            __bf16* const xt = tiles + (Sh::BUFFERS == 2 ? buffer : 0) * (Sh::X + Sh::T);
+            __bf16* const tt = xt + Sh::X;
+            if (Sh::BUFFERS == 1) __syncthreads();
+            its.sx.store(xt, its.lo, its.hi, L - c0, tid);
+            its.st.store(tt, its.lo, its.hi, R, tid);
             __syncthreads();
-            sx.store(xt, lo, hi, L - c0, tid);
-            st.store(tt, lo, hi, R, tid);
-            __syncthreads();
-            if (tile + 1 < tend) load(tile + 1);
+            if (tile + 2 < tend) load(its, tile + 2);
             Frag<NX> xf[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) xf[c] = col_frag16<NX>(xt, CS, 32 * CS, 0, 32 * wave + 16 * c, lane);
@@ -422,6 +451,12 @@ __device__ __forceinline__ void outer(const OuterArgs& p, unsigned char* lds, in
                         mma16<3, NX>(acc[c][r], tf, xf[c]);              // lane: column r16, ranks 4 g + i
                 }
             }
+        };
+        if (tbeg < tend) load(ahead[0], tbeg);
+        if (tbeg + 1 < tend) load(ahead[1], tbeg + 1);
+        for (int tile = tbeg; tile < tend; tile += 2) {
+            step(ahead[0], tile, 0);
+            if (tile + 1 < tend) step(ahead[1], tile + 1, 1);
         }
     }
     const float scale = B ? p.scaling[adapter] : 1.0f;
@@ -488,7 +523,7 @@ int launch_map(const AdapterArgs& a, int waves, hipStream_t s)
 template <typename TX, int RT, bool VEC>
 int launch_outer(const OuterArgs& a, hipStream_t s)
 {
-    constexpr int lds = kPlanes<TX> * 32 * kRowStride<8> * 2 + 3 * 32 * kRowStride<RT> * 2 + (2 * kListed + 8) * 4;
+    constexpr int lds = OuterShape<TX, RT>::LDS;
     static std::atomic<uint64_t> done{0};
     if (!allow_dynamic_lds(reinterpret_cast<const void*>(&adapter_outer_kernel<TX, RT, VEC>), lds, done)) return FPQ_ERR_LAUNCH;
     const int chunks = (a.L[0] + 127) / 128 + (a.L[1] + 127) / 128;

@@ -217,3 +217,29 @@ def test_another_stream_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(bufs, (o, lse, *grads)))
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("shape", [(32, 300, 77, 8, 8, 40), (64, 270, 33, 8, 4, 64), (128, 257, 96, 2, 2, 80), (128, 260, 1, 2, 2, 96), (128, 300, 95, 2, 2, 33),
+                                   (128, 257, 64, 2, 2, 128), (128, 257, 70, 2, 2, 160), (256, 513, 32, 1, 1, 8)])
+def test_few_keys_of_many_rows(shape, causal, t):
+    """Many blocks of rows over a tile or two of keys; samples of fewer keys and of none, with others' values behind."""
+    print(shape, causal, t, flush=True)
+    q, k, v, go = tensors(*shape, t, 41)
+    n = shape[2]
+    lens = [(7 * b) % (n + 1) if b % 3 else n for b in range(shape[0])]
+    for b in range(shape[0]):
+        k[b, lens[b]:] = float("nan")
+        v[b, lens[b]:] = float("inf")
+    scale = shape[5] ** -0.5
+    o, lse = forward(q, k, v, scale, causal, torch.tensor(lens, dtype=torch.int32, device=DEV))
+    few = sorted({0, 1, 2, shape[0] - 1, *(b for b in range(shape[0]) if lens[b] == 0)})[:6]        # samples are independent
+    a = [host(x[few]) for x in (q, k, v)]
+    some = [lens[b] for b in few]
+    scale = float(np.float32(scale))
+    want_o, want_lse = adapt.attention(*a, scale, causal, some)
+    to, tl = adapt.attention_bounds(*a, scale, causal, some, t == "bf16")[:2]
+    close(o[few], want_o, to, "o")
+    close(lse[few], want_lse, tl, "lse")
+    assert not o.isnan().any() and not lse.isnan().any()
