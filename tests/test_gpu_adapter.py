@@ -195,3 +195,13 @@ def test_another_stream_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(bufs, want))
+
+
+@pytest.mark.parametrize("x,w", PAIRS)
+def test_more_requests_than_a_list_holds(x, w):
+    """Requests of one row, of none and of many, in several lists; an adapter's rows in all of them, another's in the last only."""
+    starts = [0]
+    for i in range(1300):
+        starts.append(starts[-1] + (0 if i % 7 == 3 else 70 if i % 400 == 5 else 1))
+    of = [2 if i >= 1200 and i % 5 == 0 else i % 2 if i % 3 else -1 for i in range(1300)]
+    Call(starts[-1] + 20, 72, 40, 8, starts, of, 4, x, w).check()
