@@ -508,9 +508,10 @@ int fpq_attention_backward(const fpq_attention_args_t *args, const void *q, cons
  * a and b are contiguous; rows of the other matrices have the strides ld_* (in elements), their elements are neighbours.
  * Adapters of a smaller rank are filled up with zero rows of A and columns of B, which stay zero in training.  Rows of 16-byte
  * multiples that start at one, and ranks that are multiples of 8, are what the kernels are tuned for; others work.
- * workspace: the stated bytes, 16-byte aligned (NULL when that is 0, as for every forward call); calls that share one are ordered on
- * one stream.  Limits: R <= 128 (FPQ_ERR_UNSUPPORTED beyond); M at most 2^28, requests 2^21, N, K and the strides 2^24, adapters
- * 32767 (FPQ_ERR_SHAPE). */
+ * workspace: the stated bytes, 16-byte aligned (NULL when that is 0, as for forward calls of ranks up to 16, or where R and K are
+ * multiples of 8; a and b then start at multiples of 16 bytes if the rank is above 16); calls that share one are ordered on one stream.
+ * Limits: R <= 128 (FPQ_ERR_UNSUPPORTED beyond); M at most 2^28, requests 2^21, N, K and the strides 2^24, adapters 32767
+ * (FPQ_ERR_SHAPE). */
 typedef struct fpq_adapter_args {
     int32_t x_type, w_type; /* fpq_type */
     int64_t M, N, K, R;

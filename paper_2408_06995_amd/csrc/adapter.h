@@ -16,7 +16,7 @@
 
 namespace fpq {
 
-constexpr int kMaxRank = 128;
+constexpr int kMaxRank = 128, kPlainRank = 16;     // up to kPlainRank weights are read where they are, whatever their alignment
 
 // Weights of one contraction: [adapters][rows][cols], the contraction along the columns; or packed in the order in which the matrix
 // instructions take them, 64 lanes x 8 elements at a time, zeros outside the matrix:
@@ -40,6 +40,7 @@ struct AdapterArgs {
     const int32_t *row_start, *adapter;
     int64_t ldx, ld_base, ldy;
     int M, L1, L2, R, requests, adapters;
+    int parts;                      // of the columns of y: the workgroups of a tile
     int vec_x;                      // rows of x, 16 bytes at a time
 };
 
@@ -149,15 +150,18 @@ __device__ __forceinline__ Rows find_tile(const AdapterArgs& p, int tile)
 // Sizes only; the same for the workspace.
 struct AdapterPlan {
     int waves;                      // of a workgroup of the map: 4, or 16 (as many as the rank lets)
+    int parts_n, parts_k;           // of the columns of y and of dx
     int splits;                     // of an adapter's rows in the gradients
 };
 AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t requests, int64_t adapters);
 
-// Both weights of the backward call, packed: W1 from b [adapters][N][R], W2 from a [adapters][R][K].
+// Both weights of a call, packed: W1 from a [adapters][R][K] and W2 from b [adapters][N][R] in the forward call, W1 from b and W2
+// from a in the backward one.
 struct AdapterPack {
     const void *a, *b;
     __bf16 *w1, *w2;
     int N, K, R, adapters;
+    bool forward;
 };
 static inline int rank_groups(int64_t R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
 static inline int64_t packed_elements(int64_t len, int64_t R) { return (len + 63) / 64 * 2 * rank_groups(R) * 512; }     // of a plane: N or K

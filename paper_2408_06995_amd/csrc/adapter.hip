@@ -11,8 +11,12 @@ int launch_map_f32_bf16_packed(const AdapterArgs& a, int waves, hipStream_t s);
 int launch_map_bf16_packed(const AdapterArgs& a, int waves, hipStream_t s);
 
 // The map: four wavefronts per tile of 32 rows where the tiles fill the compute units (32768 rows of 320: 24 us; with eight 28, with
-// 16 42); else 16, which divide the columns (64 rows of 1280 9.3 us; with eight 10.0, with four 13.4).  More workgroups per tile,
-// each with a part of the columns and all of t, are slower at every size; so is packing the forward call's weights, for its own time.
+// 16 42); else 16, which divide the columns (64 rows of 1280 9.3 us; with eight 10.0, with four 13.4). Where the tiles leave most compute units
+// idle, each has several workgroups, with a part of the columns and all of t each (259 rows of 1728 -> 5056 at rank 123: 58 us, with
+// one 95; training step of 1000 rows of 1280 -> 1280 at rank 32 in bf16: 35 us, with one 41); with more tiles t's repetition costs more
+// than it gives (5003 rows of 1280 -> 5120: 55 us, in two parts 64).
+// Weights whose rows do not start at 16 bytes are packed for ranks above 16 (the same rows: read as they are 257 us); packing others
+// ahead costs what it saves.
 // The gradients' rows are cut until there are about four workgroups per compute unit, with no fewer than eight tiles each; but with
 // 400 of them not at all (5003 rows, 450 workgroups: 29 us; the sums of two parts alone take 25).
 AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t requests, int64_t adapters)
@@ -20,6 +24,9 @@ AdapterPlan plan_adapter(int64_t M, int64_t N, int64_t K, int64_t requests, int6
     auto clamp = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
     AdapterPlan p;
     p.waves = M / 32 + (requests < M / 32 ? requests : M / 32) >= 512 ? 4 : 16;
+    const int64_t most = M / 32 + requests + 2;
+    p.parts_n = (int)clamp(256 / most, 1, clamp(N / 256, 1, 8));
+    p.parts_k = (int)clamp(256 / most, 1, clamp(K / 256, 1, 8));
     const int64_t blocks = adapters * ((K + 127) / 128 + (N + 127) / 128);
     p.splits = blocks >= 400 ? 1 : (int)clamp(1024 / blocks, 1, clamp(M / 256, 1, 64));
     return p;
@@ -37,17 +44,19 @@ __global__ __launch_bounds__(256) void adapter_pack_kernel(AdapterPack p, int gr
     const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), n = second ? n2 : n1;                // an operand of 64 lanes
     if (unit * 512 >= n) return;
     const int64_t outer = unit / groups;
-    const int q = (int)(unit - outer * groups), L = second ? p.K : p.N;
-    const T* const src = static_cast<const T*>(second ? p.a : p.b) + (size_t)adapter * p.R * L;
+    const int q = (int)(unit - outer * groups);
+    const bool from_b = second == p.forward;                     // [L, R]; a is [R, L]
+    const int L = from_b ? p.N : p.K;
+    const T* const src = static_cast<const T*>(from_b ? p.b : p.a) + (size_t)adapter * p.R * L;
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        // (rank, place along N or K) of the element
+        // (rank, place along L) of the element
         const int rank = second ? 16 * q + 8 * (lane >> 5) + e : 16 * q + (lane & 15);
         const int64_t at = second ? 32 * outer + (lane & 31) : 32 * outer + 8 * (lane >> 4) + e;
         const int rc = min(rank, p.R - 1);
         const int64_t ac = min(at, (int64_t)L - 1);
-        const float x = (float)src[second ? rc * (int64_t)L + ac : ac * p.R + rc];
+        const float x = (float)src[from_b ? ac * p.R + rc : rc * (int64_t)L + ac];
         v[e] = rank < p.R && at < L ? x : 0.0f;
     }
     const Frag<NP> f = frag_of<NP>(v);
@@ -83,7 +92,7 @@ __global__ __launch_bounds__(256) void adapter_sums_kernel(const float* part_a, 
 
 int launch_adapter_pack(const AdapterPack& a, int w_type, hipStream_t s)
 {
-    const int64_t n1 = packed_elements(a.N, a.R), n2 = packed_elements(a.K, a.R), most = n1 > n2 ? n1 : n2;
+    const int64_t n1 = packed_elements(a.forward ? a.K : a.N, a.R), n2 = packed_elements(a.forward ? a.N : a.K, a.R), most = n1 > n2 ? n1 : n2;
     const dim3 grid((unsigned)((most + 2047) / 2048), 2 * a.adapters);
     const int groups = rank_groups(a.R);
     if (w_type == FPQ_TYPE_FP32)

@@ -152,8 +152,8 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
             for (int e = 0; e < 16; ++e) to.v[e] = (TX)0.0f;
         }
     };
-    const int end = p.y ? p.L2 : 0;
-    int c0 = 32 * wave;
+    const int part = blockIdx.y, per = ((p.L2 + 31) / 32 + p.parts - 1) / p.parts * 32, end = p.y ? min(p.L2, (part + 1) * per) : 0;
+    int c0 = part * per + 32 * wave;
     const int last = end - 1;                                             // (loads behind it are of its column, for nothing)
     if (c0 < end) {
         load_base(have[0], c0);
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
 #pragma unroll
                 for (int w = 0; w < NWV; ++w) v += sums[(w * 32 + m) * RP + r];
                 v *= scale1;
-                if (p.t) p.t[(size_t)(rows.lo + m) * R + r] = v;
+                if (p.t && part == 0) p.t[(size_t)(rows.lo + m) * R + r] = v;
                 v *= scale2;
             }
             ts[m * RP + r] = v;
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : NWV / 4) void adapter_map_
             tf[k] = frag_of<3>(v);
         }
         __syncthreads();                                                  // (the weights' tiles reuse t's place)
-    } else if (p.t) {
+    } else if (p.t && part == 0) {
         for (int id = threadIdx.x; id < count * R; id += 64 * NWV) p.t[(size_t)rows.lo * R + id] = 0.0f;
     }
 
@@ -491,7 +491,7 @@ int launch_map(const AdapterArgs& a, hipStream_t s)
     static std::atomic<uint64_t> done{0};
     if (!allow_dynamic_lds(reinterpret_cast<const void*>(&adapter_map_kernel<TX, W, RT, NWV, VEC, WVEC>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t tiles = (int64_t)a.M / 32 + a.requests + 2;
-    adapter_map_kernel<TX, W, RT, NWV, VEC, WVEC><<<dim3((unsigned)tiles), dim3(64 * NWV), lds, s>>>(a);
+    adapter_map_kernel<TX, W, RT, NWV, VEC, WVEC><<<dim3((unsigned)tiles, a.y ? a.parts : 1), dim3(64 * NWV), lds, s>>>(a);
     return FPQ_OK;
 }
 
@@ -499,8 +499,8 @@ template <typename TX, int W, int RT, int NWV>
 int map_of_tile(const AdapterArgs& a, hipStream_t s)
 {
     if (a.w1.vec && a.w2.vec) return a.vec_x ? launch_map<TX, W, RT, NWV, true, true>(a, s) : launch_map<TX, W, RT, NWV, false, true>(a, s);
-    if constexpr (W >= 2)
-        return FPQ_ERR_UNSUPPORTED;                  // (packed weights always are)
+    if constexpr (W >= 2 || RT > kPlainRank / 16)
+        return FPQ_ERR_UNSUPPORTED;                  // (the weights are packed then)
     else
         return a.vec_x ? launch_map<TX, W, RT, NWV, true, false>(a, s) : launch_map<TX, W, RT, NWV, false, false>(a, s);
 }
@@ -508,7 +508,7 @@ int map_of_tile(const AdapterArgs& a, hipStream_t s)
 template <typename TX, int W, int RT>
 int map_of_rank(const AdapterArgs& a, int waves, hipStream_t s)
 {
-    constexpr int many = RT * (W == 3 ? 3 : 1) <= 3 ? 16 : 8;                                // (registers)
+    constexpr int many = RT == 1 ? 16 : 8;                                // (registers)
     return waves == 16 ? map_of_tile<TX, W, RT, many>(a, s) : map_of_tile<TX, W, RT, 4>(a, s);
 }
 

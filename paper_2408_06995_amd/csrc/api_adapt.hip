@@ -174,6 +174,20 @@ int check_adapter(const fpq_adapter_args_t* p, const void* x, const void* a, con
     return FPQ_OK;
 }
 
+// Forward: whether a workspace for packed weights is asked for.  Ranks up to 16 read weights of any alignment where they are.
+bool pack_forward(int64_t R, int64_t K) { return R > kPlainRank && (R % 8 != 0 || K % 8 != 0); }
+
+// Packs the weights of a map into the workspace: W1 [R, L1], W2 [L2, R].
+int pack_weights(const fpq_adapter_args_t* p, const void* a, const void* b, bool forward, void* workspace, AdapterArgs& r, hipStream_t s)
+{
+    const int64_t planes = p->w_type == FPQ_TYPE_FP32 ? 3 : 1, n1 = packed_elements(forward ? p->K : p->N, p->R), n2 = packed_elements(forward ? p->N : p->K, p->R);
+    __bf16* const w1 = static_cast<__bf16*>(workspace);
+    __bf16* const w2 = w1 + align_up((size_t)p->adapters * planes * n1 * 2) / 2;
+    r.w1 = Weights{w1, planes * n1, n1, 0, 1};
+    r.w2 = Weights{w2, planes * n2, n2, 0, 1};
+    return launch_adapter_pack(AdapterPack{a, b, w1, w2, (int)p->N, (int)p->K, (int)p->R, (int)p->adapters, forward}, p->w_type, s);
+}
+
 AdapterArgs args_of(const fpq_adapter_args_t* p)
 {
     AdapterArgs r{};
@@ -200,15 +214,13 @@ extern "C" {
 
 size_t fpq_adapter_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
 {
-    (void)check_adapter_sizes(M, N, K, R, requests, adapters);
-    return 0;                                              // t stays in the workgroups
+    if (check_adapter_sizes(M, N, K, R, requests, adapters) != FPQ_OK) return 0;
+    return pack_forward(R, K) ? packed_weights(FPQ_TYPE_FP32, adapters, N, R) + packed_weights(FPQ_TYPE_FP32, adapters, K, R) : 0;
 }
 
 int fpq_adapter_apply(const fpq_adapter_args_t* p, const void* x, const void* a, const void* b, const void* base, void* y, float* t,
                       void* workspace, size_t workspace_bytes, void* stream)
 {
-    (void)workspace;
-    (void)workspace_bytes;
     const int st = check_adapter(p, x, a, b);
     if (st != FPQ_OK) return st;
     if (p->M == 0) return FPQ_OK;
@@ -216,7 +228,11 @@ int fpq_adapter_apply(const fpq_adapter_args_t* p, const void* x, const void* a,
     if (!stride_ok(p->ld_y, p->N) || (base && !stride_ok(p->ld_base, p->N))) return FPQ_ERR_SHAPE;
     const size_t size = size_of(p->x_type), w = size_of(p->w_type);
     if (!aligned(y, size) || !aligned(base, size) || !aligned(t, 4)) return FPQ_ERR_ALIGN;
+    const size_t need = fpq_adapter_workspace_size(p->M, p->N, p->K, p->R, p->requests, p->adapters);
+    if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 16)) return FPQ_ERR_ALIGN;
     const AdapterPlan plan = plan_adapter(p->M, p->N, p->K, p->requests, p->adapters);
+    hipStream_t s = static_cast<hipStream_t>(stream);
     AdapterArgs r = args_of(p);
     r.x = x;
     r.ldx = p->ld_x;
@@ -231,7 +247,14 @@ int fpq_adapter_apply(const fpq_adapter_args_t* p, const void* x, const void* a,
     r.L1 = (int)p->K;
     r.L2 = (int)p->N;
     r.vec_x = p->K * size % 16 == 0 && matrix_aligned(x, p->ld_x, p->M, size, 16);
-    return launch_adapter_map(r, p->x_type, p->w_type, false, plan.waves, static_cast<hipStream_t>(stream));
+    r.parts = plan.parts_n;
+    const bool packed = p->R > kPlainRank && !(r.w1.vec && r.w2.vec);
+    if (packed) {
+        if (!need) return FPQ_ERR_ALIGN;
+        const int done = pack_weights(p, a, b, true, workspace, r, s);
+        if (done != FPQ_OK) return done;
+    }
+    return launch_adapter_map(r, p->x_type, p->w_type, packed, plan.waves, s);
 }
 
 size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int64_t R, int64_t requests, int64_t adapters)
@@ -269,12 +292,11 @@ int fpq_adapter_backward(const fpq_adapter_args_t* p, const void* x, const void*
     float* const dt = reinterpret_cast<float*>(take(align_up((size_t)p->M * R * 4)));
     int done = FPQ_OK;
     if (p->M) {
-        AdapterPack pack{a, b, nullptr, nullptr, N, K, R, (int)p->adapters};
-        pack.w1 = reinterpret_cast<__bf16*>(take(packed_weights(p->w_type, p->adapters, N, R)));
-        pack.w2 = reinterpret_cast<__bf16*>(take(packed_weights(p->w_type, p->adapters, K, R)));
-        done = launch_adapter_pack(pack, p->w_type, s);
-        if (done != FPQ_OK) return done;
         AdapterArgs r = args_of(p);
+        done = pack_weights(p, a, b, false, at, r, s);
+        if (done != FPQ_OK) return done;
+        at += packed_weights(FPQ_TYPE_FP32, p->adapters, N, R) + packed_weights(FPQ_TYPE_FP32, p->adapters, K, R);
+        r.parts = plan.parts_k;
         r.x = grad_y;
         r.ldx = p->ld_grad_y;
         r.base = grad_x ? grad_x_base : nullptr;
@@ -282,9 +304,6 @@ int fpq_adapter_backward(const fpq_adapter_args_t* p, const void* x, const void*
         r.y = grad_x;
         r.ldy = p->ld_grad_x;
         r.t = dt;
-        const int64_t planes = p->w_type == FPQ_TYPE_FP32 ? 3 : 1, n1 = packed_elements(N, R), n2 = packed_elements(K, R);
-        r.w1 = Weights{pack.w1, planes * n1, n1, 0, 1};
-        r.w2 = Weights{pack.w2, planes * n2, n2, 0, 1};
         r.scale1 = p->scaling;
         r.L1 = N;
         r.L2 = K;

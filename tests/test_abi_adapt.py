@@ -173,3 +173,18 @@ def test_adapter_binding_checks():
     refused(ValueError, "one type", x, a, b.bfloat16(), s, start, of, None, y, t)
     with pytest.raises(ValueError, match="grad_a"):
         B.fpq_adapter_backward(x, a, b, s, start, of, t, y, None, x, a[:2], b)
+
+
+def test_adapter_ranks_above_16_that_are_packed():
+    """Rows off the multiples of eight elements need a workspace in the forward call; others need aligned weights."""
+    L = B.lib()
+    assert L.fpq_adapter_workspace_size(10, 32, 64, 24, 2, 3) == 0 and L.fpq_adapter_workspace_size(10, 32, 63, 16, 2, 3) == 0
+    need = L.fpq_adapter_workspace_size(10, 32, 64, 20, 2, 3)
+    # three planes of bf16 for each adapter, both lengths in steps of 64 and the rank in steps of 32
+    assert need >= 3 * 2 * 3 * 32 * (64 + 64) and L.fpq_adapter_workspace_size(10, 32, 63, 24, 2, 3) >= need
+    p, off = C.c_void_p(4096), C.c_void_p(4104)
+
+    def call(R, a, b, ws, n):
+        return L.fpq_adapter_apply(C.byref(adapter_args(x_type=1, w_type=1, R=R)), p, a, b, p, p, None, ws, n, None)
+    assert call(20, p, p, None, 0) == -6 and call(20, p, p, p, need - 1) == -6 and call(20, p, p, off, need) == -5
+    assert call(24, off, p, None, 0) == -5 and call(24, p, off, None, 0) == -5
