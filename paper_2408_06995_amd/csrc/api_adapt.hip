@@ -404,6 +404,7 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
     a.out = o;
     a.lse = lse;
     a.blocks = plan.blocks;
+    a.q_pad = plan.q_pad;
     a.splits = plan.splits;
     a.per_split = plan.per_split;
     a.vec_out = p->head_dim % 4 == 0 && rows_aligned(o, p->o_strides, p->batch, p->q_len, p->q_heads, size, 4 * size);

@@ -378,6 +378,7 @@ struct AttentionArgs {
     int vec;                    // rows of the tensors may be read 16 bytes at a time
     Strides qs, ks, vs, os, gos, gqs, gks, gvs;
     int batch, kv_heads, group, q_len, kv_len, dim, causal;
+    int q_pad;                  // rows form, gradient of the queries: a head's rows in the grid
     float scale;
     int blocks;                 // blocks of rows (or keys) per sample and key head
     int splits, per_split;      // parts of the other axis, and its keys (or tiles of queries) per part
@@ -385,9 +386,11 @@ struct AttentionArgs {
     float *part, *part_lse;     // splits > 1: results of the parts
 };
 
-// The part of the grid that a workgroup works on.  Workgroups go round-robin over the eight XCDs; each XCD takes a contiguous run
-// of them, so that the blocks that read the same keys share an L2.  Under `causal` blocks differ in length by up to their number:
-// the longest (number 0) of all heads of an XCD go first, or, where the whole grid runs at once, the longest next to the shortest.
+// The part of the grid that a workgroup works on.  Workgroups go round-robin over the eight XCDs; the blocks that read the same keys
+// go to one of them, so that they share an L2.  Samples of different lengths (lens) go to all of them: heads one by one instead of
+// runs of heads, which would be runs of samples.  Under `causal` blocks differ in length by up to their number: the longest (number
+// 0) go first, or, where the whole grid runs at once, the longest next to the shortest; with lens too, an XCD then has blocks of
+// every head, of which the resident ones that read the same keys are few but run side by side.
 struct Place {
     int bh, split, block;
 };
@@ -397,15 +400,38 @@ __device__ __forceinline__ Place place_of(const AttentionArgs& a)
     int id = blockIdx.x;
     Place p;
     if (a.causal) {
-        const bool whole = (bhs & 7) == 0;
-        const int local = whole ? bhs >> 3 : bhs;
-        if (whole) id >>= 3;
-        p.split = id % a.splits;
-        id /= a.splits;
-        p.bh = id % local + (whole ? (int)(blockIdx.x & 7) * local : 0);
-        p.block = id / local;
+        if (a.lens) {
+            p.split = id % a.splits;
+            id /= a.splits;
+            p.block = id / bhs;
+            p.bh = (int)(((int64_t)id + p.block) % bhs);
+        } else {
+            const bool whole = (bhs & 7) == 0;
+            const int local = whole ? bhs >> 3 : bhs;
+            if (whole) id >>= 3;
+            p.split = id % a.splits;
+            id /= a.splits;
+            p.bh = id % local + (whole ? (int)(blockIdx.x & 7) * local : 0);
+            p.block = id / local;
+        }
         // all resident at once, two per compute unit: a long one and a short one each
         if (total <= 512 && 2 * p.block >= a.blocks) p.block = a.blocks - 1 - (p.block - a.blocks / 2 - (a.blocks & 1));
+        return p;
+    }
+    if (a.lens) {
+        const int units = bhs * a.splits, whole = (units & ~7) * a.blocks;
+        int unit;
+        if (id < whole) {
+            const int local = id >> 3, turn = local / a.blocks;
+            unit = turn * 8 + (id & 7);
+            p.block = local - turn * a.blocks;
+        } else {
+            id -= whole;
+            unit = (units & ~7) + id / a.blocks;
+            p.block = id % a.blocks;
+        }
+        p.split = unit / bhs;
+        p.bh = unit - p.split * bhs;
         return p;
     }
     if (id < (per << 3)) id = (id & 7) * per + (id >> 3);
@@ -438,12 +464,43 @@ __device__ __forceinline__ RowRange visible(const AttentionArgs& a, int n, int f
     return v;
 }
 
+// A block of 32 NW rows of the heads of a group, one head after the other, each with q_pad rows: q_len, or, where that costs little,
+// whole blocks, so that a block has one head's rows.  Under `causal` the blocks of the most keys come first, of all heads.
+struct RowBlock {
+    RowRange range;
+    int i, g, end;              // the lane's query and head of the group, and the keys that it sees; clamped to those that exist
+    bool in;
+};
+template <int NW>
+__device__ __forceinline__ RowBlock row_block(const AttentionArgs& a, int n, int number, int wave, int l32)
+{
+    RowBlock b;
+    if (a.causal) {
+        const int per = a.q_pad / (32 * NW);
+        number = a.q_pad % (32 * NW) ? a.blocks - 1 - number : (number % a.group + 1) * per - 1 - number / a.group;
+    }
+    const int all = a.group * a.q_pad, first = number * 32 * NW, last = min(first + 32 * NW, all) - 1;
+    auto real = [&](int r) {
+        const int g = r / a.q_pad;
+        return g * a.q_len + min(r - g * a.q_pad, a.q_len - 1);
+    };
+    b.range = visible(a, n, real(first), real(last));
+    const int r = first + 32 * wave + l32, rc = min(r, all - 1);
+    b.g = rc / a.q_pad;
+    const int i = rc - b.g * a.q_pad;
+    b.i = min(i, a.q_len - 1);
+    b.in = r < all && i < a.q_len;
+    b.end = a.causal ? max(0, min(n, b.i + n - a.q_len + 1)) : n;
+    return b;
+}
+
 // Queries of a tile of the backward pass's keys kernel.
 template <int NP, int KS>
 constexpr int kKeysTile = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 6 ? 64 : 32;
 
 // How a call's kernels are chosen and cut (host): by sizes and type only, the same for the size of the workspace.
 struct AttentionPlan {
+    int q_pad;                  // AttentionArgs
     bool by_keys;               // forward: the wavefronts of a workgroup share 32 rows and divide the keys
     int waves, blocks, splits, per_split;             // waves: of a workgroup, with 32 rows (or keys) each
     int q_waves, q_blocks, q_splits, q_per_split;     // backward, gradient of the queries

@@ -37,9 +37,8 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 3 : KS <= 8 ?
     const Place at = place_of(a);
     const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
     const int rows = a.group * a.q_len, n = keys_of(a, b);
-    const int block = a.causal ? a.blocks - 1 - at.block : at.block;
-    const int r_first = block * 32 * NW, r = r_first + 32 * wave + l32;
-    const RowRange range = visible(a, n, r_first, min(r_first + 32 * NW, rows) - 1);
+    const RowBlock mine = row_block<NW>(a, n, at.block, wave, l32);
+    const RowRange range = mine.range;
     const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
     Tiles feed;
     feed.src[0] = a.fk;
@@ -49,9 +48,8 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 3 : KS <= 8 ?
     feed.init(lds_address(lds), a.dim);
     if (kbeg < kend) feed.begin(kbeg, kend);
 
-    const int rc = min(r, rows - 1), g = rc / a.q_len, i = rc - g * a.q_len, head = hk * a.group + g;
-    const int end = a.causal ? max(0, min(n, i + n - a.q_len + 1)) : n;
-    const size_t row_id = (size_t)at.bh * rows + rc;
+    const int i = mine.i, g = mine.g, end = mine.end, head = hk * a.group + g;
+    const size_t row_id = (size_t)at.bh * rows + g * a.q_len + i;
     Frag<NP> qf[KS], gf[KS];
     float delta = 0.0f;
     {
@@ -119,7 +117,7 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 3 : KS <= 8 ?
             vt += 32 * Places<KS>::RS;
         }
     }
-    if (r >= rows) return;
+    if (!mine.in) return;
     if (h == 0 && at.split == 0) {
         float* const st = a.stats + stats_at(a, (size_t)at.bh * a.group + g, i);
         st[0] = log_sum == -kInf ? -kInf : -log_sum / a.scale;

@@ -9,6 +9,7 @@ int launch_attention_backward(const AttentionArgs& a, int type, const AttentionP
 {
     AttentionArgs aq = a, ak = a;
     aq.blocks = p.q_blocks;
+    aq.q_pad = p.q_pad;
     aq.splits = p.q_splits;
     aq.per_split = p.q_per_split;
     aq.part = part_q;

@@ -77,9 +77,8 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 4 : 2) : KS <
     const Place at = place_of(a);
     const int b = at.bh / a.kv_heads, hk = at.bh - b * a.kv_heads;
     const int rows = a.group * a.q_len, n = keys_of(a, b);
-    const int block = a.causal ? a.blocks - 1 - at.block : at.block;          // the longest rows first
-    const int r_first = block * 32 * NW, r = r_first + 32 * wave + l32;
-    const RowRange range = visible(a, n, r_first, min(r_first + 32 * NW, rows) - 1);
+    const RowBlock mine = row_block<NW>(a, n, at.block, wave, l32);
+    const RowRange range = mine.range;
     const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
     Tiles feed;
     feed.src[0] = a.fk;
@@ -89,8 +88,7 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 4 : 2) : KS <
     feed.init(lds_address(lds), a.dim);
     if (kbeg < kend) feed.begin(kbeg, kend);
 
-    const int rc = min(r, rows - 1), g = rc / a.q_len, i = rc - g * a.q_len, head = hk * a.group + g;
-    const int end = a.causal ? max(0, min(n, i + n - a.q_len + 1)) : n;       // the row sees keys below it
+    const int i = mine.i, end = mine.end, head = hk * a.group + mine.g;
     Frag<NP> qf[KS];
     row_frags<T, KS, NP>(static_cast<const T*>(a.q) + b * a.qs.b + i * a.qs.t + head * a.qs.h, h, a.dim, a.vec, qf);
     Places<KS> places;
@@ -131,9 +129,9 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 4 : 2) : KS <
         }
     }
     l += __shfl_xor(l, 32);
-    if (r >= rows) return;
+    if (!mine.in) return;
 
-    const size_t row_id = (size_t)at.bh * rows + rc;                          // = (b heads + head) q_len + i
+    const size_t row_id = (size_t)at.bh * rows + mine.g * a.q_len + i;        // = (b heads + head) q_len + i
     float* const part = a.splits > 1 ? a.part + (size_t)at.split * a.batch * a.kv_heads * rows * a.dim : nullptr;
     float* const lse = a.splits > 1 ? a.part_lse + (size_t)at.split * a.batch * a.kv_heads * rows : a.lse;
     const float inv = inverse(l);

@@ -32,7 +32,10 @@ AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int
     auto waves = [&](int64_t n) { return bh * ((n + 127) / 128) >= want / 2 ? 4 : 2; };
     auto blocks = [](int64_t n, int waves) { return (int)((n + 32 * waves - 1) / (32 * waves)); };
     p.waves = p.q_waves = waves(rows);
-    p.q_blocks = blocks(rows, p.q_waves);
+    // (blocks of one head's rows where that adds no more than a tenth)
+    const int64_t whole = (q_len + 32 * p.waves - 1) / (32 * p.waves) * (32 * p.waves);
+    p.q_pad = (int)(group > 1 && 10 * whole <= 11 * q_len ? whole : q_len);
+    p.q_blocks = blocks(group * p.q_pad, p.q_waves);
     cut(kv_len, bh * p.q_blocks, want, (int)least, least, &p.q_splits, &p.q_per_split);
     // keys form: few rows, or grids of the rows form that leave half of the compute units idle
     p.by_keys = rows <= few || bh * p.q_blocks * p.q_splits < 128;
