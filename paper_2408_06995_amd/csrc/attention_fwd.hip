@@ -27,7 +27,8 @@ AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int
     // keys), of no less than takes longer than the pass that joins them.  Measured over 256 or 512 workgroups and parts of no less
     // than 64 to 512: backward of 4 x 16 heads on 4 x 2048 x 128, bf16: 604 us with 256 workgroups, 517 with 512; forward of 8 x 8 x
     // 256 x 160, bf16: 25 us with parts of 128, 13 with 256; backward of 8 x 256 x 160, fp32: 71 us with parts of 64, 127 with
-    // 256; forward and backward of 2 x 8 x 1024 x 80, fp32: 205 us with 256 workgroups, 229 with 512.
+    // 256.  In fp32, workgroups whose registers let a compute unit hold two are cut to 512 too where queries are kept (dimensions up to
+    // 80: forward of 2 x 8 x 1024 x 80 57 -> 51 us, of 8 x 4096 x 40 199 -> 164; of 4 x 8 x 512 x 96 39 -> 40, its backward 105 -> 114).
     const int64_t want = fp32 ? 256 : 512, least = fp32 ? 64 : 256;
     auto waves = [&](int64_t n) { return bh * ((n + 127) / 128) >= want / 2 ? 4 : 2; };
     auto blocks = [](int64_t n, int waves) { return (int)((n + 32 * waves - 1) / (32 * waves)); };
@@ -36,7 +37,7 @@ AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int
     const int64_t whole = (q_len + 32 * p.waves - 1) / (32 * p.waves) * (32 * p.waves);
     p.q_pad = (int)(group > 1 && 10 * whole <= 11 * q_len ? whole : q_len);
     p.q_blocks = blocks(group * p.q_pad, p.q_waves);
-    cut(kv_len, bh * p.q_blocks, want, (int)least, least, &p.q_splits, &p.q_per_split);
+    cut(kv_len, bh * p.q_blocks, ks <= 5 ? 512 : want, (int)least, least, &p.q_splits, &p.q_per_split);
     // keys form: few rows, or grids of the rows form that leave half of the compute units idle
     p.by_keys = rows <= few || bh * p.q_blocks * p.q_splits < 128;
     p.blocks = p.by_keys ? (int)((rows + few - 1) / few) : p.q_blocks;
