@@ -381,7 +381,7 @@ struct AttentionArgs {
     int q_pad;                  // rows form, gradient of the queries: a head's rows in the grid
     float scale;
     int blocks;                 // blocks of rows (or keys) per sample and key head
-    int splits, per_split;      // parts of the other axis, and its keys (or tiles of queries) per part
+    int splits;                 // parts of the other axis
     int vec_out;                // results may be stored four values at a time (bit 0: out / gq)
     float *part, *part_lse;     // splits > 1: results of the parts
 };
@@ -464,6 +464,18 @@ __device__ __forceinline__ RowRange visible(const AttentionArgs& a, int n, int f
     return v;
 }
 
+// A part of what a workgroup has to go through (keys that its rows see, tiles of queries that see its keys), in whole units: equal
+// parts of each workgroup's own, which differ under `causal` and between samples.
+struct Part {
+    int64_t beg, end;
+};
+__device__ __forceinline__ Part part_of(int64_t all, int unit, int split, int splits)
+{
+    const int64_t units = (all + unit - 1) / unit;
+    auto upto = [&](int s) { return min((units * s + splits - 1) / splits * unit, all); };      // (the first part has the first unit)
+    return {upto(split), upto(split + 1)};
+}
+
 // A block of 32 NW rows of the heads of a group, one head after the other, each with q_pad rows: q_len, or, where that costs little,
 // whole blocks, so that a block has one head's rows.  Under `causal` the blocks of the most keys come first, of all heads.
 struct RowBlock {
@@ -502,9 +514,9 @@ constexpr int kKeysTile = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 6 ? 64 : 32;
 struct AttentionPlan {
     int q_pad;                  // AttentionArgs
     bool by_keys;               // forward: the wavefronts of a workgroup share 32 rows and divide the keys
-    int waves, blocks, splits, per_split;             // waves: of a workgroup, with 32 rows (or keys) each
-    int q_waves, q_blocks, q_splits, q_per_split;     // backward, gradient of the queries
-    int k_waves, k_blocks, k_splits, k_per_split;     // backward, gradient of the keys and values
+    int waves, blocks, splits;                        // waves: of a workgroup, with 32 rows (or keys) each
+    int q_waves, q_blocks, q_splits;                  // backward, gradient of the queries
+    int k_waves, k_blocks, k_splits;                  // backward, gradient of the keys and values
 };
 AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int64_t dim, int type);
 

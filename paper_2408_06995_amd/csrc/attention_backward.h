@@ -39,7 +39,8 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 3 : KS <= 8 ?
     const int rows = a.group * a.q_len, n = keys_of(a, b);
     const RowBlock mine = row_block<NW>(a, n, at.block, wave, l32);
     const RowRange range = mine.range;
-    const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
+    const Part keys = part_of(range.hi, KT, at.split, a.splits);
+    const int kbeg = (int)keys.beg, kend = (int)keys.end;
     Tiles feed;
     feed.src[0] = a.fk;
     feed.src[1] = a.fv;
@@ -168,7 +169,8 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void a
     const int tiles_all = (a.q_len + QT - 1) / QT, skip = a.causal ? min(max(0, j_first - off) / QT, tiles_all) : 0;
     const int per_head = j_first < n ? tiles_all - skip : 0, per = max(per_head, 1);
     const int64_t tiles = (int64_t)per_head * a.group;
-    const int64_t tbeg = min((int64_t)at.split * a.per_split, tiles), tend = min(tbeg + a.per_split, tiles);
+    const Part part = part_of(tiles, 1, at.split, a.splits);
+    const int64_t tbeg = part.beg, tend = part.end;
     Tiles feed;
     int g = (int)(tbeg / per), i0 = (skip + (int)(tbeg - (int64_t)g * per)) * QT, slot = 0;
     feed.src[0] = a.fq;

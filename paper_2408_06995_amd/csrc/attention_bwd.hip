@@ -11,11 +11,9 @@ int launch_attention_backward(const AttentionArgs& a, int type, const AttentionP
     aq.blocks = p.q_blocks;
     aq.q_pad = p.q_pad;
     aq.splits = p.q_splits;
-    aq.per_split = p.q_per_split;
     aq.part = part_q;
     ak.blocks = p.k_blocks;
     ak.splits = p.k_splits;
-    ak.per_split = p.k_per_split;
     ak.part = part_kv;
     return type == FPQ_TYPE_FP32 ? launch_attention_backward_f32(aq, ak, p, s) : launch_backward<__bf16>(aq, ak, p, s);
 }

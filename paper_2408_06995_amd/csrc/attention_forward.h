@@ -79,7 +79,8 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 4 : 2) : KS <
     const int rows = a.group * a.q_len, n = keys_of(a, b);
     const RowBlock mine = row_block<NW>(a, n, at.block, wave, l32);
     const RowRange range = mine.range;
-    const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
+    const Part keys = part_of(range.hi, KT, at.split, a.splits);
+    const int kbeg = (int)keys.beg, kend = (int)keys.end;
     Tiles feed;
     feed.src[0] = a.fk;
     feed.src[1] = a.fv;
@@ -176,7 +177,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
     const int block = a.causal ? a.blocks - 1 - at.block : at.block;
     const int r_first = block * RB, r = r_first + 32 * rg + l32;
     const RowRange range = visible(a, n, r_first, min(r_first + RB, rows) - 1);
-    const int kbeg = min((int64_t)at.split * a.per_split, (int64_t)range.hi), kend = min((int64_t)kbeg + a.per_split, (int64_t)range.hi);
+    const Part keys = part_of(range.hi, KT, at.split, a.splits);
+    const int kbeg = (int)keys.beg, kend = (int)keys.end;
     const T* const kbase = static_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
     const T* const vbase = static_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
     Stage<T, KS, VEC, KT, 256> sk, sv;

@@ -5,15 +5,12 @@ namespace fpq {
 
 int launch_attention_f32(const AttentionArgs& a, bool by_keys, int waves, hipStream_t s);
 
-// Parts of an axis of `len` in units: until there are about `want` workgroups, with no fewer than `least` each.
-static void cut(int64_t len, int64_t have, int64_t want, int unit, int64_t least, int* n, int* per)
+// Parts of an axis of `len`: until there are about `want` workgroups, with no fewer than `least` each.
+static int parts_of(int64_t len, int64_t have, int64_t want, int64_t least)
 {
     int64_t s = have > 0 ? (want + have - 1) / have : 1;
     if (s > len / least) s = len / least;
-    s = s < 1 ? 1 : s > 32 ? 32 : s;
-    if (len < 1) len = 1;
-    *per = (int)(((len + s - 1) / s + unit - 1) / unit * unit);
-    *n = (int)((len + *per - 1) / *per);
+    return s < 1 ? 1 : s > 32 ? 32 : (int)s;
 }
 
 AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int64_t dim, int type)
@@ -37,19 +34,16 @@ AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int
     const int64_t whole = (q_len + 32 * p.waves - 1) / (32 * p.waves) * (32 * p.waves);
     p.q_pad = (int)(group > 1 && 10 * whole <= 11 * q_len ? whole : q_len);
     p.q_blocks = blocks(group * p.q_pad, p.q_waves);
-    cut(kv_len, bh * p.q_blocks, ks <= 5 ? 512 : want, (int)least, least, &p.q_splits, &p.q_per_split);
+    p.q_splits = parts_of(kv_len, bh * p.q_blocks, ks <= 5 ? 512 : want, least);
     // keys form: few rows, or grids of the rows form that leave half of the compute units idle
     p.by_keys = rows <= few || bh * p.q_blocks * p.q_splits < 128;
     p.blocks = p.by_keys ? (int)((rows + few - 1) / few) : p.q_blocks;
-    if (p.by_keys)
-        cut(kv_len, bh * p.blocks, 512, 128, fp32 ? 128 : 256, &p.splits, &p.per_split);
-    else
-        p.splits = p.q_splits, p.per_split = p.q_per_split;
+    p.splits = p.by_keys ? parts_of(kv_len, bh * p.blocks, 512, fp32 ? 128 : 256) : p.q_splits;
     p.k_waves = waves(kv_len);
     p.k_blocks = blocks(kv_len, p.k_waves);
     const int tile = fp32 ? kKeysTile<3, 3> : ks <= 4 ? kKeysTile<1, 4> : ks <= 6 ? kKeysTile<1, 6> : kKeysTile<1, 8>;
     const int64_t tiles = group * ((q_len + tile - 1) / tile);
-    cut(tiles, bh * p.k_blocks, want, 1, (least + tile - 1) / tile, &p.k_splits, &p.k_per_split);
+    p.k_splits = parts_of(tiles, bh * p.k_blocks, want, (least + tile - 1) / tile);
     return p;
 }
 
