@@ -33,9 +33,9 @@ int check_attention(const fpq_attention_args_t* p)
     return FPQ_OK;
 }
 
-AttentionPlan plan_of(const fpq_attention_args_t* p)
+AttentionPlan plan_of(const fpq_attention_args_t* p, bool causal)
 {
-    return plan_attention(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->q_len, p->kv_len, p->head_dim, p->type);
+    return plan_attention(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->q_len, p->kv_len, p->head_dim, p->type, causal);
 }
 
 size_t rows_of(const fpq_attention_args_t* p) { return (size_t)p->batch * p->q_heads * p->q_len; }
@@ -373,13 +373,19 @@ int fpq_adamw_step(const void* plan, int64_t pieces, double lr, double beta1, do
     return launch_adamw(plan, pieces, lr, beta1, beta2, eps, weight_decay, step, grad_scale, static_cast<hipStream_t>(stream));
 }
 
+// (what is stated is enough with and without `causal`)
 size_t fpq_attention_workspace_size(const fpq_attention_args_t* p)
 {
     if (check_attention(p) != FPQ_OK || no_rows(p)) return 0;
-    const AttentionPlan plan = plan_of(p);
     const size_t rows = rows_of(p);
-    return (plan.splits > 1 ? align_up(plan.splits * rows * p->head_dim * 4) + align_up(plan.splits * rows * 4) : 0) +
-           (plan.by_keys ? 0 : 2 * planes_size(p, keys_of(p)));
+    size_t most = 0;
+    for (bool causal : {false, true}) {
+        const AttentionPlan plan = plan_of(p, causal);
+        const size_t size = (plan.splits > 1 ? align_up(plan.splits * rows * p->head_dim * 4) + align_up(plan.splits * rows * 4) : 0) +
+                            (plan.by_keys ? 0 : 2 * planes_size(p, keys_of(p)));
+        most = size > most ? size : most;
+    }
+    return most;
 }
 
 int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* workspace,
@@ -392,7 +398,7 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
     const size_t size = size_of(p->type);
     if (!aligned(q, size) || !aligned(k, size) || !aligned(v, size) || !aligned(o, size) || !aligned(lse, 4) || !aligned(p->kv_lens, 4))
         return FPQ_ERR_ALIGN;
-    const AttentionPlan plan = plan_of(p);
+    const AttentionPlan plan = plan_of(p, p->causal);
     if (!grid_ok(p, plan.blocks, plan.splits)) return FPQ_ERR_SHAPE;
     const size_t need = fpq_attention_workspace_size(p);
     if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;
@@ -430,11 +436,15 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
 size_t fpq_attention_backward_workspace_size(const fpq_attention_args_t* p)
 {
     if (check_attention(p) != FPQ_OK) return 0;
-    const AttentionPlan plan = plan_of(p);
     const size_t dim = p->head_dim;
-    return stats_size(p) + (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
-           (plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * dim * 4) : 0) + 2 * planes_size(p, keys_of(p)) +
-           2 * planes_size(p, rows_of(p));
+    size_t most = 0;
+    for (bool causal : {false, true}) {
+        const AttentionPlan plan = plan_of(p, causal);
+        const size_t size = (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
+                            (plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * dim * 4) : 0);
+        most = size > most ? size : most;
+    }
+    return stats_size(p) + most + 2 * planes_size(p, keys_of(p)) + 2 * planes_size(p, rows_of(p));
 }
 
 int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -449,7 +459,7 @@ int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const v
     for (const void* x : {q, k, v, o, grad_o, static_cast<const void*>(grad_q), static_cast<const void*>(grad_k), static_cast<const void*>(grad_v)})
         if (!aligned(x, size)) return FPQ_ERR_ALIGN;
     if (!aligned(lse, 4) || !aligned(p->kv_lens, 4)) return FPQ_ERR_ALIGN;
-    const AttentionPlan plan = plan_of(p);
+    const AttentionPlan plan = plan_of(p, p->causal);
     if (!grid_ok(p, plan.q_blocks, plan.q_splits) || !grid_ok(p, plan.k_blocks, plan.k_splits)) return FPQ_ERR_SHAPE;
     const size_t need = fpq_attention_backward_workspace_size(p);
     if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;

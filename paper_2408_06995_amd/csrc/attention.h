@@ -518,7 +518,7 @@ struct AttentionPlan {
     int q_waves, q_blocks, q_splits;                  // backward, gradient of the queries
     int k_waves, k_blocks, k_splits;                  // backward, gradient of the keys and values
 };
-AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int64_t dim, int type);
+AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int64_t dim, int type, bool causal);
 
 // A tensor and where its planes go: [plane][batch * heads][len][cols], cols = dim rounded up to 8.
 struct Pack {
