@@ -32,6 +32,11 @@ constexpr float kInf = __builtin_inff();
 
 template <typename T>
 constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+// Planes of the probabilities and their gradients as operands.  Beside bf16 operands one, whose rounding is of the size of the
+// results' own; two in small problems (`fine`), where results hang on the roundings of so few of them that these do not average out,
+// and where matrix steps cost nothing.
+template <typename T, bool FINE>
+constexpr int kPlanesP = sizeof(T) == 4 ? 3 : FINE ? 2 : 1;
 
 // Elements of a tile row in LDS for KS steps of 16 columns: 16 bytes more, which make the row an odd number of 16-byte places, so
 // that the 16 rows of a quarter wave's read start in different banks.  Output tiles of 32 columns may reach past a row with an odd
@@ -45,10 +50,13 @@ struct Frag {
     v8bf p[NP];
 };
 
-template <int NP>
-__device__ __forceinline__ void mma(v16f& c, const Frag<NP>& a, const Frag<NP>& b)
+template <int NA, int NB>
+__device__ __forceinline__ void mma(v16f& c, const Frag<NA>& a, const Frag<NB>& b)
 {
-    if constexpr (NP == 3) {                       // small products first
+    static_assert(NA == NB || NA * NB == 2, "three planes with three, or one with one or two");
+    if constexpr (NA == 1 && NB == 2) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[0], b.p[1], c, 0, 0, 0);
+    if constexpr (NA == 2 && NB == 1) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[1], b.p[0], c, 0, 0, 0);
+    if constexpr (NA == 3) {                       // small products first
         c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[2], b.p[0], c, 0, 0, 0);
         c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[0], b.p[2], c, 0, 0, 0);
         c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[1], b.p[1], c, 0, 0, 0);
@@ -77,10 +85,10 @@ template <int NP>
 __device__ __forceinline__ void planes_of_pair(float a, float b, uint32_t (&out)[NP])
 {
     out[0] = pair_bf16(a, b);
-    if constexpr (NP == 3) {
+    if constexpr (NP >= 2) {
         const float ra = a - __uint_as_float(out[0] << 16), rb = b - __uint_as_float(out[0] & 0xffff0000u);
         out[1] = pair_bf16(ra, rb);
-        out[2] = pair_bf16(ra - __uint_as_float(out[1] << 16), rb - __uint_as_float(out[1] & 0xffff0000u));
+        if constexpr (NP == 3) out[2] = pair_bf16(ra - __uint_as_float(out[1] << 16), rb - __uint_as_float(out[1] & 0xffff0000u));
     }
 }
 
@@ -375,6 +383,7 @@ struct AttentionArgs {
     float *lse, *stats;         // stats: two values per row, from the queries kernel for the keys kernel
     const int32_t* lens;
     Source fq, fk, fv, fgo;     // as the feed reads them
+    int fine;                   // kPlanesP
     int vec;                    // rows of the tensors may be read 16 bytes at a time
     Strides qs, ks, vs, os, gos, gqs, gks, gvs;
     int batch, kv_heads, group, q_len, kv_len, dim, causal;
@@ -513,6 +522,7 @@ constexpr int kKeysTile = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 6 ? 64 : 32;
 // How a call's kernels are chosen and cut (host): by sizes and type only, the same for the size of the workspace.
 struct AttentionPlan {
     int q_pad;                  // AttentionArgs
+    bool fine;                  // kPlanesP
     bool by_keys;               // forward: the wavefronts of a workgroup share 32 rows and divide the keys
     int waves, blocks, splits;                        // waves: of a workgroup, with 32 rows (or keys) each
     int q_waves, q_blocks, q_splits;                  // backward, gradient of the queries

@@ -73,10 +73,10 @@ struct RowsShape {
     typedef Feed<NP, KS, KT, 2, NW> Tiles;
 };
 
-template <typename T, int KS, int NW>
-__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 4 : 2) : KS <= 6 ? 2 : 1) void attention_rows_kernel(AttentionArgs a)
+template <typename T, int KS, int NW, bool FINE>
+__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 && !FINE ? 4 : 2) : KS <= 6 ? 2 : 1) void attention_rows_kernel(AttentionArgs a)
 {
-    constexpr int NP = kPlanes<T>, DT = (KS + 1) / 2;
+    constexpr int NP = kPlanes<T>, PP = kPlanesP<T, FINE>, DT = (KS + 1) / 2;
     typedef RowsShape<NP, KS, NW> Sh;
     typedef typename Sh::Tiles Tiles;
     constexpr int KT = Sh::KT, NS = Sh::NS, PLANE = Tiles::PLANE / 2;
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 4 : 2) : KS <
                     float v[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = s[u][8 * t + e];
-                    const Frag<NP> pf = frag_of<NP>(v);
+                    const Frag<PP> pf = frag_of<PP>(v);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) mma<NP>(acc[d], cols_at<NP, KS>(vt, PLANE, places, 32 * u + 16 * t, d), pf);
                 }
@@ -169,11 +169,11 @@ struct KeysFormShape {
     static constexpr int LDS = TILES > JOIN ? TILES : JOIN;
 };
 
-template <typename T, int KS, bool VEC>
+template <typename T, int KS, bool VEC, bool FINE>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_keys_form_kernel(AttentionArgs a)
 {
     typedef KeysFormShape<T, KS> Sh;
-    constexpr int NP = Sh::NP, RS = Sh::RS, DT = Sh::DT, KT = Sh::KT, RG = Sh::RG, KG = Sh::KG, RB = 32 * RG;
+    constexpr int NP = Sh::NP, PP = kPlanesP<T, FINE>, RS = Sh::RS, DT = Sh::DT, KT = Sh::KT, RG = Sh::RG, KG = Sh::KG, RB = 32 * RG;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     __bf16* const kt = reinterpret_cast<__bf16*>(lds);
     __bf16* const vt = kt + Sh::TILE;
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = s[0][8 * t + e];
-            const Frag<NP> pf = frag_of<NP>(v);
+            const Frag<PP> pf = frag_of<PP>(v);
 #pragma unroll
             for (int d = 0; d < DT; ++d) mma<NP>(acc[d], col_frag<NP, RS, KT>(vt, 32 * kg + 16 * t, 32 * d, lane), pf);
         }
@@ -324,31 +324,41 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
         if (lane + 32 * d < a.dim) out[lane + 32 * d] = (T)(v[d] * inv);
 }
 
-template <typename T, int KS, int NW>
+template <typename T, int KS, int NW, bool FINE>
 int launch_rows(const AttentionArgs& a, hipStream_t s)
 {
     constexpr int lds = RowsShape<kPlanes<T>, KS, NW>::Tiles::LDS;
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_rows_kernel<T, KS, NW>), lds, done)) return FPQ_ERR_LAUNCH;
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_rows_kernel<T, KS, NW, FINE>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_rows_kernel<T, KS, NW><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
+    attention_rows_kernel<T, KS, NW, FINE><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
     return FPQ_OK;
 }
 template <typename T, int KS>
 int launch_rows(const AttentionArgs& a, int waves, hipStream_t s)
 {
-    return waves == 4 ? launch_rows<T, KS, 4>(a, s) : launch_rows<T, KS, 2>(a, s);
+    if constexpr (sizeof(T) == 2)
+        if (a.fine) return launch_rows<T, KS, 2, true>(a, s);
+    return waves == 4 ? launch_rows<T, KS, 4, false>(a, s) : launch_rows<T, KS, 2, false>(a, s);
+}
+
+template <typename T, int KS, bool VEC, bool FINE>
+int launch_keys_form(const AttentionArgs& a, hipStream_t s)
+{
+    constexpr int lds = KeysFormShape<T, KS>::LDS;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_form_kernel<T, KS, VEC, FINE>), lds, done)) return FPQ_ERR_LAUNCH;
+    const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
+    attention_keys_form_kernel<T, KS, VEC, FINE><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
+    return FPQ_OK;
 }
 
 template <typename T, int KS, bool VEC>
 int launch_keys_form(const AttentionArgs& a, hipStream_t s)
 {
-    constexpr int lds = KeysFormShape<T, KS>::LDS;
-    static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_form_kernel<T, KS, VEC>), lds, done)) return FPQ_ERR_LAUNCH;
-    const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_keys_form_kernel<T, KS, VEC><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
-    return FPQ_OK;
+    if constexpr (sizeof(T) == 2)
+        if (a.fine) return launch_keys_form<T, KS, VEC, true>(a, s);
+    return launch_keys_form<T, KS, VEC, false>(a, s);
 }
 
 template <typename T>
