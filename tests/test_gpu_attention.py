@@ -243,3 +243,36 @@ def test_few_keys_of_many_rows(shape, causal, t):
     close(o[few], want_o, to, "o")
     close(lse[few], want_lse, tl, "lse")
     assert not o.isnan().any() and not lse.isnan().any()
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("dim", [40, 64, 80, 96, 128, 157, 160])
+@pytest.mark.parametrize("shape", [(32, 150, 140, 8, 4), (3, 640, 500, 4, 2), (6, 200, 333, 8, 1)])
+def test_larger_problems(shape, dim, causal, t):
+    """Workgroups of two and four wavefronts, one plane of the probabilities in bf16, blocks of one head's rows, samples of different
+    lengths and of none; a few of the samples against the oracle, which they are independent of."""
+    print(shape, dim, causal, t, flush=True)
+    n = shape[2]
+    lens = [(37 * b + 5) % (n + 1) if b % 3 else n for b in range(shape[0])]
+    lens[1] = 0
+    q, k, v, go = tensors(*shape, dim, t, dim)
+    for b in range(shape[0]):
+        k[b, lens[b]:] = float("nan")
+        v[b, lens[b]:] = float("inf")
+    scale = dim ** -0.5
+    lens_t = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    o, lse = forward(q, k, v, scale, causal, lens_t)
+    grads = backward(q, k, v, o, lse, go, scale, causal, lens_t)
+    few = [0, 1, shape[0] - 1]
+    a = [host(x[few]) for x in (q, k, v)]
+    some = [lens[b] for b in few]
+    scale = float(np.float32(scale))
+    want_o, want_lse = adapt.attention(*a, scale, causal, some)
+    want = adapt.attention_backward(*a, host(go[few]), scale, causal, some)
+    to, tl, *tg = adapt.attention_bounds(*a, scale, causal, some, t == "bf16", host(go[few]))
+    close(o[few], want_o, to, "o")
+    close(lse[few], want_lse, tl, "lse")
+    for name, got, w, b in zip(("gq", "gk", "gv"), grads, want, tg):
+        close(got[few], w, b, name)
+    assert not any(x.isnan().any() for x in (o, lse, *grads))
