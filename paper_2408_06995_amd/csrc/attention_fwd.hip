@@ -54,7 +54,11 @@ AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int
     p.k_blocks = blocks(kv_len, p.k_waves);
     const int tile = fp32 ? kKeysTile<3, 3> : ks <= 4 ? kKeysTile<1, 4> : ks <= 6 ? kKeysTile<1, 6> : kKeysTile<1, 8>;
     const int64_t tiles = group * ((q_len + tile - 1) / tile);
-    p.k_splits = at_most(parts_of(tiles, bh * p.k_blocks, want, (least + tile - 1) / tile), tiles, fp32 ? 32 : 64);
+    // (workgroups of two wavefronts in fp32: 512, one wavefront per SIMD, up to dimension 80.  Backward of 64 heads of 4096 on 77 keys x
+    // 40: 304 -> 238 us, of 1024 on 77 x 80 125 -> 104; kernel of 448 heads of 2437 on 25 x 96 442 -> 508, backward of 256 on 77 x 160
+    // 108 -> 127.)
+    const int64_t want_k = fp32 && p.k_waves == 2 && ks <= 5 ? 512 : want;
+    p.k_splits = at_most(parts_of(tiles, bh * p.k_blocks, want_k, (least + tile - 1) / tile), tiles, fp32 ? 32 : 64);
     return p;
 }
 
