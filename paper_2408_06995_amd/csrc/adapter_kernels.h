@@ -105,7 +105,7 @@ struct MapShape {
 // time, in tiles of the 32 x 32 instruction whose lanes hold neighbouring columns.  t never leaves the workgroup unless it is
 // asked for.  Bound by the bytes of the rows, if enough of them are under way: hence two tiles of the base ahead (one: 29 us for 24),
 // and nothing loaded behind the stores, which it would wait for.
-//   32768 x 320 -> 320, rank 16, fp32 with bf16 weights: 24 us, 5.2 TB/s;  16384 x 320 -> 960, fp32: 32 us, 4.6 TB/s (its gradient
+//   32768 x 320 -> 320, rank 16, fp32 with bf16 weights: 24 us, 5.2 TB/s;  16384 x 320 -> 960, fp32: 35 us, 4.2 TB/s (its gradient
 //   24 us);  5003 ragged rows of 1280 -> 5120, rank 64, bf16: 55 us (its gradient 30): 195 workgroups, bound by the latency of a
 //   wavefront's tiles and the weights' way through LDS;  64 rows of 1280, an adapter each: 9 us, a launch and three latencies.
 // W: 0 fp32 weights, split where they are read; 1 bf16; 2, 3 packed in the order of the operands, bf16 and three
