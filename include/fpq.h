@@ -461,8 +461,9 @@ int fpq_gemm_grouped(const fpq_gemm_problem_t *problems, int count, int x_is_fp3
  * the rows that see them infinite or NaN (in FPQ_TYPE_FP32 always NaN), and under `causal` also rows of the same tile that do not.
  *
  * type: of q, k, v, o and the gradients.  Sums, maxima and log-sums are fp32.  Products of FPQ_TYPE_BF16 are exact, the
- * probabilities and their gradients are rounded to bf16 where they are multiplied; FPQ_TYPE_FP32 splits operands into three bf16
- * parts as fpq_rl_step does (an error of fp32's order; magnitudes below 2^-110 keep fewer bits).  The bits of a result do not
+ * probabilities and their gradients keep 16 bits where they are multiplied, so that results are off by little more than their own
+ * rounding; o enters the backward pass as it was rounded.  FPQ_TYPE_FP32 splits operands into three bf16 parts as fpq_rl_step does
+ * (an error of fp32's order; magnitudes below 2^-110 keep fewer bits).  The type alone decides the precision, no size does.  The bits of a result do not
  * depend on anything but the arguments: no atomics.
  * Tensors are [batch, tokens, heads, head_dim] with strides (sample, token, head; in elements) of their own, so that q, k and v can
  * be columns of one projection's result; the elements of a head are neighbours.  Rows of a multiple of 16 bytes that start at one

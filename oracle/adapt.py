@@ -109,6 +109,59 @@ def attention_bounds(q, k, v, scale, causal, lens, bf16, go=None):
     return to, tl, tq + r * np.abs(gq), tk + r * np.abs(gk), tv + r * np.abs(gv)
 
 
+def attention_spread(q, k, v, scale, causal, lens, go=None):
+    """How far results of bf16 attention are off ahead of their own rounding, for o (and, with go, for gq, gk, gv): a standard deviation per
+    element, roundings taken as independent and uniform where they are of many values, and as a bound where one is shared or made in
+    32 bits.
+
+    Probabilities and their gradients as operands keep 16 bits, u = U16^2; delta = do . o takes o as it was rounded to bf16."""
+    B, Lq, Hq, D = q.shape
+    G, third = Hq // k.shape[2], 3.0 ** -0.5
+    so, sq = np.zeros(q.shape), np.zeros(q.shape)
+    k2, k1, v2, v1 = (np.zeros(k.shape) for _ in range(4))             # squares of what is independent, and what adds up
+    for b in range(B):
+        n = keys_of(lens, b, k.shape[1])
+        for x in range(Hq):
+            Q, K, V = _head(q, k, v, b, x, G, n)
+            p, lse = _probabilities(Q, K, scale, causal)
+            mass = np.where(visible(Lq, n, causal), scale * (np.abs(Q) @ np.abs(K).T), 0.0).max(1, initial=0.0, keepdims=True)
+            # a probability's own relative error, and what it shares with its row (the sum, the log-sum)
+            s = U16 ** 2 * third + (D + 16) * U32 * mass + 8 * U32
+            row = s + (n + 16) * U32 + 2 * U32 * np.abs(np.where(np.isfinite(lse), lse, 0.0))[:, None]
+            o = p @ V
+            so[b, :, x] = s * np.sqrt((p * p) @ (V * V)) + row * np.abs(o) + (n + 8) * U32 * (p @ np.abs(V))
+            if go is None:
+                continue
+            dO = go[b, :, x].astype(np.float64)
+            dp = dO @ V.T
+            ds = p * (dp - (p * dp).sum(1, keepdims=True))
+            d_delta = np.sqrt((dO ** 2 * ((U16 * third * o) ** 2 + so[b, :, x] ** 2)).sum(1, keepdims=True)) + (D + 8) * U32 * (np.abs(dO) * np.abs(o)).sum(1, keepdims=True)
+            own = np.abs(ds) * (s + row) + p * (D + 16) * U32 * (np.abs(dO) @ np.abs(V).T)
+            sq[b, :, x] = scale * (np.sqrt((own * own) @ (K * K)) + d_delta * np.abs(p @ K) + row * np.abs(ds @ K) + (n + 8) * U32 * (np.abs(ds) @ np.abs(K)))
+            k2[b, :n, x // G] += scale ** 2 * ((own * own + (p * d_delta) ** 2).T @ (Q * Q))
+            k1[b, :n, x // G] += scale * (G * Lq + 8) * U32 * (np.abs(ds).T @ np.abs(Q))
+            v2[b, :n, x // G] += ((p * (s + row)) ** 2).T @ (dO * dO)
+            v1[b, :n, x // G] += (G * Lq + 8) * U32 * (p.T @ np.abs(dO))
+    return (so,) if go is None else (so, sq, np.sqrt(k2) + k1, np.sqrt(v2) + v1)
+
+
+def bf16(x):
+    """Rounded to bf16, to nearest even (finite values within its range)."""
+    u = np.asarray(x, np.float32).view(np.uint32).astype(np.uint64)
+    return ((u + 0x7fff + ((u >> 16) & 1)) & 0xffff0000).astype(np.uint32).view(np.float32).astype(np.float64)
+
+
+def off_in_norm(got, want, spread):
+    """The squared distance of bf16 results `got` from `want` rounded to bf16, over the largest that `spread` gives it.
+
+    A value that is off by e before it is rounded comes out one unit in the last place, w, beside the right one with a probability of
+    |e| / w: its square is w |e| + e^2 on average, and its variance at most w^3 |e|.  Four of its standard deviations, and half as much
+    again on the average for errors that share a rounding."""
+    w = np.where(want == 0, 0.0, 2.0 ** (np.floor(np.log2(np.where(want == 0, 1.0, np.abs(want)))) - 7))
+    most = 1.5 * (spread * w + spread ** 2).sum() + 4 * np.sqrt((spread * w ** 3).sum())
+    return ((got - bf16(want)) ** 2).sum() / most
+
+
 # ------------------------------------------------------------------------------------------------ AdamW
 
 BLOCK, E4M3_MAX = 256, 448.0

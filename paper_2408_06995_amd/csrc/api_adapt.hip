@@ -411,7 +411,6 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
     a.lse = lse;
     a.blocks = plan.blocks;
     a.q_pad = plan.q_pad;
-    a.fine = plan.fine;
     a.splits = plan.splits;
     a.vec_out = p->head_dim % 4 == 0 && rows_aligned(o, p->o_strides, p->batch, p->q_len, p->q_heads, size, 4 * size);
     a.vec = rows_vec(q, p->q_strides, p->batch, p->q_len, p->q_heads, p->head_dim, size) &&

@@ -30,10 +30,10 @@ struct QueriesShape {
     typedef Feed<NP, KS, KT, 2, NW> Tiles;
 };
 
-template <typename T, int KS, int NW, bool FINE>
-__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 && !FINE ? 3 : KS <= 8 ? 2 : 1) : KS <= 5 ? 2 : 1) void attention_queries_kernel(AttentionArgs a)
+template <typename T, int KS, int NW>
+__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 3 : KS <= 8 ? 2 : 1) : KS <= 5 ? 2 : 1) void attention_queries_kernel(AttentionArgs a)
 {
-    constexpr int NP = kPlanes<T>, PP = kPlanesP<T, FINE>, DT = (KS + 1) / 2;
+    constexpr int NP = kPlanes<T>, PP = kPlanesP<T>, DT = (KS + 1) / 2;
     typedef QueriesShape<NP, KS, NW> Sh;
     typedef typename Sh::Tiles Tiles;
     constexpr int KT = Sh::KT, PLANE = Tiles::PLANE / 2;
@@ -157,10 +157,10 @@ struct KeysShape {
     static constexpr int LDS = VALUES + (VLDS ? Values::TILE : 0);
 };
 
-template <typename T, int KS, int WHAT, int NW, bool FINE>
-__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 && KS <= (FINE ? 6 : 8) ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
+template <typename T, int KS, int WHAT, int NW>
+__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 && KS <= 8 ? 2 : 1) void attention_keys_kernel(AttentionArgs a)
 {
-    constexpr int NP = kPlanes<T>, PP = kPlanesP<T, FINE>, DT = (KS + 1) / 2;
+    constexpr int NP = kPlanes<T>, PP = kPlanesP<T>, DT = (KS + 1) / 2;
     typedef KeysShape<NP, KS, NW> Sh;
     typedef typename Sh::Tiles Tiles;
     constexpr int QT = Sh::QT, PLANE = Tiles::PLANE / 2;
@@ -365,42 +365,38 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(SumArgs a)
     }
 }
 
-template <typename T, int KS, int NW, bool FINE>
+template <typename T, int KS, int NW>
 int launch_queries(const AttentionArgs& a, hipStream_t s)
 {
     constexpr int lds = QueriesShape<kPlanes<T>, KS, NW>::Tiles::LDS;
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_queries_kernel<T, KS, NW, FINE>), lds, done)) return FPQ_ERR_LAUNCH;
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_queries_kernel<T, KS, NW>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_queries_kernel<T, KS, NW, FINE><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
+    attention_queries_kernel<T, KS, NW><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
     return FPQ_OK;
 }
 
-template <typename T, int KS, int WHAT, int NW, bool FINE>
+template <typename T, int KS, int WHAT, int NW>
 int launch_keys(const AttentionArgs& a, hipStream_t s)
 {
     constexpr int lds = KeysShape<kPlanes<T>, KS, NW>::LDS;
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_kernel<T, KS, WHAT, NW, FINE>), lds, done)) return FPQ_ERR_LAUNCH;
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_kernel<T, KS, WHAT, NW>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_keys_kernel<T, KS, WHAT, NW, FINE><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
+    attention_keys_kernel<T, KS, WHAT, NW><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
     return FPQ_OK;
 }
 
 template <typename T, int KS, int WHAT>
 int launch_keys(const AttentionArgs& a, int waves, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2)
-        if (a.fine) return launch_keys<T, KS, WHAT, 2, true>(a, s);
-    return waves == 4 ? launch_keys<T, KS, WHAT, 4, false>(a, s) : launch_keys<T, KS, WHAT, 2, false>(a, s);
+    return waves == 4 ? launch_keys<T, KS, WHAT, 4>(a, s) : launch_keys<T, KS, WHAT, 2>(a, s);
 }
 
 template <typename T, int KS>
 int launch_queries(const AttentionArgs& a, int waves, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2)
-        if (a.fine) return launch_queries<T, KS, 2, true>(a, s);
-    return waves == 4 ? launch_queries<T, KS, 4, false>(a, s) : launch_queries<T, KS, 2, false>(a, s);
+    return waves == 4 ? launch_queries<T, KS, 4>(a, s) : launch_queries<T, KS, 2>(a, s);
 }
 template <typename T, int KS>
 int launch_both(const AttentionArgs& aq, const AttentionArgs& ak, const AttentionPlan& p, hipStream_t s)

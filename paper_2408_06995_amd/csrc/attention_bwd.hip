@@ -10,7 +10,6 @@ int launch_attention_backward(const AttentionArgs& a, int type, const AttentionP
     AttentionArgs aq = a, ak = a;
     aq.blocks = p.q_blocks;
     aq.q_pad = p.q_pad;
-    aq.fine = ak.fine = p.fine;
     aq.splits = p.q_splits;
     aq.part = part_q;
     ak.blocks = p.k_blocks;

@@ -1,7 +1,6 @@
 // Attention, forward: o = softmax(scale q k^T) v in one pass over the keys, with the running maximum m (a lower bound of it, within
 // 2^8 after the exponential) and sum l of a row's exponentials; o and l are rescaled when m grows.  m, l and o are held in 32
-// bits; the probabilities are rounded to the operand's planes (8 bits for bf16 results, 24 for fp32) where they enter the second
-// product.
+// bits; the probabilities keep 16 bits for bf16 results and 24 for fp32 where they enter the second product.
 //
 // A wavefront has 32 rows of queries in registers and takes S^T = K Q^T per 32 keys, so that a lane holds 16 scores of one row and
 // its maximum and sum need one exchange with the lane 32 on; P^T is then the operand of O^T = V^T P^T as it lies.
@@ -73,10 +72,10 @@ struct RowsShape {
     typedef Feed<NP, KS, KT, 2, NW> Tiles;
 };
 
-template <typename T, int KS, int NW, bool FINE>
-__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 && !FINE ? 4 : 2) : KS <= 6 ? 2 : 1) void attention_rows_kernel(AttentionArgs a)
+template <typename T, int KS, int NW>
+__global__ __launch_bounds__(64 * NW, kPlanes<T> == 1 ? (KS <= 4 ? 4 : 2) : KS <= 6 ? 2 : 1) void attention_rows_kernel(AttentionArgs a)
 {
-    constexpr int NP = kPlanes<T>, PP = kPlanesP<T, FINE>, DT = (KS + 1) / 2;
+    constexpr int NP = kPlanes<T>, PP = kPlanesP<T>, DT = (KS + 1) / 2;
     typedef RowsShape<NP, KS, NW> Sh;
     typedef typename Sh::Tiles Tiles;
     constexpr int KT = Sh::KT, NS = Sh::NS, PLANE = Tiles::PLANE / 2;
@@ -169,11 +168,11 @@ struct KeysFormShape {
     static constexpr int LDS = TILES > JOIN ? TILES : JOIN;
 };
 
-template <typename T, int KS, bool VEC, bool FINE>
+template <typename T, int KS, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && VEC && KS <= 8 ? 2 : 1) void attention_keys_form_kernel(AttentionArgs a)
 {
     typedef KeysFormShape<T, KS> Sh;
-    constexpr int NP = Sh::NP, PP = kPlanesP<T, FINE>, RS = Sh::RS, DT = Sh::DT, KT = Sh::KT, RG = Sh::RG, KG = Sh::KG, RB = 32 * RG;
+    constexpr int NP = Sh::NP, PP = kPlanesP<T>, RS = Sh::RS, DT = Sh::DT, KT = Sh::KT, RG = Sh::RG, KG = Sh::KG, RB = 32 * RG;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     __bf16* const kt = reinterpret_cast<__bf16*>(lds);
     __bf16* const vt = kt + Sh::TILE;
@@ -324,41 +323,31 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a)
         if (lane + 32 * d < a.dim) out[lane + 32 * d] = (T)(v[d] * inv);
 }
 
-template <typename T, int KS, int NW, bool FINE>
+template <typename T, int KS, int NW>
 int launch_rows(const AttentionArgs& a, hipStream_t s)
 {
     constexpr int lds = RowsShape<kPlanes<T>, KS, NW>::Tiles::LDS;
     static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_rows_kernel<T, KS, NW, FINE>), lds, done)) return FPQ_ERR_LAUNCH;
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_rows_kernel<T, KS, NW>), lds, done)) return FPQ_ERR_LAUNCH;
     const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_rows_kernel<T, KS, NW, FINE><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
+    attention_rows_kernel<T, KS, NW><<<dim3((unsigned)grid), dim3(64 * NW), lds, s>>>(a);
     return FPQ_OK;
 }
 template <typename T, int KS>
 int launch_rows(const AttentionArgs& a, int waves, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2)
-        if (a.fine) return launch_rows<T, KS, 2, true>(a, s);
-    return waves == 4 ? launch_rows<T, KS, 4, false>(a, s) : launch_rows<T, KS, 2, false>(a, s);
-}
-
-template <typename T, int KS, bool VEC, bool FINE>
-int launch_keys_form(const AttentionArgs& a, hipStream_t s)
-{
-    constexpr int lds = KeysFormShape<T, KS>::LDS;
-    static std::atomic<uint64_t> done{0};
-    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_form_kernel<T, KS, VEC, FINE>), lds, done)) return FPQ_ERR_LAUNCH;
-    const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
-    attention_keys_form_kernel<T, KS, VEC, FINE><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
-    return FPQ_OK;
+    return waves == 4 ? launch_rows<T, KS, 4>(a, s) : launch_rows<T, KS, 2>(a, s);
 }
 
 template <typename T, int KS, bool VEC>
 int launch_keys_form(const AttentionArgs& a, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2)
-        if (a.fine) return launch_keys_form<T, KS, VEC, true>(a, s);
-    return launch_keys_form<T, KS, VEC, false>(a, s);
+    constexpr int lds = KeysFormShape<T, KS>::LDS;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_dynamic_lds(reinterpret_cast<const void*>(&attention_keys_form_kernel<T, KS, VEC>), lds, done)) return FPQ_ERR_LAUNCH;
+    const int64_t grid = (int64_t)a.batch * a.kv_heads * a.blocks * a.splits;
+    attention_keys_form_kernel<T, KS, VEC><<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
+    return FPQ_OK;
 }
 
 template <typename T>

@@ -27,10 +27,7 @@ AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int
     // 256.  In fp32, workgroups whose registers let a compute unit hold two are cut to 512 too where queries are kept (dimensions up to
     // 80: forward of 2 x 8 x 1024 x 80 57 -> 51 us, of 8 x 4096 x 40 199 -> 164; of 4 x 8 x 512 x 96 39 -> 40, its backward 105 -> 114).
     const int64_t want = fp32 ? 256 : 512, least = fp32 ? 64 : 256;
-    // (up to 2^18 pairs of a query and a key, where a call is latency.  24 rows on 95 keys: errors of gradients 1.5 times those of the
-    // results' own rounding, with two planes 1.0; forward and backward 70 us, with one plane 68.)
-    p.fine = !fp32 && (double)bh * (double)rows * (double)kv_len <= 0x1p18;
-    auto waves = [&](int64_t n) { return !p.fine && bh * ((n + 127) / 128) >= want / 2 ? 4 : 2; };
+    auto waves = [&](int64_t n) { return bh * ((n + 127) / 128) >= want / 2 ? 4 : 2; };
     auto blocks = [](int64_t n, int waves) { return (int)((n + 32 * waves - 1) / (32 * waves)); };
     p.waves = p.q_waves = waves(rows);
     // (blocks of one head's rows where that adds no more than a tenth)
