@@ -470,7 +470,7 @@ int fpq_gemm_grouped(const fpq_gemm_problem_t *problems, int count, int x_is_fp3
  * are what the kernels are tuned for; others work.  lse: fp32 [batch, q_heads, q_len], may be NULL in the forward call.
  * workspace: the stated bytes, 16-byte aligned, no initialisation (NULL when that is 0).  Calls that share one are ordered on
  * one stream.
- * Limits: head_dim <= 160 (FPQ_ERR_UNSUPPORTED beyond); scale positive and finite (FPQ_ERR_SCALE); q_heads a multiple of
+ * Limits: head_dim <= 160 (FPQ_ERR_UNSUPPORTED beyond); scale from 2^-100 to 2^100 (FPQ_ERR_SCALE); q_heads a multiple of
  * kv_heads; each size, and q_len times the heads of a group, at most 2^30 (FPQ_ERR_SHAPE). */
 typedef enum fpq_type { FPQ_TYPE_FP32 = 0, FPQ_TYPE_BF16 = 1 } fpq_type;
 typedef struct fpq_attention_args {

@@ -26,7 +26,9 @@ int check_attention(const fpq_attention_args_t* p)
     if (p->q_heads == 0 || p->kv_heads == 0 || p->head_dim == 0 || p->q_heads % p->kv_heads) return FPQ_ERR_SHAPE;
     if (p->head_dim > 160) return FPQ_ERR_UNSUPPORTED;
     if (p->q_heads / p->kv_heads * p->q_len > kMost) return FPQ_ERR_SHAPE;
-    if (!(p->scale > 0.0f) || isinf(p->scale)) return FPQ_ERR_SCALE;
+    // Nearer to the ends of fp32 the kernels' units overflow: the lag of the running maximum, 8 / (scale log2 e), and a row's -lse / scale
+    // are finite for every scale from here on, and a log-sum over the scale is a normal number up to there.
+    if (!(p->scale >= 0x1p-100f && p->scale <= 0x1p100f)) return FPQ_ERR_SCALE;
     // the grids, and the sizes of the partial results
     const double rows = (double)p->batch * p->q_heads * (p->q_len + 128), keys = (double)p->batch * p->kv_heads * (p->kv_len + 128);
     if (rows > 0x1p31 || keys > 0x1p36) return FPQ_ERR_SHAPE;
