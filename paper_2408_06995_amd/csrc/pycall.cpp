@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <string.h>
+#include <type_traits>
 
 #include "../../include/fpq.h"
 
@@ -20,7 +21,7 @@ PyObject* g_resolve = nullptr;      // resolver(name) -> address of the C functi
 PyObject* g_check = nullptr;        // checker(status, name): raises
 PyObject *g_format = nullptr, *g_problem = nullptr, *g_array = nullptr;   // fpq_format_t, fpq_gemm_problem_t, ctypes.Array
 PyObject *s_type, *s_data_ptr, *s_numel, *s_element_size, *s_shape, *s_stride, *s_dtype, *s_is_contiguous;
-PyObject *g_float32 = nullptr, *g_bfloat16 = nullptr;
+PyObject *g_float32 = nullptr, *g_bfloat16 = nullptr, *g_int32 = nullptr;
 PyObject *g_get_device = nullptr, *g_get_stream = nullptr;
 
 constexpr int kBad = 1;             // a Python error is set (statuses of the library are <= 0)
@@ -149,20 +150,28 @@ struct Args {
             bad = true;
         }
     }
+    // the dtype of a tensor, a new reference, and torch's own to compare it with
+    PyObject* dtype(int k)
+    {
+        if (!g_float32) {
+            PyObject* m = PyImport_ImportModule("torch");
+            if (!m) { bad = true; return nullptr; }
+            g_float32 = PyObject_GetAttrString(m, "float32");
+            g_bfloat16 = PyObject_GetAttrString(m, "bfloat16");
+            g_int32 = PyObject_GetAttrString(m, "int32");
+            Py_DECREF(m);
+            if (!g_float32 || !g_bfloat16 || !g_int32) { Py_CLEAR(g_float32); bad = true; return nullptr; }
+        }
+        PyObject* t = PyObject_GetAttr(a[k], s_dtype);
+        if (!t) bad = true;
+        return t;
+    }
     // fpq_type of a tensor
     int type(int k, const char* name)
     {
         if (bad) return 0;
-        if (!g_float32) {
-            PyObject* m = PyImport_ImportModule("torch");
-            if (!m) { bad = true; return 0; }
-            g_float32 = PyObject_GetAttrString(m, "float32");
-            g_bfloat16 = PyObject_GetAttrString(m, "bfloat16");
-            Py_DECREF(m);
-            if (!g_float32 || !g_bfloat16) { Py_CLEAR(g_float32); bad = true; return 0; }
-        }
-        PyObject* t = PyObject_GetAttr(a[k], s_dtype);
-        if (!t) { bad = true; return 0; }
+        PyObject* t = dtype(k);
+        if (!t) return 0;
         const int r = t == g_float32 ? FPQ_TYPE_FP32 : t == g_bfloat16 ? FPQ_TYPE_BF16 : -1;
         if (r < 0) {
             PyErr_Format(PyExc_TypeError, "%s: float32 or bfloat16 expected, not %S", name, t);
@@ -177,7 +186,7 @@ struct Args {
         PyErr_SetString(PyExc_ValueError, what);
         bad = true;
     }
-    // elements of a contiguous tensor of 4-byte values, given as None or with exactly n
+    // elements of a contiguous tensor of P (float or int32_t), given as None or with exactly n
     template <typename P>
     P* words(int k, int64_t n, const char* name)
     {
@@ -187,6 +196,15 @@ struct Args {
             bad = true;
             return nullptr;
         }
+        PyObject* t = dtype(k);
+        if (!t) return nullptr;
+        const bool whole = std::is_same<typename std::remove_const<P>::type, int32_t>::value;
+        if (t != (whole ? g_int32 : g_float32)) {
+            PyErr_Format(PyExc_TypeError, "%s: %s expected, not %S", name, whole ? "int32" : "float32", t);
+            bad = true;
+        }
+        Py_DECREF(t);
+        if (bad) return nullptr;
         PyObject* c = PyObject_CallMethodNoArgs(a[k], s_is_contiguous);
         if (!c || c != Py_True) {
             if (c) PyErr_Format(PyExc_ValueError, "%s: not contiguous", name);
