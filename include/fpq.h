@@ -468,8 +468,11 @@ int fpq_gemm_grouped(const fpq_gemm_problem_t *problems, int count, int x_is_fp3
  * Tensors are [batch, tokens, heads, head_dim] with strides (sample, token, head; in elements) of their own, so that q, k and v can
  * be columns of one projection's result; the elements of a head are neighbours.  Rows of a multiple of 16 bytes that start at one
  * are what the kernels are tuned for; others work.  lse: fp32 [batch, q_heads, q_len], may be NULL in the forward call.
- * workspace: the stated bytes, 16-byte aligned, no initialisation (NULL when that is 0).  Calls that share one are ordered on
- * one stream.
+ * workspace: the stated bytes, 16-byte aligned, no initialisation (NULL when that is 0).  They are enough with and without `causal`, for
+ * tensors of any layout and alignment: results of parts (at most 85 MB forward and 420 MB backward, whatever the sizes), statistics of the
+ * rows, and copies of the tensors that are packed: k and v, in the backward call q and grad_o too, in FPQ_TYPE_FP32 at 6 bytes an element, in
+ * FPQ_TYPE_BF16 only those whose rows are not what the kernels are tuned for.  A call asks for no more than it uses.  Calls that share one
+ * are ordered on one stream.
  * Limits: head_dim <= 160 (FPQ_ERR_UNSUPPORTED beyond); scale from 2^-100 to 2^100 (FPQ_ERR_SCALE); q_heads a multiple of
  * kv_heads; each size, and q_len times the heads of a group, at most 2^30 (FPQ_ERR_SHAPE). */
 typedef enum fpq_type { FPQ_TYPE_FP32 = 0, FPQ_TYPE_BF16 = 1 } fpq_type;

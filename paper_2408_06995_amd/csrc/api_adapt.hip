@@ -105,11 +105,41 @@ PackArgs pack_args(const fpq_attention_args_t* p)
     return a;
 }
 
+// Whether the feed can read a tensor as it is.
+bool feed_reads(const fpq_attention_args_t* p, const void* t, const int64_t* s, int64_t len, int64_t heads)
+{
+    return p->type == FPQ_TYPE_BF16 && rows_vec(t, s, p->batch, len, heads, p->head_dim, 2);
+}
+
+// Room for the planes of a tensor of keys or values, or of queries, that the feed cannot read as it is.
+size_t packed_keys(const fpq_attention_args_t* p, const void* t, const int64_t* s)
+{
+    return feed_reads(p, t, s, p->kv_len, p->kv_heads) ? 0 : planes_size(p, keys_of(p));
+}
+size_t packed_rows(const fpq_attention_args_t* p, const void* t, const int64_t* s)
+{
+    return feed_reads(p, t, s, p->q_len, p->q_heads) ? 0 : planes_size(p, rows_of(p));
+}
+
+// Room for the results of parts: of rows with their log-sums, of the queries' gradient, of the two of keys and values.
+size_t forward_parts(const fpq_attention_args_t* p, const AttentionPlan& plan)
+{
+    return plan.splits > 1 ? align_up(plan.splits * rows_of(p) * p->head_dim * 4) + align_up(plan.splits * rows_of(p) * 4) : 0;
+}
+size_t query_parts(const fpq_attention_args_t* p, const AttentionPlan& plan)
+{
+    return plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * p->head_dim * 4) : 0;
+}
+size_t key_parts(const fpq_attention_args_t* p, const AttentionPlan& plan)
+{
+    return plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * p->head_dim * 4) : 0;
+}
+
 // How the feed reads a tensor: as it is, or packed at `at` by the call's packing launch.
 Source source(PackArgs& pack, const fpq_attention_args_t* p, const void* t, const int64_t* s, int64_t len, int64_t heads, bool keys, char*& at)
 {
     const Strides st = strides(s, len, p->head_dim);
-    if (p->type == FPQ_TYPE_BF16 && rows_vec(t, s, p->batch, len, heads, p->head_dim, 2)) return Source{static_cast<const __bf16*>(t), st, 0};
+    if (feed_reads(p, t, s, len, heads)) return Source{static_cast<const __bf16*>(t), st, 0};
     Pack& m = pack.m[pack.count++];
     m = Pack{t, st, reinterpret_cast<__bf16*>(at), (int)heads, (int)len, keys};
     at += planes_size(p, (size_t)p->batch * len * heads);
@@ -375,16 +405,14 @@ int fpq_adamw_step(const void* plan, int64_t pieces, double lr, double beta1, do
     return launch_adamw(plan, pieces, lr, beta1, beta2, eps, weight_decay, step, grad_scale, static_cast<hipStream_t>(stream));
 }
 
-// (what is stated is enough with and without `causal`)
+// (what is stated is enough with and without `causal`, and for tensors of any layout; a call asks for what it uses)
 size_t fpq_attention_workspace_size(const fpq_attention_args_t* p)
 {
     if (check_attention(p) != FPQ_OK || no_rows(p)) return 0;
-    const size_t rows = rows_of(p);
     size_t most = 0;
     for (bool causal : {false, true}) {
         const AttentionPlan plan = plan_of(p, causal);
-        const size_t size = (plan.splits > 1 ? align_up(plan.splits * rows * p->head_dim * 4) + align_up(plan.splits * rows * 4) : 0) +
-                            (plan.by_keys ? 0 : 2 * planes_size(p, keys_of(p)));
+        const size_t size = forward_parts(p, plan) + (plan.by_keys ? 0 : 2 * planes_size(p, keys_of(p)));
         most = size > most ? size : most;
     }
     return most;
@@ -402,7 +430,7 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
         return FPQ_ERR_ALIGN;
     const AttentionPlan plan = plan_of(p, p->causal);
     if (!grid_ok(p, plan.blocks, plan.splits)) return FPQ_ERR_SHAPE;
-    const size_t need = fpq_attention_workspace_size(p);
+    const size_t need = forward_parts(p, plan) + (plan.by_keys ? 0 : packed_keys(p, k, p->k_strides) + packed_keys(p, v, p->v_strides));
     if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;
     if (need && !aligned(workspace, 16)) return FPQ_ERR_ALIGN;
     AttentionArgs a = args_of(p);
@@ -421,9 +449,8 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
     char* at = static_cast<char*>(workspace);
     if (plan.splits > 1) {
         a.part = reinterpret_cast<float*>(at);
-        at += align_up(plan.splits * rows_of(p) * p->head_dim * 4);
-        a.part_lse = reinterpret_cast<float*>(at);
-        at += align_up(plan.splits * rows_of(p) * 4);
+        a.part_lse = reinterpret_cast<float*>(at + align_up(plan.splits * rows_of(p) * p->head_dim * 4));
+        at += forward_parts(p, plan);
     }
     if (!plan.by_keys) {
         PackArgs pack = pack_args(p);
@@ -438,12 +465,10 @@ int fpq_attention(const fpq_attention_args_t* p, const void* q, const void* k, c
 size_t fpq_attention_backward_workspace_size(const fpq_attention_args_t* p)
 {
     if (check_attention(p) != FPQ_OK) return 0;
-    const size_t dim = p->head_dim;
     size_t most = 0;
     for (bool causal : {false, true}) {
         const AttentionPlan plan = plan_of(p, causal);
-        const size_t size = (plan.q_splits > 1 ? align_up(plan.q_splits * rows_of(p) * dim * 4) : 0) +
-                            (plan.k_splits > 1 ? align_up(2 * plan.k_splits * keys_of(p) * dim * 4) : 0);
+        const size_t size = query_parts(p, plan) + key_parts(p, plan);
         most = size > most ? size : most;
     }
     return stats_size(p) + most + 2 * planes_size(p, keys_of(p)) + 2 * planes_size(p, rows_of(p));
@@ -463,7 +488,8 @@ int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const v
     if (!aligned(lse, 4) || !aligned(p->kv_lens, 4)) return FPQ_ERR_ALIGN;
     const AttentionPlan plan = plan_of(p, p->causal);
     if (!grid_ok(p, plan.q_blocks, plan.q_splits) || !grid_ok(p, plan.k_blocks, plan.k_splits)) return FPQ_ERR_SHAPE;
-    const size_t need = fpq_attention_backward_workspace_size(p);
+    const size_t need = stats_size(p) + query_parts(p, plan) + key_parts(p, plan) + packed_keys(p, k, p->k_strides) + packed_keys(p, v, p->v_strides) +
+                        packed_rows(p, q, p->q_strides) + packed_rows(p, grad_o, p->grad_o_strides);
     if (need && (!workspace || workspace_bytes < need)) return FPQ_ERR_WORKSPACE;
     if (need && !aligned(workspace, 16)) return FPQ_ERR_ALIGN;
     AttentionArgs a = args_of(p);
@@ -490,9 +516,9 @@ int fpq_attention_backward(const fpq_attention_args_t* p, const void* q, const v
     a.stats = reinterpret_cast<float*>(at);
     at += stats_size(p);
     float* const part_q = reinterpret_cast<float*>(at);
-    if (plan.q_splits > 1) at += align_up(plan.q_splits * rows_of(p) * p->head_dim * 4);
+    at += query_parts(p, plan);
     float* const part_kv = reinterpret_cast<float*>(at);
-    if (plan.k_splits > 1) at += align_up(2 * plan.k_splits * keys_of(p) * p->head_dim * 4);
+    at += key_parts(p, plan);
     PackArgs pack = pack_args(p);
     a.fk = source(pack, p, k, p->k_strides, p->kv_len, p->kv_heads, true, at);
     a.fv = source(pack, p, v, p->v_strides, p->kv_len, p->kv_heads, true, at);

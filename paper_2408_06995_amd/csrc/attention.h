@@ -12,6 +12,7 @@
 // a row-major tile in LDS by the transposing read, which gives a lane four rows of its column.  Scores and their gradients
 // therefore never leave the registers, and one row-major copy of a tile serves both kinds of reads.
 #pragma once
+#include "attention_plan.h"
 #include "fpq_dev.h"
 #include "fpq_host.h"
 #include "lds_dma.h"
@@ -513,20 +514,6 @@ __device__ __forceinline__ RowBlock row_block(const AttentionArgs& a, int n, int
     b.end = a.causal ? max(0, min(n, b.i + n - a.q_len + 1)) : n;
     return b;
 }
-
-// Queries of a tile of the backward pass's keys kernel.
-template <int NP, int KS>
-constexpr int kKeysTile = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 6 ? 64 : 32;
-
-// How a call's kernels are chosen and cut (host): by sizes and type only, the same for the size of the workspace.
-struct AttentionPlan {
-    int q_pad;                  // AttentionArgs
-    bool by_keys;               // forward: the wavefronts of a workgroup share 32 rows and divide the keys
-    int waves, blocks, splits;                        // waves: of a workgroup, with 32 rows (or keys) each
-    int q_waves, q_blocks, q_splits;                  // backward, gradient of the queries
-    int k_waves, k_blocks, k_splits;                  // backward, gradient of the keys and values
-};
-AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t group, int64_t q_len, int64_t kv_len, int64_t dim, int type, bool causal);
 
 // A tensor and where its planes go: [plane][batch * heads][len][cols], cols = dim rounded up to 8.
 struct Pack {
