@@ -514,6 +514,8 @@ int fpq_attention_backward(const fpq_attention_args_t *args, const void *q, cons
  * multiples that start at one, and ranks that are multiples of 8, are what the kernels are tuned for; others work.
  * workspace: the stated bytes, 16-byte aligned (NULL when that is 0, as for forward calls of ranks up to 16, or where R and K are
  * multiples of 8; a and b then start at multiples of 16 bytes if the rank is above 16); calls that share one are ordered on one stream.
+ * Requests cost a share of a workgroup each even without rows (30000 of one row: 0.14 ms forward), and in the backward call every
+ * workgroup of the adapters' gradient reads all of them (0.5 ms; 2^21 over 64 adapters 43 ms).
  * Limits: R <= 128 (FPQ_ERR_UNSUPPORTED beyond); M at most 2^28, requests 2^21, N, K and the strides 2^24, adapters 32767
  * (FPQ_ERR_SHAPE). */
 typedef struct fpq_adapter_args {

@@ -10,7 +10,7 @@
 //
 // All of it is bound by the rows read and written (a rank of 16 makes 8 flops per byte, one of 64 in bf16 64); the adapters
 // themselves come from the caches.  Rows are cut into tiles that end with their request, so that a workgroup sees one adapter;
-// which tile a workgroup has it finds by a scan of the requests' lengths, 64 at a time.
+// which tile a workgroup has it finds by a search among the requests' first rows, 64 at a time.
 #pragma once
 #include "attention.h"
 
@@ -122,19 +122,23 @@ __device__ __forceinline__ int scan64(int v)      // inclusive sum over the lane
 }
 
 // Tile number `tile` (of TM rows) of all rows: its rows and adapter; lo == hi when there is no such tile.  The same for all lanes.
+// Numbers have gaps: the tiles of run v of rows start at number lo / TM + v.  Up to the next run's that is room for them, since rows
+// that start and end anywhere make at most one tile more than there are multiples of TM from lo to hi; and the run of a number is the last
+// that does not start past it, found with 64 guesses at a time: four reads for 2^21 requests, one for 62.
 template <int TM>
 __device__ __forceinline__ Rows find_tile(const AdapterArgs& p, int tile)
 {
-    for (int v0 = 0; v0 < p.requests + 2; v0 += 64) {
-        const Rows r = rows_of(p, v0 + (threadIdx.x & 63));
-        const int tiles = (r.hi - r.lo + TM - 1) / TM, upto = scan64(tiles);
-        const uint64_t past = __ballot(upto > tile);
-        if (past) {
-            const int who = __ffsll((unsigned long long)past) - 1;
+    int v0 = 0, n = p.requests + 2;                  // v0 <= the run < v0 + n
+    for (;;) {
+        const int step = (n + 63) / 64, at = (int)(threadIdx.x & 63) * step;
+        const Rows r = rows_of(p, at < n ? v0 + at : p.requests + 2);
+        const int first = r.lo / TM + v0 + at;
+        const int who = 63 - __builtin_clzll(__ballot(at < n && first <= tile) | 1);
+        if (step == 1) {
             Rows f;
-            const int first = __shfl(upto - tiles, who);
+            const int number = __shfl(first, who);
             f.hi = __shfl(r.hi, who);
-            f.lo = __shfl(r.lo, who) + (tile - first) * TM;
+            f.lo = __shfl(r.lo, who) + (tile - number) * TM;
             f.hi = min(f.hi, f.lo + TM);
             f.adapter = __shfl(r.adapter, who);
             f.lo = __builtin_amdgcn_readfirstlane(f.lo);
@@ -142,9 +146,9 @@ __device__ __forceinline__ Rows find_tile(const AdapterArgs& p, int tile)
             f.adapter = __builtin_amdgcn_readfirstlane(f.adapter);
             return f;
         }
-        tile -= __shfl(upto, 63);
+        v0 += who * step;
+        n = min(step, n - who * step);
     }
-    return Rows{0, 0, -1};
 }
 
 // Sizes only; the same for the workspace.
