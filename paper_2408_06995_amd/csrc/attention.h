@@ -243,11 +243,6 @@ struct Stage {
     }
 };
 
-// Strides in elements: sample, token, head.
-struct Strides {
-    int64_t b, t, h;
-};
-
 // A matrix as the feed reads it: NP planes of bf16 rows of whole 16-byte pieces.  bf16 tensors with such rows are read where they
 // are; others are packed first (attention_pack.hip).
 struct Source {
@@ -529,8 +524,8 @@ struct PackArgs {
 };
 inline Source packed_source(const Pack& p, int64_t batch, int64_t dim)
 {
-    const int64_t cols = (dim + 7) / 8 * 8;
-    return Source{p.dst, Strides{p.heads * p.len * cols, cols, p.len * cols}, batch * p.heads * p.len * cols};
+    const Strides s = packed_strides(p.heads, p.len, dim);
+    return Source{p.dst, s, batch * s.b};
 }
 int launch_pack(const PackArgs& a, int type, hipStream_t s);
 int launch_attention(const AttentionArgs& a, int type, const AttentionPlan& p, hipStream_t s);

@@ -7,6 +7,18 @@
 
 namespace fpq {
 
+// Strides in elements: sample, token, head.
+struct Strides {
+    int64_t b, t, h;
+};
+
+// Of a packed tensor: [batch][heads][len][cols], cols = dim rounded up to 8.
+inline Strides packed_strides(int64_t heads, int64_t len, int64_t dim)
+{
+    const int64_t cols = (dim + 7) / 8 * 8;
+    return {heads * len * cols, cols, len * cols};
+}
+
 // Queries of a tile of the backward pass's keys kernel.
 template <int NP, int KS>
 constexpr int kKeysTile = NP == 3 ? 32 : KS <= 4 ? 128 : KS <= 6 ? 64 : 32;

@@ -21,7 +21,9 @@ int main()
     int type, causal;
     while (scanf("%lld %lld %lld %lld %lld %lld %d %d", &b, &hk, &g, &lq, &lk, &d, &type, &causal) == 8) {
         const AttentionPlan p = plan_attention(b, hk, g, lq, lk, d, type, causal);
-        printf("%d %d %d %d %d %d %d %d %d %d %d\n", p.q_pad, p.by_keys, p.waves, p.blocks, p.splits, p.q_waves, p.q_blocks, p.q_splits, p.k_waves, p.k_blocks, p.k_splits);
+        const Strides s = packed_strides(hk, lk, d);
+        printf("%d %d %d %d %d %d %d %d %d %d %d %lld %lld %lld\n", p.q_pad, p.by_keys, p.waves, p.blocks, p.splits, p.q_waves, p.q_blocks, p.q_splits, p.k_waves, p.k_blocks, p.k_splits,
+               (long long)s.b, (long long)s.t, (long long)s.h);
     }
     return 0;
 }
@@ -39,7 +41,7 @@ def plan(tmp_path_factory):
 
     def ask(calls):
         lines = subprocess.run([out], input="\n".join(" ".join(map(str, c)) for c in calls), capture_output=True, text=True, check=True).stdout.splitlines()
-        names = "q_pad by_keys waves blocks splits q_waves q_blocks q_splits k_waves k_blocks k_splits".split()
+        names = "q_pad by_keys waves blocks splits q_waves q_blocks q_splits k_waves k_blocks k_splits stride_b stride_t stride_h".split()
         return [dict(zip(names, map(int, l.split()))) for l in lines]
     return ask
 
@@ -99,3 +101,10 @@ def test_workspaces_do_not_grow_with_parts():
         forward, backward = sizes(c)
         assert forward <= 2 * keys + 85e6, c
         assert backward <= 2 * keys + 2 * rows + b * hk * g * -(-lq // 32) * 256 + 420e6, c
+
+
+@pytest.mark.parametrize("heads,keys,dim", [(4, 1 << 29, 8), (64, 1 << 30, 160), (2, (1 << 30) - 1, 5), (3, 7, 33)])
+def test_strides_of_packed_keys(plan, heads, keys, dim):
+    """heads x keys past 2^31 and past 2^32."""
+    p, cols = plan([(2, heads, 1, 1, keys, dim, FP32, 0)])[0], -(-dim // 8) * 8
+    assert (p["stride_b"], p["stride_t"], p["stride_h"]) == (heads * keys * cols, cols, keys * cols)
