@@ -474,7 +474,8 @@ int fpq_gemm_grouped(const fpq_gemm_problem_t *problems, int count, int x_is_fp3
  * FPQ_TYPE_BF16 only those whose rows are not what the kernels are tuned for.  A call asks for no more than it uses.  Calls that share one
  * are ordered on one stream.
  * Limits: head_dim <= 160 (FPQ_ERR_UNSUPPORTED beyond); scale from 2^-100 to 2^100 (FPQ_ERR_SCALE); q_heads a multiple of
- * kv_heads; each size, and q_len times the heads of a group, at most 2^30 (FPQ_ERR_SHAPE). */
+ * kv_heads; each size, and q_len times the heads of a group, at most 2^30, batch q_heads (q_len + 128) at most 2^31 and batch kv_heads
+ * (kv_len + 128) at most 2^36, in the backward call below 2^31 (FPQ_ERR_SHAPE). */
 typedef enum fpq_type { FPQ_TYPE_FP32 = 0, FPQ_TYPE_BF16 = 1 } fpq_type;
 typedef struct fpq_attention_args {
     int32_t type;   /* fpq_type */

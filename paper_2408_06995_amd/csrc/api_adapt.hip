@@ -61,10 +61,10 @@ bool rows_vec(const void* p, const int64_t* s, int64_t batch, int64_t len, int64
     return rows_aligned(p, s, batch, len, heads, size, 16) && dim * size % 16 == 0 && (len <= 1 || (s[1] >= dim && s[1] < (int64_t)1 << 22));
 }
 
-// A workgroup per block and part: fits a grid's dimension.
+// A workgroup of up to 256 threads per block and part: a launch has fewer than 2^32 threads.
 bool grid_ok(const fpq_attention_args_t* p, int64_t blocks, int64_t parts)
 {
-    return (double)p->batch * (double)p->kv_heads * (double)blocks * (double)parts < 0x1p31;
+    return (double)p->batch * (double)p->kv_heads * (double)blocks * (double)parts < 0x1p24;
 }
 
 AttentionArgs args_of(const fpq_attention_args_t* p)
