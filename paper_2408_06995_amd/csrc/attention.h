@@ -40,11 +40,9 @@ template <typename T>
 constexpr int kPlanesP = sizeof(T) == 4 ? 3 : 2;
 
 // Elements of a tile row in LDS for KS steps of 16 columns: 16 bytes more, which make the row an odd number of 16-byte places, so
-// that the 16 rows of a quarter wave's read start in different banks.  Output tiles of 32 columns may reach past a row with an odd
-// KS: those columns of the result are not used, and the tile has kSlack bytes behind it.
+// that the 16 rows of a quarter wave's read start in different banks.
 template <int KS>
 constexpr int kRowStride = 16 * KS + 8;
-constexpr int kSlack = 64;
 
 template <int NP>
 struct Frag {

@@ -163,7 +163,8 @@ template <typename T, int KS>
 struct KeysFormShape {
     static constexpr int NP = kPlanes<T>, RS = kRowStride<KS>, DT = (KS + 1) / 2;
     static constexpr int RG = NP == 3 ? 2 : 1, KG = 4 / RG, KT = 32 * KG;      // sets of rows, wavefronts that divide the keys
-    static constexpr int TILE = NP * KT * RS, TILES = 2 * TILE * 2 + kSlack;
+    static_assert(KS % 2 == 0, "results of 32 columns are read from a tile");
+    static constexpr int TILE = NP * KT * RS, TILES = 2 * TILE * 2;
     static constexpr int JOIN = (2 * 4 * 32 + 32 * RG + 4 * DT * 32 * 33) * 4;
     static constexpr int LDS = TILES > JOIN ? TILES : JOIN;
 };
