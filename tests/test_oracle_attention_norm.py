@@ -45,7 +45,8 @@ FAULTS = {"gk times 0.9": ["gk"], "no delta": ["gq", "gk"], "half of delta": ["g
 
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("shape", [(1, 300, 300, 4, 2, 64), (2, 150, 140, 8, 4, 128), (1, 640, 500, 4, 2, 128), (1, 200, 333, 8, 1, 160),
-                                   (1, 640, 500, 4, 2, 157), (2, 257, 96, 2, 2, 80), (1, 300, 77, 4, 4, 40), (4, 64, 95, 4, 4, 40)])
+                                   (1, 640, 500, 4, 2, 157), (2, 257, 96, 2, 2, 80), (1, 300, 77, 4, 4, 40), (4, 64, 95, 4, 4, 40), (1, 150, 140, 8, 4, 160),
+                                   (1, 1000, 77, 8, 8, 40), (1, 2048, 300, 8, 8, 96), (1, 24, 95, 4, 4, 40), (1, 100, 100, 4, 4, 64), (1, 64, 64, 4, 4, 160)])
 def test_mistakes_are_outside_and_roundings_are_not(shape, causal):
     B, Lq, Lk, Hq, Hkv, D = shape
     rng = np.random.default_rng(sum(shape))
