@@ -557,8 +557,8 @@ int fpq_adapter_backward(const fpq_adapter_args_t *args, const void *x, const vo
  *   steps are called with.  The addresses and sizes are those of the plan until it is written anew.  Arrays aligned for four
  *   elements at a time (16, 8 or 4 bytes by type) are what the kernel is tuned for; others work.
  * fpq_adamw_step: lr and weight_decay finite and >= 0, 0 <= beta < 1, eps positive and finite (FPQ_ERR_SCALE otherwise); step
- *   counts from 1; grad_scale (device, one float, or NULL for 1) multiplies every gradient: a clipping factor or an inverse loss
- *   scale.
+ *   counts from 1 and is an argument of the launch, so that a captured step repeats its own; grad_scale (device, one float, or
+ *   NULL for 1) multiplies every gradient: a clipping factor or an inverse loss scale.
  * Limits: count and the elements of a tensor below 2^31 (FPQ_ERR_SHAPE). */
 typedef struct fpq_adamw_tensor {
     void *param;

@@ -10,7 +10,7 @@
 // tensor sharing a scale of their largest magnitude / 448.  A positive root never becomes code 0: it would divide the next step by
 // eps alone.  One wavefront owns a block of 256, four elements per lane.
 //
-// The work is memory traffic (28 bytes per element with 32-bit states, 14.06 with 8 bits): a workgroup takes a piece of 2048 elements
+// The work is memory traffic (28 bytes per element with 32-bit states, 16.06 with 8 bits): a workgroup takes a piece of 2048 elements
 // of one tensor, all its loads ahead of the arithmetic.  Which piece is in a table that the plan writes once, so that a step is one
 // launch with two dependent loads ahead of the data, whatever the number of tensors.  59.7 M elements, 8-bit states: 178 us, 5.4 TB/s;
 // 256 tensors of up to 20480 elements, 32-bit states and a copy in bf16 (34 MB): 9.6 us, 3.6 TB/s, of which about 3 are the launch.

@@ -8,10 +8,10 @@
 //   keys:    a wavefront keeps 32 keys and values, reads tiles of queries and do, and sums dk and dv over all heads of the group.
 // As in the forward pass p and ds go into the next product from the registers they were computed in.
 //
-// bf16, 4 x 16 heads on 4 of 2048 x 128: 512 us, 671 TFLOP/s of five products, causal 344; 4 x 8 of 4096 x 40: 441 us, 487 (padded
-// as the forward pass).  Neither unit is full: the matrix unit is busy 0.43 - 0.46 of the cycles, vector instructions 0.51 - 0.66, LDS
-// 0.21 - 0.36 (dimension 40); two or three wavefronts per SIMD do not cover a tile's chain of product, exponential, product.
-// fp32, 2 x 8 of 1024 x 80: 155 us, 87 TFLOP/s: six matrix steps for each product.
+// bf16, 4 x 16 heads on 4 of 2048 x 128: 618 us, 556 TFLOP/s of five products, causal 381; 4 x 8 of 4096 x 40: 597 us, 360 (padded
+// as the forward pass; the three products with p and ds are taken twice, for their two planes).  Neither unit is full: the matrix unit is
+// busy 0.47 - 0.52 of the cycles, vector instructions 0.62 - 0.70, LDS 0.17 - 0.26 (dimension 40); two or three wavefronts per SIMD do not
+// cover a tile's chain of product, exponential, product.  fp32, 2 x 8 of 1024 x 80: 143 us, 94 TFLOP/s: six matrix steps for each product.
 #pragma once
 #include "attention.h"
 

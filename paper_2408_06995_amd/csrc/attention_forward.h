@@ -8,12 +8,13 @@
 //   keys form: the wavefronts share one or two sets of 32 rows and divide each tile's keys; their results are joined at the end.
 //     For few rows: single tokens, small batches.
 //
-// Rows form, useful operations (4 q_len kv_len dim per head): bf16, 4 x 16 heads on 4 of 2048 x 128: 174 us, 791 TFLOP/s, causal 100;
-// 4 x 16 of 2048 x 64: 88 us, 782; 4 x 8 of 4096 x 40: 152 us, 565 (dimensions are whole steps of 16 and results of 32 columns, 48 and
-// 64 here).  What binds: vector instructions, above all 32 exponentials at a quarter of the rate per 2048 scores and one
-// multiply-add, one sum and half a rounding each (busy 0.73 of the cycles at dimension 40, the matrix unit 0.38).  fp32, 2 x 8 of
-// 2048 x 64: 109 us, 158 TFLOP/s: six products and the splitting of the probabilities into planes.
-// Keys form: 16 x 32 heads on 8, one query, up to 4096 keys of dimension 128, bf16: 35 us, 5.5 TB/s of keys and values, and 5 for the
+// Rows form, useful operations (4 q_len kv_len dim per head): bf16, 4 x 16 heads on 4 of 2048 x 128: 215 us, 640 TFLOP/s, causal 113;
+// 4 x 16 of 2048 x 64: 116 us, 592; 4 x 8 of 4096 x 40: 203 us, 423 (dimensions are whole steps of 16 and results of 32 columns, 48 and
+// 64 here; the second product is taken twice, for two planes of the probabilities).  What binds: vector instructions, above all 32
+// exponentials at a quarter of the rate per 2048 scores and one multiply-add, one sum and the split into planes each (busy 0.77 of the
+// cycles at dimension 40, the matrix unit 0.45).  fp32, 2 x 8 of 2048 x 64: 106 us, 162 TFLOP/s: six products and the splitting of the
+// probabilities into planes.
+// Keys form: 16 x 32 heads on 8, one query, up to 4096 keys of dimension 128, bf16: 36 us, 5.4 TB/s of keys and values, and 5 for the
 // join; 8 heads of 64 x 64 x 160 in fp32: 15 us, latency of eight workgroups (loads, split, two products, the join in LDS).
 #pragma once
 #include "attention.h"

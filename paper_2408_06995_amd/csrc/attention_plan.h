@@ -49,8 +49,8 @@ inline AttentionPlan plan_attention(int64_t batch, int64_t kv_heads, int64_t gro
     // Two workgroups of four wavefronts per compute unit in bf16, where one's arithmetic covers the other's matrix steps; fp32 has six
     // matrix steps for each.  Fewer rows than that: two wavefronts, and parts of the keys (of the queries, for the gradient of the
     // keys), of no less than takes longer than the pass that joins them.  Measured over 256 or 512 workgroups and parts of no less
-    // than 64 to 512: backward of 4 x 16 heads on 4 x 2048 x 128, bf16: 604 us with 256 workgroups, 517 with 512; forward of 8 x 8 x
-    // 256 x 160, bf16: 25 us with parts of 128, 13 with 256; backward of 8 x 256 x 160, fp32: 71 us with parts of 64, 127 with
+    // than 64 to 512: backward of 4 x 16 heads on 4 x 2048 x 128, bf16: 684 us with 256 workgroups, 618 with 512; forward of 8 x 8 x
+    // 256 x 160, bf16: 26 us with parts of 128, 14 with 256; backward of 8 x 256 x 160, fp32: 71 us with parts of 64, 127 with
     // 256.  In fp32, workgroups whose registers let a compute unit hold two are cut to 512 too where queries are kept (dimensions up to
     // 80: forward of 2 x 8 x 1024 x 80 57 -> 51 us, of 8 x 4096 x 40 199 -> 164; of 4 x 8 x 512 x 96 39 -> 40, its backward 105 -> 114).
     const int64_t want = fp32 ? 256 : 512, least = fp32 ? 64 : 256;
