@@ -577,6 +577,104 @@ int fpq_adamw_plan(const fpq_adamw_tensor_t *tensors, int count, void *plan, siz
 int fpq_adamw_step(const void *plan, int64_t pieces, double lr, double beta1, double beta2, double eps, double weight_decay,
                    int64_t step, const float *grad_scale, void *stream);
 
+/* ---- blocks of 8-bit and 4-bit codes with a scale each -----------------------------------------------------
+ *
+ * A row's elements in blocks of 32 neighbours, each block with one power of two as its scale: codes of the hardware's E4M3
+ * (4, 3, 7, 448), one per byte, or E2M1 (2, 1, 1, 6), two per byte, the even element in the low half.  Rows are filled up with code 0 to
+ * whole blocks: Kp = fpq_block_padded(K) codes and Kp / 32 scales a row, contiguous.  A scale byte s stands for 2^(s - 127), 255 for NaN.
+ * Every value that blocks can hold is a bf16 number (but below 2^-126, and 2^128, to which the largest magnitudes may round), so that the
+ * matrix unit takes them without a rounding of their own.
+ *
+ * fpq_block_quantize: x [M, K] of x_type with row stride ld_x.  A block's scale is the least power of two (from 2^-126 on) with which no
+ *   element is out of range, 1 where all are zero; elements are rounded to nearest, ties to even, or, with a mask [M, K] (E2M1 only; as
+ *   fpq_pack_weights takes it), down for 0 and up for others (Eq. (12)).  A block that holds an infinity or NaN is NaN as a whole.  For what training keeps of
+ *   activations (E4M3) and for weights (E2M1; once, when they are loaded).
+ * fpq_block_dequantize: out [M, K] of out_type; exact, but that bf16 rounds magnitudes below 2^-126.
+ * fpq_block_linear: y [M, N] = x W^T (+ bias) with W [N, K] as E2M1 blocks.  x and y of args->type; bias fp32 [N] or NULL.  Products with bf16 x
+ *   are exact, an fp32 x is split into three bf16 parts as in FPQ_TYPE_FP32 attention; sums are fp32.  Up to 16 rows (a token of each
+ *   request) are bound by the codes read; more are computed with the codes expanded once to bf16 in the workspace.
+ * fpq_linear_backward: the gradients of a linear layer y = x W^T (+ bias) for grad_y [M, N]: grad_x [M, K] = grad_y W, grad_w [N, K] =
+ *   grad_y^T x, of args->type, grad_bias fp32 [N] the sum of its rows.  Each of them may be NULL and is then not computed; w is needed for
+ *   grad_x, x for grad_w.  x is [M, K] of the type with stride ld_x, or, with x_scales not NULL, the E4M3 blocks that were kept of it.
+ * Infinities and NaN make what depends on them infinite or NaN, in FPQ_TYPE_FP32 always NaN.  No atomics: the same bits in every run.  Rows of
+ * multiples of 16 bytes that start at one are read where they are; others, and fp32, are packed into the workspace first.
+ * workspace: the stated bytes, 16-byte aligned, no initialisation (NULL when that is 0); calls that share one are ordered on one stream.
+ * Limits: M at most 2^28, N, K and strides at most 2^20, M N, M K and N K below 2^34 (FPQ_ERR_SHAPE). */
+int64_t fpq_block_padded(int64_t n);
+int fpq_block_quantize(const void *x, int x_type, int64_t M, int64_t K, int64_t ld_x, fpq_format_t f, const uint8_t *mask, uint8_t *codes,
+                       uint8_t *scales, void *stream);
+int fpq_block_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t M, int64_t K, fpq_format_t f, void *out, int out_type,
+                         int64_t ld_out, void *stream);
+typedef struct fpq_linear_args {
+    int32_t type; /* fpq_type */
+    int32_t reserved; /* 0 */
+    int64_t M, N, K;
+    int64_t ld_x, ld_y;                      /* fpq_block_linear; ld_x of fpq_linear_backward too, unless x holds blocks */
+    int64_t ld_w, ld_grad_y, ld_grad_x, ld_grad_w; /* fpq_linear_backward */
+} fpq_linear_args_t;
+size_t fpq_block_linear_workspace_size(int64_t M, int64_t N, int64_t K, int type);
+int fpq_block_linear(const fpq_linear_args_t *args, const void *x, const uint8_t *codes, const uint8_t *scales, const float *bias, void *y,
+                     void *workspace, size_t workspace_bytes, void *stream);
+size_t fpq_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K, int type);
+int fpq_linear_backward(const fpq_linear_args_t *args, const void *x, const uint8_t *x_scales, const void *w, const void *grad_y, void *grad_x,
+                        void *grad_w, float *grad_bias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- gated feed-forward projections, and their gradient -------------------------------------------------------
+ *
+ * Both projections of a feed-forward block, the activation and the product in one call: with W [2 N, K], the values' rows first and the
+ * gates' behind them, and bias fp32 [2 N] or NULL,
+ *   a = x W[:N]^T + bias[:N],  g = x W[N:]^T + bias[N:],  h = a act(g);  act: FPQ_GATE_SILU g sigmoid(g), FPQ_GATE_GELU g Phi(g) (erf form).
+ * x [M, K], W and h [M, N] are of args->type.  What the backward pass needs of a and g is kept in pre, if not NULL: [M, 2 N] of the type,
+ * rounded (a first, contiguous), or, with pre_scales not NULL, as E4M3 blocks: codes [M, 2 Np], Np = fpq_block_padded(N), a's blocks first, scales
+ * [M, 2 Np / 32].  h is computed from the unrounded ones.
+ * fpq_gated_backward: for grad_h [M, N], from a and g as they were kept,
+ *   da = grad_h act(g),  dg = grad_h a act'(g);  grad_x = (da, dg) W,  grad_w [2 N, K] = (da, dg)^T x (of the type), grad_bias fp32 [2 N] the sum of
+ *   their rows.  Each may be NULL.  x as in fpq_linear_backward: of the type, or its blocks with x_scales.
+ * In FPQ_TYPE_BF16 da and dg are rounded to bf16 where they are multiplied (grad_bias sums them unrounded); products, sums, infinities, order,
+ * workspaces and limits (of 2 N too) are those of fpq_linear_backward.  sigmoid is off by at most (4 + |g|) 2^-23 of it, Phi by 4e-7. */
+typedef enum fpq_gate { FPQ_GATE_SILU = 0, FPQ_GATE_GELU = 1 } fpq_gate;
+typedef struct fpq_gated_args {
+    int32_t type; /* fpq_type */
+    int32_t act;  /* fpq_gate */
+    int64_t M, N, K;
+    int64_t ld_x, ld_w, ld_h;                /* ld_x: unless x holds blocks */
+    int64_t ld_grad_h, ld_grad_x, ld_grad_w; /* backward only */
+} fpq_gated_args_t;
+size_t fpq_gated_workspace_size(int64_t M, int64_t N, int64_t K, int type);
+int fpq_gated(const fpq_gated_args_t *args, const void *x, const void *w, const float *bias, void *h, void *pre, uint8_t *pre_scales,
+              void *workspace, size_t workspace_bytes, void *stream);
+size_t fpq_gated_backward_workspace_size(int64_t M, int64_t N, int64_t K, int type);
+int fpq_gated_backward(const fpq_gated_args_t *args, const void *x, const uint8_t *x_scales, const void *w, const void *pre,
+                       const uint8_t *pre_scales, const void *grad_h, void *grad_x, void *grad_w, float *grad_bias, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/* ---- root-mean-square norm on the residual stream, and its gradient ---------------------------------------------
+ *
+ * r = x + residual, rounded to the type and written to sum (residual NULL: r = x; sum may be NULL then, or x or residual itself);
+ *   rstd = (mean of r^2 over the row + eps)^(-1/2), fp32 [M], written if not NULL;  y = r rstd w, w fp32 [K] or NULL for ones.
+ * y is written in the type, if not NULL, and, if codes is not NULL, in 8 bits: without code_scales as fpq_quantize gives it for the format f
+ * (stored one code per byte) and the scale (host, or device if scale_dev is not NULL), [M, fpq_padded_channels(K)] with code 0 behind the
+ * row, which is what fpq_gemm takes as codes where K % 16 == 0; with code_scales as E4M3 blocks (f is ignored) of [M, fpq_block_padded(K)], which
+ * fpq_linear_backward and fpq_gated_backward take.  Codes come from the unrounded y.
+ * fpq_rms_norm_backward: from sum and rstd of the forward call, with grad_y, and grad_sum (NULL for zeros) what the stream's other readers give back,
+ *   grad_x = rstd (gy w - r rstd^2 mean(gy w r)) + grad_sum, the gradient of x and of residual alike, grad_w fp32 [K] = sum over the rows of gy r rstd.
+ * grad_x or grad_w may be NULL; grad_x may be grad_y or grad_sum itself.  Sums and statistics are fp32, no atomics.  A row's infinity or NaN makes that row NaN.
+ * Matrices are of args->type with row strides ld_*; rows of multiples of 16 bytes that start at one are what the kernels are tuned for.
+ * eps >= 0 and finite (FPQ_ERR_SCALE).  workspace of the backward call: the stated bytes, 16-byte aligned, no initialisation (may be NULL
+ * without grad_w).  Limits: M at most 2^28, K and strides at most 2^20, M K below 2^34 (FPQ_ERR_SHAPE). */
+typedef struct fpq_norm_args {
+    int32_t type; /* fpq_type */
+    float eps;
+    int64_t M, K;
+    int64_t ld_x, ld_residual, ld_sum, ld_y;
+    int64_t ld_grad_y, ld_grad_sum, ld_grad_x; /* backward only; the stride of sum is ld_sum */
+} fpq_norm_args_t;
+int fpq_rms_norm(const fpq_norm_args_t *args, const void *x, const void *residual, const float *w, void *sum, void *y, float *rstd,
+                 uint8_t *codes, fpq_format_t f, float scale, const float *scale_dev, uint8_t *code_scales, void *stream);
+size_t fpq_rms_norm_backward_workspace_size(int64_t M, int64_t K);
+int fpq_rms_norm_backward(const fpq_norm_args_t *args, const void *sum, const float *w, const float *rstd, const void *grad_y,
+                          const void *grad_sum, void *grad_x, float *grad_w, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- machine-ceiling probes (for the benchmark's roofline object) -------------------------------
  *
  * What this GPU sustains with nothing but the instruction in question in the loop, to set beside the published peaks

@@ -44,6 +44,7 @@ class fpq_gemm_problem_t(C.Structure):
 
 
 FPQ_TYPE_FP32, FPQ_TYPE_BF16 = 0, 1
+FPQ_GATE_SILU, FPQ_GATE_GELU = 0, 1
 
 
 class fpq_attention_args_t(C.Structure):
@@ -65,6 +66,21 @@ class fpq_adamw_tensor_t(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32),
                 ("state_bits", C.c_int32), ("reserved", C.c_int32)]
+
+
+class fpq_linear_args_t(C.Structure):
+    _fields_ = [("type", C.c_int32), ("reserved", C.c_int32), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("ld_x", C.c_int64),
+                ("ld_y", C.c_int64), ("ld_w", C.c_int64), ("ld_grad_y", C.c_int64), ("ld_grad_x", C.c_int64), ("ld_grad_w", C.c_int64)]
+
+
+class fpq_gated_args_t(C.Structure):
+    _fields_ = [("type", C.c_int32), ("act", C.c_int32), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("ld_x", C.c_int64),
+                ("ld_w", C.c_int64), ("ld_h", C.c_int64), ("ld_grad_h", C.c_int64), ("ld_grad_x", C.c_int64), ("ld_grad_w", C.c_int64)]
+
+
+class fpq_norm_args_t(C.Structure):
+    _fields_ = [("type", C.c_int32), ("eps", C.c_float), ("M", C.c_int64), ("K", C.c_int64), ("ld_x", C.c_int64), ("ld_residual", C.c_int64),
+                ("ld_sum", C.c_int64), ("ld_y", C.c_int64), ("ld_grad_y", C.c_int64), ("ld_grad_sum", C.c_int64), ("ld_grad_x", C.c_int64)]
 
 
 class FpqError(RuntimeError):
@@ -202,6 +218,29 @@ def lib():
     L.fpq_adamw_plan.argtypes = [C.POINTER(fpq_adamw_tensor_t), i32, vp, sz, C.POINTER(i64), vp]
     L.fpq_adamw_step.restype = i32
     L.fpq_adamw_step.argtypes = [vp, i64] + [C.c_double] * 5 + [i64, f32p, vp]
+    L.fpq_block_padded.restype = i64
+    L.fpq_block_padded.argtypes = [i64]
+    L.fpq_block_quantize.restype = i32
+    L.fpq_block_quantize.argtypes = [vp, i32, i64, i64, i64, F, u8p, u8p, u8p, vp]
+    L.fpq_block_dequantize.restype = i32
+    L.fpq_block_dequantize.argtypes = [u8p, u8p, i64, i64, F, vp, i32, i64, vp]
+    for name in ("fpq_block_linear_workspace_size", "fpq_linear_backward_workspace_size", "fpq_gated_workspace_size", "fpq_gated_backward_workspace_size"):
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = [i64, i64, i64, i32]
+    L.fpq_block_linear.restype = i32
+    L.fpq_block_linear.argtypes = [C.POINTER(fpq_linear_args_t)] + [vp] * 6 + [sz, vp]
+    L.fpq_linear_backward.restype = i32
+    L.fpq_linear_backward.argtypes = [C.POINTER(fpq_linear_args_t)] + [vp] * 8 + [sz, vp]
+    L.fpq_gated.restype = i32
+    L.fpq_gated.argtypes = [C.POINTER(fpq_gated_args_t)] + [vp] * 7 + [sz, vp]
+    L.fpq_gated_backward.restype = i32
+    L.fpq_gated_backward.argtypes = [C.POINTER(fpq_gated_args_t)] + [vp] * 10 + [sz, vp]
+    L.fpq_rms_norm.restype = i32
+    L.fpq_rms_norm.argtypes = [C.POINTER(fpq_norm_args_t)] + [vp] * 7 + [F, fl, vp, vp, vp]
+    L.fpq_rms_norm_backward_workspace_size.restype = sz
+    L.fpq_rms_norm_backward_workspace_size.argtypes = [i64, i64]
+    L.fpq_rms_norm_backward.restype = i32
+    L.fpq_rms_norm_backward.argtypes = [C.POINTER(fpq_norm_args_t)] + [vp] * 8 + [sz, vp]
     L.fpq_gemm_noalloc.restype = i32
     L.fpq_gemm_noalloc.argtypes = [vp, i32, F, fl, f32p, vp, F, f32p, f32p, f32p, i64, i64, i64, i32, vp]
     _lib = L
@@ -220,7 +259,10 @@ EXPORTS = ["fpq_strerror", "fpq_format_max", "fpq_format_check", "fpq_bias_to_sc
            "fpq_int_pack_weights", "fpq_int_gemm_workspace_size", "fpq_int_gemm",
            "fpq_attention_workspace_size", "fpq_attention", "fpq_attention_backward_workspace_size", "fpq_attention_backward",
            "fpq_adapter_workspace_size", "fpq_adapter_apply", "fpq_adapter_backward_workspace_size", "fpq_adapter_backward",
-           "fpq_adamw_plan_size", "fpq_adamw_plan", "fpq_adamw_step"]
+           "fpq_adamw_plan_size", "fpq_adamw_plan", "fpq_adamw_step", "fpq_block_padded", "fpq_block_quantize", "fpq_block_dequantize",
+           "fpq_block_linear_workspace_size", "fpq_block_linear", "fpq_linear_backward_workspace_size", "fpq_linear_backward",
+           "fpq_gated_workspace_size", "fpq_gated", "fpq_gated_backward_workspace_size", "fpq_gated_backward", "fpq_rms_norm",
+           "fpq_rms_norm_backward_workspace_size", "fpq_rms_norm_backward"]
 
 
 def fmt(f):
@@ -435,6 +477,30 @@ def fpq_adapter_backward_workspace_size(M, N, K, R, requests, adapters):
     return lib().fpq_adapter_backward_workspace_size(M, N, K, R, requests, adapters)
 
 
+def fpq_block_padded(n):
+    return lib().fpq_block_padded(n)
+
+
+def fpq_block_linear_workspace_size(M, N, K, type):
+    return lib().fpq_block_linear_workspace_size(M, N, K, int(type))
+
+
+def fpq_linear_backward_workspace_size(M, N, K, type):
+    return lib().fpq_linear_backward_workspace_size(M, N, K, int(type))
+
+
+def fpq_gated_workspace_size(M, N, K, type):
+    return lib().fpq_gated_workspace_size(M, N, K, int(type))
+
+
+def fpq_gated_backward_workspace_size(M, N, K, type):
+    return lib().fpq_gated_backward_workspace_size(M, N, K, int(type))
+
+
+def fpq_rms_norm_backward_workspace_size(M, K):
+    return lib().fpq_rms_norm_backward_workspace_size(M, K)
+
+
 def _type(t, what):
     import torch
     if t.dtype not in (torch.float32, torch.bfloat16):
@@ -536,12 +602,27 @@ def fpq_rl_im2col(x, kh, kw, stride, pad, a):
 #   fpq_adapter_backward(x, a, b, scaling, row_start, adapter, t, grad_y, grad_x_base, grad_x, grad_a, grad_b, workspace=None)
 #       grad_x_base and grad_x may be None; grad_a, grad_b: float32, the shapes of a and b
 #   fpq_adamw_step(plan, pieces, lr, beta1, beta2, eps, weight_decay, step, grad_scale=None)    pieces: what fpq_adamw_plan returned
+#   fpq_block_quantize(x, f, mask, codes, scales)
+#       x: [M, K] float32 or bfloat16, rows of any stride; f: (4, 3, 7, 448) or (2, 1, 1, 6); mask: [M, K] uint8 or None; codes, scales: one byte
+#       per element (uint8 or float8_e4m3fn, contiguous): M fpq_block_padded(K) of them (half as many of four bits), M fpq_block_padded(K) / 32
+#   fpq_block_dequantize(codes, scales, f, out)
+#   fpq_block_linear(x, codes, scales, bias, y, workspace=None)                 bias: float32 [N] or None
+#   fpq_linear_backward(x, x_scales, w, grad_y, grad_x, grad_w, grad_bias, workspace=None)
+#       x: [M, K] with x_scales None, or codes with their scales; grad_x, grad_w of the type, grad_bias float32 [N], each or None
+#   fpq_gated(x, w, bias, act, h, pre=None, pre_scales=None, workspace=None)
+#       w: [2 N, K]; bias: float32 [2 N] or None; act: FPQ_GATE_*; pre: [M, 2 N] contiguous, or codes with their scales, or None
+#   fpq_gated_backward(x, x_scales, w, pre, pre_scales, act, grad_h, grad_x, grad_w, grad_bias, workspace=None)
+#   fpq_rms_norm(x, residual, w, eps, sum, y, rstd=None, codes=None, f=None, scale=None, scale_dev=None, code_scales=None)
+#       residual, w (float32 [K]), sum, y, rstd (float32 [M]) or None; codes: M fpq_padded_channels(K) bytes with f and a scale, or
+#       M fpq_block_padded(K) with code_scales
+#   fpq_rms_norm_backward(sum, w, rstd, grad_y, grad_sum, grad_x, grad_w, workspace=None)     grad_sum, grad_x, grad_w (float32 [K]) or None
 
 NATIVE = ["fpq_gemm", "fpq_gemm_noalloc", "fpq_conv2d", "fpq_gemm_codes_out", "fpq_conv2d_codes_out",
           "fpq_gemm_sparse", "fpq_conv2d_sparse", "fpq_gemm_grouped", "fpq_absmax", "fpq_quantize",
           "fpq_quantize_nhwc", "fpq_int_calibrate", "fpq_int_quantize", "fpq_int_gemm", "fpq_rl_step",
           "fpq_search_format", "fpq_attention", "fpq_attention_backward", "fpq_adapter_apply", "fpq_adapter_backward",
-          "fpq_adamw_step"]
+          "fpq_adamw_step", "fpq_block_quantize", "fpq_block_dequantize", "fpq_block_linear", "fpq_linear_backward", "fpq_gated",
+          "fpq_gated_backward", "fpq_rms_norm", "fpq_rms_norm_backward"]
 
 
 def _resolve(name):

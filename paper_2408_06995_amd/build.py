@@ -16,7 +16,8 @@ OBJ = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "quant.hip", "search.hip", "sparsity.hip", "rounding.hip", "gemm.hip", "gemm_dma.hip", "gemm_dma_q.hip", "gemm_dma_s.hip", "gemm_dma_sq.hip", "gemm_strip.hip", "gemm_strip_h.hip", "gemm_strip_q.hip", "gemm_wk.hip", "gemm_wk_q.hip", "gemm_wk16.hip", "gemm_wk16_h.hip", "peaks.hip", "gemm_sparse.hip", "igemm.hip",
            "api_adapt.hip", "attention_fwd.hip", "attention_fwd_f32.hip", "attention_bwd.hip", "attention_bwd_f32.hip", "attention_pack.hip", "adapter.hip",
            "adapter_map_f32.hip", "adapter_map_f32_bf16.hip", "adapter_map_f32_packed.hip", "adapter_map_bf16.hip",
-           "adapter_map_f32_bf16_packed.hip", "adapter_map_bf16_packed.hip", "adapter_outer.hip", "adamw.hip"]
+           "adapter_map_f32_bf16_packed.hip", "adapter_map_bf16_packed.hip", "adapter_outer.hip", "adamw.hip",
+           "api_blocks.hip", "blocks.hip", "norm.hip", "matmul.hip", "matmul_rows.hip", "matmul_gated.hip", "matmul_rows_cols.hip", "matmul_cols.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -1,0 +1,436 @@
+// C ABI of the operators around a transformer block's projections (see include/fpq.h): blocks of codes, layers on them, gradients of linear
+// layers, gated projections, the norm.  Argument validation on the host, then kernel launches on the caller's stream.
+#include <math.h>
+
+#include "blocks.h"
+
+using namespace fpq;
+
+namespace {
+
+constexpr int64_t kMostRows = (int64_t)1 << 28, kMostColumns = (int64_t)1 << 20, kMostElements = (int64_t)1 << 34;
+
+size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
+size_t size_of(int type) { return type == FPQ_TYPE_FP32 ? 4 : 2; }
+int planes_of(int type) { return type == FPQ_TYPE_FP32 ? 3 : 1; }
+bool type_ok(int type) { return type == FPQ_TYPE_FP32 || type == FPQ_TYPE_BF16; }
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+bool stride_ok(int64_t ld, int64_t cols, int64_t rows) { return rows <= 1 || (ld >= cols && ld <= kMostColumns); }
+// (a single row's stride says nothing)
+int64_t stride(int64_t ld, int64_t cols, int64_t rows) { return rows <= 1 ? (cols + 7) / 8 * 8 : ld; }
+
+int check_sizes(int64_t M, int64_t N, int64_t K)
+{
+    if (M < 0 || M > kMostRows || N < 1 || N > kMostColumns || K < 1 || K > kMostColumns) return FPQ_ERR_SHAPE;
+    if (M * N >= kMostElements || M * K >= kMostElements || N * K >= kMostElements) return FPQ_ERR_SHAPE;
+    return FPQ_OK;
+}
+
+// Which blocks a format says: 8, 4, or a status
+int block_bits(fpq_format_t f)
+{
+    if (fpq_format_check(f) != FPQ_OK) return FPQ_ERR_FORMAT;
+    if (f.ebits == 4 && f.mbits == 3 && f.bias == 7 && f.maxval == 448.0f) return 8;
+    if (f.ebits == 2 && f.mbits == 1 && f.bias == 1 && (f.maxval == 0.0f || f.maxval == 6.0f)) return 4;
+    return FPQ_ERR_UNSUPPORTED;
+}
+
+// The workspace, piece by piece.
+struct Room {
+    char* at;
+    template <typename T>
+    T* take(size_t bytes)
+    {
+        T* const r = reinterpret_cast<T*>(at);
+        at += align_up(bytes);
+        return r;
+    }
+};
+
+// Room for a matrix that the products cannot read as it is.
+size_t planes_bytes(int64_t rows, int64_t cols, int type) { return align_up((size_t)rows * round8(cols) * 2 * planes_of(type)); }
+size_t blocks_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * block_padded(cols) * 2); }
+bool reads(const void* p, int type, int64_t rows, int64_t cols, int64_t ld)
+{
+    return type == FPQ_TYPE_BF16 && aligned(p, 16) && cols % 8 == 0 && (rows <= 1 || ld % 8 == 0);
+}
+
+// A matrix as the products read it: where it is, or packed into the workspace.
+int operand(const void* p, int type, int64_t rows, int64_t cols, int64_t ld, Room& room, Operand& o, hipStream_t s)
+{
+    ld = stride(ld, cols, rows);
+    if (reads(p, type, rows, cols, ld)) {
+        o = Operand{static_cast<const __bf16*>(p), ld, 0};
+        return FPQ_OK;
+    }
+    const int64_t to = round8(cols);
+    __bf16* const dst = room.take<__bf16>((size_t)rows * to * 2 * planes_of(type));
+    o = Operand{dst, to, rows * to};
+    return launch_planes(p, type, rows, cols, ld, dst, to, rows * to, s);
+}
+int operand_of_blocks(const void* codes, const uint8_t* scales, int64_t rows, int64_t cols, bool eight, Room& room, Operand& o, hipStream_t s)
+{
+    const int64_t to = block_padded(cols);
+    __bf16* const dst = room.take<__bf16>((size_t)rows * to * 2);
+    o = Operand{dst, to, 0};
+    return launch_decode(static_cast<const uint8_t*>(codes), scales, rows, to, eight, dst, 0, to, s);
+}
+
+bool workspace_bad(const void* workspace, size_t bytes, size_t need, int* st)
+{
+    *st = need && (!workspace || bytes < need) ? FPQ_ERR_WORKSPACE : need && !aligned(workspace, 16) ? FPQ_ERR_ALIGN : FPQ_OK;
+    return *st != FPQ_OK;
+}
+
+size_t larger(size_t a, size_t b) { return a > b ? a : b; }
+
+// Partial results of grad_x [M, K] = d [M, N] w and of grad_w [N, K] = d^T x, which follow each other and share the room.
+size_t gradient_parts(int64_t M, int64_t N, int64_t K, int type)
+{
+    const int p = planes_of(type);
+    return align_up(larger(product_part_bytes(M, K, N, p, p, false, false),
+                           larger(product_part_bytes(N, K, M, p, p, true, false), product_part_bytes(N, K, M, p, 1, true, false))));
+}
+
+// The products of both gradients.  d: [M, N] as the products read it; x or its blocks; grad_x, grad_w may be null.
+int gradients(const Operand& d, int type, int64_t M, int64_t N, int64_t K, const void* x, const uint8_t* x_scales, int64_t ld_x, const void* w, int64_t ld_w,
+              void* grad_x, int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, Room& room, hipStream_t s)
+{
+    const int np = planes_of(type);
+    Operand ow{}, ox{};
+    int st = FPQ_OK;
+    if (grad_x && M) st = operand(w, type, N, K, ld_w, room, ow, s);
+    if (st == FPQ_OK && grad_w && M) st = x_scales ? operand_of_blocks(x, x_scales, M, K, true, room, ox, s) : operand(x, type, M, K, ld_x, room, ox, s);
+    if (st != FPQ_OK) return st;
+    Product p{};
+    p.a = d;
+    p.planes_a = np;
+    p.out_f32 = type == FPQ_TYPE_FP32;
+    p.col_b = true;
+    if (grad_x && M) {
+        p.b = ow;
+        p.M = M;
+        p.N = K;
+        p.K = N;
+        p.planes_b = np;
+        p.out = grad_x;
+        p.ld_out = stride(ld_grad_x, K, M);
+        st = launch_product(p, room.at, s);
+    }
+    if (st == FPQ_OK && grad_w) {
+        p.b = ox;
+        p.M = N;
+        p.N = K;
+        p.K = M;
+        p.planes_b = x_scales ? 1 : np;
+        p.col_a = true;
+        p.out = grad_w;
+        p.ld_out = stride(ld_grad_w, K, N);
+        st = launch_product(p, room.at, s);
+    }
+    return st;
+}
+
+// What both backward calls ask of x, w and the gradients
+int check_gradients(int type, int64_t M, int64_t N, int64_t K, const void* x, const uint8_t* x_scales, int64_t ld_x, const void* w, int64_t ld_w,
+                    const void* grad_x, int64_t ld_grad_x, const void* grad_w, int64_t ld_grad_w, const float* grad_bias)
+{
+    if (M && ((grad_w && !x) || (grad_x && !w))) return FPQ_ERR_NULL;
+    if (grad_x && (!stride_ok(ld_grad_x, K, M) || !stride_ok(ld_w, K, N))) return FPQ_ERR_SHAPE;
+    if (grad_w && (!stride_ok(ld_grad_w, K, N) || (!x_scales && !stride_ok(ld_x, K, M)))) return FPQ_ERR_SHAPE;
+    const size_t size = size_of(type);
+    if (!aligned(x, x_scales ? 16 : size) || !aligned(w, size) || !aligned(grad_x, size) || !aligned(grad_w, size) || !aligned(grad_bias, 4)) return FPQ_ERR_ALIGN;
+    return FPQ_OK;
+}
+
+bool norm_vec(const void* p, int64_t ld, int64_t M, int64_t K, size_t size)
+{
+    return !p || (aligned(p, 16) && K * size % 16 == 0 && (M <= 1 || ld * size % 16 == 0));
+}
+
+int check_norm(const fpq_norm_args_t* p)
+{
+    if (!p) return FPQ_ERR_NULL;
+    if (!type_ok(p->type)) return FPQ_ERR_UNSUPPORTED;
+    return check_sizes(p->M, 1, p->K);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t fpq_block_padded(int64_t n) { return n < 0 ? 0 : block_padded(n); }
+
+int fpq_block_quantize(const void* x, int x_type, int64_t M, int64_t K, int64_t ld_x, fpq_format_t f, const uint8_t* mask, uint8_t* codes, uint8_t* scales,
+                       void* stream)
+{
+    const int bits = block_bits(f);
+    if (bits < 0) return bits;
+    if (!type_ok(x_type) || (mask && bits != 4)) return FPQ_ERR_UNSUPPORTED;
+    int st = check_sizes(M, 1, K);
+    if (st != FPQ_OK) return st;
+    if (M == 0) return FPQ_OK;
+    if (!x || !codes || !scales) return FPQ_ERR_NULL;
+    if (!stride_ok(ld_x, K, M)) return FPQ_ERR_SHAPE;
+    if (!aligned(x, size_of(x_type)) || !aligned(codes, 16)) return FPQ_ERR_ALIGN;
+    return launch_block_quantize(x, x_type, M, K, stride(ld_x, K, M), bits == 8, mask, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+int fpq_block_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, fpq_format_t f, void* out, int out_type, int64_t ld_out, void* stream)
+{
+    const int bits = block_bits(f);
+    if (bits < 0) return bits;
+    if (!type_ok(out_type)) return FPQ_ERR_UNSUPPORTED;
+    int st = check_sizes(M, 1, K);
+    if (st != FPQ_OK) return st;
+    if (M == 0) return FPQ_OK;
+    if (!codes || !scales || !out) return FPQ_ERR_NULL;
+    if (!stride_ok(ld_out, K, M)) return FPQ_ERR_SHAPE;
+    if (!aligned(out, size_of(out_type)) || !aligned(codes, 16)) return FPQ_ERR_ALIGN;
+    return launch_decode(codes, scales, M, K, bits == 8, out, out_type == FPQ_TYPE_FP32, stride(ld_out, K, M), static_cast<hipStream_t>(stream));
+}
+
+size_t fpq_block_linear_workspace_size(int64_t M, int64_t N, int64_t K, int type)
+{
+    if (!type_ok(type) || check_sizes(M, N, K) != FPQ_OK || M == 0) return 0;
+    return planes_bytes(M, K, type) + blocks_bytes(N, K) + align_up(product_part_bytes(M, N, K, planes_of(type), 1, false, false));
+}
+
+int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* codes, const uint8_t* scales, const float* bias, void* y, void* workspace,
+                     size_t workspace_bytes, void* stream)
+{
+    if (!p) return FPQ_ERR_NULL;
+    if (!type_ok(p->type) || p->reserved) return FPQ_ERR_UNSUPPORTED;
+    int st = check_sizes(p->M, p->N, p->K);
+    if (st != FPQ_OK) return st;
+    if (p->M == 0) return FPQ_OK;
+    if (!x || !codes || !scales || !y) return FPQ_ERR_NULL;
+    if (!stride_ok(p->ld_x, p->K, p->M) || !stride_ok(p->ld_y, p->N, p->M)) return FPQ_ERR_SHAPE;
+    const size_t size = size_of(p->type);
+    if (!aligned(x, size) || !aligned(y, size) || !aligned(codes, 16) || !aligned(bias, 4)) return FPQ_ERR_ALIGN;
+    if (workspace_bad(workspace, workspace_bytes, fpq_block_linear_workspace_size(p->M, p->N, p->K, p->type), &st)) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Room room{static_cast<char*>(workspace)};
+    Product q{};
+    st = operand(x, p->type, p->M, p->K, p->ld_x, room, q.a, s);
+    if (st == FPQ_OK) st = operand_of_blocks(codes, scales, p->N, p->K, false, room, q.b, s);
+    if (st != FPQ_OK) return st;
+    q.M = p->M;
+    q.N = p->N;
+    q.K = p->K;
+    q.planes_a = planes_of(p->type);
+    q.planes_b = 1;
+    q.out = y;
+    q.ld_out = stride(p->ld_y, p->N, p->M);
+    q.out_f32 = p->type == FPQ_TYPE_FP32;
+    q.bias = bias;
+    return launch_product(q, room.at, s);
+}
+
+size_t fpq_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K, int type)
+{
+    if (!type_ok(type) || check_sizes(M, N, K) != FPQ_OK) return 0;
+    return planes_bytes(M, N, type) + planes_bytes(N, K, type) + larger(planes_bytes(M, K, type), blocks_bytes(M, K)) +
+           larger(gradient_parts(M, N, K, type), align_up(row_parts_bytes(M, N)));
+}
+
+int fpq_linear_backward(const fpq_linear_args_t* p, const void* x, const uint8_t* x_scales, const void* w, const void* grad_y, void* grad_x, void* grad_w,
+                        float* grad_bias, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!p) return FPQ_ERR_NULL;
+    if (!type_ok(p->type) || p->reserved) return FPQ_ERR_UNSUPPORTED;
+    const int64_t M = p->M, N = p->N, K = p->K;
+    int st = check_sizes(M, N, K);
+    if (st != FPQ_OK) return st;
+    if (M && !grad_y) return FPQ_ERR_NULL;
+    if (!stride_ok(p->ld_grad_y, N, M)) return FPQ_ERR_SHAPE;
+    if (!aligned(grad_y, size_of(p->type))) return FPQ_ERR_ALIGN;
+    st = check_gradients(p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, grad_bias);
+    if (st != FPQ_OK) return st;
+    if (workspace_bad(workspace, workspace_bytes, fpq_linear_backward_workspace_size(M, N, K, p->type), &st)) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Room room{static_cast<char*>(workspace)};
+    if (grad_bias) st = launch_column_sums(grad_y, p->type, M, N, stride(p->ld_grad_y, N, M), grad_bias, reinterpret_cast<float*>(room.at), s);
+    if (st != FPQ_OK || (!grad_x && !grad_w)) return st;
+    Operand d{};
+    if (M) st = operand(grad_y, p->type, M, N, p->ld_grad_y, room, d, s);
+    if (st != FPQ_OK) return st;
+    return gradients(d, p->type, M, N, K, x, x_scales, stride(p->ld_x, K, M), w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, room, s);
+}
+
+static int check_gated(const fpq_gated_args_t* p)
+{
+    if (!p) return FPQ_ERR_NULL;
+    if (!type_ok(p->type) || (p->act != FPQ_GATE_SILU && p->act != FPQ_GATE_GELU)) return FPQ_ERR_UNSUPPORTED;
+    return check_sizes(p->M, 2 * (p->N < 0 ? 0 : p->N > kMostColumns ? kMostColumns : p->N), p->K);
+}
+
+size_t fpq_gated_workspace_size(int64_t M, int64_t N, int64_t K, int type)
+{
+    const fpq_gated_args_t a{type, 0, M, N, K, 0, 0, 0, 0, 0, 0};
+    if (check_gated(&a) != FPQ_OK || M == 0) return 0;
+    const int p = planes_of(type);
+    return planes_bytes(M, K, type) + planes_bytes(2 * N, K, type) + align_up(product_part_bytes(M, N, K, p, p, false, true));
+}
+
+int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const float* bias, void* h, void* pre, uint8_t* pre_scales, void* workspace,
+              size_t workspace_bytes, void* stream)
+{
+    int st = check_gated(p);
+    if (st != FPQ_OK) return st;
+    const int64_t M = p->M, N = p->N, K = p->K;
+    if (M == 0) return FPQ_OK;
+    if (!x || !w || !h || (pre_scales && !pre)) return FPQ_ERR_NULL;
+    if (!stride_ok(p->ld_x, K, M) || !stride_ok(p->ld_w, K, 2 * N) || !stride_ok(p->ld_h, N, M)) return FPQ_ERR_SHAPE;
+    const size_t size = size_of(p->type);
+    if (!aligned(x, size) || !aligned(w, size) || !aligned(h, size) || !aligned(pre, pre_scales ? 16 : size) || !aligned(bias, 4)) return FPQ_ERR_ALIGN;
+    if (workspace_bad(workspace, workspace_bytes, fpq_gated_workspace_size(M, N, K, p->type), &st)) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Room room{static_cast<char*>(workspace)};
+    Product q{};
+    st = operand(x, p->type, M, K, p->ld_x, room, q.a, s);
+    if (st == FPQ_OK) st = operand(w, p->type, 2 * N, K, p->ld_w, room, q.b, s);
+    if (st != FPQ_OK) return st;
+    q.M = M;
+    q.N = N;
+    q.K = K;
+    q.planes_a = q.planes_b = planes_of(p->type);
+    q.out_f32 = p->type == FPQ_TYPE_FP32;
+    q.bias = bias;
+    q.gated = true;
+    q.gate = Gate{p->act, h, stride(p->ld_h, N, M), pre, 2 * N, pre_scales};
+    return launch_product(q, room.at, s);
+}
+
+size_t fpq_gated_backward_workspace_size(int64_t M, int64_t N, int64_t K, int type)
+{
+    const fpq_gated_args_t a{type, 0, M, N, K, 0, 0, 0, 0, 0, 0};
+    if (check_gated(&a) != FPQ_OK) return 0;
+    return planes_bytes(M, 2 * N, type) + planes_bytes(2 * N, K, type) + larger(planes_bytes(M, K, type), blocks_bytes(M, K)) +
+           larger(gradient_parts(M, 2 * N, K, type), align_up(2 * row_parts_bytes(M, N)));
+}
+
+int fpq_gated_backward(const fpq_gated_args_t* p, const void* x, const uint8_t* x_scales, const void* w, const void* pre, const uint8_t* pre_scales,
+                       const void* grad_h, void* grad_x, void* grad_w, float* grad_bias, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int st = check_gated(p);
+    if (st != FPQ_OK) return st;
+    const int64_t M = p->M, N = p->N, K = p->K;
+    if (M && (!pre || !grad_h)) return FPQ_ERR_NULL;
+    if (!stride_ok(p->ld_grad_h, N, M)) return FPQ_ERR_SHAPE;
+    const size_t size = size_of(p->type);
+    if (!aligned(grad_h, size) || !aligned(pre, pre_scales ? 16 : size)) return FPQ_ERR_ALIGN;
+    st = check_gradients(p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, grad_bias);
+    if (st != FPQ_OK) return st;
+    if (workspace_bad(workspace, workspace_bytes, fpq_gated_backward_workspace_size(M, N, K, p->type), &st)) return st;
+    if (!grad_x && !grad_w && !grad_bias) return FPQ_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Room room{static_cast<char*>(workspace)};
+    GateBackward g{};
+    g.type = p->type;
+    g.act = p->act;
+    g.M = M;
+    g.N = N;
+    g.pre = pre;
+    g.pre_scales = pre_scales;
+    g.gh = grad_h;
+    g.ld_gh = stride(p->ld_grad_h, N, M);
+    g.ld_d = round8(2 * N);
+    g.plane = M * g.ld_d;
+    __bf16* const d = room.take<__bf16>(planes_bytes(M, 2 * N, p->type));
+    if (grad_x || grad_w) g.d = d;
+    g.grad_bias = grad_bias;
+    g.part = reinterpret_cast<float*>(room.at);
+    st = launch_gate_backward(g, s);
+    if (st != FPQ_OK || !g.d) return st;
+    return gradients(Operand{d, g.ld_d, g.plane}, p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, room, s);
+}
+
+int fpq_rms_norm(const fpq_norm_args_t* p, const void* x, const void* residual, const float* w, void* sum, void* y, float* rstd, uint8_t* codes, fpq_format_t f,
+                 float scale, const float* scale_dev, uint8_t* code_scales, void* stream)
+{
+    int st = check_norm(p);
+    if (st != FPQ_OK) return st;
+    if (!(p->eps >= 0.0f) || isinf(p->eps)) return FPQ_ERR_SCALE;
+    if (codes && !code_scales) {
+        if (fpq_format_check(f) != FPQ_OK) return FPQ_ERR_FORMAT;
+        if (!scale_dev && (!(scale > 0.0f) || isinf(scale))) return FPQ_ERR_SCALE;
+    }
+    if (p->M == 0) return FPQ_OK;
+    if (!x || (residual && !sum) || (code_scales && !codes)) return FPQ_ERR_NULL;
+    const int64_t M = p->M, K = p->K;
+    if (!stride_ok(p->ld_x, K, M) || (residual && !stride_ok(p->ld_residual, K, M)) || (sum && !stride_ok(p->ld_sum, K, M)) || (y && !stride_ok(p->ld_y, K, M)))
+        return FPQ_ERR_SHAPE;
+    const size_t size = size_of(p->type);
+    if (!aligned(x, size) || !aligned(residual, size) || !aligned(sum, size) || !aligned(y, size) || !aligned(w, 4) || !aligned(rstd, 4) || !aligned(codes, 16) ||
+        !aligned(scale_dev, 4))
+        return FPQ_ERR_ALIGN;
+    NormArgs a{};
+    a.x = x;
+    a.residual = residual;
+    a.w = w;
+    a.sum = sum;
+    a.y = y;
+    a.rstd = rstd;
+    a.codes = codes;
+    a.code_scales = code_scales;
+    if (codes && !code_scales) {
+        a.f = QParams{f.mbits, f.bias, f.ebits + f.mbits, f.maxval != 0.0f ? f.maxval : fpq_format_max(f.ebits, f.mbits, f.bias)};
+        a.hardware = f.ebits == 4 && f.mbits == 3 && f.bias == 7 && f.maxval == 448.0f;
+    }
+    a.scale = scale;
+    a.scale_dev = scale_dev;
+    a.M = M;
+    a.K = K;
+    a.ld_x = stride(p->ld_x, K, M);
+    a.ld_residual = stride(p->ld_residual, K, M);
+    a.ld_sum = stride(p->ld_sum, K, M);
+    a.ld_y = stride(p->ld_y, K, M);
+    a.eps = p->eps;
+    a.vec = norm_vec(x, p->ld_x, M, K, size) && norm_vec(residual, p->ld_residual, M, K, size) && norm_vec(sum, p->ld_sum, M, K, size) &&
+            norm_vec(y, p->ld_y, M, K, size);
+    return launch_norm(a, p->type, static_cast<hipStream_t>(stream));
+}
+
+size_t fpq_rms_norm_backward_workspace_size(int64_t M, int64_t K)
+{
+    return check_sizes(M, 1, K) == FPQ_OK ? align_up(norm_part_bytes(M, K)) : 0;
+}
+
+int fpq_rms_norm_backward(const fpq_norm_args_t* p, const void* sum, const float* w, const float* rstd, const void* grad_y, const void* grad_sum, void* grad_x,
+                          float* grad_w, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int st = check_norm(p);
+    if (st != FPQ_OK) return st;
+    const int64_t M = p->M, K = p->K;
+    if (M && (!sum || !rstd || !grad_y)) return FPQ_ERR_NULL;
+    if (!stride_ok(p->ld_sum, K, M) || !stride_ok(p->ld_grad_y, K, M) || (grad_sum && !stride_ok(p->ld_grad_sum, K, M)) ||
+        (grad_x && !stride_ok(p->ld_grad_x, K, M)))
+        return FPQ_ERR_SHAPE;
+    const size_t size = size_of(p->type);
+    if (!aligned(sum, size) || !aligned(grad_y, size) || !aligned(grad_sum, size) || !aligned(grad_x, size) || !aligned(w, 4) || !aligned(rstd, 4) || !aligned(grad_w, 4))
+        return FPQ_ERR_ALIGN;
+    if (grad_w && workspace_bad(workspace, workspace_bytes, fpq_rms_norm_backward_workspace_size(M, K), &st)) return st;
+    if (!grad_x && !grad_w) return FPQ_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    NormBackward a{};
+    a.sum = sum;
+    a.w = w;
+    a.rstd = rstd;
+    a.gy = grad_y;
+    a.gs = grad_sum;
+    a.gx = grad_x;
+    a.gw = grad_w;
+    a.part = static_cast<float*>(workspace);
+    a.M = M;
+    a.K = K;
+    a.ld_sum = stride(p->ld_sum, K, M);
+    a.ld_gy = stride(p->ld_grad_y, K, M);
+    a.ld_gs = stride(p->ld_grad_sum, K, M);
+    a.ld_gx = stride(p->ld_grad_x, K, M);
+    a.vec = norm_vec(sum, p->ld_sum, M, K, size) && norm_vec(grad_y, p->ld_grad_y, M, K, size) && norm_vec(grad_sum, p->ld_grad_sum, M, K, size) &&
+            norm_vec(grad_x, p->ld_grad_x, M, K, size);
+    return launch_norm_backward(a, p->type, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,70 @@
+// Blocks of codes, packing of operands, column sums, the gated projections' elementwise gradient, and the norm: what api_blocks.hip launches.
+#pragma once
+#include "matmul.h"
+
+namespace fpq {
+
+constexpr int64_t kBlock = 32;
+static inline int64_t block_padded(int64_t n) { return (n + kBlock - 1) / kBlock * kBlock; }
+static inline int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
+
+// A matrix for the products: planes of bf16 rows of whole 16-byte pieces, zeros behind the columns.
+int launch_planes(const void* src, int type, int64_t rows, int64_t cols, int64_t ld, __bf16* dst, int64_t ld_dst, int64_t plane, hipStream_t s);
+// The same of blocks (one plane); `eight`: E4M3, else E2M1.
+int launch_decode(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, bool eight, void* dst, int f32, int64_t ld_dst, hipStream_t s);
+int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t ld, bool eight, const uint8_t* mask, uint8_t* codes, uint8_t* scales,
+                          hipStream_t s);
+
+// Sums over the rows of a matrix, in parts of rows that a second launch adds up in order.
+struct RowParts {
+    int64_t rows;               // of a part
+    int parts;
+};
+RowParts row_parts(int64_t M, int64_t cols);
+size_t row_parts_bytes(int64_t M, int64_t cols);
+int launch_column_sums(const void* x, int type, int64_t M, int64_t N, int64_t ld, float* out, float* part, hipStream_t s);
+int launch_part_sums(const float* part, int parts, int64_t cols, float* out, hipStream_t s);
+
+// (da, dg) of the gated projections as the products take them, and the bias's gradient.
+struct GateBackward {
+    int type, act;
+    int64_t M, N;
+    const void* pre;            // [M, 2 N], or codes
+    const uint8_t* pre_scales;
+    const void* gh;
+    int64_t ld_gh;
+    __bf16* d;                  // [plane][M][ld_d]; null: only the sums
+    int64_t ld_d, plane;
+    float *grad_bias, *part;    // or null
+};
+int launch_gate_backward(const GateBackward& p, hipStream_t s);
+
+struct NormArgs {
+    const void *x, *residual;
+    const float* w;
+    void *sum, *y;
+    float* rstd;
+    uint8_t *codes, *code_scales;
+    QParams f;
+    int hardware;               // f is the hardware's E4M3
+    float scale;
+    const float* scale_dev;
+    int64_t M, K, ld_x, ld_residual, ld_sum, ld_y;
+    int64_t first;              // row of a launch
+    float eps;
+    int vec;                    // all rows may be taken 16 bytes at a time
+};
+int launch_norm(const NormArgs& p, int type, hipStream_t s);
+struct NormBackward {
+    const void* sum;
+    const float *w, *rstd;
+    const void *gy, *gs;
+    void* gx;
+    float *gw, *part;
+    int64_t M, K, ld_sum, ld_gy, ld_gs, ld_gx;
+    int vec;
+};
+size_t norm_part_bytes(int64_t M, int64_t K);
+int launch_norm_backward(const NormBackward& p, int type, hipStream_t s);
+
+}  // namespace fpq

@@ -1,0 +1,336 @@
+// Blocks of codes with a power of two as their scale, and the elementwise passes around the products: planes of operands, column sums,
+// the gated projections' gradient before the products.  All are bound by memory: a lane takes eight neighbouring elements.
+#include "blocks.h"
+
+namespace fpq {
+
+namespace {
+
+// Eight elements from column k on; zeros from `cols` on.
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int64_t k, int64_t cols, bool vec, float (&v)[8])
+{
+    if (vec && k + 8 <= cols) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = *reinterpret_cast<const float4*>(row + k), b = *reinterpret_cast<const float4*>(row + k + 4);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4*>(row + k);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                v[2 * t] = __uint_as_float(w[t] << 16);
+                v[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k + e < cols ? (float)row[k + e] : 0.0f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* row, int64_t k, int64_t cols, bool vec, const float (&v)[8])
+{
+    if (vec && k + 8 <= cols) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(row + k) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4*>(row + k + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            *reinterpret_cast<uint4*>(row + k) = make_uint4(pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]), pair_bf16(v[4], v[5]), pair_bf16(v[6], v[7]));
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (k + e < cols) row[k + e] = (T)v[e];
+    }
+}
+
+// Eight values in NP planes.
+template <int NP>
+__device__ __forceinline__ void store_planes(__bf16* dst, int64_t plane, const float (&v)[8])
+{
+    const Frag<NP> f = frag_of<NP>(v);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) *reinterpret_cast<v8bf*>(dst + p * plane) = f.p[p];
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void planes_kernel(const T* src, int64_t rows, int64_t cols, int64_t ld, __bf16* dst, int64_t ld_dst, int64_t plane, int vec)
+{
+    const int64_t per = ld_dst / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= rows * per) return;
+    const int64_t r = id / per, k = (id - r * per) * 8;
+    float v[8];
+    load8(src + r * ld, k, cols, vec, v);
+    store_planes<kPlanes<T>>(dst + r * ld_dst + k, plane, v);
+}
+
+// Eight codes of a block.
+template <bool EIGHT>
+__device__ __forceinline__ void decode8(const uint8_t* codes, int64_t at, float s, float (&v)[8])
+{
+    if constexpr (EIGHT) {
+        const uint2 w = *reinterpret_cast<const uint2*>(codes + at);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t x = t ? w.y : w.x;
+            const v2f a = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+            v[4 * t] = a.x * s;
+            v[4 * t + 1] = a.y * s;
+            v[4 * t + 2] = b.x * s;
+            v[4 * t + 3] = b.y * s;
+        }
+    } else {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + at / 2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            // 1 + e + m = 4 bits in a half's place: exponent bias 1 there against 15
+            const uint32_t c = w >> (4 * e), bits = (c & 8) << 28 | (c & 7) << 22;
+            v[e] = __uint_as_float(bits) * 0x1p126f * s;
+        }
+    }
+}
+
+template <bool EIGHT, typename T>
+__global__ __launch_bounds__(256) void decode_kernel(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, int64_t padded, T* dst, int64_t ld_dst, int vec)
+{
+    const int64_t per = padded / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= rows * per) return;
+    const int64_t r = id / per, k = (id - r * per) * 8;
+    float v[8];
+    decode8<EIGHT>(codes, id * 8, scale_of(scales[id / 4]), v);
+    store8(dst + r * ld_dst, k, cols, vec, v);
+}
+
+template <bool EIGHT, typename T>
+__global__ __launch_bounds__(256) void block_quantize_kernel(const T* x, int64_t rows, int64_t cols, int64_t padded, int64_t ld, const uint8_t* mask, uint8_t* codes,
+                                                             uint8_t* scales, int vec)
+{
+    const int64_t per = padded / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool in = id < rows * per;                                 // (whole groups of four lanes)
+    const int64_t r = in ? id / per : 0, k = in ? (id - r * per) * 8 : 0;
+    float v[8];
+    load8(x + r * ld, k, cols, vec, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+    if (!in) return;
+    const uint32_t s = EIGHT ? block_scale8(top) : block_scale4(top);
+    const float i = inverse_scale(s);
+    if ((threadIdx.x & 3) == 0) scales[id / 4] = (uint8_t)s;
+    if constexpr (EIGHT) {
+        *reinterpret_cast<uint2*>(codes + id * 8) = make_uint2(codes8(v[0] * i, v[1] * i, v[2] * i, v[3] * i), codes8(v[4] * i, v[5] * i, v[6] * i, v[7] * i));
+    } else {
+        const QParams q{1, 1, 3, 6.0f};
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (k + e >= cols) break;
+            const uint32_t c = mask ? quantize_mask(v[e], i, mask[r * cols + k + e], q) : quantize_nearest(v[e], i, q);
+            w |= c << (4 * e);
+        }
+        *reinterpret_cast<uint32_t*>(codes + id * 4) = s == 255 ? 0u : w;
+    }
+}
+
+// ---- sums over rows: 64 lanes of eight columns, four wavefronts over the rows of a part
+
+constexpr int kStripColumns = 512;
+
+__device__ __forceinline__ void strip_sum(float (&sum)[8], int64_t k, int64_t cols, float* part)
+{
+    __shared__ float room[3][64 * 8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();
+    if (wave) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) room[wave - 1][e * 64 + lane] = sum[e];
+    }
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float t = (sum[e] + room[0][e * 64 + lane]) + (room[1][e * 64 + lane] + room[2][e * 64 + lane]);
+        if (k + e < cols) part[k + e] = t;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void column_sums_kernel(const T* x, int64_t M, int64_t N, int64_t ld, int64_t rows, float* part, int vec)
+{
+    const int64_t k = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8, m1 = min(M, (int64_t)(blockIdx.y + 1) * rows);
+    float sum[8] = {};
+    if (k < N)
+        for (int64_t m = (int64_t)blockIdx.y * rows + (threadIdx.x >> 6); m < m1; m += 4) {
+            float v[8];
+            load8(x + m * ld, k, N, vec, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += v[e];
+        }
+    strip_sum(sum, k, N, part + (int64_t)blockIdx.y * N);
+}
+
+// 64 columns, 16 wavefronts over the parts
+__global__ __launch_bounds__(1024) void part_sums_kernel(const float* part, int parts, int64_t cols, float* out)
+{
+    __shared__ float room[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t k = (int64_t)blockIdx.x * 64 + lane;
+    float sum = 0.0f;
+    if (k < cols)
+        for (int p = wave; p < parts; p += 16) sum += part[p * cols + k];
+    room[wave][lane] = sum;
+    __syncthreads();
+    if (wave || k >= cols) return;
+    for (int w = 1; w < 16; ++w) sum += room[w][lane];
+    out[k] = sum;
+}
+
+// KEPT: 0 the type, 1 blocks
+template <typename T, int KEPT>
+__global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward p, int64_t rows, int vec, int vec_d)
+{
+    const int64_t k = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8, m1 = min(p.M, (int64_t)(blockIdx.y + 1) * rows), N = p.N;
+    const int64_t np = (N + 31) / 32 * 32;
+    float sum_a[8] = {}, sum_g[8] = {};
+    if (k < N)
+        for (int64_t m = (int64_t)blockIdx.y * rows + (threadIdx.x >> 6); m < m1; m += 4) {
+            float a[8], g[8], gh[8], da[8], dg[8];
+            load8(static_cast<const T*>(p.gh) + m * p.ld_gh, k, N, vec & 1, gh);
+            if constexpr (KEPT) {
+                const uint8_t* const s = p.pre_scales + m * (np / 16) + k / 32;
+                const uint8_t* const c = static_cast<const uint8_t*>(p.pre) + m * 2 * np;
+                decode8<true>(c, k, scale_of(s[0]), a);
+                decode8<true>(c + np, k, scale_of(s[np / 32]), g);
+            } else {
+                const T* const row = static_cast<const T*>(p.pre) + m * 2 * N;
+                load8(row, k, N, vec & 2, a);
+                load8(row + N, k, N, vec & 2, g);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float slope;
+                da[e] = gh[e] * gate_of<true>(p.act, g[e], &slope);
+                dg[e] = gh[e] * a[e] * slope;
+                if (k + e >= N) da[e] = dg[e] = 0.0f;
+                sum_a[e] += da[e];
+                sum_g[e] += dg[e];
+            }
+            if (!p.d) continue;
+            __bf16* const d = p.d + m * p.ld_d;
+            constexpr int NP = kPlanes<T>;
+            if (vec_d) {
+                store_planes<NP>(d + k, p.plane, da);
+                store_planes<NP>(d + N + k, p.plane, dg);
+            } else {
+                const Frag<NP> fa = frag_of<NP>(da), fg = frag_of<NP>(dg);
+#pragma unroll
+                for (int q = 0; q < NP; ++q)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (k + e < N) {
+                            d[q * p.plane + k + e] = fa.p[q][e];
+                            d[q * p.plane + N + k + e] = fg.p[q][e];
+                        }
+                if (k + 8 >= N)                                     // zeros behind the row
+                    for (int q = 0; q < NP; ++q)
+                        for (int64_t c = 2 * N; c < p.ld_d; ++c) d[q * p.plane + c] = (__bf16)0.0f;
+            }
+        }
+    if (!p.part) return;
+    float* const part = p.part + (int64_t)blockIdx.y * 2 * N;
+    strip_sum(sum_a, k, N, part);
+    strip_sum(sum_g, k, N, part + N);
+}
+
+unsigned grid256(int64_t n) { return (unsigned)((n + 255) / 256); }
+bool rows_vec(const void* p, int64_t ld, int type)
+{
+    return ((uintptr_t)p & 15) == 0 && ld % (type == FPQ_TYPE_FP32 ? 4 : 8) == 0;
+}
+int launched() { return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH; }
+
+}  // namespace
+
+int launch_planes(const void* src, int type, int64_t rows, int64_t cols, int64_t ld, __bf16* dst, int64_t ld_dst, int64_t plane, hipStream_t s)
+{
+    const unsigned grid = grid256(rows * (ld_dst / 8));
+    if (!grid) return FPQ_OK;
+    const int vec = rows_vec(src, ld, type);
+    if (type == FPQ_TYPE_FP32) planes_kernel<<<dim3(grid), dim3(256), 0, s>>>(static_cast<const float*>(src), rows, cols, ld, dst, ld_dst, plane, vec);
+    else planes_kernel<<<dim3(grid), dim3(256), 0, s>>>(static_cast<const __bf16*>(src), rows, cols, ld, dst, ld_dst, plane, vec);
+    return launched();
+}
+
+int launch_decode(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, bool eight, void* dst, int f32, int64_t ld_dst, hipStream_t s)
+{
+    const int64_t padded = block_padded(cols);
+    const unsigned grid = grid256(rows * (padded / 8));
+    if (!grid) return FPQ_OK;
+    const int vec = rows_vec(dst, ld_dst, f32 ? FPQ_TYPE_FP32 : FPQ_TYPE_BF16);
+    auto run = [&](auto kernel, auto* to) { kernel<<<dim3(grid), dim3(256), 0, s>>>(codes, scales, rows, cols, padded, to, ld_dst, vec); };
+    if (f32) eight ? run(decode_kernel<true, float>, static_cast<float*>(dst)) : run(decode_kernel<false, float>, static_cast<float*>(dst));
+    else eight ? run(decode_kernel<true, __bf16>, static_cast<__bf16*>(dst)) : run(decode_kernel<false, __bf16>, static_cast<__bf16*>(dst));
+    return launched();
+}
+
+int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t ld, bool eight, const uint8_t* mask, uint8_t* codes, uint8_t* scales,
+                          hipStream_t s)
+{
+    const int64_t padded = block_padded(K);
+    const unsigned grid = grid256(M * (padded / 8));
+    if (!grid) return FPQ_OK;
+    const int vec = rows_vec(x, ld, type);
+    auto run = [&](auto kernel, auto* from) { kernel<<<dim3(grid), dim3(256), 0, s>>>(from, M, K, padded, ld, mask, codes, scales, vec); };
+    if (type == FPQ_TYPE_FP32) eight ? run(block_quantize_kernel<true, float>, static_cast<const float*>(x)) : run(block_quantize_kernel<false, float>, static_cast<const float*>(x));
+    else eight ? run(block_quantize_kernel<true, __bf16>, static_cast<const __bf16*>(x)) : run(block_quantize_kernel<false, __bf16>, static_cast<const __bf16*>(x));
+    return launched();
+}
+
+// About 1024 workgroups, of no fewer than 16 rows.
+RowParts row_parts(int64_t M, int64_t cols)
+{
+    const int64_t strips = (cols + kStripColumns - 1) / kStripColumns;
+    int64_t parts = 1024 / strips, most = (M + 15) / 16;
+    parts = parts < 1 ? 1 : parts > most ? most : parts;
+    if (parts < 1) parts = 1;
+    const int64_t rows = (M + parts - 1) / parts;
+    return RowParts{rows < 1 ? 1 : rows, (int)(rows < 1 ? 1 : (M + rows - 1) / rows)};
+}
+size_t row_parts_bytes(int64_t M, int64_t cols) { return (size_t)row_parts(M, cols).parts * cols * 4; }
+
+int launch_part_sums(const float* part, int parts, int64_t cols, float* out, hipStream_t s)
+{
+    part_sums_kernel<<<dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s>>>(part, parts, cols, out);
+    return launched();
+}
+
+int launch_column_sums(const void* x, int type, int64_t M, int64_t N, int64_t ld, float* out, float* part, hipStream_t s)
+{
+    const RowParts r = row_parts(M, N);
+    const dim3 grid((unsigned)((N + kStripColumns - 1) / kStripColumns), (unsigned)r.parts);
+    const int vec = rows_vec(x, ld, type);
+    if (type == FPQ_TYPE_FP32) column_sums_kernel<<<grid, dim3(256), 0, s>>>(static_cast<const float*>(x), M, N, ld, r.rows, part, vec);
+    else column_sums_kernel<<<grid, dim3(256), 0, s>>>(static_cast<const __bf16*>(x), M, N, ld, r.rows, part, vec);
+    const int st = launched();
+    return st == FPQ_OK ? launch_part_sums(part, r.parts, N, out, s) : st;
+}
+
+int launch_gate_backward(const GateBackward& p, hipStream_t s)
+{
+    const RowParts r = row_parts(p.M, p.N);
+    const dim3 grid((unsigned)((p.N + kStripColumns - 1) / kStripColumns), (unsigned)r.parts);
+    const int vec = (rows_vec(p.gh, p.ld_gh, p.type) ? 1 : 0) | (rows_vec(p.pre, p.N, p.type) ? 2 : 0), vec_d = p.N % 8 == 0;
+    GateBackward q = p;
+    if (!p.grad_bias) q.part = nullptr;
+    auto run = [&](auto kernel) { kernel<<<grid, dim3(256), 0, s>>>(q, r.rows, vec, vec_d); };
+    if (p.type == FPQ_TYPE_FP32) p.pre_scales ? run(gate_backward_kernel<float, 1>) : run(gate_backward_kernel<float, 0>);
+    else p.pre_scales ? run(gate_backward_kernel<__bf16, 1>) : run(gate_backward_kernel<__bf16, 0>);
+    const int st = launched();
+    return st == FPQ_OK && q.part ? launch_part_sums(q.part, r.parts, 2 * p.N, p.grad_bias, s) : st;
+}
+
+}  // namespace fpq

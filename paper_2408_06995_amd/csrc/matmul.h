@@ -1,0 +1,428 @@
+// Matrix products of the operators around the projections (gated projections, gradients of linear layers, layers on 4-bit blocks):
+//
+//   out[m, n] = sum_k A(m, k) B(n, k)
+//
+// Operands are one or three planes of bf16 (fp32 values x = h + m + l, as in attention.h; of nine products the six largest are taken,
+// beside an operand of one plane all three).  Each operand lies either with the contraction along its rows (ROW: p[m ld + k]) or along
+// its columns (COL: p[k ld + m]), so that x W^T, g W and g^T x are one kernel without a transposed copy.
+//
+// A workgroup makes a tile of BM x BN results in steps of 64 along k; tiles go from memory to LDS directly, a step ahead, into the other
+// of two buffers.  ROW tiles are read as 16 bytes of a row, COL tiles by the transposing read, which gives a lane four k of its column;
+// both in the same order of k, eight neighbours per lane.  Places of 16 bytes are exchanged within a row so that neither read meets a
+// bank twice: of a ROW tile 16 rows of one piece lie in the 16 groups of four banks, of a COL tile four rows of 64 bytes each.
+// B is the A operand of the instruction: a lane then holds four neighbouring columns n of one row m of the result.
+#pragma once
+#include "attention.h"
+#include "gemm_common.h"
+
+namespace fpq {
+
+struct Operand {
+    const __bf16* p;
+    int64_t ld, plane;          // in elements
+};
+
+// What the results of a tile become.
+enum MatmulEnd : int { kStore = 0, kGated = 1 };
+
+struct Gate {
+    int act;                    // fpq_gate
+    void* h;
+    int64_t ld_h;
+    void* pre;                  // [M, 2 N] of the type, or codes [M, 2 Np], or null
+    int64_t ld_pre;             // (type only)
+    uint8_t* pre_scales;        // codes' scales or null
+};
+
+struct MatmulArgs {
+    Operand a, b;
+    int M, N, K;                // gated: N outputs, B has 2 N rows, values first
+    int steps;                  // of 64 along K
+    uint32_t order_a, order_b;  // planes of each pass, four bits each, the first pass lowest
+    int total;                  // passes x steps
+    int slices;                 // of `total`
+    int tiles_m, tiles_n;
+    void* out;                  // kStore; slices > 1: fp32 [slice][M][N] (gated: [slice][M][2 N]) whatever the end
+    int64_t ld_out;
+    int out_f32;
+    const float* bias;          // [N] or [2 N] or null (slices == 1)
+    Gate gate;
+};
+
+constexpr int kStep = 64;
+
+// Block scales: a power of two as its biased exponent; 255 stands for NaN.
+__device__ __forceinline__ float scale_of(uint32_t e) { return e ? __uint_as_float(e == 255 ? 0x7fc00000u : e << 23) : 0x1p-127f; }
+// The least power of two with which a largest magnitude (its bits) is at most (1 + top / 2^23) 2^max_exp; 1 for zero.
+__device__ __forceinline__ uint32_t block_scale(uint32_t bits, int max_exp, uint32_t top)
+{
+    if (bits >= 0x7f800000u) return 255u;
+    if (bits == 0) return 127u;
+    const int e = (int)(bits >> 23) - max_exp + ((bits & 0x7fffffu) > top ? 1 : 0);
+    return (uint32_t)max(e, 1);
+}
+__device__ __forceinline__ uint32_t block_scale8(uint32_t bits) { return block_scale(bits, 8, 0x600000u); }      // 448 = 1.75 2^8
+__device__ __forceinline__ uint32_t block_scale4(uint32_t bits) { return block_scale(bits, 2, 0x400000u); }      // 6 = 1.5 2^2
+// 1 / scale, exact
+__device__ __forceinline__ float inverse_scale(uint32_t e) { return __uint_as_float(e == 255 ? 0x7fc00000u : (254u - e) << 23); }
+
+__device__ __forceinline__ uint32_t codes8(float a, float b, float c, float d)
+{
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// act(g) and its derivative.  SiLU: g z and z (1 + g (1 - z)) with z = 1 / (1 + e^-g), off by at most (4 + |g|) 2^-23 of z (the exponent's
+// product is rounded, exponential and reciprocal are the hardware's).  GELU: g Phi(g) and Phi(g) + g phi(g), Phi by the formula of
+// act_gelu, off by at most 4e-7.
+template <bool SLOPE>
+__device__ __forceinline__ float gate_of(int act, float g, float* slope)
+{
+    if (act == FPQ_GATE_SILU) {
+        const float z = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * g));
+        if constexpr (SLOPE) *slope = z * fmaf(g, 1.0f - z, 1.0f);
+        return g * z;
+    }
+    if constexpr (!SLOPE) return act_gelu(g);
+    const float m = fminf(fabsf(g), 1e18f), s = m * 0.84932180028801907f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.23164188f, m, 1.0f)), e = __builtin_amdgcn_exp2f(-s * s);
+    float p = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    p = fmaf(t, p, 0.5f * 1.421413741f);
+    p = fmaf(t, p, 0.5f * -0.284496736f);
+    p = fmaf(t, p, 0.5f * 0.254829592f);
+    const float half = t * p * e, z = g > 0.0f ? 1.0f - half : half;
+    if constexpr (SLOPE) *slope = fmaf(g * 0.39894228040143268f, e, z);
+    return g * z;
+}
+
+// One operand's tile of R rows (ROW) or columns (COL) and 64 k: this thread's loads of it.
+template <bool COL, int R, int NT>
+struct TileFeed {
+    static constexpr int CS = COL ? R / 8 : 8, N = R * 8, PT = (N + NT - 1) / NT, NW = NT / 64, BYTES = R * 128;
+    static_assert(N % 64 == 0 && (!COL || R >= 128), "whole wavefronts of loads; rows of COL tiles span all banks");
+    static __device__ __forceinline__ int swap(int row) { return COL ? (row & 3) << 2 : (row >> 1) & 7; }
+    unsigned off[PT];
+    // `rows` (ROW) or `cols` (COL) of the tile exist
+    __device__ __forceinline__ void init(int64_t ld, int exist)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            const int q = (wave + NW * i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ swap(row);
+            const bool in = COL ? 8 * c < exist : row < exist;
+            off[i] = in ? (unsigned)row * (unsigned)(2 * ld) + 16u * c : 0x80000000u;
+        }
+    }
+    // Starts the loads of the tile at `base`; `left` k remain (ROW: in whole pieces), `bytes` may be read from base on.
+    __device__ __forceinline__ void load(const __bf16* base, unsigned bytes, int left, unsigned lds) const
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const v4i r = make_rsrc(base, bytes);
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            if (N % (64 * NW) != 0 && wave + NW * i >= N / 64) break;
+            unsigned o = off[i];
+            if (!COL && left < kStep) {
+                const int q = (wave + NW * i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ swap(row);
+                if (8 * c >= left) o = 0x80000000u;
+            }
+            dma16(r, o, lds + (wave + NW * i) * 1024);
+        }
+    }
+};
+
+// This lane's places in a tile for its 32 T rows or columns from `first` on.
+template <bool COL, int R, int T>
+struct TilePlaces {
+    int at[COL ? T : 4];        // bytes: COL per 32 columns; ROW per 16 k
+    __device__ __forceinline__ void init(int first)
+    {
+        const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+        if constexpr (COL) {
+            const int q = 8 * h + ((lane & 15) >> 2), s = q & 3;
+#pragma unroll
+            for (int d = 0; d < T; ++d) {
+                const int c = first / 8 + 4 * d + ((lane & 16) >> 3) + ((lane & 3) >> 1);
+                at[d] = q * (2 * R) + 16 * (c ^ (s << 2)) + 8 * (lane & 1);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) at[t] = (first + r) * 128 + 16 * ((2 * t + h) ^ ((r >> 1) & 7));
+        }
+    }
+    // operand for 16 k from 16 t on
+    __device__ __forceinline__ v8bf read(const char* tile, int u, int t) const
+    {
+        if constexpr (COL) {
+            const char* p = tile + at[u] + t * 16 * (2 * R);
+            const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p));
+            const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p + 4 * (2 * R)));
+            return __builtin_bit_cast(v8bf, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            return *reinterpret_cast<const v8bf*>(tile + at[t] + u * 32 * 128);
+        }
+    }
+};
+
+// The tile of a workgroup: neighbours in time on one XCD share rows of A and columns of B, in bands of `kBand` tiles along m.
+struct MatmulPlace {
+    int m, n, slice;
+};
+__device__ __forceinline__ MatmulPlace matmul_place(const MatmulArgs& p)
+{
+    constexpr int kBand = 8;
+    const int total = gridDim.x, per = total >> 3;
+    int id = blockIdx.x;
+    if (id < per << 3) id = (id & 7) * per + (id >> 3);
+    const int tiles = p.tiles_m * p.tiles_n;
+    MatmulPlace r;
+    r.slice = id / tiles;
+    id -= r.slice * tiles;
+    const int band = id / (kBand * p.tiles_n), first = band * kBand, high = min(kBand, p.tiles_m - first);
+    id -= band * kBand * p.tiles_n;
+    r.n = id / high;
+    r.m = first + id - r.n * high;
+    return r;
+}
+
+// Four neighbouring results of a row; `vec`: they lie within the row and may be stored together.
+__device__ __forceinline__ void put4(void* out, int64_t at, int f32, int n, int N, bool vec, const float (&v)[4])
+{
+    if (f32) {
+        float* const o = static_cast<float*>(out) + at;
+        if (vec) {
+            *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N) o[e] = v[e];
+        }
+    } else {
+        __bf16* const o = static_cast<__bf16*>(out) + at;
+        if (vec) {
+            *reinterpret_cast<uint2*>(o) = make_uint2(pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N) o[e] = (__bf16)v[e];
+        }
+    }
+}
+
+// One block of 32 outputs of a row: values a and gates g, 16 of them in each of the lanes l and l + 32 (as the matrix unit leaves
+// them: places 8 (i / 4) + 4 h + i % 4 from n0 on).  Writes h and what is kept.
+__device__ __forceinline__ void gated_block(const Gate& p, int f32, int64_t m, int n0, int N, bool in, int h, const float (&a)[16], const float (&g)[16])
+{
+    const int np = (N + 31) & ~31;
+    const bool vec4 = (p.ld_h & 3) == 0 && ((uintptr_t)p.h & 15) == 0;
+    const bool vec4p = (p.ld_pre & 3) == 0 && (N & 3) == 0 && ((uintptr_t)p.pre & 15) == 0;
+    uint32_t ea = 0, eg = 0;
+    float ia = 0.0f, ig = 0.0f;
+    if (p.pre_scales) {
+        uint32_t ta = 0, tg = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool has = n0 + 8 * (i / 4) + 4 * h + i % 4 < N;
+            ta = max(ta, has ? __float_as_uint(a[i]) & 0x7fffffffu : 0u);
+            tg = max(tg, has ? __float_as_uint(g[i]) & 0x7fffffffu : 0u);
+        }
+        ta = max(ta, (uint32_t)__shfl_xor((int)ta, 32, 64));
+        tg = max(tg, (uint32_t)__shfl_xor((int)tg, 32, 64));
+        ea = block_scale8(ta);
+        eg = block_scale8(tg);
+        ia = inverse_scale(ea);
+        ig = inverse_scale(eg);
+        if (in && h == 0 && n0 < N) {
+            uint8_t* const s = p.pre_scales + m * (2 * (np / 32)) + n0 / 32;
+            s[0] = (uint8_t)ea;
+            s[np / 32] = (uint8_t)eg;
+        }
+    }
+    if (!in) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int n = n0 + 8 * q + 4 * h;
+        float va[4], vg[4], vh[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            va[e] = a[4 * q + e];
+            vg[e] = g[4 * q + e];
+            vh[e] = va[e] * gate_of<false>(p.act, vg[e], nullptr);
+        }
+        if (n < N) put4(p.h, m * p.ld_h + n, f32, n, N, vec4 && n + 4 <= N, vh);
+        if (p.pre_scales) {
+            if (n0 >= N) continue;
+            uint8_t* const c = static_cast<uint8_t*>(p.pre) + m * (2 * (int64_t)np) + n;
+            auto has = [&](int e, float x, float s) { return n + e < N ? x * s : 0.0f; };
+            *reinterpret_cast<uint32_t*>(c) = codes8(has(0, va[0], ia), has(1, va[1], ia), has(2, va[2], ia), has(3, va[3], ia));
+            *reinterpret_cast<uint32_t*>(c + np) = codes8(has(0, vg[0], ig), has(1, vg[1], ig), has(2, vg[2], ig), has(3, vg[3], ig));
+        } else if (p.pre && n < N) {
+            put4(p.pre, m * p.ld_pre + n, f32, n, N, vec4p && n + 4 <= N, va);
+            put4(p.pre, m * p.ld_pre + N + n, f32, n, N, vec4p && n + 4 <= N, vg);
+        }
+    }
+}
+
+// (waves per SIMD: the tiles' LDS lets one workgroup of eight or two of four wavefronts run on a compute unit)
+template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int END>
+__global__ __launch_bounds__(64 * WM * WN, 2) void matmul_kernel(MatmulArgs p)
+{
+    constexpr int NT = 64 * WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+    using FA = TileFeed<COLA, BM, NT>;
+    using FB = TileFeed<COLB, END == kGated ? BN / 2 : BN, NT>;
+    constexpr int STAGE = BM * 128 + BN * 128;
+    static_assert(END != kGated || (!COLB && TN == 2), "gated: a wavefront has the 32 values and the 32 gates of the same outputs");
+    extern __shared__ __align__(1024) char lds[];
+    const MatmulPlace at = matmul_place(p);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave / WN, wn = wave % WN;
+    constexpr int CB = END == kGated ? BN / 2 : BN;             // columns of the result in a tile
+    const int m0 = at.m * BM, n0 = at.n * CB;
+    const int64_t lda = p.a.ld, ldb = p.b.ld;
+
+    FA fa;
+    FB fb;
+    fa.init(lda, p.M - m0);
+    fb.init(ldb, p.N - n0);
+    const int beg = (int)((int64_t)p.total * at.slice / p.slices), end = (int)((int64_t)p.total * (at.slice + 1) / p.slices);
+    int pass = beg / p.steps, step = beg - pass * p.steps;
+    const unsigned base = lds_address(lds);
+
+    // bytes that may be read from the first element of a tile on: whole rows of what is left of the matrix
+    auto load = [&](int buf) {
+        const int k0 = step * kStep, left = p.K - k0, left8 = (left + 7) & ~7;
+        const __bf16* const pa = p.a.p + ((p.order_a >> (4 * pass)) & 15) * p.a.plane;
+        const __bf16* const pb = p.b.p + ((p.order_b >> (4 * pass)) & 15) * p.b.plane;
+        const unsigned to = base + buf * STAGE;
+        auto bytes = [&](bool col, int64_t ld, int first, int rows, int all, int count) {
+            const int64_t r = col ? min(left, kStep) : min(all - first, count);
+            return (unsigned)(2 * ((r - 1) * ld + (col ? ((all + 7) & ~7) - first : left8)));
+        };
+        fa.load(COLA ? pa + (int64_t)k0 * lda + m0 : pa + (int64_t)m0 * lda + k0, bytes(COLA, lda, m0, BM, p.M, BM), left8, to);
+        const __bf16* const qb = COLB ? pb + (int64_t)k0 * ldb + n0 : pb + (int64_t)n0 * ldb + k0;
+        fb.load(qb, bytes(COLB, ldb, n0, CB, p.N, CB), left8, to + BM * 128);
+        if constexpr (END == kGated)
+            fb.load(qb + (int64_t)p.N * ldb, bytes(false, ldb, n0, CB, p.N, CB), left8, to + BM * 128 + CB * 128);
+        if (++step == p.steps) {
+            step = 0;
+            ++pass;
+        }
+    };
+
+    TilePlaces<COLA, BM, TM> ra;
+    TilePlaces<COLB, BN, END == kGated ? 1 : TN> rb;
+    ra.init(wm * TM * 32);
+    rb.init(END == kGated ? wn * 32 : wn * TN * 32);
+    v16f acc[TM][TN];
+#pragma unroll
+    for (int u = 0; u < TM; ++u)
+#pragma unroll
+        for (int v = 0; v < TN; ++v) acc[u][v] = zero16();
+
+    if (beg < end) load(0);
+    int buf = 0;
+    for (int it = beg; it < end; ++it) {
+        dma_barrier();
+        if (it + 1 < end) load(buf ^ 1);
+        const char* const ta = lds + buf * STAGE;
+        const char* const tb = ta + BM * 128;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            v8bf a[TM], b[TN];
+#pragma unroll
+            for (int v = 0; v < TN; ++v) {
+                if constexpr (END == kGated) b[v] = rb.read(tb + v * CB * 128, 0, t);
+                else b[v] = rb.read(tb, v, t);
+            }
+#pragma unroll
+            for (int u = 0; u < TM; ++u) a[u] = ra.read(ta, u, t);
+#pragma unroll
+            for (int u = 0; u < TM; ++u)
+#pragma unroll
+                for (int v = 0; v < TN; ++v) acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[v], a[u], acc[u][v], 0, 0, 0);
+        }
+        buf ^= 1;
+    }
+
+    const int h = lane >> 5, l32 = lane & 31;
+    if (p.slices > 1) {
+        const int cols = END == kGated ? 2 * p.N : p.N;
+        float* const part = static_cast<float*>(p.out) + (int64_t)at.slice * p.M * cols;
+        const bool vec = (p.N & 3) == 0;
+#pragma unroll
+        for (int u = 0; u < TM; ++u) {
+            const int m = m0 + (wm * TM + u) * 32 + l32;
+            if (m >= p.M) continue;
+#pragma unroll
+            for (int v = 0; v < TN; ++v) {
+                const int nb = END == kGated ? n0 + wn * 32 : n0 + (wn * TN + v) * 32;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = nb + 8 * q + 4 * h;
+                    const float x[4] = {acc[u][v][4 * q], acc[u][v][4 * q + 1], acc[u][v][4 * q + 2], acc[u][v][4 * q + 3]};
+                    if (n < p.N) put4(part, (int64_t)m * cols + n + (END == kGated ? v * p.N : 0), 1, n, p.N, vec && n + 4 <= p.N, x);
+                }
+            }
+        }
+        return;
+    }
+    if constexpr (END == kGated) {
+        const int nb = n0 + wn * 32;
+        float ba[16], bg[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int n = nb + 8 * (i / 4) + 4 * h + i % 4;
+            ba[i] = p.bias && n < p.N ? p.bias[n] : 0.0f;
+            bg[i] = p.bias && n < p.N ? p.bias[p.N + n] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < TM; ++u) {
+            const int m = m0 + (wm * TM + u) * 32 + l32;
+            float a[16], g[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                a[i] = acc[u][0][i] + ba[i];
+                g[i] = acc[u][1][i] + bg[i];
+            }
+            gated_block(p.gate, p.out_f32, m, nb, p.N, m < p.M, h, a, g);
+        }
+    } else {
+        const bool vec = (p.ld_out & 3) == 0 && ((uintptr_t)p.out & 15) == 0;
+#pragma unroll
+        for (int v = 0; v < TN; ++v)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = n0 + (wn * TN + v) * 32 + 8 * q + 4 * h;
+                if (n >= p.N) continue;
+                float b[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) b[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.0f;
+#pragma unroll
+                for (int u = 0; u < TM; ++u) {
+                    const int m = m0 + (wm * TM + u) * 32 + l32;
+                    if (m >= p.M) continue;
+                    const float x[4] = {acc[u][v][4 * q] + b[0], acc[u][v][4 * q + 1] + b[1], acc[u][v][4 * q + 2] + b[2], acc[u][v][4 * q + 3] + b[3]};
+                    put4(p.out, m * p.ld_out + n, p.out_f32, n, p.N, vec && n + 4 <= p.N, x);
+                }
+            }
+    }
+}
+
+// A product as the callers give it: M, N, K, operands, `planes` of each, forms, and what becomes of it.
+struct Product {
+    Operand a, b;
+    int64_t M, N, K;
+    int planes_a, planes_b;
+    bool col_a, col_b;
+    void* out;
+    int64_t ld_out;
+    int out_f32;
+    const float* bias;
+    bool gated;
+    Gate gate;
+};
+// Bytes of partial results of a product of these sizes (0 where it is made in one slice).
+size_t product_part_bytes(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated);
+int launch_product(const Product& p, void* part, hipStream_t s);
+
+}  // namespace fpq

@@ -1,0 +1,401 @@
+// Root-mean-square norm on the residual stream, and its gradient.
+//
+// A row is read once: 64 or 256 threads hold it in registers, in pieces of 16 bytes, while its mean square (or the gradient's
+// projection on it) is summed; bound by memory.  Rows too long for that are read a second time, which the caches serve.
+#include "blocks.h"
+
+#include <utility>
+
+namespace fpq {
+
+namespace {
+
+template <typename T>
+constexpr int kPiece = 16 / (int)sizeof(T);
+
+// Elements k .. of a row; zeros from K on.  VEC: rows are whole aligned pieces.
+template <typename T, bool VEC>
+__device__ __forceinline__ void piece(const T* row, int64_t k, int64_t K, float (&v)[kPiece<T>])
+{
+    constexpr int E = kPiece<T>;
+    if constexpr (VEC) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (k < K) x = *reinterpret_cast<const uint4*>(row + k);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if constexpr (E == 4) {
+                v[t] = __uint_as_float(w[t]);
+            } else {
+                v[2 * t] = __uint_as_float(w[t] << 16);
+                v[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = k + e < K ? (float)row[k + e] : 0.0f;
+    }
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void put(T* row, int64_t k, int64_t K, const float (&v)[kPiece<T>])
+{
+    constexpr int E = kPiece<T>;
+    if constexpr (VEC) {
+        if (k >= K) return;
+        if constexpr (E == 4) *reinterpret_cast<float4*>(row + k) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint4*>(row + k) = make_uint4(pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]), pair_bf16(v[4], v[5]), pair_bf16(v[6], v[7]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (k + e < K) row[k + e] = (T)v[e];
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void weights(const float* w, int64_t k, int64_t K, float (&v)[kPiece<T>])
+{
+    constexpr int E = kPiece<T>;
+    if (!w) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = 1.0f;
+    } else if (((uintptr_t)w & 15) == 0 && k + E <= K) {
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(w + k + e);
+            v[e] = x.x, v[e + 1] = x.y, v[e + 2] = x.z, v[e + 3] = x.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = k + e < K ? w[k + e] : 0.0f;
+    }
+}
+
+// The sum over a row's threads: 64 of a wavefront, or the 256 of the workgroup (`room`: four values of this call's own).
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* room)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    if constexpr (TPR == 64) return v;
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (room[0] + room[1]) + (room[2] + room[3]);
+}
+
+// CH pieces of a row per thread; CH == 0: any number, in two passes.
+template <typename T, bool VEC, int TPR, int CH>
+__global__ __launch_bounds__(256) void norm_kernel(NormArgs p)
+{
+    constexpr int E = kPiece<T>, RPB = 256 / TPR;
+    __shared__ float room[4];
+    const int t = threadIdx.x % TPR;
+    const int64_t m = p.first + (int64_t)blockIdx.x * RPB + threadIdx.x / TPR, K = p.K;
+    if (m >= p.M) return;                                             // (whole wavefronts; with TPR 256 none)
+    const T* const x = static_cast<const T*>(p.x) + m * p.ld_x;
+    const T* const res = p.residual ? static_cast<const T*>(p.residual) + m * p.ld_residual : nullptr;
+    T* const sum = p.sum ? static_cast<T*>(p.sum) + m * p.ld_sum : nullptr;
+    // columns that are written: codes go on behind the row
+    const int64_t span = p.codes ? (p.code_scales ? (K + 31) / 32 * 32 : (K + 15) / 16 * 16) : K;
+
+    auto stream = [&](int64_t k, float (&v)[E]) {
+        piece<T, VEC>(x, k, K, v);
+        if (res) {
+            float u[E];
+            piece<T, VEC>(res, k, K, u);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = (float)(T)(v[e] + u[e]);
+        }
+    };
+    float c = 1.0f;
+    if (p.codes && !p.code_scales) c = inv_scale(p.scale, p.scale_dev);
+    auto finish = [&](int64_t k, const float (&v)[E], float rstd) {
+        float w[E], y[E];
+        weights<T>(p.w, k, K, w);
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = v[e] * rstd * w[e];
+        if (p.y) put<T, VEC>(static_cast<T*>(p.y) + m * p.ld_y, k, K, y);
+        if (!p.codes) return;
+        uint32_t q[E / 4];
+        if (p.code_scales) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if (k + e >= K) y[e] = 0.0f;
+                top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+            }
+#pragma unroll
+            for (int off = 1; off < 32 / E; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
+            if (k >= span) return;
+            const uint32_t s = block_scale8(top);
+            const float i = inverse_scale(s);
+            if (k % 32 == 0) p.code_scales[m * (span / 32) + k / 32] = (uint8_t)s;
+#pragma unroll
+            for (int e = 0; e < E; e += 4) q[e / 4] = codes8(y[e] * i, y[e + 1] * i, y[e + 2] * i, y[e + 3] * i);
+        } else {
+            if (k >= span) return;
+            auto bound = [&](int e) { return k + e < K ? fminf(fmaxf(__fmul_rn(y[e], c), -448.0f), 448.0f) : 0.0f; };
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                if (p.hardware) {
+                    q[e / 4] = codes8(bound(e), bound(e + 1), bound(e + 2), bound(e + 3));
+                } else {
+                    q[e / 4] = 0;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        if (k + e + b < K) q[e / 4] |= quantize_nearest(y[e + b], c, p.f) << (8 * b);
+                }
+            }
+        }
+        uint8_t* const to = p.codes + m * span + k;
+        if constexpr (E == 4) *reinterpret_cast<uint32_t*>(to) = q[0];
+        else *reinterpret_cast<uint2*>(to) = make_uint2(q[0], q[1]);
+    };
+
+    float ss = 0.0f;
+    if constexpr (CH > 0) {
+        float v[CH][E];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) stream((int64_t)(t + TPR * i) * E, v[i]);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) ss = fmaf(v[i][e], v[i][e], ss);
+            if (sum) put<T, VEC>(sum, (int64_t)(t + TPR * i) * E, K, v[i]);
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<TPR>(ss, room) / (float)K + p.eps);
+        if (p.rstd && t == 0) p.rstd[m] = rstd;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) finish((int64_t)(t + TPR * i) * E, v[i], rstd);
+    } else {
+        const int64_t pieces = (span + E - 1) / E, rounds = (pieces + TPR - 1) / TPR;      // (all lanes take part in every round)
+        float v[E];
+        for (int64_t i = 0; i < rounds; ++i) {
+            const int64_t k = (t + TPR * i) * E;
+            stream(k, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) ss = fmaf(v[e], v[e], ss);
+            if (sum) put<T, VEC>(sum, k, K, v);
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<TPR>(ss, room) / (float)K + p.eps);
+        if (p.rstd && t == 0) p.rstd[m] = rstd;
+        for (int64_t i = 0; i < rounds; ++i) {
+            const int64_t k = (t + TPR * i) * E;
+            if (sum) piece<T, VEC>(sum, k, K, v);
+            else stream(k, v);
+            finish(k, v, rstd);
+        }
+    }
+}
+
+// Rows blockIdx, blockIdx + gridDim, ... (of 256 / TPR at a time); the columns' sums for the weights' gradient stay with the thread.
+template <typename T, bool VEC, int TPR, int CH>
+__global__ __launch_bounds__(256) void norm_backward_kernel(NormBackward p, int own_sums)
+{
+    constexpr int E = kPiece<T>, RPB = 256 / TPR;
+    __shared__ float room[2][4];
+    const int t = threadIdx.x % TPR;
+    const int64_t K = p.K;
+    const float over = 1.0f / (float)K;
+    constexpr int C = CH > 0 ? CH : 1;
+    float w[C][E], gw[C][E];
+    if constexpr (CH > 0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            weights<T>(p.w, (int64_t)(t + TPR * i) * E, K, w[i]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) gw[i][e] = 0.0f;
+        }
+    }
+    int flip = 0;
+    for (int64_t m = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; m < p.M; m += (int64_t)gridDim.x * RPB) {
+        const T* const r = static_cast<const T*>(p.sum) + m * p.ld_sum;
+        const T* const gy = static_cast<const T*>(p.gy) + m * p.ld_gy;
+        const T* const gs = p.gs ? static_cast<const T*>(p.gs) + m * p.ld_gs : nullptr;
+        T* const gx = p.gx ? static_cast<T*>(p.gx) + m * p.ld_gx : nullptr;
+        const float rstd = p.rstd[m];
+        auto finish = [&](int64_t k, const float (&g)[E], const float (&v)[E], const float (&u)[E], float c) {
+            float o[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(rstd, fmaf(-v[e], c, g[e]), u[e]);
+            put<T, VEC>(gx, k, K, o);
+        };
+        if constexpr (CH > 0) {
+            float v[CH][E], g[CH][E], u[CH][E], dot = 0.0f;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int64_t k = (int64_t)(t + TPR * i) * E;
+                piece<T, VEC>(r, k, K, v[i]);
+                piece<T, VEC>(gy, k, K, g[i]);
+                if (gs) piece<T, VEC>(gs, k, K, u[i]);
+                else
+#pragma unroll
+                    for (int e = 0; e < E; ++e) u[i][e] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    gw[i][e] = fmaf(g[i][e] * v[i][e], rstd, gw[i][e]);
+                    g[i][e] *= w[i][e];
+                    dot = fmaf(g[i][e], v[i][e], dot);
+                }
+            const float c = row_sum<TPR>(dot, room[flip]) * over * rstd * rstd;
+            flip ^= 1;
+            if (gx)
+#pragma unroll
+                for (int i = 0; i < CH; ++i) finish((int64_t)(t + TPR * i) * E, g[i], v[i], u[i], c);
+        } else {
+            const int64_t pieces = (K + E - 1) / E;
+            float v[E], g[E], u[E], y[E], dot = 0.0f;
+            for (int64_t i = t; i < pieces; i += TPR) {
+                piece<T, VEC>(r, i * E, K, v);
+                piece<T, VEC>(gy, i * E, K, g);
+                weights<T>(p.w, i * E, K, y);
+#pragma unroll
+                for (int e = 0; e < E; ++e) dot = fmaf(g[e] * y[e], v[e], dot);
+            }
+            const float c = row_sum<TPR>(dot, room[flip]) * over * rstd * rstd;
+            flip ^= 1;
+            if (gx)
+                for (int64_t i = t; i < pieces; i += TPR) {
+                    piece<T, VEC>(r, i * E, K, v);
+                    piece<T, VEC>(gy, i * E, K, g);
+                    weights<T>(p.w, i * E, K, y);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        g[e] *= y[e];
+                        u[e] = 0.0f;
+                    }
+                    if (gs) piece<T, VEC>(gs, i * E, K, u);
+                    finish(i * E, g, v, u, c);
+                }
+        }
+    }
+    if constexpr (CH > 0) {
+        if (!own_sums) return;
+        float* const part = p.part + ((int64_t)blockIdx.x * RPB + threadIdx.x / TPR) * K;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int64_t k = (int64_t)(t + TPR * i) * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (k + e < K) part[k + e] = gw[i][e];
+        }
+    }
+}
+
+// The weights' gradient of rows too long for registers: 256 columns per workgroup, a part of the rows.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_weights_kernel(NormBackward p, int64_t rows)
+{
+    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, m1 = min(p.M, (int64_t)(blockIdx.y + 1) * rows);
+    if (k >= p.K) return;
+    float sum = 0.0f;
+    for (int64_t m = (int64_t)blockIdx.y * rows; m < m1; ++m)
+        sum = fmaf((float)static_cast<const T*>(p.gy)[m * p.ld_gy + k] * (float)static_cast<const T*>(p.sum)[m * p.ld_sum + k], p.rstd[m], sum);
+    p.part[(int64_t)blockIdx.y * p.K + k] = sum;
+}
+
+constexpr int64_t kMostRowsAtOnce = (int64_t)1 << 23;
+
+// Threads per row and pieces per thread (0: two passes).
+struct Shape {
+    int tpr, ch;
+};
+Shape shape_of(int64_t M, int64_t span, int piece)
+{
+    const int64_t pieces = (span + piece - 1) / piece;
+    if (pieces <= 64 * 4 && (M >= 512 || pieces <= 64)) return Shape{64, pieces <= 64 ? 1 : pieces <= 128 ? 2 : 4};
+    return Shape{256, pieces <= 256 ? 1 : pieces <= 512 ? 2 : pieces <= 1024 ? 4 : 0};
+}
+
+// Workgroups of the backward kernel, each of which leaves a row (or four) of partial sums.
+int64_t backward_blocks(int64_t M, Shape s)
+{
+    const int64_t rows = 256 / s.tpr, all = (M + rows - 1) / rows, most = s.tpr == 64 ? 256 : 512;
+    return all < most ? all : most;
+}
+
+template <typename T, bool VEC, typename F>
+void with_shape(Shape s, F&& run)
+{
+    auto as = [](auto a, auto b) { return std::pair<decltype(a), decltype(b)>(); };
+    using std::integral_constant;
+    if (s.tpr == 64) {
+        if (s.ch == 1) run(as(integral_constant<int, 64>(), integral_constant<int, 1>()));
+        else if (s.ch == 2) run(as(integral_constant<int, 64>(), integral_constant<int, 2>()));
+        else run(as(integral_constant<int, 64>(), integral_constant<int, 4>()));
+    } else {
+        if (s.ch == 1) run(as(integral_constant<int, 256>(), integral_constant<int, 1>()));
+        else if (s.ch == 2) run(as(integral_constant<int, 256>(), integral_constant<int, 2>()));
+        else if (s.ch == 4) run(as(integral_constant<int, 256>(), integral_constant<int, 4>()));
+        else run(as(integral_constant<int, 256>(), integral_constant<int, 0>()));
+    }
+}
+
+template <typename T, bool VEC>
+int forward(const NormArgs& p, hipStream_t s)
+{
+    const int64_t span = p.codes ? (p.code_scales ? block_padded(p.K) : padded_channels(p.K)) : p.K;
+    const Shape shape = shape_of(p.M, span, kPiece<T>);
+    const int64_t rows = 256 / shape.tpr;
+    // (a launch has fewer than 2^32 threads)
+    for (int64_t first = 0; first < p.M; first += kMostRowsAtOnce) {
+        NormArgs q = p;
+        q.first = first;
+        const dim3 grid((unsigned)(((p.M - first < kMostRowsAtOnce ? p.M - first : kMostRowsAtOnce) + rows - 1) / rows));
+        with_shape<T, VEC>(shape, [&](auto c) {
+            norm_kernel<T, VEC, decltype(c.first)::value, decltype(c.second)::value><<<grid, dim3(256), 0, s>>>(q);
+        });
+        if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
+    }
+    return FPQ_OK;
+}
+
+template <typename T, bool VEC>
+int backward(const NormBackward& p, hipStream_t s)
+{
+    if (p.M == 0) return p.gw ? launch_part_sums(p.part, 0, p.K, p.gw, s) : FPQ_OK;
+    const Shape shape = shape_of(p.M, p.K, kPiece<T>);
+    const int64_t blocks = backward_blocks(p.M, shape);
+    const bool own = p.gw && shape.ch;
+    if (p.gx || own)
+        with_shape<T, VEC>(shape, [&](auto c) {
+            norm_backward_kernel<T, VEC, decltype(c.first)::value, decltype(c.second)::value><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(p, own);
+        });
+    if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
+    if (!p.gw) return FPQ_OK;
+    if (own) return launch_part_sums(p.part, (int)(blocks * (256 / shape.tpr)), p.K, p.gw, s);
+    const RowParts r = row_parts(p.M, p.K);
+    norm_weights_kernel<T><<<dim3((unsigned)((p.K + 255) / 256), (unsigned)r.parts), dim3(256), 0, s>>>(p, r.rows);
+    if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
+    return launch_part_sums(p.part, r.parts, p.K, p.gw, s);
+}
+
+}  // namespace
+
+size_t norm_part_bytes(int64_t M, int64_t K)
+{
+    size_t most = row_parts_bytes(M, K);
+    for (int piece : {4, 8}) {
+        const Shape s = shape_of(M, K, piece);
+        const size_t n = (size_t)backward_blocks(M, s) * (256 / s.tpr) * K * 4;
+        if (s.ch && n > most) most = n;
+    }
+    return most;
+}
+
+int launch_norm(const NormArgs& p, int type, hipStream_t s)
+{
+    if (type == FPQ_TYPE_FP32) return p.vec ? forward<float, true>(p, s) : forward<float, false>(p, s);
+    return p.vec ? forward<__bf16, true>(p, s) : forward<__bf16, false>(p, s);
+}
+
+int launch_norm_backward(const NormBackward& p, int type, hipStream_t s)
+{
+    if (type == FPQ_TYPE_FP32) return p.vec ? backward<float, true>(p, s) : backward<float, false>(p, s);
+    return p.vec ? backward<__bf16, true>(p, s) : backward<__bf16, false>(p, s);
+}
+
+}  // namespace fpq

@@ -559,6 +559,215 @@ int do_adamw_step(Args& A)
     return invoke(A, fn, A.p(0), A.l(1), A.real(2), A.real(3), A.real(4), A.real(5), A.real(6), A.l(7), scale, A.stream());
 }
 
+// ---- blocks, linear layers, gated projections, norm
+
+constexpr int64_t kBlock = 32;
+int64_t padded_to(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// A matrix of `rows` x `cols` (negative: any; they receive its own) and of `type` (negative: either), or None where that is allowed: its row stride
+int64_t matrix(Args& A, int k, int64_t& rows, int64_t& cols, int& type, const char* name, bool optional = false)
+{
+    if (A.bad || (optional && A.a[k] == Py_None)) return 0;
+    if (A.a[k] == Py_None) {
+        PyErr_Format(PyExc_TypeError, "%s: a tensor expected", name);
+        A.bad = true;
+        return 0;
+    }
+    int64_t n[2] = {}, s[2] = {};
+    A.layout(k, 2, n, s, name);
+    const int t = A.type(k, name);
+    if (A.bad) return 0;
+    if (rows < 0) rows = n[0];
+    if (cols < 0) cols = n[1];
+    if (type < 0) type = t;
+    if (n[0] != rows || n[1] != cols || t != type) {
+        PyErr_Format(PyExc_ValueError, "%s: %lld rows of %lld elements and one type expected", name, (long long)rows, (long long)cols);
+        A.bad = true;
+    }
+    return s[0];
+}
+// Contiguous bytes (codes, scales, masks), or None where that is allowed
+uint8_t* bytes_of(Args& A, int k, int64_t n, const char* name, bool optional = false)
+{
+    if (A.bad || (optional && A.a[k] == Py_None)) return nullptr;
+    if (A.a[k] == Py_None || A.method(A.a[k], s_numel) != (size_t)n || A.method(A.a[k], s_element_size) != 1) {
+        if (!A.bad) PyErr_Format(PyExc_ValueError, "%s: %lld bytes expected", name, (long long)n);
+        A.bad = true;
+        return nullptr;
+    }
+    PyObject* c = PyObject_CallMethodNoArgs(A.a[k], s_is_contiguous);
+    if (!c || c != Py_True) {
+        if (c) PyErr_Format(PyExc_ValueError, "%s: not contiguous", name);
+        A.bad = true;
+    }
+    Py_XDECREF(c);
+    return A.bp(k);
+}
+int do_block_quantize(Args& A)
+{
+    FN(fpq_block_quantize);
+    int64_t M = -1, K = -1;
+    int type = -1;
+    const int64_t ld = matrix(A, 0, M, K, type, "x");
+    const fpq_format_t f = A.fmt(1);
+    const int64_t codes = padded_to(K, kBlock) / (1 + f.ebits + f.mbits <= 4 ? 2 : 1);
+    const uint8_t* const mask = bytes_of(A, 2, M * K, "mask", true);
+    uint8_t *const to = bytes_of(A, 3, M * codes, "codes"), *const scales = bytes_of(A, 4, M * (padded_to(K, kBlock) / kBlock), "scales");
+    return invoke(A, fn, A.p(0), type, M, K, ld, f, mask, to, scales, A.stream());
+}
+int do_block_dequantize(Args& A)
+{
+    FN(fpq_block_dequantize);
+    int64_t M = -1, K = -1;
+    int type = -1;
+    const int64_t ld = matrix(A, 3, M, K, type, "out");
+    const fpq_format_t f = A.fmt(2);
+    const int64_t codes = padded_to(K, kBlock) / (1 + f.ebits + f.mbits <= 4 ? 2 : 1);
+    const uint8_t *const from = bytes_of(A, 0, M * codes, "codes"), *const scales = bytes_of(A, 1, M * (padded_to(K, kBlock) / kBlock), "scales");
+    return invoke(A, fn, from, scales, M, K, f, A.p(3), type, ld, A.stream());
+}
+int do_block_linear(Args& A)
+{
+    FN(fpq_block_linear);
+    fpq_linear_args_t r;
+    memset(&r, 0, sizeof r);
+    r.M = r.N = r.K = -1;
+    int type = -1;
+    r.ld_x = matrix(A, 0, r.M, r.K, type, "x");
+    r.ld_y = matrix(A, 4, r.M, r.N, type, "y");
+    r.type = type;
+    const uint8_t *const codes = bytes_of(A, 1, r.N * (padded_to(r.K, kBlock) / 2), "codes"), *const scales = bytes_of(A, 2, r.N * (padded_to(r.K, kBlock) / kBlock), "scales");
+    const float* const bias = A.words<const float>(3, r.N, "bias");
+    return invoke(A, fn, &r, A.p(0), codes, scales, bias, A.p(4), A.p(5), A.bytes(5), A.stream());
+}
+// x of a backward call: a matrix [M, K], or its blocks where the scales (the argument behind it) are given; None where no gradient needs it
+int64_t kept_rows(Args& A, int k, int64_t& M, int64_t& K, int& type)
+{
+    if (A.bad || A.a[k] == Py_None) return 0;
+    if (A.a[k + 1] == Py_None) return matrix(A, k, M, K, type, "x");
+    bytes_of(A, k, M * padded_to(K, kBlock), "x: codes");
+    bytes_of(A, k + 1, M * (padded_to(K, kBlock) / kBlock), "x_scales");
+    return 0;
+}
+int do_linear_backward(Args& A)
+{
+    FN(fpq_linear_backward);
+    fpq_linear_args_t r;
+    memset(&r, 0, sizeof r);
+    r.M = r.N = r.K = -1;
+    int type = -1;
+    r.ld_grad_y = matrix(A, 3, r.M, r.N, type, "grad_y");
+    r.ld_w = matrix(A, 2, r.N, r.K, type, "w");
+    r.ld_x = kept_rows(A, 0, r.M, r.K, type);
+    r.ld_grad_x = matrix(A, 4, r.M, r.K, type, "grad_x", true);
+    r.ld_grad_w = matrix(A, 5, r.N, r.K, type, "grad_w", true);
+    r.type = type;
+    float* const gb = A.words<float>(6, r.N, "grad_bias");
+    return invoke(A, fn, &r, A.p(0), (const uint8_t*)A.bp(1), A.p(2), A.p(3), A.p(4), A.p(5), gb, A.p(7), A.bytes(7), A.stream());
+}
+// What the forward pass keeps: [M, 2 N] of the type, contiguous, or blocks
+void kept_pre(Args& A, int k, int64_t M, int64_t N, int type)
+{
+    if (A.bad || A.a[k] == Py_None) return;
+    if (A.a[k + 1] != Py_None) {
+        bytes_of(A, k, M * 2 * padded_to(N, kBlock), "pre: codes");
+        bytes_of(A, k + 1, M * 2 * (padded_to(N, kBlock) / kBlock), "pre_scales");
+        return;
+    }
+    int64_t cols = 2 * N;
+    const int64_t ld = matrix(A, k, M, cols, type, "pre");
+    A.same(M <= 1 || ld == cols, "pre: not contiguous");
+}
+int do_gated(Args& A)
+{
+    FN(fpq_gated);
+    fpq_gated_args_t r;
+    memset(&r, 0, sizeof r);
+    r.M = r.N = r.K = -1;
+    int type = -1;
+    r.ld_x = matrix(A, 0, r.M, r.K, type, "x");
+    r.ld_h = matrix(A, 4, r.M, r.N, type, "h");
+    int64_t rows = 2 * r.N;
+    r.ld_w = matrix(A, 1, rows, r.K, type, "w");
+    r.type = type;
+    r.act = A.i(3);
+    const float* const bias = A.words<const float>(2, 2 * r.N, "bias");
+    kept_pre(A, 5, r.M, r.N, type);
+    return invoke(A, fn, &r, A.p(0), A.p(1), bias, A.p(4), A.p(5), A.bp(6), A.p(7), A.bytes(7), A.stream());
+}
+int do_gated_backward(Args& A)
+{
+    FN(fpq_gated_backward);
+    fpq_gated_args_t r;
+    memset(&r, 0, sizeof r);
+    r.M = r.N = r.K = -1;
+    int type = -1;
+    r.ld_grad_h = matrix(A, 6, r.M, r.N, type, "grad_h");
+    int64_t rows = 2 * r.N;
+    r.ld_w = matrix(A, 2, rows, r.K, type, "w");
+    r.ld_x = kept_rows(A, 0, r.M, r.K, type);
+    r.ld_grad_x = matrix(A, 7, r.M, r.K, type, "grad_x", true);
+    r.ld_grad_w = matrix(A, 8, rows, r.K, type, "grad_w", true);
+    r.type = type;
+    r.act = A.i(5);
+    if (!A.bad && A.a[3] == Py_None) {
+        PyErr_SetString(PyExc_TypeError, "pre: a tensor expected");
+        A.bad = true;
+    }
+    kept_pre(A, 3, r.M, r.N, type);
+    float* const gb = A.words<float>(9, 2 * r.N, "grad_bias");
+    return invoke(A, fn, &r, A.p(0), (const uint8_t*)A.bp(1), A.p(2), A.p(3), (const uint8_t*)A.bp(4), A.p(6), A.p(7), A.p(8), gb, A.p(10), A.bytes(10), A.stream());
+}
+int do_rms_norm(Args& A)
+{
+    FN(fpq_rms_norm);
+    fpq_norm_args_t r;
+    memset(&r, 0, sizeof r);
+    r.M = r.K = -1;
+    int type = -1;
+    r.ld_x = matrix(A, 0, r.M, r.K, type, "x");
+    r.ld_residual = matrix(A, 1, r.M, r.K, type, "residual", true);
+    r.ld_sum = matrix(A, 4, r.M, r.K, type, "sum", true);
+    r.ld_y = matrix(A, 5, r.M, r.K, type, "y", true);
+    r.type = type;
+    r.eps = A.f(3);
+    const float* const w = A.words<const float>(2, r.K, "w");
+    float* const rstd = A.words<float>(6, r.M, "rstd");
+    fpq_format_t f;
+    memset(&f, 0, sizeof f);
+    uint8_t *codes = nullptr, *scales = nullptr;
+    float scale = 0.0f;
+    const float* dev = nullptr;
+    if (A.a[7] != Py_None) {
+        const bool blocks = A.a[11] != Py_None;
+        codes = bytes_of(A, 7, r.M * padded_to(r.K, blocks ? kBlock : 16), "codes");
+        if (blocks) {
+            scales = bytes_of(A, 11, r.M * (padded_to(r.K, kBlock) / kBlock), "code_scales");
+        } else {
+            f = A.fmt(8);
+            scale = A.a[9] == Py_None ? 0.0f : A.f(9);
+            dev = A.words<const float>(10, 1, "scale_dev");
+        }
+    }
+    return invoke(A, fn, &r, A.p(0), A.p(1), w, A.p(4), A.p(5), rstd, codes, f, scale, dev, scales, A.stream());
+}
+int do_rms_norm_backward(Args& A)
+{
+    FN(fpq_rms_norm_backward);
+    fpq_norm_args_t r;
+    memset(&r, 0, sizeof r);
+    r.M = r.K = -1;
+    int type = -1;
+    r.ld_sum = matrix(A, 0, r.M, r.K, type, "sum");
+    r.ld_grad_y = matrix(A, 3, r.M, r.K, type, "grad_y");
+    r.ld_grad_sum = matrix(A, 4, r.M, r.K, type, "grad_sum", true);
+    r.ld_grad_x = matrix(A, 5, r.M, r.K, type, "grad_x", true);
+    r.type = type;
+    const float *const w = A.words<const float>(1, r.K, "w"), *const rstd = A.words<const float>(2, r.M, "rstd");
+    float* const gw = A.words<float>(6, r.K, "grad_w");
+    return invoke(A, fn, &r, A.p(0), w, rstd, A.p(3), A.p(4), A.p(5), gw, A.p(7), A.bytes(7), A.stream());
+}
+
 // ---- names, parameters and defaults
 
 enum { kMaxParams = 26 };
@@ -597,6 +806,14 @@ Entry g_entries[] = {
     {"fpq_adapter_backward", do_adapter_backward,
      "x a b scaling row_start adapter t grad_y grad_x_base grad_x grad_a grad_b workspace", 12},
     {"fpq_adamw_step", do_adamw_step, "plan pieces lr beta1 beta2 eps weight_decay step grad_scale", 8},
+    {"fpq_block_quantize", do_block_quantize, "x f mask codes scales", 5},
+    {"fpq_block_dequantize", do_block_dequantize, "codes scales f out", 4},
+    {"fpq_block_linear", do_block_linear, "x codes scales bias y workspace", 5},
+    {"fpq_linear_backward", do_linear_backward, "x x_scales w grad_y grad_x grad_w grad_bias workspace", 7},
+    {"fpq_gated", do_gated, "x w bias act h pre pre_scales workspace", 5},
+    {"fpq_gated_backward", do_gated_backward, "x x_scales w pre pre_scales act grad_h grad_x grad_w grad_bias workspace", 10},
+    {"fpq_rms_norm", do_rms_norm, "x residual w eps sum y rstd codes f scale scale_dev code_scales", 6},
+    {"fpq_rms_norm_backward", do_rms_norm_backward, "sum w rstd grad_y grad_sum grad_x grad_w workspace", 7},
 };
 constexpr int kEntries = sizeof g_entries / sizeof g_entries[0];
 

@@ -1,0 +1,214 @@
+"""Blocks of 8-bit and 4-bit codes against the oracle: codes and scales bit for bit, layers on 4-bit blocks and the gradients of linear layers
+within the bounds that their roundings give."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks
+from paper_2408_06995_amd import binding as B
+from gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+E4M3, E2M1 = (4, 3, 7, 448.0), (2, 1, 1, 6.0)
+
+
+def room(n):
+    return torch.empty(max(int(n), 16), dtype=torch.uint8, device=DEV)
+
+
+def nan(*shape, t=torch.float32):
+    return torch.full(shape, float("nan"), dtype=t, device=DEV)
+
+
+def host(x):
+    return x.detach().double().cpu().numpy()
+
+
+def within(name, got, want, off):
+    err = np.abs(host(got) - want)
+    bad = ~(err <= off)
+    assert not bad.any(), "%s: %d of %d outside, worst %.3g of the bound" % (name, bad.sum(), bad.size, np.nanmax(err / (off + 1e-300)))
+
+
+def rows(g, M, K, t, ld=None):
+    """[M, K] on the GPU, of a wider matrix if `ld`; NaN behind the rows."""
+    x = torch.full((M, ld or K), float("nan"))
+    x[:, :K] = torch.randn(M, K, generator=g) * torch.exp(torch.randn(M, 1, generator=g))
+    return x.to(t).to(DEV)[:, :K]
+
+
+def quantize(x, f, mask=None):
+    M, K = x.shape
+    bits = 8 if f is E4M3 else 4
+    codes, scales = room(M * blocks.padded(K) * bits // 8)[:M * blocks.padded(K) * bits // 8], room(M * blocks.padded(K) // 32)[:M * blocks.padded(K) // 32]
+    codes, scales = codes.fill_(0xee).view(M, -1), scales.fill_(0xee).view(M, -1)
+    B.fpq_block_quantize(x, f, mask, codes, scales)
+    return codes, scales
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("f", [E4M3, E2M1], ids=["e4m3", "e2m1"])
+@pytest.mark.parametrize("M,K,ld", [(1, 1, None), (1, 32, None), (3, 33, None), (5, 320, None), (64, 1280, 1288), (7, 77, 83), (129, 1000, 1001), (2, 8192, None)])
+def test_codes(M, K, ld, f, t):
+    print(M, K, ld, f, t, flush=True)
+    g = torch.Generator().manual_seed(M + K)
+    x = rows(g, M, K, TYPES[t], ld)
+    if K > 64:
+        x[0, :32] = 0
+        x[M - 1, 40] = 1e-38
+    bits = 8 if f is E4M3 else 4
+    for mask in [None] if bits == 8 else [None, torch.randint(0, 2, (M, K), generator=g, dtype=torch.uint8)]:
+        codes, scales = quantize(x, f, None if mask is None else mask.to(DEV))
+        want, s = blocks.block_quantize(host(x), bits, None if mask is None else mask.numpy())
+        got = codes.cpu().numpy()
+        assert np.array_equal(scales.cpu().numpy(), s)
+        assert np.array_equal(got if bits == 8 else blocks.unpack(got), want)
+        for to in (torch.float32, torch.bfloat16):
+            out = nan(M, K + 3, t=to)
+            B.fpq_block_dequantize(codes, scales, f, out[:, :K])
+            v = torch.from_numpy(blocks.block_values(want, s, bits, K)).to(to)
+            assert torch.equal(out[:, :K].cpu(), v) and out[:, K:].isnan().all()
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("f", [E4M3, E2M1], ids=["e4m3", "e2m1"])
+def test_special_values(f, t):
+    """Ends of the range, ties, subnormals, values next to a power of two; infinities and NaN make their block NaN and no other."""
+    bits = 8 if f is E4M3 else 4
+    x = torch.zeros(12, 64, dtype=TYPES[t])
+    x[0, 0], x[0, 33] = float("inf"), 3.0
+    x[1, 31], x[1, 40] = float("nan"), -2.0
+    x[2, 5] = -float("inf")
+    x[3, :4] = torch.tensor([3e38, -3e38, 1.0, 1e30])
+    x[4, :4] = torch.tensor([1e-38, -1e-38, 1e-39, 0.0])
+    x[5, :8] = torch.tensor([448.0, 449.0 if t == "fp32" else 450.0, 1.75, 1.875, 2.0, -0.0, 6.0, 6.03125])
+    x[6, :3] = torch.tensor([1.0, 2.0 ** -9, 2.0 ** -10])
+    x[7, 0] = 1.75
+    x[8, 0] = 1.7578125
+    x[9, 0] = 1.5
+    x[10, 0] = 1.5078125
+    x[11, :32] = torch.linspace(-1, 1, 32).to(TYPES[t])
+    codes, scales = quantize(x.to(DEV), f)
+    want, s = blocks.block_quantize(x.double().numpy(), bits)
+    assert np.array_equal(scales.cpu().numpy(), s)
+    out = nan(12, 64)
+    B.fpq_block_dequantize(codes, scales, f, out)
+    v = blocks.block_values(want, s, bits, 64)
+    v[np.repeat(s == 255, 32, 1)] = np.nan
+    # 3e38 = 3.53 2^126 rounds to 4 2^126 = 2^128 in E2M1, which is infinity in fp32
+    with np.errstate(over="ignore"):
+        v = v.astype(np.float32)
+    assert np.array_equal(host(out), v, equal_nan=True)
+
+
+def linear_case(M, N, K, t, kept, ld=0, seed=1):
+    g = torch.Generator().manual_seed(seed)
+    t = TYPES[t]
+    x, gy = rows(g, M, K, t, ld and K + ld), rows(g, M, N, t, ld and N + ld)
+    w = (rows(g, N, K, torch.float32) * K ** -0.5).to(t)
+    if ld:
+        w = torch.nn.functional.pad(w, (0, ld), value=float("nan"))[:, :K]
+    if kept:
+        kept = quantize(x, E4M3)
+        x = kept[0]
+    return x, kept[1] if kept else None, w, gy
+
+
+def check_linear(M, N, K, t, kept, ld=0, seed=1):
+    x, scales, w, gy = linear_case(M, N, K, t, kept, ld, seed)
+    gx, gw, gb = nan(M, K + ld, t=TYPES[t])[:, :K], nan(N, K + ld, t=TYPES[t])[:, :K], nan(N)
+    B.fpq_linear_backward(x, scales, w, gy, gx, gw, gb, room(B.fpq_linear_backward_workspace_size(M, N, K, int(t == "bf16"))))
+    xv = blocks.block_values(x.cpu().numpy(), scales.cpu().numpy(), 8, K) if kept else host(x)
+    (wx, ox), (ww, ow), (wb, ob) = blocks.linear_backward(xv, host(w), host(gy), t == "bf16")
+    within("grad_x", gx, wx, ox)
+    within("grad_w", gw, ww, ow)
+    within("grad_bias", gb, wb, ob)
+    return x, scales, w, gy, gx, gw, gb
+
+
+@pytest.mark.parametrize("kept", [False, True], ids=["x", "blocks"])
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 320, 64), (2, 8, 40), (33, 130, 257), (64, 64, 64), (65, 128, 72), (300, 960, 320), (129, 257, 1000), (1500, 40, 24),
+                                   (5003, 64, 128)])
+def test_linear_gradients(M, N, K, t, kept):
+    print(M, N, K, t, kept, flush=True)
+    check_linear(M, N, K, t, kept)
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("ld", [8, 3])
+def test_linear_gradients_of_strided_rows(ld, t):
+    check_linear(130, 136, 72, t, False, ld)
+    check_linear(77, 61, 131, t, False, ld)
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+def test_linear_gradients_in_large_tiles(t):
+    check_linear(3600, 3700, 72, t, True)            # 256 x 256 tiles in grad_w, many k in grad_x
+    check_linear(4000, 136, 3700, t, False)          # 256 x 256 tiles in grad_x
+
+
+def test_gradients_one_by_one_and_of_no_rows():
+    x, scales, w, gy, gx, gw, gb = check_linear(70, 48, 96, "bf16", True)
+    ws = room(B.fpq_linear_backward_workspace_size(70, 48, 96, 1))
+    for which in range(3):
+        out = [nan(70, 96, t=torch.bfloat16), nan(48, 96, t=torch.bfloat16), nan(48)]
+        some = [o if i == which else None for i, o in enumerate(out)]
+        B.fpq_linear_backward(x if which == 1 else None, scales if which == 1 else None, w, gy, *some, ws)
+        assert torch.equal(out[which], (gx, gw, gb)[which])
+    for t in TYPES.values():
+        gw, gb = nan(48, 96, t=t), nan(48)
+        e = torch.empty(0, 96, dtype=t, device=DEV)
+        B.fpq_linear_backward(e, None, w.to(t), torch.empty(0, 48, dtype=t, device=DEV), e, gw, gb, ws)
+        assert not gw.any() and not gb.any()
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K,ld", [(1, 1, 1, 0), (1, 320, 64, 0), (1, 1000, 4096, 0), (2, 77, 33, 0), (5, 640, 320, 0), (8, 48, 1280, 8), (15, 130, 97, 3), (16, 1280, 640, 0),
+                                      (17, 1280, 640, 0), (33, 64, 31, 0), (200, 320, 768, 0), (129, 250, 1001, 5)])
+def test_layers_on_4_bit_blocks(M, N, K, ld, t):
+    print(M, N, K, ld, t, flush=True)
+    g = torch.Generator().manual_seed(M + N + K)
+    t_ = TYPES[t]
+    x, w, bias = rows(g, M, K, t_, ld and K + ld), rows(g, N, K, torch.float32), torch.randn(N, generator=g).to(DEV)
+    codes, scales = quantize(w, E2M1)
+    wv = blocks.block_values(blocks.unpack(codes.cpu().numpy()), scales.cpu().numpy(), 4, K)
+    ws = room(B.fpq_block_linear_workspace_size(M, N, K, int(t == "bf16")))
+    for b in (bias, None):
+        y = nan(M, N + ld, t=t_)
+        B.fpq_block_linear(x, codes, scales, b, y[:, :N], ws)
+        within("y", y[:, :N], *blocks.block_linear(host(x), wv, None if b is None else host(b), t == "bf16"))
+        assert y[:, N:].isnan().all()
+
+
+def test_rows_do_not_depend_on_each_other():
+    """A row's bits are the same alone and among others of the same kernel, and NaN stays in its row."""
+    g = torch.Generator().manual_seed(2)
+    w = rows(g, 640, 320, torch.float32)
+    codes, scales = quantize(w, E2M1)
+    x = rows(g, 16, 320, torch.bfloat16)
+    y, z = nan(16, 640, t=torch.bfloat16), nan(16, 640, t=torch.bfloat16)
+    ws = room(B.fpq_block_linear_workspace_size(16, 640, 320, 1))
+    B.fpq_block_linear(x, codes, scales, None, y, ws)
+    x2 = x.clone()
+    x2[3, 7], x2[5, 0] = float("nan"), float("inf")
+    B.fpq_block_linear(x2, codes, scales, None, z, ws)
+    keep = [m for m in range(16) if m not in (3, 5)]
+    assert torch.equal(y[keep], z[keep]) and z[3].isnan().all() and not z[5].isfinite().any()
+    one = nan(1, 640, t=torch.bfloat16)
+    B.fpq_block_linear(x[4:5], codes, scales, None, one, ws)
+    assert torch.equal(one, y[4:5])
+
+
+def test_layers_on_nan_blocks():
+    """A block whose scale is 255 makes its output column NaN, for few rows and for many."""
+    g = torch.Generator().manual_seed(4)
+    codes, scales = quantize(rows(g, 64, 96, torch.float32), E2M1)
+    scales[9, 1] = 255
+    for M in (1, 40):
+        for t in TYPES.values():
+            y = nan(M, 64, t=t).zero_()
+            B.fpq_block_linear(rows(g, M, 96, t), codes, scales, None, y, room(B.fpq_block_linear_workspace_size(M, 64, 96, int(t == torch.bfloat16))))
+            assert y[:, 9].isnan().all() and y[:, :9].isfinite().all() and y[:, 10:].isfinite().all()
