@@ -591,8 +591,8 @@ int fpq_adamw_step(const void *plan, int64_t pieces, double lr, double beta1, do
  *   activations (E4M3) and for weights (E2M1; once, when they are loaded).
  * fpq_block_dequantize: out [M, K] of out_type; exact, but that bf16 rounds magnitudes below 2^-126.
  * fpq_block_linear: y [M, N] = x W^T (+ bias) with W [N, K] as E2M1 blocks.  x and y of args->type; bias fp32 [N] or NULL.  Products with bf16 x
- *   are exact, an fp32 x is split into three bf16 parts as in FPQ_TYPE_FP32 attention; sums are fp32.  Up to 16 rows (a token of each
- *   request) are bound by the codes read; more are computed with the codes expanded once to bf16 in the workspace.
+ *   are exact, an fp32 x is split into three bf16 parts as in FPQ_TYPE_FP32 attention; sums are fp32.  Up to 64 rows (a token of each
+ *   request) are bound by the codes read and need no workspace; more are computed with the codes expanded once to bf16 in it.
  * fpq_linear_backward: the gradients of a linear layer y = x W^T (+ bias) for grad_y [M, N]: grad_x [M, K] = grad_y W, grad_w [N, K] =
  *   grad_y^T x, of args->type, grad_bias fp32 [N] the sum of its rows.  Each of them may be NULL and is then not computed; w is needed for
  *   grad_x, x for grad_w.  x is [M, K] of the type with stride ld_x, or, with x_scales not NULL, the E4M3 blocks that were kept of it.

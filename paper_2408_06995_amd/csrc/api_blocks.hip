@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include "blocks.h"
+#include "rows.h"
 
 using namespace fpq;
 
@@ -143,6 +144,26 @@ int check_gradients(int type, int64_t M, int64_t N, int64_t K, const void* x, co
     return FPQ_OK;
 }
 
+RowsArgs rows_args(const void* x, int type, int64_t M, int64_t N, int64_t K, int64_t ld_x, const float* bias)
+{
+    RowsArgs r{};
+    r.x = x;
+    r.ld_x = stride(ld_x, K, M);
+    r.M = (int)M;
+    r.N = (int)N;
+    r.K = (int)K;
+    r.bias = bias;
+    r.f32 = type == FPQ_TYPE_FP32;
+    r.vec_x = aligned(x, 16) && K % 8 == 0 && r.ld_x * size_of(type) % 16 == 0;
+    return r;
+}
+
+// Whether the form of few rows takes gated projections: weights read where they are.
+bool few_rows(const fpq_gated_args_t* p, const void* w)
+{
+    return p->M <= kFewRows && aligned(w, 16) && p->K % 8 == 0 && p->ld_w * size_of(p->type) % 16 == 0;
+}
+
 bool norm_vec(const void* p, int64_t ld, int64_t M, int64_t K, size_t size)
 {
     return !p || (aligned(p, 16) && K * size % 16 == 0 && (M <= 1 || ld * size % 16 == 0));
@@ -192,7 +213,7 @@ int fpq_block_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M,
 
 size_t fpq_block_linear_workspace_size(int64_t M, int64_t N, int64_t K, int type)
 {
-    if (!type_ok(type) || check_sizes(M, N, K) != FPQ_OK || M == 0) return 0;
+    if (!type_ok(type) || check_sizes(M, N, K) != FPQ_OK || M <= kFewRows) return 0;
     return planes_bytes(M, K, type) + blocks_bytes(N, K) + align_up(product_part_bytes(M, N, K, planes_of(type), 1, false, false));
 }
 
@@ -210,6 +231,17 @@ int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* c
     if (!aligned(x, size) || !aligned(y, size) || !aligned(codes, 16) || !aligned(bias, 4)) return FPQ_ERR_ALIGN;
     if (workspace_bad(workspace, workspace_bytes, fpq_block_linear_workspace_size(p->M, p->N, p->K, p->type), &st)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (p->M <= kFewRows) {
+        RowsArgs r = rows_args(x, p->type, p->M, p->N, p->K, p->ld_x, bias);
+        const int64_t kp = block_padded(p->K);
+        r.w = codes;
+        r.ld_w = kp / 2;
+        r.scales = scales;
+        r.ld_s = kp / kBlock;
+        r.out = y;
+        r.ld_out = stride(p->ld_y, p->N, p->M);
+        return p->M <= 4 && token_blocks_lds(p->M, p->K, r.f32) <= 65536 ? launch_token_blocks(r, s) : launch_rows_blocks(r, s);
+    }
     Room room{static_cast<char*>(workspace)};
     Product q{};
     st = operand(x, p->type, p->M, p->K, p->ld_x, room, q.a, s);
@@ -286,6 +318,13 @@ int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const flo
     if (!aligned(x, size) || !aligned(w, size) || !aligned(h, size) || !aligned(pre, pre_scales ? 16 : size) || !aligned(bias, 4)) return FPQ_ERR_ALIGN;
     if (workspace_bad(workspace, workspace_bytes, fpq_gated_workspace_size(M, N, K, p->type), &st)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (few_rows(p, w)) {
+        RowsArgs r = rows_args(x, p->type, M, N, K, p->ld_x, bias);
+        r.w = w;
+        r.ld_w = p->ld_w;
+        r.gate = Gate{p->act, h, stride(p->ld_h, N, M), pre, 2 * N, pre_scales};
+        return launch_rows_gated(r, s);
+    }
     Room room{static_cast<char*>(workspace)};
     Product q{};
     st = operand(x, p->type, M, K, p->ld_x, room, q.a, s);

@@ -50,8 +50,9 @@ def test_block_linear_refusals():
         assert f(**{kw: None}) == -1
     for kw in (dict(x=ODD), dict(y=ODD), dict(codes=C.c_void_p(4104)), dict(bias=C.c_void_p(4098))):
         assert f(**kw) == -5, kw
-    need = L.fpq_block_linear_workspace_size(20, 48, 40, 1)
-    assert need > 0 and f(ws=None) == -6 and f(n=need - 1) == -6 and f(ws=C.c_void_p(4104)) == -5
+    need, many = L.fpq_block_linear_workspace_size(200, 48, 40, 1), linear(M=200)
+    assert need > 0 and f(many, ws=None) == -6 and f(many, n=need - 1) == -6 and f(many, ws=C.c_void_p(4104)) == -5
+    assert L.fpq_block_linear_workspace_size(64, 48, 40, 1) == 0
     assert f(linear(M=0), x=None, ws=None, n=0) == 0
     for bad in ((-1, 48, 40, 1), (20, 0, 40, 1), (20, 48, 40, 2), (20, 48, 1 << 21, 1)):
         assert L.fpq_block_linear_workspace_size(*bad) == 0 and L.fpq_linear_backward_workspace_size(*bad) == 0 and L.fpq_gated_workspace_size(*bad) == 0

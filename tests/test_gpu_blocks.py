@@ -166,8 +166,8 @@ def test_gradients_one_by_one_and_of_no_rows():
 
 
 @pytest.mark.parametrize("t", ["fp32", "bf16"])
-@pytest.mark.parametrize("M,N,K,ld", [(1, 1, 1, 0), (1, 320, 64, 0), (1, 1000, 4096, 0), (2, 77, 33, 0), (5, 640, 320, 0), (8, 48, 1280, 8), (15, 130, 97, 3), (16, 1280, 640, 0),
-                                      (17, 1280, 640, 0), (33, 64, 31, 0), (200, 320, 768, 0), (129, 250, 1001, 5)])
+@pytest.mark.parametrize("M,N,K,ld", [(1, 1, 1, 0), (1, 320, 64, 0), (1, 1000, 4096, 0), (2, 77, 33, 0), (3, 50, 2080, 0), (4, 33, 4097, 3), (4, 17, 8192, 0), (1, 20, 20000, 0), (5, 640, 320, 0), (8, 48, 1280, 8), (15, 130, 97, 3), (16, 1280, 640, 0),
+                                      (17, 1280, 640, 0), (31, 130, 97, 3), (33, 64, 31, 0), (64, 20000, 64, 0), (65, 320, 768, 0), (7, 16400, 320, 0), (200, 320, 768, 0), (129, 250, 1001, 5)])
 def test_layers_on_4_bit_blocks(M, N, K, ld, t):
     print(M, N, K, ld, t, flush=True)
     g = torch.Generator().manual_seed(M + N + K)
@@ -197,9 +197,9 @@ def test_rows_do_not_depend_on_each_other():
     B.fpq_block_linear(x2, codes, scales, None, z, ws)
     keep = [m for m in range(16) if m not in (3, 5)]
     assert torch.equal(y[keep], z[keep]) and z[3].isnan().all() and not z[5].isfinite().any()
-    one = nan(1, 640, t=torch.bfloat16)
-    B.fpq_block_linear(x[4:5], codes, scales, None, one, ws)
-    assert torch.equal(one, y[4:5])
+    some = nan(6, 640, t=torch.bfloat16)
+    B.fpq_block_linear(x[4:10], codes, scales, None, some, ws)
+    assert torch.equal(some, y[4:10])
 
 
 def test_layers_on_nan_blocks():
@@ -207,7 +207,7 @@ def test_layers_on_nan_blocks():
     g = torch.Generator().manual_seed(4)
     codes, scales = quantize(rows(g, 64, 96, torch.float32), E2M1)
     scales[9, 1] = 255
-    for M in (1, 40):
+    for M in (1, 40, 100):
         for t in TYPES.values():
             y = nan(M, 64, t=t).zero_()
             B.fpq_block_linear(rows(g, M, 96, t), codes, scales, None, y, room(B.fpq_block_linear_workspace_size(M, 64, 96, int(t == torch.bfloat16))))

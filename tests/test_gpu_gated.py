@@ -86,7 +86,7 @@ class Call:
 
 @pytest.mark.parametrize("keep", ["type", "blocks"])
 @pytest.mark.parametrize("t", ["fp32", "bf16"])
-@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 320, 64), (2, 33, 40), (16, 1280, 320), (17, 64, 1288), (33, 130, 257), (64, 32, 64), (65, 100, 72), (300, 480, 320), (129, 257, 1000),
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 320, 64), (2, 33, 40), (16, 1280, 320), (17, 64, 1288), (31, 77, 328), (50, 96, 200), (33, 130, 257), (64, 32, 64), (65, 100, 72), (300, 480, 320), (129, 257, 1000),
                                    (1500, 20, 24)])
 def test_sizes(M, N, K, t, keep):
     print(M, N, K, t, keep, flush=True)
