@@ -163,13 +163,24 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const T* x, int64_t M,
 {
     const int64_t k = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8, m1 = min(M, (int64_t)(blockIdx.y + 1) * rows);
     float sum[8] = {};
-    if (k < N)
-        for (int64_t m = (int64_t)blockIdx.y * rows + (threadIdx.x >> 6); m < m1; m += 4) {
+    int64_t m = (int64_t)blockIdx.y * rows + (threadIdx.x >> 6);
+    if (k < N) {
+        for (; m + 12 < m1; m += 16) {                               // four rows' loads at once
+            float v[4][8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load8(x + (m + 4 * i) * ld, k, N, vec, v[i]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += v[i][e];
+        }
+        for (; m < m1; m += 4) {
             float v[8];
             load8(x + m * ld, k, N, vec, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += v[e];
         }
+    }
     strip_sum(sum, k, N, part + (int64_t)blockIdx.y * N);
 }
 
@@ -180,8 +191,17 @@ __global__ __launch_bounds__(1024) void part_sums_kernel(const float* part, int 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t k = (int64_t)blockIdx.x * 64 + lane;
     float sum = 0.0f;
-    if (k < cols)
-        for (int p = wave; p < parts; p += 16) sum += part[p * cols + k];
+    if (k < cols) {
+        int p = wave;
+        for (; p + 112 < parts; p += 128) {                          // eight loads at once
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = part[(int64_t)(p + 16 * i) * cols + k];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        for (; p < parts; p += 16) sum += part[(int64_t)p * cols + k];
+    }
     room[wave][lane] = sum;
     __syncthreads();
     if (wave || k >= cols) return;
@@ -290,11 +310,11 @@ int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t
     return launched();
 }
 
-// About 1024 workgroups, of no fewer than 16 rows.
+// About 1024 workgroups, of no fewer than 16 rows, and no more parts than their sum is quick with.
 RowParts row_parts(int64_t M, int64_t cols)
 {
     const int64_t strips = (cols + kStripColumns - 1) / kStripColumns;
-    int64_t parts = 1024 / strips, most = (M + 15) / 16;
+    int64_t parts = 1024 / strips < 256 ? 1024 / strips : 256, most = (M + 15) / 16;
     parts = parts < 1 ? 1 : parts > most ? most : parts;
     if (parts < 1) parts = 1;
     const int64_t rows = (M + parts - 1) / parts;

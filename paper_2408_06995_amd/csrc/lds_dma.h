@@ -19,6 +19,15 @@ __device__ __forceinline__ void dma16(v4i rsrc, unsigned voff, unsigned lds_addr
                  : "memory");
 }
 
+// The same where the order to the program's own LDS accesses is kept by other means (barriers that clobber memory): those may be moved
+// across it.
+__device__ __forceinline__ void dma16_free(v4i rsrc, unsigned voff, unsigned lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(rsrc));
+}
+
 // The same with four bytes per lane.
 __device__ __forceinline__ void dma4(v4i rsrc, unsigned voff, unsigned lds_addr)
 {

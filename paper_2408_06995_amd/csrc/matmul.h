@@ -6,11 +6,12 @@
 // beside an operand of one plane all three).  Each operand lies either with the contraction along its rows (ROW: p[m ld + k]) or along
 // its columns (COL: p[k ld + m]), so that x W^T, g W and g^T x are one kernel without a transposed copy.
 //
-// A workgroup makes a tile of BM x BN results in steps of 64 along k; tiles go from memory to LDS directly, a step ahead, into the other
-// of two buffers.  ROW tiles are read as 16 bytes of a row, COL tiles by the transposing read, which gives a lane four k of its column;
-// both in the same order of k, eight neighbours per lane.  Places of 16 bytes are exchanged within a row so that neither read meets a
+// A workgroup makes a tile of BM x BN results in steps of 32 along k; tiles go from memory to LDS directly into a ring of stages, of which
+// all but one are on their way.  ROW tiles are read as 16 bytes of a row, COL tiles by the transposing read, which gives a lane four k of its
+// column; both in the same order of k, eight neighbours per lane.  Places of 16 bytes are exchanged within a row so that neither read meets a
 // bank twice: of a ROW tile 16 rows of one piece lie in the 16 groups of four banks, of a COL tile four rows of 64 bytes each.
-// B is the A operand of the instruction: a lane then holds four neighbouring columns n of one row m of the result.
+// B is the A operand of the instruction: a lane then holds four neighbouring columns n of one row m of the result.  Operands are read one
+// product of 16 k ahead, across the barrier too, so that the matrix unit has work while the workgroup meets.
 #pragma once
 #include "attention.h"
 #include "gemm_common.h"
@@ -37,9 +38,9 @@ struct Gate {
 struct MatmulArgs {
     Operand a, b;
     int M, N, K;                // gated: N outputs, B has 2 N rows, values first
-    int steps;                  // of 64 along K
+    int steps;                  // along K
     uint32_t order_a, order_b;  // planes of each pass, four bits each, the first pass lowest
-    int total;                  // passes x steps
+    int passes, total;          // passes x steps
     int slices;                 // of `total`
     int tiles_m, tiles_n;
     void* out;                  // kStore; slices > 1: fp32 [slice][M][N] (gated: [slice][M][2 N]) whatever the end
@@ -49,7 +50,7 @@ struct MatmulArgs {
     Gate gate;
 };
 
-constexpr int kStep = 64;
+constexpr int kStep = 32;       // k of a step, or twice as many: tiles whose rows hold whole lines of 128 bytes
 
 // Block scales: a power of two as its biased exponent; 255 stands for NaN.
 __device__ __forceinline__ float scale_of(uint32_t e) { return e ? __uint_as_float(e == 255 ? 0x7fc00000u : e << 23) : 0x1p-127f; }
@@ -96,51 +97,76 @@ __device__ __forceinline__ float gate_of(int act, float g, float* slope)
     return g * z;
 }
 
-// One operand's tile of R rows (ROW) or columns (COL) and 64 k: this thread's loads of it.
-template <bool COL, int R, int NT>
+// ROW tiles of 64 or 128 bytes a row: place c ^ row_swap holds piece c.
+template <int KS>
+__device__ __forceinline__ int row_swap(int row)
+{
+    return KS == 32 ? (row >> 2) & 3 : (row >> 1) & 7;
+}
+
+// One operand's tile of R rows (ROW) or columns (COL) and KS k: this thread's loads of it.  Every wavefront makes the same number: where
+// they do not divide, some load a piece that another one loads too.
+template <bool COL, int R, int KS, int NW>
 struct TileFeed {
-    static constexpr int CS = COL ? R / 8 : 8, N = R * 8, PT = (N + NT - 1) / NT, NW = NT / 64, BYTES = R * 128;
-    static_assert(N % 64 == 0 && (!COL || R >= 128), "whole wavefronts of loads; rows of COL tiles span all banks");
-    static __device__ __forceinline__ int swap(int row) { return COL ? (row & 3) << 2 : (row >> 1) & 7; }
+    static constexpr int CS = COL ? R / 8 : KS / 8, N = R * KS / 512, PT = (N + NW - 1) / NW;
+    static_assert(R % 32 == 0 && (!COL || R >= 128), "whole wavefronts of loads; rows of COL tiles span all banks");
+    // (COL tiles of 160 columns need no exchange: their rows are 64 bytes further round the banks each)
+    static __device__ __forceinline__ int swap(int row) { return !COL ? row_swap<KS>(row) : R % 128 == 0 ? (row & 3) << 2 : 0; }
     unsigned off[PT];
-    // `rows` (ROW) or `cols` (COL) of the tile exist
+    static __device__ __forceinline__ int place(int wave, int i)
+    {
+        const int n = wave + NW * i;
+        return N % NW != 0 && n >= N ? n % N : n;
+    }
+    // `exist` rows (ROW) or columns (COL) of the tile exist
     __device__ __forceinline__ void init(int64_t ld, int exist)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
         for (int i = 0; i < PT; ++i) {
-            const int q = (wave + NW * i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ swap(row);
+            const int q = place(wave, i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ swap(row);
             const bool in = COL ? 8 * c < exist : row < exist;
             off[i] = in ? (unsigned)row * (unsigned)(2 * ld) + 16u * c : 0x80000000u;
         }
     }
-    // Starts the loads of the tile at `base`; `left` k remain (ROW: in whole pieces), `bytes` may be read from base on.
-    __device__ __forceinline__ void load(const __bf16* base, unsigned bytes, int left, unsigned lds) const
+    uint64_t base, step;        // bytes: of the step's tile, and to the next one
+    unsigned full, row;         // bytes that may be read from base on; of a row of k (COL)
+    // The first step of a pass: the tile's first element, and what there is from it on: `rows` rows of `cols` elements of k (ROW), or `cols`
+    // columns (COL).
+    __device__ __forceinline__ void start(const __bf16* p, int64_t ld, int rows, int cols)
     {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const v4i r = make_rsrc(base, bytes);
-#pragma unroll
-        for (int i = 0; i < PT; ++i) {
-            if (N % (64 * NW) != 0 && wave + NW * i >= N / 64) break;
-            unsigned o = off[i];
-            if (!COL && left < kStep) {
-                const int q = (wave + NW * i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ swap(row);
-                if (8 * c >= left) o = 0x80000000u;
-            }
-            dma16(r, o, lds + (wave + NW * i) * 1024);
-        }
+        base = reinterpret_cast<uint64_t>(p);
+        step = COL ? (uint64_t)(2 * KS * ld) : 2 * KS;
+        full = (unsigned)(2 * ((COL ? KS - 1 : rows - 1) * ld + cols));
+        row = (unsigned)(2 * ld);
+    }
+    // Descriptor of the step's loads, of which `left` k are there; none where not `live`: then the loads write zeros.
+    __device__ __forceinline__ v4i window(int left, bool live) const
+    {
+        const unsigned n = COL ? full - (unsigned)(KS - min(left, KS)) * row : full;
+        return make_rsrc(reinterpret_cast<const void*>(base), live ? n : 0u);
+    }
+    // Load i; `lane_out`: this lane's piece of k is not there (ROW).
+    __device__ __forceinline__ void load(const v4i& r, unsigned lds, bool lane_out, int i) const
+    {
+        dma16_free(r, !COL && lane_out ? 0x80000000u : off[i], lds + place(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i) * 1024);
+    }
+    __device__ __forceinline__ void advance()
+    {
+        base += step;
+        if (!COL) full -= 2 * KS;
     }
 };
 
 // This lane's places in a tile for its 32 T rows or columns from `first` on.
-template <bool COL, int R, int T>
+template <bool COL, int R, int KS, int T>
 struct TilePlaces {
-    int at[COL ? T : 4];        // bytes: COL per 32 columns; ROW per 16 k
+    int at[COL ? T : KS / 16];        // bytes: COL per 32 columns; ROW per 16 k
     __device__ __forceinline__ void init(int first)
     {
         const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
         if constexpr (COL) {
-            const int q = 8 * h + ((lane & 15) >> 2), s = q & 3;
+            const int q = 8 * h + ((lane & 15) >> 2), s = R % 128 == 0 ? q & 3 : 0;
 #pragma unroll
             for (int d = 0; d < T; ++d) {
                 const int c = first / 8 + 4 * d + ((lane & 16) >> 3) + ((lane & 3) >> 1);
@@ -148,7 +174,7 @@ struct TilePlaces {
             }
         } else {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) at[t] = (first + r) * 128 + 16 * ((2 * t + h) ^ ((r >> 1) & 7));
+            for (int t = 0; t < KS / 16; ++t) at[t] = (first + r) * (2 * KS) + 16 * ((2 * t + h) ^ row_swap<KS>(r));
         }
     }
     // operand for 16 k from 16 t on
@@ -160,7 +186,7 @@ struct TilePlaces {
             const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p + 4 * (2 * R)));
             return __builtin_bit_cast(v8bf, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            return *reinterpret_cast<const v8bf*>(tile + at[t] + u * 32 * 128);
+            return *reinterpret_cast<const v8bf*>(tile + at[t] + u * 32 * (2 * KS));
         }
     }
 };
@@ -264,15 +290,22 @@ __device__ __forceinline__ void gated_block(const Gate& p, int f32, int64_t m, i
     }
 }
 
-// (waves per SIMD: the tiles' LDS lets one workgroup of eight or two of four wavefronts run on a compute unit)
-template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int END>
-__global__ __launch_bounds__(64 * WM * WN, 2) void matmul_kernel(MatmulArgs p)
+// All but the last COUNT loads of this wavefront have landed, its reads of LDS are done, and all wavefronts are here.
+template <int COUNT>
+__device__ __forceinline__ void stage_barrier()
 {
-    constexpr int NT = 64 * WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-    using FA = TileFeed<COLA, BM, NT>;
-    using FB = TileFeed<COLB, END == kGated ? BN / 2 : BN, NT>;
-    constexpr int STAGE = BM * 128 + BN * 128;
-    static_assert(END != kGated || (!COLB && TN == 2), "gated: a wavefront has the 32 values and the 32 gates of the same outputs");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COUNT) : "memory");
+}
+
+// KS: k of a step; STAGES: of the ring.  (Two wavefronts per SIMD: one workgroup of eight, or two of four.)
+template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int END>
+__global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2) void matmul_kernel(MatmulArgs p)
+{
+    constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, G = END == kGated ? TN / 2 : TN;
+    using FA = TileFeed<COLA, BM, KS, NW>;
+    using FB = TileFeed<COLB, END == kGated ? BN / 2 : BN, KS, NW>;
+    constexpr int STAGE = (BM + BN) * 2 * KS, LOADS = FA::PT + FB::PT * (END == kGated ? 2 : 1);
+    static_assert(END != kGated || (!COLB && TN % 2 == 0), "gated: a wavefront has the values and the gates of the same outputs");
     extern __shared__ __align__(1024) char lds[];
     const MatmulPlace at = matmul_place(p);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave / WN, wn = wave % WN;
@@ -281,67 +314,137 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void matmul_kernel(MatmulArgs p)
     const int64_t lda = p.a.ld, ldb = p.b.ld;
 
     FA fa;
-    FB fb;
+    FB fb, fg;                  // fg: gates
     fa.init(lda, p.M - m0);
     fb.init(ldb, p.N - n0);
     const int beg = (int)((int64_t)p.total * at.slice / p.slices), end = (int)((int64_t)p.total * (at.slice + 1) / p.slices);
-    int pass = beg / p.steps, step = beg - pass * p.steps;
+    int pass = beg / p.steps, left = p.K - (beg - pass * p.steps) * KS, todo = end - beg;      // k of the pass and steps that are not loaded yet
     const unsigned base = lds_address(lds);
-
-    // bytes that may be read from the first element of a tile on: whole rows of what is left of the matrix
-    auto load = [&](int buf) {
-        const int k0 = step * kStep, left = p.K - k0, left8 = (left + 7) & ~7;
-        const __bf16* const pa = p.a.p + ((p.order_a >> (4 * pass)) & 15) * p.a.plane;
-        const __bf16* const pb = p.b.p + ((p.order_b >> (4 * pass)) & 15) * p.b.plane;
-        const unsigned to = base + buf * STAGE;
-        auto bytes = [&](bool col, int64_t ld, int first, int rows, int all, int count) {
-            const int64_t r = col ? min(left, kStep) : min(all - first, count);
-            return (unsigned)(2 * ((r - 1) * ld + (col ? ((all + 7) & ~7) - first : left8)));
-        };
-        fa.load(COLA ? pa + (int64_t)k0 * lda + m0 : pa + (int64_t)m0 * lda + k0, bytes(COLA, lda, m0, BM, p.M, BM), left8, to);
-        const __bf16* const qb = COLB ? pb + (int64_t)k0 * ldb + n0 : pb + (int64_t)n0 * ldb + k0;
-        fb.load(qb, bytes(COLB, ldb, n0, CB, p.N, CB), left8, to + BM * 128);
-        if constexpr (END == kGated)
-            fb.load(qb + (int64_t)p.N * ldb, bytes(false, ldb, n0, CB, p.N, CB), left8, to + BM * 128 + CB * 128);
-        if (++step == p.steps) {
-            step = 0;
+    unsigned to = base;
+    const int k_lane = KS == 32 ? 8 * ((lane & 3) ^ ((lane >> 4) & 3)) : 8 * ((lane & 7) ^ ((lane >> 4 & 3) | (wave & 1) << 2));                   // of a step: this lane's piece of a ROW tile
+    auto start = [&]() {
+        const int k0 = p.K - left, left8 = (left + 7) & ~7;
+        const __bf16* const pa = p.a.p + ((p.order_a >> (4 * min(pass, 7))) & 15) * p.a.plane;
+        const __bf16* const pb = p.b.p + ((p.order_b >> (4 * min(pass, 7))) & 15) * p.b.plane;
+        if constexpr (COLA) fa.start(pa + (int64_t)k0 * lda + m0, lda, 0, ((p.M + 7) & ~7) - m0);
+        else fa.start(pa + (int64_t)m0 * lda + k0, lda, min(p.M - m0, BM), left8);
+        if constexpr (COLB) fb.start(pb + (int64_t)k0 * ldb + n0, ldb, 0, ((p.N + 7) & ~7) - n0);
+        else fb.start(pb + (int64_t)n0 * ldb + k0, ldb, min(p.N - n0, CB), left8);
+        if constexpr (END == kGated) fg.start(pb + (int64_t)(p.N + n0) * ldb + k0, ldb, min(p.N - n0, CB), left8);
+    };
+    v4i wa, wb, wg;
+    bool lane_out;
+    // A step's loads: their descriptors, load i of LOADS, and the way to the next step.  Behind the last one they write zeros, so that every
+    // step has the same number of loads on their way.
+    auto windows = [&]() {
+        wa = fa.window(left, todo > 0);
+        wb = fb.window(left, todo > 0);
+        if constexpr (END == kGated) wg = fg.window(left, todo > 0);
+        lane_out = k_lane >= ((left + 7) & ~7);
+    };
+    auto load = [&](int i) {
+        if (i < FA::PT) fa.load(wa, to, lane_out, i);
+        else if (i < FA::PT + FB::PT) fb.load(wb, to + BM * 2 * KS, lane_out, i - FA::PT);
+        else if (END == kGated) fg.load(wg, to + BM * 2 * KS + CB * 2 * KS, lane_out, i - FA::PT - FB::PT);
+    };
+    auto loaded = [&]() {
+        fa.advance();
+        fb.advance();
+        if constexpr (END == kGated) fg.advance();
+        --todo;
+        left -= KS;
+        to = to + STAGE == base + STAGES * STAGE ? base : to + STAGE;
+        if (left <= 0) {
+            left = p.K;
             ++pass;
+            start();
         }
     };
 
-    TilePlaces<COLA, BM, TM> ra;
-    TilePlaces<COLB, BN, END == kGated ? 1 : TN> rb;
+    TilePlaces<COLA, BM, KS, TM> ra;
+    TilePlaces<COLB, BN, KS, G> rb;
     ra.init(wm * TM * 32);
-    rb.init(END == kGated ? wn * 32 : wn * TN * 32);
+    rb.init(wn * G * 32);
     v16f acc[TM][TN];
 #pragma unroll
     for (int u = 0; u < TM; ++u)
 #pragma unroll
         for (int v = 0; v < TN; ++v) acc[u][v] = zero16();
 
-    if (beg < end) load(0);
-    int buf = 0;
-    for (int it = beg; it < end; ++it) {
-        dma_barrier();
-        if (it + 1 < end) load(buf ^ 1);
-        const char* const ta = lds + buf * STAGE;
-        const char* const tb = ta + BM * 128;
+    struct Operands {
+        v8bf a[TM], b[TN];
+    };
+    // Read i of the TM + TN of a step's half t, product i of its TM TN.
+    auto read = [&](Operands& o, const char* ta, int t, int i) {
+        const char* const tb = ta + BM * 2 * KS;
+        if (i < TN) o.b[i] = rb.read(tb + i / G * CB * 2 * KS, i % G, t);
+        else if (i < TN + TM) o.a[i - TN] = ra.read(ta, i - TN, t);
+    };
+    auto multiply = [&](const Operands& o, int i) {
+        const int u = i / TN, v = i % TN;
+        acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.b[v], o.a[u], acc[u][v], 0, 0, 0);
+    };
+
+    if (beg < end) {
+        start();
+        if constexpr (END == kGated)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            v8bf a[TM], b[TN];
+            for (int i = 0; i < FB::PT; ++i) fg.off[i] = fb.off[i];
+        Operands even, odd;
 #pragma unroll
-            for (int v = 0; v < TN; ++v) {
-                if constexpr (END == kGated) b[v] = rb.read(tb + v * CB * 128, 0, t);
-                else b[v] = rb.read(tb, v, t);
-            }
+        for (int s = 0; s < STAGES - 1; ++s) {
+            windows();
 #pragma unroll
-            for (int u = 0; u < TM; ++u) a[u] = ra.read(ta, u, t);
-#pragma unroll
-            for (int u = 0; u < TM; ++u)
-#pragma unroll
-                for (int v = 0; v < TN; ++v) acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[v], a[u], acc[u][v], 0, 0, 0);
+            for (int i = 0; i < LOADS; ++i) load(i);
+            loaded();
         }
-        buf ^= 1;
+        const char* tile = lds;
+        // Products of one half, and between them the reads of the other and the loads of a step ahead, one at a time: they are issued
+        // while the matrix unit is busy.
+        constexpr int MM = TM * TN, RD = TM + TN;
+        auto half = [&](const Operands& now, Operands& next, int t, auto loads) {
+#pragma unroll
+            for (int i = 0; i < (MM > RD ? MM : RD); ++i) {
+                if (i < MM) multiply(now, i);
+                if (i < RD) read(next, tile, t, i);
+                if constexpr (decltype(loads)::value) {
+                    constexpr int EACH = (LOADS + MM - 1) / MM;
+#pragma unroll
+                    for (int j = 0; j < EACH; ++j)
+                        if (i * EACH + j < LOADS) load(i * EACH + j);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto advance = [&]() { tile = tile + STAGE == lds + STAGES * STAGE ? lds : tile + STAGE; };
+        stage_barrier<(STAGES - 2) * LOADS>();
+#pragma unroll
+        for (int i = 0; i < RD; ++i) read(even, tile, 0, i);
+        windows();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(i);
+        loaded();
+        half(even, odd, 1, std::false_type());
+        if constexpr (KS == 64) {
+            half(odd, even, 2, std::false_type());
+            half(even, odd, 3, std::false_type());
+        }
+        advance();
+        for (int it = beg + 1; it < end; ++it) {
+            stage_barrier<(STAGES - 2) * LOADS>();
+            windows();
+            half(odd, even, 0, std::true_type());
+            loaded();
+            half(even, odd, 1, std::false_type());
+            if constexpr (KS == 64) {
+                half(odd, even, 2, std::false_type());
+                half(even, odd, 3, std::false_type());
+            }
+            advance();
+        }
+#pragma unroll
+        for (int i = 0; i < MM; ++i) multiply(odd, i);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 
     const int h = lane >> 5, l32 = lane & 31;
@@ -355,36 +458,39 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void matmul_kernel(MatmulArgs p)
             if (m >= p.M) continue;
 #pragma unroll
             for (int v = 0; v < TN; ++v) {
-                const int nb = END == kGated ? n0 + wn * 32 : n0 + (wn * TN + v) * 32;
+                const int nb = n0 + (wn * G + v % G) * 32;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int n = nb + 8 * q + 4 * h;
                     const float x[4] = {acc[u][v][4 * q], acc[u][v][4 * q + 1], acc[u][v][4 * q + 2], acc[u][v][4 * q + 3]};
-                    if (n < p.N) put4(part, (int64_t)m * cols + n + (END == kGated ? v * p.N : 0), 1, n, p.N, vec && n + 4 <= p.N, x);
+                    if (n < p.N) put4(part, (int64_t)m * cols + n + (END == kGated ? v / G * p.N : 0), 1, n, p.N, vec && n + 4 <= p.N, x);
                 }
             }
         }
         return;
     }
     if constexpr (END == kGated) {
-        const int nb = n0 + wn * 32;
-        float ba[16], bg[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int n = nb + 8 * (i / 4) + 4 * h + i % 4;
-            ba[i] = p.bias && n < p.N ? p.bias[n] : 0.0f;
-            bg[i] = p.bias && n < p.N ? p.bias[p.N + n] : 0.0f;
-        }
-#pragma unroll
-        for (int u = 0; u < TM; ++u) {
-            const int m = m0 + (wm * TM + u) * 32 + l32;
-            float a[16], g[16];
+        for (int v = 0; v < G; ++v) {
+            const int nb = n0 + (wn * G + v) * 32;
+            float ba[16], bg[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                a[i] = acc[u][0][i] + ba[i];
-                g[i] = acc[u][1][i] + bg[i];
+                const int n = nb + 8 * (i / 4) + 4 * h + i % 4;
+                ba[i] = p.bias && n < p.N ? p.bias[n] : 0.0f;
+                bg[i] = p.bias && n < p.N ? p.bias[p.N + n] : 0.0f;
             }
-            gated_block(p.gate, p.out_f32, m, nb, p.N, m < p.M, h, a, g);
+#pragma unroll
+            for (int u = 0; u < TM; ++u) {
+                const int m = m0 + (wm * TM + u) * 32 + l32;
+                float a[16], g[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    a[i] = acc[u][v][i] + ba[i];
+                    g[i] = acc[u][G + v][i] + bg[i];
+                }
+                gated_block(p.gate, p.out_f32, m, nb, p.N, m < p.M, h, a, g);
+            }
         }
     } else {
         const bool vec = (p.ld_out & 3) == 0 && ((uintptr_t)p.out & 15) == 0;

@@ -15,15 +15,38 @@ int passes(int planes_a, int planes_b) { return planes_a * planes_b == 9 ? 6 : p
 Plan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated)
 {
     auto tiles = [&](int t) { return ((M + kTileM[t] - 1) / kTileM[t]) * ((N + kTileN[t] / (gated ? 2 : 1) - 1) / (kTileN[t] / (gated ? 2 : 1))); };
-    const int64_t total = passes(planes_a, planes_b) * ((K + kStep - 1) / kStep);
-    Plan p{kTile128, 1};
-    if (tiles(kTile256) >= 200) p.tile = kTile256;
-    else if (!col_a && M <= 32) p.tile = kTile32;
-    const int64_t wanted = p.tile == kTile256 ? 256 : 512, n = tiles(p.tile);
-    // parts of no fewer than eight steps, and no more than 16 of them
-    int64_t most = total / 8 < 16 ? total / 8 : 16;
-    if (n * 2 <= wanted && most > 1) p.slices = (int)(wanted / n < most ? wanted / n : most);
-    return p;
+    const double steps = passes(planes_a, planes_b) * (double)((K + 63) / 64);
+    if (!col_a && M <= 32) {
+        // bound by B's bytes: parts of no fewer than eight steps until two workgroups per compute unit have work
+        const int64_t n = tiles(kTile32);
+        int64_t most = (int64_t)(steps / 8 < 16 ? steps / 8 : 16), slices = 512 / n < most ? 512 / n : most;
+        return Plan{kTile32, slices > 1 ? (int)slices : 1};
+    }
+    // What a call takes, in microseconds: rounds of workgroups over 256 compute units, at 0.45 us for 128 x 128 x 64 on one (1.2 PFLOP/s on
+    // all).  A workgroup of 256 or 192 rows has its compute unit alone, and four steps' time of its own at its start and end; two of 128 rows
+    // share one, hide half of that behind each other and take 1.2 of the time.  Slices cost the partial results' way to memory and back and a launch.
+    Plan best{kTile128, 1};
+    double least = 1e30;
+    for (int t : {kTile256, kTile192, kTile128}) {
+        if (t == kTile192 && col_a) continue;
+        for (int s = 1; s <= 32; s = s < 4 ? s + 1 : s + s / 4) {
+            if (s > 1 && steps / s < 8) break;
+            const int64_t n = tiles(t) * s;
+            double us;
+            if (t == kTile128) {
+                const int64_t rest = n % 512;
+                us = ((double)(n / 512) * 2 + (rest == 0 ? 0.0 : rest <= 256 ? 1.25 : 2.0)) * 0.45 * 1.2 * (steps / s + 2);
+            } else {
+                us = (double)((n + 255) / 256) * (kTileM[t] / 64) * 0.45 * (steps / s + 4);
+            }
+            if (s > 1) us += 4 + (double)s * M * N * (gated ? 2 : 1) * 8 / 4.5e6;
+            if (us < least) {
+                least = us;
+                best = Plan{t, s};
+            }
+        }
+    }
+    return best;
 }
 
 struct SumArgs {
@@ -68,31 +91,72 @@ __global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p)
     put4(p.out, m * p.ld_out + n, p.out_f32, n, (int)p.N, vec && (p.ld_out & 3) == 0 && ((uintptr_t)p.out & 15) == 0, v);
 }
 
-// A wavefront per 32 rows and 32 outputs, as the product's kernel leaves them.
+// Four outputs of a row per thread, eight threads a block of 32.
 __global__ __launch_bounds__(256) void matmul_sum_gated_kernel(SumArgs p)
 {
-    const int lane = threadIdx.x & 63, h = lane >> 5;
-    const int64_t blocks = (p.N + 31) / 32, id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), row = id / blocks, m = row * 32 + (lane & 31);
-    if (row * 32 >= p.M) return;
-    const int n0 = (int)(id - row * blocks) * 32, N = (int)p.N;
-    const bool in = m < p.M;
-    float a[16], g[16];
+    const int64_t per = (p.N + 31) / 32 * 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool in = id < p.M * per;                                  // (whole blocks of lanes)
+    const int64_t m = in ? id / per : 0;
+    const int n = in ? (int)(id - m * per) * 4 : 0, N = (int)p.N;
+    float a[4], g[4], v[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int n = n0 + 8 * (i / 4) + 4 * h + i % 4;
-        a[i] = p.bias && n < N ? p.bias[n] : 0.0f;
-        g[i] = p.bias && n < N ? p.bias[N + n] : 0.0f;
+    for (int e = 0; e < 4; ++e) {
+        a[e] = p.bias && n + e < N ? p.bias[n + e] : 0.0f;
+        g[e] = p.bias && n + e < N ? p.bias[N + n + e] : 0.0f;
     }
+    const bool vec = (N & 3) == 0 && n < N;
     for (int s = 0; s < p.slices; ++s) {
-        const float* const x = p.part + (s * p.M + (in ? m : 0)) * 2 * N;
+        const float* const x = p.part + (s * p.M + m) * 2 * N + n;
+        if (vec) {
+            const float4 t = *reinterpret_cast<const float4*>(x), u = *reinterpret_cast<const float4*>(x + N);
+            a[0] += t.x, a[1] += t.y, a[2] += t.z, a[3] += t.w;
+            g[0] += u.x, g[1] += u.y, g[2] += u.z, g[3] += u.w;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int n = n0 + 8 * (i / 4) + 4 * h + i % 4;
-            a[i] += n < N ? x[n] : 0.0f;
-            g[i] += n < N ? x[N + n] : 0.0f;
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N) {
+                    a[e] += x[e];
+                    g[e] += x[N + e];
+                }
         }
     }
-    gated_block(p.gate, p.out_f32, m, n0, N, in, h, a, g);
+    const Gate& q = p.gate;
+    if (q.pre_scales) {
+        uint32_t ta = 0, tg = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (n + e >= N) a[e] = g[e] = 0.0f;
+            ta = max(ta, __float_as_uint(a[e]) & 0x7fffffffu);
+            tg = max(tg, __float_as_uint(g[e]) & 0x7fffffffu);
+        }
+#pragma unroll
+        for (int off = 1; off < 8; off <<= 1) {
+            ta = max(ta, (uint32_t)__shfl_xor((int)ta, off, 64));
+            tg = max(tg, (uint32_t)__shfl_xor((int)tg, off, 64));
+        }
+        if (in) {
+            const uint32_t ea = block_scale8(ta), eg = block_scale8(tg);
+            const float ia = inverse_scale(ea), ig = inverse_scale(eg);
+            const int np = (N + 31) & ~31;
+            uint8_t* const c = static_cast<uint8_t*>(q.pre) + m * (2 * (int64_t)np) + n;
+            *reinterpret_cast<uint32_t*>(c) = codes8(a[0] * ia, a[1] * ia, a[2] * ia, a[3] * ia);
+            *reinterpret_cast<uint32_t*>(c + np) = codes8(g[0] * ig, g[1] * ig, g[2] * ig, g[3] * ig);
+            if (n % 32 == 0) {
+                uint8_t* const s = q.pre_scales + m * (2 * (np / 32)) + n / 32;
+                s[0] = (uint8_t)ea;
+                s[np / 32] = (uint8_t)eg;
+            }
+        }
+    }
+    if (!in || n >= N) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a[e] * gate_of<false>(q.act, g[e], nullptr);
+    put4(q.h, m * q.ld_h + n, p.out_f32, n, N, (q.ld_h & 3) == 0 && ((uintptr_t)q.h & 15) == 0 && n + 4 <= N, v);
+    if (q.pre && !q.pre_scales) {
+        const bool vp = (N & 3) == 0 && ((uintptr_t)q.pre & 15) == 0;
+        put4(q.pre, m * q.ld_pre + n, p.out_f32, n, N, vp, a);
+        put4(q.pre, m * q.ld_pre + N + n, p.out_f32, n, N, vp, g);
+    }
 }
 
 }  // namespace
@@ -114,11 +178,10 @@ int launch_product(const Product& q, void* part, hipStream_t s)
     p.M = (int)q.M;
     p.N = (int)q.N;
     p.K = (int)q.K;
-    p.steps = q.K ? (int)((q.K + kStep - 1) / kStep) : 1;
     if (q.planes_a == 3 && q.planes_b == 3) p.order_a = 0x001102, p.order_b = 0x010120;
     else if (q.planes_a == 3) p.order_a = 0x012;
     else if (q.planes_b == 3) p.order_b = 0x012;
-    p.total = q.K ? p.steps * passes(q.planes_a, q.planes_b) : 0;      // (no rows to sum over: zeros)
+    p.passes = passes(q.planes_a, q.planes_b);
     p.slices = plan.slices;
     const int cols = kTileN[plan.tile] / (q.gated ? 2 : 1);
     p.tiles_m = (int)((q.M + kTileM[plan.tile] - 1) / kTileM[plan.tile]);
@@ -135,8 +198,8 @@ int launch_product(const Product& q, void* part, hipStream_t s)
     if (st != FPQ_OK || plan.slices == 1) return st;
     const SumArgs r{static_cast<const float*>(part), q.M, q.N, plan.slices, q.out, q.ld_out, q.out_f32, q.bias, q.gate};
     if (q.gated) {
-        const int64_t waves = ((q.M + 31) / 32) * ((q.N + 31) / 32);
-        matmul_sum_gated_kernel<<<dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s>>>(r);
+        const int64_t threads = q.M * ((q.N + 31) / 32 * 8);
+        matmul_sum_gated_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(r);
     } else {
         const int64_t threads = q.M * ((q.N + 3) / 4);
         matmul_sum_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(r);

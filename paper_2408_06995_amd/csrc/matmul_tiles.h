@@ -4,16 +4,18 @@
 
 namespace fpq {
 
-// Tiles: results and wavefronts of a workgroup.
-enum MatmulTile : int { kTile256 = 0, kTile128 = 1, kTile32 = 2 };
-constexpr int kTileM[3] = {256, 128, 32}, kTileN[3] = {256, 128, 256};
+// Tiles: results of a workgroup.
+enum MatmulTile : int { kTile256 = 0, kTile192 = 1, kTile128 = 2, kTile32 = 3 };
+constexpr int kTileM[4] = {256, 192, 128, 32}, kTileN[4] = {256, 256, 128, 256};
 
-template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int END>
-int launch_matmul_tile(const MatmulArgs& p, hipStream_t s)
+template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int END>
+int launch_matmul_tile(MatmulArgs p, hipStream_t s)
 {
+    p.steps = p.K ? (p.K + KS - 1) / KS : 1;
+    p.total = p.K ? p.steps * p.passes : 0;             // (nothing to sum over: zeros)
     static std::atomic<uint64_t> done{0};
-    constexpr int bytes = 2 * (BM + BN) * 128;
-    const auto kernel = matmul_kernel<COLA, COLB, BM, BN, WM, WN, END>;
+    constexpr int bytes = STAGES * (BM + BN) * 2 * KS;
+    const auto kernel = matmul_kernel<COLA, COLB, BM, BN, WM, WN, KS, STAGES, END>;
     if (!allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, done)) return FPQ_ERR_LAUNCH;
     kernel<<<dim3((unsigned)((int64_t)p.tiles_m * p.tiles_n * p.slices)), dim3(64 * WM * WN), bytes, s>>>(p);
     return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
@@ -22,10 +24,12 @@ int launch_matmul_tile(const MatmulArgs& p, hipStream_t s)
 template <bool COLA, bool COLB, int END>
 int launch_matmul_form(const MatmulArgs& p, int tile, hipStream_t s)
 {
-    if (tile == kTile256) return launch_matmul_tile<COLA, COLB, 256, 256, 2, 4, END>(p, s);
-    if constexpr (!COLA)
-        if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, END>(p, s);
-    return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, END>(p, s);
+    if (tile == kTile256) return launch_matmul_tile<COLA, COLB, 256, 256, 2, 4, 64, 2, END>(p, s);
+    if constexpr (!COLA) {
+        if (tile == kTile192) return launch_matmul_tile<COLA, COLB, 192, 256, 2, 4, 64, 2, END>(p, s);
+        if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, 32, 4, END>(p, s);
+    }
+    return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 2, END>(p, s);
 }
 
 int launch_matmul_rows(const MatmulArgs& p, int tile, hipStream_t s);
