@@ -236,57 +236,105 @@ __device__ __forceinline__ void put4(void* out, int64_t at, int f32, int n, int 
     }
 }
 
-// One block of 32 outputs of a row: values a and gates g, 16 of them in each of the lanes l and l + 32 (as the matrix unit leaves
-// them: places 8 (i / 4) + 4 h + i % 4 from n0 on).  Writes h and what is kept.
-__device__ __forceinline__ void gated_block(const Gate& p, int f32, int64_t m, int n0, int N, bool in, int h, const float (&a)[16], const float (&g)[16])
-{
-    const int np = (N + 31) & ~31;
-    const bool vec4 = (p.ld_h & 3) == 0 && ((uintptr_t)p.h & 15) == 0;
-    const bool vec4p = (p.ld_pre & 3) == 0 && (N & 3) == 0 && ((uintptr_t)p.pre & 15) == 0;
-    uint32_t ea = 0, eg = 0;
-    float ia = 0.0f, ig = 0.0f;
-    if (p.pre_scales) {
-        uint32_t ta = 0, tg = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const bool has = n0 + 8 * (i / 4) + 4 * h + i % 4 < N;
-            ta = max(ta, has ? __float_as_uint(a[i]) & 0x7fffffffu : 0u);
-            tg = max(tg, has ? __float_as_uint(g[i]) & 0x7fffffffu : 0u);
-        }
-        ta = max(ta, (uint32_t)__shfl_xor((int)ta, 32, 64));
-        tg = max(tg, (uint32_t)__shfl_xor((int)tg, 32, 64));
-        ea = block_scale8(ta);
-        eg = block_scale8(tg);
-        ia = inverse_scale(ea);
-        ig = inverse_scale(eg);
-        if (in && h == 0 && n0 < N) {
-            uint8_t* const s = p.pre_scales + m * (2 * (np / 32)) + n0 / 32;
-            s[0] = (uint8_t)ea;
-            s[np / 32] = (uint8_t)eg;
-        }
+// Rows of 32 results of a wavefront, on their way to memory through LDS in whole pieces of 16 bytes: as the matrix unit leaves them a
+// lane has four of a row's results, and stores of 8 or 16 bytes a row cost the L2 a request each (of 84 MB as codes 8 bytes at a time:
+// 40 us).  Lane (h, l32) puts the results 8 q + 4 h + {0..3} of row l32; then the 64 lanes store B bytes of each of the 32 rows.
+template <int B>
+struct RowStage {
+    static constexpr int STRIDE = B + 16, LANES = B / 16;   // (an odd number of places of 16 bytes, or nearly: rows start in different banks)
+    char* room;
+    template <typename V>
+    __device__ __forceinline__ void put(int q, V v) const
+    {
+        const int lane = threadIdx.x & 63;
+        *reinterpret_cast<V*>(room + (lane & 31) * STRIDE + (2 * q + (lane >> 5)) * (int)sizeof(V)) = v;
     }
-    if (!in) return;
+    // `rows` rows exist, and `bytes` of each
+    __device__ __forceinline__ void flush(char* to, int64_t ld, int rows, int bytes) const
+    {
+        asm volatile("" ::: "memory");                   // (a wavefront's accesses of LDS are carried out in order)
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < B / 32; ++i) {
+            const int id = i * 64 + lane, r = id / LANES, at = id % LANES * 16;
+            const uint4 v = *reinterpret_cast<const uint4*>(room + r * STRIDE + at);
+            if (r < rows && at < bytes) *reinterpret_cast<uint4*>(to + r * ld + at) = v;
+        }
+        asm volatile("" ::: "memory");
+    }
+};
+
+// Four results of each q = 0 .. 3 of 32 rows from column n on, in the type.
+template <typename F>
+__device__ __forceinline__ void put_rows(char* room, void* out, int64_t ld, int f32, int64_t m0, int rows, int n, int N, bool pieces, F&& value)
+{
+    const int lane = threadIdx.x & 63, h = lane >> 5, left = min(N - n, 32);
+    if (f32) {
+        if (pieces) {
+            const RowStage<128> s{room};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s.put(q, make_float4(value(4 * q), value(4 * q + 1), value(4 * q + 2), value(4 * q + 3)));
+            s.flush(reinterpret_cast<char*>(static_cast<float*>(out) + m0 * ld + n), 4 * ld, rows, 4 * left);
+            return;
+        }
+    } else if (pieces) {
+        const RowStage<64> s{room};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s.put(q, make_uint2(pair_bf16(value(4 * q), value(4 * q + 1)), pair_bf16(value(4 * q + 2), value(4 * q + 3))));
+        s.flush(reinterpret_cast<char*>(static_cast<__bf16*>(out) + m0 * ld + n), 2 * ld, rows, 2 * left);
+        return;
+    }
+    if ((lane & 31) >= rows) return;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const int n = n0 + 8 * q + 4 * h;
-        float va[4], vg[4], vh[4];
+        const float v[4] = {value(4 * q), value(4 * q + 1), value(4 * q + 2), value(4 * q + 3)};
+        const int c = n + 8 * q + 4 * h;
+        if (c < N) put4(out, (m0 + (lane & 31)) * ld + c, f32, c, N, false, v);
+    }
+}
+
+// A block of 32 outputs of 32 rows: values a and gates g, 16 of a row in each of the lanes l and l + 32 (as the matrix unit leaves
+// them: places 8 (i / 4) + 4 h + i % 4 from n0 on).  Writes h and what is kept; of blocks the codes, and the scales of a row, values' and gates', to
+// scales[row][0], [row][SCALES].
+template <int SCALES>
+__device__ __forceinline__ void gated_block(const Gate& p, int f32, int64_t m0, int rows, int n0, int N, const float (&a)[16], const float (&g)[16], char* room,
+                                            uint8_t* scales)
+{
+    const int lane = threadIdx.x & 63, h = lane >> 5, np = (N + 31) & ~31, e = f32 ? 4 : 8;
+    if (n0 >= N) return;
+    auto whole = [&](const void* o, int64_t ld) { return N % e == 0 && ld % e == 0 && ((uintptr_t)o & 15) == 0; };
+    put_rows(room, p.h, p.ld_h, f32, m0, rows, n0, N, whole(p.h, p.ld_h), [&](int i) { return a[i] * gate_of<false>(p.act, g[i], nullptr); });
+    if (!p.pre) return;
+    if (!p.pre_scales) {
+        const bool w = whole(p.pre, p.ld_pre);
+        put_rows(room, p.pre, p.ld_pre, f32, m0, rows, n0, N, w, [&](int i) { return a[i]; });
+        // (the gates' columns are those from N on; N is a whole number of pieces where the values' rows are)
+        put_rows(room, f32 ? static_cast<void*>(static_cast<float*>(p.pre) + N) : static_cast<void*>(static_cast<__bf16*>(p.pre) + N), p.ld_pre, f32, m0, rows, n0, N, w,
+                 [&](int i) { return g[i]; });
+        return;
+    }
+    auto codes = [&](auto part, const float (&v)[16], uint8_t* to, uint8_t* scale) {
+        constexpr bool PART = decltype(part)::value;                  // of the 32 columns not all are there
+        auto at = [&](int i) { return !PART || n0 + 8 * (i / 4) + 4 * h + i % 4 < N ? v[i] : 0.0f; };
+        uint32_t top = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            va[e] = a[4 * q + e];
-            vg[e] = g[4 * q + e];
-            vh[e] = va[e] * gate_of<false>(p.act, vg[e], nullptr);
-        }
-        if (n < N) put4(p.h, m * p.ld_h + n, f32, n, N, vec4 && n + 4 <= N, vh);
-        if (p.pre_scales) {
-            if (n0 >= N) continue;
-            uint8_t* const c = static_cast<uint8_t*>(p.pre) + m * (2 * (int64_t)np) + n;
-            auto has = [&](int e, float x, float s) { return n + e < N ? x * s : 0.0f; };
-            *reinterpret_cast<uint32_t*>(c) = codes8(has(0, va[0], ia), has(1, va[1], ia), has(2, va[2], ia), has(3, va[3], ia));
-            *reinterpret_cast<uint32_t*>(c + np) = codes8(has(0, vg[0], ig), has(1, vg[1], ig), has(2, vg[2], ig), has(3, vg[3], ig));
-        } else if (p.pre && n < N) {
-            put4(p.pre, m * p.ld_pre + n, f32, n, N, vec4p && n + 4 <= N, va);
-            put4(p.pre, m * p.ld_pre + N + n, f32, n, N, vec4p && n + 4 <= N, vg);
-        }
+        for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(at(i)) & 0x7fffffffu);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+        const uint32_t s = block_scale8(top);
+        const float r = inverse_scale(s);
+        const RowStage<32> stage{room};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) stage.put(q, codes8(at(4 * q) * r, at(4 * q + 1) * r, at(4 * q + 2) * r, at(4 * q + 3) * r));
+        stage.flush(reinterpret_cast<char*>(to), 2 * (int64_t)np, rows, 32);
+        if (h == 0) scale[(lane & 31) * 2 * SCALES] = (uint8_t)s;
+    };
+    uint8_t* const to = static_cast<uint8_t*>(p.pre) + m0 * (2 * (int64_t)np) + n0;
+    if (n0 + 32 <= N) {
+        codes(std::false_type(), a, to, scales);
+        codes(std::false_type(), g, to + np, scales + SCALES);
+    } else {
+        codes(std::true_type(), a, to, scales);
+        codes(std::true_type(), g, to + np, scales + SCALES);
     }
 }
 
@@ -470,6 +518,10 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         return;
     }
     if constexpr (END == kGated) {
+        __syncthreads();                                        // the ring is free
+        constexpr int SC = WN * G, ROOM = RowStage<128>::STRIDE * 32;
+        static_assert(NW * ROOM + BM * 2 * SC <= STAGES * STAGE, "room for the results on their way");
+        uint8_t* const scales = reinterpret_cast<uint8_t*>(lds) + NW * ROOM;     // [BM][values, gates][blocks of the tile]
 #pragma unroll
         for (int v = 0; v < G; ++v) {
             const int nb = n0 + (wn * G + v) * 32;
@@ -482,35 +534,52 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
             }
 #pragma unroll
             for (int u = 0; u < TM; ++u) {
-                const int m = m0 + (wm * TM + u) * 32 + l32;
+                const int row = (wm * TM + u) * 32, m = m0 + row;
+                if (m >= p.M) break;
                 float a[16], g[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     a[i] = acc[u][v][i] + ba[i];
                     g[i] = acc[u][G + v][i] + bg[i];
                 }
-                gated_block(p.gate, p.out_f32, m, nb, p.N, m < p.M, h, a, g);
+                gated_block<SC>(p.gate, p.out_f32, m, min(p.M - m, 32), nb, p.N, a, g, lds + wave * ROOM, scales + row * 2 * SC + wn * G + v);
+            }
+        }
+        if (p.gate.pre_scales) {
+            __syncthreads();
+            // a row's scales of the tile lie together
+            const int all = (p.N + 31) / 32, first = n0 / 32, here = min(all - first, SC);
+            const bool words = SC == 4 && here == 4 && all % 4 == 0 && ((uintptr_t)p.gate.pre_scales & 3) == 0;
+            for (int i = threadIdx.x; i < 2 * min(BM, p.M - m0); i += 64 * NW) {
+                uint8_t* const to = p.gate.pre_scales + (int64_t)(m0 + i / 2) * (2 * all) + i % 2 * all + first;
+                if (words) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(scales + i * SC);
+                else
+                    for (int k = 0; k < here; ++k) to[k] = scales[i * SC + k];
             }
         }
     } else {
-        const bool vec = (p.ld_out & 3) == 0 && ((uintptr_t)p.out & 15) == 0;
+        __syncthreads();                                        // the ring is free
+        constexpr int ROOM = RowStage<128>::STRIDE * 32;
+        static_assert(NW * ROOM <= STAGES * STAGE, "room for the results on their way");
+        const int e = p.out_f32 ? 4 : 8;
+        const bool whole = p.N % e == 0 && p.ld_out % e == 0 && ((uintptr_t)p.out & 15) == 0;
 #pragma unroll
-        for (int v = 0; v < TN; ++v)
+        for (int v = 0; v < TN; ++v) {
+            const int nb = n0 + (wn * TN + v) * 32;
+            if (nb >= p.N) continue;
+            float b[16];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = n0 + (wn * TN + v) * 32 + 8 * q + 4 * h;
-                if (n >= p.N) continue;
-                float b[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) b[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.0f;
-#pragma unroll
-                for (int u = 0; u < TM; ++u) {
-                    const int m = m0 + (wm * TM + u) * 32 + l32;
-                    if (m >= p.M) continue;
-                    const float x[4] = {acc[u][v][4 * q] + b[0], acc[u][v][4 * q + 1] + b[1], acc[u][v][4 * q + 2] + b[2], acc[u][v][4 * q + 3] + b[3]};
-                    put4(p.out, m * p.ld_out + n, p.out_f32, n, p.N, vec && n + 4 <= p.N, x);
-                }
+            for (int i = 0; i < 16; ++i) {
+                const int n = nb + 8 * (i / 4) + 4 * h + i % 4;
+                b[i] = p.bias && n < p.N ? p.bias[n] : 0.0f;
             }
+#pragma unroll
+            for (int u = 0; u < TM; ++u) {
+                const int m = m0 + (wm * TM + u) * 32;
+                if (m >= p.M) break;
+                put_rows(lds + wave * ROOM, p.out, p.ld_out, p.out_f32, m, min(p.M - m, 32), nb, p.N, whole, [&](int i) { return acc[u][v][i] + b[i]; });
+            }
+        }
     }
 }
 
