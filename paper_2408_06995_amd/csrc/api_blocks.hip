@@ -56,25 +56,22 @@ bool reads(const void* p, int type, int64_t rows, int64_t cols, int64_t ld)
     return type == FPQ_TYPE_BF16 && aligned(p, 16) && cols % 8 == 0 && (rows <= 1 || ld % 8 == 0);
 }
 
-// A matrix as the products read it: where it is, or packed into the workspace.
-int operand(const void* p, int type, int64_t rows, int64_t cols, int64_t ld, Room& room, Operand& o, hipStream_t s)
+// A matrix as the products read it: where it is, or packed into the workspace by the launch that `packs` is collected for.
+Operand operand(const void* p, int type, int64_t rows, int64_t cols, int64_t ld, Room& room, PackList& packs)
 {
     ld = stride(ld, cols, rows);
-    if (reads(p, type, rows, cols, ld)) {
-        o = Operand{static_cast<const __bf16*>(p), ld, 0};
-        return FPQ_OK;
-    }
+    if (reads(p, type, rows, cols, ld)) return Operand{static_cast<const __bf16*>(p), ld, 0};
     const int64_t to = round8(cols);
     __bf16* const dst = room.take<__bf16>((size_t)rows * to * 2 * planes_of(type));
-    o = Operand{dst, to, rows * to};
-    return launch_planes(p, type, rows, cols, ld, dst, to, rows * to, s);
+    packs.m[packs.count++] = PackItem{p, nullptr, rows, cols, ld, dst, to, rows * to, 0, type, 0};
+    return Operand{dst, to, rows * to};
 }
-int operand_of_blocks(const void* codes, const uint8_t* scales, int64_t rows, int64_t cols, bool eight, Room& room, Operand& o, hipStream_t s)
+Operand operand_of_blocks(const void* codes, const uint8_t* scales, int64_t rows, int64_t cols, int bits, Room& room, PackList& packs)
 {
     const int64_t to = block_padded(cols);
     __bf16* const dst = room.take<__bf16>((size_t)rows * to * 2);
-    o = Operand{dst, to, 0};
-    return launch_decode(static_cast<const uint8_t*>(codes), scales, rows, to, eight, dst, 0, to, s);
+    packs.m[packs.count++] = PackItem{codes, scales, rows, to, to, dst, to, 0, 0, bits, 0};
+    return Operand{dst, to, 0};
 }
 
 bool workspace_bad(const void* workspace, size_t bytes, size_t need, int* st)
@@ -93,15 +90,15 @@ size_t gradient_parts(int64_t M, int64_t N, int64_t K, int type)
                            larger(product_part_bytes(N, K, M, p, p, true, false), product_part_bytes(N, K, M, p, 1, true, false))));
 }
 
-// The products of both gradients.  d: [M, N] as the products read it; x or its blocks; grad_x, grad_w may be null.
+// The products of both gradients.  d: [M, N] as the products read it, or to be packed with the others; x or its blocks; grad_x, grad_w may be null.
 int gradients(const Operand& d, int type, int64_t M, int64_t N, int64_t K, const void* x, const uint8_t* x_scales, int64_t ld_x, const void* w, int64_t ld_w,
-              void* grad_x, int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, Room& room, hipStream_t s)
+              void* grad_x, int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, Room& room, PackList& packs, hipStream_t s)
 {
     const int np = planes_of(type);
     Operand ow{}, ox{};
-    int st = FPQ_OK;
-    if (grad_x && M) st = operand(w, type, N, K, ld_w, room, ow, s);
-    if (st == FPQ_OK && grad_w && M) st = x_scales ? operand_of_blocks(x, x_scales, M, K, true, room, ox, s) : operand(x, type, M, K, ld_x, room, ox, s);
+    if (grad_x && M) ow = operand(w, type, N, K, ld_w, room, packs);
+    if (grad_w && M) ox = x_scales ? operand_of_blocks(x, x_scales, M, K, 8, room, packs) : operand(x, type, M, K, ld_x, room, packs);
+    int st = packs.count ? launch_packs(packs, s) : FPQ_OK;
     if (st != FPQ_OK) return st;
     Product p{};
     p.a = d;
@@ -243,9 +240,11 @@ int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* c
         return p->M <= 4 && token_blocks_lds(p->M, p->K, r.f32) <= 65536 ? launch_token_blocks(r, s) : launch_rows_blocks(r, s);
     }
     Room room{static_cast<char*>(workspace)};
+    PackList packs{};
     Product q{};
-    st = operand(x, p->type, p->M, p->K, p->ld_x, room, q.a, s);
-    if (st == FPQ_OK) st = operand_of_blocks(codes, scales, p->N, p->K, false, room, q.b, s);
+    q.a = operand(x, p->type, p->M, p->K, p->ld_x, room, packs);
+    q.b = operand_of_blocks(codes, scales, p->N, p->K, 4, room, packs);
+    st = launch_packs(packs, s);
     if (st != FPQ_OK) return st;
     q.M = p->M;
     q.N = p->N;
@@ -284,10 +283,10 @@ int fpq_linear_backward(const fpq_linear_args_t* p, const void* x, const uint8_t
     Room room{static_cast<char*>(workspace)};
     if (grad_bias) st = launch_column_sums(grad_y, p->type, M, N, stride(p->ld_grad_y, N, M), grad_bias, reinterpret_cast<float*>(room.at), s);
     if (st != FPQ_OK || (!grad_x && !grad_w)) return st;
+    PackList packs{};
     Operand d{};
-    if (M) st = operand(grad_y, p->type, M, N, p->ld_grad_y, room, d, s);
-    if (st != FPQ_OK) return st;
-    return gradients(d, p->type, M, N, K, x, x_scales, stride(p->ld_x, K, M), w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, room, s);
+    if (M) d = operand(grad_y, p->type, M, N, p->ld_grad_y, room, packs);
+    return gradients(d, p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, room, packs, s);
 }
 
 static int check_gated(const fpq_gated_args_t* p)
@@ -326,9 +325,11 @@ int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const flo
         return launch_rows_gated(r, s);
     }
     Room room{static_cast<char*>(workspace)};
+    PackList packs{};
     Product q{};
-    st = operand(x, p->type, M, K, p->ld_x, room, q.a, s);
-    if (st == FPQ_OK) st = operand(w, p->type, 2 * N, K, p->ld_w, room, q.b, s);
+    q.a = operand(x, p->type, M, K, p->ld_x, room, packs);
+    q.b = operand(w, p->type, 2 * N, K, p->ld_w, room, packs);
+    st = packs.count ? launch_packs(packs, s) : FPQ_OK;
     if (st != FPQ_OK) return st;
     q.M = M;
     q.N = N;
@@ -382,7 +383,8 @@ int fpq_gated_backward(const fpq_gated_args_t* p, const void* x, const uint8_t* 
     g.part = reinterpret_cast<float*>(room.at);
     st = launch_gate_backward(g, s);
     if (st != FPQ_OK || !g.d) return st;
-    return gradients(Operand{d, g.ld_d, g.plane}, p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, room, s);
+    PackList packs{};
+    return gradients(Operand{d, g.ld_d, g.plane}, p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, room, packs, s);
 }
 
 int fpq_rms_norm(const fpq_norm_args_t* p, const void* x, const void* residual, const float* w, void* sum, void* y, float* rstd, uint8_t* codes, fpq_format_t f,

@@ -8,9 +8,24 @@ constexpr int64_t kBlock = 32;
 static inline int64_t block_padded(int64_t n) { return (n + kBlock - 1) / kBlock * kBlock; }
 static inline int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
 
-// A matrix for the products: planes of bf16 rows of whole 16-byte pieces, zeros behind the columns.
-int launch_planes(const void* src, int type, int64_t rows, int64_t cols, int64_t ld, __bf16* dst, int64_t ld_dst, int64_t plane, hipStream_t s);
-// The same of blocks (one plane); `eight`: E4M3, else E2M1.
+// Matrices for the products, packed in one launch: planes of bf16 rows of whole 16-byte pieces, zeros behind the columns; of fp32 or bf16
+// matrices, or of blocks (one plane; `scales`).
+struct PackItem {
+    const void* src;
+    const uint8_t* scales;
+    int64_t rows, cols, ld;
+    __bf16* dst;
+    int64_t ld_dst, plane;
+    int64_t first;              // workgroup of the launch
+    int kind;                   // FPQ_TYPE_FP32, FPQ_TYPE_BF16, or 8 or 4: blocks
+    int vec;
+};
+struct PackList {
+    PackItem m[3];
+    int count;
+};
+int launch_packs(PackList& p, hipStream_t s);
+// `eight`: E4M3 blocks, else E2M1.
 int launch_decode(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, bool eight, void* dst, int f32, int64_t ld_dst, hipStream_t s);
 int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t ld, bool eight, const uint8_t* mask, uint8_t* codes, uint8_t* scales,
                           hipStream_t s);

@@ -55,17 +55,6 @@ __device__ __forceinline__ void store_planes(__bf16* dst, int64_t plane, const f
     for (int p = 0; p < NP; ++p) *reinterpret_cast<v8bf*>(dst + p * plane) = f.p[p];
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void planes_kernel(const T* src, int64_t rows, int64_t cols, int64_t ld, __bf16* dst, int64_t ld_dst, int64_t plane, int vec)
-{
-    const int64_t per = ld_dst / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= rows * per) return;
-    const int64_t r = id / per, k = (id - r * per) * 8;
-    float v[8];
-    load8(src + r * ld, k, cols, vec, v);
-    store_planes<kPlanes<T>>(dst + r * ld_dst + k, plane, v);
-}
-
 // Eight codes of a block.
 template <bool EIGHT>
 __device__ __forceinline__ void decode8(const uint8_t* codes, int64_t at, float s, float (&v)[8])
@@ -90,6 +79,25 @@ __device__ __forceinline__ void decode8(const uint8_t* codes, int64_t at, float 
             v[e] = __uint_as_float(bits) * 0x1p126f * s;
         }
     }
+}
+
+__global__ __launch_bounds__(256) void pack_kernel(PackList p)
+{
+    const PackItem& q = p.count > 2 && blockIdx.x >= p.m[2].first ? p.m[2] : p.count > 1 && blockIdx.x >= p.m[1].first ? p.m[1] : p.m[0];
+    const int64_t per = q.ld_dst / 8, id = (int64_t)(blockIdx.x - q.first) * 256 + threadIdx.x;
+    if (id >= q.rows * per) return;
+    const int64_t r = id / per, k = (id - r * per) * 8;
+    __bf16* const dst = q.dst + r * q.ld_dst + k;
+    float v[8];
+    if (q.kind == FPQ_TYPE_FP32) {
+        load8(static_cast<const float*>(q.src) + r * q.ld, k, q.cols, q.vec, v);
+        store_planes<3>(dst, q.plane, v);
+        return;
+    }
+    if (q.kind == FPQ_TYPE_BF16) load8(static_cast<const __bf16*>(q.src) + r * q.ld, k, q.cols, q.vec, v);
+    else if (q.kind == 8) decode8<true>(static_cast<const uint8_t*>(q.src), id * 8, scale_of(q.scales[id / 4]), v);
+    else decode8<false>(static_cast<const uint8_t*>(q.src), id * 8, scale_of(q.scales[id / 4]), v);
+    store_planes<1>(dst, 0, v);
 }
 
 template <bool EIGHT, typename T>
@@ -140,7 +148,9 @@ __global__ __launch_bounds__(256) void block_quantize_kernel(const T* x, int64_t
 
 constexpr int kStripColumns = 512;
 
-__device__ __forceinline__ void strip_sum(float (&sum)[8], int64_t k, int64_t cols, float* part)
+// WIDE: a lane has eight neighbouring columns; else a column of each of eight groups of 64.
+template <bool WIDE>
+__device__ __forceinline__ void strip_sum(float (&sum)[8], int64_t first, int64_t cols, float* part)
 {
     __shared__ float room[3][64 * 8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -154,7 +164,8 @@ __device__ __forceinline__ void strip_sum(float (&sum)[8], int64_t k, int64_t co
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float t = (sum[e] + room[0][e * 64 + lane]) + (room[1][e * 64 + lane] + room[2][e * 64 + lane]);
-        if (k + e < cols) part[k + e] = t;
+        const int64_t k = WIDE ? first + 8 * lane + e : first + 64 * e + lane;
+        if (k < cols) part[k] = t;
     }
 }
 
@@ -181,7 +192,7 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const T* x, int64_t M,
             for (int e = 0; e < 8; ++e) sum[e] += v[e];
         }
     }
-    strip_sum(sum, k, N, part + (int64_t)blockIdx.y * N);
+    strip_sum<true>(sum, (int64_t)blockIdx.x * kStripColumns, N, part + (int64_t)blockIdx.y * N);
 }
 
 // 64 columns, 16 wavefronts over the parts
@@ -209,40 +220,63 @@ __global__ __launch_bounds__(1024) void part_sums_kernel(const float* part, int 
     out[k] = sum;
 }
 
-// KEPT: 0 the type, 1 blocks
-template <typename T, int KEPT>
-__global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward p, int64_t rows, int vec, int vec_d)
+// KEPT: 0 the type, 1 blocks.  WIDE: a lane has eight neighbouring columns of rows that are whole pieces; else, one column of each of eight
+// neighbouring groups of 64, so that a wavefront's accesses are whole lines either way.
+template <typename T, int KEPT, bool WIDE>
+__global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward p, int64_t rows)
 {
-    const int64_t k = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8, m1 = min(p.M, (int64_t)(blockIdx.y + 1) * rows), N = p.N;
-    const int64_t np = (N + 31) / 32 * 32;
+    const int lane = threadIdx.x & 63;
+    const int64_t first = (int64_t)blockIdx.x * kStripColumns, m1 = min(p.M, (int64_t)(blockIdx.y + 1) * rows), N = p.N;
+    const int64_t k = first + 8 * lane, np = (N + 31) / 32 * 32;
+    constexpr int NP = kPlanes<T>;
+    auto col = [&](int e) { return WIDE ? k + e : first + 64 * e + lane; };
     float sum_a[8] = {}, sum_g[8] = {};
-    if (k < N)
+    if (!WIDE || k < N)
         for (int64_t m = (int64_t)blockIdx.y * rows + (threadIdx.x >> 6); m < m1; m += 4) {
             float a[8], g[8], gh[8], da[8], dg[8];
-            load8(static_cast<const T*>(p.gh) + m * p.ld_gh, k, N, vec & 1, gh);
-            if constexpr (KEPT) {
-                const uint8_t* const s = p.pre_scales + m * (np / 16) + k / 32;
-                const uint8_t* const c = static_cast<const uint8_t*>(p.pre) + m * 2 * np;
-                decode8<true>(c, k, scale_of(s[0]), a);
-                decode8<true>(c + np, k, scale_of(s[np / 32]), g);
+            const T* const up = static_cast<const T*>(p.gh) + m * p.ld_gh;
+            if constexpr (WIDE) {
+                load8(up, k, N, true, gh);
+                if constexpr (KEPT) {
+                    const uint8_t* const s = p.pre_scales + m * (np / 16) + k / 32;
+                    const uint8_t* const c = static_cast<const uint8_t*>(p.pre) + m * 2 * np;
+                    decode8<true>(c, k, scale_of(s[0]), a);
+                    decode8<true>(c + np, k, scale_of(s[np / 32]), g);
+                } else {
+                    const T* const row = static_cast<const T*>(p.pre) + m * 2 * N;
+                    load8(row, k, N, true, a);
+                    load8(row + N, k, N, true, g);
+                }
             } else {
-                const T* const row = static_cast<const T*>(p.pre) + m * 2 * N;
-                load8(row, k, N, vec & 2, a);
-                load8(row + N, k, N, vec & 2, g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int64_t c = col(e);
+                    const bool in = c < N;
+                    gh[e] = in ? (float)up[c] : 0.0f;
+                    if constexpr (KEPT) {
+                        const uint8_t* const s = p.pre_scales + m * (np / 16) + c / 32;
+                        const uint8_t* const q = static_cast<const uint8_t*>(p.pre) + m * 2 * np + c;
+                        a[e] = in ? __builtin_amdgcn_cvt_f32_fp8(q[0], 0) * scale_of(s[0]) : 0.0f;
+                        g[e] = in ? __builtin_amdgcn_cvt_f32_fp8(q[np], 0) * scale_of(s[np / 32]) : 0.0f;
+                    } else {
+                        const T* const row = static_cast<const T*>(p.pre) + m * 2 * N;
+                        a[e] = in ? (float)row[c] : 0.0f;
+                        g[e] = in ? (float)row[N + c] : 0.0f;
+                    }
+                }
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float slope;
                 da[e] = gh[e] * gate_of<true>(p.act, g[e], &slope);
                 dg[e] = gh[e] * a[e] * slope;
-                if (k + e >= N) da[e] = dg[e] = 0.0f;
+                if (!WIDE && col(e) >= N) da[e] = dg[e] = 0.0f;
                 sum_a[e] += da[e];
                 sum_g[e] += dg[e];
             }
             if (!p.d) continue;
             __bf16* const d = p.d + m * p.ld_d;
-            constexpr int NP = kPlanes<T>;
-            if (vec_d) {
+            if constexpr (WIDE) {
                 store_planes<NP>(d + k, p.plane, da);
                 store_planes<NP>(d + N + k, p.plane, dg);
             } else {
@@ -250,20 +284,21 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward p, int6
 #pragma unroll
                 for (int q = 0; q < NP; ++q)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (k + e < N) {
-                            d[q * p.plane + k + e] = fa.p[q][e];
-                            d[q * p.plane + N + k + e] = fg.p[q][e];
+                    for (int e = 0; e < 8; ++e) {
+                        const int64_t c = col(e);
+                        if (c < N) {
+                            d[q * p.plane + c] = fa.p[q][e];
+                            d[q * p.plane + N + c] = fg.p[q][e];
+                        } else if (c < N + p.ld_d - 2 * N) {         // zeros behind the row
+                            d[q * p.plane + N + c] = (__bf16)0.0f;
                         }
-                if (k + 8 >= N)                                     // zeros behind the row
-                    for (int q = 0; q < NP; ++q)
-                        for (int64_t c = 2 * N; c < p.ld_d; ++c) d[q * p.plane + c] = (__bf16)0.0f;
+                    }
             }
         }
     if (!p.part) return;
     float* const part = p.part + (int64_t)blockIdx.y * 2 * N;
-    strip_sum(sum_a, k, N, part);
-    strip_sum(sum_g, k, N, part + N);
+    strip_sum<WIDE>(sum_a, first, N, part);
+    strip_sum<WIDE>(sum_g, first, N, part + N);
 }
 
 unsigned grid256(int64_t n) { return (unsigned)((n + 255) / 256); }
@@ -275,13 +310,27 @@ int launched() { return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNC
 
 }  // namespace
 
-int launch_planes(const void* src, int type, int64_t rows, int64_t cols, int64_t ld, __bf16* dst, int64_t ld_dst, int64_t plane, hipStream_t s)
+int launch_packs(PackList& p, hipStream_t s)
 {
-    const unsigned grid = grid256(rows * (ld_dst / 8));
-    if (!grid) return FPQ_OK;
-    const int vec = rows_vec(src, ld, type);
-    if (type == FPQ_TYPE_FP32) planes_kernel<<<dim3(grid), dim3(256), 0, s>>>(static_cast<const float*>(src), rows, cols, ld, dst, ld_dst, plane, vec);
-    else planes_kernel<<<dim3(grid), dim3(256), 0, s>>>(static_cast<const __bf16*>(src), rows, cols, ld, dst, ld_dst, plane, vec);
+    int64_t at = 0;
+    for (int i = 0; i < p.count; ++i) {
+        PackItem& q = p.m[i];
+        q.first = at;
+        q.vec = q.kind != 8 && q.kind != 4 && rows_vec(q.src, q.ld, q.kind);
+        const int64_t blocks = (q.rows * (q.ld_dst / 8) + 255) / 256;
+        if (at && at + blocks >= (int64_t)1 << 24) {                 // (a launch has fewer than 2^32 threads)
+            PackList one{{p.m[i]}, 1};
+            const int st = launch_packs(one, s);
+            if (st != FPQ_OK) return st;
+            for (int j = i + 1; j < p.count; ++j) p.m[j - 1] = p.m[j];
+            --p.count;
+            --i;
+            continue;
+        }
+        at += blocks;
+    }
+    if (!at) return FPQ_OK;
+    pack_kernel<<<dim3((unsigned)at), dim3(256), 0, s>>>(p);
     return launched();
 }
 
@@ -343,12 +392,17 @@ int launch_gate_backward(const GateBackward& p, hipStream_t s)
 {
     const RowParts r = row_parts(p.M, p.N);
     const dim3 grid((unsigned)((p.N + kStripColumns - 1) / kStripColumns), (unsigned)r.parts);
-    const int vec = (rows_vec(p.gh, p.ld_gh, p.type) ? 1 : 0) | (rows_vec(p.pre, p.N, p.type) ? 2 : 0), vec_d = p.N % 8 == 0;
+    const bool wide = p.N % 8 == 0 && rows_vec(p.gh, p.ld_gh, p.type) && (p.pre_scales || rows_vec(p.pre, p.N, p.type));
     GateBackward q = p;
     if (!p.grad_bias) q.part = nullptr;
-    auto run = [&](auto kernel) { kernel<<<grid, dim3(256), 0, s>>>(q, r.rows, vec, vec_d); };
-    if (p.type == FPQ_TYPE_FP32) p.pre_scales ? run(gate_backward_kernel<float, 1>) : run(gate_backward_kernel<float, 0>);
-    else p.pre_scales ? run(gate_backward_kernel<__bf16, 1>) : run(gate_backward_kernel<__bf16, 0>);
+    auto run = [&](auto kernel) { kernel<<<grid, dim3(256), 0, s>>>(q, r.rows); };
+    auto kept = [&](auto t, auto w) {
+        using T = decltype(t);
+        constexpr bool W = decltype(w)::value;
+        p.pre_scales ? run(gate_backward_kernel<T, 1, W>) : run(gate_backward_kernel<T, 0, W>);
+    };
+    if (p.type == FPQ_TYPE_FP32) wide ? kept(0.0f, std::true_type()) : kept(0.0f, std::false_type());
+    else wide ? kept((__bf16)0.0f, std::true_type()) : kept((__bf16)0.0f, std::false_type());
     const int st = launched();
     return st == FPQ_OK && q.part ? launch_part_sums(q.part, r.parts, 2 * p.N, p.grad_bias, s) : st;
 }

@@ -264,32 +264,37 @@ struct RowStage {
     }
 };
 
-// Four results of each q = 0 .. 3 of 32 rows from column n on, in the type.
+// Four results of each q = 0 .. 3 of 32 rows from column n on, in the type.  `pieces`: rows are whole aligned pieces of 16 bytes; others are
+// stored an element at a time, 32 lanes to a row.
 template <typename F>
 __device__ __forceinline__ void put_rows(char* room, void* out, int64_t ld, int f32, int64_t m0, int rows, int n, int N, bool pieces, F&& value)
 {
-    const int lane = threadIdx.x & 63, h = lane >> 5, left = min(N - n, 32);
-    if (f32) {
-        if (pieces) {
-            const RowStage<128> s{room};
-#pragma unroll
-            for (int q = 0; q < 4; ++q) s.put(q, make_float4(value(4 * q), value(4 * q + 1), value(4 * q + 2), value(4 * q + 3)));
-            s.flush(reinterpret_cast<char*>(static_cast<float*>(out) + m0 * ld + n), 4 * ld, rows, 4 * left);
-            return;
+    const int lane = threadIdx.x & 63, left = min(N - n, 32);
+    auto elements = [&](auto* to, int stride) {
+        using T = std::remove_reference_t<decltype(*to)>;
+        asm volatile("" ::: "memory");
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+            const int r = 2 * i + (lane >> 5), c = lane & 31;
+            const T v = reinterpret_cast<const T*>(room + r * stride)[c];
+            if (r < rows && c < left) to[r * ld + c] = v;
         }
-    } else if (pieces) {
+        asm volatile("" ::: "memory");
+    };
+    if (f32) {
+        float* const to = static_cast<float*>(out) + m0 * ld + n;
+        const RowStage<128> s{room};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s.put(q, make_float4(value(4 * q), value(4 * q + 1), value(4 * q + 2), value(4 * q + 3)));
+        if (pieces) s.flush(reinterpret_cast<char*>(to), 4 * ld, rows, 4 * left);
+        else elements(to, s.STRIDE);
+    } else {
+        uint16_t* const to = static_cast<uint16_t*>(out) + m0 * ld + n;
         const RowStage<64> s{room};
 #pragma unroll
         for (int q = 0; q < 4; ++q) s.put(q, make_uint2(pair_bf16(value(4 * q), value(4 * q + 1)), pair_bf16(value(4 * q + 2), value(4 * q + 3))));
-        s.flush(reinterpret_cast<char*>(static_cast<__bf16*>(out) + m0 * ld + n), 2 * ld, rows, 2 * left);
-        return;
-    }
-    if ((lane & 31) >= rows) return;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const float v[4] = {value(4 * q), value(4 * q + 1), value(4 * q + 2), value(4 * q + 3)};
-        const int c = n + 8 * q + 4 * h;
-        if (c < N) put4(out, (m0 + (lane & 31)) * ld + c, f32, c, N, false, v);
+        if (pieces) s.flush(reinterpret_cast<char*>(to), 2 * ld, rows, 2 * left);
+        else elements(to, s.STRIDE);
     }
 }
 

@@ -22,27 +22,29 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, b
         int64_t most = (int64_t)(steps / 8 < 16 ? steps / 8 : 16), slices = 512 / n < most ? 512 / n : most;
         return Plan{kTile32, slices > 1 ? (int)slices : 1};
     }
-    // What a call takes, in microseconds: rounds of workgroups over 256 compute units, at 0.45 us for 128 x 128 x 64 on one (1.2 PFLOP/s on
-    // all).  A workgroup of 256 or 192 rows has its compute unit alone, and four steps' time of its own at its start and end; two of 128 rows
-    // share one, hide half of that behind each other and take 1.2 of the time.  Slices cost the partial results' way to memory and back and a launch.
+    // What a call takes, in microseconds: rounds of as many workgroups as run at once, each of steps / slices and what a workgroup needs
+    // at its start and end.  A step of 64 k takes `full` where the chip is full (1.2 PFLOP/s) and no less than `alone`; a round that is not full, its
+    // share.  Workgroups of 256 and 192 rows have their compute unit alone; two of 128 rows share one and hide one's waits behind the other, or one with
+    // a ring of four stages has it alone.  Slices cost the partial results' way to memory and back and a launch.  (Measured: 2048 x 4096 with 64
+    // steps 1.07 of 192 rows; 1280 x 1280 with 192 steps 1.09 of 256 rows, 0.66 of 128 and 0.43 deep.)
+    struct Kind {
+        int tile, at_once;
+        double full, alone, ends;
+    };
+    static const Kind kinds[] = {{kTile256, 256, 1.8, 1.2, 4}, {kTile192, 256, 1.35, 1.05, 4}, {kTile128, 512, 1.08, 0.66, 2}, {kTile128Deep, 256, 0.56, 0.43, 3}};
     Plan best{kTile128, 1};
     double least = 1e30;
-    for (int t : {kTile256, kTile192, kTile128}) {
-        if (t == kTile192 && col_a) continue;
+    for (const Kind& k : kinds) {
+        if (k.tile == kTile192 && col_a) continue;
         for (int s = 1; s <= 32; s = s < 4 ? s + 1 : s + s / 4) {
             if (s > 1 && steps / s < 8) break;
-            const int64_t n = tiles(t) * s;
-            double us;
-            if (t == kTile128) {
-                const int64_t rest = n % 512;
-                us = ((double)(n / 512) * 2 + (rest == 0 ? 0.0 : rest <= 256 ? 1.25 : 2.0)) * 0.45 * 1.2 * (steps / s + 2);
-            } else {
-                us = (double)((n + 255) / 256) * (kTileM[t] / 64) * 0.45 * (steps / s + 4);
-            }
+            const int64_t n = tiles(k.tile) * s, rest = n % k.at_once;
+            const double part = k.full * rest / k.at_once;
+            double us = ((double)(n / k.at_once) * k.full + (rest ? (part > k.alone ? part : k.alone) : 0.0)) * (steps / s + k.ends);
             if (s > 1) us += 4 + (double)s * M * N * (gated ? 2 : 1) * 8 / 4.5e6;
             if (us < least) {
                 least = us;
-                best = Plan{t, s};
+                best = Plan{k.tile, s};
             }
         }
     }

@@ -5,8 +5,8 @@
 namespace fpq {
 
 // Tiles: results of a workgroup.
-enum MatmulTile : int { kTile256 = 0, kTile192 = 1, kTile128 = 2, kTile32 = 3 };
-constexpr int kTileM[4] = {256, 192, 128, 32}, kTileN[4] = {256, 256, 128, 256};
+enum MatmulTile : int { kTile256 = 0, kTile192 = 1, kTile128 = 2, kTile128Deep = 3, kTile32 = 4 };
+constexpr int kTileM[5] = {256, 192, 128, 128, 32}, kTileN[5] = {256, 256, 128, 128, 256};
 
 template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int END>
 int launch_matmul_tile(MatmulArgs p, hipStream_t s)
@@ -29,6 +29,7 @@ int launch_matmul_form(const MatmulArgs& p, int tile, hipStream_t s)
         if (tile == kTile192) return launch_matmul_tile<COLA, COLB, 192, 256, 2, 4, 64, 2, END>(p, s);
         if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, 32, 4, END>(p, s);
     }
+    if (tile == kTile128Deep) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 4, END>(p, s);
     return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 2, END>(p, s);
 }
 
