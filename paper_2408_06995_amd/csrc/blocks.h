@@ -68,6 +68,7 @@ struct NormArgs {
     int64_t first;              // row of a launch
     float eps;
     int vec;                    // all rows may be taken 16 bytes at a time
+    int past;                   // results are stored past the L2
 };
 int launch_norm(const NormArgs& p, int type, hipStream_t s);
 struct NormBackward {
@@ -77,7 +78,7 @@ struct NormBackward {
     void* gx;
     float *gw, *part;
     int64_t M, K, ld_sum, ld_gy, ld_gs, ld_gx;
-    int vec;
+    int vec, past;
 };
 size_t norm_part_bytes(int64_t M, int64_t K);
 int launch_norm_backward(const NormBackward& p, int type, hipStream_t s);

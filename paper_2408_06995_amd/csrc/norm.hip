@@ -13,38 +13,54 @@ namespace {
 template <typename T>
 constexpr int kPiece = 16 / (int)sizeof(T);
 
-// Elements k .. of a row; zeros from K on.  VEC: rows are whole aligned pieces.
+// Elements k .. of a row as they lie in memory, zeros from K on; and as numbers.  VEC: rows are whole aligned pieces.
+template <typename T, bool VEC>
+__device__ __forceinline__ uint4 raw_piece(const T* row, int64_t k, int64_t K)
+{
+    constexpr int E = kPiece<T>;
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if constexpr (VEC) {
+        if (k < K) x = *reinterpret_cast<const uint4*>(row + k);
+    } else {
+        T v[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = k + e < K ? row[k + e] : (T)0.0f;
+        __builtin_memcpy(&x, v, 16);
+    }
+    return x;
+}
+template <typename T>
+__device__ __forceinline__ void numbers(const uint4& x, float (&v)[kPiece<T>])
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        if constexpr (sizeof(T) == 4) {
+            v[t] = __uint_as_float(w[t]);
+        } else {
+            v[2 * t] = __uint_as_float(w[t] << 16);
+            v[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
+        }
+    }
+}
 template <typename T, bool VEC>
 __device__ __forceinline__ void piece(const T* row, int64_t k, int64_t K, float (&v)[kPiece<T>])
 {
-    constexpr int E = kPiece<T>;
-    if constexpr (VEC) {
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (k < K) x = *reinterpret_cast<const uint4*>(row + k);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            if constexpr (E == 4) {
-                v[t] = __uint_as_float(w[t]);
-            } else {
-                v[2 * t] = __uint_as_float(w[t] << 16);
-                v[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = k + e < K ? (float)row[k + e] : 0.0f;
-    }
+    numbers<T>(raw_piece<T, VEC>(row, k, K), v);
 }
 
+// `past`: results that the L2 cannot hold go past it (kPast).
 template <typename T, bool VEC>
-__device__ __forceinline__ void put(T* row, int64_t k, int64_t K, const float (&v)[kPiece<T>])
+__device__ __forceinline__ void put(T* row, int64_t k, int64_t K, const float (&v)[kPiece<T>], int past)
 {
     constexpr int E = kPiece<T>;
     if constexpr (VEC) {
         if (k >= K) return;
-        if constexpr (E == 4) *reinterpret_cast<float4*>(row + k) = make_float4(v[0], v[1], v[2], v[3]);
-        else *reinterpret_cast<uint4*>(row + k) = make_uint4(pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]), pair_bf16(v[4], v[5]), pair_bf16(v[6], v[7]));
+        v4i o;
+        if constexpr (E == 4) o = v4i{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
+        else o = v4i{(int)pair_bf16(v[0], v[1]), (int)pair_bf16(v[2], v[3]), (int)pair_bf16(v[4], v[5]), (int)pair_bf16(v[6], v[7])};
+        if (past) __builtin_nontemporal_store(o, reinterpret_cast<v4i*>(row + k));
+        else *reinterpret_cast<v4i*>(row + k) = o;
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -71,15 +87,17 @@ __device__ __forceinline__ void weights(const float* w, int64_t k, int64_t K, fl
     }
 }
 
-// The sum over a row's threads: 64 of a wavefront, or the 256 of the workgroup (`room`: four values of this call's own).
+// The sum over a row's TPR threads: neighbours in a wavefront, or two or four wavefronts (`room`: four values of this call's own).
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* room)
 {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    if constexpr (TPR == 64) return v;
-    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    for (int off = (TPR < 64 ? TPR : 64) / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    if constexpr (TPR <= 64) return v;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) room[wave] = v;
     __syncthreads();
+    if constexpr (TPR == 128) return room[wave & 2] + room[wave | 1];
     return (room[0] + room[1]) + (room[2] + room[3]);
 }
 
@@ -90,11 +108,11 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs p)
     constexpr int E = kPiece<T>, RPB = 256 / TPR;
     __shared__ float room[4];
     const int t = threadIdx.x % TPR;
-    const int64_t m = p.first + (int64_t)blockIdx.x * RPB + threadIdx.x / TPR, K = p.K;
-    if (m >= p.M) return;                                             // (whole wavefronts; with TPR 256 none)
+    const int64_t row = p.first + (int64_t)blockIdx.x * RPB + threadIdx.x / TPR, m = min(row, p.M - 1), K = p.K;
+    const bool in = row < p.M;                                        // (others take part in sums, and store nothing)
     const T* const x = static_cast<const T*>(p.x) + m * p.ld_x;
     const T* const res = p.residual ? static_cast<const T*>(p.residual) + m * p.ld_residual : nullptr;
-    T* const sum = p.sum ? static_cast<T*>(p.sum) + m * p.ld_sum : nullptr;
+    T* const sum = p.sum && in ? static_cast<T*>(p.sum) + m * p.ld_sum : nullptr;
     // columns that are written: codes go on behind the row
     const int64_t span = p.codes ? (p.code_scales ? (K + 31) / 32 * 32 : (K + 15) / 16 * 16) : K;
 
@@ -114,7 +132,7 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs p)
         weights<T>(p.w, k, K, w);
 #pragma unroll
         for (int e = 0; e < E; ++e) y[e] = v[e] * rstd * w[e];
-        if (p.y) put<T, VEC>(static_cast<T*>(p.y) + m * p.ld_y, k, K, y);
+        if (p.y && in) put<T, VEC>(static_cast<T*>(p.y) + m * p.ld_y, k, K, y, p.past);
         if (!p.codes) return;
         uint32_t q[E / 4];
         if (p.code_scales) {
@@ -126,14 +144,14 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs p)
             }
 #pragma unroll
             for (int off = 1; off < 32 / E; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
-            if (k >= span) return;
+            if (k >= span || !in) return;
             const uint32_t s = block_scale8(top);
             const float i = inverse_scale(s);
             if (k % 32 == 0) p.code_scales[m * (span / 32) + k / 32] = (uint8_t)s;
 #pragma unroll
             for (int e = 0; e < E; e += 4) q[e / 4] = codes8(y[e] * i, y[e + 1] * i, y[e + 2] * i, y[e + 3] * i);
         } else {
-            if (k >= span) return;
+            if (k >= span || !in) return;
             auto bound = [&](int e) { return k + e < K ? fminf(fmaxf(__fmul_rn(y[e], c), -448.0f), 448.0f) : 0.0f; };
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
@@ -161,10 +179,10 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs p)
         for (int i = 0; i < CH; ++i) {
 #pragma unroll
             for (int e = 0; e < E; ++e) ss = fmaf(v[i][e], v[i][e], ss);
-            if (sum) put<T, VEC>(sum, (int64_t)(t + TPR * i) * E, K, v[i]);
+            if (sum) put<T, VEC>(sum, (int64_t)(t + TPR * i) * E, K, v[i], p.past);
         }
         const float rstd = 1.0f / sqrtf(row_sum<TPR>(ss, room) / (float)K + p.eps);
-        if (p.rstd && t == 0) p.rstd[m] = rstd;
+        if (p.rstd && in && t == 0) p.rstd[m] = rstd;
 #pragma unroll
         for (int i = 0; i < CH; ++i) finish((int64_t)(t + TPR * i) * E, v[i], rstd);
     } else {
@@ -175,10 +193,10 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs p)
             stream(k, v);
 #pragma unroll
             for (int e = 0; e < E; ++e) ss = fmaf(v[e], v[e], ss);
-            if (sum) put<T, VEC>(sum, k, K, v);
+            if (sum) put<T, VEC>(sum, k, K, v, p.past);
         }
         const float rstd = 1.0f / sqrtf(row_sum<TPR>(ss, room) / (float)K + p.eps);
-        if (p.rstd && t == 0) p.rstd[m] = rstd;
+        if (p.rstd && in && t == 0) p.rstd[m] = rstd;
         for (int64_t i = 0; i < rounds; ++i) {
             const int64_t k = (t + TPR * i) * E;
             if (sum) piece<T, VEC>(sum, k, K, v);
@@ -194,6 +212,7 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackward p, int 
 {
     constexpr int E = kPiece<T>, RPB = 256 / TPR;
     __shared__ float room[2][4];
+    __shared__ float all[CH > 0 && RPB > 1 ? 256 * CH * E : 1];
     const int t = threadIdx.x % TPR;
     const int64_t K = p.K;
     const float over = 1.0f / (float)K;
@@ -207,44 +226,65 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackward p, int 
             for (int e = 0; e < E; ++e) gw[i][e] = 0.0f;
         }
     }
+    // A row's pieces as they come from memory, a row ahead.
+    uint4 rv[C], rg[C], ru[C];
+    auto load = [&](int64_t first) {
+        const int64_t m = min(first + threadIdx.x / TPR, p.M - 1);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int64_t k = (int64_t)(t + TPR * i) * E;
+            rv[i] = raw_piece<T, VEC>(static_cast<const T*>(p.sum) + m * p.ld_sum, k, K);
+            rg[i] = raw_piece<T, VEC>(static_cast<const T*>(p.gy) + m * p.ld_gy, k, K);
+            ru[i] = p.gs ? raw_piece<T, VEC>(static_cast<const T*>(p.gs) + m * p.ld_gs, k, K) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    const int64_t begin = (int64_t)blockIdx.x * RPB, stride = (int64_t)gridDim.x * RPB;
+    if constexpr (CH > 0) load(begin);
     int flip = 0;
-    for (int64_t m = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; m < p.M; m += (int64_t)gridDim.x * RPB) {
+    for (int64_t first = begin; first < p.M; first += stride) {
+        const int64_t row = first + threadIdx.x / TPR, m = min(row, p.M - 1);
+        const bool in = row < p.M;                                    // (others take part in sums, and give nothing)
         const T* const r = static_cast<const T*>(p.sum) + m * p.ld_sum;
         const T* const gy = static_cast<const T*>(p.gy) + m * p.ld_gy;
         const T* const gs = p.gs ? static_cast<const T*>(p.gs) + m * p.ld_gs : nullptr;
-        T* const gx = p.gx ? static_cast<T*>(p.gx) + m * p.ld_gx : nullptr;
+        T* const gx = p.gx && in ? static_cast<T*>(p.gx) + m * p.ld_gx : nullptr;
         const float rstd = p.rstd[m];
         auto finish = [&](int64_t k, const float (&g)[E], const float (&v)[E], const float (&u)[E], float c) {
             float o[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = fmaf(rstd, fmaf(-v[e], c, g[e]), u[e]);
-            put<T, VEC>(gx, k, K, o);
+            put<T, VEC>(gx, k, K, o, p.past);
         };
         if constexpr (CH > 0) {
-            float v[CH][E], g[CH][E], u[CH][E], dot = 0.0f;
+            uint4 nv[C], ng[C], nu[C];
+#pragma unroll
+            for (int i = 0; i < C; ++i) nv[i] = rv[i], ng[i] = rg[i], nu[i] = ru[i];
+            if (first + stride < p.M) load(first + stride);
+            float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int64_t k = (int64_t)(t + TPR * i) * E;
-                piece<T, VEC>(r, k, K, v[i]);
-                piece<T, VEC>(gy, k, K, g[i]);
-                if (gs) piece<T, VEC>(gs, k, K, u[i]);
-                else
-#pragma unroll
-                    for (int e = 0; e < E; ++e) u[i][e] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
+                float v[E], g[E];
+                numbers<T>(nv[i], v);
+                numbers<T>(ng[i], g);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    gw[i][e] = fmaf(g[i][e] * v[i][e], rstd, gw[i][e]);
-                    g[i][e] *= w[i][e];
-                    dot = fmaf(g[i][e], v[i][e], dot);
+                    gw[i][e] = fmaf(g[e] * v[e], in ? rstd : 0.0f, gw[i][e]);
+                    dot = fmaf(g[e] * w[i][e], v[e], dot);
                 }
+            }
             const float c = row_sum<TPR>(dot, room[flip]) * over * rstd * rstd;
             flip ^= 1;
             if (gx)
 #pragma unroll
-                for (int i = 0; i < CH; ++i) finish((int64_t)(t + TPR * i) * E, g[i], v[i], u[i], c);
+                for (int i = 0; i < CH; ++i) {
+                    float v[E], g[E], u[E];
+                    numbers<T>(nv[i], v);
+                    numbers<T>(ng[i], g);
+                    numbers<T>(nu[i], u);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) g[e] *= w[i][e];
+                    finish((int64_t)(t + TPR * i) * E, g, v, u, c);
+                }
         } else {
             const int64_t pieces = (K + E - 1) / E;
             float v[E], g[E], u[E], y[E], dot = 0.0f;
@@ -274,13 +314,28 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackward p, int 
     }
     if constexpr (CH > 0) {
         if (!own_sums) return;
-        float* const part = p.part + ((int64_t)blockIdx.x * RPB + threadIdx.x / TPR) * K;
+        float* const part = p.part + (int64_t)blockIdx.x * K;
+        if constexpr (RPB == 1) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int64_t k = (int64_t)(t + TPR * i) * E;
+            for (int i = 0; i < CH; ++i) {
+                const int64_t k = (int64_t)(t + TPR * i) * E;
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (k + e < K) part[k + e] = gw[i][e];
+                for (int e = 0; e < E; ++e)
+                    if (k + e < K) part[k + e] = gw[i][e];
+            }
+        } else {
+            // the workgroup's rows, one after the other: [row][column]
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) all[threadIdx.x / TPR * (TPR * CH * E) + (t + TPR * i) * E + e] = gw[i][e];
+            __syncthreads();
+            for (int k = threadIdx.x; k < K; k += 256) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int r = 0; r < RPB; ++r) sum += all[r * (TPR * CH * E) + k];
+                part[k] = sum;
+            }
         }
     }
 }
@@ -297,40 +352,51 @@ __global__ __launch_bounds__(256) void norm_weights_kernel(NormBackward p, int64
     p.part[(int64_t)blockIdx.y * p.K + k] = sum;
 }
 
+// Results larger than the L2 (8 x 4 MB) leave no line of theirs there for a reader, and push the rows that are read out: stored past it, 32768 rows of 320 in
+// bf16 take 15.6 us for 19.7, 8192 of 5120 with their gradient 131 for 144.
+constexpr int64_t kPast = (int64_t)32 << 20;
 constexpr int64_t kMostRowsAtOnce = (int64_t)1 << 23;
 
 // Threads per row and pieces per thread (0: two passes).
 struct Shape {
     int tpr, ch;
 };
-Shape shape_of(int64_t M, int64_t span, int piece)
+// Widths of 320 2^n and of powers of two leave no thread of a group without a piece: five or four of them each; few rows are spread over more
+// threads.  (32768 rows of 320 in bf16: 22.5 us with one piece for 40 of 64 threads, 19.7 with five for eight.)
+constexpr Shape kShapes[] = {{8, 4}, {8, 5}, {16, 4}, {16, 5}, {32, 4}, {32, 5}, {64, 4}, {64, 5}, {128, 4}, {128, 5}, {256, 4}, {256, 5}};
+constexpr Shape kFewShapes[] = {{64, 1}, {256, 1}, {256, 2}, {256, 4}, {256, 5}};
+constexpr Shape kPlainShapes[] = {{64, 1}, {64, 4}, {256, 4}};           // rows that are no whole pieces
+// (the backward kernel holds three tensors' pieces, those of the next row and two rows of sums and weights: no more than three pieces if they suffice)
+constexpr Shape kBackwardShapes[] = {{16, 3}, {32, 2}, {32, 3}, {64, 2}, {64, 3}, {128, 2}, {128, 3}, {256, 2}, {256, 3}, {256, 4}, {256, 5}};
+Shape shape_of(int64_t M, int64_t span, int piece, bool vec, bool back)
 {
     const int64_t pieces = (span + piece - 1) / piece;
-    if (pieces <= 64 * 4 && (M >= 512 || pieces <= 64)) return Shape{64, pieces <= 64 ? 1 : pieces <= 128 ? 2 : 4};
-    return Shape{256, pieces <= 256 ? 1 : pieces <= 512 ? 2 : pieces <= 1024 ? 4 : 0};
+    auto first = [&](const auto& list) {
+        for (const Shape& s : list)
+            if ((int64_t)s.tpr * s.ch >= pieces) return s;
+        return Shape{256, 0};
+    };
+    return !vec ? first(kPlainShapes) : M * pieces < 65536 ? first(kFewShapes) : back ? first(kBackwardShapes) : first(kShapes);
 }
 
-// Workgroups of the backward kernel, each of which leaves a row (or four) of partial sums.
+// Workgroups of the backward kernel, each of which leaves a row of partial sums.
 int64_t backward_blocks(int64_t M, Shape s)
 {
-    const int64_t rows = 256 / s.tpr, all = (M + rows - 1) / rows, most = s.tpr == 64 ? 256 : 512;
+    const int64_t rows = 256 / s.tpr, all = (M + rows - 1) / rows, most = 512;
     return all < most ? all : most;
 }
 
-template <typename T, bool VEC, typename F>
+template <bool BACK, bool VEC, int I = 0, typename F>
 void with_shape(Shape s, F&& run)
 {
-    auto as = [](auto a, auto b) { return std::pair<decltype(a), decltype(b)>(); };
-    using std::integral_constant;
-    if (s.tpr == 64) {
-        if (s.ch == 1) run(as(integral_constant<int, 64>(), integral_constant<int, 1>()));
-        else if (s.ch == 2) run(as(integral_constant<int, 64>(), integral_constant<int, 2>()));
-        else run(as(integral_constant<int, 64>(), integral_constant<int, 4>()));
-    } else {
-        if (s.ch == 1) run(as(integral_constant<int, 256>(), integral_constant<int, 1>()));
-        else if (s.ch == 2) run(as(integral_constant<int, 256>(), integral_constant<int, 2>()));
-        else if (s.ch == 4) run(as(integral_constant<int, 256>(), integral_constant<int, 4>()));
-        else run(as(integral_constant<int, 256>(), integral_constant<int, 0>()));
+    constexpr Shape fwd[] = {{8, 4}, {8, 5}, {16, 4}, {16, 5}, {32, 4}, {32, 5}, {64, 4}, {64, 5}, {128, 4}, {128, 5}, {256, 4}, {256, 5}, {64, 1}, {256, 1}, {256, 2}, {256, 0}};
+    constexpr Shape bwd[] = {{16, 3}, {32, 2}, {32, 3}, {64, 2}, {64, 3}, {128, 2}, {128, 3}, {256, 2}, {256, 3}, {256, 4}, {256, 5}, {64, 1}, {256, 1}, {256, 0}};
+    constexpr Shape plain[] = {{64, 1}, {64, 4}, {256, 4}, {256, 0}};
+    constexpr int N = !VEC ? 4 : BACK ? 14 : 16;
+    if constexpr (I < N) {
+        constexpr Shape c = !VEC ? plain[I < 4 ? I : 0] : BACK ? bwd[I < 14 ? I : 0] : fwd[I];
+        if (s.tpr == c.tpr && s.ch == c.ch) run(std::pair<std::integral_constant<int, c.tpr>, std::integral_constant<int, c.ch>>());
+        else with_shape<BACK, VEC, I + 1>(s, run);
     }
 }
 
@@ -338,14 +404,15 @@ template <typename T, bool VEC>
 int forward(const NormArgs& p, hipStream_t s)
 {
     const int64_t span = p.codes ? (p.code_scales ? block_padded(p.K) : padded_channels(p.K)) : p.K;
-    const Shape shape = shape_of(p.M, span, kPiece<T>);
+    const Shape shape = shape_of(p.M, span, kPiece<T>, VEC, false);
     const int64_t rows = 256 / shape.tpr;
     // (a launch has fewer than 2^32 threads)
     for (int64_t first = 0; first < p.M; first += kMostRowsAtOnce) {
         NormArgs q = p;
         q.first = first;
+        q.past = p.M * p.K * (int64_t)sizeof(T) * ((p.sum != nullptr) + (p.y != nullptr)) > kPast;
         const dim3 grid((unsigned)(((p.M - first < kMostRowsAtOnce ? p.M - first : kMostRowsAtOnce) + rows - 1) / rows));
-        with_shape<T, VEC>(shape, [&](auto c) {
+        with_shape<false, VEC>(shape, [&](auto c) {
             norm_kernel<T, VEC, decltype(c.first)::value, decltype(c.second)::value><<<grid, dim3(256), 0, s>>>(q);
         });
         if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
@@ -357,16 +424,18 @@ template <typename T, bool VEC>
 int backward(const NormBackward& p, hipStream_t s)
 {
     if (p.M == 0) return p.gw ? launch_part_sums(p.part, 0, p.K, p.gw, s) : FPQ_OK;
-    const Shape shape = shape_of(p.M, p.K, kPiece<T>);
+    const Shape shape = shape_of(p.M, p.K, kPiece<T>, VEC, true);
     const int64_t blocks = backward_blocks(p.M, shape);
     const bool own = p.gw && shape.ch;
     if (p.gx || own)
-        with_shape<T, VEC>(shape, [&](auto c) {
-            norm_backward_kernel<T, VEC, decltype(c.first)::value, decltype(c.second)::value><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(p, own);
+        with_shape<true, VEC>(shape, [&](auto c) {
+            NormBackward q = p;
+            q.past = p.M * p.K * (int64_t)sizeof(T) > kPast;
+            norm_backward_kernel<T, VEC, decltype(c.first)::value, decltype(c.second)::value><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(q, own);
         });
     if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
     if (!p.gw) return FPQ_OK;
-    if (own) return launch_part_sums(p.part, (int)(blocks * (256 / shape.tpr)), p.K, p.gw, s);
+    if (own) return launch_part_sums(p.part, (int)blocks, p.K, p.gw, s);
     const RowParts r = row_parts(p.M, p.K);
     norm_weights_kernel<T><<<dim3((unsigned)((p.K + 255) / 256), (unsigned)r.parts), dim3(256), 0, s>>>(p, r.rows);
     if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
@@ -378,11 +447,12 @@ int backward(const NormBackward& p, hipStream_t s)
 size_t norm_part_bytes(int64_t M, int64_t K)
 {
     size_t most = row_parts_bytes(M, K);
-    for (int piece : {4, 8}) {
-        const Shape s = shape_of(M, K, piece);
-        const size_t n = (size_t)backward_blocks(M, s) * (256 / s.tpr) * K * 4;
-        if (s.ch && n > most) most = n;
-    }
+    for (int piece : {4, 8})
+        for (bool vec : {false, true}) {
+            const Shape s = shape_of(M, K, piece, vec, true);
+            const size_t n = (size_t)backward_blocks(M, s) * K * 4;
+            if (s.ch && n > most) most = n;
+        }
     return most;
 }
 

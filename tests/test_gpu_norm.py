@@ -81,6 +81,14 @@ def test_sizes(M, K, t):
 
 
 @pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,K", [(4100, 128), (4101, 160), (2050, 256), (1700, 320), (1025, 512), (901, 640), (530, 1024), (451, 1280), (260, 2048), (231, 2560), (131, 4096),
+                                 (121, 5120), (70, 8192), (61, 10240), (66000, 8)])
+def test_many_rows(M, K, t):
+    print(M, K, t, flush=True)
+    check(M, K, t)
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
 @pytest.mark.parametrize("residual,weights", [(False, True), (True, False), (False, False)])
 def test_without_residual_or_weights(residual, weights, t):
     check(37, 160, t, 0, residual, weights)
