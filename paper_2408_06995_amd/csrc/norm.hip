@@ -59,8 +59,13 @@ __device__ __forceinline__ void put(T* row, int64_t k, int64_t K, const float (&
         v4i o;
         if constexpr (E == 4) o = v4i{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
         else o = v4i{(int)pair_bf16(v[0], v[1]), (int)pair_bf16(v[2], v[3]), (int)pair_bf16(v[4], v[5]), (int)pair_bf16(v[6], v[7])};
-        if (past) __builtin_nontemporal_store(o, reinterpret_cast<v4i*>(row + k));
-        else *reinterpret_cast<v4i*>(row + k) = o;
+        if (past) {
+            asm volatile("");                                         // (keeps the two stores from being made one, the ordinary)
+            __builtin_nontemporal_store(o, reinterpret_cast<v4i*>(row + k));
+            asm volatile("");
+        } else {
+            *reinterpret_cast<v4i*>(row + k) = o;
+        }
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
