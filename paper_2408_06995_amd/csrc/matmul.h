@@ -109,22 +109,22 @@ __device__ __forceinline__ int row_swap(int row)
 template <bool COL, int R, int KS, int NW>
 struct TileFeed {
     static constexpr int CS = COL ? R / 8 : KS / 8, N = R * KS / 512, PT = (N + NW - 1) / NW;
-    static_assert(R % 32 == 0 && (!COL || R >= 128), "whole wavefronts of loads; rows of COL tiles span all banks");
-    // (COL tiles of 160 columns need no exchange: their rows are 64 bytes further round the banks each)
-    static __device__ __forceinline__ int swap(int row) { return !COL ? row_swap<KS>(row) : R % 128 == 0 ? (row & 3) << 2 : 0; }
+    static_assert(R % 32 == 0 && (!COL || R % 128 == 0), "whole wavefronts of loads; rows of COL tiles span all banks");
+    static __device__ __forceinline__ int swap(int row) { return COL ? (row & 3) << 2 : row_swap<KS>(row); }
     unsigned off[PT];
     static __device__ __forceinline__ int place(int wave, int i)
     {
         const int n = wave + NW * i;
         return N % NW != 0 && n >= N ? n % N : n;
     }
-    // `exist` rows (ROW) or columns (COL) of the tile exist
+    // `exist` rows (ROW) or columns (COL) of the tile exist; FOLD: the tile's second half is those rows of another matrix.
+    template <bool FOLD>
     __device__ __forceinline__ void init(int64_t ld, int exist)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
         for (int i = 0; i < PT; ++i) {
-            const int q = place(wave, i) * 64 + lane, row = q / CS, c = (q - row * CS) ^ swap(row);
+            const int q = place(wave, i) * 64 + lane, line = q / CS, c = (q - line * CS) ^ swap(line), row = FOLD ? line % (R / 2) : line;
             const bool in = COL ? 8 * c < exist : row < exist;
             off[i] = in ? (unsigned)row * (unsigned)(2 * ld) + 16u * c : 0x80000000u;
         }
@@ -140,11 +140,12 @@ struct TileFeed {
         full = (unsigned)(2 * ((COL ? KS - 1 : rows - 1) * ld + cols));
         row = (unsigned)(2 * ld);
     }
-    // Descriptor of the step's loads, of which `left` k are there; none where not `live`: then the loads write zeros.
-    __device__ __forceinline__ v4i window(int left, bool live) const
+    // Descriptor of the step's loads, `from` elements further (another plane, or the gates), of which `left` k are there; of nothing where not
+    // `live`: then the loads write zeros.
+    __device__ __forceinline__ v4i window(int left, bool live, int64_t from) const
     {
         const unsigned n = COL ? full - (unsigned)(KS - min(left, KS)) * row : full;
-        return make_rsrc(reinterpret_cast<const void*>(base), live ? n : 0u);
+        return make_rsrc(reinterpret_cast<const void*>(base + 2 * from), live ? n : 0u);
     }
     // Load i; `lane_out`: this lane's piece of k is not there (ROW).
     __device__ __forceinline__ void load(const v4i& r, unsigned lds, bool lane_out, int i) const
@@ -166,7 +167,7 @@ struct TilePlaces {
     {
         const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
         if constexpr (COL) {
-            const int q = 8 * h + ((lane & 15) >> 2), s = R % 128 == 0 ? q & 3 : 0;
+            const int q = 8 * h + ((lane & 15) >> 2), s = q & 3;
 #pragma unroll
             for (int d = 0; d < T; ++d) {
                 const int c = first / 8 + 4 * d + ((lane & 16) >> 3) + ((lane & 3) >> 1);
@@ -350,14 +351,16 @@ __device__ __forceinline__ void stage_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COUNT) : "memory");
 }
 
-// KS: k of a step; STAGES: of the ring.  (Two wavefronts per SIMD: one workgroup of eight, or two of four.)
-template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int END>
+// KS: k of a step; STAGES: of the ring; PL: planes of both operands in a stage, whose six products are made from one read of each, or 1: a
+// pass over k for each.  (Two wavefronts per SIMD: one workgroup of eight, or two of four.)
+template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int PL, int END>
 __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2) void matmul_kernel(MatmulArgs p)
 {
     constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, G = END == kGated ? TN / 2 : TN;
     using FA = TileFeed<COLA, BM, KS, NW>;
-    using FB = TileFeed<COLB, END == kGated ? BN / 2 : BN, KS, NW>;
-    constexpr int STAGE = (BM + BN) * 2 * KS, LOADS = FA::PT + FB::PT * (END == kGated ? 2 : 1);
+    using FB = TileFeed<COLB, BN, KS, NW>;
+    constexpr int TILE_A = BM * 2 * KS, TILE_B = BN * 2 * KS, STAGE = PL * (TILE_A + TILE_B), LOADS = PL * (FA::PT + FB::PT);
+    static_assert(PL == 1 || PL == 3, "planes");
     static_assert(END != kGated || (!COLB && TN % 2 == 0), "gated: a wavefront has the values and the gates of the same outputs");
     extern __shared__ __align__(1024) char lds[];
     const MatmulPlace at = matmul_place(p);
@@ -367,9 +370,10 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
     const int64_t lda = p.a.ld, ldb = p.b.ld;
 
     FA fa;
-    FB fb, fg;                  // fg: gates
-    fa.init(lda, p.M - m0);
-    fb.init(ldb, p.N - n0);
+    FB fb;
+    fa.template init<false>(lda, p.M - m0);
+    fb.template init<END == kGated>(ldb, p.N - n0);
+    const int64_t gates = (int64_t)p.N * ldb;                   // from a value's row to its gate's
     const int beg = (int)((int64_t)p.total * at.slice / p.slices), end = (int)((int64_t)p.total * (at.slice + 1) / p.slices);
     int pass = beg / p.steps, left = p.K - (beg - pass * p.steps) * KS, todo = end - beg;      // k of the pass and steps that are not loaded yet
     const unsigned base = lds_address(lds);
@@ -383,27 +387,30 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         else fa.start(pa + (int64_t)m0 * lda + k0, lda, min(p.M - m0, BM), left8);
         if constexpr (COLB) fb.start(pb + (int64_t)k0 * ldb + n0, ldb, 0, ((p.N + 7) & ~7) - n0);
         else fb.start(pb + (int64_t)n0 * ldb + k0, ldb, min(p.N - n0, CB), left8);
-        if constexpr (END == kGated) fg.start(pb + (int64_t)(p.N + n0) * ldb + k0, ldb, min(p.N - n0, CB), left8);
     };
-    v4i wa, wb, wg;
+    v4i wa[PL], wb[PL], wg[PL];
     bool lane_out;
     // A step's loads: their descriptors, load i of LOADS, and the way to the next step.  Behind the last one they write zeros, so that every
     // step has the same number of loads on their way.
     auto windows = [&]() {
-        wa = fa.window(left, todo > 0);
-        wb = fb.window(left, todo > 0);
-        if constexpr (END == kGated) wg = fg.window(left, todo > 0);
+#pragma unroll
+        for (int q = 0; q < PL; ++q) {
+            wa[q] = fa.window(left, todo > 0, q * p.a.plane);
+            wb[q] = fb.window(left, todo > 0, q * p.b.plane);
+            if constexpr (END == kGated) wg[q] = fb.window(left, todo > 0, q * p.b.plane + gates);
+        }
         lane_out = k_lane >= ((left + 7) & ~7);
     };
     auto load = [&](int i) {
-        if (i < FA::PT) fa.load(wa, to, lane_out, i);
-        else if (i < FA::PT + FB::PT) fb.load(wb, to + BM * 2 * KS, lane_out, i - FA::PT);
-        else if (END == kGated) fg.load(wg, to + BM * 2 * KS + CB * 2 * KS, lane_out, i - FA::PT - FB::PT);
+        constexpr int EACH = FA::PT + FB::PT;
+        const int q = i / EACH, j = i % EACH;
+        if (j < FA::PT) fa.load(wa[q], to + q * TILE_A, lane_out, j);
+        else if (END == kGated && FB::place(wave, j - FA::PT) >= FB::N / 2) fb.load(wg[q], to + PL * TILE_A + q * TILE_B, lane_out, j - FA::PT);
+        else fb.load(wb[q], to + PL * TILE_A + q * TILE_B, lane_out, j - FA::PT);
     };
     auto loaded = [&]() {
         fa.advance();
         fb.advance();
-        if constexpr (END == kGated) fg.advance();
         --todo;
         left -= KS;
         to = to + STAGE == base + STAGES * STAGE ? base : to + STAGE;
@@ -425,24 +432,23 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         for (int v = 0; v < TN; ++v) acc[u][v] = zero16();
 
     struct Operands {
-        v8bf a[TM], b[TN];
+        v8bf a[PL][TM], b[PL][TN];
     };
-    // Read i of the TM + TN of a step's half t, product i of its TM TN.
+    // Read i of the PL (TM + TN) of a step's half t, product i of its TM TN (PL == 3: six times that, small ones first).
+    constexpr int MM = TM * TN * (PL == 3 ? 6 : 1), RD = PL * (TM + TN);
     auto read = [&](Operands& o, const char* ta, int t, int i) {
-        const char* const tb = ta + BM * 2 * KS;
-        if (i < TN) o.b[i] = rb.read(tb + i / G * CB * 2 * KS, i % G, t);
-        else if (i < TN + TM) o.a[i - TN] = ra.read(ta, i - TN, t);
+        const int q = i / (TM + TN), j = i % (TM + TN);
+        if (j < TN) o.b[q][j] = rb.read(ta + PL * TILE_A + q * TILE_B + j / G * CB * 2 * KS, j % G, t);
+        else o.a[q][j - TN] = ra.read(ta + q * TILE_A, j - TN, t);
     };
     auto multiply = [&](const Operands& o, int i) {
-        const int u = i / TN, v = i % TN;
-        acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.b[v], o.a[u], acc[u][v], 0, 0, 0);
+        constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+        const int c = i / (TM * TN), u = i % (TM * TN) / TN, v = i % TN;
+        acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.b[PL == 3 ? pb[c] : 0][v], o.a[PL == 3 ? pa[c] : 0][u], acc[u][v], 0, 0, 0);
     };
 
     if (beg < end) {
         start();
-        if constexpr (END == kGated)
-#pragma unroll
-            for (int i = 0; i < FB::PT; ++i) fg.off[i] = fb.off[i];
         Operands even, odd;
 #pragma unroll
         for (int s = 0; s < STAGES - 1; ++s) {
@@ -454,7 +460,6 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         const char* tile = lds;
         // Products of one half, and between them the reads of the other and the loads of a step ahead, one at a time: they are issued
         // while the matrix unit is busy.
-        constexpr int MM = TM * TN, RD = TM + TN;
         auto half = [&](const Operands& now, Operands& next, int t, auto loads) {
 #pragma unroll
             for (int i = 0; i < (MM > RD ? MM : RD); ++i) {
@@ -500,24 +505,23 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 
-    const int h = lane >> 5, l32 = lane & 31;
+    const int h = lane >> 5;
     if (p.slices > 1) {
+        __syncthreads();                                        // the ring is free
+        constexpr int ROOM = RowStage<128>::STRIDE * 32;
+        static_assert(NW * ROOM <= STAGES * STAGE, "room for the results on their way");
         const int cols = END == kGated ? 2 * p.N : p.N;
         float* const part = static_cast<float*>(p.out) + (int64_t)at.slice * p.M * cols;
-        const bool vec = (p.N & 3) == 0;
 #pragma unroll
-        for (int u = 0; u < TM; ++u) {
-            const int m = m0 + (wm * TM + u) * 32 + l32;
-            if (m >= p.M) continue;
+        for (int v = 0; v < TN; ++v) {
+            const int nb = n0 + (wn * G + v % G) * 32;
+            if (nb >= p.N) continue;
 #pragma unroll
-            for (int v = 0; v < TN; ++v) {
-                const int nb = n0 + (wn * G + v % G) * 32;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = nb + 8 * q + 4 * h;
-                    const float x[4] = {acc[u][v][4 * q], acc[u][v][4 * q + 1], acc[u][v][4 * q + 2], acc[u][v][4 * q + 3]};
-                    if (n < p.N) put4(part, (int64_t)m * cols + n + (END == kGated ? v / G * p.N : 0), 1, n, p.N, vec && n + 4 <= p.N, x);
-                }
+            for (int u = 0; u < TM; ++u) {
+                const int m = m0 + (wm * TM + u) * 32;
+                if (m >= p.M) break;
+                put_rows(lds + wave * ROOM, part + (END == kGated ? v / G * p.N : 0), cols, 1, m, min(p.M - m, 32), nb, p.N, (p.N & 3) == 0,
+                         [&](int i) { return acc[u][v][i]; });
             }
         }
         return;

@@ -5,17 +5,18 @@
 namespace fpq {
 
 // Tiles: results of a workgroup.
-enum MatmulTile : int { kTile256 = 0, kTile192 = 1, kTile128 = 2, kTile128Deep = 3, kTile32 = 4 };
-constexpr int kTileM[5] = {256, 192, 128, 128, 32}, kTileN[5] = {256, 256, 128, 128, 256};
+enum MatmulTile : int { kTile256 = 0, kTile192 = 1, kTile128 = 2, kTile128Deep = 3, kTile32 = 4, kPlanes256 = 5, kPlanes128 = 6 };
+constexpr int kTileM[7] = {256, 192, 128, 128, 32, 256, 128}, kTileN[7] = {256, 256, 128, 128, 256, 128, 128};
 
-template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int END>
+template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int PL, int END>
 int launch_matmul_tile(MatmulArgs p, hipStream_t s)
 {
     p.steps = p.K ? (p.K + KS - 1) / KS : 1;
+    if (PL == 3) p.passes = 1, p.order_a = p.order_b = 0;
     p.total = p.K ? p.steps * p.passes : 0;             // (nothing to sum over: zeros)
     static std::atomic<uint64_t> done{0};
-    constexpr int bytes = STAGES * (BM + BN) * 2 * KS;
-    const auto kernel = matmul_kernel<COLA, COLB, BM, BN, WM, WN, KS, STAGES, END>;
+    constexpr int bytes = STAGES * PL * (BM + BN) * 2 * KS;
+    const auto kernel = matmul_kernel<COLA, COLB, BM, BN, WM, WN, KS, STAGES, PL, END>;
     if (!allow_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes, done)) return FPQ_ERR_LAUNCH;
     kernel<<<dim3((unsigned)((int64_t)p.tiles_m * p.tiles_n * p.slices)), dim3(64 * WM * WN), bytes, s>>>(p);
     return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
@@ -24,13 +25,15 @@ int launch_matmul_tile(MatmulArgs p, hipStream_t s)
 template <bool COLA, bool COLB, int END>
 int launch_matmul_form(const MatmulArgs& p, int tile, hipStream_t s)
 {
-    if (tile == kTile256) return launch_matmul_tile<COLA, COLB, 256, 256, 2, 4, 64, 2, END>(p, s);
+    if (tile == kTile256) return launch_matmul_tile<COLA, COLB, 256, 256, 2, 4, 64, 2, 1, END>(p, s);
     if constexpr (!COLA) {
-        if (tile == kTile192) return launch_matmul_tile<COLA, COLB, 192, 256, 2, 4, 64, 2, END>(p, s);
-        if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, 32, 4, END>(p, s);
+        if (tile == kTile192) return launch_matmul_tile<COLA, COLB, 192, 256, 2, 4, 64, 2, 1, END>(p, s);
+        if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, 32, 4, 1, END>(p, s);
     }
-    if (tile == kTile128Deep) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 4, END>(p, s);
-    return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 2, END>(p, s);
+    if (tile == kTile128Deep) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 4, 1, END>(p, s);
+    if (tile == kPlanes256) return launch_matmul_tile<COLA, COLB, 256, 128, 4, 2, 32, 2, 3, END>(p, s);
+    if (tile == kPlanes128) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 32, 3, 3, END>(p, s);
+    return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 2, 1, END>(p, s);
 }
 
 int launch_matmul_rows(const MatmulArgs& p, int tile, hipStream_t s);
