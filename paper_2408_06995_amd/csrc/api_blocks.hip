@@ -63,14 +63,14 @@ Operand operand(const void* p, int type, int64_t rows, int64_t cols, int64_t ld,
     if (reads(p, type, rows, cols, ld)) return Operand{static_cast<const __bf16*>(p), ld, 0};
     const int64_t to = round8(cols);
     __bf16* const dst = room.take<__bf16>((size_t)rows * to * 2 * planes_of(type));
-    packs.m[packs.count++] = PackItem{p, nullptr, rows, cols, ld, dst, to, rows * to, 0, type, 0};
+    packs.m[packs.count++] = PackItem{p, nullptr, rows, cols, ld, dst, to, rows * to, 0, {}, type, 0};
     return Operand{dst, to, rows * to};
 }
 Operand operand_of_blocks(const void* codes, const uint8_t* scales, int64_t rows, int64_t cols, int bits, Room& room, PackList& packs)
 {
     const int64_t to = block_padded(cols);
     __bf16* const dst = room.take<__bf16>((size_t)rows * to * 2);
-    packs.m[packs.count++] = PackItem{codes, scales, rows, to, to, dst, to, 0, 0, bits, 0};
+    packs.m[packs.count++] = PackItem{codes, scales, rows, to, to, dst, to, 0, 0, {}, bits, 0};
     return Operand{dst, to, 0};
 }
 

@@ -17,6 +17,7 @@ struct PackItem {
     __bf16* dst;
     int64_t ld_dst, plane;
     int64_t first;              // workgroup of the launch
+    RowOf pieces;               // of eight elements
     int kind;                   // FPQ_TYPE_FP32, FPQ_TYPE_BF16, or 8 or 4: blocks
     int vec;
 };

@@ -81,66 +81,95 @@ __device__ __forceinline__ void decode8(const uint8_t* codes, int64_t at, float 
     }
 }
 
+constexpr int kEach = 2;                // pieces of eight elements per thread
+
+template <int KIND>
+__device__ __forceinline__ void pack_pieces(const PackItem& q, int64_t id0)
+{
+    const int64_t per = q.pieces.per, n = q.rows * per;
+    constexpr int NP = KIND == FPQ_TYPE_FP32 ? 3 : 1;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t id = id0 + 256 * i;
+        if (id >= n) return;
+        const int64_t r = row_at(q.pieces, id), k = (id - r * per) * 8;
+        float v[8];
+        if constexpr (KIND == FPQ_TYPE_FP32) load8(static_cast<const float*>(q.src) + r * q.ld, k, q.cols, q.vec, v);
+        else if constexpr (KIND == FPQ_TYPE_BF16) load8(static_cast<const __bf16*>(q.src) + r * q.ld, k, q.cols, q.vec, v);
+        else decode8<KIND == 8>(static_cast<const uint8_t*>(q.src), id * 8, scale_of(q.scales[id / 4]), v);
+        store_planes<NP>(q.dst + r * q.ld_dst + k, q.plane, v);
+    }
+}
+
 __global__ __launch_bounds__(256) void pack_kernel(PackList p)
 {
-    const PackItem& q = p.count > 2 && blockIdx.x >= p.m[2].first ? p.m[2] : p.count > 1 && blockIdx.x >= p.m[1].first ? p.m[1] : p.m[0];
-    const int64_t per = q.ld_dst / 8, id = (int64_t)(blockIdx.x - q.first) * 256 + threadIdx.x;
-    if (id >= q.rows * per) return;
-    const int64_t r = id / per, k = (id - r * per) * 8;
-    __bf16* const dst = q.dst + r * q.ld_dst + k;
-    float v[8];
-    if (q.kind == FPQ_TYPE_FP32) {
-        load8(static_cast<const float*>(q.src) + r * q.ld, k, q.cols, q.vec, v);
-        store_planes<3>(dst, q.plane, v);
-        return;
-    }
-    if (q.kind == FPQ_TYPE_BF16) load8(static_cast<const __bf16*>(q.src) + r * q.ld, k, q.cols, q.vec, v);
-    else if (q.kind == 8) decode8<true>(static_cast<const uint8_t*>(q.src), id * 8, scale_of(q.scales[id / 4]), v);
-    else decode8<false>(static_cast<const uint8_t*>(q.src), id * 8, scale_of(q.scales[id / 4]), v);
-    store_planes<1>(dst, 0, v);
+    const int which = p.count > 2 && blockIdx.x >= p.m[2].first ? 2 : p.count > 1 && blockIdx.x >= p.m[1].first ? 1 : 0;
+    const PackItem q = which == 2 ? p.m[2] : which == 1 ? p.m[1] : p.m[0];
+    const int64_t id0 = (int64_t)(blockIdx.x - q.first) * (256 * kEach) + threadIdx.x;
+    if (q.kind == FPQ_TYPE_FP32) pack_pieces<FPQ_TYPE_FP32>(q, id0);
+    else if (q.kind == FPQ_TYPE_BF16) pack_pieces<FPQ_TYPE_BF16>(q, id0);
+    else if (q.kind == 8) pack_pieces<8>(q, id0);
+    else pack_pieces<4>(q, id0);
 }
 
 template <bool EIGHT, typename T>
-__global__ __launch_bounds__(256) void decode_kernel(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, int64_t padded, T* dst, int64_t ld_dst, int vec)
+__global__ __launch_bounds__(256) void decode_kernel(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, RowOf pieces, T* dst, int64_t ld_dst, int vec)
 {
-    const int64_t per = padded / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= rows * per) return;
-    const int64_t r = id / per, k = (id - r * per) * 8;
-    float v[8];
-    decode8<EIGHT>(codes, id * 8, scale_of(scales[id / 4]), v);
-    store8(dst + r * ld_dst, k, cols, vec, v);
+    const int64_t n = rows * pieces.per, id0 = (int64_t)blockIdx.x * (256 * kEach) + threadIdx.x;
+    float v[kEach][8];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t id = min(id0 + 256 * i, n - 1);
+        decode8<EIGHT>(codes, id * 8, scale_of(scales[id / 4]), v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t id = id0 + 256 * i;
+        if (id >= n) return;
+        const int64_t r = row_at(pieces, id);
+        store8(dst + r * ld_dst, (id - r * pieces.per) * 8, cols, vec, v[i]);
+    }
 }
 
 template <bool EIGHT, typename T>
-__global__ __launch_bounds__(256) void block_quantize_kernel(const T* x, int64_t rows, int64_t cols, int64_t padded, int64_t ld, const uint8_t* mask, uint8_t* codes,
+__global__ __launch_bounds__(256) void block_quantize_kernel(const T* x, int64_t rows, int64_t cols, RowOf pieces, int64_t ld, const uint8_t* mask, uint8_t* codes,
                                                              uint8_t* scales, int vec)
 {
-    const int64_t per = padded / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const bool in = id < rows * per;                                 // (whole groups of four lanes)
-    const int64_t r = in ? id / per : 0, k = in ? (id - r * per) * 8 : 0;
-    float v[8];
-    load8(x + r * ld, k, cols, vec, v);
-    uint32_t top = 0;
+    const int64_t n = rows * pieces.per, id0 = (int64_t)blockIdx.x * (256 * kEach) + threadIdx.x;
+    float all[kEach][8];
+    int64_t row[kEach];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
-    if (!in) return;
-    const uint32_t s = EIGHT ? block_scale8(top) : block_scale4(top);
-    const float i = inverse_scale(s);
-    if ((threadIdx.x & 3) == 0) scales[id / 4] = (uint8_t)s;
-    if constexpr (EIGHT) {
-        *reinterpret_cast<uint2*>(codes + id * 8) = make_uint2(codes8(v[0] * i, v[1] * i, v[2] * i, v[3] * i), codes8(v[4] * i, v[5] * i, v[6] * i, v[7] * i));
-    } else {
-        const QParams q{1, 1, 3, 6.0f};
-        uint32_t w = 0;
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t id = min(id0 + 256 * i, n - 1);                // (n is a multiple of four: a block's lanes stay together)
+        row[i] = row_at(pieces, id);
+        load8(x + row[i] * ld, (id - row[i] * pieces.per) * 8, cols, vec, all[i]);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (k + e >= cols) break;
-            const uint32_t c = mask ? quantize_mask(v[e], i, mask[r * cols + k + e], q) : quantize_nearest(v[e], i, q);
-            w |= c << (4 * e);
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t id = id0 + 256 * i, k = (id - row[i] * pieces.per) * 8;
+        const float (&v)[8] = all[i];
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+        if (id >= n) continue;
+        const uint32_t s = EIGHT ? block_scale8(top) : block_scale4(top);
+        const float r = inverse_scale(s);
+        if ((threadIdx.x & 3) == 0) scales[id / 4] = (uint8_t)s;
+        if constexpr (EIGHT) {
+            *reinterpret_cast<uint2*>(codes + id * 8) = make_uint2(codes8(v[0] * r, v[1] * r, v[2] * r, v[3] * r), codes8(v[4] * r, v[5] * r, v[6] * r, v[7] * r));
+        } else {
+            const QParams q{1, 1, 3, 6.0f};
+            uint32_t w = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (k + e >= cols) break;
+                const uint32_t c = mask ? quantize_mask(v[e], r, mask[row[i] * cols + k + e], q) : quantize_nearest(v[e], r, q);
+                w |= c << (4 * e);
+            }
+            *reinterpret_cast<uint32_t*>(codes + id * 4) = s == 255 ? 0u : w;
         }
-        *reinterpret_cast<uint32_t*>(codes + id * 4) = s == 255 ? 0u : w;
     }
 }
 
@@ -301,7 +330,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward p, int6
     strip_sum<WIDE>(sum_g, first, N, part + N);
 }
 
-unsigned grid256(int64_t n) { return (unsigned)((n + 255) / 256); }
+unsigned grid_of(int64_t pieces) { return (unsigned)((pieces + 256 * kEach - 1) / (256 * kEach)); }
 bool rows_vec(const void* p, int64_t ld, int type)
 {
     return ((uintptr_t)p & 15) == 0 && ld % (type == FPQ_TYPE_FP32 ? 4 : 8) == 0;
@@ -317,7 +346,8 @@ int launch_packs(PackList& p, hipStream_t s)
         PackItem& q = p.m[i];
         q.first = at;
         q.vec = q.kind != 8 && q.kind != 4 && rows_vec(q.src, q.ld, q.kind);
-        const int64_t blocks = (q.rows * (q.ld_dst / 8) + 255) / 256;
+        q.pieces = row_of(q.rows, q.ld_dst / 8);
+        const int64_t blocks = grid_of(q.rows * (q.ld_dst / 8));
         if (at && at + blocks >= (int64_t)1 << 24) {                 // (a launch has fewer than 2^32 threads)
             PackList one{{p.m[i]}, 1};
             const int st = launch_packs(one, s);
@@ -337,10 +367,10 @@ int launch_packs(PackList& p, hipStream_t s)
 int launch_decode(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, bool eight, void* dst, int f32, int64_t ld_dst, hipStream_t s)
 {
     const int64_t padded = block_padded(cols);
-    const unsigned grid = grid256(rows * (padded / 8));
+    const unsigned grid = grid_of(rows * (padded / 8));
     if (!grid) return FPQ_OK;
     const int vec = rows_vec(dst, ld_dst, f32 ? FPQ_TYPE_FP32 : FPQ_TYPE_BF16);
-    auto run = [&](auto kernel, auto* to) { kernel<<<dim3(grid), dim3(256), 0, s>>>(codes, scales, rows, cols, padded, to, ld_dst, vec); };
+    auto run = [&](auto kernel, auto* to) { kernel<<<dim3(grid), dim3(256), 0, s>>>(codes, scales, rows, cols, row_of(rows, padded / 8), to, ld_dst, vec); };
     if (f32) eight ? run(decode_kernel<true, float>, static_cast<float*>(dst)) : run(decode_kernel<false, float>, static_cast<float*>(dst));
     else eight ? run(decode_kernel<true, __bf16>, static_cast<__bf16*>(dst)) : run(decode_kernel<false, __bf16>, static_cast<__bf16*>(dst));
     return launched();
@@ -350,10 +380,10 @@ int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t
                           hipStream_t s)
 {
     const int64_t padded = block_padded(K);
-    const unsigned grid = grid256(M * (padded / 8));
+    const unsigned grid = grid_of(M * (padded / 8));
     if (!grid) return FPQ_OK;
     const int vec = rows_vec(x, ld, type);
-    auto run = [&](auto kernel, auto* from) { kernel<<<dim3(grid), dim3(256), 0, s>>>(from, M, K, padded, ld, mask, codes, scales, vec); };
+    auto run = [&](auto kernel, auto* from) { kernel<<<dim3(grid), dim3(256), 0, s>>>(from, M, K, row_of(M, padded / 8), ld, mask, codes, scales, vec); };
     if (type == FPQ_TYPE_FP32) eight ? run(block_quantize_kernel<true, float>, static_cast<const float*>(x)) : run(block_quantize_kernel<false, float>, static_cast<const float*>(x));
     else eight ? run(block_quantize_kernel<true, __bf16>, static_cast<const __bf16*>(x)) : run(block_quantize_kernel<false, __bf16>, static_cast<const __bf16*>(x));
     return launched();
@@ -363,7 +393,7 @@ int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t
 RowParts row_parts(int64_t M, int64_t cols)
 {
     const int64_t strips = (cols + kStripColumns - 1) / kStripColumns;
-    int64_t parts = 1024 / strips < 256 ? 1024 / strips : 256, most = (M + 15) / 16;
+    int64_t parts = 1024 / strips < 512 ? 1024 / strips : 512, most = (M + 15) / 16;
     parts = parts < 1 ? 1 : parts > most ? most : parts;
     if (parts < 1) parts = 1;
     const int64_t rows = (M + parts - 1) / parts;

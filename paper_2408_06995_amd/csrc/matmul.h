@@ -23,6 +23,15 @@ struct Operand {
     int64_t ld, plane;          // in elements
 };
 
+// Rows of `per` units each, for kernels whose threads take a unit: the row of unit `id`.
+struct RowOf {
+    int64_t per;
+    Divisor by;
+    int fits;                   // all numbers of units fit 31 bits
+};
+static inline RowOf row_of(int64_t rows, int64_t per) { return RowOf{per, divisor(per < ((int64_t)1 << 31) ? per : 1), rows * per < (int64_t)1 << 31}; }
+__device__ __forceinline__ int64_t row_at(const RowOf& r, int64_t id) { return r.fits ? (int64_t)divide((int)id, r.by) : id / r.per; }
+
 // What the results of a tile become.
 enum MatmulEnd : int { kStore = 0, kGated = 1 };
 

@@ -33,7 +33,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, b
         double full, alone, ends;
     };
     static const Kind kinds[] = {{kTile256, 256, 1.8, 1.2, 4}, {kTile192, 256, 1.35, 1.05, 4}, {kTile128, 512, 1.08, 0.66, 2}, {kTile128Deep, 256, 0.56, 0.43, 3},
-                                 {kPlanes256, 256, 0.84, 0.8, 3}, {kPlanes128, 256, 0.5, 0.38, 3}};
+                                 {kPlanes256, 256, 0.84, 0.62, 3}, {kPlanes128, 256, 0.5, 0.38, 3}};
     Plan best{kTile128, 1};
     double least = 1e30;
     for (const Kind& k : kinds) {
@@ -63,14 +63,15 @@ struct SumArgs {
     int out_f32;
     const float* bias;
     Gate gate;
+    RowOf rows;                 // of the threads
 };
 
 // Four columns of a row per thread.
 __global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p)
 {
-    const int64_t per = (p.N + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t per = p.rows.per, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (id >= p.M * per) return;
-    const int64_t m = id / per;
+    const int64_t m = row_at(p.rows, id);
     const int n = (int)(id - m * per) * 4;
     const bool vec = (p.N & 3) == 0;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -99,9 +100,9 @@ __global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p)
 // Four outputs of a row per thread, eight threads a block of 32.
 __global__ __launch_bounds__(256) void matmul_sum_gated_kernel(SumArgs p)
 {
-    const int64_t per = (p.N + 31) / 32 * 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t per = p.rows.per, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const bool in = id < p.M * per;                                  // (whole blocks of lanes)
-    const int64_t m = in ? id / per : 0;
+    const int64_t m = in ? row_at(p.rows, id) : 0;
     const int n = in ? (int)(id - m * per) * 4 : 0, N = (int)p.N;
     float a[4], g[4], v[4];
 #pragma unroll
@@ -201,7 +202,8 @@ int launch_product(const Product& q, void* part, hipStream_t s)
              : q.col_b ? launch_matmul_rows_cols(p, plan.tile, s)
                        : launch_matmul_rows(p, plan.tile, s);
     if (st != FPQ_OK || plan.slices == 1) return st;
-    const SumArgs r{static_cast<const float*>(part), q.M, q.N, plan.slices, q.out, q.ld_out, q.out_f32, q.bias, q.gate};
+    const SumArgs r{static_cast<const float*>(part), q.M, q.N, plan.slices, q.out, q.ld_out, q.out_f32, q.bias, q.gate,
+                    row_of(q.M, q.gated ? (q.N + 31) / 32 * 8 : (q.N + 3) / 4)};
     if (q.gated) {
         const int64_t threads = q.M * ((q.N + 31) / 32 * 8);
         matmul_sum_gated_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(r);
