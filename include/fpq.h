@@ -658,7 +658,8 @@ int fpq_gated_backward(const fpq_gated_args_t *args, const void *x, const uint8_
  * fpq_linear_backward and fpq_gated_backward take.  Codes come from the unrounded y.
  * fpq_rms_norm_backward: from sum and rstd of the forward call, with grad_y, and grad_sum (NULL for zeros) what the stream's other readers give back,
  *   grad_x = rstd (gy w - r rstd^2 mean(gy w r)) + grad_sum, the gradient of x and of residual alike, grad_w fp32 [K] = sum over the rows of gy r rstd.
- * grad_x or grad_w may be NULL; grad_x may be grad_y or grad_sum itself.  Sums and statistics are fp32, no atomics.  A row's infinity or NaN makes that row NaN.
+ * grad_x or grad_w may be NULL; grad_x may be grad_y or grad_sum itself.  Sums and statistics are fp32, no atomics.  A NaN makes its row NaN; an infinity
+ * becomes NaN and leaves zeros beside it; with eps 0 a row of zeros is NaN.
  * Matrices are of args->type with row strides ld_*; rows of multiples of 16 bytes that start at one are what the kernels are tuned for.
  * eps >= 0 and finite (FPQ_ERR_SCALE).  workspace of the backward call: the stated bytes, 16-byte aligned, no initialisation (may be NULL
  * without grad_w).  Limits: M at most 2^28, K and strides at most 2^20, M K below 2^34 (FPQ_ERR_SHAPE). */

@@ -155,10 +155,13 @@ RowsArgs rows_args(const void* x, int type, int64_t M, int64_t N, int64_t K, int
     return r;
 }
 
-// Whether the form of few rows takes gated projections: weights read where they are.
+// Whether the form of few rows takes gated projections: weights read where they are.  In bf16 up to 16 rows, more only of weights that the L2 holds: in
+// 64 rows their share of the matrix unit and x again in every workgroup cost more than the tiles' rows without a result (48 rows of 4096 -> 10240:
+// 55.8 us, in tiles 36.4; of 1280 -> 5120: 14.2 and 16.2).  In fp32 tiles have to pack the weights first (64 rows of 4096 -> 10240: 143 us, in tiles 281).
 bool few_rows(const fpq_gated_args_t* p, const void* w)
 {
-    return p->M <= kFewRows && aligned(w, 16) && p->K % 8 == 0 && p->ld_w * size_of(p->type) % 16 == 0;
+    const bool fits = p->type == FPQ_TYPE_FP32 || p->M <= 16 || 4 * p->N * p->K <= (int64_t)32 << 20;
+    return p->M <= kFewRows && fits && aligned(w, 16) && p->K % 8 == 0 && p->ld_w * size_of(p->type) % 16 == 0;
 }
 
 bool norm_vec(const void* p, int64_t ld, int64_t M, int64_t K, size_t size)
@@ -237,7 +240,7 @@ int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* c
         r.ld_s = kp / kBlock;
         r.out = y;
         r.ld_out = stride(p->ld_y, p->N, p->M);
-        return p->M <= 4 && token_blocks_lds(p->M, p->K, r.f32) <= 65536 ? launch_token_blocks(r, s) : launch_rows_blocks(r, s);
+        return p->M <= (r.f32 ? 4 : 2) && token_blocks_lds(p->M, p->K, r.f32) <= 65536 ? launch_token_blocks(r, s) : launch_rows_blocks(r, s);
     }
     Room room{static_cast<char*>(workspace)};
     PackList packs{};

@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackward p, int 
                 numbers<T>(ng[i], g);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    gw[i][e] = fmaf(g[e] * v[e], in ? rstd : 0.0f, gw[i][e]);
+                    if (in) gw[i][e] = fmaf(g[e] * v[e], rstd, gw[i][e]);
                     dot = fmaf(g[e] * w[i][e], v[e], dot);
                 }
             }
