@@ -207,7 +207,8 @@ def _results(c, s):
         if c["keep"] == "type":
             s["pre"] = torch.empty(M, 2 * N, dtype=TYPES[c["type"]], device=DEVICE)
         elif c["keep"] == "blocks":
-            s["pre"], s["pre_scales"] = room(M * 2 * _padded(N)).view(M, -1), room(M * 2 * _padded(N) // BLOCK)[:M * 2 * _padded(N) // BLOCK].view(M, -1)
+            n = M * 2 * _padded(N)
+            s["pre"], s["pre_scales"] = room(n)[:n].view(M, -1), room(n // BLOCK)[:n // BLOCK].view(M, -1)
         s["ws"] = room(fpq.fpq_gated_workspace_size(M, N, K, t))
         if c["train"]:
             s["gx"], s["gw"] = like("x"), like("w")
