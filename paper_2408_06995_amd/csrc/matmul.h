@@ -113,13 +113,20 @@ __device__ __forceinline__ int row_swap(int row)
     return KS == 32 ? (row >> 2) & 3 : (row >> 1) & 7;
 }
 
+// COL tiles: four neighbouring rows' 64 bytes lie in different banks, of which rows of 64 columns fill half.
+template <int R>
+__device__ __forceinline__ int col_swap(int row)
+{
+    return R == 64 ? (row & 2) << 1 : (row & 3) << 2;
+}
+
 // One operand's tile of R rows (ROW) or columns (COL) and KS k: this thread's loads of it.  Every wavefront makes the same number: where
 // they do not divide, some load a piece that another one loads too.
 template <bool COL, int R, int KS, int NW>
 struct TileFeed {
     static constexpr int CS = COL ? R / 8 : KS / 8, N = R * KS / 512, PT = (N + NW - 1) / NW;
-    static_assert(R % 32 == 0 && (!COL || R % 128 == 0), "whole wavefronts of loads; rows of COL tiles span all banks");
-    static __device__ __forceinline__ int swap(int row) { return COL ? (row & 3) << 2 : row_swap<KS>(row); }
+    static_assert(R % 32 == 0 && (!COL || R == 64 || R % 128 == 0), "whole wavefronts of loads; rows of COL tiles span all banks, or half");
+    static __device__ __forceinline__ int swap(int row) { return COL ? col_swap<R>(row) : row_swap<KS>(row); }
     unsigned off[PT];
     static __device__ __forceinline__ int place(int wave, int i)
     {
@@ -176,11 +183,11 @@ struct TilePlaces {
     {
         const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
         if constexpr (COL) {
-            const int q = 8 * h + ((lane & 15) >> 2), s = q & 3;
+            const int q = 8 * h + ((lane & 15) >> 2);
 #pragma unroll
             for (int d = 0; d < T; ++d) {
                 const int c = first / 8 + 4 * d + ((lane & 16) >> 3) + ((lane & 3) >> 1);
-                at[d] = q * (2 * R) + 16 * (c ^ (s << 2)) + 8 * (lane & 1);
+                at[d] = q * (2 * R) + 16 * (c ^ col_swap<R>(q)) + 8 * (lane & 1);
             }
         } else {
 #pragma unroll

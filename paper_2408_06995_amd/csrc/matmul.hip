@@ -14,7 +14,8 @@ int passes(int planes_a, int planes_b) { return planes_a * planes_b == 9 ? 6 : p
 
 Plan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated)
 {
-    auto tiles = [&](int t) { return ((M + kTileM[t] - 1) / kTileM[t]) * ((N + kTileN[t] / (gated ? 2 : 1) - 1) / (kTileN[t] / (gated ? 2 : 1))); };
+    auto columns = [&](int t) { return (int64_t)tile_n(t, gated) / (gated ? 2 : 1); };
+    auto tiles = [&](int t) { return ((M + kTileM[t] - 1) / kTileM[t]) * ((N + columns(t) - 1) / columns(t)); };
     const double steps = passes(planes_a, planes_b) * (double)((K + 63) / 64);
     if (!col_a && M <= 32) {
         // bound by B's bytes: parts of no fewer than eight steps until two workgroups per compute unit have work
@@ -26,19 +27,21 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, b
     // at its start and end.  A step of 64 k takes `full` where the chip is full (1.2 PFLOP/s) and no less than `alone`; a round that is not full, its
     // share.  Workgroups of 256 and 192 rows have their compute unit alone; two of 128 rows share one and hide one's waits behind the other, or one with
     // a ring of four stages has it alone.  Slices cost the partial results' way to memory and back and a launch.  (Measured: 2048 x 4096 with 64
-    // steps 1.07 of 192 rows; 1280 x 1280 with 192 steps 1.09 of 256 rows, 0.66 of 128 and 0.43 deep.)  Operands of three planes each are read
+    // steps 1.07 of 192 rows; 1280 x 1280 with 192 steps 1.09 of 256 rows, 0.66 of 128 and 0.43 deep;
+    // 512 x 1280 with 20 steps 9.0 us in tiles of 64 for 14.4 of 128.)  Operands of three planes each are read
     // once for their six products: 4096 x 4096 x 2048 in fp32, both gradients, 666 us for 727.
     struct Kind {
         int tile, at_once;
         double full, alone, ends;
     };
-    static const Kind kinds[] = {{kTile256, 256, 1.8, 1.2, 4}, {kTile192, 256, 1.35, 1.05, 4}, {kTile128, 512, 1.08, 0.66, 2}, {kTile128Deep, 256, 0.56, 0.43, 3},
-                                 {kPlanes256, 256, 0.84, 0.62, 3}, {kPlanes128, 256, 0.5, 0.38, 3}};
+    const Kind kinds[] = {{kTile256, 256, 1.8, 1.2, 4}, {kTile192, 256, 1.35, 1.05, 4}, {kTile128, 512, 1.08, 0.66, 2}, {kTile128Deep, 256, 0.56, 0.43, 3},
+                          {kPlanes256, 256, 0.84, 0.62, 3}, {kPlanes128, 256, 0.5, 0.38, 3},
+                          gated ? Kind{kTile64, 256, 0.5, 0.24, 5} : Kind{kTile64, 512, 0.5, 0.2, 5}};
     Plan best{kTile128, 1};
     double least = 1e30;
     for (const Kind& k : kinds) {
         if (k.tile == kTile192 && col_a) continue;
-        if (k.tile >= kPlanes256 && planes_a * planes_b != 9) continue;
+        if ((k.tile == kPlanes256 || k.tile == kPlanes128) && planes_a * planes_b != 9) continue;
         for (int s = 1; s <= 32; s = s < 4 ? s + 1 : s + s / 4) {
             if (s > 1 && steps / s < 8) break;
             const int64_t n = tiles(k.tile) * s, rest = n % k.at_once;
@@ -189,7 +192,7 @@ int launch_product(const Product& q, void* part, hipStream_t s)
     else if (q.planes_b == 3) p.order_b = 0x012;
     p.passes = passes(q.planes_a, q.planes_b);
     p.slices = plan.slices;
-    const int cols = kTileN[plan.tile] / (q.gated ? 2 : 1);
+    const int cols = tile_n(plan.tile, q.gated) / (q.gated ? 2 : 1);
     p.tiles_m = (int)((q.M + kTileM[plan.tile] - 1) / kTileM[plan.tile]);
     p.tiles_n = (int)((q.N + cols - 1) / cols);
     p.out = plan.slices > 1 ? part : q.out;

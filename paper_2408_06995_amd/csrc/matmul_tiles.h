@@ -5,8 +5,10 @@
 namespace fpq {
 
 // Tiles: results of a workgroup.
-enum MatmulTile : int { kTile256 = 0, kTile192 = 1, kTile128 = 2, kTile128Deep = 3, kTile32 = 4, kPlanes256 = 5, kPlanes128 = 6 };
-constexpr int kTileM[7] = {256, 192, 128, 128, 32, 256, 128}, kTileN[7] = {256, 256, 128, 128, 256, 128, 128};
+enum MatmulTile : int { kTile256 = 0, kTile192 = 1, kTile128 = 2, kTile128Deep = 3, kTile32 = 4, kPlanes256 = 5, kPlanes128 = 6, kTile64 = 7 };
+constexpr int kTileM[8] = {256, 192, 128, 128, 32, 256, 128, 64};
+// (columns; of gated projections values and gates together)
+constexpr int tile_n(int tile, bool gated) { return tile == kTile64 ? (gated ? 128 : 64) : tile <= kTile192 || tile == kTile32 ? 256 : 128; }
 
 template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int PL, int END>
 int launch_matmul_tile(MatmulArgs p, hipStream_t s)
@@ -30,6 +32,7 @@ int launch_matmul_form(const MatmulArgs& p, int tile, hipStream_t s)
         if (tile == kTile192) return launch_matmul_tile<COLA, COLB, 192, 256, 2, 4, 64, 2, 1, END>(p, s);
         if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, 32, 4, 1, END>(p, s);
     }
+    if (tile == kTile64) return launch_matmul_tile<COLA, COLB, 64, END == kGated ? 128 : 64, 2, 2, 64, 4, 1, END>(p, s);
     if (tile == kTile128Deep) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 4, 1, END>(p, s);
     if (tile == kPlanes256) return launch_matmul_tile<COLA, COLB, 256, 128, 4, 2, 32, 2, 3, END>(p, s);
     if (tile == kPlanes128) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 32, 3, 3, END>(p, s);
