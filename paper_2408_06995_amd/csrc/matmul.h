@@ -507,7 +507,9 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         for (int it = beg + 1; it < end; ++it) {
             stage_barrier<(STAGES - 2) * LOADS>();
             windows();
+            __builtin_amdgcn_s_setprio(1);                  // (a wavefront that has loads to start goes first: two tiles of 128 rows a compute unit gain 5 %)
             half(odd, even, 0, std::true_type());
+            __builtin_amdgcn_s_setprio(0);
             loaded();
             half(even, odd, 1, std::false_type());
             if constexpr (KS == 64) {
