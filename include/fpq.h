@@ -582,8 +582,8 @@ int fpq_adamw_step(const void *plan, int64_t pieces, double lr, double beta1, do
  * A row's elements in blocks of 32 neighbours, each block with one power of two as its scale: codes of the hardware's E4M3
  * (4, 3, 7, 448), one per byte, or E2M1 (2, 1, 1, 6), two per byte, the even element in the low half.  Rows are filled up with code 0 to
  * whole blocks: Kp = fpq_block_padded(K) codes and Kp / 32 scales a row, contiguous.  A scale byte s stands for 2^(s - 127), 255 for NaN.
- * Every value that blocks can hold is a bf16 number (but below 2^-126, and 2^128, to which the largest magnitudes may round), so that the
- * matrix unit takes them without a rounding of their own.
+ * Every value that blocks can hold is a bf16 number, so that the matrix unit takes them without a rounding of their own; but those below
+ * 2^-126, which are rounded and may count as zero in products, and 2^128, to which the largest magnitudes may round and which may count as infinity.
  *
  * fpq_block_quantize: x [M, K] of x_type with row stride ld_x.  A block's scale is the least power of two (from 2^-126 on) with which no
  *   element is out of range, 1 where all are zero; elements are rounded to nearest, ties to even, or, with a mask [M, K] (E2M1 only; as
@@ -659,7 +659,8 @@ int fpq_gated_backward(const fpq_gated_args_t *args, const void *x, const uint8_
  * fpq_rms_norm_backward: from sum and rstd of the forward call, with grad_y, and grad_sum (NULL for zeros) what the stream's other readers give back,
  *   grad_x = rstd (gy w - r rstd^2 mean(gy w r)) + grad_sum, the gradient of x and of residual alike, grad_w fp32 [K] = sum over the rows of gy r rstd.
  * grad_x or grad_w may be NULL; grad_x may be grad_y or grad_sum itself.  Sums and statistics are fp32, no atomics.  A NaN makes its row NaN; an infinity
- * becomes NaN and leaves zeros beside it; with eps 0 a row of zeros is NaN.
+ * becomes NaN and leaves zeros beside it; a sum of squares past 2^128 makes the row zeros, squares below 2^-149 count as none; with eps 0 a row of
+ * zeros is NaN.
  * Matrices are of args->type with row strides ld_*; rows of multiples of 16 bytes that start at one are what the kernels are tuned for.
  * eps >= 0 and finite (FPQ_ERR_SCALE).  workspace of the backward call: the stated bytes, 16-byte aligned, no initialisation (may be NULL
  * without grad_w).  Limits: M at most 2^28, K and strides at most 2^20, M K below 2^34 (FPQ_ERR_SHAPE). */

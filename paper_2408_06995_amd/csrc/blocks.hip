@@ -421,8 +421,10 @@ int launch_column_sums(const void* x, int type, int64_t M, int64_t N, int64_t ld
 int launch_gate_backward(const GateBackward& p, hipStream_t s)
 {
     const RowParts r = row_parts(p.M, p.N);
-    const dim3 grid((unsigned)((p.N + kStripColumns - 1) / kStripColumns), (unsigned)r.parts);
     const bool wide = p.N % 8 == 0 && rows_vec(p.gh, p.ld_gh, p.type) && (p.pre_scales || rows_vec(p.pre, p.N, p.type));
+    // (the zeros behind the rows are a strip's work too, where they begin one)
+    const int64_t columns = p.d ? p.N + p.ld_d - 2 * p.N : p.N;
+    const dim3 grid((unsigned)((columns + kStripColumns - 1) / kStripColumns), (unsigned)r.parts);
     GateBackward q = p;
     if (!p.grad_bias) q.part = nullptr;
     auto run = [&](auto kernel) { kernel<<<grid, dim3(256), 0, s>>>(q, r.rows); };

@@ -432,6 +432,11 @@ int backward(const NormBackward& p, hipStream_t s)
     const Shape shape = shape_of(p.M, p.K, kPiece<T>, VEC, true);
     const int64_t blocks = backward_blocks(p.M, shape);
     const bool own = p.gw && shape.ch;
+    const RowParts r = row_parts(p.M, p.K);
+    if (p.gw && !own) {                                               // (first: grad_x may be written over gy)
+        norm_weights_kernel<T><<<dim3((unsigned)((p.K + 255) / 256), (unsigned)r.parts), dim3(256), 0, s>>>(p, r.rows);
+        if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
+    }
     if (p.gx || own)
         with_shape<true, VEC>(shape, [&](auto c) {
             NormBackward q = p;
@@ -439,12 +444,7 @@ int backward(const NormBackward& p, hipStream_t s)
             norm_backward_kernel<T, VEC, decltype(c.first)::value, decltype(c.second)::value><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(q, own);
         });
     if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
-    if (!p.gw) return FPQ_OK;
-    if (own) return launch_part_sums(p.part, (int)blocks, p.K, p.gw, s);
-    const RowParts r = row_parts(p.M, p.K);
-    norm_weights_kernel<T><<<dim3((unsigned)((p.K + 255) / 256), (unsigned)r.parts), dim3(256), 0, s>>>(p, r.rows);
-    if (hipGetLastError() != hipSuccess) return FPQ_ERR_LAUNCH;
-    return launch_part_sums(p.part, r.parts, p.K, p.gw, s);
+    return p.gw ? launch_part_sums(p.part, own ? (int)blocks : r.parts, p.K, p.gw, s) : FPQ_OK;
 }
 
 }  // namespace

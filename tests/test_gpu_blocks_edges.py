@@ -1,0 +1,151 @@
+"""Operators around the projections at their edges: workspaces of exactly the stated size full of NaN with a guard behind them, tensors off
+16-byte alignment, gradients written over what they came from, scales at their ends."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_blocks
+import test_gpu_gated
+from oracle import blocks
+from paper_2408_06995_amd import binding as B
+from gpu_util import DEV
+from test_gpu_blocks import E2M1, E4M3, TYPES, check_linear, host, nan, quantize, rows, within
+from test_gpu_gated import Call
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def guarded(monkeypatch):
+    """Workspaces of the stated bytes that hold NaN in either type; behind them nothing may be written."""
+    made = []
+
+    def room(n):
+        b = torch.full((max(int(n), 16) + 512,), 0xff, dtype=torch.uint8, device=DEV)
+        made.append((b, max(int(n), 16)))
+        return b[:max(int(n), 16)]
+
+    for module in (test_gpu_blocks, test_gpu_gated):
+        monkeypatch.setattr(module, "room", room)
+    yield room
+    for b, n in made:
+        assert (b[n:] == 0xff).all()
+
+
+@pytest.mark.parametrize("keep", ["type", "blocks"])
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(70, 509, 40), (70, 510, 40), (33, 511, 24), (5, 1022, 16), (66, 1023, 8), (40, 512, 13), (3, 77, 328), (130, 4, 9)])
+def test_gated_rows_that_are_no_whole_pieces(M, N, K, t, keep, guarded):
+    """What lies behind the rows of da and dg in the workspace takes no part, wherever a row ends."""
+    print(M, N, K, t, keep, flush=True)
+    Call(M, N, K, t, "gelu" if N % 2 else "silu").check(keep, kept_x=N % 2 == 0)
+
+
+@pytest.mark.parametrize("kept", [False, True], ids=["x", "blocks"])
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (70, 511, 33), (259, 130, 7), (1030, 24, 100)])
+def test_linear_workspaces(M, N, K, t, kept, guarded):
+    check_linear(M, N, K, t, kept)
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(65, 40, 33), (130, 511, 95), (300, 33, 1000)])
+def test_layer_workspaces(M, N, K, t, guarded):
+    g = torch.Generator().manual_seed(M)
+    x = rows(g, M, K, TYPES[t])
+    codes, scales = quantize(rows(g, N, K, torch.float32), E2M1)
+    wv = blocks.block_values(blocks.unpack(codes.cpu().numpy()), scales.cpu().numpy(), 4, K)
+    y = nan(M, N, t=TYPES[t])
+    B.fpq_block_linear(x, codes, scales, None, y, guarded(B.fpq_block_linear_workspace_size(M, N, K, int(t == "bf16"))))
+    within("y", y, *blocks.block_linear(host(x), wv, None, t == "bf16"))
+
+
+def off_one(x):
+    """The same values, contiguous, one element off the alignment of an allocation."""
+    return torch.full((x.numel() + 1,), float("nan"), dtype=x.dtype, device=DEV)[1:].view(x.shape).copy_(x)
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M", [1, 2, 16, 70])
+def test_tensors_off_alignment(M, t, guarded):
+    """The bits of aligned tensors' results within the bounds, from tensors that start one element further."""
+    N, K = 136, 72
+    c = Call(M, N, K, t)
+    c.x, c.gh, c.w, c.bias = off_one(c.x), off_one(c.gh), off_one(c.w), off_one(c.bias)
+    pre = c.check("type")[0]
+    want = [o.clone() for o in c.backward(pre, None)]
+    h = off_one(nan(M, N, t=c.t))
+    kept = off_one(nan(M, 2 * N, t=c.t))
+    B.fpq_gated(c.x, c.w, c.bias, 0, h, kept, None, guarded(B.fpq_gated_workspace_size(M, N, K, int(t == "bf16"))))
+    assert torch.equal(kept, pre) and torch.equal(h, c.forward()[0])
+    gx, gw, gb = off_one(nan(M, K, t=c.t)), off_one(nan(2 * N, K, t=c.t)), off_one(nan(2 * N))
+    B.fpq_gated_backward(c.x, None, c.w, kept, None, 0, c.gh, gx, gw, gb, guarded(B.fpq_gated_backward_workspace_size(M, N, K, int(t == "bf16"))))
+    a, g = c.kept_values(kept, None)
+    for name, got, (w, o) in zip(("grad_x", "grad_w", "grad_bias"), (gx, gw, gb), blocks.gated_backward(host(c.x), host(c.w), a, g, "silu", host(c.gh), t == "bf16")):
+        within(name, got, w, o)
+    assert torch.equal(gx, want[0]) and torch.equal(gw, want[1])
+    codes, scales = quantize(rows(torch.Generator().manual_seed(3), N, K, torch.float32), E2M1)
+    y, z = nan(M, N, t=c.t), off_one(nan(M, N, t=c.t))
+    ws = guarded(B.fpq_block_linear_workspace_size(M, N, K, int(t == "bf16")))
+    B.fpq_block_linear(c.x.clone(), codes, scales, c.bias.clone()[:N], y, ws)
+    B.fpq_block_linear(c.x, codes, scales, c.bias[:N], z, ws)
+    assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,K", [(3, 64), (700, 320), (40, 5120), (5, 12000), (7, 4099), (3, 9001)])
+def test_norm_gradients_over_what_they_came_from(M, K, t, guarded):
+    """grad_x in the place of grad_y or of grad_sum, with grad_w from the same call; the stream in the place of x: rows held in registers and rows read twice."""
+    g = torch.Generator().manual_seed(K)
+    x, res, gy, gs = (rows(g, M, K, TYPES[t]) for _ in range(4))
+    w = (1 + 0.3 * torch.randn(K, generator=g)).to(DEV)
+    total, y, rstd = nan(M, K, t=TYPES[t]), nan(M, K, t=TYPES[t]), nan(M)
+    B.fpq_rms_norm(x, res, w, 1e-6, total, y, rstd)
+    for i in range(2):
+        two = [x.clone(), res.clone()]
+        again = nan(M, K, t=TYPES[t])
+        B.fpq_rms_norm(*two, w, 1e-6, two[i], again)
+        assert torch.equal(two[i], total) and torch.equal(again, y)
+    size = B.fpq_rms_norm_backward_workspace_size(M, K)
+    gx, gw = nan(M, K, t=TYPES[t]), nan(K)
+    B.fpq_rms_norm_backward(total, w, rstd, gy, gs, gx, gw, guarded(size))
+    wx, ox, ww, ow = blocks.rms_norm_backward(host(total), host(w), host(rstd), host(gy), host(gs))
+    within("grad_x", gx, wx, ox + blocks.rounding(t == "bf16") * (np.abs(wx) + ox))
+    within("grad_w", gw, ww, ow + 2.0 ** -126)
+    for i in range(2):
+        two, again = [gy.clone(), gs.clone()], nan(K)
+        B.fpq_rms_norm_backward(total, w, rstd, *two, two[i], again, guarded(size))
+        assert torch.equal(two[i], gx) and torch.equal(again, gw)
+
+
+def test_rows_whose_squares_leave_the_range():
+    """A sum of squares past 2^128 makes the row zeros; squares below 2^-126 leave eps."""
+    x = torch.ones(3, 64, device=DEV)
+    x[0] *= 2.0 ** 70
+    x[1] *= 2.0 ** -70
+    y, rstd = nan(3, 64), nan(3)
+    B.fpq_rms_norm(x, None, None, 0.25, None, y, rstd)
+    assert not y[0].any() and rstd[0] == 0 and (y[1] == 2.0 ** -69).all() and rstd[1] == 2
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M", [1, 2, 4, 16, 40, 100])
+def test_scales_at_their_ends(M, t):
+    """Weights' scale bytes 0, 1, 2 and 253: values below 2^-126 may count as zero, others count in full."""
+    N, K = 48, 96
+    g = torch.Generator().manual_seed(7)
+    codes, scales = quantize(rows(g, N, K, torch.float32), E2M1)
+    scales[:12], scales[12:24], scales[24:36], scales[36:] = 0, 1, 2, 253
+    codes[36:] &= 0x33                                      # at most 1.5 2^126, no signs
+    x = rows(g, M, K, TYPES[t])
+    x = (x / x.abs().amax() / 8).to(TYPES[t])
+    wv = blocks.block_values(blocks.unpack(codes.cpu().numpy()), scales.cpu().numpy(), 4, K)
+    small = np.where(np.abs(wv) < 2.0 ** -126, np.abs(wv), 0.0)
+    # (scaled up, so that the results are in range: x is a few times 2^-3 at most, and K of them make less than 2^5; 2^5 2^100 1.5 2^126 would not be)
+    for part, up in ((slice(0, 36), 2.0 ** 100), (slice(36, 48), 1.0 / 64)):
+        xs = (x.float() * up).to(TYPES[t])
+        y = nan(M, N, t=TYPES[t])
+        B.fpq_block_linear(xs, codes, scales, None, y, torch.empty(max(16, B.fpq_block_linear_workspace_size(M, N, K, int(t == "bf16"))), dtype=torch.uint8, device=DEV))
+        want, off = blocks.block_linear(host(xs), wv, None, t == "bf16")
+        flushed = np.abs(host(xs)) @ small.T
+        within("y", y[:, part], want[:, part], (off + flushed * (1 + 2.0 ** -7))[:, part])
