@@ -661,7 +661,7 @@ int fpq_gated_backward(const fpq_gated_args_t *args, const void *x, const uint8_
  * grad_x or grad_w may be NULL; grad_x may be grad_y or grad_sum itself.  Sums and statistics are fp32, no atomics.  A NaN makes its row NaN; an infinity
  * becomes NaN and leaves zeros beside it; a sum of squares past 2^128 makes the row zeros, squares below 2^-149 count as none; with eps 0 a row of
  * zeros is NaN.
- * Matrices are of args->type with row strides ld_*; rows of multiples of 16 bytes that start at one are what the kernels are tuned for.
+ * Matrices are of args->type with row strides ld_*; rows of multiples of 16 bytes are what the kernels are tuned for.
  * eps >= 0 and finite (FPQ_ERR_SCALE).  workspace of the backward call: the stated bytes, 16-byte aligned, no initialisation (may be NULL
  * without grad_w).  Limits: M at most 2^28, K and strides at most 2^20, M K below 2^34 (FPQ_ERR_SHAPE). */
 typedef struct fpq_norm_args {

@@ -63,14 +63,14 @@ Operand operand(const void* p, int type, int64_t rows, int64_t cols, int64_t ld,
     if (reads(p, type, rows, cols, ld)) return Operand{static_cast<const __bf16*>(p), ld, 0};
     const int64_t to = round8(cols);
     __bf16* const dst = room.take<__bf16>((size_t)rows * to * 2 * planes_of(type));
-    packs.m[packs.count++] = PackItem{p, nullptr, rows, cols, ld, dst, to, rows * to, 0, {}, type, 0};
+    packs.m[packs.count++] = PackItem{p, nullptr, rows, cols, ld, dst, to, rows * to, 0, {}, type};
     return Operand{dst, to, rows * to};
 }
 Operand operand_of_blocks(const void* codes, const uint8_t* scales, int64_t rows, int64_t cols, int bits, Room& room, PackList& packs)
 {
     const int64_t to = block_padded(cols);
     __bf16* const dst = room.take<__bf16>((size_t)rows * to * 2);
-    packs.m[packs.count++] = PackItem{codes, scales, rows, to, to, dst, to, 0, 0, {}, bits, 0};
+    packs.m[packs.count++] = PackItem{codes, scales, rows, to, to, dst, to, 0, 0, {}, bits};
     return Operand{dst, to, 0};
 }
 
@@ -151,22 +151,16 @@ RowsArgs rows_args(const void* x, int type, int64_t M, int64_t N, int64_t K, int
     r.K = (int)K;
     r.bias = bias;
     r.f32 = type == FPQ_TYPE_FP32;
-    r.vec_x = aligned(x, 16) && K % 8 == 0 && r.ld_x * size_of(type) % 16 == 0;
     return r;
 }
 
 // Whether the form of few rows takes gated projections: weights read where they are.  In bf16 up to 16 rows, more only of weights that the L2 holds: in
 // 64 rows their share of the matrix unit and x again in every workgroup cost more than the tiles' rows without a result (48 rows of 4096 -> 10240:
 // 55.8 us, in tiles 36.4; of 1280 -> 5120: 14.2 and 16.2).  In fp32 tiles have to pack the weights first (64 rows of 4096 -> 10240: 143 us, in tiles 281).
-bool few_rows(const fpq_gated_args_t* p, const void* w)
+bool few_rows(const fpq_gated_args_t* p)
 {
     const bool fits = p->type == FPQ_TYPE_FP32 || p->M <= 16 || 4 * p->N * p->K <= (int64_t)32 << 20;
-    return p->M <= kFewRows && fits && aligned(w, 16) && p->K % 8 == 0 && p->ld_w * size_of(p->type) % 16 == 0;
-}
-
-bool norm_vec(const void* p, int64_t ld, int64_t M, int64_t K, size_t size)
-{
-    return !p || (aligned(p, 16) && K * size % 16 == 0 && (M <= 1 || ld * size % 16 == 0));
+    return p->M <= kFewRows && fits;
 }
 
 int check_norm(const fpq_norm_args_t* p)
@@ -320,7 +314,7 @@ int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const flo
     if (!aligned(x, size) || !aligned(w, size) || !aligned(h, size) || !aligned(pre, pre_scales ? 16 : size) || !aligned(bias, 4)) return FPQ_ERR_ALIGN;
     if (workspace_bad(workspace, workspace_bytes, fpq_gated_workspace_size(M, N, K, p->type), &st)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (few_rows(p, w)) {
+    if (few_rows(p)) {
         RowsArgs r = rows_args(x, p->type, M, N, K, p->ld_x, bias);
         r.w = w;
         r.ld_w = p->ld_w;
@@ -431,8 +425,6 @@ int fpq_rms_norm(const fpq_norm_args_t* p, const void* x, const void* residual, 
     a.ld_sum = stride(p->ld_sum, K, M);
     a.ld_y = stride(p->ld_y, K, M);
     a.eps = p->eps;
-    a.vec = norm_vec(x, p->ld_x, M, K, size) && norm_vec(residual, p->ld_residual, M, K, size) && norm_vec(sum, p->ld_sum, M, K, size) &&
-            norm_vec(y, p->ld_y, M, K, size);
     return launch_norm(a, p->type, static_cast<hipStream_t>(stream));
 }
 
@@ -472,8 +464,6 @@ int fpq_rms_norm_backward(const fpq_norm_args_t* p, const void* sum, const float
     a.ld_gy = stride(p->ld_grad_y, K, M);
     a.ld_gs = stride(p->ld_grad_sum, K, M);
     a.ld_gx = stride(p->ld_grad_x, K, M);
-    a.vec = norm_vec(sum, p->ld_sum, M, K, size) && norm_vec(grad_y, p->ld_grad_y, M, K, size) && norm_vec(grad_sum, p->ld_grad_sum, M, K, size) &&
-            norm_vec(grad_x, p->ld_grad_x, M, K, size);
     return launch_norm_backward(a, p->type, s);
 }
 

@@ -19,7 +19,6 @@ struct PackItem {
     int64_t first;              // workgroup of the launch
     RowOf pieces;               // of eight elements
     int kind;                   // FPQ_TYPE_FP32, FPQ_TYPE_BF16, or 8 or 4: blocks
-    int vec;
 };
 struct PackList {
     PackItem m[3];
@@ -68,7 +67,6 @@ struct NormArgs {
     int64_t M, K, ld_x, ld_residual, ld_sum, ld_y;
     int64_t first;              // row of a launch
     float eps;
-    int vec;                    // all rows may be taken 16 bytes at a time
     int past;                   // results are stored past the L2
 };
 int launch_norm(const NormArgs& p, int type, hipStream_t s);
@@ -79,7 +77,7 @@ struct NormBackward {
     void* gx;
     float *gw, *part;
     int64_t M, K, ld_sum, ld_gy, ld_gs, ld_gx;
-    int vec, past;
+    int past;
 };
 size_t norm_part_bytes(int64_t M, int64_t K);
 int launch_norm_backward(const NormBackward& p, int type, hipStream_t s);

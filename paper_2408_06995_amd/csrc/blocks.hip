@@ -8,15 +8,18 @@ namespace {
 
 // Eight elements from column k on; zeros from `cols` on.
 template <typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t k, int64_t cols, bool vec, float (&v)[8])
+__device__ __forceinline__ void load8(const T* row, int64_t k, int64_t cols, float (&v)[8])
 {
-    if (vec && k + 8 <= cols) {
+    if (k + 8 <= cols) {
         if constexpr (sizeof(T) == 4) {
-            const float4 a = *reinterpret_cast<const float4*>(row + k), b = *reinterpret_cast<const float4*>(row + k + 4);
-            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+            const piece16 a = *reinterpret_cast<const piece16*>(row + k), b = *reinterpret_cast<const piece16*>(row + k + 4);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                v[t] = __uint_as_float(a[t]);
+                v[4 + t] = __uint_as_float(b[t]);
+            }
         } else {
-            const uint4 x = *reinterpret_cast<const uint4*>(row + k);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            const piece16 w = *reinterpret_cast<const piece16*>(row + k);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 v[2 * t] = __uint_as_float(w[t] << 16);
@@ -30,14 +33,16 @@ __device__ __forceinline__ void load8(const T* row, int64_t k, int64_t cols, boo
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T* row, int64_t k, int64_t cols, bool vec, const float (&v)[8])
+__device__ __forceinline__ void store8(T* row, int64_t k, int64_t cols, const float (&v)[8])
 {
-    if (vec && k + 8 <= cols) {
+    if (k + 8 <= cols) {
         if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4*>(row + k) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4*>(row + k + 4) = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+            for (int t = 0; t < 8; t += 4)
+                *reinterpret_cast<piece16*>(row + k + t) =
+                    piece16{__float_as_uint(v[t]), __float_as_uint(v[t + 1]), __float_as_uint(v[t + 2]), __float_as_uint(v[t + 3])};
         } else {
-            *reinterpret_cast<uint4*>(row + k) = make_uint4(pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]), pair_bf16(v[4], v[5]), pair_bf16(v[6], v[7]));
+            *reinterpret_cast<piece16*>(row + k) = piece16{pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]), pair_bf16(v[4], v[5]), pair_bf16(v[6], v[7])};
         }
     } else {
 #pragma unroll
@@ -46,13 +51,21 @@ __device__ __forceinline__ void store8(T* row, int64_t k, int64_t cols, bool vec
     }
 }
 
-// Eight values in NP planes.
+// Eight values in NP planes; of fewer than eight the first `some`.
 template <int NP>
-__device__ __forceinline__ void store_planes(__bf16* dst, int64_t plane, const float (&v)[8])
+__device__ __forceinline__ void store_planes(__bf16* dst, int64_t plane, const float (&v)[8], int64_t some = 8)
 {
     const Frag<NP> f = frag_of<NP>(v);
+    if (some >= 8) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p) *reinterpret_cast<v8bf*>(dst + p * plane) = f.p[p];
+        for (int p = 0; p < NP; ++p) *reinterpret_cast<piece16*>(dst + p * plane) = __builtin_bit_cast(piece16, f.p[p]);
+    } else {
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+                if (e < some) dst[p * plane + e] = f.p[p][e];
+    }
 }
 
 // Eight codes of a block.
@@ -94,8 +107,8 @@ __device__ __forceinline__ void pack_pieces(const PackItem& q, int64_t id0)
         if (id >= n) return;
         const int64_t r = row_at(q.pieces, id), k = (id - r * per) * 8;
         float v[8];
-        if constexpr (KIND == FPQ_TYPE_FP32) load8(static_cast<const float*>(q.src) + r * q.ld, k, q.cols, q.vec, v);
-        else if constexpr (KIND == FPQ_TYPE_BF16) load8(static_cast<const __bf16*>(q.src) + r * q.ld, k, q.cols, q.vec, v);
+        if constexpr (KIND == FPQ_TYPE_FP32) load8(static_cast<const float*>(q.src) + r * q.ld, k, q.cols, v);
+        else if constexpr (KIND == FPQ_TYPE_BF16) load8(static_cast<const __bf16*>(q.src) + r * q.ld, k, q.cols, v);
         else decode8<KIND == 8>(static_cast<const uint8_t*>(q.src), id * 8, scale_of(q.scales[id / 4]), v);
         store_planes<NP>(q.dst + r * q.ld_dst + k, q.plane, v);
     }
@@ -113,7 +126,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackList p)
 }
 
 template <bool EIGHT, typename T>
-__global__ __launch_bounds__(256) void decode_kernel(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, RowOf pieces, T* dst, int64_t ld_dst, int vec)
+__global__ __launch_bounds__(256) void decode_kernel(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, RowOf pieces, T* dst, int64_t ld_dst)
 {
     const int64_t n = rows * pieces.per, id0 = (int64_t)blockIdx.x * (256 * kEach) + threadIdx.x;
     float v[kEach][8];
@@ -127,13 +140,13 @@ __global__ __launch_bounds__(256) void decode_kernel(const uint8_t* codes, const
         const int64_t id = id0 + 256 * i;
         if (id >= n) return;
         const int64_t r = row_at(pieces, id);
-        store8(dst + r * ld_dst, (id - r * pieces.per) * 8, cols, vec, v[i]);
+        store8(dst + r * ld_dst, (id - r * pieces.per) * 8, cols, v[i]);
     }
 }
 
 template <bool EIGHT, typename T>
 __global__ __launch_bounds__(256) void block_quantize_kernel(const T* x, int64_t rows, int64_t cols, RowOf pieces, int64_t ld, const uint8_t* mask, uint8_t* codes,
-                                                             uint8_t* scales, int vec)
+                                                             uint8_t* scales)
 {
     const int64_t n = rows * pieces.per, id0 = (int64_t)blockIdx.x * (256 * kEach) + threadIdx.x;
     float all[kEach][8];
@@ -142,7 +155,7 @@ __global__ __launch_bounds__(256) void block_quantize_kernel(const T* x, int64_t
     for (int i = 0; i < kEach; ++i) {
         const int64_t id = min(id0 + 256 * i, n - 1);                // (n is a multiple of four: a block's lanes stay together)
         row[i] = row_at(pieces, id);
-        load8(x + row[i] * ld, (id - row[i] * pieces.per) * 8, cols, vec, all[i]);
+        load8(x + row[i] * ld, (id - row[i] * pieces.per) * 8, cols, all[i]);
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -177,8 +190,7 @@ __global__ __launch_bounds__(256) void block_quantize_kernel(const T* x, int64_t
 
 constexpr int kStripColumns = 512;
 
-// WIDE: a lane has eight neighbouring columns; else a column of each of eight groups of 64.
-template <bool WIDE>
+// A lane's sums of eight neighbouring columns, over the four wavefronts.
 __device__ __forceinline__ void strip_sum(float (&sum)[8], int64_t first, int64_t cols, float* part)
 {
     __shared__ float room[3][64 * 8];
@@ -193,13 +205,13 @@ __device__ __forceinline__ void strip_sum(float (&sum)[8], int64_t first, int64_
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float t = (sum[e] + room[0][e * 64 + lane]) + (room[1][e * 64 + lane] + room[2][e * 64 + lane]);
-        const int64_t k = WIDE ? first + 8 * lane + e : first + 64 * e + lane;
+        const int64_t k = first + 8 * lane + e;
         if (k < cols) part[k] = t;
     }
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void column_sums_kernel(const T* x, int64_t M, int64_t N, int64_t ld, int64_t rows, float* part, int vec)
+__global__ __launch_bounds__(256) void column_sums_kernel(const T* x, int64_t M, int64_t N, int64_t ld, int64_t rows, float* part)
 {
     const int64_t k = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8, m1 = min(M, (int64_t)(blockIdx.y + 1) * rows);
     float sum[8] = {};
@@ -208,7 +220,7 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const T* x, int64_t M,
         for (; m + 12 < m1; m += 16) {                               // four rows' loads at once
             float v[4][8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load8(x + (m + 4 * i) * ld, k, N, vec, v[i]);
+            for (int i = 0; i < 4; ++i) load8(x + (m + 4 * i) * ld, k, N, v[i]);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -216,12 +228,12 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const T* x, int64_t M,
         }
         for (; m < m1; m += 4) {
             float v[8];
-            load8(x + m * ld, k, N, vec, v);
+            load8(x + m * ld, k, N, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += v[e];
         }
     }
-    strip_sum<true>(sum, (int64_t)blockIdx.x * kStripColumns, N, part + (int64_t)blockIdx.y * N);
+    strip_sum(sum, (int64_t)blockIdx.x * kStripColumns, N, part + (int64_t)blockIdx.y * N);
 }
 
 // 64 columns, 16 wavefronts over the parts
@@ -249,92 +261,57 @@ __global__ __launch_bounds__(1024) void part_sums_kernel(const float* part, int 
     out[k] = sum;
 }
 
-// KEPT: 0 the type, 1 blocks.  WIDE: a lane has eight neighbouring columns of rows that are whole pieces; else, one column of each of eight
-// neighbouring groups of 64, so that a wavefront's accesses are whole lines either way.
-template <typename T, int KEPT, bool WIDE>
+// KEPT: 0 the type, 1 blocks.
+template <typename T, int KEPT>
 __global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward p, int64_t rows)
 {
-    const int lane = threadIdx.x & 63;
     const int64_t first = (int64_t)blockIdx.x * kStripColumns, m1 = min(p.M, (int64_t)(blockIdx.y + 1) * rows), N = p.N;
-    const int64_t k = first + 8 * lane, np = (N + 31) / 32 * 32;
+    const int64_t k = first + 8 * (threadIdx.x & 63), np = (N + 31) / 32 * 32;
     constexpr int NP = kPlanes<T>;
-    auto col = [&](int e) { return WIDE ? k + e : first + 64 * e + lane; };
     float sum_a[8] = {}, sum_g[8] = {};
-    if (!WIDE || k < N)
+    if (k < N)
         for (int64_t m = (int64_t)blockIdx.y * rows + (threadIdx.x >> 6); m < m1; m += 4) {
             float a[8], g[8], gh[8], da[8], dg[8];
-            const T* const up = static_cast<const T*>(p.gh) + m * p.ld_gh;
-            if constexpr (WIDE) {
-                load8(up, k, N, true, gh);
-                if constexpr (KEPT) {
-                    const uint8_t* const s = p.pre_scales + m * (np / 16) + k / 32;
-                    const uint8_t* const c = static_cast<const uint8_t*>(p.pre) + m * 2 * np;
-                    decode8<true>(c, k, scale_of(s[0]), a);
-                    decode8<true>(c + np, k, scale_of(s[np / 32]), g);
-                } else {
-                    const T* const row = static_cast<const T*>(p.pre) + m * 2 * N;
-                    load8(row, k, N, true, a);
-                    load8(row + N, k, N, true, g);
-                }
+            load8(static_cast<const T*>(p.gh) + m * p.ld_gh, k, N, gh);
+            if constexpr (KEPT) {
+                const uint8_t* const s = p.pre_scales + m * (np / 16) + k / 32;
+                const uint8_t* const c = static_cast<const uint8_t*>(p.pre) + m * 2 * np;
+                decode8<true>(c, k, scale_of(s[0]), a);
+                decode8<true>(c + np, k, scale_of(s[np / 32]), g);
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int64_t c = col(e);
-                    const bool in = c < N;
-                    gh[e] = in ? (float)up[c] : 0.0f;
-                    if constexpr (KEPT) {
-                        const uint8_t* const s = p.pre_scales + m * (np / 16) + c / 32;
-                        const uint8_t* const q = static_cast<const uint8_t*>(p.pre) + m * 2 * np + c;
-                        a[e] = in ? __builtin_amdgcn_cvt_f32_fp8(q[0], 0) * scale_of(s[0]) : 0.0f;
-                        g[e] = in ? __builtin_amdgcn_cvt_f32_fp8(q[np], 0) * scale_of(s[np / 32]) : 0.0f;
-                    } else {
-                        const T* const row = static_cast<const T*>(p.pre) + m * 2 * N;
-                        a[e] = in ? (float)row[c] : 0.0f;
-                        g[e] = in ? (float)row[N + c] : 0.0f;
-                    }
-                }
+                const T* const row = static_cast<const T*>(p.pre) + m * 2 * N;
+                load8(row, k, N, a);
+                load8(row + N, k, N, g);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float slope;
                 da[e] = gh[e] * gate_of<true>(p.act, g[e], &slope);
                 dg[e] = gh[e] * a[e] * slope;
-                if (!WIDE && col(e) >= N) da[e] = dg[e] = 0.0f;
                 sum_a[e] += da[e];
                 sum_g[e] += dg[e];
             }
             if (!p.d) continue;
-            __bf16* const d = p.d + m * p.ld_d;
-            if constexpr (WIDE) {
-                store_planes<NP>(d + k, p.plane, da);
-                store_planes<NP>(d + N + k, p.plane, dg);
-            } else {
-                const Frag<NP> fa = frag_of<NP>(da), fg = frag_of<NP>(dg);
+            __bf16* const d = p.d + m * p.ld_d + k;
+            store_planes<NP>(d, p.plane, da, N - k);
+            const int64_t left = p.ld_d - N - k;
+            if (N - k < 8) {                                          // the row's end, and up to six zeros behind it
 #pragma unroll
-                for (int q = 0; q < NP; ++q)
+                for (int e = 0; e < 8; ++e)
+                    if (k + e >= N) dg[e] = 0.0f;
+                for (int64_t e = 8; e < left; ++e)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int64_t c = col(e);
-                        if (c < N) {
-                            d[q * p.plane + c] = fa.p[q][e];
-                            d[q * p.plane + N + c] = fg.p[q][e];
-                        } else if (c < N + p.ld_d - 2 * N) {         // zeros behind the row
-                            d[q * p.plane + N + c] = (__bf16)0.0f;
-                        }
-                    }
+                    for (int q = 0; q < NP; ++q) d[q * p.plane + N + e] = (__bf16)0.0f;
             }
+            store_planes<NP>(d + N, p.plane, dg, left);
         }
     if (!p.part) return;
     float* const part = p.part + (int64_t)blockIdx.y * 2 * N;
-    strip_sum<WIDE>(sum_a, first, N, part);
-    strip_sum<WIDE>(sum_g, first, N, part + N);
+    strip_sum(sum_a, first, N, part);
+    strip_sum(sum_g, first, N, part + N);
 }
 
 unsigned grid_of(int64_t pieces) { return (unsigned)((pieces + 256 * kEach - 1) / (256 * kEach)); }
-bool rows_vec(const void* p, int64_t ld, int type)
-{
-    return ((uintptr_t)p & 15) == 0 && ld % (type == FPQ_TYPE_FP32 ? 4 : 8) == 0;
-}
 int launched() { return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH; }
 
 }  // namespace
@@ -345,7 +322,6 @@ int launch_packs(PackList& p, hipStream_t s)
     for (int i = 0; i < p.count; ++i) {
         PackItem& q = p.m[i];
         q.first = at;
-        q.vec = q.kind != 8 && q.kind != 4 && rows_vec(q.src, q.ld, q.kind);
         q.pieces = row_of(q.rows, q.ld_dst / 8);
         const int64_t blocks = grid_of(q.rows * (q.ld_dst / 8));
         if (at && at + blocks >= (int64_t)1 << 24) {                 // (a launch has fewer than 2^32 threads)
@@ -369,8 +345,7 @@ int launch_decode(const uint8_t* codes, const uint8_t* scales, int64_t rows, int
     const int64_t padded = block_padded(cols);
     const unsigned grid = grid_of(rows * (padded / 8));
     if (!grid) return FPQ_OK;
-    const int vec = rows_vec(dst, ld_dst, f32 ? FPQ_TYPE_FP32 : FPQ_TYPE_BF16);
-    auto run = [&](auto kernel, auto* to) { kernel<<<dim3(grid), dim3(256), 0, s>>>(codes, scales, rows, cols, row_of(rows, padded / 8), to, ld_dst, vec); };
+    auto run = [&](auto kernel, auto* to) { kernel<<<dim3(grid), dim3(256), 0, s>>>(codes, scales, rows, cols, row_of(rows, padded / 8), to, ld_dst); };
     if (f32) eight ? run(decode_kernel<true, float>, static_cast<float*>(dst)) : run(decode_kernel<false, float>, static_cast<float*>(dst));
     else eight ? run(decode_kernel<true, __bf16>, static_cast<__bf16*>(dst)) : run(decode_kernel<false, __bf16>, static_cast<__bf16*>(dst));
     return launched();
@@ -382,8 +357,7 @@ int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t
     const int64_t padded = block_padded(K);
     const unsigned grid = grid_of(M * (padded / 8));
     if (!grid) return FPQ_OK;
-    const int vec = rows_vec(x, ld, type);
-    auto run = [&](auto kernel, auto* from) { kernel<<<dim3(grid), dim3(256), 0, s>>>(from, M, K, row_of(M, padded / 8), ld, mask, codes, scales, vec); };
+    auto run = [&](auto kernel, auto* from) { kernel<<<dim3(grid), dim3(256), 0, s>>>(from, M, K, row_of(M, padded / 8), ld, mask, codes, scales); };
     if (type == FPQ_TYPE_FP32) eight ? run(block_quantize_kernel<true, float>, static_cast<const float*>(x)) : run(block_quantize_kernel<false, float>, static_cast<const float*>(x));
     else eight ? run(block_quantize_kernel<true, __bf16>, static_cast<const __bf16*>(x)) : run(block_quantize_kernel<false, __bf16>, static_cast<const __bf16*>(x));
     return launched();
@@ -411,9 +385,8 @@ int launch_column_sums(const void* x, int type, int64_t M, int64_t N, int64_t ld
 {
     const RowParts r = row_parts(M, N);
     const dim3 grid((unsigned)((N + kStripColumns - 1) / kStripColumns), (unsigned)r.parts);
-    const int vec = rows_vec(x, ld, type);
-    if (type == FPQ_TYPE_FP32) column_sums_kernel<<<grid, dim3(256), 0, s>>>(static_cast<const float*>(x), M, N, ld, r.rows, part, vec);
-    else column_sums_kernel<<<grid, dim3(256), 0, s>>>(static_cast<const __bf16*>(x), M, N, ld, r.rows, part, vec);
+    if (type == FPQ_TYPE_FP32) column_sums_kernel<<<grid, dim3(256), 0, s>>>(static_cast<const float*>(x), M, N, ld, r.rows, part);
+    else column_sums_kernel<<<grid, dim3(256), 0, s>>>(static_cast<const __bf16*>(x), M, N, ld, r.rows, part);
     const int st = launched();
     return st == FPQ_OK ? launch_part_sums(part, r.parts, N, out, s) : st;
 }
@@ -421,20 +394,12 @@ int launch_column_sums(const void* x, int type, int64_t M, int64_t N, int64_t ld
 int launch_gate_backward(const GateBackward& p, hipStream_t s)
 {
     const RowParts r = row_parts(p.M, p.N);
-    const bool wide = p.N % 8 == 0 && rows_vec(p.gh, p.ld_gh, p.type) && (p.pre_scales || rows_vec(p.pre, p.N, p.type));
-    // (the zeros behind the rows are a strip's work too, where they begin one)
-    const int64_t columns = p.d ? p.N + p.ld_d - 2 * p.N : p.N;
-    const dim3 grid((unsigned)((columns + kStripColumns - 1) / kStripColumns), (unsigned)r.parts);
+    const dim3 grid((unsigned)((p.N + kStripColumns - 1) / kStripColumns), (unsigned)r.parts);
     GateBackward q = p;
     if (!p.grad_bias) q.part = nullptr;
     auto run = [&](auto kernel) { kernel<<<grid, dim3(256), 0, s>>>(q, r.rows); };
-    auto kept = [&](auto t, auto w) {
-        using T = decltype(t);
-        constexpr bool W = decltype(w)::value;
-        p.pre_scales ? run(gate_backward_kernel<T, 1, W>) : run(gate_backward_kernel<T, 0, W>);
-    };
-    if (p.type == FPQ_TYPE_FP32) wide ? kept(0.0f, std::true_type()) : kept(0.0f, std::false_type());
-    else wide ? kept((__bf16)0.0f, std::true_type()) : kept((__bf16)0.0f, std::false_type());
+    if (p.type == FPQ_TYPE_FP32) p.pre_scales ? run(gate_backward_kernel<float, 1>) : run(gate_backward_kernel<float, 0>);
+    else p.pre_scales ? run(gate_backward_kernel<__bf16, 1>) : run(gate_backward_kernel<__bf16, 0>);
     const int st = launched();
     return st == FPQ_OK && q.part ? launch_part_sums(q.part, r.parts, 2 * p.N, p.grad_bias, s) : st;
 }

@@ -18,6 +18,9 @@
 
 namespace fpq {
 
+// Sixteen bytes at the address of any element: the hardware takes them in one access, which costs more only where a line ends within.
+typedef uint32_t piece16 __attribute__((ext_vector_type(4), aligned(2), may_alias));
+
 struct Operand {
     const __bf16* p;
     int64_t ld, plane;          // in elements
@@ -229,25 +232,27 @@ __device__ __forceinline__ MatmulPlace matmul_place(const MatmulArgs& p)
     return r;
 }
 
-// Four neighbouring results of a row; `vec`: they lie within the row and may be stored together.
-__device__ __forceinline__ void put4(void* out, int64_t at, int f32, int n, int N, bool vec, const float (&v)[4])
+// Four neighbouring results of a row from column n on, as far as there are N.
+typedef uint32_t piece8 __attribute__((ext_vector_type(2), aligned(2), may_alias));
+__device__ __forceinline__ void put4(void* out, int64_t at, int f32, int n, int N, const float (&v)[4])
 {
+    const bool all = n + 4 <= N;
     if (f32) {
         float* const o = static_cast<float*>(out) + at;
-        if (vec) {
-            *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+        if (all) {
+            *reinterpret_cast<piece16*>(o) = piece16{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 3; ++e)
                 if (n + e < N) o[e] = v[e];
         }
     } else {
         __bf16* const o = static_cast<__bf16*>(out) + at;
-        if (vec) {
-            *reinterpret_cast<uint2*>(o) = make_uint2(pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]));
+        if (all) {
+            *reinterpret_cast<piece8*>(o) = piece8{pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3])};
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 3; ++e)
                 if (n + e < N) o[e] = (__bf16)v[e];
         }
     }
@@ -266,52 +271,44 @@ struct RowStage {
         const int lane = threadIdx.x & 63;
         *reinterpret_cast<V*>(room + (lane & 31) * STRIDE + (2 * q + (lane >> 5)) * (int)sizeof(V)) = v;
     }
-    // `rows` rows exist, and `bytes` of each
-    __device__ __forceinline__ void flush(char* to, int64_t ld, int rows, int bytes) const
+    // `rows` rows exist, and `bytes` of each, elements of type T
+    template <typename T>
+    __device__ __forceinline__ void flush(T* to, int64_t ld, int rows, int bytes) const
     {
         asm volatile("" ::: "memory");                   // (a wavefront's accesses of LDS are carried out in order)
         const int lane = threadIdx.x & 63;
+        if (bytes % 16 == 0) {
 #pragma unroll
-        for (int i = 0; i < B / 32; ++i) {
-            const int id = i * 64 + lane, r = id / LANES, at = id % LANES * 16;
-            const uint4 v = *reinterpret_cast<const uint4*>(room + r * STRIDE + at);
-            if (r < rows && at < bytes) *reinterpret_cast<uint4*>(to + r * ld + at) = v;
+            for (int i = 0; i < B / 32; ++i) {
+                const int id = i * 64 + lane, r = id / LANES, at = id % LANES * 16;
+                const uint4 v = *reinterpret_cast<const uint4*>(room + r * STRIDE + at);
+                if (r < rows && at < bytes) *reinterpret_cast<piece16*>(to + r * ld + at / (int)sizeof(T)) = __builtin_bit_cast(piece16, v);
+            }
+        } else {                                         // (the last columns of a matrix: an element at a time)
+            const int n = bytes / (int)sizeof(T);
+#pragma unroll 1
+            for (int r = lane >> 5; r < rows; r += 2)
+                if ((lane & 31) < n) to[r * ld + (lane & 31)] = reinterpret_cast<const T*>(room + r * STRIDE)[lane & 31];
         }
         asm volatile("" ::: "memory");
     }
 };
 
-// Four results of each q = 0 .. 3 of 32 rows from column n on, in the type.  `pieces`: rows are whole aligned pieces of 16 bytes; others are
-// stored an element at a time, 32 lanes to a row.
+// Four results of each q = 0 .. 3 of 32 rows from column n on, in the type.
 template <typename F>
-__device__ __forceinline__ void put_rows(char* room, void* out, int64_t ld, int f32, int64_t m0, int rows, int n, int N, bool pieces, F&& value)
+__device__ __forceinline__ void put_rows(char* room, void* out, int64_t ld, int f32, int64_t m0, int rows, int n, int N, F&& value)
 {
-    const int lane = threadIdx.x & 63, left = min(N - n, 32);
-    auto elements = [&](auto* to, int stride) {
-        using T = std::remove_reference_t<decltype(*to)>;
-        asm volatile("" ::: "memory");
-#pragma unroll 4
-        for (int i = 0; i < 16; ++i) {
-            const int r = 2 * i + (lane >> 5), c = lane & 31;
-            const T v = reinterpret_cast<const T*>(room + r * stride)[c];
-            if (r < rows && c < left) to[r * ld + c] = v;
-        }
-        asm volatile("" ::: "memory");
-    };
+    const int left = min(N - n, 32);
     if (f32) {
-        float* const to = static_cast<float*>(out) + m0 * ld + n;
         const RowStage<128> s{room};
 #pragma unroll
         for (int q = 0; q < 4; ++q) s.put(q, make_float4(value(4 * q), value(4 * q + 1), value(4 * q + 2), value(4 * q + 3)));
-        if (pieces) s.flush(reinterpret_cast<char*>(to), 4 * ld, rows, 4 * left);
-        else elements(to, s.STRIDE);
+        s.flush(static_cast<uint32_t*>(out) + m0 * ld + n, ld, rows, 4 * left);
     } else {
-        uint16_t* const to = static_cast<uint16_t*>(out) + m0 * ld + n;
         const RowStage<64> s{room};
 #pragma unroll
         for (int q = 0; q < 4; ++q) s.put(q, make_uint2(pair_bf16(value(4 * q), value(4 * q + 1)), pair_bf16(value(4 * q + 2), value(4 * q + 3))));
-        if (pieces) s.flush(reinterpret_cast<char*>(to), 2 * ld, rows, 2 * left);
-        else elements(to, s.STRIDE);
+        s.flush(static_cast<uint16_t*>(out) + m0 * ld + n, ld, rows, 2 * left);
     }
 }
 
@@ -322,42 +319,33 @@ template <int SCALES>
 __device__ __forceinline__ void gated_block(const Gate& p, int f32, int64_t m0, int rows, int n0, int N, const float (&a)[16], const float (&g)[16], char* room,
                                             uint8_t* scales)
 {
-    const int lane = threadIdx.x & 63, h = lane >> 5, np = (N + 31) & ~31, e = f32 ? 4 : 8;
+    const int lane = threadIdx.x & 63, h = lane >> 5, np = (N + 31) & ~31;
     if (n0 >= N) return;
-    auto whole = [&](const void* o, int64_t ld) { return N % e == 0 && ld % e == 0 && ((uintptr_t)o & 15) == 0; };
-    put_rows(room, p.h, p.ld_h, f32, m0, rows, n0, N, whole(p.h, p.ld_h), [&](int i) { return a[i] * gate_of<false>(p.act, g[i], nullptr); });
+    put_rows(room, p.h, p.ld_h, f32, m0, rows, n0, N, [&](int i) { return a[i] * gate_of<false>(p.act, g[i], nullptr); });
     if (!p.pre) return;
     if (!p.pre_scales) {
-        const bool w = whole(p.pre, p.ld_pre);
-        put_rows(room, p.pre, p.ld_pre, f32, m0, rows, n0, N, w, [&](int i) { return a[i]; });
-        // (the gates' columns are those from N on; N is a whole number of pieces where the values' rows are)
-        put_rows(room, f32 ? static_cast<void*>(static_cast<float*>(p.pre) + N) : static_cast<void*>(static_cast<__bf16*>(p.pre) + N), p.ld_pre, f32, m0, rows, n0, N, w,
+        put_rows(room, p.pre, p.ld_pre, f32, m0, rows, n0, N, [&](int i) { return a[i]; });
+        put_rows(room, f32 ? static_cast<void*>(static_cast<float*>(p.pre) + N) : static_cast<void*>(static_cast<__bf16*>(p.pre) + N), p.ld_pre, f32, m0, rows, n0, N,
                  [&](int i) { return g[i]; });
         return;
     }
-    auto codes = [&](auto part, const float (&v)[16], uint8_t* to, uint8_t* scale) {
-        constexpr bool PART = decltype(part)::value;                  // of the 32 columns not all are there
-        auto at = [&](int i) { return !PART || n0 + 8 * (i / 4) + 4 * h + i % 4 < N ? v[i] : 0.0f; };
+    // (columns behind the last are zeros)
+    auto codes = [&](const float (&x)[16], uint8_t* to, uint8_t* scale) {
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(at(i)) & 0x7fffffffu);
+        for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
         top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
         const uint32_t s = block_scale8(top);
         const float r = inverse_scale(s);
         const RowStage<32> stage{room};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) stage.put(q, codes8(at(4 * q) * r, at(4 * q + 1) * r, at(4 * q + 2) * r, at(4 * q + 3) * r));
-        stage.flush(reinterpret_cast<char*>(to), 2 * (int64_t)np, rows, 32);
+        for (int q = 0; q < 4; ++q) stage.put(q, codes8(x[4 * q] * r, x[4 * q + 1] * r, x[4 * q + 2] * r, x[4 * q + 3] * r));
+        stage.flush(to, 2 * (int64_t)np, rows, 32);
         if (h == 0) scale[(lane & 31) * 2 * SCALES] = (uint8_t)s;
     };
     uint8_t* const to = static_cast<uint8_t*>(p.pre) + m0 * (2 * (int64_t)np) + n0;
-    if (n0 + 32 <= N) {
-        codes(std::false_type(), a, to, scales);
-        codes(std::false_type(), g, to + np, scales + SCALES);
-    } else {
-        codes(std::true_type(), a, to, scales);
-        codes(std::true_type(), g, to + np, scales + SCALES);
-    }
+    codes(a, to, scales);
+    codes(g, to + np, scales + SCALES);
 }
 
 // All but the last COUNT loads of this wavefront have landed, its reads of LDS are done, and all wavefronts are here.
@@ -538,7 +526,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
             for (int u = 0; u < TM; ++u) {
                 const int m = m0 + (wm * TM + u) * 32;
                 if (m >= p.M) break;
-                put_rows(lds + wave * ROOM, part + (END == kGated ? v / G * p.N : 0), cols, 1, m, min(p.M - m, 32), nb, p.N, (p.N & 3) == 0,
+                put_rows(lds + wave * ROOM, part + (END == kGated ? v / G * p.N : 0), cols, 1, m, min(p.M - m, 32), nb, p.N,
                          [&](int i) { return acc[u][v][i]; });
             }
         }
@@ -569,6 +557,11 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
                     a[i] = acc[u][v][i] + ba[i];
                     g[i] = acc[u][G + v][i] + bg[i];
                 }
+                if (nb + 32 > p.N) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (nb + 8 * (i / 4) + 4 * h + i % 4 >= p.N) a[i] = g[i] = 0.0f;
+                }
                 gated_block<SC>(p.gate, p.out_f32, m, min(p.M - m, 32), nb, p.N, a, g, lds + wave * ROOM, scales + row * 2 * SC + wn * G + v);
             }
         }
@@ -588,8 +581,6 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         __syncthreads();                                        // the ring is free
         constexpr int ROOM = RowStage<128>::STRIDE * 32;
         static_assert(NW * ROOM <= STAGES * STAGE, "room for the results on their way");
-        const int e = p.out_f32 ? 4 : 8;
-        const bool whole = p.N % e == 0 && p.ld_out % e == 0 && ((uintptr_t)p.out & 15) == 0;
 #pragma unroll
         for (int v = 0; v < TN; ++v) {
             const int nb = n0 + (wn * TN + v) * 32;
@@ -604,7 +595,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
             for (int u = 0; u < TM; ++u) {
                 const int m = m0 + (wm * TM + u) * 32;
                 if (m >= p.M) break;
-                put_rows(lds + wave * ROOM, p.out, p.ld_out, p.out_f32, m, min(p.M - m, 32), nb, p.N, whole, [&](int i) { return acc[u][v][i] + b[i]; });
+                put_rows(lds + wave * ROOM, p.out, p.ld_out, p.out_f32, m, min(p.M - m, 32), nb, p.N, [&](int i) { return acc[u][v][i] + b[i]; });
             }
         }
     }

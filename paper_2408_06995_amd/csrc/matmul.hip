@@ -76,16 +76,14 @@ __global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p)
     if (id >= p.M * per) return;
     const int64_t m = row_at(p.rows, id);
     const int n = (int)(id - m * per) * 4;
-    const bool vec = (p.N & 3) == 0;
+    const bool all = n + 4 <= p.N;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < p.slices; ++s) {
         const float* const x = p.part + (s * p.M + m) * p.N + n;
-        if (vec) {
-            const float4 t = *reinterpret_cast<const float4*>(x);
-            v[0] += t.x;
-            v[1] += t.y;
-            v[2] += t.z;
-            v[3] += t.w;
+        if (all) {
+            const piece16 t = *reinterpret_cast<const piece16*>(x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += __uint_as_float(t[e]);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -97,7 +95,7 @@ __global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p)
         for (int e = 0; e < 4; ++e)
             if (n + e < p.N) v[e] += p.bias[n + e];
     }
-    put4(p.out, m * p.ld_out + n, p.out_f32, n, (int)p.N, vec && (p.ld_out & 3) == 0 && ((uintptr_t)p.out & 15) == 0, v);
+    put4(p.out, m * p.ld_out + n, p.out_f32, n, (int)p.N, v);
 }
 
 // Four outputs of a row per thread, eight threads a block of 32.
@@ -113,13 +111,16 @@ __global__ __launch_bounds__(256) void matmul_sum_gated_kernel(SumArgs p)
         a[e] = p.bias && n + e < N ? p.bias[n + e] : 0.0f;
         g[e] = p.bias && n + e < N ? p.bias[N + n + e] : 0.0f;
     }
-    const bool vec = (N & 3) == 0 && n < N;
+    const bool all = n + 4 <= N;
     for (int s = 0; s < p.slices; ++s) {
         const float* const x = p.part + (s * p.M + m) * 2 * N + n;
-        if (vec) {
-            const float4 t = *reinterpret_cast<const float4*>(x), u = *reinterpret_cast<const float4*>(x + N);
-            a[0] += t.x, a[1] += t.y, a[2] += t.z, a[3] += t.w;
-            g[0] += u.x, g[1] += u.y, g[2] += u.z, g[3] += u.w;
+        if (all) {
+            const piece16 t = *reinterpret_cast<const piece16*>(x), u = *reinterpret_cast<const piece16*>(x + N);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] += __uint_as_float(t[e]);
+                g[e] += __uint_as_float(u[e]);
+            }
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -160,11 +161,10 @@ __global__ __launch_bounds__(256) void matmul_sum_gated_kernel(SumArgs p)
     if (!in || n >= N) return;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = a[e] * gate_of<false>(q.act, g[e], nullptr);
-    put4(q.h, m * q.ld_h + n, p.out_f32, n, N, (q.ld_h & 3) == 0 && ((uintptr_t)q.h & 15) == 0 && n + 4 <= N, v);
+    put4(q.h, m * q.ld_h + n, p.out_f32, n, N, v);
     if (q.pre && !q.pre_scales) {
-        const bool vp = (N & 3) == 0 && ((uintptr_t)q.pre & 15) == 0;
-        put4(q.pre, m * q.ld_pre + n, p.out_f32, n, N, vp, a);
-        put4(q.pre, m * q.ld_pre + N + n, p.out_f32, n, N, vp, g);
+        put4(q.pre, m * q.ld_pre + n, p.out_f32, n, N, a);
+        put4(q.pre, m * q.ld_pre + N + n, p.out_f32, n, N, g);
     }
 }
 

@@ -13,15 +13,15 @@ namespace {
 template <typename T>
 constexpr int kPiece = 16 / (int)sizeof(T);
 
-// Elements k .. of a row as they lie in memory, zeros from K on; and as numbers.  VEC: rows are whole aligned pieces.
+// Elements k .. of a row as they lie in memory, zeros from K on; and as numbers.  VEC: rows are whole pieces.
 template <typename T, bool VEC>
 __device__ __forceinline__ uint4 raw_piece(const T* row, int64_t k, int64_t K)
 {
     constexpr int E = kPiece<T>;
     uint4 x = make_uint4(0, 0, 0, 0);
-    if constexpr (VEC) {
-        if (k < K) x = *reinterpret_cast<const uint4*>(row + k);
-    } else {
+    if (VEC ? k < K : k + E <= K) {
+        x = __builtin_bit_cast(uint4, *reinterpret_cast<const piece16*>(row + k));
+    } else if constexpr (!VEC) {
         T v[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = k + e < K ? row[k + e] : (T)0.0f;
@@ -54,19 +54,18 @@ template <typename T, bool VEC>
 __device__ __forceinline__ void put(T* row, int64_t k, int64_t K, const float (&v)[kPiece<T>], int past)
 {
     constexpr int E = kPiece<T>;
-    if constexpr (VEC) {
-        if (k >= K) return;
-        v4i o;
-        if constexpr (E == 4) o = v4i{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
-        else o = v4i{(int)pair_bf16(v[0], v[1]), (int)pair_bf16(v[2], v[3]), (int)pair_bf16(v[4], v[5]), (int)pair_bf16(v[6], v[7])};
+    if (VEC ? k < K : k + E <= K) {
+        piece16 o;
+        if constexpr (E == 4) o = piece16{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        else o = piece16{pair_bf16(v[0], v[1]), pair_bf16(v[2], v[3]), pair_bf16(v[4], v[5]), pair_bf16(v[6], v[7])};
         if (past) {
             asm volatile("");                                         // (keeps the two stores from being made one, the ordinary)
-            __builtin_nontemporal_store(o, reinterpret_cast<v4i*>(row + k));
+            __builtin_nontemporal_store(o, reinterpret_cast<piece16*>(row + k));
             asm volatile("");
         } else {
-            *reinterpret_cast<v4i*>(row + k) = o;
+            *reinterpret_cast<piece16*>(row + k) = o;
         }
-    } else {
+    } else if constexpr (!VEC) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
             if (k + e < K) row[k + e] = (T)v[e];
@@ -80,11 +79,12 @@ __device__ __forceinline__ void weights(const float* w, int64_t k, int64_t K, fl
     if (!w) {
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = 1.0f;
-    } else if (((uintptr_t)w & 15) == 0 && k + E <= K) {
+    } else if (k + E <= K) {
 #pragma unroll
         for (int e = 0; e < E; e += 4) {
-            const float4 x = *reinterpret_cast<const float4*>(w + k + e);
-            v[e] = x.x, v[e + 1] = x.y, v[e + 2] = x.z, v[e + 3] = x.w;
+            const piece16 x = *reinterpret_cast<const piece16*>(w + k + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[e + i] = __uint_as_float(x[i]);
         }
     } else {
 #pragma unroll
@@ -463,14 +463,14 @@ size_t norm_part_bytes(int64_t M, int64_t K)
 
 int launch_norm(const NormArgs& p, int type, hipStream_t s)
 {
-    if (type == FPQ_TYPE_FP32) return p.vec ? forward<float, true>(p, s) : forward<float, false>(p, s);
-    return p.vec ? forward<__bf16, true>(p, s) : forward<__bf16, false>(p, s);
+    if (type == FPQ_TYPE_FP32) return p.K % 4 == 0 ? forward<float, true>(p, s) : forward<float, false>(p, s);
+    return p.K % 8 == 0 ? forward<__bf16, true>(p, s) : forward<__bf16, false>(p, s);
 }
 
 int launch_norm_backward(const NormBackward& p, int type, hipStream_t s)
 {
-    if (type == FPQ_TYPE_FP32) return p.vec ? backward<float, true>(p, s) : backward<float, false>(p, s);
-    return p.vec ? backward<__bf16, true>(p, s) : backward<__bf16, false>(p, s);
+    if (type == FPQ_TYPE_FP32) return p.K % 4 == 0 ? backward<float, true>(p, s) : backward<float, false>(p, s);
+    return p.K % 8 == 0 ? backward<__bf16, true>(p, s) : backward<__bf16, false>(p, s);
 }
 
 }  // namespace fpq

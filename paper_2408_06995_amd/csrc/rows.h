@@ -24,7 +24,6 @@ struct RowsArgs {
     void* out;                          // not gated
     int64_t ld_out;
     int f32;                            // type of x and the results
-    int vec_x;                          // 16-byte pieces of x may be loaded
     Gate gate;
 };
 
@@ -52,15 +51,15 @@ __device__ __forceinline__ void mma16(v4f& c, const Frag<NA>& a, const Frag<NB>&
 // Eight values of a row of x from k on as an operand; zeros for rows and columns that are not there.
 template <typename T>
 struct RowPiece {
-    uint4 v[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* row, int k, int K, bool in, int vec)
+    piece16 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* row, int k, int K, bool in)
     {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = piece16{0, 0, 0, 0};
         if (!in || k >= K) return;
-        if (vec) {
+        if (k + 8 <= K) {
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = reinterpret_cast<const uint4*>(row + k)[i];
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = reinterpret_cast<const piece16*>(row + k)[i];
         } else {
             T e[8];
 #pragma unroll
@@ -93,7 +92,7 @@ struct Turn {
     {
         const W* const w = static_cast<const W*>(a.w) + row * a.ld_w;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) p[s].load(w, k0 + k(s, q), a.K, true, 1);
+        for (int s = 0; s < STEPS; ++s) p[s].load(w, k0 + k(s, q), a.K, true);
     }
     __device__ __forceinline__ void settle() {}
     __device__ __forceinline__ Frag<kPlanes<W>> frag(int s) const { return p[s].frag(); }
@@ -185,7 +184,7 @@ __global__ __launch_bounds__(64 * WV) void rows_kernel(RowsArgs a)
 #pragma unroll
         for (int s = 0; s < U::STEPS; ++s)
 #pragma unroll
-            for (int u = 0; u < MT; ++u) p[u][s].load(x[u], k0 + U::k(s, q), a.K, 16 * u + r < a.M, a.vec_x);
+            for (int u = 0; u < MT; ++u) p[u][s].load(x[u], k0 + U::k(s, q), a.K, 16 * u + r < a.M);
     };
     auto load_w = [&](int k0) {
 #pragma unroll

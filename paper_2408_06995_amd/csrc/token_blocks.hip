@@ -48,9 +48,9 @@ __global__ __launch_bounds__(256) void token_blocks_kernel(RowsArgs a)
         const T* const x = static_cast<const T*>(a.x) + m * a.ld_x;
         for (int i = threadIdx.x; i < pieces; i += 256) {
             const int k = i * E, b = i / P, c = b >> 6, l = b & 63;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (a.vec_x) {
-                if (k < a.K) v = *reinterpret_cast<const uint4*>(x + k);
+            uint4 v;
+            if (k + E <= a.K) {
+                v = __builtin_bit_cast(uint4, *reinterpret_cast<const piece16*>(x + k));
             } else {
                 T e[E];
 #pragma unroll
