@@ -91,8 +91,9 @@ size_t gradient_parts(int64_t M, int64_t N, int64_t K, int type)
 }
 
 // The products of both gradients.  d: [M, N] as the products read it, or to be packed with the others; x or its blocks; grad_x, grad_w may be null.
+// grad_bias: the sums of d beside grad_w, or null.
 int gradients(const Operand& d, int type, int64_t M, int64_t N, int64_t K, const void* x, const uint8_t* x_scales, int64_t ld_x, const void* w, int64_t ld_w,
-              void* grad_x, int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, Room& room, PackList& packs, hipStream_t s)
+              void* grad_x, int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, float* grad_bias, Room& room, PackList& packs, hipStream_t s)
 {
     const int np = planes_of(type);
     Operand ow{}, ox{};
@@ -124,6 +125,7 @@ int gradients(const Operand& d, int type, int64_t M, int64_t N, int64_t K, const
         p.col_a = true;
         p.out = grad_w;
         p.ld_out = stride(ld_grad_w, K, N);
+        p.sums = grad_bias;
         st = launch_product(p, room.at, s);
     }
     return st;
@@ -278,12 +280,15 @@ int fpq_linear_backward(const fpq_linear_args_t* p, const void* x, const uint8_t
     if (workspace_bad(workspace, workspace_bytes, fpq_linear_backward_workspace_size(M, N, K, p->type), &st)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     Room room{static_cast<char*>(workspace)};
-    if (grad_bias) st = launch_column_sums(grad_y, p->type, M, N, stride(p->ld_grad_y, N, M), grad_bias, reinterpret_cast<float*>(room.at), s);
+    // The bias's gradient comes with the weights' where their product gives both, else from a pass of its own.
+    const int np = planes_of(p->type);
+    const bool both = grad_bias && grad_w && product_sums(N, K, M, np, x_scales ? 1 : np);
+    if (grad_bias && !both) st = launch_column_sums(grad_y, p->type, M, N, stride(p->ld_grad_y, N, M), grad_bias, reinterpret_cast<float*>(room.at), s);
     if (st != FPQ_OK || (!grad_x && !grad_w)) return st;
     PackList packs{};
     Operand d{};
     if (M) d = operand(grad_y, p->type, M, N, p->ld_grad_y, room, packs);
-    return gradients(d, p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, room, packs, s);
+    return gradients(d, p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, both ? grad_bias : nullptr, room, packs, s);
 }
 
 static int check_gated(const fpq_gated_args_t* p)
@@ -381,7 +386,7 @@ int fpq_gated_backward(const fpq_gated_args_t* p, const void* x, const uint8_t* 
     st = launch_gate_backward(g, s);
     if (st != FPQ_OK || !g.d) return st;
     PackList packs{};
-    return gradients(Operand{d, g.ld_d, g.plane}, p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, room, packs, s);
+    return gradients(Operand{d, g.ld_d, g.plane}, p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, nullptr, room, packs, s);
 }
 
 int fpq_rms_norm(const fpq_norm_args_t* p, const void* x, const void* residual, const float* w, void* sum, void* y, float* rstd, uint8_t* codes, fpq_format_t f,

@@ -35,8 +35,8 @@ struct RowOf {
 static inline RowOf row_of(int64_t rows, int64_t per) { return RowOf{per, divisor(per < ((int64_t)1 << 31) ? per : 1), rows * per < (int64_t)1 << 31}; }
 __device__ __forceinline__ int64_t row_at(const RowOf& r, int64_t id) { return r.fits ? (int64_t)divide((int)id, r.by) : id / r.per; }
 
-// What the results of a tile become.
-enum MatmulEnd : int { kStore = 0, kGated = 1 };
+// What the results of a tile become.  kSums: stored, and the sums of A over k beside them (a bias's gradient beside the weights').
+enum MatmulEnd : int { kStore = 0, kGated = 1, kSums = 2 };
 
 struct Gate {
     int act;                    // fpq_gate
@@ -59,6 +59,7 @@ struct MatmulArgs {
     int64_t ld_out;
     int out_f32;
     const float* bias;          // [N] or [2 N] or null (slices == 1)
+    float* sums;                // kSums: [slice][M]
     Gate gate;
 };
 
@@ -434,6 +435,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
     for (int u = 0; u < TM; ++u)
 #pragma unroll
         for (int v = 0; v < TN; ++v) acc[u][v] = zero16();
+    float sums[TM] = {};                                        // kSums: of this lane's k
 
     struct Operands {
         v8bf a[PL][TM], b[PL][TN];
@@ -451,7 +453,17 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.b[PL == 3 ? pb[c] : 0][v], o.a[PL == 3 ? pa[c] : 0][u], acc[u][v], 0, 0, 0);
     };
 
-    if (beg < end) {
+    // The sums of A: its values times one, two at a time, by vector instructions that run beside the products.
+    // Only the first wavefronts along n make them, in a loop of their own.
+    auto add = [&](const Operands& o, int i) {
+        const v8bf a = o.a[i / TM][i % TM];
+        const v2bf one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sums[i % TM] = __builtin_amdgcn_fdot2_f32_bf16(v2bf{a[2 * k], a[2 * k + 1]}, one, sums[i % TM], false);
+    };
+
+    auto run = [&](auto with) {
+        constexpr bool SUMS = decltype(with)::value;
         start();
         Operands even, odd;
 #pragma unroll
@@ -469,6 +481,8 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
             for (int i = 0; i < (MM > RD ? MM : RD); ++i) {
                 if (i < MM) multiply(now, i);
                 if (i < RD) read(next, tile, t, i);
+                if constexpr (SUMS)
+                    if (i < PL * TM) add(now, i);
                 if constexpr (decltype(loads)::value) {
                     constexpr int EACH = (LOADS + MM - 1) / MM;
 #pragma unroll
@@ -508,10 +522,26 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         }
 #pragma unroll
         for (int i = 0; i < MM; ++i) multiply(odd, i);
+        if constexpr (SUMS) {
+#pragma unroll
+            for (int i = 0; i < PL * TM; ++i) add(odd, i);
+        }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    if (beg < end) {
+        if (END == kSums && at.n == 0 && wn == 0) run(std::integral_constant<bool, END == kSums>());
+        else run(std::false_type());
     }
 
     const int h = lane >> 5;
+    if constexpr (END == kSums) {
+#pragma unroll
+        for (int u = 0; u < TM; ++u) {
+            const float all = sums[u] + __shfl_xor(sums[u], 32, 64);
+            const int m = m0 + (wm * TM + u) * 32 + lane;
+            if (at.n == 0 && wn == 0 && h == 0 && m < p.M) p.sums[(int64_t)at.slice * p.M + m] = all;
+        }
+    }
     if (p.slices > 1) {
         __syncthreads();                                        // the ring is free
         constexpr int ROOM = RowStage<128>::STRIDE * 32;
@@ -611,11 +641,14 @@ struct Product {
     int64_t ld_out;
     int out_f32;
     const float* bias;
+    float* sums;                // of A over k (col_a; where product_sums allows it), or null
     bool gated;
     Gate gate;
 };
 // Bytes of partial results of a product of these sizes (0 where it is made in one slice).
 size_t product_part_bytes(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated);
+// Whether a product of these sizes with A and B by columns can give the sums of A.
+bool product_sums(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b);
 int launch_product(const Product& p, void* part, hipStream_t s);
 
 }  // namespace fpq

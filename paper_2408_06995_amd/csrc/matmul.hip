@@ -65,15 +65,24 @@ struct SumArgs {
     int64_t ld_out;
     int out_f32;
     const float* bias;
+    const float* sums;          // [slice][M], to be added up into sums_out, or null
+    float* sums_out;
     Gate gate;
     RowOf rows;                 // of the threads
 };
 
-// Four columns of a row per thread.
+// Four columns of a row per thread; behind them a thread for each row's sum of A.
 __global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p)
 {
     const int64_t per = p.rows.per, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= p.M * per) return;
+    if (id >= p.M * per) {
+        const int64_t r = id - p.M * per;
+        if (!p.sums || r >= p.M) return;
+        float t = 0.0f;
+        for (int s = 0; s < p.slices; ++s) t += p.sums[s * p.M + r];
+        p.sums_out[r] = t;
+        return;
+    }
     const int64_t m = row_at(p.rows, id);
     const int n = (int)(id - m * per) * 4;
     const bool all = n + 4 <= p.N;
@@ -174,7 +183,16 @@ size_t product_part_bytes(int64_t M, int64_t N, int64_t K, int planes_a, int pla
 {
     if (M == 0 || N == 0) return 0;
     const Plan p = plan_product(M, N, K, planes_a, planes_b, col_a, gated);
-    return p.slices > 1 ? (size_t)p.slices * M * N * (gated ? 2 : 1) * 4 : 0;
+    return p.slices > 1 ? (size_t)p.slices * M * (N * (gated ? 2 : 1) + (col_a ? 1 : 0)) * 4 : 0;
+}
+
+// Several passes over k read a plane of A more than once, unless there is but one plane of B or a tile takes all in one pass.  And the wavefronts that
+// make the sums are slower: in tiles of 256 x 256, of which large products are one round, that is more than a pass for the sums (8192 x 4096 -> 4096
+// with both gradients: 500 us, 481 with a pass); elsewhere it is less (5003 x 5120 -> 1280: 176 for 178, 32768 x 320 -> 960 99 for 107, 300 x 320 -> 960 18 for 25).
+bool product_sums(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b)
+{
+    const int tile = plan_product(M, N, K, planes_a, planes_b, true, false).tile;
+    return tile != kTile256 && (planes_b == 1 || tile == kPlanes256 || tile == kPlanes128);
 }
 
 int launch_product(const Product& q, void* part, hipStream_t s)
@@ -199,19 +217,21 @@ int launch_product(const Product& q, void* part, hipStream_t s)
     p.ld_out = q.ld_out;
     p.out_f32 = q.out_f32;
     p.bias = q.bias;
+    float* const sums = static_cast<float*>(part) + (size_t)plan.slices * q.M * q.N;       // (behind the partial results)
+    p.sums = plan.slices > 1 ? sums : q.sums;
     p.gate = q.gate;
     int st = q.gated ? launch_matmul_gated(p, plan.tile, s)
-             : q.col_a ? launch_matmul_cols(p, plan.tile, s)
+             : q.col_a ? (q.sums ? launch_matmul_cols_sums(p, plan.tile, s) : launch_matmul_cols(p, plan.tile, s))
              : q.col_b ? launch_matmul_rows_cols(p, plan.tile, s)
                        : launch_matmul_rows(p, plan.tile, s);
     if (st != FPQ_OK || plan.slices == 1) return st;
-    const SumArgs r{static_cast<const float*>(part), q.M, q.N, plan.slices, q.out, q.ld_out, q.out_f32, q.bias, q.gate,
+    const SumArgs r{static_cast<const float*>(part), q.M, q.N, plan.slices, q.out, q.ld_out, q.out_f32, q.bias, q.sums ? sums : nullptr, q.sums, q.gate,
                     row_of(q.M, q.gated ? (q.N + 31) / 32 * 8 : (q.N + 3) / 4)};
     if (q.gated) {
         const int64_t threads = q.M * ((q.N + 31) / 32 * 8);
         matmul_sum_gated_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(r);
     } else {
-        const int64_t threads = q.M * ((q.N + 3) / 4);
+        const int64_t threads = q.M * ((q.N + 3) / 4) + (q.sums ? q.M : 0);
         matmul_sum_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(r);
     }
     return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;

@@ -27,7 +27,8 @@ int launch_matmul_tile(MatmulArgs p, hipStream_t s)
 template <bool COLA, bool COLB, int END>
 int launch_matmul_form(const MatmulArgs& p, int tile, hipStream_t s)
 {
-    if (tile == kTile256) return launch_matmul_tile<COLA, COLB, 256, 256, 2, 4, 64, 2, 1, END>(p, s);
+    if constexpr (END != kSums)
+        if (tile == kTile256) return launch_matmul_tile<COLA, COLB, 256, 256, 2, 4, 64, 2, 1, END>(p, s);
     if constexpr (!COLA) {
         if (tile == kTile192) return launch_matmul_tile<COLA, COLB, 192, 256, 2, 4, 64, 2, 1, END>(p, s);
         if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, 32, 4, 1, END>(p, s);
@@ -43,5 +44,6 @@ int launch_matmul_rows(const MatmulArgs& p, int tile, hipStream_t s);
 int launch_matmul_gated(const MatmulArgs& p, int tile, hipStream_t s);
 int launch_matmul_rows_cols(const MatmulArgs& p, int tile, hipStream_t s);
 int launch_matmul_cols(const MatmulArgs& p, int tile, hipStream_t s);
+int launch_matmul_cols_sums(const MatmulArgs& p, int tile, hipStream_t s);
 
 }  // namespace fpq
