@@ -363,11 +363,11 @@ int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t
     return launched();
 }
 
-// About 1024 workgroups, of no fewer than 16 rows, and no more parts than their sum is quick with.
+// About 1024 workgroups, of no fewer than eight rows, and no more parts than their sum is quick with.
 RowParts row_parts(int64_t M, int64_t cols)
 {
     const int64_t strips = (cols + kStripColumns - 1) / kStripColumns;
-    int64_t parts = 1024 / strips < 512 ? 1024 / strips : 512, most = (M + 15) / 16;
+    int64_t parts = 1024 / strips < 512 ? 1024 / strips : 512, most = (M + 7) / 8;
     parts = parts < 1 ? 1 : parts > most ? most : parts;
     if (parts < 1) parts = 1;
     const int64_t rows = (M + parts - 1) / parts;

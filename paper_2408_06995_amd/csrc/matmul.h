@@ -454,7 +454,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
     };
 
     // The sums of A: its values times one, two at a time, by vector instructions that run beside the products.
-    // Only the first wavefronts along n make them, in a loop of their own.
+    // Only the first tiles along n make them, in loops of their own, each wavefront of one of the operands that it shares with another.
     auto add = [&](const Operands& o, int i) {
         const v8bf a = o.a[i / TM][i % TM];
         const v2bf one = {(__bf16)1.0f, (__bf16)1.0f};
@@ -463,7 +463,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
     };
 
     auto run = [&](auto with) {
-        constexpr bool SUMS = decltype(with)::value;
+        constexpr int SUMS = decltype(with)::value;             // of the operands u that this wavefront sums up: -1 none
         start();
         Operands even, odd;
 #pragma unroll
@@ -481,8 +481,8 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
             for (int i = 0; i < (MM > RD ? MM : RD); ++i) {
                 if (i < MM) multiply(now, i);
                 if (i < RD) read(next, tile, t, i);
-                if constexpr (SUMS)
-                    if (i < PL * TM) add(now, i);
+                if constexpr (SUMS >= 0)
+                    if (i < PL * TM && i % TM == SUMS) add(now, i);
                 if constexpr (decltype(loads)::value) {
                     constexpr int EACH = (LOADS + MM - 1) / MM;
 #pragma unroll
@@ -522,15 +522,18 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         }
 #pragma unroll
         for (int i = 0; i < MM; ++i) multiply(odd, i);
-        if constexpr (SUMS) {
+        if constexpr (SUMS >= 0) {
 #pragma unroll
-            for (int i = 0; i < PL * TM; ++i) add(odd, i);
+            for (int i = 0; i < PL * TM; ++i)
+                if (i % TM == SUMS) add(odd, i);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
+    if constexpr (END == kSums) static_assert(TM <= WN && WN == 2, "wavefront n sums operand n");
     if (beg < end) {
-        if (END == kSums && at.n == 0 && wn == 0) run(std::integral_constant<bool, END == kSums>());
-        else run(std::false_type());
+        if (END != kSums || at.n || wn >= TM) run(std::integral_constant<int, -1>());
+        else if (wn == 0) run(std::integral_constant<int, END == kSums ? 0 : -1>());
+        else run(std::integral_constant<int, END == kSums ? TM - 1 : -1>());
     }
 
     const int h = lane >> 5;
@@ -539,7 +542,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
         for (int u = 0; u < TM; ++u) {
             const float all = sums[u] + __shfl_xor(sums[u], 32, 64);
             const int m = m0 + (wm * TM + u) * 32 + lane;
-            if (at.n == 0 && wn == 0 && h == 0 && m < p.M) p.sums[(int64_t)at.slice * p.M + m] = all;
+            if (at.n == 0 && wn == u && h == 0 && m < p.M) p.sums[(int64_t)at.slice * p.M + m] = all;
         }
     }
     if (p.slices > 1) {
