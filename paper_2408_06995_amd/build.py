@@ -17,7 +17,7 @@ SOURCES = ["api.hip", "quant.hip", "search.hip", "sparsity.hip", "rounding.hip",
            "api_adapt.hip", "attention_fwd.hip", "attention_fwd_f32.hip", "attention_bwd.hip", "attention_bwd_f32.hip", "attention_pack.hip", "adapter.hip",
            "adapter_map_f32.hip", "adapter_map_f32_bf16.hip", "adapter_map_f32_packed.hip", "adapter_map_bf16.hip",
            "adapter_map_f32_bf16_packed.hip", "adapter_map_bf16_packed.hip", "adapter_outer.hip", "adamw.hip",
-           "api_blocks.hip", "blocks.hip", "norm.hip", "matmul.hip", "matmul_rows.hip", "matmul_gated.hip", "matmul_rows_cols.hip", "matmul_cols.hip", "matmul_cols_sums.hip", "rows_blocks.hip", "token_blocks.hip", "rows_gated.hip"]
+           "api_blocks.hip", "blocks.hip", "norm.hip", "matmul.hip", "matmul_rows.hip", "matmul_gated.hip", "matmul_rows_cols.hip", "matmul_cols.hip", "matmul_cols_sums.hip", "matmul_both.hip", "matmul_both_sums.hip", "rows_blocks.hip", "token_blocks.hip", "rows_gated.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

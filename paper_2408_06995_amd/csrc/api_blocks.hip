@@ -82,12 +82,13 @@ bool workspace_bad(const void* workspace, size_t bytes, size_t need, int* st)
 
 size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 
-// Partial results of grad_x [M, K] = d [M, N] w and of grad_w [N, K] = d^T x, which follow each other and share the room.
+// Partial results of grad_x [M, K] = d [M, N] w and of grad_w [N, K] = d^T x, which follow each other and share the room, or come together.
 size_t gradient_parts(int64_t M, int64_t N, int64_t K, int type)
 {
     const int p = planes_of(type);
-    return align_up(larger(product_part_bytes(M, K, N, p, p, false, false),
-                           larger(product_part_bytes(N, K, M, p, p, true, false), product_part_bytes(N, K, M, p, 1, true, false))));
+    const size_t one = larger(product_part_bytes(M, K, N, p, p, false, false),
+                              larger(product_part_bytes(N, K, M, p, p, true, false), product_part_bytes(N, K, M, p, 1, true, false)));
+    return align_up(larger(one, larger(products_part_bytes(M, N, K, p, false), products_part_bytes(M, N, K, p, true))));
 }
 
 // The products of both gradients.  d: [M, N] as the products read it, or to be packed with the others; x or its blocks; grad_x, grad_w may be null.
@@ -101,34 +102,29 @@ int gradients(const Operand& d, int type, int64_t M, int64_t N, int64_t K, const
     if (grad_w && M) ox = x_scales ? operand_of_blocks(x, x_scales, M, K, 8, room, packs) : operand(x, type, M, K, ld_x, room, packs);
     int st = packs.count ? launch_packs(packs, s) : FPQ_OK;
     if (st != FPQ_OK) return st;
-    Product p{};
-    p.a = d;
-    p.planes_a = np;
-    p.out_f32 = type == FPQ_TYPE_FP32;
-    p.col_b = true;
-    if (grad_x && M) {
-        p.b = ow;
-        p.M = M;
-        p.N = K;
-        p.K = N;
-        p.planes_b = np;
-        p.out = grad_x;
-        p.ld_out = stride(ld_grad_x, K, M);
-        st = launch_product(p, room.at, s);
-    }
-    if (st == FPQ_OK && grad_w) {
-        p.b = ox;
-        p.M = N;
-        p.N = K;
-        p.K = M;
-        p.planes_b = x_scales ? 1 : np;
-        p.col_a = true;
-        p.out = grad_w;
-        p.ld_out = stride(ld_grad_w, K, N);
-        p.sums = grad_bias;
-        st = launch_product(p, room.at, s);
-    }
-    return st;
+    Product px{}, pw{};
+    px.a = pw.a = d;
+    px.planes_a = pw.planes_a = np;
+    px.out_f32 = pw.out_f32 = type == FPQ_TYPE_FP32;
+    px.col_b = pw.col_b = pw.col_a = true;
+    px.b = ow;
+    px.M = M;
+    px.N = K;
+    px.K = N;
+    px.planes_b = np;
+    px.out = grad_x;
+    px.ld_out = stride(ld_grad_x, K, M);
+    pw.b = ox;
+    pw.M = N;
+    pw.N = K;
+    pw.K = M;
+    pw.planes_b = x_scales ? 1 : np;
+    pw.out = grad_w;
+    pw.ld_out = stride(ld_grad_w, K, N);
+    pw.sums = grad_bias;
+    if (grad_x && grad_w && M) return launch_products(px, pw, room.at, s);
+    if (grad_x && M) return launch_product(px, room.at, s);
+    return grad_w ? launch_product(pw, room.at, s) : FPQ_OK;
 }
 
 // What both backward calls ask of x, w and the gradients
@@ -282,7 +278,7 @@ int fpq_linear_backward(const fpq_linear_args_t* p, const void* x, const uint8_t
     Room room{static_cast<char*>(workspace)};
     // The bias's gradient comes with the weights' where their product gives both, else from a pass of its own.
     const int np = planes_of(p->type);
-    const bool both = grad_bias && grad_w && product_sums(N, K, M, np, x_scales ? 1 : np);
+    const bool both = grad_bias && grad_w && ((grad_x && products_join(M, N, K, np, x_scales)) || product_sums(N, K, M, np, x_scales ? 1 : np));
     if (grad_bias && !both) st = launch_column_sums(grad_y, p->type, M, N, stride(p->ld_grad_y, N, M), grad_bias, reinterpret_cast<float*>(room.at), s);
     if (st != FPQ_OK || (!grad_x && !grad_w)) return st;
     PackList packs{};

@@ -219,11 +219,10 @@ struct TilePlaces {
 struct MatmulPlace {
     int m, n, slice;
 };
-__device__ __forceinline__ MatmulPlace matmul_place(const MatmulArgs& p)
+__device__ __forceinline__ MatmulPlace matmul_place(const MatmulArgs& p, int id)
 {
     constexpr int kBand = 8;
-    const int total = gridDim.x, per = total >> 3;
-    int id = blockIdx.x;
+    const int total = p.tiles_m * p.tiles_n * p.slices, per = total >> 3;
     if (id < per << 3) id = (id & 7) * per + (id >> 3);
     const int tiles = p.tiles_m * p.tiles_n;
     MatmulPlace r;
@@ -360,9 +359,9 @@ __device__ __forceinline__ void stage_barrier()
 }
 
 // KS: k of a step; STAGES: of the ring; PL: planes of both operands in a stage, whose six products are made from one read of each, or 1: a
-// pass over k for each.  (Two wavefronts per SIMD: one workgroup of eight, or two of four.)
+// pass over k for each.
 template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int PL, int END>
-__global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2) void matmul_kernel(MatmulArgs p)
+__device__ __forceinline__ void matmul_tile(const MatmulArgs& p, int id)
 {
     constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, G = END == kGated ? TN / 2 : TN;
     using FA = TileFeed<COLA, BM, KS, NW>;
@@ -371,7 +370,7 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
     static_assert(PL == 1 || PL == 3, "planes");
     static_assert(END != kGated || (!COLB && TN % 2 == 0), "gated: a wavefront has the values and the gates of the same outputs");
     extern __shared__ __align__(1024) char lds[];
-    const MatmulPlace at = matmul_place(p);
+    const MatmulPlace at = matmul_place(p, id);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave / WN, wn = wave % WN;
     constexpr int CB = END == kGated ? BN / 2 : BN;             // columns of the result in a tile
     const int m0 = at.m * BM, n0 = at.n * CB;
@@ -638,6 +637,23 @@ __global__ __launch_bounds__(64 * WM * WN, BM / WM * BN / WN > 128 * 80 ? 1 : 2)
     }
 }
 
+// (Two wavefronts per SIMD: one workgroup of eight, or two of four.)
+template <bool COLA, bool COLB, int BM, int BN, int WM, int WN, int KS, int STAGES, int PL, int END>
+__global__ __launch_bounds__(64 * WM * WN, 2) void matmul_kernel(MatmulArgs p)
+{
+    matmul_tile<COLA, COLB, BM, BN, WM, WN, KS, STAGES, PL, END>(p, blockIdx.x);
+}
+
+// d w and d^T x: those of the two whose workgroups take longer are the first `first`.
+template <int BM, int BN, int WM, int WN, int KS, int STAGES, int PL, int END>
+__global__ __launch_bounds__(64 * WM * WN, 2) void matmul_both_kernel(MatmulArgs x, MatmulArgs w, int first, int x_first)
+{
+    const bool front = (int)blockIdx.x < first;
+    const int id = front ? blockIdx.x : blockIdx.x - first;
+    if (front == (x_first != 0)) matmul_tile<false, true, BM, BN, WM, WN, KS, STAGES, PL, kStore>(x, id);
+    else matmul_tile<true, true, BM, BN, WM, WN, KS, STAGES, PL, END>(w, id);
+}
+
 // A product as the callers give it: M, N, K, operands, `planes` of each, forms, and what becomes of it.
 struct Product {
     Operand a, b;
@@ -657,5 +673,10 @@ size_t product_part_bytes(int64_t M, int64_t N, int64_t K, int planes_a, int pla
 // Whether a product of these sizes with A and B by columns can give the sums of A.
 bool product_sums(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b);
 int launch_product(const Product& p, void* part, hipStream_t s);
+// Both gradients of y = x w^T for d [M, N], x [M, K]: x.M, N, K = M, K, N, by rows and by columns, w.M, N, K = N, K, M, both by columns.  In one launch where
+// products_join says so (`planes`: of d, w and, if not `blocks`, x), else one after the other.
+bool products_join(int64_t M, int64_t N, int64_t K, int planes, bool blocks);
+size_t products_part_bytes(int64_t M, int64_t N, int64_t K, int planes, bool blocks);
+int launch_products(const Product& x, const Product& w, void* part, hipStream_t s);
 
 }  // namespace fpq

@@ -1,5 +1,6 @@
 // Matrix products: the choice of tile and slices, and the sum of the slices.
 #include "matmul_tiles.h"
+#include <math.h>
 
 namespace fpq {
 
@@ -7,50 +8,117 @@ namespace {
 
 struct Plan {
     int tile, slices;
+    double us;                  // estimate
 };
 
 // Passes of the planes: the largest products of two operands, small ones first.
 int passes(int planes_a, int planes_b) { return planes_a * planes_b == 9 ? 6 : planes_a * planes_b; }
 
+// What a call takes, in microseconds: rounds of as many workgroups as run at once, each of steps / slices and what a workgroup needs
+// at its start and end.  A step of 64 k takes `full` where the chip is full (1.2 PFLOP/s) and no less than `alone`; a round that is not full, its
+// share.  Workgroups of 256 and 192 rows have their compute unit alone; two of 128 rows share one and hide one's waits behind the other, or one with
+// a ring of four stages has it alone.  Slices cost the partial results' way to memory and back and a launch.  (Measured: 2048 x 4096 with 64
+// steps 1.07 of 192 rows; 1280 x 1280 with 192 steps 1.09 of 256 rows, 0.66 of 128 and 0.43 deep;
+// 512 x 1280 with 20 steps 9.0 us in tiles of 64 for 14.4 of 128.)  Operands of three planes each are read
+// once for their six products: 4096 x 4096 x 2048 in fp32, both gradients, 666 us for 727.
+struct Kind {
+    int tile, at_once;
+    double full, alone, ends;
+};
+constexpr Kind kKinds[] = {{kTile256, 256, 1.8, 1.2, 4}, {kTile192, 256, 1.35, 1.05, 4}, {kTile128, 512, 1.08, 0.66, 2}, {kTile128Deep, 256, 0.56, 0.43, 3},
+                           {kPlanes256, 256, 0.84, 0.62, 3}, {kPlanes128, 256, 0.5, 0.38, 3}, {kTile64, 512, 0.5, 0.2, 5}};
+constexpr Kind kGated64{kTile64, 256, 0.5, 0.24, 5};
+constexpr double kLaunch = 4;
+
+int64_t tiles_of(int t, int64_t M, int64_t N, bool gated)
+{
+    const int64_t columns = tile_n(t, gated) / (gated ? 2 : 1);
+    return ((M + kTileM[t] - 1) / kTileM[t]) * ((N + columns - 1) / columns);
+}
+double steps_of(int64_t K, int planes_a, int planes_b) { return passes(planes_a, planes_b) * (double)((K + 63) / 64); }
+bool takes_planes(int t) { return t == kPlanes256 || t == kPlanes128; }
+// slices that are tried
+int next_slices(int s) { return s < 4 ? s + 1 : s + s / 4; }
+double sums_us(int s, int64_t M, int64_t N, bool gated) { return s > 1 ? (double)s * M * N * (gated ? 2 : 1) * 8 / 4.5e6 : 0.0; }
+
 Plan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated)
 {
-    auto columns = [&](int t) { return (int64_t)tile_n(t, gated) / (gated ? 2 : 1); };
-    auto tiles = [&](int t) { return ((M + kTileM[t] - 1) / kTileM[t]) * ((N + columns(t) - 1) / columns(t)); };
-    const double steps = passes(planes_a, planes_b) * (double)((K + 63) / 64);
+    const double steps = steps_of(K, planes_a, planes_b);
     if (!col_a && M <= 32) {
         // bound by B's bytes: parts of no fewer than eight steps until two workgroups per compute unit have work
-        const int64_t n = tiles(kTile32);
+        const int64_t n = tiles_of(kTile32, M, N, gated);
         int64_t most = (int64_t)(steps / 8 < 16 ? steps / 8 : 16), slices = 512 / n < most ? 512 / n : most;
-        return Plan{kTile32, slices > 1 ? (int)slices : 1};
+        if (slices < 1) slices = 1;
+        const double rounds = (double)(n * slices) / 512;
+        return Plan{kTile32, (int)slices, (rounds > 1 ? rounds : 1) * 0.3 * (steps / slices + 5) + (slices > 1 ? kLaunch : 0)};
     }
-    // What a call takes, in microseconds: rounds of as many workgroups as run at once, each of steps / slices and what a workgroup needs
-    // at its start and end.  A step of 64 k takes `full` where the chip is full (1.2 PFLOP/s) and no less than `alone`; a round that is not full, its
-    // share.  Workgroups of 256 and 192 rows have their compute unit alone; two of 128 rows share one and hide one's waits behind the other, or one with
-    // a ring of four stages has it alone.  Slices cost the partial results' way to memory and back and a launch.  (Measured: 2048 x 4096 with 64
-    // steps 1.07 of 192 rows; 1280 x 1280 with 192 steps 1.09 of 256 rows, 0.66 of 128 and 0.43 deep;
-    // 512 x 1280 with 20 steps 9.0 us in tiles of 64 for 14.4 of 128.)  Operands of three planes each are read
-    // once for their six products: 4096 x 4096 x 2048 in fp32, both gradients, 666 us for 727.
-    struct Kind {
-        int tile, at_once;
-        double full, alone, ends;
-    };
-    const Kind kinds[] = {{kTile256, 256, 1.8, 1.2, 4}, {kTile192, 256, 1.35, 1.05, 4}, {kTile128, 512, 1.08, 0.66, 2}, {kTile128Deep, 256, 0.56, 0.43, 3},
-                          {kPlanes256, 256, 0.84, 0.62, 3}, {kPlanes128, 256, 0.5, 0.38, 3},
-                          gated ? Kind{kTile64, 256, 0.5, 0.24, 5} : Kind{kTile64, 512, 0.5, 0.2, 5}};
-    Plan best{kTile128, 1};
-    double least = 1e30;
-    for (const Kind& k : kinds) {
+    Plan best{kTile128, 1, 1e30};
+    for (Kind k : kKinds) {
         if (k.tile == kTile192 && col_a) continue;
-        if ((k.tile == kPlanes256 || k.tile == kPlanes128) && planes_a * planes_b != 9) continue;
-        for (int s = 1; s <= 32; s = s < 4 ? s + 1 : s + s / 4) {
+        if (takes_planes(k.tile) && planes_a * planes_b != 9) continue;
+        if (k.tile == kTile64 && gated) k = kGated64;
+        for (int s = 1; s <= 32; s = next_slices(s)) {
             if (s > 1 && steps / s < 8) break;
-            const int64_t n = tiles(k.tile) * s, rest = n % k.at_once;
+            const int64_t n = tiles_of(k.tile, M, N, gated) * s, rest = n % k.at_once;
             const double part = k.full * rest / k.at_once;
             double us = ((double)(n / k.at_once) * k.full + (rest ? (part > k.alone ? part : k.alone) : 0.0)) * (steps / s + k.ends);
-            if (s > 1) us += 4 + (double)s * M * N * (gated ? 2 : 1) * 8 / 4.5e6;
-            if (us < least) {
-                least = us;
-                best = Plan{k.tile, s};
+            if (s > 1) us += kLaunch + sums_us(s, M, N, gated);
+            if (us < best.us) best = Plan{k.tile, s, us};
+        }
+    }
+    return best;
+}
+
+// Workgroups of two lengths (in steps), the long ones first, each where there is room next.  As many as run at once: the short ones share their
+// compute units until they end.  More: steps take `full` as long as all units are busy, then `alone`.
+double both_us(const Kind& k, int64_t na, double a, int64_t nb, double b)
+{
+    const int64_t nl = a >= b ? na : nb, ns = a >= b ? nb : na, slots = k.at_once;
+    const double l = a >= b ? a : b, s = a >= b ? b : a, share = k.full * (nl + ns) / slots, busy = (nl * l + ns * s) / slots;
+    if (nl + ns <= slots) {
+        const double us = s * (share > k.alone ? share : k.alone) + (l - s) * k.alone;
+        return us > busy * k.full ? us : busy * k.full;
+    }
+    const int64_t more = nl % slots;                // slots with one long workgroup more than the others
+    const double low = (double)(nl / slots) * l, high = low + (more ? l : 0);
+    double end = busy > high ? busy : high;
+    for (int i = 0; i < 6; ++i) {                   // the next time at which enough short ones have ended
+        const double ql = end > low ? floor((end - low) / s + 1e-9) : 0, qh = end > high ? floor((end - high) / s + 1e-9) : 0;
+        if ((slots - more) * ql + more * qh >= ns) break;
+        const double el = low + (ql + 1) * s, eh = high + (qh + 1) * s;
+        end = el < eh || !more ? el : eh;
+    }
+    return busy * k.full + (end - busy) * k.alone;
+}
+
+// Both gradients in one launch: their workgroups fill the chip together where neither does alone, and there is a launch less, or two.  (Linear layers in
+// bf16 with the blocks made, one after the other and together: 300 x 320 -> 960 18.2 and 14.8 us, 2048 x 1280 -> 1280 38.2 and 33.9, 8192 x 640 -> 640 41.6 and 33.8, 32768 x
+// 320 -> 960 98 and 82; gated ones with the forward call 999 x 333 -> 1283 in fp32 98.7 and 87.5, 532 x 2230 -> 8939 in bf16 293 and 273.)
+struct PlanBoth {
+    int tile, slices_x, slices_w;               // tile < 0: one after the other
+};
+PlanBoth plan_both(int64_t M, int64_t N, int64_t K, int planes, bool blocks)
+{
+    const int planes_x = blocks ? 1 : planes;
+    PlanBoth best{-1, 1, 1};
+    if (M == 0) return best;
+    const double steps_x = steps_of(N, planes, planes), steps_w = steps_of(M, planes, planes_x);
+    const Plan x = plan_product(M, K, N, planes, planes, false, false), w = plan_product(N, K, M, planes, planes_x, true, false);
+    double least = (x.us + w.us + kLaunch);
+    for (const Kind& k : kKinds) {
+        if (k.tile != kTile64 && k.tile != kTile128 && k.tile != kTile128Deep && k.tile != kPlanes128) continue;
+        if (takes_planes(k.tile) != (planes * planes_x == 9)) continue;
+        const int64_t tx = tiles_of(k.tile, M, K, false), tw = tiles_of(k.tile, N, K, false);
+        for (int a = 1; a <= 32; a = next_slices(a)) {
+            if (a > 1 && steps_x / a < 8) break;
+            for (int b = 1; b <= 32; b = next_slices(b)) {
+                if (b > 1 && steps_w / b < 8) break;
+                double us = both_us(k, tx * a, steps_x / a + k.ends, tw * b, steps_w / b + k.ends);
+                if (a > 1 || b > 1) us += kLaunch + sums_us(a, M, K, false) + sums_us(b, N, K, false);
+                if (us < least) {
+                    least = us;
+                    best = PlanBoth{k.tile, a, b};
+                }
             }
         }
     }
@@ -72,9 +140,9 @@ struct SumArgs {
 };
 
 // Four columns of a row per thread; behind them a thread for each row's sum of A.
-__global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p)
+__device__ __forceinline__ void sum_piece(const SumArgs& p, int64_t id)
 {
-    const int64_t per = p.rows.per, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t per = p.rows.per;
     if (id >= p.M * per) {
         const int64_t r = id - p.M * per;
         if (!p.sums || r >= p.M) return;
@@ -105,6 +173,13 @@ __global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p)
             if (n + e < p.N) v[e] += p.bias[n + e];
     }
     put4(p.out, m * p.ld_out + n, p.out_f32, n, (int)p.N, v);
+}
+__global__ __launch_bounds__(256) void matmul_sum_kernel(SumArgs p) { sum_piece(p, (int64_t)blockIdx.x * 256 + threadIdx.x); }
+// The first `first` workgroups' and the others'
+__global__ __launch_bounds__(256) void matmul_sum_both_kernel(SumArgs x, SumArgs w, unsigned first)
+{
+    if (blockIdx.x < first) sum_piece(x, (int64_t)blockIdx.x * 256 + threadIdx.x);
+    else sum_piece(w, (int64_t)(blockIdx.x - first) * 256 + threadIdx.x);
 }
 
 // Four outputs of a row per thread, eight threads a block of 32.
@@ -177,13 +252,56 @@ __global__ __launch_bounds__(256) void matmul_sum_gated_kernel(SumArgs p)
     }
 }
 
+size_t part_bytes(int slices, int64_t M, int64_t N, bool col_a, bool gated)
+{
+    return slices > 1 ? (size_t)slices * M * (N * (gated ? 2 : 1) + (col_a ? 1 : 0)) * 4 : 0;
+}
+
+MatmulArgs args_of(const Product& q, int tile, int slices, void* part)
+{
+    MatmulArgs p{};
+    p.a = q.a;
+    p.b = q.b;
+    p.M = (int)q.M;
+    p.N = (int)q.N;
+    p.K = (int)q.K;
+    if (q.planes_a == 3 && q.planes_b == 3) p.order_a = 0x001102, p.order_b = 0x010120;
+    else if (q.planes_a == 3) p.order_a = 0x012;
+    else if (q.planes_b == 3) p.order_b = 0x012;
+    p.passes = passes(q.planes_a, q.planes_b);
+    p.slices = slices;
+    const int cols = tile_n(tile, q.gated) / (q.gated ? 2 : 1);
+    p.tiles_m = (int)((q.M + kTileM[tile] - 1) / kTileM[tile]);
+    p.tiles_n = (int)((q.N + cols - 1) / cols);
+    p.out = slices > 1 ? part : q.out;
+    p.ld_out = q.ld_out;
+    p.out_f32 = q.out_f32;
+    p.bias = q.bias;
+    // (the partial sums lie behind the partial results)
+    p.sums = slices > 1 ? static_cast<float*>(part) + (size_t)slices * q.M * q.N : q.sums;
+    p.gate = q.gate;
+    return p;
+}
+SumArgs sum_args_of(const Product& q, int slices, const void* part)
+{
+    const float* const from = static_cast<const float*>(part);
+    return SumArgs{from, q.M, q.N, slices, q.out, q.ld_out, q.out_f32, q.bias, q.sums ? from + (size_t)slices * q.M * q.N : nullptr, q.sums, q.gate,
+                   row_of(q.M, q.gated ? (q.N + 31) / 32 * 8 : (q.N + 3) / 4)};
+}
+unsigned sum_grid(const Product& q)
+{
+    const int64_t threads = q.gated ? q.M * ((q.N + 31) / 32 * 8) : q.M * ((q.N + 3) / 4) + (q.sums ? q.M : 0);
+    return (unsigned)((threads + 255) / 256);
+}
+int launched() { return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH; }
+
 }  // namespace
 
 size_t product_part_bytes(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated)
 {
     if (M == 0 || N == 0) return 0;
     const Plan p = plan_product(M, N, K, planes_a, planes_b, col_a, gated);
-    return p.slices > 1 ? (size_t)p.slices * M * (N * (gated ? 2 : 1) + (col_a ? 1 : 0)) * 4 : 0;
+    return part_bytes(p.slices, M, N, col_a, gated);
 }
 
 // Several passes over k read a plane of A more than once, unless there is but one plane of B or a tile takes all in one pass.  And the wavefronts that
@@ -199,42 +317,40 @@ int launch_product(const Product& q, void* part, hipStream_t s)
 {
     if (q.M == 0 || q.N == 0) return FPQ_OK;
     const Plan plan = plan_product(q.M, q.N, q.K, q.planes_a, q.planes_b, q.col_a, q.gated);
-    MatmulArgs p{};
-    p.a = q.a;
-    p.b = q.b;
-    p.M = (int)q.M;
-    p.N = (int)q.N;
-    p.K = (int)q.K;
-    if (q.planes_a == 3 && q.planes_b == 3) p.order_a = 0x001102, p.order_b = 0x010120;
-    else if (q.planes_a == 3) p.order_a = 0x012;
-    else if (q.planes_b == 3) p.order_b = 0x012;
-    p.passes = passes(q.planes_a, q.planes_b);
-    p.slices = plan.slices;
-    const int cols = tile_n(plan.tile, q.gated) / (q.gated ? 2 : 1);
-    p.tiles_m = (int)((q.M + kTileM[plan.tile] - 1) / kTileM[plan.tile]);
-    p.tiles_n = (int)((q.N + cols - 1) / cols);
-    p.out = plan.slices > 1 ? part : q.out;
-    p.ld_out = q.ld_out;
-    p.out_f32 = q.out_f32;
-    p.bias = q.bias;
-    float* const sums = static_cast<float*>(part) + (size_t)plan.slices * q.M * q.N;       // (behind the partial results)
-    p.sums = plan.slices > 1 ? sums : q.sums;
-    p.gate = q.gate;
-    int st = q.gated ? launch_matmul_gated(p, plan.tile, s)
-             : q.col_a ? (q.sums ? launch_matmul_cols_sums(p, plan.tile, s) : launch_matmul_cols(p, plan.tile, s))
-             : q.col_b ? launch_matmul_rows_cols(p, plan.tile, s)
-                       : launch_matmul_rows(p, plan.tile, s);
+    const MatmulArgs p = args_of(q, plan.tile, plan.slices, part);
+    const int st = q.gated ? launch_matmul_gated(p, plan.tile, s)
+                   : q.col_a ? (q.sums ? launch_matmul_cols_sums(p, plan.tile, s) : launch_matmul_cols(p, plan.tile, s))
+                   : q.col_b ? launch_matmul_rows_cols(p, plan.tile, s)
+                             : launch_matmul_rows(p, plan.tile, s);
     if (st != FPQ_OK || plan.slices == 1) return st;
-    const SumArgs r{static_cast<const float*>(part), q.M, q.N, plan.slices, q.out, q.ld_out, q.out_f32, q.bias, q.sums ? sums : nullptr, q.sums, q.gate,
-                    row_of(q.M, q.gated ? (q.N + 31) / 32 * 8 : (q.N + 3) / 4)};
-    if (q.gated) {
-        const int64_t threads = q.M * ((q.N + 31) / 32 * 8);
-        matmul_sum_gated_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(r);
-    } else {
-        const int64_t threads = q.M * ((q.N + 3) / 4) + (q.sums ? q.M : 0);
-        matmul_sum_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(r);
+    const SumArgs r = sum_args_of(q, plan.slices, part);
+    if (q.gated) matmul_sum_gated_kernel<<<dim3(sum_grid(q)), dim3(256), 0, s>>>(r);
+    else matmul_sum_kernel<<<dim3(sum_grid(q)), dim3(256), 0, s>>>(r);
+    return launched();
+}
+
+bool products_join(int64_t M, int64_t N, int64_t K, int planes, bool blocks) { return plan_both(M, N, K, planes, blocks).tile >= 0; }
+
+size_t products_part_bytes(int64_t M, int64_t N, int64_t K, int planes, bool blocks)
+{
+    const PlanBoth p = plan_both(M, N, K, planes, blocks);
+    return p.tile < 0 ? 0 : part_bytes(p.slices_x, M, K, false, false) + part_bytes(p.slices_w, N, K, true, false);
+}
+
+int launch_products(const Product& x, const Product& w, void* part, hipStream_t s)
+{
+    const PlanBoth plan = plan_both(x.M, w.M, x.N, x.planes_a, w.planes_b != x.planes_a);
+    if (plan.tile < 0) {
+        const int st = launch_product(x, part, s);
+        return st == FPQ_OK ? launch_product(w, part, s) : st;
     }
-    return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNCH;
+    char* const part_w = static_cast<char*>(part) + part_bytes(plan.slices_x, x.M, x.N, false, false);
+    const MatmulArgs ax = args_of(x, plan.tile, plan.slices_x, part), aw = args_of(w, plan.tile, plan.slices_w, part_w);
+    const int st = w.sums ? launch_matmul_both_sums(ax, aw, plan.tile, s) : launch_matmul_both(ax, aw, plan.tile, s);
+    if (st != FPQ_OK || (plan.slices_x == 1 && plan.slices_w == 1)) return st;
+    const unsigned first = plan.slices_x > 1 ? sum_grid(x) : 0, rest = plan.slices_w > 1 ? sum_grid(w) : 0;
+    matmul_sum_both_kernel<<<dim3(first + rest), dim3(256), 0, s>>>(sum_args_of(x, plan.slices_x, part), sum_args_of(w, plan.slices_w, part_w), first);
+    return launched();
 }
 
 }  // namespace fpq
