@@ -594,8 +594,8 @@ int fpq_adamw_step(const void *plan, int64_t pieces, double lr, double beta1, do
  *   are exact, an fp32 x is split into three bf16 parts as in FPQ_TYPE_FP32 attention; sums are fp32.  Up to 64 rows (a token of each
  *   request) are bound by the codes read and need no workspace; more are computed with the codes expanded once to bf16 in it.
  * fpq_linear_backward: the gradients of a linear layer y = x W^T (+ bias) for grad_y [M, N]: grad_x [M, K] = grad_y W, grad_w [N, K] =
- *   grad_y^T x, of args->type, grad_bias fp32 [N] the sum of its rows.  Each of them may be NULL and is then not computed (grad_bias with and
- *   without grad_w may differ in the order of its sums); w is needed for grad_x, x for grad_w.  x is [M, K] of the type with stride ld_x, or, with x_scales not NULL, the E4M3 blocks that were kept of it.
+ *   grad_y^T x, of args->type, grad_bias fp32 [N] the sum of its rows.  Each of them may be NULL and is then not computed (which are asked
+ *   for may change the order of the others' sums); w is needed for grad_x, x for grad_w.  x is [M, K] of the type with stride ld_x, or, with x_scales not NULL, the E4M3 blocks that were kept of it.
  * Infinities and NaN make what depends on them infinite or NaN, in FPQ_TYPE_FP32 always NaN.  No atomics: the same bits in every run.  Rows of
  * multiples of 16 bytes that start at one are read where they are; others, and fp32, are packed into the workspace first.
  * workspace: the stated bytes, 16-byte aligned, no initialisation (NULL when that is 0); calls that share one are ordered on one stream.
