@@ -149,3 +149,30 @@ def test_scales_at_their_ends(M, t):
         want, off = blocks.block_linear(host(xs), wv, None, t == "bf16")
         flushed = np.abs(host(xs)) @ small.T
         within("y", y[:, part], want[:, part], (off + flushed * (1 + 2.0 ** -7))[:, part])
+
+
+@pytest.mark.parametrize("kept", [False, True], ids=["x", "blocks"])
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(3003, 2995, 3001), (2503, 2497, 2501), (4099, 641, 639), (1501, 1283, 1277), (2999, 1001, 1299), (8195, 127, 321)])
+def test_linear_gradients_in_every_tile(M, N, K, t, kept, guarded):
+    """All gradients together (in one launch or one after the other) and each alone: rows and columns at the ends and at random in full length."""
+    print(M, N, K, t, kept, flush=True)
+    x, scales, w, gy = test_gpu_blocks.linear_case(M, N, K, t, kept)
+    bf16 = t == "bf16"
+    g = np.random.RandomState(M)
+    ms, ns = (np.unique(np.concatenate([[0, 1, n - 2, n - 1], g.randint(0, n, 44)])) for n in (M, N))
+    xv = blocks.block_values(x.cpu().numpy(), scales.cpu().numpy(), 8, K) if kept else host(x)
+    gyv, r = host(gy), blocks.rounding(bf16)
+    want_x, want_w = blocks.product(gyv[ms], host(w).T, r), blocks.product(gyv[:, ns].T, xv.T, r)
+    want_b = blocks.linear_backward(np.zeros((M, 1)), np.zeros((N, 1)), gyv, bf16)[2]
+    for which in ((True, True, True), (True, False, False), (False, True, False), (False, True, True), (True, True, False)):
+        gx, gw, gb = (nan(*s, t=d) if on else None for on, s, d in zip(which, ((M, K), (N, K), (N,)), (TYPES[t], TYPES[t], torch.float32)))
+        B.fpq_linear_backward(x, scales, w, gy, gx, gw, gb, guarded(B.fpq_linear_backward_workspace_size(M, N, K, int(bf16))))
+        if gx is not None:
+            within("grad_x", gx[ms], *want_x)
+            assert gx.isfinite().all()
+        if gw is not None:
+            within("grad_w", gw[ns], *want_w)
+            assert gw.isfinite().all()
+        if gb is not None:
+            within("grad_bias", gb, *want_b)
