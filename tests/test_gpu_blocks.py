@@ -146,8 +146,8 @@ def test_linear_gradients_of_strided_rows(ld, t):
 
 @pytest.mark.parametrize("t", ["fp32", "bf16"])
 def test_linear_gradients_in_large_tiles(t):
-    check_linear(3600, 3700, 72, t, True)            # 256 x 256 tiles in grad_w, many k in grad_x
-    check_linear(4000, 136, 3700, t, False)          # 256 x 256 tiles in grad_x
+    check_linear(3600, 3700, 72, t, True)            # few columns of x, many of y
+    check_linear(4000, 136, 3700, t, False)          # one after the other
 
 
 def test_gradients_one_by_one_and_of_no_rows():

@@ -176,3 +176,19 @@ def test_linear_gradients_in_every_tile(M, N, K, t, kept, guarded):
             assert gw.isfinite().all()
         if gb is not None:
             within("grad_bias", gb, *want_b)
+
+
+@pytest.mark.parametrize("keep", ["type", "blocks"])
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(3001, 1501, 1001), (2047, 2563, 513), (2003, 1283, 333), (999, 1283, 333), (1000, 700, 2000), (3600, 1800, 72)])
+def test_gated_in_every_tile(M, N, K, t, keep, guarded):
+    """Rows at the ends and at random in full length, what is kept of them too."""
+    print(M, N, K, t, keep, flush=True)
+    c = Call(M, N, K, t, "silu" if N % 2 else "gelu")
+    h, pre, scales = c.forward(keep)
+    ms = np.unique(np.concatenate([[0, 1, M - 2, M - 1], np.random.RandomState(N).randint(0, M, 44)]))
+    want, off, ag, d_ag = blocks.gated(host(c.x)[ms], host(c.w), host(c.bias), c.act, t == "bf16")
+    within("h", h[ms], want, off)
+    c.M = len(ms)
+    c.check_kept(pre[ms], None if scales is None else scales[ms], ag, d_ag)
+    assert h.isfinite().all()

@@ -110,7 +110,7 @@ def test_strided_rows(ld, t):
 
 @pytest.mark.parametrize("t", ["fp32", "bf16"])
 def test_large_tiles(t):
-    Call(3600, 1800, 72, t, "gelu").check("blocks")      # 256 x 256 tiles forward
+    Call(3600, 1800, 72, t, "gelu").check("blocks")      # many tiles
     Call(40, 3000, 1000, t, "silu").check("type")        # parts along k
 
 
