@@ -108,11 +108,11 @@ PlanBoth plan_both(int64_t M, int64_t N, int64_t K, int planes, bool blocks)
     for (const Kind& k : kKinds) {
         if (k.tile != kTile64 && k.tile != kTile128 && k.tile != kTile128Deep && k.tile != kPlanes128) continue;
         if (takes_planes(k.tile) != (planes * planes_x == 9)) continue;
-        const int64_t tx = tiles_of(k.tile, M, K, false), tw = tiles_of(k.tile, N, K, false);
+        const int64_t tx = tiles_of(k.tile, M, K, false), tw = tiles_of(k.tile, N, K, false), most = 3 * k.at_once;      // (more parts gain nothing)
         for (int a = 1; a <= 32; a = next_slices(a)) {
-            if (a > 1 && steps_x / a < 8) break;
+            if (a > 1 && (steps_x / a < 8 || tx * a > most)) break;
             for (int b = 1; b <= 32; b = next_slices(b)) {
-                if (b > 1 && steps_w / b < 8) break;
+                if (b > 1 && (steps_w / b < 8 || tx * a + tw * b > most)) break;
                 double us = both_us(k, tx * a, steps_x / a + k.ends, tw * b, steps_w / b + k.ends);
                 if (a > 1 || b > 1) us += kLaunch + sums_us(a, M, K, false) + sums_us(b, N, K, false);
                 if (us < least) {
