@@ -265,7 +265,9 @@ __global__ __launch_bounds__(1024) void part_sums_kernel(const float* part, int 
 }
 
 // da = gh act(g), dg = gh a act'(g), in the planes that the products read, and their column sums.  A strip of 512 columns and a part of the rows per workgroup: the
-// sums stay in registers, and what the products read is written in whole lines.  KEPT: 0 the type, 1 blocks.
+// sums stay in registers, and what the products read is written in whole lines.  In bf16 da and dg
+// are rounded once for the products: the gradients are then off by 0.0024 of their norm, 0.0017 by their own rounding alone; two planes would double
+// products that take 450 of 716 us (8192 x 1280 -> 5120 and back).  KEPT: 0 the type, 1 blocks.
 template <typename T, int KEPT>
 __global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward p, int64_t rows)
 {
