@@ -166,9 +166,19 @@ def gated_backward(x, w, a, g, act, gh, bf16):
     off = np.concatenate([np.abs(gh) * df, np.abs(gh * a) * ds], 1) + 4 * U32 * np.abs(d)
     gb = d.sum(0)
     off_gb = off.sum(0) + (len(x) + 2) * U32 * (np.abs(d) + off).sum(0) + 2.0 ** -126
-    # (a part of an operand below the smallest normal number may be zero: what is left out of three parts is below 2^-125)
-    as_operand = off + (U16 if bf16 else 2 * U32) * (np.abs(d) + off) + 2.0 ** -125
+    # (of two bf16 parts or three; one below the smallest normal number may be zero: what is left out is below 2^-125)
+    as_operand = off + (U16 ** 2 if bf16 else 2 * U32) * (np.abs(d) + off) + 2.0 ** -125
     return product(d, w.T, r, as_operand), product(d.T, x.T, r, as_operand.T), (gb, off_gb)
+
+
+def gated_spread(x, w, a, g, act, gh):
+    """How far bf16 grad_x and grad_w are off ahead of their own rounding: a standard deviation per element, da and dg as operands of 16 bits,
+    whose roundings are independent and uniform, and bounds for the activation and for sums in 32 bits."""
+    f, slope, df, ds = gate(g, act)
+    d = np.concatenate([gh * f, gh * a * slope], 1)
+    own = np.concatenate([np.abs(gh) * df, np.abs(gh * a) * ds], 1) + (U16 ** 2 * 3.0 ** -0.5 + 4 * U32) * np.abs(d)
+    sums = lambda p, q: np.sqrt((p[0] * p[0]) @ (q * q)) + (len(q) + 16) * U32 * (np.abs(p[1]) @ np.abs(q))
+    return sums((own, d), w), sums((own.T, d.T), x)
 
 
 # ------------------------------------------------------------------------------------------------ norm

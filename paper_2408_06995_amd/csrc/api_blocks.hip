@@ -49,7 +49,7 @@ struct Room {
 };
 
 // Room for a matrix that the products cannot read as it is.
-size_t planes_bytes(int64_t rows, int64_t cols, int type) { return align_up((size_t)rows * round8(cols) * 2 * planes_of(type)); }
+size_t planes_bytes(int64_t rows, int64_t cols, int planes) { return align_up((size_t)rows * round8(cols) * 2 * planes); }
 size_t blocks_bytes(int64_t rows, int64_t cols) { return align_up((size_t)rows * block_padded(cols) * 2); }
 bool reads(const void* p, int type, int64_t rows, int64_t cols, int64_t ld)
 {
@@ -82,18 +82,18 @@ bool workspace_bad(const void* workspace, size_t bytes, size_t need, int* st)
 
 size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 
-// Partial results of grad_x [M, K] = d [M, N] w and of grad_w [N, K] = d^T x, which follow each other and share the room, or come together.
-size_t gradient_parts(int64_t M, int64_t N, int64_t K, int type)
+// Partial results of grad_x [M, K] = d [M, N] w and of grad_w [N, K] = d^T x, which follow each other and share the room, or come together; x in its type or
+// in blocks.
+size_t gradient_parts(int64_t M, int64_t N, int64_t K, int planes_d, int planes)
 {
-    const int p = planes_of(type);
-    const size_t one = larger(product_part_bytes(M, K, N, p, p, false, false),
-                              larger(product_part_bytes(N, K, M, p, p, true, false), product_part_bytes(N, K, M, p, 1, true, false)));
-    return align_up(larger(one, larger(products_part_bytes(M, N, K, p, false), products_part_bytes(M, N, K, p, true))));
+    const size_t one = larger(product_part_bytes(M, K, N, planes_d, planes, false, false),
+                              larger(product_part_bytes(N, K, M, planes_d, planes, true, false), product_part_bytes(N, K, M, planes_d, 1, true, false)));
+    return align_up(larger(one, larger(products_part_bytes(M, N, K, {planes_d, planes, planes}), products_part_bytes(M, N, K, {planes_d, planes, 1}))));
 }
 
-// The products of both gradients.  d: [M, N] as the products read it, or to be packed with the others; x or its blocks; grad_x, grad_w may be null.
+// The products of both gradients.  d: [M, N] in planes_d planes as the products read it, or to be packed with the others; x or its blocks; grad_x, grad_w may be null.
 // grad_bias: the sums of d beside grad_w, or null.
-int gradients(const Operand& d, int type, int64_t M, int64_t N, int64_t K, const void* x, const uint8_t* x_scales, int64_t ld_x, const void* w, int64_t ld_w,
+int gradients(const Operand& d, int planes_d, int type, int64_t M, int64_t N, int64_t K, const void* x, const uint8_t* x_scales, int64_t ld_x, const void* w, int64_t ld_w,
               void* grad_x, int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, float* grad_bias, Room& room, PackList& packs, hipStream_t s)
 {
     const int np = planes_of(type);
@@ -104,7 +104,7 @@ int gradients(const Operand& d, int type, int64_t M, int64_t N, int64_t K, const
     if (st != FPQ_OK) return st;
     Product px{}, pw{};
     px.a = pw.a = d;
-    px.planes_a = pw.planes_a = np;
+    px.planes_a = pw.planes_a = planes_d;
     px.out_f32 = pw.out_f32 = type == FPQ_TYPE_FP32;
     px.col_b = pw.col_b = pw.col_a = true;
     px.b = ow;
@@ -206,7 +206,7 @@ int fpq_block_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M,
 size_t fpq_block_linear_workspace_size(int64_t M, int64_t N, int64_t K, int type)
 {
     if (!type_ok(type) || check_sizes(M, N, K) != FPQ_OK || M <= kFewRows) return 0;
-    return planes_bytes(M, K, type) + blocks_bytes(N, K) + align_up(product_part_bytes(M, N, K, planes_of(type), 1, false, false));
+    return planes_bytes(M, K, planes_of(type)) + blocks_bytes(N, K) + align_up(product_part_bytes(M, N, K, planes_of(type), 1, false, false));
 }
 
 int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* codes, const uint8_t* scales, const float* bias, void* y, void* workspace,
@@ -256,8 +256,9 @@ int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* c
 size_t fpq_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K, int type)
 {
     if (!type_ok(type) || check_sizes(M, N, K) != FPQ_OK) return 0;
-    return planes_bytes(M, N, type) + planes_bytes(N, K, type) + larger(planes_bytes(M, K, type), blocks_bytes(M, K)) +
-           larger(gradient_parts(M, N, K, type), align_up(row_parts_bytes(M, N)));
+    const int p = planes_of(type);
+    return planes_bytes(M, N, p) + planes_bytes(N, K, p) + larger(planes_bytes(M, K, p), blocks_bytes(M, K)) +
+           larger(gradient_parts(M, N, K, p, p), align_up(row_parts_bytes(M, N)));
 }
 
 int fpq_linear_backward(const fpq_linear_args_t* p, const void* x, const uint8_t* x_scales, const void* w, const void* grad_y, void* grad_x, void* grad_w,
@@ -278,13 +279,13 @@ int fpq_linear_backward(const fpq_linear_args_t* p, const void* x, const uint8_t
     Room room{static_cast<char*>(workspace)};
     // The bias's gradient comes with the weights' where their product gives both, else from a pass of its own.
     const int np = planes_of(p->type);
-    const bool both = grad_bias && grad_w && ((grad_x && products_join(M, N, K, np, x_scales)) || product_sums(N, K, M, np, x_scales ? 1 : np));
+    const bool both = grad_bias && grad_w && ((grad_x && products_join(M, N, K, {np, np, x_scales ? 1 : np})) || product_sums(N, K, M, np, x_scales ? 1 : np));
     if (grad_bias && !both) st = launch_column_sums(grad_y, p->type, M, N, stride(p->ld_grad_y, N, M), grad_bias, reinterpret_cast<float*>(room.at), s);
     if (st != FPQ_OK || (!grad_x && !grad_w)) return st;
     PackList packs{};
     Operand d{};
     if (M) d = operand(grad_y, p->type, M, N, p->ld_grad_y, room, packs);
-    return gradients(d, p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, both ? grad_bias : nullptr, room, packs, s);
+    return gradients(d, np, p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, both ? grad_bias : nullptr, room, packs, s);
 }
 
 static int check_gated(const fpq_gated_args_t* p)
@@ -299,7 +300,7 @@ size_t fpq_gated_workspace_size(int64_t M, int64_t N, int64_t K, int type)
     const fpq_gated_args_t a{type, 0, M, N, K, 0, 0, 0, 0, 0, 0};
     if (check_gated(&a) != FPQ_OK || M == 0) return 0;
     const int p = planes_of(type);
-    return planes_bytes(M, K, type) + planes_bytes(2 * N, K, type) + align_up(product_part_bytes(M, N, K, p, p, false, true));
+    return planes_bytes(M, K, p) + planes_bytes(2 * N, K, p) + align_up(product_part_bytes(M, N, K, p, p, false, true));
 }
 
 int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const float* bias, void* h, void* pre, uint8_t* pre_scales, void* workspace,
@@ -344,8 +345,9 @@ size_t fpq_gated_backward_workspace_size(int64_t M, int64_t N, int64_t K, int ty
 {
     const fpq_gated_args_t a{type, 0, M, N, K, 0, 0, 0, 0, 0, 0};
     if (check_gated(&a) != FPQ_OK) return 0;
-    return planes_bytes(M, 2 * N, type) + planes_bytes(2 * N, K, type) + larger(planes_bytes(M, K, type), blocks_bytes(M, K)) +
-           larger(gradient_parts(M, 2 * N, K, type), align_up(2 * row_parts_bytes(M, N)));
+    const int p = planes_of(type), pd = gate_planes(type);
+    return planes_bytes(M, 2 * N, pd) + planes_bytes(2 * N, K, p) + larger(planes_bytes(M, K, p), blocks_bytes(M, K)) +
+           larger(gradient_parts(M, 2 * N, K, pd, p), align_up(2 * row_parts_bytes(M, N)));
 }
 
 int fpq_gated_backward(const fpq_gated_args_t* p, const void* x, const uint8_t* x_scales, const void* w, const void* pre, const uint8_t* pre_scales,
@@ -375,14 +377,14 @@ int fpq_gated_backward(const fpq_gated_args_t* p, const void* x, const uint8_t* 
     g.ld_gh = stride(p->ld_grad_h, N, M);
     g.ld_d = round8(2 * N);
     g.plane = M * g.ld_d;
-    __bf16* const d = room.take<__bf16>(planes_bytes(M, 2 * N, p->type));
+    __bf16* const d = room.take<__bf16>(planes_bytes(M, 2 * N, gate_planes(p->type)));
     if (grad_x || grad_w) g.d = d;
     g.grad_bias = grad_bias;
     g.part = reinterpret_cast<float*>(room.at);
     st = launch_gate_backward(g, s);
     if (st != FPQ_OK || !g.d) return st;
     PackList packs{};
-    return gradients(Operand{d, g.ld_d, g.plane}, p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, nullptr, room, packs, s);
+    return gradients(Operand{d, g.ld_d, g.plane}, gate_planes(p->type), p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, nullptr, room, packs, s);
 }
 
 int fpq_rms_norm(const fpq_norm_args_t* p, const void* x, const void* residual, const float* w, void* sum, void* y, float* rstd, uint8_t* codes, fpq_format_t f,

@@ -40,6 +40,9 @@ size_t row_parts_bytes(int64_t M, int64_t cols);
 int launch_column_sums(const void* x, int type, int64_t M, int64_t N, int64_t ld, float* out, float* part, hipStream_t s);
 int launch_part_sums(const float* part, int parts, int64_t cols, float* out, hipStream_t s);
 
+// Planes of (da, dg) as operands.  Beside bf16 operands two, 16 significant bits: one would round them by as much as the gradients are rounded
+// themselves, errors of 0.0024 of a gradient's norm for 0.0017 (8192 x 1280 -> 5120 with the forward call: 717 us, with two 1166).
+static inline int gate_planes(int type) { return type == FPQ_TYPE_FP32 ? 3 : 2; }
 // (da, dg) of the gated projections as the products take them, and the bias's gradient.
 struct GateBackward {
     int type, act;

@@ -265,15 +265,13 @@ __global__ __launch_bounds__(1024) void part_sums_kernel(const float* part, int 
 }
 
 // da = gh act(g), dg = gh a act'(g), in the planes that the products read, and their column sums.  A strip of 512 columns and a part of the rows per workgroup: the
-// sums stay in registers, and what the products read is written in whole lines.  In bf16 da and dg
-// are rounded once for the products: the gradients are then off by 0.0024 of their norm, 0.0017 by their own rounding alone; two planes would double
-// products that take 450 of 716 us (8192 x 1280 -> 5120 and back).  KEPT: 0 the type, 1 blocks.
+// sums stay in registers, and what the products read is written in whole lines.  KEPT: 0 the type, 1 blocks.
 template <typename T, int KEPT>
 __global__ __launch_bounds__(256) void gate_backward_kernel(GateBackward p, int64_t rows)
 {
     const int64_t first = (int64_t)blockIdx.x * kStripColumns, m1 = min(p.M, (int64_t)(blockIdx.y + 1) * rows), N = p.N;
     const int64_t k = first + 8 * (threadIdx.x & 63), np = (N + 31) / 32 * 32;
-    constexpr int NP = kPlanes<T>;
+    constexpr int NP = sizeof(T) == 4 ? 3 : 2;                         // gate_planes
     float sum_a[8] = {}, sum_g[8] = {};
     if (k < N)
         for (int64_t m = (int64_t)blockIdx.y * rows + (threadIdx.x >> 6); m < m1; m += 4) {

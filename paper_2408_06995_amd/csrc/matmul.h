@@ -2,8 +2,8 @@
 //
 //   out[m, n] = sum_k A(m, k) B(n, k)
 //
-// Operands are one or three planes of bf16 (fp32 values x = h + m + l, as in attention.h; of nine products the six largest are taken,
-// beside an operand of one plane all three).  Each operand lies either with the contraction along its rows (ROW: p[m ld + k]) or along
+// Operands are one to three planes of bf16 (fp32 values x = h + m + l, as in attention.h, or h + m; of nine products the six largest are taken,
+// beside an operand of one plane all).  Each operand lies either with the contraction along its rows (ROW: p[m ld + k]) or along
 // its columns (COL: p[k ld + m]), so that x W^T, g W and g^T x are one kernel without a transposed copy.
 //
 // A workgroup makes a tile of BM x BN results in steps of 32 or 64 along k; tiles go from memory to LDS directly into a ring of stages, of which
@@ -673,10 +673,14 @@ size_t product_part_bytes(int64_t M, int64_t N, int64_t K, int planes_a, int pla
 // Whether a product of these sizes with A and B by columns can give the sums of A.
 bool product_sums(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b);
 int launch_product(const Product& p, void* part, hipStream_t s);
-// Both gradients of y = x w^T for d [M, N], x [M, K]: x.M, N, K = M, K, N, by rows and by columns, w.M, N, K = N, K, M, both by columns.  In one launch where
-// products_join says so (`planes`: of d, w and, if not `blocks`, x), else one after the other.
-bool products_join(int64_t M, int64_t N, int64_t K, int planes, bool blocks);
-size_t products_part_bytes(int64_t M, int64_t N, int64_t K, int planes, bool blocks);
+// Planes of what both gradients of a layer are made from: d [M, N], w [N, K], x [M, K].
+struct Planes {
+    int d, w, x;
+};
+// Both gradients of y = x w^T for d: x.M, N, K = M, K, N, by rows and by columns, w.M, N, K = N, K, M, both by columns.  In one launch where
+// products_join says so, else one after the other.
+bool products_join(int64_t M, int64_t N, int64_t K, Planes planes);
+size_t products_part_bytes(int64_t M, int64_t N, int64_t K, Planes planes);
 int launch_products(const Product& x, const Product& w, void* part, hipStream_t s);
 
 }  // namespace fpq

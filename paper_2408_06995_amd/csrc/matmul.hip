@@ -97,17 +97,16 @@ double both_us(const Kind& k, int64_t na, double a, int64_t nb, double b)
 struct PlanBoth {
     int tile, slices_x, slices_w;               // tile < 0: one after the other
 };
-PlanBoth plan_both(int64_t M, int64_t N, int64_t K, int planes, bool blocks)
+PlanBoth plan_both(int64_t M, int64_t N, int64_t K, Planes p)
 {
-    const int planes_x = blocks ? 1 : planes;
     PlanBoth best{-1, 1, 1};
     if (M == 0) return best;
-    const double steps_x = steps_of(N, planes, planes), steps_w = steps_of(M, planes, planes_x);
-    const Plan x = plan_product(M, K, N, planes, planes, false, false), w = plan_product(N, K, M, planes, planes_x, true, false);
+    const double steps_x = steps_of(N, p.d, p.w), steps_w = steps_of(M, p.d, p.x);
+    const Plan x = plan_product(M, K, N, p.d, p.w, false, false), w = plan_product(N, K, M, p.d, p.x, true, false);
     double least = (x.us + w.us + kLaunch);
     for (const Kind& k : kKinds) {
         if (k.tile != kTile64 && k.tile != kTile128 && k.tile != kTile128Deep && k.tile != kPlanes128) continue;
-        if (takes_planes(k.tile) != (planes * planes_x == 9)) continue;
+        if (takes_planes(k.tile) != (p.d * p.x == 9)) continue;
         const int64_t tx = tiles_of(k.tile, M, K, false), tw = tiles_of(k.tile, N, K, false), most = 3 * k.at_once;      // (more parts gain nothing)
         for (int a = 1; a <= 32; a = next_slices(a)) {
             if (a > 1 && (steps_x / a < 8 || tx * a > most)) break;
@@ -265,9 +264,10 @@ MatmulArgs args_of(const Product& q, int tile, int slices, void* part)
     p.M = (int)q.M;
     p.N = (int)q.N;
     p.K = (int)q.K;
+    // (small products first)
     if (q.planes_a == 3 && q.planes_b == 3) p.order_a = 0x001102, p.order_b = 0x010120;
     else if (q.planes_a == 3) p.order_a = 0x012;
-    else if (q.planes_b == 3) p.order_b = 0x012;
+    else if (q.planes_a == 2) p.order_a = 0x01;
     p.passes = passes(q.planes_a, q.planes_b);
     p.slices = slices;
     const int cols = tile_n(tile, q.gated) / (q.gated ? 2 : 1);
@@ -329,17 +329,17 @@ int launch_product(const Product& q, void* part, hipStream_t s)
     return launched();
 }
 
-bool products_join(int64_t M, int64_t N, int64_t K, int planes, bool blocks) { return plan_both(M, N, K, planes, blocks).tile >= 0; }
+bool products_join(int64_t M, int64_t N, int64_t K, Planes planes) { return plan_both(M, N, K, planes).tile >= 0; }
 
-size_t products_part_bytes(int64_t M, int64_t N, int64_t K, int planes, bool blocks)
+size_t products_part_bytes(int64_t M, int64_t N, int64_t K, Planes planes)
 {
-    const PlanBoth p = plan_both(M, N, K, planes, blocks);
+    const PlanBoth p = plan_both(M, N, K, planes);
     return p.tile < 0 ? 0 : part_bytes(p.slices_x, M, K, false, false) + part_bytes(p.slices_w, N, K, true, false);
 }
 
 int launch_products(const Product& x, const Product& w, void* part, hipStream_t s)
 {
-    const PlanBoth plan = plan_both(x.M, w.M, x.N, x.planes_a, w.planes_b != x.planes_a);
+    const PlanBoth plan = plan_both(x.M, w.M, x.N, Planes{x.planes_a, x.planes_b, w.planes_b});
     if (plan.tile < 0) {
         const int st = launch_product(x, part, s);
         return st == FPQ_OK ? launch_product(w, part, s) : st;
