@@ -158,7 +158,10 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs p)
             for (int e = 0; e < E; e += 4) q[e / 4] = codes8(y[e] * i, y[e + 1] * i, y[e + 2] * i, y[e + 3] * i);
         } else {
             if (k >= span || !in) return;
-            auto bound = [&](int e) { return k + e < K ? fminf(fmaxf(__fmul_rn(y[e], c), -448.0f), 448.0f) : 0.0f; };
+            auto bound = [&](int e) {                                 // (NaN keeps its sign, as in fpq_quantize)
+                const float v = __fmul_rn(y[e], c);
+                return k + e < K ? copysignf(fminf(fabsf(v), 448.0f), v) : 0.0f;
+            };
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
                 if (p.hardware) {
