@@ -3,7 +3,8 @@
 // Bound by the codes' bytes: every code is read once, 1 KB of a row at a time (a lane has a block of 32 codes, 16 bytes, and its scale), and a
 // wavefront's loads for four rows of weights go out together.  x is in LDS, in the order in which the lanes read it: piece i of 16 bytes of
 // all lanes' blocks lie side by side.  bf16: codes become pairs of bf16 in the conversion instruction and are summed by the two-element dot
-// product; fp32: pairs of fp32 and fused multiply-adds.  A block's sum is multiplied by its scale once.  5120 -> 20480: one row 12.3 us in bf16 (4.5 TB/s
+// product; fp32: pairs of fp32 and fused multiply-adds.  The conversion takes the scale too: a block's sum without it could leave the range where
+// the products do not.  5120 -> 20480: one row 12.3 us in bf16 (4.5 TB/s
 // with the launch), on the matrix unit 22.9; two rows 18.3 and 23.3, three 20.5 and 24.1 (but 5120 -> 5120 9.5 and 8.6); in fp32 one row 16.5 and 31.2, four the same.
 #include "rows.h"
 
@@ -69,15 +70,13 @@ __global__ __launch_bounds__(256) void token_blocks_kernel(RowsArgs a)
         for (int m = 0; m < M; ++m) acc[r][m] = 0.0f;
     for (int c = 0; c < chunks; ++c) {
         uint4 now[R];
-        float f[R], part[R][M];
+        float f[R];
+        const bool in = c * 64 + lane < blocks;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             now[r] = code[r];
-            f[r] = scale_of(scale[r]);
-#pragma unroll
-            for (int m = 0; m < M; ++m) part[r][m] = 0.0f;
+            f[r] = in ? scale_of(scale[r]) : 1.0f;
         }
-        const bool in = c * 64 + lane < blocks;
         if (c + 1 < chunks) load(c + 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {                                 // eight codes of the block
@@ -92,19 +91,19 @@ __global__ __launch_bounds__(256) void token_blocks_kernel(RowsArgs a)
                 auto pair = [&](auto byte) {
                     constexpr int B = decltype(byte)::value;
                     if constexpr (sizeof(T) == 2) {
-                        const v2bf v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, 1.0f, B);
+                        const v2bf v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, f[r], B);
 #pragma unroll
                         for (int m = 0; m < M; ++m) {
                             const uint32_t u = B == 0 ? x[m][0].x : B == 1 ? x[m][0].y : B == 2 ? x[m][0].z : x[m][0].w;
-                            part[r][m] = __builtin_amdgcn_fdot2_f32_bf16(v, __builtin_bit_cast(v2bf, u), part[r][m], false);
+                            acc[r][m] = __builtin_amdgcn_fdot2_f32_bf16(v, __builtin_bit_cast(v2bf, u), acc[r][m], false);
                         }
                     } else {
-                        const v2f v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, B);
+                        const v2f v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, f[r], B);
 #pragma unroll
                         for (int m = 0; m < M; ++m) {
                             const uint4 u = x[m][B / 2];
-                            part[r][m] = fmaf(v.x, __uint_as_float(B % 2 ? u.z : u.x), part[r][m]);
-                            part[r][m] = fmaf(v.y, __uint_as_float(B % 2 ? u.w : u.y), part[r][m]);
+                            acc[r][m] = fmaf(v.x, __uint_as_float(B % 2 ? u.z : u.x), acc[r][m]);
+                            acc[r][m] = fmaf(v.y, __uint_as_float(B % 2 ? u.w : u.y), acc[r][m]);
                         }
                     }
                 };
@@ -114,11 +113,6 @@ __global__ __launch_bounds__(256) void token_blocks_kernel(RowsArgs a)
                 pair(std::integral_constant<int, 3>());
             }
         }
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int m = 0; m < M; ++m)
-                if (in) acc[r][m] = fmaf(part[r][m], f[r], acc[r][m]);
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1)

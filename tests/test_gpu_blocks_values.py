@@ -1,4 +1,4 @@
-"""Operators around the projections at values far out: NaN where codes are made."""
+"""Operators around the projections at values far out: NaN where codes are made, products near the ends of the range."""
 import numpy as np
 import pytest
 import torch
@@ -6,7 +6,7 @@ import torch
 from oracle import blocks
 from paper_2408_06995_amd import binding as B
 from gpu_util import DEV
-from test_gpu_blocks import E4M3, nan, rows
+from test_gpu_blocks import E2M1, E4M3, TYPES, host, nan, quantize, room, rows, within
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,22 @@ def test_codes_of_norms_that_are_nan(K, f):
         want = (want if want.size == 8 * K else blocks.unpack(want[None])).reshape(8, K)
         got = codes.cpu().numpy()
         assert np.array_equal(got[:, :K], want) and not got[:, K:].any()
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 16, 64, 70])
+@pytest.mark.parametrize("x_exp,w_exp", [(125, -30), (120, -7), (-100, -30), (-60, -60), (-20, 100)])
+def test_layers_whose_products_are_in_range(x_exp, w_exp, M, t):
+    """Large x with small weights and the other way round: what is in range as a product counts in full."""
+    print(x_exp, w_exp, M, t, flush=True)
+    N, K = 40, 2000
+    g = torch.Generator().manual_seed(M)
+    codes, scales = quantize(rows(g, N, K, torch.float32), E2M1)
+    scales.fill_(127 + w_exp)
+    x = torch.rand(M, K, generator=g) + 0.5
+    x[:, 1::2] *= -1
+    x = torch.ldexp(x.double(), torch.tensor(x_exp)).to(TYPES[t]).to(DEV)
+    wv = blocks.block_values(blocks.unpack(codes.cpu().numpy()), scales.cpu().numpy(), 4, K)
+    y = nan(M, N, t=TYPES[t])
+    B.fpq_block_linear(x, codes, scales, None, y, room(B.fpq_block_linear_workspace_size(M, N, K, int(t == "bf16"))))
+    within("y", y, *blocks.block_linear(host(x), wv, None, t == "bf16"))
