@@ -155,10 +155,9 @@ RowsArgs rows_args(const void* x, int type, int64_t M, int64_t N, int64_t K, int
 // Whether the form of few rows takes gated projections: weights read where they are.  In bf16 up to 16 rows, more only of weights that the L2 holds: in
 // 64 rows their share of the matrix unit and x again in every workgroup cost more than the tiles' rows without a result (48 rows of 4096 -> 10240:
 // 55.8 us, in tiles 36.4; of 1280 -> 5120: 14.2 and 16.2).  In fp32 tiles have to pack the weights first (64 rows of 4096 -> 10240: 143 us, in tiles 281).
-bool few_rows(const fpq_gated_args_t* p)
+bool few_rows(int64_t M, int64_t N, int64_t K, int type)
 {
-    const bool fits = p->type == FPQ_TYPE_FP32 || p->M <= 16 || 4 * p->N * p->K <= (int64_t)32 << 20;
-    return p->M <= kFewRows && fits;
+    return M <= kFewRows && (type == FPQ_TYPE_FP32 || M <= 16 || 4 * N * K <= (int64_t)32 << 20);
 }
 
 int check_norm(const fpq_norm_args_t* p)
@@ -298,7 +297,9 @@ static int check_gated(const fpq_gated_args_t* p)
 size_t fpq_gated_workspace_size(int64_t M, int64_t N, int64_t K, int type)
 {
     const fpq_gated_args_t a{type, 0, M, N, K, 0, 0, 0, 0, 0, 0};
-    if (check_gated(&a) != FPQ_OK || M == 0) return 0;
+    if (check_gated(&a) != FPQ_OK || M <= 16) return 0;
+    // (nothing is kept there by the form of few rows; from 17 rows on, which form runs changes how large a workspace has to be, not whether there is one)
+    if (few_rows(M, N, K, type)) return align_up(1);
     const int p = planes_of(type);
     return planes_bytes(M, K, p) + planes_bytes(2 * N, K, p) + align_up(product_part_bytes(M, N, K, p, p, false, true));
 }
@@ -316,7 +317,7 @@ int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const flo
     if (!aligned(x, size) || !aligned(w, size) || !aligned(h, size) || !aligned(pre, pre_scales ? 16 : size) || !aligned(bias, 4)) return FPQ_ERR_ALIGN;
     if (workspace_bad(workspace, workspace_bytes, fpq_gated_workspace_size(M, N, K, p->type), &st)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (few_rows(p)) {
+    if (few_rows(M, N, K, p->type)) {
         RowsArgs r = rows_args(x, p->type, M, N, K, p->ld_x, bias);
         r.w = w;
         r.ld_w = p->ld_w;
