@@ -748,6 +748,9 @@ int do_rms_norm(Args& A)
             scale = A.a[9] == Py_None ? 0.0f : A.f(9);
             dev = A.words<const float>(10, 1, "scale_dev");
         }
+    } else if (!A.bad && A.a[11] != Py_None) {
+        PyErr_SetString(PyExc_ValueError, "code_scales: no codes");
+        A.bad = true;
     }
     return invoke(A, fn, &r, A.p(0), A.p(1), w, A.p(4), A.p(5), rstd, codes, f, scale, dev, scales, A.stream());
 }
