@@ -11,4 +11,3 @@ def test_scales_without_codes_are_refused():
     scales = torch.zeros(0, 2, dtype=torch.uint8)
     with pytest.raises(ValueError, match="code_scales: no codes"):
         B.fpq_rms_norm(x, None, None, 1e-6, x, x, None, None, None, None, None, scales)
-    B.fpq_rms_norm(x, None, None, 1e-6, x, x, None, torch.zeros(0, 64, dtype=torch.uint8), None, None, None, scales)
