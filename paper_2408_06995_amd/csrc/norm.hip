@@ -5,6 +5,7 @@
 // 8192 x 5120 in bf16: forward with the residual 62 us (5.4 TB/s), backward 65 with the weights' gradient (5.2); 32768 x 320 with codes 15.2 (4.9).
 #include "blocks.h"
 
+#include <iterator>
 #include <utility>
 
 namespace fpq {
@@ -375,6 +376,7 @@ struct Shape {
 constexpr Shape kShapes[] = {{8, 4}, {8, 5}, {16, 4}, {16, 5}, {32, 4}, {32, 5}, {64, 4}, {64, 5}, {128, 4}, {128, 5}, {256, 4}, {256, 5}};
 constexpr Shape kFewShapes[] = {{64, 1}, {256, 1}, {256, 2}, {256, 4}, {256, 5}};
 constexpr Shape kPlainShapes[] = {{64, 1}, {64, 4}, {256, 4}};           // rows that are no whole pieces
+constexpr Shape kTwoPasses{256, 0};                                       // rows longer than those
 // (the backward kernel holds three tensors' pieces, those of the next row and two rows of sums and weights: no more than three pieces if they suffice)
 constexpr Shape kBackwardShapes[] = {{16, 3}, {32, 2}, {32, 3}, {64, 2}, {64, 3}, {128, 2}, {128, 3}, {256, 2}, {256, 3}, {256, 4}, {256, 5}};
 Shape shape_of(int64_t M, int64_t span, int piece, bool vec, bool back)
@@ -383,7 +385,7 @@ Shape shape_of(int64_t M, int64_t span, int piece, bool vec, bool back)
     auto first = [&](const auto& list) {
         for (const Shape& s : list)
             if ((int64_t)s.tpr * s.ch >= pieces) return s;
-        return Shape{256, 0};
+        return kTwoPasses;
     };
     return !vec ? first(kPlainShapes) : M * pieces < 65536 ? first(kFewShapes) : back ? first(kBackwardShapes) : first(kShapes);
 }
@@ -395,18 +397,26 @@ int64_t backward_blocks(int64_t M, Shape s)
     return all < most ? all : most;
 }
 
-template <bool BACK, bool VEC, int I = 0, typename F>
+// Runs `run` with the shape's numbers as constants: those of shape_of's own lists, so that each has its kernel.
+template <const auto& LIST, int I = 0, typename F>
+bool among(Shape s, F&& run)
+{
+    if constexpr (I < (int)std::size(LIST)) {
+        constexpr Shape c = LIST[I];
+        if (s.tpr != c.tpr || s.ch != c.ch) return among<LIST, I + 1>(s, run);
+        run(std::pair<std::integral_constant<int, c.tpr>, std::integral_constant<int, c.ch>>());
+        return true;
+    }
+    return false;
+}
+template <bool BACK, bool VEC, typename F>
 void with_shape(Shape s, F&& run)
 {
-    constexpr Shape fwd[] = {{8, 4}, {8, 5}, {16, 4}, {16, 5}, {32, 4}, {32, 5}, {64, 4}, {64, 5}, {128, 4}, {128, 5}, {256, 4}, {256, 5}, {64, 1}, {256, 1}, {256, 2}, {256, 0}};
-    constexpr Shape bwd[] = {{16, 3}, {32, 2}, {32, 3}, {64, 2}, {64, 3}, {128, 2}, {128, 3}, {256, 2}, {256, 3}, {256, 4}, {256, 5}, {64, 1}, {256, 1}, {256, 0}};
-    constexpr Shape plain[] = {{64, 1}, {64, 4}, {256, 4}, {256, 0}};
-    constexpr int N = !VEC ? 4 : BACK ? 14 : 16;
-    if constexpr (I < N) {
-        constexpr Shape c = !VEC ? plain[I < 4 ? I : 0] : BACK ? bwd[I < 14 ? I : 0] : fwd[I];
-        if (s.tpr == c.tpr && s.ch == c.ch) run(std::pair<std::integral_constant<int, c.tpr>, std::integral_constant<int, c.ch>>());
-        else with_shape<BACK, VEC, I + 1>(s, run);
-    }
+    bool found;
+    if constexpr (!VEC) found = among<kPlainShapes>(s, run);
+    else if constexpr (BACK) found = among<kFewShapes>(s, run) || among<kBackwardShapes>(s, run);
+    else found = among<kFewShapes>(s, run) || among<kShapes>(s, run);
+    if (!found) run(std::pair<std::integral_constant<int, kTwoPasses.tpr>, std::integral_constant<int, kTwoPasses.ch>>());
 }
 
 template <typename T, bool VEC>
