@@ -320,6 +320,10 @@ int launched() { return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNC
 
 }  // namespace
 
+// One launch, of fewer than 2^24 workgroups (2^32 threads) whatever the operands: they are [M, N], [N, K] and [M, K] with M <= 2^28, N, K <= 2^20 and fewer than 2^34
+// elements each.  Rows filled up to multiples of 8, or 32 as blocks, make at most 2^34 72 / 65 and 2^34 96 / 65 elements of 4096 a workgroup, together 10.8 M
+// workgroups; [N, K] adds at most 2.1 M while it has no more than 2^33, and with more all columns are 2^13 and up, the filling below 1 / 250, and the three
+// 12.7 M.
 int launch_packs(PackList& p, hipStream_t s)
 {
     int64_t at = 0;
@@ -327,17 +331,7 @@ int launch_packs(PackList& p, hipStream_t s)
         PackItem& q = p.m[i];
         q.first = at;
         q.pieces = row_of(q.rows, q.ld_dst / 8);
-        const int64_t blocks = grid_of(q.rows * (q.ld_dst / 8));
-        if (at && at + blocks >= (int64_t)1 << 24) {                 // (a launch has fewer than 2^32 threads)
-            PackList one{{p.m[i]}, 1};
-            const int st = launch_packs(one, s);
-            if (st != FPQ_OK) return st;
-            for (int j = i + 1; j < p.count; ++j) p.m[j - 1] = p.m[j];
-            --p.count;
-            --i;
-            continue;
-        }
-        at += blocks;
+        at += grid_of(q.rows * (q.ld_dst / 8));
     }
     if (!at) return FPQ_OK;
     pack_kernel<<<dim3((unsigned)at), dim3(256), 0, s>>>(p);
