@@ -57,16 +57,21 @@ int launch_matmul_both_form(const MatmulArgs& x, const MatmulArgs& w, int tile, 
 template <bool COLA, bool COLB, int END>
 int launch_matmul_form(const MatmulArgs& p, int tile, hipStream_t s)
 {
+    // (both by rows and no gates: layers on 4-bit blocks, which have more than 64 rows here and weights of one plane)
+    constexpr bool FEW_OR_PLANES = COLB || END == kGated;
     if constexpr (END != kSums)
         if (tile == kTile256) return launch_matmul_tile<COLA, COLB, 256, 256, 2, 4, 64, 2, 1, END>(p, s);
     if constexpr (!COLA) {
         if (tile == kTile192) return launch_matmul_tile<COLA, COLB, 192, 256, 2, 4, 64, 2, 1, END>(p, s);
-        if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, 32, 4, 1, END>(p, s);
+        if constexpr (FEW_OR_PLANES)
+            if (tile == kTile32) return launch_matmul_tile<COLA, COLB, 32, 256, 1, 4, 32, 4, 1, END>(p, s);
     }
     if (tile == kTile64) return launch_matmul_tile<COLA, COLB, 64, END == kGated ? 128 : 64, 2, 2, 64, 4, 1, END>(p, s);
     if (tile == kTile128Deep) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 4, 1, END>(p, s);
-    if (tile == kPlanes256) return launch_matmul_tile<COLA, COLB, 256, 128, 4, 2, 32, 2, 3, END>(p, s);
-    if (tile == kPlanes128) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 32, 3, 3, END>(p, s);
+    if constexpr (FEW_OR_PLANES) {
+        if (tile == kPlanes256) return launch_matmul_tile<COLA, COLB, 256, 128, 4, 2, 32, 2, 3, END>(p, s);
+        if (tile == kPlanes128) return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 32, 3, 3, END>(p, s);
+    }
     return launch_matmul_tile<COLA, COLB, 128, 128, 2, 2, 64, 2, 1, END>(p, s);
 }
 
