@@ -457,7 +457,8 @@ __device__ __forceinline__ void matmul_tile(const MatmulArgs& p, int id)
     };
 
     // The sums of A: its values times one, two at a time, by vector instructions that run beside the products.
-    // Only the first tiles along n make them, in loops of their own, each wavefront of one of the operands that it shares with another.
+    // Only the first tiles along n make them, in loops of their own, each wavefront of one of the operands that it shares with another.  What 16 steps
+    // gave, 256 or 384 pairs a lane, is set aside, so that no sum's roundings grow with the length (4 M equal rows in fp32: off by 1e-7 for 0.0017).
     auto add = [&](const Operands& o, int i) {
         const v8bf a = o.a[i / TM][i % TM];
         const v2bf one = {(__bf16)1.0f, (__bf16)1.0f};
@@ -467,6 +468,7 @@ __device__ __forceinline__ void matmul_tile(const MatmulArgs& p, int id)
 
     auto run = [&](auto with) {
         constexpr int SUMS = decltype(with)::value;             // of the operands u that this wavefront sums up: -1 none
+        float aside = 0.0f;
         start();
         Operands even, odd;
 #pragma unroll
@@ -522,6 +524,11 @@ __device__ __forceinline__ void matmul_tile(const MatmulArgs& p, int id)
                 half(even, odd, 3, std::false_type());
             }
             advance();
+            if constexpr (SUMS >= 0)
+                if (((it - beg) & 15) == 15) {
+                    aside += sums[SUMS];
+                    sums[SUMS] = 0.0f;
+                }
         }
 #pragma unroll
         for (int i = 0; i < MM; ++i) multiply(odd, i);
@@ -529,6 +536,7 @@ __device__ __forceinline__ void matmul_tile(const MatmulArgs& p, int id)
 #pragma unroll
             for (int i = 0; i < PL * TM; ++i)
                 if (i % TM == SUMS) add(odd, i);
+            sums[SUMS] += aside;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
