@@ -631,7 +631,8 @@ int fpq_linear_backward(const fpq_linear_args_t *args, const void *x, const uint
  *   da = grad_h act(g),  dg = grad_h a act'(g);  grad_x = (da, dg) W,  grad_w [2 N, K] = (da, dg)^T x (of the type), grad_bias fp32 [2 N] the sum of
  *   their rows.  Each may be NULL.  x as in fpq_linear_backward: of the type, or its blocks with x_scales.
  * In FPQ_TYPE_BF16 da and dg keep 16 bits where they are multiplied (grad_bias sums them unrounded); products, sums, infinities, order,
- * workspaces and limits (of 2 N too) are those of fpq_linear_backward; fpq_gated needs no workspace for up to 16 rows.  sigmoid is off by at most (4 + |g|) 2^-23 of it, Phi by 4e-7. */
+ * workspaces and limits (of 2 N too) are those of fpq_linear_backward; fpq_gated needs no workspace for up to 16 rows.  sigmoid is off by at most (4 + |g|) 2^-23 of it
+ * (below 2^-126 it may be zero), Phi by 4e-7. */
 typedef enum fpq_gate { FPQ_GATE_SILU = 0, FPQ_GATE_GELU = 1 } fpq_gate;
 typedef struct fpq_gated_args {
     int32_t type; /* fpq_type */

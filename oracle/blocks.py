@@ -136,8 +136,14 @@ def gate(g, act):
         e = np.exp(-big)
         z = np.where(g >= 0, 1 / (1 + e), e / (1 + e))
         dz = (4 + big) * 2.0 ** -23 * z
-        # (a sigmoid below the smallest normal number, 2^-126, may be zero)
-        return g * z, z * (1 + g * (1 - z)), big * (dz + U32 * z + 2.0 ** -126), (dz + U32) * (1 + big) * 2 + 4 * U32 * (1 + big)
+        # The slope z s, s = 1 + g q, q = 1 - z.  z = 1 / (1 + e^-g) is off by the exponential's (1 + |g|) 2^-23 as far as it counts in the sum, by the sum's
+        # 2^-24 and the reciprocal's 2^-23; q by that and a rounding, s by |g| times as much and a rounding.  (A sigmoid below the smallest normal
+        # number, 2^-126, may be zero.)
+        q = np.where(g >= 0, e / (1 + e), 1 / (1 + e))
+        s = 1 + g * q
+        d_z = z * (q * (1 + big) + 2) * 2.0 ** -23 + 2.0 ** -126
+        d_s = big * (d_z + U32 * q) + U32 * np.abs(s)
+        return g * z, z * s, big * (dz + U32 * z + 2.0 ** -126), z * d_s + d_z * (np.abs(s) + d_s) + 2 * U32 * np.abs(z * s)
     z = 0.5 * (1 + _erf(g * 0.5 ** 0.5))
     z = np.where(g < -1, 0.5 * np.vectorize(math.erfc, otypes=[np.float64])(-g * 0.5 ** 0.5), z)
     phi = np.exp(-0.5 * g * g) * (2 * math.pi) ** -0.5

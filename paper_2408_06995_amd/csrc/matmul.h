@@ -91,7 +91,7 @@ __device__ __forceinline__ uint32_t codes8(float a, float b, float c, float d)
 }
 
 // act(g) and its derivative.  SiLU: g z and z (1 + g (1 - z)) with z = 1 / (1 + e^-g), off by at most (4 + |g|) 2^-23 of z (the exponent's
-// product is rounded, exponential and reciprocal are the hardware's).  GELU: g Phi(g) and Phi(g) + g phi(g), Phi by the formula of
+// product is rounded, exponential and reciprocal are the hardware's; below 2^-126, g of -87.3, it may be zero).  GELU: g Phi(g) and Phi(g) + g phi(g), Phi by the formula of
 // act_gelu, off by at most 4e-7.
 template <bool SLOPE>
 __device__ __forceinline__ float gate_of(int act, float g, float* slope)
