@@ -82,19 +82,36 @@ bool workspace_bad(const void* workspace, size_t bytes, size_t need, int* st)
 
 size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 
-// Partial results of grad_x [M, K] = d [M, N] w and of grad_w [N, K] = d^T x, which follow each other and share the room, or come together; x in its type or
-// in blocks.
-size_t gradient_parts(int64_t M, int64_t N, int64_t K, int planes_d, int planes)
+// The plans of grad_x [M, K] = d [M, N] w and grad_w [N, K] = d^T x: for x in its type and in blocks, of which a call takes one and its workspace's size the
+// larger.  Products that follow each other share the room of partial results.
+struct GradientPlans {
+    GradientPlan values, blocks;
+    size_t parts;
+};
+GradientPlans plans_of(int64_t M, int64_t N, int64_t K, int planes_d, int planes)
 {
-    const size_t one = larger(product_part_bytes(M, K, N, planes_d, planes, false, false),
-                              larger(product_part_bytes(N, K, M, planes_d, planes, true, false), product_part_bytes(N, K, M, planes_d, 1, true, false)));
-    return align_up(larger(one, larger(products_part_bytes(M, N, K, {planes_d, planes, planes}), products_part_bytes(M, N, K, {planes_d, planes, 1}))));
+    GradientPlans p;
+    p.values = plan_gradients(M, N, K, {planes_d, planes, planes});
+    p.blocks = planes == 1 ? p.values : plan_gradients(M, N, K, {planes_d, planes, 1});
+    p.parts = align_up(larger(gradient_part_bytes(p.values, M, N, K), gradient_part_bytes(p.blocks, M, N, K)));
+    return p;
+}
+size_t linear_backward_bytes(int64_t M, int64_t N, int64_t K, int type, const GradientPlans& plans)
+{
+    const int p = planes_of(type);
+    return planes_bytes(M, N, p) + planes_bytes(N, K, p) + larger(planes_bytes(M, K, p), blocks_bytes(M, K)) + larger(plans.parts, align_up(row_parts_bytes(M, N)));
+}
+size_t gated_backward_bytes(int64_t M, int64_t N, int64_t K, int type, const GradientPlans& plans)
+{
+    const int p = planes_of(type), pd = gate_planes(type);
+    return planes_bytes(M, 2 * N, pd) + planes_bytes(2 * N, K, p) + larger(planes_bytes(M, K, p), blocks_bytes(M, K)) +
+           larger(plans.parts, align_up(2 * row_parts_bytes(M, N)));
 }
 
 // The products of both gradients.  d: [M, N] in planes_d planes as the products read it, or to be packed with the others; x or its blocks; grad_x, grad_w may be null.
 // grad_bias: the sums of d beside grad_w, or null.
 int gradients(const Operand& d, int planes_d, int type, int64_t M, int64_t N, int64_t K, const void* x, const uint8_t* x_scales, int64_t ld_x, const void* w, int64_t ld_w,
-              void* grad_x, int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, float* grad_bias, Room& room, PackList& packs, hipStream_t s)
+              void* grad_x, int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, float* grad_bias, const GradientPlan& plan, Room& room, PackList& packs, hipStream_t s)
 {
     const int np = planes_of(type);
     Operand ow{}, ox{};
@@ -122,9 +139,9 @@ int gradients(const Operand& d, int planes_d, int type, int64_t M, int64_t N, in
     pw.out = grad_w;
     pw.ld_out = stride(ld_grad_w, K, N);
     pw.sums = grad_bias;
-    if (grad_x && grad_w && M) return launch_products(px, pw, room.at, s);
-    if (grad_x && M) return launch_product(px, room.at, s);
-    return grad_w ? launch_product(pw, room.at, s) : FPQ_OK;
+    if (grad_x && grad_w && M) return launch_products(px, pw, plan, room.at, s);
+    if (grad_x && M) return launch_product(px, plan.x, room.at, s);
+    return grad_w ? launch_product(pw, plan.w, room.at, s) : FPQ_OK;
 }
 
 // What both backward calls ask of x, w and the gradients
@@ -202,10 +219,15 @@ int fpq_block_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M,
     return launch_decode(codes, scales, M, K, bits == 8, out, out_type == FPQ_TYPE_FP32, stride(ld_out, K, M), static_cast<hipStream_t>(stream));
 }
 
+static size_t block_linear_bytes(int64_t M, int64_t N, int64_t K, int type, const ProductPlan& plan)
+{
+    return planes_bytes(M, K, planes_of(type)) + blocks_bytes(N, K) + align_up(product_part_bytes(plan, M, N, false, false));
+}
+
 size_t fpq_block_linear_workspace_size(int64_t M, int64_t N, int64_t K, int type)
 {
     if (!type_ok(type) || check_sizes(M, N, K) != FPQ_OK || M <= kFewRows) return 0;
-    return planes_bytes(M, K, planes_of(type)) + blocks_bytes(N, K) + align_up(product_part_bytes(M, N, K, planes_of(type), 1, false, false));
+    return block_linear_bytes(M, N, K, type, plan_product(M, N, K, planes_of(type), 1, false, false));
 }
 
 int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* codes, const uint8_t* scales, const float* bias, void* y, void* workspace,
@@ -220,7 +242,6 @@ int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* c
     if (!stride_ok(p->ld_x, p->K, p->M) || !stride_ok(p->ld_y, p->N, p->M)) return FPQ_ERR_SHAPE;
     const size_t size = size_of(p->type);
     if (!aligned(x, size) || !aligned(y, size) || !aligned(codes, 16) || !aligned(bias, 4)) return FPQ_ERR_ALIGN;
-    if (workspace_bad(workspace, workspace_bytes, fpq_block_linear_workspace_size(p->M, p->N, p->K, p->type), &st)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (p->M <= kFewRows) {
         RowsArgs r = rows_args(x, p->type, p->M, p->N, p->K, p->ld_x, bias);
@@ -233,6 +254,8 @@ int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* c
         r.ld_out = stride(p->ld_y, p->N, p->M);
         return p->M <= (r.f32 ? 4 : 2) && token_blocks_lds(p->M, p->K, r.f32) <= 65536 ? launch_token_blocks(r, s) : launch_rows_blocks(r, s);
     }
+    const ProductPlan plan = plan_product(p->M, p->N, p->K, planes_of(p->type), 1, false, false);
+    if (workspace_bad(workspace, workspace_bytes, block_linear_bytes(p->M, p->N, p->K, p->type, plan), &st)) return st;
     Room room{static_cast<char*>(workspace)};
     PackList packs{};
     Product q{};
@@ -249,15 +272,13 @@ int fpq_block_linear(const fpq_linear_args_t* p, const void* x, const uint8_t* c
     q.ld_out = stride(p->ld_y, p->N, p->M);
     q.out_f32 = p->type == FPQ_TYPE_FP32;
     q.bias = bias;
-    return launch_product(q, room.at, s);
+    return launch_product(q, plan, room.at, s);
 }
 
 size_t fpq_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K, int type)
 {
     if (!type_ok(type) || check_sizes(M, N, K) != FPQ_OK) return 0;
-    const int p = planes_of(type);
-    return planes_bytes(M, N, p) + planes_bytes(N, K, p) + larger(planes_bytes(M, K, p), blocks_bytes(M, K)) +
-           larger(gradient_parts(M, N, K, p, p), align_up(row_parts_bytes(M, N)));
+    return linear_backward_bytes(M, N, K, type, plans_of(M, N, K, planes_of(type), planes_of(type)));
 }
 
 int fpq_linear_backward(const fpq_linear_args_t* p, const void* x, const uint8_t* x_scales, const void* w, const void* grad_y, void* grad_x, void* grad_w,
@@ -273,18 +294,20 @@ int fpq_linear_backward(const fpq_linear_args_t* p, const void* x, const uint8_t
     if (!aligned(grad_y, size_of(p->type))) return FPQ_ERR_ALIGN;
     st = check_gradients(p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, grad_bias);
     if (st != FPQ_OK) return st;
-    if (workspace_bad(workspace, workspace_bytes, fpq_linear_backward_workspace_size(M, N, K, p->type), &st)) return st;
+    const int np = planes_of(p->type);
+    const GradientPlans plans = plans_of(M, N, K, np, np);
+    if (workspace_bad(workspace, workspace_bytes, linear_backward_bytes(M, N, K, p->type, plans), &st)) return st;
+    const GradientPlan& plan = x_scales ? plans.blocks : plans.values;
     hipStream_t s = static_cast<hipStream_t>(stream);
     Room room{static_cast<char*>(workspace)};
     // The bias's gradient comes with the weights' where their product gives both, else from a pass of its own.
-    const int np = planes_of(p->type);
-    const bool both = grad_bias && grad_w && ((grad_x && products_join(M, N, K, {np, np, x_scales ? 1 : np})) || product_sums(N, K, M, np, x_scales ? 1 : np));
+    const bool both = grad_bias && grad_w && ((grad_x && plan.tile >= 0) || plan_sums(plan, x_scales ? 1 : np));
     if (grad_bias && !both) st = launch_column_sums(grad_y, p->type, M, N, stride(p->ld_grad_y, N, M), grad_bias, reinterpret_cast<float*>(room.at), s);
     if (st != FPQ_OK || (!grad_x && !grad_w)) return st;
     PackList packs{};
     Operand d{};
     if (M) d = operand(grad_y, p->type, M, N, p->ld_grad_y, room, packs);
-    return gradients(d, np, p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, both ? grad_bias : nullptr, room, packs, s);
+    return gradients(d, np, p->type, M, N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, both ? grad_bias : nullptr, plan, room, packs, s);
 }
 
 static int check_gated(const fpq_gated_args_t* p)
@@ -294,14 +317,19 @@ static int check_gated(const fpq_gated_args_t* p)
     return check_sizes(p->M, 2 * (p->N < 0 ? 0 : p->N > kMostColumns ? kMostColumns : p->N), p->K);
 }
 
+static size_t gated_bytes(int64_t M, int64_t N, int64_t K, int type, const ProductPlan& plan)
+{
+    const int p = planes_of(type);
+    return planes_bytes(M, K, p) + planes_bytes(2 * N, K, p) + align_up(product_part_bytes(plan, M, N, false, true));
+}
+
 size_t fpq_gated_workspace_size(int64_t M, int64_t N, int64_t K, int type)
 {
     const fpq_gated_args_t a{type, 0, M, N, K, 0, 0, 0, 0, 0, 0};
     if (check_gated(&a) != FPQ_OK || M <= 16) return 0;
     // (nothing is kept there by the form of few rows; from 17 rows on, which form runs changes how large a workspace has to be, not whether there is one)
     if (few_rows(M, N, K, type)) return align_up(1);
-    const int p = planes_of(type);
-    return planes_bytes(M, K, p) + planes_bytes(2 * N, K, p) + align_up(product_part_bytes(M, N, K, p, p, false, true));
+    return gated_bytes(M, N, K, type, plan_product(M, N, K, planes_of(type), planes_of(type), false, true));
 }
 
 int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const float* bias, void* h, void* pre, uint8_t* pre_scales, void* workspace,
@@ -315,15 +343,17 @@ int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const flo
     if (!stride_ok(p->ld_x, K, M) || !stride_ok(p->ld_w, K, 2 * N) || !stride_ok(p->ld_h, N, M)) return FPQ_ERR_SHAPE;
     const size_t size = size_of(p->type);
     if (!aligned(x, size) || !aligned(w, size) || !aligned(h, size) || !aligned(pre, pre_scales ? 16 : size) || !aligned(bias, 4)) return FPQ_ERR_ALIGN;
-    if (workspace_bad(workspace, workspace_bytes, fpq_gated_workspace_size(M, N, K, p->type), &st)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (few_rows(M, N, K, p->type)) {
+        if (workspace_bad(workspace, workspace_bytes, fpq_gated_workspace_size(M, N, K, p->type), &st)) return st;
         RowsArgs r = rows_args(x, p->type, M, N, K, p->ld_x, bias);
         r.w = w;
         r.ld_w = p->ld_w;
         r.gate = Gate{p->act, h, stride(p->ld_h, N, M), pre, 2 * N, pre_scales};
         return launch_rows_gated(r, s);
     }
+    const ProductPlan plan = plan_product(M, N, K, planes_of(p->type), planes_of(p->type), false, true);
+    if (workspace_bad(workspace, workspace_bytes, gated_bytes(M, N, K, p->type, plan), &st)) return st;
     Room room{static_cast<char*>(workspace)};
     PackList packs{};
     Product q{};
@@ -339,16 +369,14 @@ int fpq_gated(const fpq_gated_args_t* p, const void* x, const void* w, const flo
     q.bias = bias;
     q.gated = true;
     q.gate = Gate{p->act, h, stride(p->ld_h, N, M), pre, 2 * N, pre_scales};
-    return launch_product(q, room.at, s);
+    return launch_product(q, plan, room.at, s);
 }
 
 size_t fpq_gated_backward_workspace_size(int64_t M, int64_t N, int64_t K, int type)
 {
     const fpq_gated_args_t a{type, 0, M, N, K, 0, 0, 0, 0, 0, 0};
     if (check_gated(&a) != FPQ_OK) return 0;
-    const int p = planes_of(type), pd = gate_planes(type);
-    return planes_bytes(M, 2 * N, pd) + planes_bytes(2 * N, K, p) + larger(planes_bytes(M, K, p), blocks_bytes(M, K)) +
-           larger(gradient_parts(M, 2 * N, K, pd, p), align_up(2 * row_parts_bytes(M, N)));
+    return gated_backward_bytes(M, N, K, type, plans_of(M, 2 * N, K, gate_planes(type), planes_of(type)));
 }
 
 int fpq_gated_backward(const fpq_gated_args_t* p, const void* x, const uint8_t* x_scales, const void* w, const void* pre, const uint8_t* pre_scales,
@@ -363,7 +391,8 @@ int fpq_gated_backward(const fpq_gated_args_t* p, const void* x, const uint8_t* 
     if (!aligned(grad_h, size) || !aligned(pre, pre_scales ? 16 : size)) return FPQ_ERR_ALIGN;
     st = check_gradients(p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, grad_bias);
     if (st != FPQ_OK) return st;
-    if (workspace_bad(workspace, workspace_bytes, fpq_gated_backward_workspace_size(M, N, K, p->type), &st)) return st;
+    const GradientPlans plans = plans_of(M, 2 * N, K, gate_planes(p->type), planes_of(p->type));
+    if (workspace_bad(workspace, workspace_bytes, gated_backward_bytes(M, N, K, p->type, plans), &st)) return st;
     if (!grad_x && !grad_w && !grad_bias) return FPQ_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
     Room room{static_cast<char*>(workspace)};
@@ -385,7 +414,8 @@ int fpq_gated_backward(const fpq_gated_args_t* p, const void* x, const uint8_t* 
     st = launch_gate_backward(g, s);
     if (st != FPQ_OK || !g.d) return st;
     PackList packs{};
-    return gradients(Operand{d, g.ld_d, g.plane}, gate_planes(p->type), p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, nullptr, room, packs, s);
+    return gradients(Operand{d, g.ld_d, g.plane}, gate_planes(p->type), p->type, M, 2 * N, K, x, x_scales, p->ld_x, w, p->ld_w, grad_x, p->ld_grad_x, grad_w, p->ld_grad_w, nullptr,
+                     x_scales ? plans.blocks : plans.values, room, packs, s);
 }
 
 int fpq_rms_norm(const fpq_norm_args_t* p, const void* x, const void* residual, const float* w, void* sum, void* y, float* rstd, uint8_t* codes, fpq_format_t f,

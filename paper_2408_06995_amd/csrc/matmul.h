@@ -672,23 +672,37 @@ struct Product {
     int64_t ld_out;
     int out_f32;
     const float* bias;
-    float* sums;                // of A over k (col_a; where product_sums allows it), or null
+    float* sums;                // of A over k (col_a; where plan_sums allows it), or null
     bool gated;
     Gate gate;
 };
-// Bytes of partial results of a product of these sizes (0 where it is made in one slice).
-size_t product_part_bytes(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated);
-// Whether a product of these sizes with A and B by columns can give the sums of A.
-bool product_sums(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b);
-int launch_product(const Product& p, void* part, hipStream_t s);
+// How a product is made: its tile (matmul_tiles.h), in how many slices of k, and an estimate of its time.  By sizes and planes alone, so that the same
+// plan gives the workspace's size and the launch.
+struct ProductPlan {
+    int tile, slices;
+    double us;
+};
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated);
+// Bytes of partial results (0 where it is made in one slice).
+size_t product_part_bytes(const ProductPlan& plan, int64_t M, int64_t N, bool col_a, bool gated);
+int launch_product(const Product& p, const ProductPlan& plan, void* part, hipStream_t s);
+
 // Planes of what both gradients of a layer are made from: d [M, N], w [N, K], x [M, K].
 struct Planes {
     int d, w, x;
 };
-// Both gradients of y = x w^T for d: x.M, N, K = M, K, N, by rows and by columns, w.M, N, K = N, K, M, both by columns.  In one launch where
-// products_join says so, else one after the other.
-bool products_join(int64_t M, int64_t N, int64_t K, Planes planes);
-size_t products_part_bytes(int64_t M, int64_t N, int64_t K, Planes planes);
-int launch_products(const Product& x, const Product& w, void* part, hipStream_t s);
+// Both gradients of y = x w^T for d: each on its own, and together in one launch where that is faster (tile >= 0).  A call makes this once: it takes the host
+// some microseconds.
+struct GradientPlan {
+    ProductPlan x, w;
+    int tile, slices_x, slices_w;
+};
+GradientPlan plan_gradients(int64_t M, int64_t N, int64_t K, Planes planes);
+// Bytes of partial results of whichever gradients are made.
+size_t gradient_part_bytes(const GradientPlan& plan, int64_t M, int64_t N, int64_t K);
+// Whether grad_w can give the sums of d in a launch of its own; together with grad_x it always can.
+bool plan_sums(const GradientPlan& plan, int planes_x);
+// x.M, N, K = M, K, N, by rows and by columns, w.M, N, K = N, K, M, both by columns.
+int launch_products(const Product& x, const Product& w, const GradientPlan& plan, void* part, hipStream_t s);
 
 }  // namespace fpq

@@ -6,11 +6,6 @@ namespace fpq {
 
 namespace {
 
-struct Plan {
-    int tile, slices;
-    double us;                  // estimate
-};
-
 // Passes of the planes: the largest products of two operands, small ones first.
 int passes(int planes_a, int planes_b) { return planes_a * planes_b == 9 ? 6 : planes_a * planes_b; }
 
@@ -41,34 +36,6 @@ bool takes_planes(int t) { return t == kPlanes256 || t == kPlanes128; }
 int next_slices(int s) { return s < 4 ? s + 1 : s + s / 4; }
 double sums_us(int s, int64_t M, int64_t N, bool gated) { return s > 1 ? (double)s * M * N * (gated ? 2 : 1) * 8 / 4.5e6 : 0.0; }
 
-Plan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated)
-{
-    const double steps = steps_of(K, planes_a, planes_b);
-    if (!col_a && M <= 32) {
-        // bound by B's bytes: parts of no fewer than eight steps until two workgroups per compute unit have work
-        const int64_t n = tiles_of(kTile32, M, N, gated);
-        int64_t most = (int64_t)(steps / 8 < 16 ? steps / 8 : 16), slices = 512 / n < most ? 512 / n : most;
-        if (slices < 1) slices = 1;
-        const double rounds = (double)(n * slices) / 512;
-        return Plan{kTile32, (int)slices, (rounds > 1 ? rounds : 1) * 0.3 * (steps / slices + 5) + (slices > 1 ? kLaunch : 0)};
-    }
-    Plan best{kTile128, 1, 1e30};
-    for (Kind k : kKinds) {
-        if (k.tile == kTile192 && col_a) continue;
-        if (takes_planes(k.tile) && planes_a * planes_b != 9) continue;
-        if (k.tile == kTile64 && gated) k = kGated64;
-        for (int s = 1; s <= 32; s = next_slices(s)) {
-            if (s > 1 && steps / s < 8) break;
-            const int64_t n = tiles_of(k.tile, M, N, gated) * s, rest = n % k.at_once;
-            const double part = k.full * rest / k.at_once;
-            double us = ((double)(n / k.at_once) * k.full + (rest ? (part > k.alone ? part : k.alone) : 0.0)) * (steps / s + k.ends);
-            if (s > 1) us += kLaunch + sums_us(s, M, N, gated);
-            if (us < best.us) best = Plan{k.tile, s, us};
-        }
-    }
-    return best;
-}
-
 // Workgroups of two lengths (in steps), the long ones first, each where there is room next.  As many as run at once: the short ones share their
 // compute units until they end.  More: steps take `full` as long as all units are busy, then `alone`.
 double both_us(const Kind& k, int64_t na, double a, int64_t nb, double b)
@@ -89,39 +56,6 @@ double both_us(const Kind& k, int64_t na, double a, int64_t nb, double b)
         end = el < eh || !more ? el : eh;
     }
     return busy * k.full + (end - busy) * k.alone;
-}
-
-// Both gradients in one launch: their workgroups fill the chip together where neither does alone, and there is a launch less, or two.  (Linear layers in
-// bf16 with the blocks made, one after the other and together: 300 x 320 -> 960 18.2 and 14.8 us, 2048 x 1280 -> 1280 38.2 and 33.9, 8192 x 640 -> 640 41.6 and 33.8, 32768 x
-// 320 -> 960 98 and 82; gated ones with the forward call 999 x 333 -> 1283 in fp32 98.7 and 87.5, 532 x 2230 -> 8939 in bf16 293 and 273.)
-struct PlanBoth {
-    int tile, slices_x, slices_w;               // tile < 0: one after the other
-};
-PlanBoth plan_both(int64_t M, int64_t N, int64_t K, Planes p)
-{
-    PlanBoth best{-1, 1, 1};
-    if (M == 0) return best;
-    const double steps_x = steps_of(N, p.d, p.w), steps_w = steps_of(M, p.d, p.x);
-    const Plan x = plan_product(M, K, N, p.d, p.w, false, false), w = plan_product(N, K, M, p.d, p.x, true, false);
-    double least = (x.us + w.us + kLaunch);
-    for (const Kind& k : kKinds) {
-        if (k.tile != kTile64 && k.tile != kTile128 && k.tile != kTile128Deep && k.tile != kPlanes128) continue;
-        if (takes_planes(k.tile) != (p.d * p.x == 9)) continue;
-        const int64_t tx = tiles_of(k.tile, M, K, false), tw = tiles_of(k.tile, N, K, false), most = 3 * k.at_once;      // (more parts gain nothing)
-        for (int a = 1; a <= 32; a = next_slices(a)) {
-            if (a > 1 && (steps_x / a < 8 || tx * a > most)) break;
-            for (int b = 1; b <= 32; b = next_slices(b)) {
-                if (b > 1 && (steps_w / b < 8 || tx * a + tw * b > most)) break;
-                double us = both_us(k, tx * a, steps_x / a + k.ends, tw * b, steps_w / b + k.ends);
-                if (a > 1 || b > 1) us += kLaunch + sums_us(a, M, K, false) + sums_us(b, N, K, false);
-                if (us < least) {
-                    least = us;
-                    best = PlanBoth{k.tile, a, b};
-                }
-            }
-        }
-    }
-    return best;
 }
 
 struct SumArgs {
@@ -297,26 +231,85 @@ int launched() { return hipGetLastError() == hipSuccess ? FPQ_OK : FPQ_ERR_LAUNC
 
 }  // namespace
 
-size_t product_part_bytes(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated)
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool col_a, bool gated)
 {
-    if (M == 0 || N == 0) return 0;
-    const Plan p = plan_product(M, N, K, planes_a, planes_b, col_a, gated);
-    return part_bytes(p.slices, M, N, col_a, gated);
+    const double steps = steps_of(K, planes_a, planes_b);
+    if (!col_a && M <= 32) {
+        // bound by B's bytes: parts of no fewer than eight steps until two workgroups per compute unit have work
+        const int64_t n = tiles_of(kTile32, M, N, gated);
+        int64_t most = (int64_t)(steps / 8 < 16 ? steps / 8 : 16), slices = 512 / n < most ? 512 / n : most;
+        if (slices < 1) slices = 1;
+        const double rounds = (double)(n * slices) / 512;
+        return ProductPlan{kTile32, (int)slices, (rounds > 1 ? rounds : 1) * 0.3 * (steps / slices + 5) + (slices > 1 ? kLaunch : 0)};
+    }
+    ProductPlan best{kTile128, 1, 1e30};
+    for (Kind k : kKinds) {
+        if (k.tile == kTile192 && col_a) continue;
+        if (takes_planes(k.tile) && planes_a * planes_b != 9) continue;
+        if (k.tile == kTile64 && gated) k = kGated64;
+        for (int s = 1; s <= 32; s = next_slices(s)) {
+            if (s > 1 && steps / s < 8) break;
+            const int64_t n = tiles_of(k.tile, M, N, gated) * s, rest = n % k.at_once;
+            const double part = k.full * rest / k.at_once;
+            double us = ((double)(n / k.at_once) * k.full + (rest ? (part > k.alone ? part : k.alone) : 0.0)) * (steps / s + k.ends);
+            if (s > 1) us += kLaunch + sums_us(s, M, N, gated);
+            if (us < best.us) best = ProductPlan{k.tile, s, us};
+        }
+    }
+    return best;
+}
+
+// Both gradients in one launch: their workgroups fill the chip together where neither does alone, and there is a launch less, or two.  (Linear layers in
+// bf16 with the blocks made, one after the other and together: 300 x 320 -> 960 18.2 and 14.8 us, 2048 x 1280 -> 1280 38.2 and 33.9, 8192 x 640 -> 640 41.6 and 33.8, 32768 x
+// 320 -> 960 98 and 82; gated ones with the forward call 999 x 333 -> 1283 in fp32 98.7 and 87.5, 532 x 2230 -> 8939 in bf16 293 and 273.)
+GradientPlan plan_gradients(int64_t M, int64_t N, int64_t K, Planes p)
+{
+    GradientPlan best{M ? plan_product(M, K, N, p.d, p.w, false, false) : ProductPlan{}, plan_product(N, K, M, p.d, p.x, true, false), -1, 1, 1};
+    if (M == 0) return best;
+    const double steps_x = steps_of(N, p.d, p.w), steps_w = steps_of(M, p.d, p.x);
+    double least = (best.x.us + best.w.us + kLaunch);
+    for (const Kind& k : kKinds) {
+        if (k.tile != kTile64 && k.tile != kTile128 && k.tile != kTile128Deep && k.tile != kPlanes128) continue;
+        if (takes_planes(k.tile) != (p.d * p.x == 9)) continue;
+        const int64_t tx = tiles_of(k.tile, M, K, false), tw = tiles_of(k.tile, N, K, false), most = 3 * k.at_once;      // (more parts gain nothing)
+        for (int a = 1; a <= 32; a = next_slices(a)) {
+            if (a > 1 && (steps_x / a < 8 || tx * a > most)) break;
+            for (int b = 1; b <= 32; b = next_slices(b)) {
+                if (b > 1 && (steps_w / b < 8 || tx * a + tw * b > most)) break;
+                double us = both_us(k, tx * a, steps_x / a + k.ends, tw * b, steps_w / b + k.ends);
+                if (a > 1 || b > 1) us += kLaunch + sums_us(a, M, K, false) + sums_us(b, N, K, false);
+                if (us < least) {
+                    least = us;
+                    best.tile = k.tile, best.slices_x = a, best.slices_w = b;
+                }
+            }
+        }
+    }
+    return best;
+}
+
+size_t product_part_bytes(const ProductPlan& plan, int64_t M, int64_t N, bool col_a, bool gated) { return part_bytes(plan.slices, M, N, col_a, gated); }
+
+size_t gradient_part_bytes(const GradientPlan& plan, int64_t M, int64_t N, int64_t K)
+{
+    const size_t x = part_bytes(plan.x.slices, M, K, false, false), w = part_bytes(plan.w.slices, N, K, true, false);
+    const size_t both = plan.tile < 0 ? 0 : part_bytes(plan.slices_x, M, K, false, false) + part_bytes(plan.slices_w, N, K, true, false);
+    const size_t one = x > w ? x : w;
+    return one > both ? one : both;
 }
 
 // Several passes over k read a plane of A more than once, unless there is but one plane of B or a tile takes all in one pass.  And the wavefronts that
 // make the sums are slower: in tiles of 256 x 256, of which large products are one round, that is more than a pass for the sums (8192 x 4096 -> 4096
 // with both gradients: 500 us, 481 with a pass); elsewhere it is less (5003 x 5120 -> 1280: 176 for 178, 32768 x 320 -> 960 99 for 107, 300 x 320 -> 960 18 for 25).
-bool product_sums(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b)
+bool plan_sums(const GradientPlan& plan, int planes_x)
 {
-    const int tile = plan_product(M, N, K, planes_a, planes_b, true, false).tile;
-    return tile != kTile256 && (planes_b == 1 || tile == kPlanes256 || tile == kPlanes128);
+    const int tile = plan.w.tile;
+    return tile != kTile256 && (planes_x == 1 || tile == kPlanes256 || tile == kPlanes128);
 }
 
-int launch_product(const Product& q, void* part, hipStream_t s)
+int launch_product(const Product& q, const ProductPlan& plan, void* part, hipStream_t s)
 {
     if (q.M == 0 || q.N == 0) return FPQ_OK;
-    const Plan plan = plan_product(q.M, q.N, q.K, q.planes_a, q.planes_b, q.col_a, q.gated);
     const MatmulArgs p = args_of(q, plan.tile, plan.slices, part);
     const int st = q.gated ? launch_matmul_gated(p, plan.tile, s)
                    : q.col_a ? (q.sums ? launch_matmul_cols_sums(p, plan.tile, s) : launch_matmul_cols(p, plan.tile, s))
@@ -329,20 +322,11 @@ int launch_product(const Product& q, void* part, hipStream_t s)
     return launched();
 }
 
-bool products_join(int64_t M, int64_t N, int64_t K, Planes planes) { return plan_both(M, N, K, planes).tile >= 0; }
-
-size_t products_part_bytes(int64_t M, int64_t N, int64_t K, Planes planes)
+int launch_products(const Product& x, const Product& w, const GradientPlan& plan, void* part, hipStream_t s)
 {
-    const PlanBoth p = plan_both(M, N, K, planes);
-    return p.tile < 0 ? 0 : part_bytes(p.slices_x, M, K, false, false) + part_bytes(p.slices_w, N, K, true, false);
-}
-
-int launch_products(const Product& x, const Product& w, void* part, hipStream_t s)
-{
-    const PlanBoth plan = plan_both(x.M, w.M, x.N, Planes{x.planes_a, x.planes_b, w.planes_b});
     if (plan.tile < 0) {
-        const int st = launch_product(x, part, s);
-        return st == FPQ_OK ? launch_product(w, part, s) : st;
+        const int st = launch_product(x, plan.x, part, s);
+        return st == FPQ_OK ? launch_product(w, plan.w, part, s) : st;
     }
     char* const part_w = static_cast<char*>(part) + part_bytes(plan.slices_x, x.M, x.N, false, false);
     const MatmulArgs ax = args_of(x, plan.tile, plan.slices_x, part), aw = args_of(w, plan.tile, plan.slices_w, part_w);

@@ -1,4 +1,4 @@
-"""Workspaces of gated calls of few rows: none for tokens, and no room for packed weights where they are read in place."""
+"""Workspaces of gated calls of few rows, none for tokens and no room for packed weights where they are read in place; and of calls without rows."""
 import pytest
 import torch
 
@@ -16,6 +16,14 @@ def test_sizes_of_few_rows():
         assert size(65, N, K, 0) >= 65 * K * 6 + 2 * N * K * 6
     # bf16 above 16 rows: weights of more than 32 MB run in tiles, where odd rows of them are packed
     assert 0 < size(17, 1280, 5120, 1) <= 256 and size(17, 10240, 4097, 1) > 2 * 10240 * 4097 * 2
+
+
+def test_sizes_without_rows():
+    """Sums over no rows are zeros: the gradients have a workspace, the others none."""
+    L = B.lib()
+    for t in (0, 1):
+        assert L.fpq_linear_backward_workspace_size(0, 48, 40, t) > 0 and L.fpq_gated_backward_workspace_size(0, 48, 40, t) > 0
+        assert L.fpq_block_linear_workspace_size(0, 48, 40, t) == 0 and L.fpq_gated_workspace_size(0, 48, 40, t) == 0
 
 
 @pytest.mark.gpu
