@@ -596,7 +596,7 @@ int fpq_adamw_step(const void *plan, int64_t pieces, double lr, double beta1, do
  * fpq_linear_backward: the gradients of a linear layer y = x W^T (+ bias) for grad_y [M, N]: grad_x [M, K] = grad_y W, grad_w [N, K] =
  *   grad_y^T x, of args->type, grad_bias fp32 [N] the sum of its rows.  Each of them may be NULL and is then not computed (which are asked
  *   for may change the order of the others' sums); w is needed for grad_x, x for grad_w.  x is [M, K] of the type with stride ld_x, or, with x_scales not NULL, the E4M3 blocks that were kept of it.
- * Infinities and NaN make what depends on them infinite or NaN, in FPQ_TYPE_FP32 always NaN.  No atomics: the same bits in every run.  Rows of
+ * Infinities and NaN, and fp32 magnitudes that bf16 rounds to 2^128, make what depends on them infinite or NaN.  No atomics: the same bits in every run.  Rows of
  * multiples of 16 bytes that start at one are read where they are; others, and fp32, are packed into the workspace first.
  * workspace: the stated bytes, 16-byte aligned, no initialisation (NULL when that is 0); calls that share one are ordered on one stream.
  * Limits: M at most 2^28, N, K and strides at most 2^20, M N, M K and N K below 2^34 (FPQ_ERR_SHAPE). */

@@ -1,4 +1,4 @@
-"""Operators around the projections at values far out: NaN where codes are made, products near the ends of the range."""
+"""Operators around the projections at values far out: NaN where codes are made, products near the ends of the range, infinities."""
 import numpy as np
 import pytest
 import torch
@@ -48,3 +48,34 @@ def test_layers_whose_products_are_in_range(x_exp, w_exp, M, t):
     y = nan(M, N, t=TYPES[t])
     B.fpq_block_linear(x, codes, scales, None, y, room(B.fpq_block_linear_workspace_size(M, N, K, int(t == "bf16"))))
     within("y", y, *blocks.block_linear(host(x), wv, None, t == "bf16"))
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M", [2, 4, 5, 16, 40, 70])
+def test_infinities_stay_in_their_rows(M, t):
+    """A row of x with an infinity or NaN has no finite result and no other row is touched; grad_bias, grad_x and grad_w of such a row the same."""
+    print(M, t, flush=True)
+    N, K = 48, 96
+    g = torch.Generator().manual_seed(M)
+    codes, scales = quantize(rows(g, N, K, torch.float32).clamp(min=0.1), E2M1)              # (no zeros among them)
+    x, gy, w = rows(g, M, K, TYPES[t]), rows(g, M, N, TYPES[t]), rows(g, N, K, TYPES[t])
+    ty = int(t == "bf16")
+    for bad in (float("inf"), -float("inf"), float("nan")):
+        a, b = x.clone(), gy.clone()
+        a[1, 37], b[1, 11] = bad, bad
+        y = nan(M, N, t=TYPES[t])
+        B.fpq_block_linear(a, codes, scales, None, y, room(B.fpq_block_linear_workspace_size(M, N, K, ty)))
+        finite = y.isfinite().all(1).cpu()
+        assert not y[1].isfinite().any() and finite.sum() == M - 1
+        gx, gw, gb = nan(M, K, t=TYPES[t]), nan(N, K, t=TYPES[t]), nan(N)
+        for out in ((gx, gw, gb), (None, None, gb), (gx, None, None), (None, gw, gb)):
+            for o in out:
+                if o is not None:
+                    o.zero_()
+            B.fpq_linear_backward(x, None, w, b, *out, room(B.fpq_linear_backward_workspace_size(M, N, K, ty)))
+            if out[0] is not None:
+                assert not gx[1].isfinite().any() and gx.isfinite().all(1).sum() == M - 1
+            if out[1] is not None:
+                assert not gw[11].isfinite().any() and gw.isfinite().all(1).sum() == N - 1
+            if out[2] is not None:
+                assert not gb[11].isfinite() and gb.isfinite().sum() == N - 1
