@@ -2,7 +2,7 @@
 // the gated projections' gradient before the products.  All are bound by memory: a lane takes eight neighbouring elements, 16 bytes or
 // twice as many at any address, and two such pieces, so that there are enough loads on their way.  Read and written together: planes of 10240 x 4096 in fp32 6.3
 // TB/s (66 us), blocks back to bf16 6.1 (5003 x 5120: 12.8 us), to blocks 4.7 (16.5 us), the gated gradient of 8192 x 5120 from
-// blocks 5.2 (66 us), column sums of 32768 x 960 in bf16 4.5 (13.9 us).
+// blocks 5.6 (90 us), column sums of 32768 x 960 in bf16 4.5 (13.9 us).
 #include "blocks.h"
 
 namespace fpq {
@@ -361,8 +361,8 @@ int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t
     return launched();
 }
 
-// About 1024 workgroups, of no fewer than four rows (300 x 320 -> 1280 with its gradient in bf16: 25.6 us,
-// 26.7 with eight), and no more parts than their sum is
+// About 1024 workgroups, of no fewer than four rows (300 x 320 -> 1280 with its gradient in bf16: 30.7 us,
+// 31.4 with eight), and no more parts than their sum is
 // quick with.
 RowParts row_parts(int64_t M, int64_t cols)
 {

@@ -14,8 +14,8 @@
 // product of 16 k ahead, across the barrier too, so that the matrix unit has work while the workgroup meets.
 //
 // Large products are bound by the matrix unit and the power it may draw (a loop of nothing but its instructions reaches 1.85 PFLOP/s): 4096 x 4096 x 4096 in bf16
-// with either operand by columns 108 us, 1.27 PFLOP/s; the gated forward of 8192 x 1280 -> 2 x 5120 with blocks kept 235 us, 0.91, of which
-// some 40 are the ends of its five rounds; in fp32 2048 x 1280 -> 2 x 5120 300 us, 1.07 in bf16 products.  Smaller ones wait for their first loads and are
+// with either operand by columns 108 us, 1.27 PFLOP/s; the gated forward of 8192 x 1280 -> 2 x 5120 with blocks kept 222 us on its own, 0.97, and
+// 241 to 261 among a training step's kernels, of which some 40 are the ends of its five rounds; in fp32 2048 x 1280 -> 2 x 5120 300 us, 1.07 in bf16 products.  Smaller ones wait for their first loads and are
 // quantized by tiles (the choice is made in matmul.hip).
 #pragma once
 #include "attention.h"

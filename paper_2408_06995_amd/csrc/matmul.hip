@@ -261,7 +261,8 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int planes_a, int plan
 
 // Both gradients in one launch: their workgroups fill the chip together where neither does alone, and there is a launch less, or two.  (Linear layers in
 // bf16 with the blocks made, one after the other and together: 300 x 320 -> 960 18.2 and 14.8 us, 2048 x 1280 -> 1280 38.2 and 33.9, 8192 x 640 -> 640 41.6 and 33.8, 32768 x
-// 320 -> 960 98 and 82; gated ones with the forward call 999 x 333 -> 1283 in fp32 98.7 and 87.5, 532 x 2230 -> 8939 in bf16 293 and 273.)
+// 320 -> 960 98 and 82; gated ones in bf16 without the bias's, 300 x 320 -> 1280 22.6 and 18.2, 2048 x 1280 -> 1280 85 and 72, 2928 x 64 -> 799 36 and 28; with the forward call 999 x
+// 333 -> 1283 in fp32 98.7 and 87.5.)
 GradientPlan plan_gradients(int64_t M, int64_t N, int64_t K, Planes p)
 {
     GradientPlan best{M ? plan_product(M, K, N, p.d, p.w, false, false) : ProductPlan{}, plan_product(N, K, M, p.d, p.x, true, false), -1, 1, 1};
