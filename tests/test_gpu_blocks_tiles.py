@@ -1,5 +1,5 @@
 """Products of the operators around the projections in the tiles that no other test runs: layers on 4-bit blocks in large tiles and in slices, gated
-projections of 17 to 64 rows on weights that the L2 does not hold, gradients of few rows, norms of odd widths.  Of large results rows at the ends and at
+projections of 17 to 64 rows on weights that the L2 does not hold, gradients of few rows, norms of odd widths and large ones in place.  Of large results rows at the ends and at
 random, in full length."""
 import numpy as np
 import pytest
@@ -92,3 +92,32 @@ def test_few_rows_of_many_columns(M, N, K, t):
 def test_norm_of_odd_widths(M, K, t):
     print(M, K, t, flush=True)
     test_gpu_norm.check(M, K, t)
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,K", [(3000, 12000), (3001, 11999), (6000, 5120), (40000, 320)])
+def test_large_norms_in_place(M, K, t):
+    """Results that the L2 does not hold, over what they came from: rows in registers and rows read twice."""
+    print(M, K, t, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(K)
+    x, res, gy, gs = (torch.randn(M, K, generator=g, device=DEV).to(TYPES[t]) for _ in range(4))
+    w = 1 + 0.3 * torch.randn(K, generator=g, device=DEV)
+    total, y, rstd = nan(M, K, t=TYPES[t]), nan(M, K, t=TYPES[t]), nan(M)
+    B.fpq_rms_norm(x, res, w, 1e-6, total, y, rstd)
+    assert torch.equal(total, (x.float() + res.float()).to(TYPES[t]))
+    ms = some(M, K, 20)
+    wy, oy, _, _ = blocks.rms_norm(host(total[ms]), host(w), 1e-6)
+    within("y", y[ms], wy, oy + blocks.rounding(t == "bf16") * (np.abs(wy) + oy))
+    for i in range(2):
+        two, again = [x.clone(), res.clone()], nan(M, K, t=TYPES[t])
+        B.fpq_rms_norm(*two, w, 1e-6, two[i], again)
+        assert torch.equal(two[i], total) and torch.equal(again, y)
+    ws = test_gpu_blocks.room(B.fpq_rms_norm_backward_workspace_size(M, K))
+    gx, gw = nan(M, K, t=TYPES[t]), nan(K)
+    B.fpq_rms_norm_backward(total, w, rstd, gy, gs, gx, gw, ws)
+    wx, ox, _, _ = blocks.rms_norm_backward(host(total[ms]), host(w), host(rstd[ms]), host(gy[ms]), host(gs[ms]))
+    within("grad_x", gx[ms], wx, ox + blocks.rounding(t == "bf16") * (np.abs(wx) + ox))
+    for i in range(2):
+        two, again = [gy.clone(), gs.clone()], nan(K)
+        B.fpq_rms_norm_backward(total, w, rstd, *two, two[i], again, ws)
+        assert torch.equal(two[i], gx) and torch.equal(again, gw)
