@@ -363,11 +363,13 @@ int launch_block_quantize(const void* x, int type, int64_t M, int64_t K, int64_t
 
 // About 1024 workgroups, of no fewer than four rows (300 x 320 -> 1280 with its gradient in bf16: 30.7 us,
 // 31.4 with eight), and no more parts than their sum is
-// quick with.
+// quick with; but parts of no more than some 8192 rows, 2048 a lane, so that no sum's roundings grow with the number of rows (2^26 rows of ones and tenths: off by
+// 3e-4 with 512 parts).
 RowParts row_parts(int64_t M, int64_t cols)
 {
     const int64_t strips = (cols + kStripColumns - 1) / kStripColumns;
     int64_t parts = 1024 / strips < 512 ? 1024 / strips : 512, most = (M + 3) / 4;
+    if (parts < M / 8192) parts = M / 8192;
     parts = parts < 1 ? 1 : parts > most ? most : parts;
     if (parts < 1) parts = 1;
     const int64_t rows = (M + parts - 1) / parts;

@@ -390,10 +390,10 @@ Shape shape_of(int64_t M, int64_t span, int piece, bool vec, bool back)
     return !vec ? first(kPlainShapes) : M * pieces < 65536 ? first(kFewShapes) : back ? first(kBackwardShapes) : first(kShapes);
 }
 
-// Workgroups of the backward kernel, each of which leaves a row of partial sums.
+// Workgroups of the backward kernel, each of which leaves a row of partial sums: of no more than some 2048 rows a thread, as in row_parts.
 int64_t backward_blocks(int64_t M, Shape s)
 {
-    const int64_t rows = 256 / s.tpr, all = (M + rows - 1) / rows, most = 512;
+    const int64_t rows = 256 / s.tpr, all = (M + rows - 1) / rows, most = all / 2048 > 512 ? all / 2048 : 512;
     return all < most ? all : most;
 }
 
